@@ -340,6 +340,152 @@ ultramem_status ultramem_shard_pool(ultramem_layer *layer, const int64_t *idx, c
                                     int32_t n, const int32_t *slot_pos, const void *back_rows,
                                     void *out, void *stream);
 
+/* ---- the decoder block around the layer ------------------------------------
+ * A decoder block puts the layer next to attention and norms.  The calls below
+ * serve that: a paged cache of keys and values with the attention that reads
+ * it, and the norms before and after a block fused with its gate and residual
+ * scale, with their gradient.  They take no layer handle and keep nothing
+ * between calls; scratch is a workspace that the caller passes.  All pointers
+ * are DEVICE; every call is asynchronous on `stream`, never waits for the
+ * GPU, and may be captured in a CUDA graph.
+ *
+ * The cache holds pages of page_size tokens for all key/value heads.  A slot
+ * is page * page_size + the token's place in the page; a request's block table
+ * row lists its pages in order.  Lengths stay on the device. */
+typedef struct ultramem_kv_cache {
+    void *k, *v;         /* [n_pages][kv_heads][page_size][head_dim], 16-byte aligned        */
+    int32_t n_pages;     /* n_pages * page_size and n_pages * kv_heads < 2^31                */
+    int32_t kv_heads;    /* 1..1024                                                          */
+    int32_t page_size;   /* tokens a page: 16, 32, 64, 128 or 256                            */
+    int32_t head_dim;    /* a multiple of 8, up to 256                                       */
+    int32_t dtype;       /* ULTRAMEM_F32 or ULTRAMEM_BF16, also of q, new k and v, and out   */
+} ultramem_kv_cache;
+
+/* Pages and slots for a step's new tokens.  Request r of n_seqs has
+ * ctx_lens[r] cached tokens and brings new_lens[r] (negative counts as 0).
+ *   block_table [n_seqs][table_width]: row r's first ceil(ctx/page_size)
+ *           entries are read, the entries of new pages are written;
+ *   free_pages, free_count [1]: the free list; new pages are taken from its
+ *           end, request by request (page k of the call's new ones is
+ *           free_pages[free_count - 1 - k]);
+ *   q_start [n_seqs + 1]: first token of each request in the packed batch
+ *           (exclusive sum of new_lens);
+ *   slots   [n_tokens]: the slot of each token, -1 for those of refused
+ *           requests and past the batch;
+ *   kv_lens [n_seqs]: ctx + new; 0 for a refused request, whose rows then
+ *           attend to nothing;
+ *   free_left [1]: the free list's length after the call;
+ *   balance [1]: free_count less the pages asked for up to the last request
+ *           that was served: free_left when none was refused before it, and
+ *           below zero the number of pages that the step was short of.
+ * A request is refused, and its table row left alone, when its pages and
+ * those that it and earlier requests need exceed the free list, its row is
+ * too narrow, or its tokens reach past n_tokens.  Outputs must not overlap
+ * inputs (except the table, updated in place).  Repeating the call with the
+ * same inputs gives the same result.  ULTRAMEM_EINVAL for a page size that a
+ * cache cannot have, negative sizes or null pointers. */
+ultramem_status ultramem_paged_plan(const int32_t *ctx_lens, const int32_t *new_lens,
+                                    int32_t n_seqs, int32_t page_size, int32_t *block_table,
+                                    int32_t table_width, const int32_t *free_pages,
+                                    const int32_t *free_count, int32_t n_tokens, int32_t *q_start,
+                                    int32_t *kv_lens, int32_t *slots, int32_t *free_left,
+                                    int32_t *balance, void *stream);
+
+/* The new tokens' keys and values k, v [n_tokens][kv_heads][head_dim] (rows of
+ * tokens k_stride and v_stride elements apart) into their slots.  Slots
+ * outside the cache (-1) are skipped; two tokens must not share a slot. */
+ultramem_status ultramem_paged_append(const ultramem_kv_cache *cache, const void *k,
+                                      int64_t k_stride, const void *v, int64_t v_stride,
+                                      const int32_t *slots, int32_t n_tokens, void *stream);
+
+/* Attention of each request's new tokens over its pages, causal: row i of the
+ * n_r new tokens of request r (packed: q_start [n_seqs + 1]) has position
+ * p = kv_lens[r] - n_r + i and sees the keys 0..p (the new tokens' keys are
+ * appended first; single-token decode is n_r = 1).
+ *   s_j = scale q . k_j,  out = sum_j softmax(s)_j v_j,  lse = log sum_j e^(s_j)
+ * q [n_tokens][q_heads][head_dim] with tokens q_stride elements apart; head h
+ * reads key/value head h / (q_heads / kv_heads) (q_heads a multiple of
+ * kv_heads, at most 64 to one); out [n_tokens][q_heads][head_dim] contiguous;
+ * lse fp32 [n_tokens][q_heads] or NULL.  A row that sees no key gets out = 0
+ * and lse = -inf.  kv_lens is capped at what the table's row can hold; a table
+ * entry outside the cache reads as zeros.  Cache entries past a request's
+ * length are never used, whatever they hold.  Keys and values that only
+ * later rows of the same request see may meet a row with weight 0: a
+ * non-finite value there may make the row NaN.  Scores, sums and outputs
+ * accumulate in fp32; with bf16 storage the weights enter the second product
+ * as bf16.
+ * max_new: an upper bound of n_r known on the host; it chooses the kernel and
+ * the workspace (a larger n_r is still computed right).  Rows of out that
+ * belong to no request are not written.  workspace: 16-byte aligned, at least
+ * ultramem_paged_attention_workspace bytes, not shared by calls that overlap.
+ * ULTRAMEM_EINVAL for invalid sizes, types or null pointers and a scale that
+ * is not positive and finite. */
+ultramem_status ultramem_paged_attention(const ultramem_kv_cache *cache, const void *q,
+                                         int64_t q_stride, int32_t q_heads,
+                                         const int32_t *q_start, const int32_t *kv_lens,
+                                         const int32_t *block_table, int32_t table_width,
+                                         int32_t n_seqs, int32_t n_tokens, int32_t max_new,
+                                         float scale, void *out, float *lse, void *workspace,
+                                         int64_t workspace_bytes, void *stream);
+/* Bytes of workspace for such calls (0 for arguments that the call refuses). */
+int64_t ultramem_paged_attention_workspace(int32_t dtype, int32_t q_heads, int32_t kv_heads,
+                                           int32_t head_dim, int32_t max_new);
+
+enum { ULTRAMEM_NORM_RMS = 0, ULTRAMEM_NORM_LAYER = 1 };
+enum {
+    ULTRAMEM_GATE_NONE = 0,
+    ULTRAMEM_GATE_CHANNEL = 1,   /* fp32 [dim], one factor a channel            */
+    ULTRAMEM_GATE_TOKEN = 2,     /* dtype [n_tokens], one factor a token        */
+    ULTRAMEM_GATE_FULL = 3       /* dtype [n_tokens][dim]                       */
+};
+
+/* The norms after one block and before the next, with the block's gate and
+ * the residual scale between them:
+ *   z = N_post(y),  u = res_scale r + out_scale gate (.) z,  n = N_pre(u)
+ * N(x) = x / sqrt(mean x^2 + eps) (.) w                      (ULTRAMEM_NORM_RMS)
+ * N(x) = (x - mean x) / sqrt(var x + eps) (.) w + b           (ULTRAMEM_NORM_LAYER,
+ *        the population variance)
+ * y [n_tokens][dim] is the block's output, r the residual stream before it.
+ * Statistics and sums are fp32.  N_pre reads u as stored, so the gradient
+ * below, taken from the stored u, is the gradient of this function. */
+typedef struct ultramem_block_norm_args {
+    const void *y;          /* [n_tokens][dim] dtype, rows ld_y elements apart           */
+    const void *gate;       /* by gate_mode, contiguous; NULL with ULTRAMEM_GATE_NONE    */
+    const float *w_post, *b_post;   /* [dim] fp32; a NULL gain is 1, a NULL bias 0       */
+    const float *w_pre, *b_pre;     /* biases only with ULTRAMEM_NORM_LAYER              */
+    int64_t ld_y, ld_r;     /* elements between rows of y and of r (u in the backward)   */
+    int32_t n_tokens;       /* 0 launches nothing                                        */
+    int32_t dim;            /* 1..8192                                                   */
+    int32_t dtype;          /* ULTRAMEM_F32 or ULTRAMEM_BF16                             */
+    int32_t kind;           /* ULTRAMEM_NORM_*                                           */
+    int32_t post, pre;      /* 1: the norm is there; 0: z = y, no n                      */
+    int32_t gate_mode;      /* ULTRAMEM_GATE_*                                           */
+    float res_scale, out_scale, eps;   /* finite; eps >= 0                               */
+} ultramem_block_norm_args;
+
+/* u [n_tokens][dim] and, with pre, n [n_tokens][dim] (else NULL), contiguous.
+ * u may be r itself (contiguous), and n may be y. */
+ultramem_status ultramem_block_norm(const ultramem_block_norm_args *args, const void *r, void *u,
+                                    void *n, void *stream);
+
+/* The gradient at the y and u of a forward (u as it was stored; args->ld_r is
+ * its row distance).  du, dn: gradients of u (NULL: zero; rows ld_du apart)
+ * and n (with pre; rows ld_dn apart).  Outputs, each NULL to skip:
+ *   dy, dr [n_tokens][dim] dtype, contiguous; dy may be du or dn, and dr may
+ *           be the other, when those are contiguous;
+ *   dgate   fp32 [dim] for a channel gate, dtype [n_tokens] for a token gate,
+ *           dtype [n_tokens][dim] for a full one;
+ *   dw_post, db_post, dw_pre, db_pre  fp32 [dim] (written, not accumulated).
+ * The sums over tokens are added in a fixed order.  workspace: 16-byte
+ * aligned, at least ultramem_block_norm_backward_workspace bytes. */
+ultramem_status ultramem_block_norm_backward(const ultramem_block_norm_args *args, const void *u,
+                                             const void *du, int64_t ld_du, const void *dn,
+                                             int64_t ld_dn, void *dy, void *dr, void *dgate,
+                                             float *dw_post, float *db_post, float *dw_pre,
+                                             float *db_pre, void *workspace,
+                                             int64_t workspace_bytes, void *stream);
+int64_t ultramem_block_norm_backward_workspace(int64_t n_tokens, int32_t dim);
+
 /* Failure-path hooks for tests; they inject failures on the host or behind
  * a bounded wait, never a device fault.
  *

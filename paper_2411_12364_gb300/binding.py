@@ -30,7 +30,10 @@ EXPORTS = ("ultramem_create", "ultramem_destroy", "ultramem_forward",
            "ultramem_retrieve_exact", "ultramem_lookup_reduce_backward",
            "ultramem_debug_wait_probe", "ultramem_debug_fail_alloc",
            "ultramem_debug_live_allocations", "ultramem_debug_candidates",
-           "ultramem_shard_route", "ultramem_shard_lookup", "ultramem_shard_pool")
+           "ultramem_shard_route", "ultramem_shard_lookup", "ultramem_shard_pool",
+           "ultramem_paged_plan", "ultramem_paged_append", "ultramem_paged_attention",
+           "ultramem_paged_attention_workspace", "ultramem_block_norm",
+           "ultramem_block_norm_backward", "ultramem_block_norm_backward_workspace")
 
 
 class Config(C.Structure):
@@ -47,6 +50,19 @@ class Weights(C.Structure):
                 ("t", C.c_void_p), ("values", C.c_void_p), ("w_proj", C.c_void_p),
                 ("perm", C.c_void_p), ("conv_w", C.c_void_p), ("conv_b", C.c_void_p),
                 ("ln_g", C.c_void_p), ("ln_b", C.c_void_p)]
+
+
+class KVCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + [(name, C.c_int32) for name in (
+        "n_pages", "kv_heads", "page_size", "head_dim", "dtype")]
+
+
+class BlockNormArgs(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in (
+        "y", "gate", "w_post", "b_post", "w_pre", "b_pre")] + \
+        [("ld_y", C.c_int64), ("ld_r", C.c_int64)] + [(name, C.c_int32) for name in (
+            "n_tokens", "dim", "dtype", "kind", "post", "pre", "gate_mode")] + \
+        [(name, C.c_float) for name in ("res_scale", "out_scale", "eps")]
 
 
 class UltraMemError(RuntimeError):
@@ -127,6 +143,23 @@ def load(path: str | None = None) -> C.CDLL:
         lib.ultramem_shard_lookup.restype = I32
         lib.ultramem_shard_pool.argtypes = [P, P, P, I32, P, P, P, P]
         lib.ultramem_shard_pool.restype = I32
+        F = C.c_float
+        lib.ultramem_paged_plan.argtypes = [P, P, I32, I32, P, I32, P, P, I32, P, P, P, P, P, P]
+        lib.ultramem_paged_plan.restype = I32
+        lib.ultramem_paged_append.argtypes = [P, P, I64, P, I64, P, I32, P]
+        lib.ultramem_paged_append.restype = I32
+        lib.ultramem_paged_attention.argtypes = [P, P, I64, I32, P, P, P, I32, I32, I32, I32, F,
+                                                 P, P, P, I64, P]
+        lib.ultramem_paged_attention.restype = I32
+        lib.ultramem_paged_attention_workspace.argtypes = [I32] * 5
+        lib.ultramem_paged_attention_workspace.restype = I64
+        lib.ultramem_block_norm.argtypes = [P, P, P, P, P]
+        lib.ultramem_block_norm.restype = I32
+        lib.ultramem_block_norm_backward.argtypes = [P, P, P, I64, P, I64, P, P, P, P, P, P, P, P,
+                                                     I64, P]
+        lib.ultramem_block_norm_backward.restype = I32
+        lib.ultramem_block_norm_backward_workspace.argtypes = [I64, I32]
+        lib.ultramem_block_norm_backward_workspace.restype = I64
         _lib = lib
         return lib
 

@@ -1232,6 +1232,8 @@ cudaError_t launch_copy16(const void *src, void *dst, size_t bytes, cudaStream_t
     return cudaGetLastError();
 }
 
+ultramem_status status_from_cuda(cudaError_t e) { return from_cuda(e); }
+
 int device_sm_count() {
     static int n = 0;
     if (!n) {

@@ -255,6 +255,10 @@ constexpr size_t kSmemReserved = 1024;    // the driver's reservation per CTA
 
 int device_sm_count();
 
+// The status of a CUDA call for entry points defined outside ultramem.cu (the
+// error's text is kept for ultramem_last_error).
+ultramem_status status_from_cuda(cudaError_t e);
+
 // Host buffers: the device address of mapped pinned memory (null otherwise),
 // and a 16-byte copy kernel (host link or device memory).
 const void *mapped_host(const void *p, size_t bytes);

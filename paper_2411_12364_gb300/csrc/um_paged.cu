@@ -1,0 +1,631 @@
+// um_paged.cu -- the paged key/value cache: pages for a step's new tokens
+// (paged_plan), the new keys and values into their pages (paged_append), and
+// the attention kernel of the storages and head widths that the tensor-core
+// kernels do not take, with the kernel that joins split tiles.
+#include "um_paged.cuh"
+
+namespace um {
+namespace paged {
+namespace {
+
+// ---- plan ----------------------------------------------------------------
+// One integer pass over the requests' lengths: prefix sums of the new tokens
+// (q_start) and of the pages they need.  It is bound by latency, so it is one
+// launch: every block of the grid takes both prefix sums over all requests
+// itself (a few KB from L2) and then serves its own run of the new tokens.
+// The thread that holds the first token of a new page enters that page in
+// the table, so the table's writes are spread like the tokens; the pages that
+// a token reads from the table are the context's, which nothing writes.
+struct PlanArgs {
+    const int32_t *ctx, *fresh, *free_pages, *free_count;
+    int32_t *table, *q_start, *kv_lens, *slots, *free_left, *balance;
+    int n_seqs, n_tokens, page_shift, table_width;
+};
+
+struct PlanRequest {
+    int ctx, n;
+    int64_t need;               // new pages; 0 when the table is too narrow
+    bool fits;
+    __device__ __forceinline__ void read(const PlanArgs &a, int r) {
+        ctx = max(0, a.ctx[r]);
+        n = max(0, a.fresh[r]);
+        const int mask = (1 << a.page_shift) - 1;
+        const int64_t full = ((int64_t)ctx + n + mask) >> a.page_shift;
+        fits = full <= a.table_width && (int64_t)ctx + n <= INT32_MAX;
+        need = fits ? full - (((int64_t)ctx + mask) >> a.page_shift) : 0;
+    }
+    // upto: the pages needed by this and all earlier requests
+    __device__ __forceinline__ bool granted(const PlanArgs &a, int64_t upto, int64_t tok0,
+                                            int free) const {
+        return fits && (need == 0 || upto <= free) && tok0 + n <= a.n_tokens;
+    }
+};
+
+template <int THREADS> __global__ void __launch_bounds__(THREADS) plan_kernel(PlanArgs a) {
+    __shared__ int64_t warp_need[THREADS / 32], warp_tok[THREADS / 32];
+    __shared__ int64_t need_at[THREADS], tok_at[THREADS + 1];   // before thread i's run
+    __shared__ unsigned long long taken, asked;
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    const int per = (a.n_seqs + THREADS - 1) / THREADS;
+    const int r0 = min(a.n_seqs, tid * per), r1 = min(a.n_seqs, r0 + per);
+    const int free = max(0, *a.free_count);
+    PlanRequest q;
+    int64_t need = 0, tok = 0;
+    for (int r = r0; r < r1; ++r) {
+        q.read(a, r);
+        need += q.need;
+        tok += q.n;
+    }
+    int64_t need_to = need, tok_to = tok;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t x = __shfl_up_sync(0xffffffffu, need_to, o);
+        const int64_t y = __shfl_up_sync(0xffffffffu, tok_to, o);
+        if (lane >= o) {
+            need_to += x;
+            tok_to += y;
+        }
+    }
+    if (lane == 31) {
+        warp_need[w] = need_to;
+        warp_tok[w] = tok_to;
+    }
+    if (tid == 0) taken = asked = 0;
+    __syncthreads();
+    int64_t need_b = need_to - need, tok_b = tok_to - tok, total = 0;
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) {
+        if (i < w) {
+            need_b += warp_need[i];
+            tok_b += warp_tok[i];
+        }
+        total += warp_tok[i];
+    }
+    need_at[tid] = need_b;
+    tok_at[tid] = tok_b;
+    if (tid == 0) tok_at[THREADS] = total;
+
+    if (blockIdx.x == 0) {   // the requests' own outputs
+        int64_t upto = need_b, at = tok_b, last = 0, served = 0;
+        for (int r = r0; r < r1; ++r) {
+            q.read(a, r);
+            upto += q.need;
+            const bool ok = q.granted(a, upto, at, free);
+            if (ok && q.need) last = upto;
+            if (ok) served = upto;
+            a.q_start[r] = (int32_t)min(at, (int64_t)INT32_MAX);
+            a.kv_lens[r] = ok ? q.ctx + q.n : 0;
+            at += q.n;
+        }
+        if (last) atomicMax(&taken, (unsigned long long)last);
+        if (served) atomicMax(&asked, (unsigned long long)served);
+    }
+    __syncthreads();
+    if (blockIdx.x == 0 && tid == 0) {
+        a.q_start[a.n_seqs] = (int32_t)min(total, (int64_t)INT32_MAX);
+        *a.free_left = free - (int)taken;
+        *a.balance = (int32_t)max((int64_t)INT32_MIN, (int64_t)free - (int64_t)asked);
+    }
+
+    const int tokens = (int)min(total, (int64_t)a.n_tokens);
+    for (int i = blockIdx.x * THREADS + tid; i < a.n_tokens; i += gridDim.x * THREADS) {
+        if (i >= tokens) {   // past the batch's tokens
+            a.slots[i] = -1;
+            continue;
+        }
+        int lo = 0, hi = THREADS - 1;   // the last run that starts at or before i
+        while (lo < hi) {
+            const int m = (lo + hi + 1) >> 1;
+            if (tok_at[m] <= i)
+                lo = m;
+            else
+                hi = m - 1;
+        }
+        int64_t upto = need_at[lo], at = tok_at[lo];
+        int r = lo * per;
+        for (;; ++r) {
+            q.read(a, r);
+            upto += q.need;
+            if (at + q.n > i) break;
+            at += q.n;
+        }
+        int64_t slot = -1;
+        if (q.granted(a, upto, at, free)) {
+            const int mask = (1 << a.page_shift) - 1;
+            const int pos = q.ctx + (int)(i - at), col = pos >> a.page_shift;
+            const int old = (int)(((int64_t)q.ctx + mask) >> a.page_shift);
+            int32_t *entry = a.table + (int64_t)r * a.table_width + col;
+            int page;
+            if (col < old) {
+                page = *entry;
+            } else {
+                page = a.free_pages[free - 1 - (upto - q.need + (col - old))];
+                if ((pos & mask) == 0) *entry = page;
+            }
+            slot = page < 0 ? -1 : ((int64_t)page << a.page_shift) + (pos & mask);
+        }
+        a.slots[i] = slot <= INT32_MAX ? (int32_t)slot : -1;
+    }
+}
+
+// ---- append --------------------------------------------------------------
+// A scatter of whole rows: each thread moves one piece (16 bytes where the
+// rows are aligned to that, else one element) of a token's keys and the same
+// piece of its values.  Bound by memory: each byte is read and written once.
+template <typename W>
+__global__ void __launch_bounds__(256) append_kernel(const W *k, const W *v, int64_t k_stride,
+                                                     int64_t v_stride, const int32_t *slots,
+                                                     W *k_cache, W *v_cache, int n_tokens,
+                                                     int heads, int words, int page_shift,
+                                                     int64_t n_slots) {
+    const int per_token = heads * words;
+    const int64_t total = (int64_t)n_tokens * per_token;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+        const int t = (int)(i / per_token), j = (int)(i - (int64_t)t * per_token);
+        const int slot = slots[t];
+        if (slot < 0 || slot >= n_slots) continue;
+        const W x = k[t * k_stride + j], y = v[t * v_stride + j];
+        const int h = j / words, c = j - h * words;
+        const int page = slot >> page_shift, at = slot & ((1 << page_shift) - 1);
+        const int64_t dst = ((((int64_t)page * heads + h) << page_shift) + at) * words + c;
+        k_cache[dst] = x;
+        v_cache[dst] = y;
+    }
+}
+
+// ---- attention, CUDA cores --------------------------------------------------
+// fp32 storage, and bf16 heads wider than the tensor-core kernels take.  A
+// block holds a tile of ROWS rows and walks its keys in blocks of kKeys: the
+// scores of the block by dot products from shared memory, the running maximum
+// and sum of each row, the values added into registers.  Bound by the fp32
+// pipes (and at few rows by shared-memory reads); sums are fp32 throughout.
+constexpr int kKeys = 32;
+constexpr int kThreads = 256;
+
+template <int ROWS> __host__ __device__ constexpr size_t rows_smem(int dp) {
+    // q [ROWS][dp + 4], k [kKeys][dp + 4], v [kKeys][dp], p [ROWS][kKeys + 1]
+    return sizeof(float) * ((size_t)(ROWS + kKeys) * (dp + 4) + (size_t)kKeys * dp +
+                            (size_t)ROWS * (kKeys + 1));
+}
+
+template <typename T, int ROWS, int ND>   // head dims padded to 64 ND
+__global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
+    constexpr int DP = 64 * ND, LD = DP + 4;
+    constexpr int RPT = ROWS / 16;            // rows a thread accumulates
+    constexpr int TPR = kThreads / ROWS;      // threads of a row's softmax
+    constexpr int KPT = kKeys / TPR;          // keys each of them holds
+    extern __shared__ float smem[];
+    float *qs = smem, *ks = qs + ROWS * LD, *vs = ks + kKeys * LD, *ps = vs + kKeys * DP;
+    __shared__ float alpha[ROWS], denom[ROWS], top[ROWS];
+    __shared__ int64_t scratch[kThreads / 32 + 1];
+    __shared__ Cursor cur;
+    __shared__ int pages[kKeys];
+    const int tid = threadIdx.x, page_mask = (1 << a.page_shift) - 1;
+    place_share<kThreads>(a, blockIdx.x, gridDim.x, kKeys, 4 * kKeys, scratch, &cur);
+    int4 *desc = a.part_desc + 2 * blockIdx.x;
+    if (tid == 0) desc[0] = desc[1] = make_int4(kPartNone, 0, 0, 0);
+    Walk wk;
+    wk.begin(a, cur);
+    const int rg = tid >> 4, cg = tid & 15;   // this thread's rows rg RPT.., columns 4 cg + 64 i
+    const int srow = tid / TPR, spos = tid % TPR;
+    while (wk.next(a, kKeys)) {
+        const int n_rows = wk.n_tok * a.group;
+        __syncthreads();
+        for (int i = tid; i < ROWS * DP; i += kThreads) {
+            const int row = i / DP, c = i - row * DP;
+            float x = 0.f;
+            if (row < n_rows && c < a.D)
+                x = to_f(static_cast<const T *>(
+                    a.q)[(wk.tok0 + row / a.group) * a.q_stride +
+                         (int64_t)(wk.h * a.group + row % a.group) * a.D + c]);
+            qs[row * LD + c] = x;
+        }
+        float acc[RPT][4 * ND];
+#pragma unroll
+        for (int i = 0; i < RPT; ++i)
+#pragma unroll
+            for (int c = 0; c < 4 * ND; ++c) acc[i][c] = 0.f;
+        // each thread of a row keeps the row's maximum; the sum is its share
+        float m = -INFINITY, l = 0.f;
+        const int limit = min(wk.kv, wk.pos0 + srow / a.group + 1);   // keys this row sees
+        for (int j = wk.j0; j < wk.j1; ++j) {
+            const int key0 = j * kKeys;
+            __syncthreads();
+            if (tid < kKeys) pages[tid] = page_of(a, wk.c.r, key0 + tid, wk.kv);
+            __syncthreads();
+            for (int i = tid; i < kKeys * DP; i += kThreads) {
+                const int key = i / DP, c = i - key * DP;
+                float x = 0.f, y = 0.f;
+                if (pages[key] >= 0 && c < a.D) {
+                    const int64_t at = ((((int64_t)pages[key] * a.kv_heads + wk.h)
+                                         << a.page_shift) + ((key0 + key) & page_mask)) * a.D + c;
+                    x = to_f(static_cast<const T *>(a.k)[at]);
+                    y = to_f(static_cast<const T *>(a.v)[at]);
+                }
+                ks[key * LD + c] = x;
+                vs[key * DP + c] = y;
+            }
+            __syncthreads();
+            // scores: this thread's row, keys spos + TPR i
+            float s[KPT];
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) s[i] = 0.f;
+            for (int c = 0; c < DP; c += 4) {
+                const float4 x = *reinterpret_cast<const float4 *>(qs + srow * LD + c);
+#pragma unroll
+                for (int i = 0; i < KPT; ++i) {
+                    const float4 y =
+                        *reinterpret_cast<const float4 *>(ks + (spos + TPR * i) * LD + c);
+                    s[i] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[i]))));
+                }
+            }
+            float mx = m;
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) {
+                s[i] = key0 + spos + TPR * i < limit ? s[i] * a.scale_log2 : -INFINITY;
+                mx = fmaxf(mx, s[i]);
+            }
+#pragma unroll
+            for (int o = TPR / 2; o > 0; o >>= 1)
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            const float base = mx == -INFINITY ? 0.f : mx;   // a row without keys so far
+            const float f = exp2f(m - base);
+            m = mx;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) {
+                const float p = exp2f(s[i] - base);
+                l += p;
+                ps[srow * (kKeys + 1) + spos + TPR * i] = p;
+            }
+            if (spos == 0) alpha[srow] = f;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < RPT; ++i) {
+                const float g = alpha[rg * RPT + i];
+#pragma unroll
+                for (int c = 0; c < 4 * ND; ++c) acc[i][c] *= g;
+            }
+            for (int key = 0; key < kKeys; ++key) {
+                float p[RPT];
+#pragma unroll
+                for (int i = 0; i < RPT; ++i) p[i] = ps[(rg * RPT + i) * (kKeys + 1) + key];
+#pragma unroll
+                for (int d = 0; d < ND; ++d) {
+                    const float4 y =
+                        *reinterpret_cast<const float4 *>(vs + key * DP + 64 * d + 4 * cg);
+#pragma unroll
+                    for (int i = 0; i < RPT; ++i) {
+                        acc[i][4 * d] = fmaf(p[i], y.x, acc[i][4 * d]);
+                        acc[i][4 * d + 1] = fmaf(p[i], y.y, acc[i][4 * d + 1]);
+                        acc[i][4 * d + 2] = fmaf(p[i], y.z, acc[i][4 * d + 2]);
+                        acc[i][4 * d + 3] = fmaf(p[i], y.w, acc[i][4 * d + 3]);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int o = TPR / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        __syncthreads();
+        if (spos == 0) {
+            denom[srow] = l;
+            top[srow] = m;
+        }
+        __syncthreads();
+        const int64_t rec = (int64_t)blockIdx.x * 2 + wk.slot;
+        if (wk.part != kPartNone && tid == 0)
+            desc[wk.slot] = make_int4(wk.part, wk.tok0, wk.n_tok, wk.h);
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+            const int row = rg * RPT + i;
+            if (row >= n_rows) continue;
+            if (wk.part != kPartNone) {
+                float *o = a.part_o + (rec * a.rows + row) * DP + 4 * cg;
+#pragma unroll
+                for (int d = 0; d < ND; ++d)
+                    *reinterpret_cast<float4 *>(o + 64 * d) = make_float4(
+                        acc[i][4 * d], acc[i][4 * d + 1], acc[i][4 * d + 2], acc[i][4 * d + 3]);
+                if (cg == 0) a.part_ml[rec * a.rows + row] = make_float2(top[row], denom[row]);
+                continue;
+            }
+            const int64_t head = (int64_t)(wk.tok0 + row / a.group) * a.q_heads +
+                                 wk.h * a.group + row % a.group;
+            const float r = denom[row] > 0.f ? 1.f / denom[row] : denom[row];
+            T *o = static_cast<T *>(a.out) + head * a.D;
+#pragma unroll
+            for (int c = 0; c < 4 * ND; ++c) {
+                const int col = 64 * (c >> 2) + 4 * cg + (c & 3);
+                if (col < a.D) o[col] = from_f<T>(denom[row] == 0.f ? 0.f : acc[i][c] * r);
+            }
+            if (a.lse && cg == 0)
+                a.lse[head] = denom[row] == 0.f ? -INFINITY
+                                                : (top[row] + log2f(denom[row])) / kLog2e;
+        }
+    }
+}
+
+// ---- join of split tiles ----------------------------------------------------
+// Block (c, y) joins rows 8 y.. of the tile that begins in share c and ends in
+// a later one: weights 2^(m_i - max m) over the shares' partials, in share
+// order, so the result does not depend on which share finished first.
+template <typename T, int DP>
+__global__ void __launch_bounds__(256) combine_kernel(AttnArgs a, int ctas) {
+    pdl_wait();
+    const int c = blockIdx.x, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    __shared__ int last;
+    int slot = -1;
+    int4 d;
+    for (int s = 0; s < 2; ++s) {
+        const int4 e = a.part_desc[2 * c + s];
+        if (e.x == kPartFirst) {
+            slot = s;
+            d = e;
+        }
+    }
+    if (slot < 0) return;   // the same in the whole block
+    if (threadIdx.x == 0) last = ctas - 1;
+    __syncthreads();
+    for (int i = c + 1 + (int)threadIdx.x; i < ctas; i += 256)
+        if (a.part_desc[2 * i].x == kPartLast) {
+            atomicMin(&last, i);
+            break;
+        }
+    __syncthreads();
+    const int row = blockIdx.y * 8 + w;
+    if (row >= d.z * a.group) return;
+    const int end = last;
+    const int64_t first = ((int64_t)2 * c + slot) * a.rows + row;
+    float m = a.part_ml[first].x;
+    for (int i = c + 1 + lane; i <= end; i += 32)
+        if (a.part_desc[2 * i].x >= kPartMiddle)
+            m = fmaxf(m, a.part_ml[(int64_t)2 * i * a.rows + row].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float base = m == -INFINITY ? 0.f : m;
+    float sum = 0.f, acc[DP / 32];
+#pragma unroll
+    for (int k = 0; k < DP / 32; ++k) acc[k] = 0.f;
+    for (int i = c; i <= end; ++i) {
+        if (i > c && a.part_desc[2 * i].x < kPartMiddle) continue;   // no block of this tile
+        const int64_t at = i == c ? first : (int64_t)2 * i * a.rows + row;
+        const float2 ml = a.part_ml[at];
+        const float f = exp2f(ml.x - base);
+        sum = fmaf(f, ml.y, sum);
+#pragma unroll
+        for (int k = 0; k < DP / 32; ++k)
+            acc[k] = fmaf(f, a.part_o[at * DP + lane + 32 * k], acc[k]);
+    }
+    const int64_t head = (int64_t)(d.y + row / a.group) * a.q_heads + d.w * a.group + row % a.group;
+    T *o = static_cast<T *>(a.out) + head * a.D;
+    const float r = 1.f / sum;
+#pragma unroll
+    for (int k = 0; k < DP / 32; ++k)
+        if (lane + 32 * k < a.D) o[lane + 32 * k] = from_f<T>(sum == 0.f ? 0.f : acc[k] * r);
+    if (a.lse && lane == 0) a.lse[head] = sum == 0.f ? -INFINITY : (m + log2f(sum)) / kLog2e;
+}
+
+template <typename T> cudaError_t combine(const AttnArgs &a, int ctas, int dp, bool pdl,
+                                          cudaStream_t st) {
+    const dim3 grid(ctas, (a.rows + 7) / 8);
+    switch (dp) {
+    case 64: return launch_kernel(pdl, combine_kernel<T, 64>, grid, 256, 0, st, a, ctas);
+    case 128: return launch_kernel(pdl, combine_kernel<T, 128>, grid, 256, 0, st, a, ctas);
+    case 192: return launch_kernel(pdl, combine_kernel<T, 192>, grid, 256, 0, st, a, ctas);
+    default: return launch_kernel(pdl, combine_kernel<T, 256>, grid, 256, 0, st, a, ctas);
+    }
+}
+
+template <typename T, int ROWS, int ND> cudaError_t rows_go(const AttnArgs &a, int ctas,
+                                                            cudaStream_t st) {
+    constexpr size_t smem = rows_smem<ROWS>(64 * ND);
+    static const cudaError_t set = cudaFuncSetAttribute(
+        rows_kernel<T, ROWS, ND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (set != cudaSuccess) return set;
+    rows_kernel<T, ROWS, ND><<<ctas, kThreads, smem, st>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename T, int ROWS> cudaError_t rows_dim(const AttnArgs &a, int ctas,
+                                                     cudaStream_t st) {
+    switch ((a.D + 63) / 64) {
+    case 1: return rows_go<T, ROWS, 1>(a, ctas, st);
+    case 2: return rows_go<T, ROWS, 2>(a, ctas, st);
+    case 3: return rows_go<T, ROWS, 3>(a, ctas, st);
+    default: return rows_go<T, ROWS, 4>(a, ctas, st);
+    }
+}
+
+// ---- the call's plan --------------------------------------------------------
+
+struct Layout {
+    int ctas, rows, tq, dp;
+    int64_t o, ml, desc, total;     // byte offsets in the workspace
+};
+
+Layout layout_of(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_t max_new) {
+    Layout l = {};
+    const int group = q_heads / kv_heads;
+    const int64_t rows = (int64_t)max_new * group;
+    l.dp = (dim + 63) / 64 * 64;
+    l.rows = rows <= 16 ? 16 : 64;
+    l.tq = l.rows / group;
+    l.ctas = 2 * device_sm_count();
+    (void)dtype;
+    l.o = 0;
+    l.ml = l.o + (int64_t)l.ctas * 2 * l.rows * l.dp * 4;
+    l.desc = l.ml + (int64_t)l.ctas * 2 * l.rows * 8;
+    l.total = l.desc + (int64_t)l.ctas * 2 * 16;
+    return l;
+}
+
+int shift_of(int32_t page_size) {
+    int s = 0;
+    while ((1 << s) < page_size) ++s;
+    return s;
+}
+
+bool page_size_ok(int32_t p) { return p >= 16 && p <= 256 && (p & (p - 1)) == 0; }
+
+bool cache_ok(const ultramem_kv_cache *c) {
+    return c && c->k && c->v && c->n_pages > 0 && c->kv_heads > 0 && c->kv_heads <= 1024 &&
+           c->head_dim > 0 && c->head_dim <= kMaxHeadDim && c->head_dim % 8 == 0 &&
+           page_size_ok(c->page_size) &&
+           (c->dtype == ULTRAMEM_F32 || c->dtype == ULTRAMEM_BF16) &&
+           ((uintptr_t)c->k & 15) == 0 && ((uintptr_t)c->v & 15) == 0 &&
+           (int64_t)c->n_pages * c->page_size <= INT32_MAX &&
+           (int64_t)c->n_pages * c->kv_heads <= INT32_MAX;
+}
+
+bool heads_ok(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_t max_new) {
+    return (dtype == ULTRAMEM_F32 || dtype == ULTRAMEM_BF16) && kv_heads > 0 && kv_heads <= 1024 &&
+           q_heads > 0 && q_heads % kv_heads == 0 && q_heads / kv_heads <= 64 && dim > 0 &&
+           dim <= kMaxHeadDim && dim % 8 == 0 && max_new >= 0;
+}
+
+}  // namespace
+
+cudaError_t launch_combine(const AttnArgs &a, int ctas, int dp, int dtype, bool pdl,
+                           cudaStream_t st) {
+    return dtype == ULTRAMEM_BF16 ? combine<__nv_bfloat16>(a, ctas, dp, pdl, st)
+                                  : combine<float>(a, ctas, dp, pdl, st);
+}
+
+}  // namespace paged
+}  // namespace um
+
+using namespace um::paged;
+
+extern "C" ultramem_status ultramem_paged_plan(const int32_t *ctx_lens, const int32_t *new_lens,
+                                               int32_t n_seqs, int32_t page_size,
+                                               int32_t *block_table, int32_t table_width,
+                                               const int32_t *free_pages,
+                                               const int32_t *free_count, int32_t n_tokens,
+                                               int32_t *q_start, int32_t *kv_lens,
+                                               int32_t *slots, int32_t *free_left,
+                                               int32_t *balance, void *stream) {
+    if (n_seqs < 0 || n_tokens < 0 || table_width < 0 || !page_size_ok(page_size) || !free_count ||
+        !q_start || !free_left || !balance || free_left == free_count || balance == free_count ||
+        balance == free_left)
+        return ULTRAMEM_EINVAL;
+    if (n_seqs > 0 && (!ctx_lens || !new_lens || !kv_lens || kv_lens == ctx_lens ||
+                       kv_lens == new_lens || (table_width > 0 && !block_table)))
+        return ULTRAMEM_EINVAL;
+    if (n_tokens > 0 && (!slots || !free_pages)) return ULTRAMEM_EINVAL;
+    PlanArgs a = {ctx_lens, new_lens,  free_pages, free_count, block_table,
+                  q_start,  kv_lens,   slots,      free_left,  balance,
+                  n_seqs,   n_tokens,  shift_of(page_size),    table_width};
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaGetLastError();
+    // more than 256 requests: wider blocks, so that no thread walks many
+    const int threads = n_seqs <= 256 ? 256 : 1024;
+    int64_t grid = ((int64_t)n_tokens + threads - 1) / threads;
+    const int64_t most = um::device_sm_count();
+    grid = grid < 1 ? 1 : grid > most ? most : grid;
+    if (threads == 256)
+        plan_kernel<256><<<(unsigned)grid, 256, 0, st>>>(a);
+    else
+        plan_kernel<1024><<<(unsigned)grid, 1024, 0, st>>>(a);
+    return um::status_from_cuda(cudaGetLastError());
+}
+
+extern "C" ultramem_status ultramem_paged_append(const ultramem_kv_cache *c, const void *k,
+                                                 int64_t k_stride, const void *v, int64_t v_stride,
+                                                 const int32_t *slots, int32_t n_tokens,
+                                                 void *stream) {
+    if (!cache_ok(c) || n_tokens < 0) return ULTRAMEM_EINVAL;
+    if (n_tokens == 0) return ULTRAMEM_OK;
+    const int row = c->kv_heads * c->head_dim;
+    if (!k || !v || !slots || k_stride < row || v_stride < row) return ULTRAMEM_EINVAL;
+    const int es = c->dtype == ULTRAMEM_BF16 ? 2 : 4;
+    if (((uintptr_t)k | (uintptr_t)v) % es) return ULTRAMEM_EINVAL;
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaGetLastError();
+    const int shift = shift_of(c->page_size);
+    const int64_t n_slots = (int64_t)c->n_pages << shift;
+    const bool wide = (((uintptr_t)k | (uintptr_t)v) & 15) == 0 && k_stride * es % 16 == 0 &&
+                      v_stride * es % 16 == 0;
+    const int per = wide ? 16 / es : 1;
+    const int64_t total = (int64_t)n_tokens * (row / per);
+    const int64_t most = (int64_t)um::device_sm_count() * 64;
+    const int64_t blocks = (total + 255) / 256;
+    const unsigned grid = (unsigned)(blocks < most ? blocks : most);
+    const int words = c->head_dim / per;
+    if (wide)
+        append_kernel<uint4><<<grid, 256, 0, st>>>(
+            static_cast<const uint4 *>(k), static_cast<const uint4 *>(v), k_stride / per,
+            v_stride / per, slots, static_cast<uint4 *>(c->k), static_cast<uint4 *>(c->v),
+            n_tokens, c->kv_heads, words, shift, n_slots);
+    else if (es == 2)
+        append_kernel<uint16_t><<<grid, 256, 0, st>>>(
+            static_cast<const uint16_t *>(k), static_cast<const uint16_t *>(v), k_stride, v_stride,
+            slots, static_cast<uint16_t *>(c->k), static_cast<uint16_t *>(c->v), n_tokens,
+            c->kv_heads, words, shift, n_slots);
+    else
+        append_kernel<uint32_t><<<grid, 256, 0, st>>>(
+            static_cast<const uint32_t *>(k), static_cast<const uint32_t *>(v), k_stride, v_stride,
+            slots, static_cast<uint32_t *>(c->k), static_cast<uint32_t *>(c->v), n_tokens,
+            c->kv_heads, words, shift, n_slots);
+    return um::status_from_cuda(cudaGetLastError());
+}
+
+extern "C" int64_t ultramem_paged_attention_workspace(int32_t dtype, int32_t q_heads,
+                                                      int32_t kv_heads, int32_t head_dim,
+                                                      int32_t max_new) {
+    if (!heads_ok(dtype, q_heads, kv_heads, head_dim, max_new)) return 0;
+    return layout_of(dtype, q_heads, kv_heads, head_dim, max_new).total;
+}
+
+extern "C" ultramem_status ultramem_paged_attention(
+    const ultramem_kv_cache *c, const void *q, int64_t q_stride, int32_t q_heads,
+    const int32_t *q_start, const int32_t *kv_lens, const int32_t *block_table,
+    int32_t table_width, int32_t n_seqs, int32_t n_tokens, int32_t max_new, float scale, void *out,
+    float *lse, void *workspace, int64_t workspace_bytes, void *stream) {
+    if (!cache_ok(c) || !heads_ok(c->dtype, q_heads, c->kv_heads, c->head_dim, max_new) ||
+        n_seqs < 0 || n_tokens < 0 || table_width < 0 || !(scale > 0.f) || !(scale < INFINITY))
+        return ULTRAMEM_EINVAL;
+    if (n_tokens == 0 || n_seqs == 0 || max_new == 0) return ULTRAMEM_OK;
+    const int es = c->dtype == ULTRAMEM_BF16 ? 2 : 4;
+    if (!q || !q_start || !kv_lens || !out || q_stride < (int64_t)q_heads * c->head_dim ||
+        (uintptr_t)q % es || (uintptr_t)out % es || (table_width > 0 && !block_table) ||
+        !workspace || ((uintptr_t)workspace & 15))
+        return ULTRAMEM_EINVAL;
+    const Layout l = layout_of(c->dtype, q_heads, c->kv_heads, c->head_dim, max_new);
+    if (workspace_bytes < l.total) return ULTRAMEM_EINVAL;
+    AttnArgs a = {};
+    a.q = q;
+    a.k = c->k;
+    a.v = c->v;
+    a.table = block_table;
+    a.q_start = q_start;
+    a.kv_lens = kv_lens;
+    a.out = out;
+    a.lse = lse;
+    char *ws = static_cast<char *>(workspace);
+    a.part_o = reinterpret_cast<float *>(ws + l.o);
+    a.part_ml = reinterpret_cast<float2 *>(ws + l.ml);
+    a.part_desc = reinterpret_cast<int4 *>(ws + l.desc);
+    a.q_stride = q_stride;
+    a.n_seqs = n_seqs;
+    a.n_tokens = n_tokens;
+    a.q_heads = q_heads;
+    a.kv_heads = c->kv_heads;
+    a.group = q_heads / c->kv_heads;
+    a.D = c->head_dim;
+    a.page_shift = shift_of(c->page_size);
+    a.table_width = table_width;
+    a.n_pages = c->n_pages;
+    a.rows = l.rows;
+    a.tq = l.tq;
+    a.scale = scale;
+    a.scale_log2 = scale * kLog2e;
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaGetLastError();
+    cudaError_t e;
+    if (c->dtype == ULTRAMEM_BF16)
+        e = l.rows == 16 ? rows_dim<__nv_bfloat16, 16>(a, l.ctas, st)
+                         : rows_dim<__nv_bfloat16, 64>(a, l.ctas, st);
+    else
+        e = l.rows == 16 ? rows_dim<float, 16>(a, l.ctas, st) : rows_dim<float, 64>(a, l.ctas, st);
+    if (e == cudaSuccess) e = launch_combine(a, l.ctas, l.dp, c->dtype, true, st);
+    return um::status_from_cuda(e);
+}
