@@ -430,6 +430,10 @@ ultramem_status ultramem_paged_attention(const ultramem_kv_cache *cache, const v
 /* Bytes of workspace for such calls (0 for arguments that the call refuses). */
 int64_t ultramem_paged_attention_workspace(int32_t dtype, int32_t q_heads, int32_t kv_heads,
                                            int32_t head_dim, int32_t max_new);
+/* Synchronises `stream`, then reads and clears the attention kernels' error
+ * word: ULTRAMEM_ETIMEOUT if a bounded wait gave up in a call since the last
+ * check (its output is then meaningless; never expected). */
+ultramem_status ultramem_paged_check(void *stream);
 
 enum { ULTRAMEM_NORM_RMS = 0, ULTRAMEM_NORM_LAYER = 1 };
 enum {

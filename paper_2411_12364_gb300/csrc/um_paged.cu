@@ -437,25 +437,82 @@ template <typename T, int ROWS> cudaError_t rows_dim(const AttnArgs &a, int ctas
 
 // ---- the call's plan --------------------------------------------------------
 
+// Which kernel serves a call.  The tensor-core kernels take bf16 heads up to
+// 128 wide; a call of at most 16 rows a request and key/value head reads each
+// key for those rows alone and goes to the decode kernel (M = 16), any other
+// to the 2 x 128-row kernel.  Everything else runs on the CUDA cores.
+enum Path { kRows16, kRows64, kDecode, kPrefill };
+
+Path path_of(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_t max_new,
+             bool tensor) {
+    const bool few = (int64_t)max_new * (q_heads / kv_heads) <= 16;
+    if (dtype == ULTRAMEM_BF16 && dim <= 128 && tensor) return few ? kDecode : kPrefill;
+    return few ? kRows16 : kRows64;
+}
+
 struct Layout {
     int ctas, rows, tq, dp;
     int64_t o, ml, desc, total;     // byte offsets in the workspace
 };
 
-Layout layout_of(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_t max_new) {
+Layout layout_of(Path path, int32_t group, int32_t dim) {
     Layout l = {};
-    const int group = q_heads / kv_heads;
-    const int64_t rows = (int64_t)max_new * group;
     l.dp = (dim + 63) / 64 * 64;
-    l.rows = rows <= 16 ? 16 : 64;
-    l.tq = l.rows / group;
-    l.ctas = 2 * device_sm_count();
-    (void)dtype;
+    l.ctas = path == kPrefill ? device_sm_count() : 2 * device_sm_count();
+    if (path == kPrefill) {
+        l.tq = 2 * (128 / group);
+        l.rows = l.tq * group;
+    } else {
+        l.rows = path == kRows64 ? 64 : 16;
+        l.tq = l.rows / group;
+    }
     l.o = 0;
     l.ml = l.o + (int64_t)l.ctas * 2 * l.rows * l.dp * 4;
-    l.desc = l.ml + (int64_t)l.ctas * 2 * l.rows * 8;
+    l.desc = (l.ml + (int64_t)l.ctas * 2 * l.rows * 8 + 15) & ~15ll;
     l.total = l.desc + (int64_t)l.ctas * 2 * 16;
     return l;
+}
+
+// A map of 64-column boxes over a bf16 tensor [outer][mid][inner] with the
+// given strides in elements; zeros outside.
+bool encode(CUtensorMap *map, const void *base, uint64_t inner, uint64_t mid, uint64_t outer,
+            uint64_t mid_stride, uint64_t outer_stride, uint32_t box_mid, uint32_t box_outer) {
+    using Fn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
+                            const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                            const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Fn fn = [] {
+        cudaDriverEntryPointQueryResult q;
+        void *f = nullptr;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000,
+                                             cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<Fn>(f);
+    }();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {inner, mid, outer};
+    const cuuint64_t strides[2] = {mid_stride * 2, outer_stride * 2};
+    const cuuint32_t box[3] = {64, box_mid, box_outer}, step[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides,
+              box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+           CUDA_SUCCESS;
+}
+
+// Set by a kernel whose bounded wait gave up; read and cleared by
+// ultramem_paged_check.
+__device__ int g_error;
+
+int *error_word() {
+    static int *const p = [] {
+        void *a = nullptr;
+        if (cudaGetSymbolAddress(&a, g_error) != cudaSuccess) cudaGetLastError();
+        return static_cast<int *>(a);
+    }();
+    return p;
 }
 
 int shift_of(int32_t page_size) {
@@ -572,7 +629,15 @@ extern "C" int64_t ultramem_paged_attention_workspace(int32_t dtype, int32_t q_h
                                                       int32_t kv_heads, int32_t head_dim,
                                                       int32_t max_new) {
     if (!heads_ok(dtype, q_heads, kv_heads, head_dim, max_new)) return 0;
-    return layout_of(dtype, q_heads, kv_heads, head_dim, max_new).total;
+    // the largest of the kernels that the call may take: a query or output that
+    // is not aligned for the tensor-core ones goes to the CUDA cores
+    int64_t most = 0;
+    for (const bool tensor : {false, true}) {
+        const Path p = path_of(dtype, q_heads, kv_heads, head_dim, max_new, tensor);
+        const int64_t n = layout_of(p, q_heads / kv_heads, head_dim).total;
+        most = n > most ? n : most;
+    }
+    return most;
 }
 
 extern "C" ultramem_status ultramem_paged_attention(
@@ -589,8 +654,17 @@ extern "C" ultramem_status ultramem_paged_attention(
         (uintptr_t)q % es || (uintptr_t)out % es || (table_width > 0 && !block_table) ||
         !workspace || ((uintptr_t)workspace & 15))
         return ULTRAMEM_EINVAL;
-    const Layout l = layout_of(c->dtype, q_heads, c->kv_heads, c->head_dim, max_new);
-    if (workspace_bytes < l.total) return ULTRAMEM_EINVAL;
+    if (workspace_bytes < ultramem_paged_attention_workspace(c->dtype, q_heads, c->kv_heads,
+                                                             c->head_dim, max_new))
+        return ULTRAMEM_EINVAL;
+    const int group = q_heads / c->kv_heads;
+    // 4-byte fragments of q and out suffice for the decode kernel; TMA wants
+    // rows of q on 16-byte boundaries
+    const bool few = (int64_t)max_new * group <= 16;
+    const int align = few ? 4 : 16;
+    const bool tensor = ((uintptr_t)q | (uintptr_t)out) % align == 0 && q_stride * es % align == 0;
+    const Path path = path_of(c->dtype, q_heads, c->kv_heads, c->head_dim, max_new, tensor);
+    const Layout l = layout_of(path, group, c->head_dim);
     AttnArgs a = {};
     a.q = q;
     a.k = c->k;
@@ -609,7 +683,7 @@ extern "C" ultramem_status ultramem_paged_attention(
     a.n_tokens = n_tokens;
     a.q_heads = q_heads;
     a.kv_heads = c->kv_heads;
-    a.group = q_heads / c->kv_heads;
+    a.group = group;
     a.D = c->head_dim;
     a.page_shift = shift_of(c->page_size);
     a.table_width = table_width;
@@ -620,12 +694,42 @@ extern "C" ultramem_status ultramem_paged_attention(
     a.scale_log2 = scale * kLog2e;
     cudaStream_t st = (cudaStream_t)stream;
     cudaGetLastError();
-    cudaError_t e;
-    if (c->dtype == ULTRAMEM_BF16)
-        e = l.rows == 16 ? rows_dim<__nv_bfloat16, 16>(a, l.ctas, st)
-                         : rows_dim<__nv_bfloat16, 64>(a, l.ctas, st);
-    else
-        e = l.rows == 16 ? rows_dim<float, 16>(a, l.ctas, st) : rows_dim<float, 64>(a, l.ctas, st);
+    cudaError_t e = cudaSuccess;
+    const bool bf = c->dtype == ULTRAMEM_BF16;
+    if (path == kDecode || path == kPrefill) {
+        if (!(a.err = error_word())) return ULTRAMEM_ECUDA;
+        CUtensorMap mq, mk, mv;
+        const uint64_t D = c->head_dim, P = c->page_size;
+        const uint64_t outer = (uint64_t)c->n_pages * c->kv_heads;
+        const uint32_t box = path == kDecode ? decode_box_rows(c->page_size)
+                                             : prefill_box_rows(c->page_size);
+        if (!encode(&mk, c->k, D, P, outer, D, P * D, box, 1) ||
+            !encode(&mv, c->v, D, P, outer, D, P * D, box, 1))
+            return ULTRAMEM_ECUDA;
+        if (path == kDecode) {
+            e = launch_decode(a, mk, mv, l.ctas, st);
+        } else {
+            if (!encode(&mq, q, D, q_heads, n_tokens, D, q_stride, group, l.tq / 2))
+                return ULTRAMEM_ECUDA;
+            e = launch_prefill(a, mq, mk, mv, l.ctas, st);
+        }
+    } else if (path == kRows16) {
+        e = bf ? rows_dim<__nv_bfloat16, 16>(a, l.ctas, st) : rows_dim<float, 16>(a, l.ctas, st);
+    } else {
+        e = bf ? rows_dim<__nv_bfloat16, 64>(a, l.ctas, st) : rows_dim<float, 64>(a, l.ctas, st);
+    }
     if (e == cudaSuccess) e = launch_combine(a, l.ctas, l.dp, c->dtype, true, st);
     return um::status_from_cuda(e);
+}
+
+extern "C" ultramem_status ultramem_paged_check(void *stream) {
+    int *word = error_word();
+    if (!word) return ULTRAMEM_ENODEV;
+    int err = 0;
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t e = cudaMemcpyAsync(&err, word, sizeof err, cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaMemsetAsync(word, 0, sizeof err, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e != cudaSuccess) return um::status_from_cuda(e);
+    return err & um::kErrTimeout ? ULTRAMEM_ETIMEOUT : ULTRAMEM_OK;
 }

@@ -203,14 +203,24 @@ struct Walk {
     }
 };
 
-// Keys of block j of the cache: the page of key `key` of request r, or -1
-// when the table has none (read as zeros).
+// The page of key `key` of request r, or -1 past its length and where the
+// table names no page of the cache (read as zeros).
 __device__ __forceinline__ int page_of(const AttnArgs &a, int r, int key, int kv) {
     if (key >= kv) return -1;
     const int p = a.table[(int64_t)r * a.table_width + (key >> a.page_shift)];
     return p < 0 || p >= a.n_pages ? -1 : p;
 }
 
+// bf16, heads up to 128 wide: at most 16 rows a tile (um_paged_decode.cu), or
+// two halves of 128 rows (um_paged_prefill.cu).  The maps are over the cache
+// as [pages x heads][page size][head width] with boxes of 64 columns x
+// *_box_rows tokens, and over q as [tokens][heads][width].
+int decode_box_rows(int page_size);
+int prefill_box_rows(int page_size);
+cudaError_t launch_decode(const AttnArgs &a, const CUtensorMap &k, const CUtensorMap &v, int ctas,
+                          cudaStream_t st);
+cudaError_t launch_prefill(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &k,
+                           const CUtensorMap &v, int ctas, cudaStream_t st);
 cudaError_t launch_combine(const AttnArgs &a, int ctas, int dp, int dtype, bool pdl,
                            cudaStream_t st);
 

@@ -1,0 +1,510 @@
+// um_paged_prefill.cu -- attention over the paged cache for chunks of new
+// tokens (bf16, heads up to 128 wide), on the tensor cores.
+//
+// One persistent CTA an SM works on tiles of 2 x 128 rows (new tokens x the
+// query heads of one key/value head, token-major, so that a key block is read
+// once for the whole group) against blocks of 128 keys:
+//   S_i = Q_i K^T        tcgen05.mma, both operands from shared memory
+//   P_i = 2^(S_i - m)    128 threads a half, one row each, S read from TMEM
+//   O_i += P_i V         tcgen05.mma, P from TMEM, V from shared memory
+// with S_0, S_1, O_0, O_1 in TMEM (512 columns at width 128); P_i takes S_i's
+// columns as bf16.  The two halves are what keeps the tensor cores busy: while
+// the threads of one half turn S into P, the tensor cores run the other
+// half's products.  Per block and half the products take 1024 cycles of the
+// tensor pipe at width 128 and the exponentials and their bookkeeping about
+// as many issue slots of one warp a scheduler, so the kernel is bound by
+// these two together.
+//
+// The maximum that the exponents refer to is not raised for every block, only
+// when a row's new maximum passes it by 2^8: the output and the sum refer to
+// the same value, so the quotient is the same, and the pass over O in TMEM
+// that a raise costs is rare.
+//
+// Warps: 0-3 and 4-7 the halves' softmax and output, 8 the products (one
+// thread), 9 the copies (TMA: K and V blocks, a box per page, in a ring; Q
+// per tile), 10 clears what a last page holds past the request's length.
+#include "um_paged.cuh"
+#include "um_tc.cuh"
+
+namespace um {
+namespace paged {
+namespace {
+
+constexpr int kKeys = 128;
+constexpr int kHalfRows = 128;
+constexpr int kThreads = 352;
+constexpr uint32_t kHalfBytes = 128 * 128;     // 128 rows x 64 columns of bf16
+constexpr float kRaise = 8.f;                  // log2 units
+
+template <int DP> struct Cfg {
+    static constexpr int kHalves = DP / 64;                   // 64-column halves of a row
+    static constexpr uint32_t kTile = kHalfBytes * kHalves;   // 128 rows
+    static constexpr int kStages = DP == 128 ? 5 : 10;
+    static constexpr size_t kSmem = (size_t)kTile * (2 + kStages) + 1024;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0],"
+        " {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+        "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+        "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+        "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() {
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+// D += A B with A (the weights, 16-bit pairs along a row) in TMEM
+__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc,
+                                            uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+// The values as the B operand: [key][64 columns] rows of 128 bytes, swizzled,
+// columns (N) contiguous: 8 keys are 1024 bytes apart (stride offset), the
+// next 64 columns a half (leading offset).
+__device__ __forceinline__ uint64_t desc_mn_sw128(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(kHalfBytes >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+constexpr uint32_t kBColumnsContiguous = 1u << 16;   // instruction descriptor: B is N-major
+
+// a wait of a whole warp, with one answer for all lanes
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) {
+    return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity));
+}
+
+// What each role needs of the tile at hand: blocks [j0, e[i]) of half i.
+struct Halves {
+    int n_tok[2], e[2], end;
+    __device__ __forceinline__ Halves(const Walk &wk, int tq_half) {
+        n_tok[0] = min(wk.n_tok, tq_half);
+        n_tok[1] = max(0, wk.n_tok - tq_half);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int sees = n_tok[i] ? wk.pos0 + i * tq_half + n_tok[i] : 0;   // keys
+            e[i] = max(wk.j0, min(wk.j1, (max(0, sees) + kKeys - 1) / kKeys));
+        }
+        end = max(e[0], e[1]);
+    }
+    __device__ __forceinline__ bool live(const Walk &wk) const { return end > wk.j0; }
+    // the block that holds the request's last page, when that page has places
+    // past the length; -1 without one among [j0, end)
+    __device__ __forceinline__ int tail(const Walk &wk, int page_mask) const {
+        const int j = wk.kv / kKeys;
+        return (wk.kv & page_mask) && j >= wk.j0 && j < end ? j : -1;
+    }
+};
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+    prefill_kernel(const __grid_constant__ CUtensorMap map_q,
+                   const __grid_constant__ CUtensorMap map_k,
+                   const __grid_constant__ CUtensorMap map_v, AttnArgs a, int box_rows) {
+    using C = Cfg<DP>;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t kv_full[C::kStages], kv_empty[C::kStages], kv_raw[C::kStages];
+    __shared__ uint64_t q_full, q_empty, s_full[2], p_full[2], o_full[2], drained;
+    __shared__ int64_t scratch[kThreads / 32 + 1];
+    __shared__ Cursor cur;
+    __shared__ uint32_t tmem_base;
+    uint8_t *qs = raw + ((1024 - (tc::smem_u32(raw) & 1023)) & 1023);
+    uint8_t *ring = qs + 2 * C::kTile;
+    const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int s = 0; s < C::kStages; ++s) {
+            tc::mbar_init(&kv_full[s], 1);
+            tc::mbar_init(&kv_empty[s], 1);
+            tc::mbar_init(&kv_raw[s], 1);
+        }
+        tc::mbar_init(&q_full, 1);
+        tc::mbar_init(&q_empty, 1);
+        tc::mbar_init(&drained, 1);
+        for (int i = 0; i < 2; ++i) {
+            tc::mbar_init(&s_full[i], 1);
+            tc::mbar_init(&p_full[i], kHalfRows);
+            tc::mbar_init(&o_full[i], 1);
+        }
+        tc::fence_mbar_init();
+    }
+    pdl_wait();
+    place_share<kThreads>(a, blockIdx.x, gridDim.x, kKeys, 2 * kKeys, scratch, &cur);
+    if (w == 8) tc::tmem_alloc(&tmem_base, 512);
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    pdl_trigger();
+    const uint32_t tmem = tmem_base;
+    const uint32_t tmem_s[2] = {tmem, tmem + 128}, tmem_o[2] = {tmem + 256, tmem + 256 + DP};
+    const int tq_half = a.tq / 2;
+    const int page_mask = (1 << a.page_shift) - 1;
+    Walk wk;
+    wk.begin(a, cur);
+    bool ok = true;
+
+    if (w < 8) {
+        // ---- softmax and output of half i: thread = row ----
+        const int i = w >> 2, row = (w & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((w & 3) * 32) << 16;
+        const uint32_t ts = tmem_s[i] + lanes, to = tmem_o[i] + lanes;
+        int4 *desc = a.part_desc + 2 * blockIdx.x;
+        if (tid == 0) desc[0] = desc[1] = make_int4(kPartNone, 0, 0, 0);
+        const int tok = row / a.group, g = row - tok * a.group;
+        uint32_t blocks = 0, tiles = 0;      // done so far by this half: barrier phases
+        while (ok && wk.next(a, kKeys)) {
+            const Halves hv(wk, tq_half);
+            const bool mine = tok < hv.n_tok[i] && tok < tq_half;
+            const int pos = wk.pos0 + i * tq_half + tok;
+            const int limit = mine ? min(wk.kv, pos + 1) : 0;   // keys this row sees
+            // keys that all rows of the half see: below it no masking
+            const int all_see = hv.n_tok[i] == tq_half && tq_half * a.group == kHalfRows
+                                    ? wk.pos0 + i * tq_half + 1 : 0;
+            float m = -INFINITY, l = 0.f;
+            for (int j = wk.j0; j < hv.e[i]; ++j) {
+                if (!warp_wait(&s_full[i], blocks & 1)) {
+                    ok = false;
+                    break;
+                }
+                ++blocks;
+                tc::tc_fence_after();
+                uint32_t s[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tc::tmem_ld32_nowait(ts + 32 * c, s[c]);
+                tc::tmem_ld_wait();
+                if ((j + 1) * kKeys > all_see) {
+                    const int left = limit - j * kKeys;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (32 * c + k >= left) s[c][k] = 0xff800000u;   // -inf
+                }
+                float mx[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    mx[c] = __uint_as_float(s[c][0]);
+#pragma unroll
+                    for (int k = 1; k < 32; ++k) mx[c] = fmaxf(mx[c], __uint_as_float(s[c][k]));
+                }
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                const bool raise = (top - m) * a.scale_log2 > kRaise ||
+                                   (m == -INFINITY && top > -INFINITY);
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float f = raise ? ex2((m - top) * a.scale_log2) : 1.f;
+                    if (raise) m = top;
+                    l *= f;
+                    if (j > wk.j0) {   // S_i is there, so all earlier products are done
+#pragma unroll
+                        for (int c = 0; c < DP / 32; ++c) {
+                            uint32_t o[32];
+                            tc::tmem_ld32_nowait(to + 32 * c, o);
+                            tc::tmem_ld_wait();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tmem_st32(to + 32 * c, o);
+                        }
+                    }
+                }
+                const float shift = m == -INFINITY ? 0.f : -m * a.scale_log2;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                uint32_t p[2][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int k = 0; k < 32; k += 2) {
+                        const float x = ex2(fmaf(__uint_as_float(s[c][k]), a.scale_log2, shift));
+                        const float y =
+                            ex2(fmaf(__uint_as_float(s[c][k + 1]), a.scale_log2, shift));
+                        sum[k & 2] += x;
+                        sum[(k & 2) + 1] += y;
+                        // weights as the A operand: one rounding to bf16, as
+                        // large as that of the values; the sum keeps fp32
+                        const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+                        p[c >> 1][16 * (c & 1) + (k >> 1)] =
+                            *reinterpret_cast<const uint32_t *>(&b);
+                    }
+                tmem_st32(ts, p[0]);
+                tmem_st32(ts + 32, p[1]);
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                tmem_st_wait();
+                tc::tc_fence_before();
+                tc::mbar_arrive(&p_full[i]);
+            }
+            if (!ok) break;
+            const bool any = hv.e[i] > wk.j0;
+            if (any) {
+                if (!warp_wait(&o_full[i], tiles & 1)) {
+                    ok = false;
+                    break;
+                }
+                ++tiles;
+                tc::tc_fence_after();
+            }
+            if (wk.part != kPartNone && tid == 0)
+                desc[wk.slot] = make_int4(wk.part, wk.tok0, wk.n_tok, wk.h);
+            const int64_t rec = ((int64_t)blockIdx.x * 2 + wk.slot) * a.rows +
+                                i * tq_half * a.group + row;
+            const int64_t head = (int64_t)(wk.tok0 + i * tq_half + tok) * a.q_heads +
+                                 wk.h * a.group + g;
+            const bool none = l == 0.f;
+            const float r = none ? 0.f : 1.f / l;
+            const float top = m == -INFINITY ? -INFINITY : m * a.scale_log2;
+            if (mine) {
+                if (wk.part != kPartNone)
+                    a.part_ml[rec] = make_float2(top, l);
+                else if (a.lse)
+                    a.lse[head] = none ? -INFINITY : (top + log2f(l)) / kLog2e;
+            }
+#pragma unroll
+            for (int c = 0; c < DP / 32; ++c) {
+                uint32_t o[32];
+                if (any) {
+                    tc::tmem_ld32_nowait(to + 32 * c, o);
+                    tc::tmem_ld_wait();
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) o[k] = 0u;
+                }
+                if (!mine) continue;
+                if (wk.part != kPartNone) {
+                    float4 *dst = reinterpret_cast<float4 *>(a.part_o + rec * DP + 32 * c);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        dst[k] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]),
+                                             __uint_as_float(o[4 * k + 2]),
+                                             __uint_as_float(o[4 * k + 3]));
+                    continue;
+                }
+                __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + head * a.D + 32 * c;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (32 * c + 8 * k < a.D) {
+                        uint32_t q[4];
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            const __nv_bfloat162 b = __floats2bfloat162_rn(
+                                none ? 0.f : __uint_as_float(o[8 * k + 2 * x]) * r,
+                                none ? 0.f : __uint_as_float(o[8 * k + 2 * x + 1]) * r);
+                            q[x] = *reinterpret_cast<const uint32_t *>(&b);
+                        }
+                        *reinterpret_cast<uint4 *>(dst + 8 * k) =
+                            make_uint4(q[0], q[1], q[2], q[3]);
+                    }
+            }
+            tc::tc_fence_before();   // O is read: the next tile's products may write it
+        }
+        if (!ok && lane == 0) atomicOr(a.err, kErrTimeout);
+    } else if (w == 8 && lane == 0) {
+        // ---- products: one thread issues, in an order that alternates the
+        // halves: P_0 V, next S_0, P_1 V, next S_1 ----
+        constexpr uint32_t idesc_s = tc::idesc_bf16_f32(128, kKeys);
+        constexpr uint32_t idesc_o = tc::idesc_bf16_f32(128, DP) | kBColumnsContiguous;
+        const uint32_t q_addr = tc::smem_u32(qs), kv_addr = tc::smem_u32(ring);
+        int stage = 0;
+        uint32_t phase = 0, tiles = 0, p_phase[2] = {0, 0};
+        auto advance = [&] {
+            if (++stage == C::kStages) {
+                stage = 0;
+                phase ^= 1;
+            }
+        };
+        auto scores = [&](int i, int st) {
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k) {
+                const uint32_t off = (k >> 2) * kHalfBytes + (k & 3) * 32;
+                tc::mma_bf16(tmem_s[i], tc::desc_k_sw128(q_addr + i * C::kTile + off),
+                             tc::desc_k_sw128(kv_addr + st * C::kTile + off), idesc_s, k > 0);
+            }
+            tc::mma_commit(&s_full[i]);
+        };
+        while (ok && wk.next(a, kKeys)) {
+            const Halves hv(wk, tq_half);
+            if (!hv.live(wk)) continue;
+            if (!(ok = tc::mbar_wait(&q_full, tiles & 1))) break;
+            ++tiles;
+            if (!(ok = tc::mbar_wait(&kv_full[stage], phase))) break;
+            tc::tc_fence_after();
+            for (int i = 0; i < 2; ++i)
+                if (wk.j0 < hv.e[i]) scores(i, stage);
+            tc::mma_commit(&kv_empty[stage]);
+            if (wk.j0 + 1 == hv.end) tc::mma_commit(&q_empty);
+            advance();
+            for (int j = wk.j0; ok && j < hv.end; ++j) {
+                const int sv = stage;
+                if (!(ok = tc::mbar_wait(&kv_full[stage], phase))) break;
+                tc::tc_fence_after();
+                advance();
+                const bool more = j + 1 < hv.end;
+                const int sk = stage;
+                if (more && !(ok = tc::mbar_wait(&kv_full[stage], phase))) break;
+                for (int i = 0; i < 2; ++i) {
+                    if (j < hv.e[i]) {
+                        if (!(ok = tc::mbar_wait(&p_full[i], p_phase[i]))) break;
+                        p_phase[i] ^= 1;
+                        tc::tc_fence_after();
+#pragma unroll
+                        for (int k = 0; k < kKeys / 16; ++k)
+                            mma_bf16_ts(tmem_o[i], tmem_s[i] + 8 * k,
+                                        desc_mn_sw128(kv_addr + sv * C::kTile + k * 16 * 128),
+                                        idesc_o, j > wk.j0 || k > 0);
+                        if (j + 1 == hv.e[i]) tc::mma_commit(&o_full[i]);
+                    }
+                    if (j + 1 < hv.e[i]) scores(i, sk);
+                }
+                if (!ok) break;
+                tc::mma_commit(&kv_empty[sv]);
+                if (more) {
+                    tc::mma_commit(&kv_empty[sk]);
+                    if (j + 2 == hv.end) tc::mma_commit(&q_empty);
+                    advance();
+                }
+            }
+        }
+        if (!ok) {
+            atomicOr(a.err, kErrTimeout);
+            tc::mma_commit(&drained);          // products in flight end before TMEM is freed
+            tc::mbar_wait(&drained, 0);
+        }
+    } else if (w == 9) {
+        // ---- copies: the whole warp, a lane per page of the block ----
+        if (lane == 0) {
+            tc::prefetch_tensormap(&map_q);
+            tc::prefetch_tensormap(&map_k);
+            tc::prefetch_tensormap(&map_v);
+        }
+        const int pages = kKeys / box_rows;
+        const uint32_t q_bytes = (uint32_t)(tq_half * a.group) * 128 * C::kHalves;
+        int stage = 0, issued = 0;
+        uint32_t phase = 0, tiles = 0;
+        while (ok && wk.next(a, kKeys)) {
+            const Halves hv(wk, tq_half);
+            if (!hv.live(wk)) continue;
+            const int tail = hv.tail(wk, page_mask);
+            if (!(ok = warp_wait(&q_empty, (tiles & 1) ^ 1))) break;
+            ++tiles;
+            if (lane == 0) {
+                const int n = hv.n_tok[1] ? 2 : 1;
+                tc::mbar_arrive_expect_tx(&q_full, n * q_bytes);
+                for (int i = 0; i < n; ++i)
+#pragma unroll
+                    for (int x = 0; x < C::kHalves; ++x)
+                        tc::tma_load_3d(qs + i * C::kTile + x * kHalfBytes, &map_q, &q_full,
+                                        64 * x, wk.h * a.group, wk.tok0 + i * tq_half);
+            }
+            for (int j = wk.j0; ok && j < hv.end; ++j) {
+                const int key = j * kKeys + lane * box_rows;
+                int z = a.n_pages * a.kv_heads;             // outside: reads zeros
+                if (lane < pages) {
+                    const int p = page_of(a, wk.c.r, key, wk.kv);
+                    if (p >= 0) z = p * a.kv_heads + wk.h;
+                }
+#pragma unroll
+                for (int which = 0; which < 2; ++which) {   // K, then V
+                    if (!(ok = warp_wait(&kv_empty[stage], phase ^ 1))) break;
+                    uint64_t *bar = which && j == tail ? &kv_raw[stage] : &kv_full[stage];
+                    if (lane == 0) tc::mbar_arrive_expect_tx(bar, C::kTile);
+                    __syncwarp();
+                    if (lane < pages) {
+                        uint8_t *dst = ring + (size_t)stage * C::kTile + lane * box_rows * 128;
+#pragma unroll
+                        for (int x = 0; x < C::kHalves; ++x)
+                            tc::tma_load_3d(dst + x * kHalfBytes, which ? &map_v : &map_k, bar,
+                                            64 * x, key & page_mask, z);
+                    }
+                    ++issued;
+                    if (++stage == C::kStages) {
+                        stage = 0;
+                        phase ^= 1;
+                    }
+                }
+            }
+        }
+        if (!ok) {   // leave nothing in flight: wait for the copies issued last
+            if (lane == 0) atomicOr(a.err, kErrTimeout);
+            if (tiles) tc::mbar_wait(&q_full, (tiles - 1) & 1);
+            for (int k = 0; k < C::kStages && k < issued; ++k) {
+                if (--stage < 0) {
+                    stage = C::kStages - 1;
+                    phase ^= 1;
+                }
+                tc::mbar_wait(&kv_full[stage], phase);
+            }
+        }
+    } else if (w == 10) {
+        // ---- the last page's places past the length may hold anything, and
+        // weight 0 times that could be NaN: clear them in V's copy ----
+        int stage = 0;
+        uint32_t raw_phase = 0;               // a bit a stage
+        while (ok && wk.next(a, kKeys)) {
+            const Halves hv(wk, tq_half);
+            if (!hv.live(wk)) continue;
+            const int tail = hv.tail(wk, page_mask);
+            const int n = 2 * (hv.end - wk.j0);              // stages this tile takes
+            if (tail >= 0) {
+                const int st = (stage + 2 * (tail - wk.j0) + 1) % C::kStages;
+                if (!(ok = warp_wait(&kv_raw[st], (raw_phase >> st) & 1))) break;
+                raw_phase ^= 1u << st;
+                const int from = wk.kv - tail * kKeys;
+                const int to = min(kKeys, (from | page_mask) + 1);
+                uint8_t *v = ring + (size_t)st * C::kTile;
+                for (int x = 0; x < C::kHalves; ++x)
+                    for (int k = from * 8 + lane; k < to * 8; k += 32)
+                        *reinterpret_cast<uint4 *>(v + x * kHalfBytes + k * 16) =
+                            make_uint4(0, 0, 0, 0);
+                tc::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) tc::mbar_arrive(&kv_full[st]);
+            }
+            stage = (stage + n) % C::kStages;
+        }
+        if (!ok && lane == 0) atomicOr(a.err, kErrTimeout);
+    }
+    __syncwarp();
+    __syncthreads();
+    if (w == 8) tc::tmem_dealloc(tmem, 512);
+}
+
+template <int DP>
+cudaError_t go(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v,
+               int ctas, cudaStream_t st) {
+    static const cudaError_t set = cudaFuncSetAttribute(
+        prefill_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<DP>::kSmem);
+    if (set != cudaSuccess) return set;
+    prefill_kernel<DP><<<ctas, kThreads, Cfg<DP>::kSmem, st>>>(
+        q, k, v, a, prefill_box_rows(1 << a.page_shift));
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+int prefill_box_rows(int page_size) { return page_size < kKeys ? page_size : kKeys; }
+
+cudaError_t launch_prefill(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &k,
+                           const CUtensorMap &v, int ctas, cudaStream_t st) {
+    return a.D <= 64 ? go<64>(a, q, k, v, ctas, st) : go<128>(a, q, k, v, ctas, st);
+}
+
+}  // namespace paged
+}  // namespace um

@@ -145,3 +145,8 @@ def paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new:
         None if lse is None else lse.data_ptr(), ws.data_ptr(), nbytes, _b._stream()),
         "ultramem_paged_attention")
     return (out, lse) if with_lse else out
+
+
+def paged_check() -> int:
+    """Syncs the current stream and returns the attention kernels' status."""
+    return int(_b.load().ultramem_paged_check(_b._stream()))
