@@ -9,17 +9,23 @@
 // variance under the root).
 //
 // What bounds it: every entry of y and r is read once and every entry of u
-// and n written once, about 30 operations apart, so the bound is memory.
-// A row stays in registers between its two norms: a warp owns a row of up to
-// 1024 entries (no block barrier), a block a wider one.  Blocks are
-// persistent, so that the gains, biases and the per-channel gate are read
-// once per block, into registers.
+// and n written once, about 30 operations apart, so the bound is memory.  A
+// row lies in the registers of one warp (up to 256 entries), one block (up to
+// 4096) or a cluster of two blocks, 8 entries a thread, between its two norms.
+// The rows' sums are chains of barriers, so the bytes in flight must not
+// depend on them: each thread copies its own 16-byte pieces of the next rows
+// into shared memory (cp.async), three rows ahead (two in fp32 storage), and
+// waits for its own copies only.  Blocks are persistent, so that the gains,
+// biases and the per-channel gate are read once per block, into registers.
 #include "um_internal.cuh"
+#include "um_pair.cuh"
+#include "um_tc.cuh"
 
 namespace um {
 namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
+constexpr int kSumSlots = 32 * 3;   // warps of a row x values of a sum
 
 struct NormArgs {
     const void *y, *r, *gate;      // r: the residual (forward), u as stored (backward)
@@ -34,198 +40,331 @@ struct NormArgs {
 };
 
 // ---- a row in registers ------------------------------------------------
-// Thread t of the TPR threads of a row holds 8 NV entries.  With 16-byte
-// aligned rows (VEC) these are NV runs of 8 (run v: entries 8 (t + TPR v)..),
-// one or two 16-byte accesses each; otherwise single entries t + TPR e, so
-// that a warp's accesses are still consecutive.
-template <int NV, bool VEC, int TPR> struct Row {
-    static constexpr int kN = 8 * NV;
-    __device__ static __forceinline__ int col(int t, int e) {
-        return VEC ? 8 * (t + TPR * (e >> 3)) + (e & 7) : t + TPR * e;
+// Thread t of the NT CL threads of a row holds 8 entries as 4 pairs.  With
+// 16-byte aligned rows (VEC) these are one run, entries 8 t.., one or two
+// 16-byte accesses; otherwise single entries t + NT CL e, so that a warp's
+// accesses are still consecutive.
+constexpr int kP = 4;
+
+template <bool VEC, int TPR> __device__ __forceinline__ int col_of(int t, int e) {
+    return VEC ? 8 * t + e : t + TPR * e;
+}
+
+__device__ __forceinline__ void widen(F2 (&x)[kP], const uint4 *q, __nv_bfloat16) {
+    const uint32_t w[4] = {q[0].x, q[0].y, q[0].z, q[0].w};
+#pragma unroll
+    for (int i = 0; i < kP; ++i)
+        x[i] = f2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+}
+__device__ __forceinline__ void widen(F2 (&x)[kP], const uint4 *q, float) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        x[2 * i] = f2(__uint_as_float(q[i].x), __uint_as_float(q[i].y));
+        x[2 * i + 1] = f2(__uint_as_float(q[i].z), __uint_as_float(q[i].w));
     }
-    template <typename T>
-    __device__ static __forceinline__ void load(float (&x)[kN], const T *row, int t, int D) {
-        if constexpr (VEC) {
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int c = 8 * (t + TPR * v);
-                if constexpr (sizeof(T) == 2) {
-                    uint4 q = make_uint4(0, 0, 0, 0);
-                    if (c < D) q = *reinterpret_cast<const uint4 *>(row + c);
-                    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x[8 * v + 2 * i] = __uint_as_float(w[i] << 16);
-                        x[8 * v + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (c + 4 * i < D) q = *reinterpret_cast<const float4 *>(row + c + 4 * i);
-                        x[8 * v + 4 * i] = q.x;
-                        x[8 * v + 4 * i + 1] = q.y;
-                        x[8 * v + 4 * i + 2] = q.z;
-                        x[8 * v + 4 * i + 3] = q.w;
-                    }
-                }
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < kN; ++e) {
-                const int c = t + TPR * e;
-                x[e] = c < D ? to_f(row[c]) : 0.f;
-            }
-        }
+}
+
+// the pair as stored
+__device__ __forceinline__ uint32_t pack(F2 x) {
+    const float2 v = split(x);
+    const __nv_bfloat162 b = __floats2bfloat162_rn(v.x, v.y);
+    return *reinterpret_cast<const uint32_t *>(&b);
+}
+__device__ __forceinline__ F2 as_stored(F2 x, __nv_bfloat16) {
+    const uint32_t w = pack(x);
+    return f2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+__device__ __forceinline__ F2 as_stored(F2 x, float) { return x; }
+
+// A thread's way to the rows of up to MAXK tensors: the ring of its own
+// copies (VEC), or plain loads.
+template <typename T, bool VEC, int NT, int CL, int S, int MAXK> struct Feed {
+    static constexpr int kPieces = sizeof(T) / 2;            // 16-byte pieces of 8 entries
+    const T *base[MAXK];
+    int64_t ld[MAXK], first, step, T_rows;
+    int t, D;
+    uint4 *ring;                                             // [S][MAXK][kPieces] x threads
+
+    static constexpr size_t smem_bytes(int threads) {
+        return VEC ? sizeof(uint4) * S * MAXK * kPieces * threads : 0;
     }
-    template <typename T>
-    __device__ static __forceinline__ void store(T *row, const float (&x)[kN], int t, int D) {
+    __device__ __forceinline__ uint4 *at(int stage, int k, int i) const {
+        return ring + ((stage * MAXK + k) * kPieces + i) * blockDim.x + threadIdx.x;
+    }
+    // starts the copies of this thread's it-th row
+    __device__ __forceinline__ void issue(int stage, int64_t it) {
         if constexpr (VEC) {
+            const int64_t row = first + it * step;
+            if (row < T_rows && 8 * t < D) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int c = 8 * (t + TPR * v);
-                if constexpr (sizeof(T) == 2) {
-                    if (c < D) {
-                        uint32_t w[4];
+                for (int k = 0; k < MAXK; ++k)
+                    if (base[k])
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const __nv_bfloat162 b =
-                                __floats2bfloat162_rn(x[8 * v + 2 * i], x[8 * v + 2 * i + 1]);
-                            w[i] = *reinterpret_cast<const uint32_t *>(&b);
+                        for (int i = 0; i < kPieces; ++i) {
+                            // fp32 rows of 4 mod 8 entries end inside a run
+                            const int c = 8 * t + 16 / (int)sizeof(T) * i;
+                            const int bytes = c < D ? 16 : 0;
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                             (uint32_t)__cvta_generic_to_shared(at(stage, k, i))),
+                                         "l"(base[k] + row * ld[k] + (bytes ? c : 0)), "r"(bytes)
+                                         : "memory");
                         }
-                        *reinterpret_cast<uint4 *>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (c + 4 * i < D)
-                            *reinterpret_cast<float4 *>(row + c + 4 * i) =
-                                make_float4(x[8 * v + 4 * i], x[8 * v + 4 * i + 1],
-                                            x[8 * v + 4 * i + 2], x[8 * v + 4 * i + 3]);
-                }
             }
-        } else {
-#pragma unroll
-            for (int e = 0; e < kN; ++e) {
-                const int c = t + TPR * e;
-                if (c < D) row[c] = from_f<T>(x[e]);
-            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         }
     }
-    // a parameter vector, or `fill` everywhere without one
-    __device__ static __forceinline__ void param(float (&x)[kN], const float *p, float fill, int t,
-                                                 int D) {
+    __device__ __forceinline__ void wait() {
+        if constexpr (VEC) asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+    }
+    // the row's entries of tensor k (zeros past D and without a tensor)
+    __device__ __forceinline__ void take(F2 (&x)[kP], int k, int stage, int64_t row) {
+        if constexpr (VEC) {
+            if (base[k] && 8 * t < D) {
+                uint4 q[kPieces];
 #pragma unroll
-        for (int e = 0; e < kN; ++e) {
-            const int c = col(t, e);
-            x[e] = c < D ? (p ? p[c] : fill) : 0.f;
+                for (int i = 0; i < kPieces; ++i) q[i] = *at(stage, k, i);
+                widen(x, q, T());
+                return;
+            }
+#pragma unroll
+            for (int e = 0; e < kP; ++e) x[e] = f2(0.f);
+        } else {
+            float v[2 * kP];
+#pragma unroll
+            for (int e = 0; e < 2 * kP; ++e) {
+                const int c = t + NT * CL * e;
+                v[e] = base[k] && c < D ? to_f(base[k][row * ld[k] + c]) : 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < kP; ++e) x[e] = f2(v[2 * e], v[2 * e + 1]);
+        }
+    }
+    __device__ __forceinline__ void put(void *out, int64_t row, const F2 (&x)[kP]) const {
+        T *dst = static_cast<T *>(out) + row * D;
+        if constexpr (VEC && sizeof(T) == 2) {
+            if (8 * t < D)
+                *reinterpret_cast<uint4 *>(dst + 8 * t) =
+                    make_uint4(pack(x[0]), pack(x[1]), pack(x[2]), pack(x[3]));
+        } else if constexpr (VEC) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (8 * t + 4 * i < D) {
+                    const float2 lo = split(x[2 * i]), hi = split(x[2 * i + 1]);
+                    *reinterpret_cast<float4 *>(dst + 8 * t + 4 * i) =
+                        make_float4(lo.x, lo.y, hi.x, hi.y);
+                }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kP; ++e) {
+                const float2 v = split(x[e]);
+                const int c = t + NT * CL * 2 * e;
+                if (c < D) dst[c] = from_f<T>(v.x);
+                if (c + NT * CL < D) dst[c + NT * CL] = from_f<T>(v.y);
+            }
         }
     }
 };
 
-// Sums of K values over the TPR threads of a row, returned to all of them.
-// A block of several warps leaves its warps' sums in shared memory, in one
-// of two buffers in turn, so that one barrier serves each sum.
-template <int K, int TPR> struct RowSum {
-    float (*buf)[32 * 3];
+// a parameter vector, or `fill` everywhere without one; zeros past D
+template <bool VEC, int TPR>
+__device__ __forceinline__ void param(F2 (&x)[kP], const float *p, float fill, int t, int D) {
+    if constexpr (VEC) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (8 * t + 4 * i < D)
+                v = p ? *reinterpret_cast<const float4 *>(p + 8 * t + 4 * i)
+                      : make_float4(fill, fill, fill, fill);
+            x[2 * i] = f2(v.x, v.y);
+            x[2 * i + 1] = f2(v.z, v.w);
+        }
+    } else {
+        float v[2 * kP];
+#pragma unroll
+        for (int e = 0; e < 2 * kP; ++e) {
+            const int c = t + TPR * e;
+            v[e] = c < D ? (p ? p[c] : fill) : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < kP; ++e) x[e] = f2(v[2 * e], v[2 * e + 1]);
+    }
+}
+
+// clears the entries past D
+template <bool VEC, int TPR> __device__ __forceinline__ void clip(F2 (&x)[kP], int t, int D) {
+    if (col_of<VEC, TPR>(t, 7) < D) return;   // the thread's last entry is its largest column
+#pragma unroll
+    for (int e = 0; e < kP; ++e) {
+        const float2 v = split(x[e]);
+        x[e] = f2(col_of<VEC, TPR>(t, 2 * e) < D ? v.x : 0.f,
+                  col_of<VEC, TPR>(t, 2 * e + 1) < D ? v.y : 0.f);
+    }
+}
+
+// Sums of K values over the threads of a row, returned to all of them.  The
+// warps of a row leave their sums in shared memory (both blocks' of a
+// cluster), in one of two buffers in turn, so that one barrier serves a sum.
+template <int NT, int CL> struct RowSum {
+    float (*buf)[kSumSlots];
     int turn;
-    __device__ __forceinline__ void operator()(float (&v)[K]) {
+    template <int K> __device__ __forceinline__ void operator()(float (&v)[K]) {
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1)
 #pragma unroll
             for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(kFull, v[k], off);
-        if constexpr (TPR > 32) {
+        if constexpr (NT * CL > 32) {
+            constexpr int kWarps = NT * CL / 32;
             float *b = buf[turn];
             turn ^= 1;
             const int w = threadIdx.x >> 5;
-            if ((threadIdx.x & 31) == 0)
+            if constexpr (CL == 1) {
+                if ((threadIdx.x & 31) == 0)
 #pragma unroll
-                for (int k = 0; k < K; ++k) b[w * K + k] = v[k];
-            __syncthreads();
+                    for (int k = 0; k < K; ++k) b[k * kWarps + w] = v[k];
+                __syncthreads();
+            } else {
+                const uint32_t rank = tc::cluster_ctarank(), lane = threadIdx.x & 31;
+                if (lane < CL) {   // lane i writes to block i
+                    const uint32_t dst =
+                        tc::mapa_shared(tc::smem_u32(b + rank * (NT / 32) + w), lane);
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst + 4 * k * kWarps),
+                                     "f"(v[k])
+                                     : "memory");
+                }
+                tc::cluster_sync();
+            }
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                v[k] = 0.f;
+                if constexpr (kWarps % 4 == 0) {
+                    F2 s = f2(0.f);
+#pragma unroll 2   // more loads at once cost registers that wide rows do not have
+                    for (int i = 0; i < kWarps; i += 4) {
+                        const float4 x = *reinterpret_cast<const float4 *>(b + k * kWarps + i);
+                        s = s + (f2(x.x, x.y) + f2(x.z, x.w));
+                    }
+                    v[k] = both(s);
+                } else {
+                    v[k] = 0.f;
 #pragma unroll
-                for (int i = 0; i < TPR / 32; ++i) v[k] += b[i * K + k];
+                    for (int i = 0; i < kWarps; ++i) v[k] += b[k * kWarps + i];
+                }
             }
         }
     }
 };
 
-// x <- the normalised row (entries past D stay 0); the mean (0 for rms) is
+// x <- the normalised row (entries past D stay 0); the mean (layer) is
 // subtracted before the squares are summed, so nothing cancels
-template <int NV, bool VEC, int TPR, bool LAYER, typename Sum>
-__device__ __forceinline__ void normalise(float (&x)[8 * NV], const NormArgs &a, int t, Sum &sum) {
-    using R = Row<NV, VEC, TPR>;
+template <bool VEC, int NT, int CL, bool LAYER, typename Sum>
+__device__ __forceinline__ void normalise(F2 (&x)[kP], int D, float inv, float eps, int t,
+                                          Sum &sum) {
     float s[1];
     if constexpr (LAYER) {
-        s[0] = 0.f;
-#pragma unroll
-        for (int e = 0; e < R::kN; ++e) s[0] += x[e];
+        s[0] = both((x[0] + x[1]) + (x[2] + x[3]));
         sum(s);
-        const float mean = s[0] / (float)a.D;
+        const F2 mean = f2(-s[0] * inv);
 #pragma unroll
-        for (int e = 0; e < R::kN; ++e) x[e] = R::col(t, e) < a.D ? x[e] - mean : 0.f;
+        for (int e = 0; e < kP; ++e) x[e] = x[e] + mean;
+        clip<VEC, NT * CL>(x, t, D);
     }
-    s[0] = 0.f;
+    F2 q = x[0] * x[0];
 #pragma unroll
-    for (int e = 0; e < R::kN; ++e) s[0] = fmaf(x[e], x[e], s[0]);
+    for (int e = 1; e < kP; ++e) q = fma2(x[e], x[e], q);
+    s[0] = both(q);
     sum(s);
-    const float rstd = 1.f / sqrtf(s[0] / (float)a.D + a.eps);
+    const F2 rstd = f2(rsqrtf(fmaf(s[0], inv, eps)));
 #pragma unroll
-    for (int e = 0; e < R::kN; ++e) x[e] *= rstd;
+    for (int e = 0; e < kP; ++e) x[e] = x[e] * rstd;
 }
 
-// One row per TPR threads; block = max(TPR, 32 * warps), grid-stride rows.
-template <typename T, int NV, bool VEC, int TPR, bool LAYER>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) block_norm_kernel(NormArgs a) {
-    using R = Row<NV, VEC, TPR>;
-    constexpr int N = R::kN;
-    __shared__ float buf[2][32 * 3];
-    RowSum<1, TPR> sum{buf, 0};
-    const int t = TPR == 32 ? threadIdx.x & 31 : threadIdx.x;
-    const int64_t groups = TPR == 32 ? (int64_t)gridDim.x * (blockDim.x >> 5) : gridDim.x;
-    const int64_t first = TPR == 32 ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)
-                                    : blockIdx.x;
-    float wp[N], bp[N], wn[N], bn[N], gc[N];
-    R::param(wp, a.w_post, 1.f, t, a.D);
-    R::param(wn, a.w_pre, 1.f, t, a.D);
-    if constexpr (LAYER) {
-        R::param(bp, a.b_post, 0.f, t, a.D);
-        R::param(bn, a.b_pre, 0.f, t, a.D);
+template <typename T> constexpr int kAhead = sizeof(T) == 2 ? 3 : 2;   // rows in flight
+
+// What the first norm's gain and bias, the per-channel gate and the output's
+// scale make of a normalised row, as one factor and one offset a channel:
+// out_scale gate (.) (w x + b) = W x + B.  (x itself without the first norm.)
+template <bool VEC, int TPR, bool LAYER>
+__device__ __forceinline__ void fold_post(F2 (&W)[kP], F2 (&B)[kP], const NormArgs &a, int t) {
+    F2 g[kP];
+    const bool channel = a.gate_mode == ULTRAMEM_GATE_CHANNEL;
+    param<VEC, TPR>(g, channel ? static_cast<const float *>(a.gate) : nullptr, 1.f, t, a.D);
+    param<VEC, TPR>(W, a.post ? a.w_post : nullptr, 1.f, t, a.D);
+    if constexpr (LAYER) param<VEC, TPR>(B, a.post ? a.b_post : nullptr, 0.f, t, a.D);
+    const F2 s = f2(a.out_scale);
+#pragma unroll
+    for (int e = 0; e < kP; ++e) {
+        g[e] = g[e] * s;
+        W[e] = W[e] * g[e];
+        if constexpr (LAYER) B[e] = B[e] * g[e];
     }
-    R::param(gc, a.gate_mode == ULTRAMEM_GATE_CHANNEL ? static_cast<const float *>(a.gate) : nullptr,
-             1.f, t, a.D);
-    for (int64_t row = first; row < a.T; row += groups) {
-        float z[N], u[N];
-        R::load(z, static_cast<const T *>(a.y) + row * a.ld_y, t, a.D);
-        R::load(u, static_cast<const T *>(a.r) + row * a.ld_r, t, a.D);
-        float gt = a.out_scale;
-        float g[N];
-        if (a.gate_mode == ULTRAMEM_GATE_FULL)
-            R::load(g, static_cast<const T *>(a.gate) + row * a.D, t, a.D);
-        else if (a.gate_mode == ULTRAMEM_GATE_TOKEN)
-            gt *= to_f(static_cast<const T *>(a.gate)[row]);
-        if (a.post) {
-            normalise<NV, VEC, TPR, LAYER>(z, a, t, sum);
+}
+
+// A row per NT CL threads, grid-stride; rows of one warp go four to a block.
+template <typename T, bool VEC, int NT, int CL, bool LAYER>
+__global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArgs a) {
+    constexpr int TPR = NT * CL, S = kAhead<T>;
+    extern __shared__ uint4 ring[];
+    __shared__ __align__(16) float buf[2][kSumSlots];
+    RowSum<NT, CL> sum{buf, 0};
+    const int rank = CL > 1 ? (int)tc::cluster_ctarank() : 0;
+    const int t = NT == 32 ? (threadIdx.x & 31) : threadIdx.x + NT * rank;
+    const int rows = NT == 32 ? blockDim.x >> 5 : 1;
+    const bool full = a.gate_mode == ULTRAMEM_GATE_FULL;
+    const float inv = 1.f / (float)a.D;
+    Feed<T, VEC, NT, CL, S, 3> in;
+    in.base[0] = static_cast<const T *>(a.y);
+    in.base[1] = static_cast<const T *>(a.r);
+    in.base[2] = full ? static_cast<const T *>(a.gate) : nullptr;
+    in.ld[0] = a.ld_y;
+    in.ld[1] = a.ld_r;
+    in.ld[2] = a.D;
+    in.first = (int64_t)(blockIdx.x / CL) * rows + (NT == 32 ? threadIdx.x >> 5 : 0);
+    in.step = (int64_t)(gridDim.x / CL) * rows;
+    in.T_rows = a.T;
+    in.t = t;
+    in.D = a.D;
+    in.ring = ring;
 #pragma unroll
-            for (int e = 0; e < N; ++e) z[e] = LAYER ? fmaf(z[e], wp[e], bp[e]) : z[e] * wp[e];
+    for (int i = 0; i < S; ++i) in.issue(i, i);
+    F2 W[kP], B[kP], wn[kP], bn[kP];
+    fold_post<VEC, TPR, LAYER>(W, B, a, t);
+    param<VEC, TPR>(wn, a.w_pre, 1.f, t, a.D);
+    if constexpr (LAYER) param<VEC, TPR>(bn, a.b_pre, 0.f, t, a.D);
+    const F2 res = f2(a.res_scale);
+    int stage = 0;
+    int64_t it = 0;
+    for (int64_t row = in.first; row < a.T; row += in.step, ++it) {
+        F2 z[kP], u[kP], g[kP];
+        in.wait();
+        in.take(z, 0, stage, row);
+        in.take(u, 1, stage, row);
+        if (full) in.take(g, 2, stage, row);
+        in.issue(stage, it + S);
+        stage = stage + 1 == S ? 0 : stage + 1;
+        if (a.post) normalise<VEC, NT, CL, LAYER>(z, a.D, inv, a.eps, t, sum);
+#pragma unroll
+        for (int e = 0; e < kP; ++e) z[e] = LAYER ? fma2(z[e], W[e], B[e]) : z[e] * W[e];
+        if (full) {
+#pragma unroll
+            for (int e = 0; e < kP; ++e) z[e] = z[e] * g[e];
+        } else if (a.gate_mode == ULTRAMEM_GATE_TOKEN) {
+            const F2 gt = f2(to_f(static_cast<const T *>(a.gate)[row]));
+#pragma unroll
+            for (int e = 0; e < kP; ++e) z[e] = z[e] * gt;
         }
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            z[e] *= a.gate_mode == ULTRAMEM_GATE_FULL ? g[e] : gc[e];
-            u[e] = fmaf(gt, z[e], a.res_scale * u[e]);
-        }
-        R::store(static_cast<T *>(a.u) + row * a.D, u, t, a.D);
+        for (int e = 0; e < kP; ++e) u[e] = fma2(res, u[e], z[e]);
+        in.put(a.u, row, u);
         if (a.pre) {
             // The second norm reads the stream as stored, so that the
             // gradient taken from the stored stream is that of this function.
 #pragma unroll
-            for (int e = 0; e < N; ++e) u[e] = to_f(from_f<T>(u[e]));
-            normalise<NV, VEC, TPR, LAYER>(u, a, t, sum);
+            for (int e = 0; e < kP; ++e) u[e] = as_stored(u[e], T());
+            normalise<VEC, NT, CL, LAYER>(u, a.D, inv, a.eps, t, sum);
 #pragma unroll
-            for (int e = 0; e < N; ++e) u[e] = LAYER ? fmaf(u[e], wn[e], bn[e]) : u[e] * wn[e];
-            R::store(static_cast<T *>(a.n) + row * a.D, u, t, a.D);
+            for (int e = 0; e < kP; ++e) u[e] = LAYER ? fma2(u[e], wn[e], bn[e]) : u[e] * wn[e];
+            in.put(a.n, row, u);
         }
     }
 }
@@ -233,241 +372,355 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) block_norm_kernel(NormA
 // ---- the gradient ------------------------------------------------------
 // With û, ŷ the normalised rows and g = w (.) d for the gradient d of a
 // norm's output, the gradient of its input is
-//   rstd (g - mean(g) - û mean(g û))      (rms: without mean(g)),
-// d û summed over the rows is the gain's gradient and d the bias's.  One
-// pass over y, u, du and dn gives everything: the rows' statistics are taken
-// again from the rows themselves.  The column sums stay in registers over a
-// block's rows and leave as one partial row per block, which a second kernel
-// adds in the blocks' order (no atomics: the result does not depend on the
-// schedule).
-enum { kColWPost, kColWPre, kColGate, kColBPost, kColBPre };   // order of the partial rows
+//   rstd (g - mean(g) - û mean(g û))      (rms: without mean(g)).
+// One pass over y, u, du and dn gives everything: the rows' statistics are
+// taken again from the rows themselves.  With gv the gradient gu of the
+// stream times a token's or entry's gate, two column sums serve the first
+// norm and a per-channel gate together,
+//   P = sum gv ŷ,  Q = sum gv:   dw_post = out_scale gate P,
+//   db_post = out_scale gate Q,  dgate = out_scale (w_post P + b_post Q),
+// and sum dn û, sum dn are those of the second norm.  They stay in registers
+// over a block's rows and leave as one partial row per block, which a second
+// kernel adds in the blocks' order (no atomics: the result does not depend on
+// the schedule).
+enum { kColP, kColPre, kColQ, kColBPre };   // order of the partial rows (the last two: layer)
 
-template <typename T, int NV, bool VEC, int TPR, bool LAYER>
-__global__ void __launch_bounds__(TPR) block_norm_backward_kernel(NormArgs a) {
-    using R = Row<NV, VEC, TPR>;
-    constexpr int N = R::kN;
-    __shared__ float buf[2][32 * 3];
-    RowSum<3, TPR> sum{buf, 0};
-    const int t = threadIdx.x;
-    float wp[N], bp[N], wn[N], gc[N];
-    float c_wp[N], c_wn[N], c_g[N], c_bp[N], c_bn[N];
-    R::param(wp, a.w_post, 1.f, t, a.D);
-    R::param(wn, a.w_pre, 1.f, t, a.D);
-    if constexpr (LAYER) R::param(bp, a.b_post, 0.f, t, a.D);
-    const bool channel = a.gate_mode == ULTRAMEM_GATE_CHANNEL;
-    R::param(gc, channel ? static_cast<const float *>(a.gate) : nullptr, 1.f, t, a.D);
-#pragma unroll
-    for (int e = 0; e < N; ++e) c_wp[e] = c_wn[e] = c_g[e] = c_bp[e] = c_bn[e] = 0.f;
+template <typename T, bool VEC, int NT, int CL, bool LAYER>
+__global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
+    block_norm_backward_kernel(NormArgs a) {
+    constexpr int TPR = NT * CL, S = kAhead<T>;
+    extern __shared__ uint4 ring[];
+    __shared__ __align__(16) float buf[2][kSumSlots];
+    RowSum<NT, CL> sum{buf, 0};
+    const int t = threadIdx.x + (CL > 1 ? NT * (int)tc::cluster_ctarank() : 0);
+    const bool full = a.gate_mode == ULTRAMEM_GATE_FULL;
+    const bool token = a.gate_mode == ULTRAMEM_GATE_TOKEN;
     const float inv = 1.f / (float)a.D;
+    Feed<T, VEC, NT, CL, S, 5> in;
+    in.base[0] = static_cast<const T *>(a.y);
+    in.base[1] = a.pre ? static_cast<const T *>(a.r) : nullptr;
+    in.base[2] = a.pre ? static_cast<const T *>(a.dn) : nullptr;
+    in.base[3] = static_cast<const T *>(a.du);
+    in.base[4] = full ? static_cast<const T *>(a.gate) : nullptr;
+    in.ld[0] = a.ld_y;
+    in.ld[1] = a.ld_r;
+    in.ld[2] = a.ld_dn;
+    in.ld[3] = a.ld_du;
+    in.ld[4] = a.D;
+    in.first = blockIdx.x / CL;
+    in.step = gridDim.x / CL;
+    in.T_rows = a.T;
+    in.t = t;
+    in.D = a.D;
+    in.ring = ring;
+#pragma unroll
+    for (int i = 0; i < S; ++i) in.issue(i, i);
+    F2 W[kP], B[kP], wn[kP];
+    F2 c_p[kP], c_pre[kP], c_q[kP], c_bpre[kP];
+    fold_post<VEC, TPR, LAYER>(W, B, a, t);
+    param<VEC, TPR>(wn, a.w_pre, 1.f, t, a.D);
+#pragma unroll
+    for (int e = 0; e < kP; ++e) c_p[e] = c_pre[e] = c_q[e] = c_bpre[e] = f2(0.f);
+    const F2 res = f2(a.res_scale);
 
-    for (int64_t row = blockIdx.x; row < a.T; row += gridDim.x) {
-        float y[N], u[N], gu[N], dn[N], g[N];
-        R::load(y, static_cast<const T *>(a.y) + row * a.ld_y, t, a.D);
-        if (a.pre) {
-            R::load(u, static_cast<const T *>(a.r) + row * a.ld_r, t, a.D);
-            R::load(dn, static_cast<const T *>(a.dn) + row * a.ld_dn, t, a.D);
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) u[e] = dn[e] = 0.f;
-        }
-        if (a.du)
-            R::load(gu, static_cast<const T *>(a.du) + row * a.ld_du, t, a.D);
-        else
-#pragma unroll
-            for (int e = 0; e < N; ++e) gu[e] = 0.f;
-        float gt = a.out_scale;
-        if (a.gate_mode == ULTRAMEM_GATE_FULL)
-            R::load(g, static_cast<const T *>(a.gate) + row * a.D, t, a.D);
-        else if (a.gate_mode == ULTRAMEM_GATE_TOKEN)
-            gt *= to_f(static_cast<const T *>(a.gate)[row]);
+    int stage = 0;
+    int64_t it = 0;
+    for (int64_t row = in.first; row < a.T; row += in.step, ++it) {
+        F2 y[kP], u[kP], gu[kP], dn[kP], g[kP];
+        in.wait();
+        in.take(y, 0, stage, row);
+        in.take(u, 1, stage, row);
+        in.take(dn, 2, stage, row);
+        in.take(gu, 3, stage, row);
+        if (full) in.take(g, 4, stage, row);
+        in.issue(stage, it + S);
+        stage = stage + 1 == S ? 0 : stage + 1;
+        const float gt = token ? to_f(static_cast<const T *>(a.gate)[row]) : 1.f;
 
         // statistics of y and u, and the sums of the second norm's gradient
         float s[3], mean_g = 0.f;
         if constexpr (LAYER) {
-            s[0] = s[1] = s[2] = 0.f;
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                s[0] += y[e];
-                s[1] += u[e];
-                s[2] = fmaf(wn[e], dn[e], s[2]);
-            }
+            for (int e = 0; e < kP; ++e) c_bpre[e] = c_bpre[e] + dn[e];
+        }
+        F2 wd[kP];
+#pragma unroll
+        for (int e = 0; e < kP; ++e) wd[e] = wn[e] * dn[e];
+        if constexpr (LAYER) {
+            s[0] = both((y[0] + y[1]) + (y[2] + y[3]));
+            s[1] = both((u[0] + u[1]) + (u[2] + u[3]));
+            s[2] = both((wd[0] + wd[1]) + (wd[2] + wd[3]));
             sum(s);
-            const float my = a.post ? s[0] * inv : 0.f, mu = s[1] * inv;
+            const F2 my = f2(a.post ? -s[0] * inv : 0.f), mu = f2(-s[1] * inv);
             mean_g = s[2] * inv;
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const bool in = R::col(t, e) < a.D;
-                y[e] = in ? y[e] - my : 0.f;
-                u[e] = in ? u[e] - mu : 0.f;
+            for (int e = 0; e < kP; ++e) {
+                y[e] = y[e] + my;
+                u[e] = u[e] + mu;
             }
+            clip<VEC, TPR>(y, t, a.D);
+            clip<VEC, TPR>(u, t, a.D);
         }
-        s[0] = s[1] = s[2] = 0.f;
+        {
+            F2 q0 = y[0] * y[0], q1 = u[0] * u[0], q2 = wd[0] * u[0];
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            s[0] = fmaf(y[e], y[e], s[0]);
-            s[1] = fmaf(u[e], u[e], s[1]);
-            s[2] = fmaf(wn[e] * dn[e], u[e], s[2]);
+            for (int e = 1; e < kP; ++e) {
+                q0 = fma2(y[e], y[e], q0);
+                q1 = fma2(u[e], u[e], q1);
+                q2 = fma2(wd[e], u[e], q2);
+            }
+            s[0] = both(q0);
+            s[1] = both(q1);
+            s[2] = both(q2);
         }
         sum(s);
-        const float ry = a.post ? 1.f / sqrtf(s[0] * inv + a.eps) : 1.f;
-        const float ru = a.pre ? 1.f / sqrtf(s[1] * inv + a.eps) : 0.f;
-        const float mean_gu = s[2] * ru * inv;
+        const float ry = a.post ? rsqrtf(fmaf(s[0], inv, a.eps)) : 1.f;
+        const float ru = a.pre ? rsqrtf(fmaf(s[1], inv, a.eps)) : 0.f;
+        const F2 ry2 = f2(ry), ru2 = f2(ru), m_gu = f2(-s[2] * ru * inv), m_g = f2(-mean_g);
+        F2 gy[kP];
+        F2 q0 = f2(0.f), q1 = f2(0.f), q2 = f2(0.f);
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float uh = u[e] * ru;
-            gu[e] = fmaf(ru, fmaf(wn[e], dn[e], -fmaf(uh, mean_gu, mean_g)), gu[e]);
-            c_wn[e] = fmaf(dn[e], uh, c_wn[e]);
-            if constexpr (LAYER) c_bn[e] += dn[e];
-            y[e] *= ry;   // from here the normalised row
-            u[e] = a.res_scale * gu[e];
+        for (int e = 0; e < kP; ++e) {
+            const F2 uh = u[e] * ru2;
+            c_pre[e] = fma2(dn[e], uh, c_pre[e]);
+            F2 d = fma2(uh, m_gu, wd[e]);
+            if constexpr (LAYER) d = d + m_g;
+            gu[e] = fma2(ru2, d, gu[e]);
+            y[e] = y[e] * ry2;                 // from here the normalised row
+            u[e] = res * gu[e];
         }
-        if (a.dr) R::store(static_cast<T *>(a.dr) + row * a.D, u, t, a.D);
-
-        // through the gate: d gate = out_scale z gu, d z = out_scale gate gu
-        s[0] = s[1] = s[2] = 0.f;
+        if constexpr (LAYER) clip<VEC, TPR>(gu, t, a.D);
+        if (a.dr) in.put(a.dr, row, u);
+        if (full || token) {
+            // through a gate of the row: its gradient out_scale z gu, and gv
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float z = LAYER ? fmaf(y[e], wp[e], bp[e]) : y[e] * wp[e];
-            const float zg = (a.post ? z : y[e]) * gu[e];
-            if (channel) c_g[e] = fmaf(a.out_scale, zg, c_g[e]);
-            s[2] += zg;
-            u[e] = a.out_scale * zg;
-            gu[e] *= gt * (a.gate_mode == ULTRAMEM_GATE_FULL ? g[e] : gc[e]);
-            if (a.post) {
-                c_wp[e] = fmaf(gu[e], y[e], c_wp[e]);
-                if constexpr (LAYER) c_bp[e] += R::col(t, e) < a.D ? gu[e] : 0.f;
-                gu[e] *= wp[e];
-                if constexpr (LAYER) s[0] += R::col(t, e) < a.D ? gu[e] : 0.f;
-                s[1] = fmaf(gu[e], y[e], s[1]);
+            for (int e = 0; e < kP; ++e) {
+                u[e] = (LAYER ? fma2(W[e], y[e], B[e]) : W[e] * y[e]) * gu[e];
+                q2 = q2 + u[e];
+                gu[e] = gu[e] * (full ? g[e] : f2(gt));
             }
+            if (full && a.dgate_rows) in.put(a.dgate_rows, row, u);
         }
-        if (a.gate_mode == ULTRAMEM_GATE_FULL && a.dgate_rows)
-            R::store(static_cast<T *>(a.dgate_rows) + row * a.D, u, t, a.D);
-        sum(s);
-        if (a.gate_mode == ULTRAMEM_GATE_TOKEN && a.dgate_rows && t == 0)
-            static_cast<T *>(a.dgate_rows)[row] = from_f<T>(a.out_scale * s[2]);
-        if (a.post) {
-            const float m0 = s[0] * inv, m1 = s[1] * inv;
 #pragma unroll
-            for (int e = 0; e < N; ++e) gu[e] = ry * (gu[e] - fmaf(y[e], m1, m0));
+        for (int e = 0; e < kP; ++e) {
+            c_p[e] = fma2(gu[e], y[e], c_p[e]);
+            if constexpr (LAYER) c_q[e] = c_q[e] + gu[e];
+            gy[e] = W[e] * gu[e];
+            if constexpr (LAYER) q0 = q0 + gy[e];
+            q1 = fma2(gy[e], y[e], q1);
         }
-        if (a.dy) R::store(static_cast<T *>(a.dy) + row * a.D, gu, t, a.D);
+        float s2[LAYER ? 3 : 2];
+        s2[0] = both(q1);
+        s2[1] = both(q2);
+        if constexpr (LAYER) s2[2] = both(q0);
+        sum(s2);
+        if (token && a.dgate_rows && t == 0)
+            static_cast<T *>(a.dgate_rows)[row] = from_f<T>(s2[1]);
+        const F2 m1 = f2(a.post ? -s2[0] * inv : 0.f);
+        F2 m0 = f2(0.f);
+        if constexpr (LAYER) m0 = f2(a.post ? -s2[2] * inv : 0.f);
+#pragma unroll
+        for (int e = 0; e < kP; ++e) {
+            F2 d = fma2(y[e], m1, gy[e]);
+            if constexpr (LAYER) d = d + m0;
+            gy[e] = ry2 * d;
+        }
+        if (a.dy) in.put(a.dy, row, gy);
     }
 
-    const int n_cols = LAYER ? 5 : 3;
-    float *part = a.part + (int64_t)blockIdx.x * n_cols * a.D;
+    pdl_trigger();
+    float *part = a.part + (int64_t)(blockIdx.x / CL) * (LAYER ? 4 : 2) * a.D;
+    auto leave = [&](int k, const F2 (&c)[kP]) {
+        float *dst = part + (int64_t)k * a.D;
+        if constexpr (VEC) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const int c = R::col(t, e);
-        if (c >= a.D) continue;
-        part[kColWPost * a.D + c] = c_wp[e];
-        part[kColWPre * a.D + c] = c_wn[e];
-        part[kColGate * a.D + c] = c_g[e];
-        if constexpr (LAYER) {
-            part[kColBPost * a.D + c] = c_bp[e];
-            part[kColBPre * a.D + c] = c_bn[e];
+            for (int i = 0; i < 2; ++i)
+                if (8 * t + 4 * i < a.D) {
+                    const float2 lo = split(c[2 * i]), hi = split(c[2 * i + 1]);
+                    *reinterpret_cast<float4 *>(dst + 8 * t + 4 * i) =
+                        make_float4(lo.x, lo.y, hi.x, hi.y);
+                }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kP; ++e) {
+                const float2 v = split(c[e]);
+                const int at = t + TPR * 2 * e;
+                if (at < a.D) dst[at] = v.x;
+                if (at + TPR < a.D) dst[at + TPR] = v.y;
+            }
         }
+    };
+    leave(kColP, c_p);
+    leave(kColPre, c_pre);
+    if constexpr (LAYER) {
+        leave(kColQ, c_q);
+        leave(kColBPre, c_bpre);
     }
 }
 
 struct ColOut {
-    float *out[5];
+    float *dw_post, *db_post, *dgate, *dw_pre, *db_pre;   // null: not wanted
+    const float *w_post, *b_post, *gate;                  // null: ones, zeros, ones
+    float out_scale;
 };
 
-// out[k][c] = sum over the blocks of part[b][k][c]: 32 columns a block, 8
-// warps over the partial rows.
-__global__ void __launch_bounds__(256) column_sum_kernel(const float *part, int blocks, int n_cols,
-                                                         int D, ColOut o) {
-    __shared__ float s[8][33];
-    const int k = blockIdx.y;
-    if (!o.out[k]) return;
+// The column sums over the blocks' partial rows, 32 columns a block, 32 warps
+// over the rows; blockIdx.y 0: the first norm's and the gate's, 1: the second's.
+__global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int blocks,
+                                                          int layer, int D, ColOut o) {
+    __shared__ float s[2][32][33];
+    const int n_cols = layer ? 4 : 2, which = blockIdx.y;
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-    float v = 0.f;
-    if (c < D)
-        for (int b = w; b < blocks; b += 8) v += part[((int64_t)b * n_cols + k) * D + c];
-    s[w][lane] = v;
-    __syncthreads();
-    if (w == 0 && c < D) {
-#pragma unroll
-        for (int i = 1; i < 8; ++i) v += s[i][lane];
-        o.out[k][c] = v;
+    pdl_wait();
+    float v = 0.f, q = 0.f;
+    if (c < D) {
+#pragma unroll 4
+        for (int b = w; b < blocks; b += 32) {
+            const float *row = part + ((int64_t)b * n_cols + which) * D + c;
+            v += row[0];
+            if (layer) q += row[2 * (int64_t)D];
+        }
     }
+    s[0][w][lane] = v;
+    s[1][w][lane] = q;
+    __syncthreads();
+    if (w != 0 || c >= D) return;
+#pragma unroll
+    for (int i = 1; i < 32; ++i) {
+        v += s[0][i][lane];
+        q += s[1][i][lane];
+    }
+    if (which == 1) {
+        if (o.dw_pre) o.dw_pre[c] = v;
+        if (o.db_pre) o.db_pre[c] = q;
+        return;
+    }
+    const float g = o.out_scale * (o.gate ? o.gate[c] : 1.f);
+    if (o.dw_post) o.dw_post[c] = g * v;
+    if (o.db_post) o.db_post[c] = g * q;
+    if (o.dgate)
+        o.dgate[c] = o.out_scale *
+                     fmaf(o.w_post ? o.w_post[c] : 1.f, v, (o.b_post ? o.b_post[c] : 0.f) * q);
 }
 
 // ---- launches ----------------------------------------------------------
 
 constexpr int kMaxDim = 8192;
 
-template <typename T, bool VEC, bool LAYER> struct Forward {
-    template <int NV, int TPR> static cudaError_t go(const NormArgs &a, cudaStream_t st) {
-        // up to 2048 threads an SM; few rows spread over the SMs first
-        const int sms = device_sm_count();
-        int rows = TPR == 32 ? 4 : 1;
-        if (TPR == 32 && a.T < 4 * (int64_t)sms) rows = 1;
-        const int threads = rows * TPR;
-        const int64_t want = (a.T + rows - 1) / rows, most = (int64_t)sms * (2048 / (TPR < 128 ? 128 : TPR));
-        const unsigned grid = (unsigned)(want < most ? want : most);
-        block_norm_kernel<T, NV, VEC, TPR, LAYER><<<grid, threads, 0, st>>>(a);
-        return cudaGetLastError();
-    }
-    static cudaError_t launch(const NormArgs &a, cudaStream_t st) {
-        const int v = (a.D + 7) / 8;
-        if (v <= 32) return go<1, 32>(a, st);
-        if (v <= 64) return go<2, 32>(a, st);
-        if (v <= 128) return go<1, 128>(a, st);
-        if (v <= 256) return go<1, 256>(a, st);
-        if (v <= 512) return go<1, 512>(a, st);
-        return go<1, 1024>(a, st);
-    }
-};
-
-int backward_tpr(int D) {
+// Threads of a row: 8 entries each, a power of two from a warp up.
+int row_threads(int D) {
     const int v = (D + 7) / 8;
     int t = 32;
-    while (t < v && t < 1024) t *= 2;
+    while (t < v) t *= 2;
     return t;
 }
 
-// Blocks of the gradient's first kernel: as many as fit at about 96
-// registers a thread, and no more than 8 an SM (each leaves a partial row).
-int backward_blocks(int64_t T, int D) {
-    const int tpr = backward_tpr(D);
-    int per_sm = 640 / tpr;
-    per_sm = per_sm < 1 ? 1 : per_sm > 8 ? 8 : per_sm;
-    const int64_t most = (int64_t)device_sm_count() * per_sm;
-    return (int)(T < most ? T : most);
+// Dynamic shared memory and grid of a persistent kernel: as many blocks as
+// the SMs hold, asked of the driver once per kernel.
+template <auto K> int resident_blocks(int threads, size_t smem) {
+    static const int n = [&] {
+        int b = 0;
+        if (cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
+                cudaSuccess ||
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&b, K, threads, smem) != cudaSuccess) {
+            cudaGetLastError();
+            return 0;
+        }
+        return b;
+    }();
+    return n;
 }
 
-template <typename T, bool VEC, bool LAYER> struct Backward {
-    template <int NV, int TPR> static cudaError_t go(const NormArgs &a, cudaStream_t st) {
-        block_norm_backward_kernel<T, NV, VEC, TPR, LAYER>
-            <<<backward_blocks(a.T, a.D), TPR, 0, st>>>(a);
-        return cudaGetLastError();
+template <auto K> cudaError_t run_rows(const NormArgs &a, int64_t units, int threads, int cl,
+                                       size_t smem, int64_t most, int *groups, cudaStream_t st) {
+    const int fit = resident_blocks<K>(threads, smem);
+    if (fit < 1) return cudaErrorInvalidConfiguration;
+    int64_t grid = (int64_t)device_sm_count() * fit / cl;   // clusters (or blocks)
+    grid = grid < most ? grid : most;
+    grid = grid < units ? grid : units;
+    grid = grid < 1 ? 1 : grid;
+    *groups = (int)grid;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(grid * cl));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = cl;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = cl > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, K, a);
+}
+
+template <typename T, bool VEC, bool LAYER> struct Forward {
+    template <int NT, int CL> static cudaError_t go(const NormArgs &a, int *groups, cudaStream_t st) {
+        constexpr int threads = NT == 32 ? 128 : NT;
+        constexpr size_t smem = Feed<T, VEC, NT, CL, kAhead<T>, 3>::smem_bytes(threads);
+        const int64_t units = NT == 32 ? (a.T + 3) / 4 : a.T;
+        return run_rows<block_norm_kernel<T, VEC, NT, CL, LAYER>>(a, units, threads, CL, smem,
+                                                                  INT64_MAX, groups, st);
     }
-    static cudaError_t launch(const NormArgs &a, cudaStream_t st) {
-        switch (backward_tpr(a.D)) {
-        case 32: return go<1, 32>(a, st);
-        case 64: return go<1, 64>(a, st);
-        case 128: return go<1, 128>(a, st);
-        case 256: return go<1, 256>(a, st);
-        case 512: return go<1, 512>(a, st);
-        default: return go<1, 1024>(a, st);
+    static cudaError_t launch(const NormArgs &a, int *groups, cudaStream_t st) {
+        switch (row_threads(a.D)) {
+        case 32: return go<32, 1>(a, groups, st);
+        case 64: return go<64, 1>(a, groups, st);
+        case 128: return go<128, 1>(a, groups, st);
+        case 256: return go<256, 1>(a, groups, st);
+        case 512: return go<512, 1>(a, groups, st);
+        default: return go<512, 2>(a, groups, st);
         }
     }
 };
 
+// Partial rows of the gradient's column sums, one per block (or cluster): as
+// many as the SMs hold at 128 registers a thread (64 at rows of one warp, so
+// that the second kernel's sums stay short), and no more than rows.
+int64_t partial_rows(int64_t T, int D) {
+    const int threads = row_threads(D);
+    int per_sm2 = threads > 512 ? 1 : 2 * (512 / threads);   // per two SMs
+    if (per_sm2 > 16) per_sm2 = 16;
+    const int64_t sms = device_sm_count(), most = sms * per_sm2 / 2;
+    int64_t n = (T + 3) / 4;   // a partial row is written and read again: 4 rows of work at least
+    if (n < sms) n = T < sms ? T : sms;
+    return n < most ? n : most;
+}
+
+template <typename T, bool VEC, bool LAYER> struct Backward {
+    template <int NT, int CL> static cudaError_t go(const NormArgs &a, int *groups, cudaStream_t st) {
+        constexpr size_t smem = Feed<T, VEC, NT, CL, kAhead<T>, 5>::smem_bytes(NT);
+        return run_rows<block_norm_backward_kernel<T, VEC, NT, CL, LAYER>>(
+            a, a.T, NT, CL, smem, partial_rows(a.T, a.D), groups, st);
+    }
+    static cudaError_t launch(const NormArgs &a, int *groups, cudaStream_t st) {
+        switch (row_threads(a.D)) {
+        case 32: return go<32, 1>(a, groups, st);
+        case 64: return go<64, 1>(a, groups, st);
+        case 128: return go<128, 1>(a, groups, st);
+        case 256: return go<256, 1>(a, groups, st);
+        case 512: return go<512, 1>(a, groups, st);
+        default: return go<512, 2>(a, groups, st);
+        }
+    }
+};
+
+// groups: the blocks (or clusters) launched
 template <template <typename, bool, bool> class Op>
-cudaError_t dispatch(const NormArgs &a, int dtype, bool layer, bool vec, cudaStream_t st) {
+cudaError_t dispatch(const NormArgs &a, int dtype, bool layer, bool vec, int *groups,
+                     cudaStream_t st) {
     if (dtype == ULTRAMEM_BF16) {
         if (vec)
-            return layer ? Op<__nv_bfloat16, true, true>::launch(a, st)
-                         : Op<__nv_bfloat16, true, false>::launch(a, st);
-        return layer ? Op<__nv_bfloat16, false, true>::launch(a, st)
-                     : Op<__nv_bfloat16, false, false>::launch(a, st);
+            return layer ? Op<__nv_bfloat16, true, true>::launch(a, groups, st)
+                         : Op<__nv_bfloat16, true, false>::launch(a, groups, st);
+        return layer ? Op<__nv_bfloat16, false, true>::launch(a, groups, st)
+                     : Op<__nv_bfloat16, false, false>::launch(a, groups, st);
     }
     if (vec)
-        return layer ? Op<float, true, true>::launch(a, st) : Op<float, true, false>::launch(a, st);
-    return layer ? Op<float, false, true>::launch(a, st) : Op<float, false, false>::launch(a, st);
+        return layer ? Op<float, true, true>::launch(a, groups, st)
+                     : Op<float, true, false>::launch(a, groups, st);
+    return layer ? Op<float, false, true>::launch(a, groups, st)
+                 : Op<float, false, false>::launch(a, groups, st);
 }
 
 bool valid(const ultramem_block_norm_args *p) {
@@ -533,17 +786,19 @@ extern "C" ultramem_status ultramem_block_norm(const ultramem_block_norm_args *p
     a.r = r;
     a.u = u;
     a.n = n;
-    const void *gate_rows = p->gate_mode == ULTRAMEM_GATE_FULL ? p->gate : nullptr;
-    const bool vec = um::rows_aligned(p->dtype, p->dim, {p->y, r, u, n, gate_rows},
+    const void *channel_or_full = p->gate_mode == ULTRAMEM_GATE_TOKEN ? nullptr : p->gate;
+    const bool vec = um::rows_aligned(p->dtype, p->dim, {p->y, r, u, n, p->w_post, p->b_post, p->w_pre, p->b_pre,
+                                       channel_or_full},
                                       {p->ld_y, p->ld_r});
     cudaGetLastError();
+    int groups = 0;
     return um::status_from_cuda(um::dispatch<um::Forward>(
-        a, p->dtype, p->kind == ULTRAMEM_NORM_LAYER, vec, (cudaStream_t)stream));
+        a, p->dtype, p->kind == ULTRAMEM_NORM_LAYER, vec, &groups, (cudaStream_t)stream));
 }
 
 extern "C" int64_t ultramem_block_norm_backward_workspace(int64_t n_tokens, int32_t dim) {
     if (n_tokens < 0 || dim < 1 || dim > um::kMaxDim) return 0;
-    return (int64_t)um::backward_blocks(n_tokens, dim) * 5 * dim * (int64_t)sizeof(float);
+    return um::partial_rows(n_tokens, dim) * 4 * dim * (int64_t)sizeof(float);
 }
 
 extern "C" ultramem_status ultramem_block_norm_backward(
@@ -558,10 +813,15 @@ extern "C" ultramem_status ultramem_block_norm_backward(
     const int D = p->dim;
     cudaStream_t st = (cudaStream_t)stream;
     float *channel_gate = p->gate_mode == ULTRAMEM_GATE_CHANNEL ? static_cast<float *>(dgate) : nullptr;
-    um::ColOut cols = {{dw_post, dw_pre, channel_gate, db_post, db_pre}};
+    const um::ColOut cols = {dw_post, db_post, channel_gate, dw_pre, db_pre,
+                             p->post ? p->w_post : nullptr, p->post ? p->b_post : nullptr,
+                             p->gate_mode == ULTRAMEM_GATE_CHANNEL ? static_cast<const float *>(p->gate)
+                                                                   : nullptr,
+                             p->out_scale};
+    float *const sums[5] = {dw_post, db_post, channel_gate, dw_pre, db_pre};
     cudaGetLastError();
     if (p->n_tokens == 0) {   // empty sums
-        for (float *o : cols.out)
+        for (float *o : sums)
             if (o) {
                 cudaError_t e = cudaMemsetAsync(o, 0, sizeof(float) * D, st);
                 if (e != cudaSuccess) return um::status_from_cuda(e);
@@ -585,18 +845,18 @@ extern "C" ultramem_status ultramem_block_norm_backward(
     const bool full = p->gate_mode == ULTRAMEM_GATE_FULL;
     const bool vec = um::rows_aligned(
         p->dtype, D,
-        {p->y, p->pre ? u : nullptr, du, dn, dy, dr, full ? p->gate : nullptr, full ? dgate : nullptr},
+        {p->y, p->pre ? u : nullptr, du, dn, dy, dr, p->w_post, p->b_post, p->w_pre, p->b_pre,
+         p->gate_mode == ULTRAMEM_GATE_TOKEN ? nullptr : p->gate, full ? dgate : nullptr},
         {p->ld_y, p->pre ? p->ld_r : 0, du ? ld_du : 0, dn ? ld_dn : 0});
     const bool layer = p->kind == ULTRAMEM_NORM_LAYER;
-    cudaError_t e = um::dispatch<um::Backward>(a, p->dtype, layer, vec, st);
+    int groups = 0;
+    cudaError_t e = um::dispatch<um::Backward>(a, p->dtype, layer, vec, &groups, st);
     if (e != cudaSuccess) return um::status_from_cuda(e);
     bool any = false;
-    for (float *o : cols.out) any = any || o;
+    for (float *o : sums) any = any || o;
     if (any) {
-        const int n_cols = layer ? 5 : 3;
-        um::column_sum_kernel<<<dim3((D + 31) / 32, n_cols), 256, 0, st>>>(
-            a.part, um::backward_blocks(p->n_tokens, D), n_cols, D, cols);
-        e = cudaGetLastError();
+        e = um::launch_kernel(true, um::column_sum_kernel, dim3((D + 31) / 32, 2), 1024, 0, st,
+                              (const float *)a.part, groups, layer ? 1 : 0, D, cols);
     }
     return um::status_from_cuda(e);
 }

@@ -345,16 +345,25 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
 }
 
 // ---- join of split tiles ----------------------------------------------------
-// Block (c, y) joins rows 8 y.. of the tile that begins in share c and ends in
-// a later one: weights 2^(m_i - max m) over the shares' partials, in share
-// order, so the result does not depend on which share finished first.
-template <typename T, int DP>
+// Block (c, y) joins rows of the tile that begins in share c and ends in a
+// later one: weights 2^(m_i - max m) over the shares' partials, added in a
+// fixed order, so the result does not depend on which share finished first.
+// A long axis with few rows leaves many partials of few rows (one request of
+// 131072 keys: 76 of 4): there the 8 warps of a block share one row's
+// partials (WPR = 8); chunks leave two or three of up to 256 rows: a warp a
+// row (WPR = 1).  One warp a row at 76 partials took 82 us, eight take 6.
+template <typename T, int DP, int WPR>
 __global__ void __launch_bounds__(256) combine_kernel(AttnArgs a, int ctas) {
+    constexpr int kRowsOfBlock = 8 / WPR, kC = DP / 32;
+    extern __shared__ float weight[];        // [kRowsOfBlock][ctas]
+    __shared__ float2 total[kRowsOfBlock];   // maximum, sum
+    __shared__ float part[WPR == 1 ? 1 : WPR][WPR == 1 ? 1 : DP];
+    __shared__ int last;
     pdl_wait();
     const int c = blockIdx.x, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    __shared__ int last;
     int slot = -1;
-    int4 d;
+    int4 d = make_int4(0, 0, 0, 0);
+#pragma unroll
     for (int s = 0; s < 2; ++s) {
         const int4 e = a.part_desc[2 * c + s];
         if (e.x == kPartFirst) {
@@ -362,7 +371,8 @@ __global__ void __launch_bounds__(256) combine_kernel(AttnArgs a, int ctas) {
             d = e;
         }
     }
-    if (slot < 0) return;   // the same in the whole block
+    const int row0 = blockIdx.y * kRowsOfBlock;
+    if (slot < 0 || row0 >= d.z * a.group) return;   // the same in the whole block
     if (threadIdx.x == 0) last = ctas - 1;
     __syncthreads();
     for (int i = c + 1 + (int)threadIdx.x; i < ctas; i += 256)
@@ -371,47 +381,84 @@ __global__ void __launch_bounds__(256) combine_kernel(AttnArgs a, int ctas) {
             break;
         }
     __syncthreads();
-    const int row = blockIdx.y * 8 + w;
-    if (row >= d.z * a.group) return;
-    const int end = last;
-    const int64_t first = ((int64_t)2 * c + slot) * a.rows + row;
-    float m = a.part_ml[first].x;
-    for (int i = c + 1 + lane; i <= end; i += 32)
-        if (a.part_desc[2 * i].x >= kPartMiddle)
-            m = fmaxf(m, a.part_ml[(int64_t)2 * i * a.rows + row].x);
+    const int n = last - c + 1;              // shares of this tile
+    const int local = w / WPR, row = row0 + local;
+    const bool live = row < d.z * a.group;
+    auto record = [&](int i) {               // the i-th share's row
+        return ((int64_t)2 * (c + i) + (i ? 0 : slot)) * a.rows + row;
+    };
+    if (w % WPR == 0 && live) {              // a warp: the row's maximum, weights and sum
+        float m = -INFINITY;
+        for (int i = lane; i < n; i += 32)
+            if (i == 0 || a.part_desc[2 * (c + i)].x >= kPartMiddle)
+                m = fmaxf(m, a.part_ml[record(i)].x);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float base = m == -INFINITY ? 0.f : m;
-    float sum = 0.f, acc[DP / 32];
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const float base = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
+        for (int i = lane; i < n; i += 32) {
+            float f = 0.f;                   // a share without a block of this tile
+            if (i == 0 || a.part_desc[2 * (c + i)].x >= kPartMiddle) {
+                const float2 ml = a.part_ml[record(i)];
+                f = exp2f(ml.x - base);
+                sum = fmaf(f, ml.y, sum);
+            }
+            weight[local * ctas + i] = f;
+        }
 #pragma unroll
-    for (int k = 0; k < DP / 32; ++k) acc[k] = 0.f;
-    for (int i = c; i <= end; ++i) {
-        if (i > c && a.part_desc[2 * i].x < kPartMiddle) continue;   // no block of this tile
-        const int64_t at = i == c ? first : (int64_t)2 * i * a.rows + row;
-        const float2 ml = a.part_ml[at];
-        const float f = exp2f(ml.x - base);
-        sum = fmaf(f, ml.y, sum);
-#pragma unroll
-        for (int k = 0; k < DP / 32; ++k)
-            acc[k] = fmaf(f, a.part_o[at * DP + lane + 32 * k], acc[k]);
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) total[local] = make_float2(m, sum);
     }
+    __syncthreads();
+    float acc[kC];
+#pragma unroll
+    for (int k = 0; k < kC; ++k) acc[k] = 0.f;
+    if (live) {
+#pragma unroll 4
+        for (int i = w % WPR; i < n; i += WPR) {
+            const float f = weight[local * ctas + i];
+            if (f == 0.f) continue;          // also what an absent partial holds
+            const float *o = a.part_o + record(i) * DP + lane;
+#pragma unroll
+            for (int k = 0; k < kC; ++k) acc[k] = fmaf(f, o[32 * k], acc[k]);
+        }
+    }
+    if constexpr (WPR > 1) {
+#pragma unroll
+        for (int k = 0; k < kC; ++k) part[w][lane + 32 * k] = acc[k];
+        __syncthreads();
+        if (w != 0) return;
+#pragma unroll
+        for (int k = 0; k < kC; ++k)
+            for (int i = 1; i < WPR; ++i) acc[k] += part[i][lane + 32 * k];
+    }
+    if (!live) return;
+    const float2 ml = total[local];
     const int64_t head = (int64_t)(d.y + row / a.group) * a.q_heads + d.w * a.group + row % a.group;
     T *o = static_cast<T *>(a.out) + head * a.D;
-    const float r = 1.f / sum;
+    const float r = 1.f / ml.y;
 #pragma unroll
-    for (int k = 0; k < DP / 32; ++k)
-        if (lane + 32 * k < a.D) o[lane + 32 * k] = from_f<T>(sum == 0.f ? 0.f : acc[k] * r);
-    if (a.lse && lane == 0) a.lse[head] = sum == 0.f ? -INFINITY : (m + log2f(sum)) / kLog2e;
+    for (int k = 0; k < kC; ++k)
+        if (lane + 32 * k < a.D) o[lane + 32 * k] = from_f<T>(ml.y == 0.f ? 0.f : acc[k] * r);
+    if (a.lse && lane == 0) a.lse[head] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) / kLog2e;
+}
+
+template <typename T, int DP>
+cudaError_t combine_dim(const AttnArgs &a, int ctas, bool pdl, cudaStream_t st) {
+    if (a.rows <= 16)
+        return launch_kernel(pdl, combine_kernel<T, DP, 8>, dim3(ctas, a.rows), 256,
+                             sizeof(float) * ctas, st, a, ctas);
+    return launch_kernel(pdl, combine_kernel<T, DP, 1>, dim3(ctas, (a.rows + 7) / 8), 256,
+                         sizeof(float) * 8 * ctas, st, a, ctas);
 }
 
 template <typename T> cudaError_t combine(const AttnArgs &a, int ctas, int dp, bool pdl,
                                           cudaStream_t st) {
-    const dim3 grid(ctas, (a.rows + 7) / 8);
     switch (dp) {
-    case 64: return launch_kernel(pdl, combine_kernel<T, 64>, grid, 256, 0, st, a, ctas);
-    case 128: return launch_kernel(pdl, combine_kernel<T, 128>, grid, 256, 0, st, a, ctas);
-    case 192: return launch_kernel(pdl, combine_kernel<T, 192>, grid, 256, 0, st, a, ctas);
-    default: return launch_kernel(pdl, combine_kernel<T, 256>, grid, 256, 0, st, a, ctas);
+    case 64: return combine_dim<T, 64>(a, ctas, pdl, st);
+    case 128: return combine_dim<T, 128>(a, ctas, pdl, st);
+    case 192: return combine_dim<T, 192>(a, ctas, pdl, st);
+    default: return combine_dim<T, 256>(a, ctas, pdl, st);
     }
 }
 
@@ -451,7 +498,7 @@ Path path_of(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim, int3
 }
 
 struct Layout {
-    int ctas, rows, tq, dp;
+    int ctas, rows, tq, dp, extra;
     int64_t o, ml, desc, total;     // byte offsets in the workspace
 };
 
@@ -466,6 +513,8 @@ Layout layout_of(Path path, int32_t group, int32_t dim) {
         l.rows = path == kRows64 ? 64 : 16;
         l.tq = l.rows / group;
     }
+    // one block of the kernel's keys: what a tile costs besides its keys
+    l.extra = path == kPrefill ? 128 : path == kDecode ? 64 : 32;
     l.o = 0;
     l.ml = l.o + (int64_t)l.ctas * 2 * l.rows * l.dp * 4;
     l.desc = (l.ml + (int64_t)l.ctas * 2 * l.rows * 8 + 15) & ~15ll;
@@ -690,6 +739,7 @@ extern "C" ultramem_status ultramem_paged_attention(
     a.n_pages = c->n_pages;
     a.rows = l.rows;
     a.tq = l.tq;
+    a.extra = l.extra;
     a.scale = scale;
     a.scale_log2 = scale * kLog2e;
     cudaStream_t st = (cudaStream_t)stream;

@@ -5,8 +5,9 @@
 // The rows of a request that read one key/value head are its new tokens x
 // the query heads of that head's group, token-major.  A tile is TQ tokens of
 // one request for one key/value head.  Its length is the number of keys its
-// last token sees (at least 1), and the lengths of all tiles, laid end to end
-// in the order (request, head, tile), form one axis.  CTA c of C takes the
+// last token sees (at least 1) and a fixed cost in keys (reading the queries,
+// writing the output), and the lengths of all tiles, laid end to end in the
+// order (request, head, tile), form one axis.  CTA c of C takes the
 // c-th of C equal shares of that axis, so the CTAs finish together whatever
 // the requests' lengths are, without any table made on the host.  A share
 // boundary inside a tile is moved to the next block of KB keys.  A tile that
@@ -38,6 +39,7 @@ struct AttnArgs {
     int page_shift, table_width, n_pages;
     int rows;                   // rows of a tile, padded (the partials' stride)
     int tq;                     // tokens of a tile
+    int extra;                  // a tile's fixed cost, in keys
     float scale, scale_log2;    // the scores' factor, and times log2(e)
 };
 
@@ -58,22 +60,22 @@ struct Request {
         if (kv < 0) kv = 0;
     }
     __device__ __forceinline__ int tiles(int tq) const { return (n + tq - 1) / tq; }
-    // keys the last token of tile t sees, at least 1 (the tile's length)
-    __device__ __forceinline__ int length(int t, int tq) const {
+    // keys the last token of tile t sees, at least 1
+    __device__ __forceinline__ int keys(int t, int tq) const {
         const int last = min((t + 1) * tq, n);
         return max(1, kv - n + last);
     }
-    // sum of the lengths of the first t < tiles() tiles: kv - n + (i + 1) tq
-    // each, but 1 where that is below 1
-    __device__ __forceinline__ int64_t before(int t, int tq) const {
+    // where tile t < tiles() starts: the keys and fixed costs of the tiles
+    // before it, kv - n + (i + 1) tq keys each, but 1 where that is below 1
+    __device__ __forceinline__ int64_t before(int t, const AttnArgs &a) const {
         const int64_t c = (int64_t)kv - n;
-        const int64_t flat = c < 0 ? min((int64_t)t, -c / tq) : 0;   // tiles of length 1
+        const int64_t flat = c < 0 ? min((int64_t)t, -c / a.tq) : 0;   // tiles of 1 key
         const int64_t m = t - flat;
-        return flat + m * c + (int64_t)tq * (m * flat + m * (m + 1) / 2);
+        return flat + m * c + (int64_t)a.tq * (m * flat + m * (m + 1) / 2) + (int64_t)t * a.extra;
     }
-    __device__ __forceinline__ int64_t per_head(int tq) const {
-        const int t = tiles(tq);
-        return t ? before(t - 1, tq) + length(t - 1, tq) : 0;
+    __device__ __forceinline__ int64_t per_head(const AttnArgs &a) const {
+        const int t = tiles(a.tq);
+        return t ? before(t - 1, a) + keys(t - 1, a.tq) + a.extra : 0;
     }
 };
 
@@ -97,7 +99,7 @@ __device__ __forceinline__ void place_share(const AttnArgs &a, int c, int ctas, 
     Request q;
     for (int r = r0; r < r1; ++r) {
         q.read(a, r);
-        mine += q.per_head(a.tq) * a.kv_heads;
+        mine += q.per_head(a) * a.kv_heads;
     }
     int64_t upto = mine;
 #pragma unroll
@@ -124,7 +126,7 @@ __device__ __forceinline__ void place_share(const AttnArgs &a, int c, int ctas, 
         int64_t rest = lo - at, head = 0;
         for (; r < r1; ++r) {
             q.read(a, r);
-            head = q.per_head(a.tq);
+            head = q.per_head(a);
             if (rest < head * a.kv_heads) break;
             rest -= head * a.kv_heads;
         }
@@ -133,7 +135,7 @@ __device__ __forceinline__ void place_share(const AttnArgs &a, int c, int ctas, 
         int t0 = 0, t1 = q.tiles(a.tq) - 1;   // the last tile that starts at or before rest
         while (t0 < t1) {
             const int m = (t0 + t1 + 1) >> 1;
-            if (q.before(m, a.tq) <= rest)
+            if (q.before(m, a) <= rest)
                 t0 = m;
             else
                 t1 = m - 1;
@@ -141,7 +143,7 @@ __device__ __forceinline__ void place_share(const AttnArgs &a, int c, int ctas, 
         cur->r = r;
         cur->h = h;
         cur->t = t0;
-        cur->off = rest - q.before(t0, a.tq);
+        cur->off = rest - q.before(t0, a);
         cur->left = hi - lo;
     }
     __syncthreads();
@@ -175,16 +177,16 @@ struct Walk {
                     c.h = a.kv_heads - 1;
                 }
             }
-            const int len = q.length(c.t, a.tq);
-            const int64_t take = min(c.left, (int64_t)len - c.off);
+            const int keys = q.keys(c.t, a.tq);
+            const int64_t len = (int64_t)keys + a.extra, take = min(c.left, len - c.off);
             tok0 = q.tok0 + c.t * a.tq;
             n_tok = min(a.tq, q.n - c.t * a.tq);
             h = c.h;
             kv = q.kv;
             pos0 = q.kv - q.n + c.t * a.tq;
-            blocks = (len + kb - 1) / kb;
-            j0 = (int)((c.off + kb - 1) / kb);
-            j1 = (int)((c.off + take + kb - 1) / kb);
+            blocks = (keys + kb - 1) / kb;
+            j0 = (int)min((int64_t)blocks, (c.off + kb - 1) / kb);
+            j1 = (int)min((int64_t)blocks, (c.off + take + kb - 1) / kb);
             slot = first ? 0 : 1;
             first = false;
             c.left -= take;

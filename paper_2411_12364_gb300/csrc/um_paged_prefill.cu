@@ -24,6 +24,7 @@
 // thread), 9 the copies (TMA: K and V blocks, a box per page, in a ring; Q
 // per tile), 10 clears what a last page holds past the request's length.
 #include "um_paged.cuh"
+#include "um_pair.cuh"
 #include "um_tc.cuh"
 
 namespace um {
@@ -32,7 +33,10 @@ namespace {
 
 constexpr int kKeys = 128;
 constexpr int kHalfRows = 128;
-constexpr int kThreads = 352;
+constexpr int kThreads = 384;
+// registers of a thread: 384 x 168 at launch, split 2 x 128 x 208 + 128 x 88
+constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
+static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * 168, "register split");
 constexpr uint32_t kHalfBytes = 128 * 128;     // 128 rows x 64 columns of bf16
 constexpr float kRaise = 8.f;                  // log2 units
 
@@ -49,17 +53,19 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0],"
-        " {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0],"
+        " {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
         "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
-        "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
-        "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
-        "r"(r[29]), "r"(r[30]), "r"(r[31])
+        "r"(r[15])
         : "memory");
+}
+// ties the values of a TMEM load to this point, after its wait
+__device__ __forceinline__ void arrived(uint32_t (&r)[32]) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k) asm volatile("" : "+r"(r[k]));
 }
 __device__ __forceinline__ void tmem_st_wait() {
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -89,6 +95,18 @@ __device__ __forceinline__ uint64_t desc_mn_sw128(uint32_t saddr) {
     return d;
 }
 constexpr uint32_t kBColumnsContiguous = 1u << 16;   // instruction descriptor: B is N-major
+
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xffffffff;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(r));
+    return r != 0;
+}
+// the same value in every lane, and known to be
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 // a wait of a whole warp, with one answer for all lanes
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) {
@@ -164,6 +182,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
 
     if (w < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         // ---- softmax and output of half i: thread = row ----
         const int i = w >> 2, row = (w & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((w & 3) * 32) << 16;
@@ -171,6 +190,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         int4 *desc = a.part_desc + 2 * blockIdx.x;
         if (tid == 0) desc[0] = desc[1] = make_int4(kPartNone, 0, 0, 0);
         const int tok = row / a.group, g = row - tok * a.group;
+        const F2 scale = f2(a.scale_log2);
         uint32_t blocks = 0, tiles = 0;      // done so far by this half: barrier phases
         while (ok && wk.next(a, kKeys)) {
             const Halves hv(wk, tq_half);
@@ -192,6 +212,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tc::tmem_ld32_nowait(ts + 32 * c, s[c]);
                 tc::tmem_ld_wait();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) arrived(s[c]);
                 if ((j + 1) * kKeys > all_see) {
                     const int left = limit - j * kKeys;
 #pragma unroll
@@ -203,9 +225,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                 float mx[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    mx[c] = __uint_as_float(s[c][0]);
+                    mx[c] = fmaxf(__uint_as_float(s[c][0]), __uint_as_float(s[c][1]));
 #pragma unroll
-                    for (int k = 1; k < 32; ++k) mx[c] = fmaxf(mx[c], __uint_as_float(s[c][k]));
+                    for (int k = 2; k < 32; k += 2)
+                        mx[c] = max3(mx[c], __uint_as_float(s[c][k]), __uint_as_float(s[c][k + 1]));
                 }
                 const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 const bool raise = (top - m) * a.scale_log2 > kRaise ||
@@ -216,38 +239,36 @@ __global__ void __launch_bounds__(kThreads, 1)
                     l *= f;
                     if (j > wk.j0) {   // S_i is there, so all earlier products are done
 #pragma unroll
-                        for (int c = 0; c < DP / 32; ++c) {
-                            uint32_t o[32];
-                            tc::tmem_ld32_nowait(to + 32 * c, o);
-                            tc::tmem_ld_wait();
+                        for (int c = 0; c < DP / 16; ++c) {
+                            float o[16];
+                            uint32_t x[16];
+                            tc::tmem_ld16(to + 16 * c, o);
 #pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                            tmem_st32(to + 32 * c, o);
+                            for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(o[k] * f);
+                            tmem_st16(to + 16 * c, x);
                         }
                     }
                 }
-                const float shift = m == -INFINITY ? 0.f : -m * a.scale_log2;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                uint32_t p[2][32];
+                const F2 shift = f2(m == -INFINITY ? 0.f : -m * a.scale_log2);
+                F2 sum[2] = {f2(0.f), f2(0.f)};
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t p[16];
 #pragma unroll
-                    for (int k = 0; k < 32; k += 2) {
-                        const float x = ex2(fmaf(__uint_as_float(s[c][k]), a.scale_log2, shift));
-                        const float y =
-                            ex2(fmaf(__uint_as_float(s[c][k + 1]), a.scale_log2, shift));
-                        sum[k & 2] += x;
-                        sum[(k & 2) + 1] += y;
+                    for (int k = 0; k < 16; ++k) {
+                        const float2 y = split(fma2(f2(__uint_as_float(s[c][2 * k]),
+                                                       __uint_as_float(s[c][2 * k + 1])),
+                                                    scale, shift));
+                        const float e0 = ex2(y.x), e1 = ex2(y.y);
+                        sum[k & 1] = sum[k & 1] + f2(e0, e1);
                         // weights as the A operand: one rounding to bf16, as
                         // large as that of the values; the sum keeps fp32
-                        const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
-                        p[c >> 1][16 * (c & 1) + (k >> 1)] =
-                            *reinterpret_cast<const uint32_t *>(&b);
+                        const __nv_bfloat162 b = __floats2bfloat162_rn(e0, e1);
+                        p[k] = *reinterpret_cast<const uint32_t *>(&b);
                     }
-                tmem_st32(ts, p[0]);
-                tmem_st32(ts + 32, p[1]);
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    tmem_st16(ts + 16 * c, p);
+                }
+                l += both(sum[0] + sum[1]);
                 tmem_st_wait();
                 tc::tc_fence_before();
                 tc::mbar_arrive(&p_full[i]);
@@ -283,6 +304,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (any) {
                     tc::tmem_ld32_nowait(to + 32 * c, o);
                     tc::tmem_ld_wait();
+                    arrived(o);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 32; ++k) o[k] = 0u;
@@ -316,12 +338,22 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::tc_fence_before();   // O is read: the next tile's products may write it
         }
         if (!ok && lane == 0) atomicOr(a.err, kErrTimeout);
-    } else if (w == 8 && lane == 0) {
-        // ---- products: one thread issues, in an order that alternates the
-        // halves: P_0 V, next S_0, P_1 V, next S_1 ----
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    }
+    if (w == 8) {
+        // ---- products: one elected thread issues, in an order that alternates
+        // the halves: P_0 V, next S_0, P_1 V, next S_1.  The whole warp walks
+        // and waits, so that descriptors and loop bounds are warp-uniform:
+        // with one thread in this branch each product took 115 cycles to
+        // issue, more than it takes to run ----
         constexpr uint32_t idesc_s = tc::idesc_bf16_f32(128, kKeys);
         constexpr uint32_t idesc_o = tc::idesc_bf16_f32(128, DP) | kBColumnsContiguous;
-        const uint32_t q_addr = tc::smem_u32(qs), kv_addr = tc::smem_u32(ring);
+        const bool leader = elect_one();
+        const uint64_t q_desc = tc::desc_k_sw128(tc::smem_u32(qs));
+        const uint64_t k_desc = tc::desc_k_sw128(tc::smem_u32(ring));
+        const uint64_t v_desc = desc_mn_sw128(tc::smem_u32(ring));
+        const uint32_t tmem_u = uniform(tmem);
         int stage = 0;
         uint32_t phase = 0, tiles = 0, p_phase[2] = {0, 0};
         auto advance = [&] {
@@ -330,62 +362,75 @@ __global__ void __launch_bounds__(kThreads, 1)
                 phase ^= 1;
             }
         };
+        auto commit = [&](uint64_t *bar) {
+            if (leader) tc::mma_commit(bar);
+        };
         auto scores = [&](int i, int st) {
+            const uint64_t qd = q_desc + (uint32_t)i * (C::kTile >> 4);
+            const uint64_t kd = k_desc + (uint32_t)st * (C::kTile >> 4);
+            if (leader) {
 #pragma unroll
-            for (int k = 0; k < DP / 16; ++k) {
-                const uint32_t off = (k >> 2) * kHalfBytes + (k & 3) * 32;
-                tc::mma_bf16(tmem_s[i], tc::desc_k_sw128(q_addr + i * C::kTile + off),
-                             tc::desc_k_sw128(kv_addr + st * C::kTile + off), idesc_s, k > 0);
+                for (int k = 0; k < DP / 16; ++k) {
+                    const uint32_t off = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
+                    tc::mma_bf16(tmem_u + 128 * i, qd + off, kd + off, idesc_s, k > 0);
+                }
             }
-            tc::mma_commit(&s_full[i]);
+            commit(&s_full[i]);
+        };
+        auto output = [&](int i, int st, bool add) {
+            const uint64_t vd = v_desc + (uint32_t)st * (C::kTile >> 4);
+            if (leader) {
+#pragma unroll
+                for (int k = 0; k < kKeys / 16; ++k)
+                    mma_bf16_ts(tmem_u + 256 + DP * i, tmem_u + 128 * i + 8 * k,
+                                vd + k * (16 * 128 >> 4), idesc_o, add || k > 0);
+            }
         };
         while (ok && wk.next(a, kKeys)) {
             const Halves hv(wk, tq_half);
             if (!hv.live(wk)) continue;
-            if (!(ok = tc::mbar_wait(&q_full, tiles & 1))) break;
+            const int j0 = uniform(wk.j0), end = uniform(hv.end);
+            const int e[2] = {(int)uniform(hv.e[0]), (int)uniform(hv.e[1])};
+            if (!(ok = warp_wait(&q_full, tiles & 1))) break;
             ++tiles;
-            if (!(ok = tc::mbar_wait(&kv_full[stage], phase))) break;
+            if (!(ok = warp_wait(&kv_full[stage], phase))) break;
             tc::tc_fence_after();
-            for (int i = 0; i < 2; ++i)
-                if (wk.j0 < hv.e[i]) scores(i, stage);
-            tc::mma_commit(&kv_empty[stage]);
-            if (wk.j0 + 1 == hv.end) tc::mma_commit(&q_empty);
+            if (j0 < e[0]) scores(0, stage);
+            if (j0 < e[1]) scores(1, stage);
+            commit(&kv_empty[stage]);
+            if (j0 + 1 == end) commit(&q_empty);
             advance();
-            for (int j = wk.j0; ok && j < hv.end; ++j) {
+            for (int j = j0; j < end; ++j) {
                 const int sv = stage;
-                if (!(ok = tc::mbar_wait(&kv_full[stage], phase))) break;
-                tc::tc_fence_after();
+                if (!(ok = warp_wait(&kv_full[stage], phase))) break;
                 advance();
-                const bool more = j + 1 < hv.end;
+                const bool more = j + 1 < end;
                 const int sk = stage;
-                if (more && !(ok = tc::mbar_wait(&kv_full[stage], phase))) break;
+                if (more && !(ok = warp_wait(&kv_full[stage], phase))) break;
+#pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    if (j < hv.e[i]) {
-                        if (!(ok = tc::mbar_wait(&p_full[i], p_phase[i]))) break;
+                    if (j < e[i]) {
+                        if (!(ok = warp_wait(&p_full[i], p_phase[i]))) break;
                         p_phase[i] ^= 1;
                         tc::tc_fence_after();
-#pragma unroll
-                        for (int k = 0; k < kKeys / 16; ++k)
-                            mma_bf16_ts(tmem_o[i], tmem_s[i] + 8 * k,
-                                        desc_mn_sw128(kv_addr + sv * C::kTile + k * 16 * 128),
-                                        idesc_o, j > wk.j0 || k > 0);
-                        if (j + 1 == hv.e[i]) tc::mma_commit(&o_full[i]);
+                        output(i, sv, j > j0);
+                        if (j + 1 == e[i]) commit(&o_full[i]);
                     }
-                    if (j + 1 < hv.e[i]) scores(i, sk);
+                    if (j + 1 < e[i]) scores(i, sk);
                 }
                 if (!ok) break;
-                tc::mma_commit(&kv_empty[sv]);
+                commit(&kv_empty[sv]);
                 if (more) {
-                    tc::mma_commit(&kv_empty[sk]);
-                    if (j + 2 == hv.end) tc::mma_commit(&q_empty);
+                    commit(&kv_empty[sk]);
+                    if (j + 2 == end) commit(&q_empty);
                     advance();
                 }
             }
         }
         if (!ok) {
-            atomicOr(a.err, kErrTimeout);
-            tc::mma_commit(&drained);          // products in flight end before TMEM is freed
-            tc::mbar_wait(&drained, 0);
+            if (leader) atomicOr(a.err, kErrTimeout);
+            commit(&drained);                  // products in flight end before TMEM is freed
+            warp_wait(&drained, 0);
         }
     } else if (w == 9) {
         // ---- copies: the whole warp, a lane per page of the block ----
