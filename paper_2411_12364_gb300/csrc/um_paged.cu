@@ -514,11 +514,11 @@ Layout layout_of(Path path, int32_t group, int32_t dim) {
         l.tq = l.rows / group;
     }
     // one block of the kernel's keys: what a tile costs besides its keys
-    l.extra = path == kPrefill ? 128 : path == kDecode ? 64 : 32;
+    l.extra = path == kPrefill ? (l.dp == 128 ? 384 : 256) : path == kDecode ? 64 : 32;
     l.o = 0;
     l.ml = l.o + (int64_t)l.ctas * 2 * l.rows * l.dp * 4;
     l.desc = (l.ml + (int64_t)l.ctas * 2 * l.rows * 8 + 15) & ~15ll;
-    l.total = l.desc + (int64_t)l.ctas * 2 * 16;
+    l.total = l.desc + (int64_t)l.ctas * 2 * 16 + 128;   // and room to align the start to 128
     return l;
 }
 
@@ -723,7 +723,7 @@ extern "C" ultramem_status ultramem_paged_attention(
     a.kv_lens = kv_lens;
     a.out = out;
     a.lse = lse;
-    char *ws = static_cast<char *>(workspace);
+    char *ws = reinterpret_cast<char *>(((uintptr_t)workspace + 127) & ~(uintptr_t)127);
     a.part_o = reinterpret_cast<float *>(ws + l.o);
     a.part_ml = reinterpret_cast<float2 *>(ws + l.ml);
     a.part_desc = reinterpret_cast<int4 *>(ws + l.desc);

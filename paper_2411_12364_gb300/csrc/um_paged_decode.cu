@@ -119,13 +119,14 @@ __global__ void __launch_bounds__(kThreads, 2)
         bool ok = true;
         int issued = 0;
         while (ok && wk.next(a, kKeys)) {
+            // the table's entry for a block is read a block ahead
+            int page = lane < pages ? page_of(a, wk.c.r, wk.j0 * kKeys + lane * box_rows, wk.kv)
+                                    : -1;
             for (int j = wk.j0; ok && j < wk.j1; ++j) {
                 const int key = j * kKeys + lane * box_rows;
-                int z = a.n_pages * a.kv_heads;             // outside: reads zeros
-                if (lane < pages) {
-                    const int p = page_of(a, wk.c.r, key, wk.kv);
-                    if (p >= 0) z = p * a.kv_heads + wk.h;
-                }
+                // outside the cache: reads zeros
+                const int z = page < 0 ? a.n_pages * a.kv_heads : page * a.kv_heads + wk.h;
+                page = lane < pages ? page_of(a, wk.c.r, key + kKeys, wk.kv) : -1;
                 if (!__all_sync(0xffffffffu, tc::mbar_wait(&empty[stage], phase ^ 1))) {
                     ok = false;
                     break;

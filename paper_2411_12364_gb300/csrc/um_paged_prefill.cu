@@ -20,8 +20,8 @@
 // the same value, so the quotient is the same, and the pass over O in TMEM
 // that a raise costs is rare.
 //
-// Warps: 0-3 and 4-7 the halves' softmax and output, 8 the products (one
-// thread), 9 the copies (TMA: K and V blocks, a box per page, in a ring; Q
+// Warps: 0-3 and 4-7 the halves' softmax and output, 8 and 11 the halves'
+// products (one thread each), 9 the copies (TMA: K and V blocks, a box per page, in a ring; Q
 // per tile), 10 clears what a last page holds past the request's length.
 #include "um_paged.cuh"
 #include "um_pair.cuh"
@@ -38,6 +38,7 @@ constexpr int kThreads = 384;
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * 168, "register split");
 constexpr uint32_t kHalfBytes = 128 * 128;     // 128 rows x 64 columns of bf16
+constexpr int kMost = 96;                      // keys whose weights are handed over first
 constexpr float kRaise = 8.f;                  // log2 units
 
 template <int DP> struct Cfg {
@@ -61,6 +62,12 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
         "r"(r[15])
         : "memory");
+}
+// 32 bytes, a whole sector, by one thread (dst 32-byte aligned)
+__device__ __forceinline__ void store32(void *dst, const uint32_t *r) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(r[0]),
+                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
 // ties the values of a TMEM load to this point, after its wait
 __device__ __forceinline__ void arrived(uint32_t (&r)[32]) {
@@ -143,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     using C = Cfg<DP>;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t kv_full[C::kStages], kv_empty[C::kStages], kv_raw[C::kStages];
-    __shared__ uint64_t q_full, q_empty, s_full[2], p_full[2], o_full[2], drained;
+    __shared__ uint64_t q_full, q_empty, s_full[2], p_most[2], p_full[2], o_full[2], turn[2], drained[2];
     __shared__ int64_t scratch[kThreads / 32 + 1];
     __shared__ Cursor cur;
     __shared__ uint32_t tmem_base;
@@ -153,16 +160,18 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (tid == 0) {
         for (int s = 0; s < C::kStages; ++s) {
             tc::mbar_init(&kv_full[s], 1);
-            tc::mbar_init(&kv_empty[s], 1);
+            tc::mbar_init(&kv_empty[s], 2);      // both halves' products
             tc::mbar_init(&kv_raw[s], 1);
         }
         tc::mbar_init(&q_full, 1);
-        tc::mbar_init(&q_empty, 1);
-        tc::mbar_init(&drained, 1);
+        tc::mbar_init(&q_empty, 2);
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&s_full[i], 1);
+            tc::mbar_init(&p_most[i], kHalfRows);
             tc::mbar_init(&p_full[i], kHalfRows);
             tc::mbar_init(&o_full[i], 1);
+            tc::mbar_init(&turn[i], 1);
+            tc::mbar_init(&drained[i], 1);
         }
         tc::fence_mbar_init();
     }
@@ -191,15 +200,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (tid == 0) desc[0] = desc[1] = make_int4(kPartNone, 0, 0, 0);
         const int tok = row / a.group, g = row - tok * a.group;
         const F2 scale = f2(a.scale_log2);
+        const bool wide = a.D % 16 == 0 && ((uintptr_t)a.out & 31) == 0;
         uint32_t blocks = 0, tiles = 0;      // done so far by this half: barrier phases
         while (ok && wk.next(a, kKeys)) {
             const Halves hv(wk, tq_half);
             const bool mine = tok < hv.n_tok[i] && tok < tq_half;
             const int pos = wk.pos0 + i * tq_half + tok;
             const int limit = mine ? min(wk.kv, pos + 1) : 0;   // keys this row sees
-            // keys that all rows of the half see: below it no masking
-            const int all_see = hv.n_tok[i] == tq_half && tq_half * a.group == kHalfRows
-                                    ? wk.pos0 + i * tq_half + 1 : 0;
+            // keys that all rows of the half see: below it no masking (rows past
+            // the tile's tokens hold whatever lies there and are not stored)
+            const int all_see = wk.pos0 + i * tq_half + 1;
             float m = -INFINITY, l = 0.f;
             for (int j = wk.j0; j < hv.e[i]; ++j) {
                 if (!warp_wait(&s_full[i], blocks & 1)) {
@@ -267,6 +277,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                         p[k] = *reinterpret_cast<const uint32_t *>(&b);
                     }
                     tmem_st16(ts + 16 * c, p);
+                    if (c == kMost / 32 - 1) {   // the product over these keys may start
+                        tmem_st_wait();
+                        tc::tc_fence_before();
+                        tc::mbar_arrive(&p_most[i]);
+                    }
                 }
                 l += both(sum[0] + sum[1]);
                 tmem_st_wait();
@@ -311,29 +326,31 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
                 if (!mine) continue;
                 if (wk.part != kPartNone) {
-                    float4 *dst = reinterpret_cast<float4 *>(a.part_o + rec * DP + 32 * c);
+                    float *dst = a.part_o + rec * DP + 32 * c;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        dst[k] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]),
-                                             __uint_as_float(o[4 * k + 2]),
-                                             __uint_as_float(o[4 * k + 3]));
+                    for (int k = 0; k < 4; ++k) store32(dst + 8 * k, &o[8 * k]);
                     continue;
                 }
                 __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + head * a.D + 32 * c;
+                uint32_t q[16];
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (32 * c + 8 * k < a.D) {
-                        uint32_t q[4];
+                for (int k = 0; k < 16; ++k) {
+                    const __nv_bfloat162 b = __floats2bfloat162_rn(
+                        none ? 0.f : __uint_as_float(o[2 * k]) * r,
+                        none ? 0.f : __uint_as_float(o[2 * k + 1]) * r);
+                    q[k] = *reinterpret_cast<const uint32_t *>(&b);
+                }
+                if (wide) {
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            const __nv_bfloat162 b = __floats2bfloat162_rn(
-                                none ? 0.f : __uint_as_float(o[8 * k + 2 * x]) * r,
-                                none ? 0.f : __uint_as_float(o[8 * k + 2 * x + 1]) * r);
-                            q[x] = *reinterpret_cast<const uint32_t *>(&b);
-                        }
-                        *reinterpret_cast<uint4 *>(dst + 8 * k) =
-                            make_uint4(q[0], q[1], q[2], q[3]);
-                    }
+                    for (int k = 0; k < 2; ++k)
+                        if (32 * c + 16 * k < a.D) store32(dst + 16 * k, &q[8 * k]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (32 * c + 8 * k < a.D)
+                            *reinterpret_cast<uint4 *>(dst + 8 * k) =
+                                make_uint4(q[4 * k], q[4 * k + 1], q[4 * k + 2], q[4 * k + 3]);
+                }
             }
             tc::tc_fence_before();   // O is read: the next tile's products may write it
         }
@@ -341,21 +358,26 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     }
-    if (w == 8) {
-        // ---- products: one elected thread issues, in an order that alternates
-        // the halves: P_0 V, next S_0, P_1 V, next S_1.  The whole warp walks
-        // and waits, so that descriptors and loop bounds are warp-uniform:
-        // with one thread in this branch each product took 115 cycles to
-        // issue, more than it takes to run ----
+    if (w == 8 || w == 11) {
+        // ---- products of half i, issued by one elected thread.  A warp for
+        // each half, because a wait, a commit and a product cost the issuing
+        // warp 60 to 110, 100 and 24 cycles: one warp for both halves was
+        // busy for longer than the products run.  The whole warp walks and
+        // waits, so that descriptors and bounds are warp-uniform (with one
+        // thread in this branch a product took 115 cycles to issue).  The halves
+        // take turns, a block's output product and the next scores at a time:
+        // left to themselves they may fall into step, and then their softmax
+        // and their products collide (3090 instead of 2410 cycles a block) ----
         constexpr uint32_t idesc_s = tc::idesc_bf16_f32(128, kKeys);
         constexpr uint32_t idesc_o = tc::idesc_bf16_f32(128, DP) | kBColumnsContiguous;
+        const int i = w == 8 ? 0 : 1;
         const bool leader = elect_one();
-        const uint64_t q_desc = tc::desc_k_sw128(tc::smem_u32(qs));
+        const uint64_t q_desc = tc::desc_k_sw128(tc::smem_u32(qs + i * C::kTile));
         const uint64_t k_desc = tc::desc_k_sw128(tc::smem_u32(ring));
         const uint64_t v_desc = desc_mn_sw128(tc::smem_u32(ring));
-        const uint32_t tmem_u = uniform(tmem);
+        const uint32_t t_s = uniform(tmem) + 128 * i, t_o = uniform(tmem) + 256 + DP * i;
         int stage = 0;
-        uint32_t phase = 0, tiles = 0, p_phase[2] = {0, 0};
+        uint32_t phase = 0, tiles = 0, p_phase = 0, turns = 0;
         auto advance = [&] {
             if (++stage == C::kStages) {
                 stage = 0;
@@ -365,38 +387,35 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto commit = [&](uint64_t *bar) {
             if (leader) tc::mma_commit(bar);
         };
-        auto scores = [&](int i, int st) {
-            const uint64_t qd = q_desc + (uint32_t)i * (C::kTile >> 4);
+        auto scores = [&](int st) {
             const uint64_t kd = k_desc + (uint32_t)st * (C::kTile >> 4);
             if (leader) {
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k) {
                     const uint32_t off = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
-                    tc::mma_bf16(tmem_u + 128 * i, qd + off, kd + off, idesc_s, k > 0);
+                    tc::mma_bf16(t_s, q_desc + off, kd + off, idesc_s, k > 0);
                 }
+                tc::mma_commit(&s_full[i]);
             }
-            commit(&s_full[i]);
         };
-        auto output = [&](int i, int st, bool add) {
+        auto output = [&](int st, int k0, int k1, bool add) {   // keys 16 k0 .. 16 k1
             const uint64_t vd = v_desc + (uint32_t)st * (C::kTile >> 4);
             if (leader) {
 #pragma unroll
-                for (int k = 0; k < kKeys / 16; ++k)
-                    mma_bf16_ts(tmem_u + 256 + DP * i, tmem_u + 128 * i + 8 * k,
-                                vd + k * (16 * 128 >> 4), idesc_o, add || k > 0);
+                for (int k = k0; k < k1; ++k)
+                    mma_bf16_ts(t_o, t_s + 8 * k, vd + k * (16 * 128 >> 4), idesc_o, add || k > 0);
             }
         };
         while (ok && wk.next(a, kKeys)) {
             const Halves hv(wk, tq_half);
             if (!hv.live(wk)) continue;
             const int j0 = uniform(wk.j0), end = uniform(hv.end);
-            const int e[2] = {(int)uniform(hv.e[0]), (int)uniform(hv.e[1])};
+            const int e = uniform(i == 0 ? hv.e[0] : hv.e[1]);   // blocks past e: no products
             if (!(ok = warp_wait(&q_full, tiles & 1))) break;
             ++tiles;
             if (!(ok = warp_wait(&kv_full[stage], phase))) break;
             tc::tc_fence_after();
-            if (j0 < e[0]) scores(0, stage);
-            if (j0 < e[1]) scores(1, stage);
+            if (j0 < e) scores(stage);
             commit(&kv_empty[stage]);
             if (j0 + 1 == end) commit(&q_empty);
             advance();
@@ -407,18 +426,22 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool more = j + 1 < end;
                 const int sk = stage;
                 if (more && !(ok = warp_wait(&kv_full[stage], phase))) break;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (j < e[i]) {
-                        if (!(ok = warp_wait(&p_full[i], p_phase[i]))) break;
-                        p_phase[i] ^= 1;
-                        tc::tc_fence_after();
-                        output(i, sv, j > j0);
-                        if (j + 1 == e[i]) commit(&o_full[i]);
-                    }
-                    if (j + 1 < e[i]) scores(i, sk);
+                if (j < e && !(ok = warp_wait(&p_most[i], p_phase))) break;
+                // half 0 goes first: it waits for half 1's turn before, half 1
+                // for half 0's at this block
+                if (!(ok = warp_wait(&turn[i ^ 1], (turns & 1) ^ (i == 0)))) break;
+                ++turns;
+                if (j < e) {
+                    tc::tc_fence_after();
+                    output(sv, 0, kMost / 16, j > j0);
+                    if (!(ok = warp_wait(&p_full[i], p_phase))) break;
+                    p_phase ^= 1;
+                    tc::tc_fence_after();
+                    output(sv, kMost / 16, kKeys / 16, true);
+                    if (j + 1 == e) commit(&o_full[i]);
                 }
-                if (!ok) break;
+                if (j + 1 < e) scores(sk);
+                if (leader) tc::mbar_arrive(&turn[i]);
                 commit(&kv_empty[sv]);
                 if (more) {
                     commit(&kv_empty[sk]);
@@ -429,16 +452,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (!ok) {
             if (leader) atomicOr(a.err, kErrTimeout);
-            commit(&drained);                  // products in flight end before TMEM is freed
-            warp_wait(&drained, 0);
+            commit(&drained[i]);               // products in flight end before TMEM is freed
+            warp_wait(&drained[i], 0);
         }
     } else if (w == 9) {
-        // ---- copies: the whole warp, a lane per page of the block ----
+        // ---- copies: the lanes read the table, one elected thread issues ----
         if (lane == 0) {
             tc::prefetch_tensormap(&map_q);
             tc::prefetch_tensormap(&map_k);
             tc::prefetch_tensormap(&map_v);
         }
+        const bool leader = elect_one();
         const int pages = kKeys / box_rows;
         const uint32_t q_bytes = (uint32_t)(tq_half * a.group) * 128 * C::kHalves;
         int stage = 0, issued = 0;
@@ -458,25 +482,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                         tc::tma_load_3d(qs + i * C::kTile + x * kHalfBytes, &map_q, &q_full,
                                         64 * x, wk.h * a.group, wk.tok0 + i * tq_half);
             }
+            // the table's entry for a block is read a block ahead
+            int page = lane < pages ? page_of(a, wk.c.r, wk.j0 * kKeys + lane * box_rows, wk.kv)
+                                    : -1;
             for (int j = wk.j0; ok && j < hv.end; ++j) {
                 const int key = j * kKeys + lane * box_rows;
-                int z = a.n_pages * a.kv_heads;             // outside: reads zeros
-                if (lane < pages) {
-                    const int p = page_of(a, wk.c.r, key, wk.kv);
-                    if (p >= 0) z = p * a.kv_heads + wk.h;
-                }
+                // outside the cache: reads zeros
+                const int z = page < 0 ? a.n_pages * a.kv_heads : page * a.kv_heads + wk.h;
+                page = lane < pages ? page_of(a, wk.c.r, key + kKeys, wk.kv) : -1;
 #pragma unroll
                 for (int which = 0; which < 2; ++which) {   // K, then V
                     if (!(ok = warp_wait(&kv_empty[stage], phase ^ 1))) break;
                     uint64_t *bar = which && j == tail ? &kv_raw[stage] : &kv_full[stage];
-                    if (lane == 0) tc::mbar_arrive_expect_tx(bar, C::kTile);
-                    __syncwarp();
-                    if (lane < pages) {
-                        uint8_t *dst = ring + (size_t)stage * C::kTile + lane * box_rows * 128;
+                    if (leader) tc::mbar_arrive_expect_tx(bar, C::kTile);
+                    // the pages one by one with uniform coordinates: a copy a
+                    // lane took longer to issue than a block of 16-token pages
+                    // takes to compute
+#pragma unroll 8
+                    for (int p = 0; p < pages; ++p) {
+                        const int zp = (int)__shfl_sync(0xffffffffu, z, p);
+                        const int rp = (j * kKeys + p * box_rows) & page_mask;
+                        if (leader) {
+                            uint8_t *dst = ring + (size_t)stage * C::kTile + p * box_rows * 128;
 #pragma unroll
-                        for (int x = 0; x < C::kHalves; ++x)
-                            tc::tma_load_3d(dst + x * kHalfBytes, which ? &map_v : &map_k, bar,
-                                            64 * x, key & page_mask, z);
+                            for (int x = 0; x < C::kHalves; ++x)
+                                tc::tma_load_3d(dst + x * kHalfBytes, which ? &map_v : &map_k, bar,
+                                                64 * x, rp, zp);
+                        }
                     }
                     ++issued;
                     if (++stage == C::kStages) {
