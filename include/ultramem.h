@@ -374,7 +374,7 @@ typedef struct ultramem_kv_cache {
  *           requests and past the batch;
  *   kv_lens [n_seqs]: ctx + new; 0 for a refused request, whose rows then
  *           attend to nothing;
- *   free_left [1]: the free list's length after the call;
+ *   free_left [1]: the free list's length after the call (NULL to skip);
  *   balance [1]: free_count less the pages asked for up to the last request
  *           that was served: free_left when none was refused before it, and
  *           below zero the number of pages that the step was short of.

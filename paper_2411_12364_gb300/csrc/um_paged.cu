@@ -1,7 +1,7 @@
 // um_paged.cu -- the paged key/value cache: pages for a step's new tokens
 // (paged_plan), the new keys and values into their pages (paged_append), and
 // the attention kernel of the storages and head widths that the tensor-core
-// kernels do not take, with the kernel that joins split tiles.
+// kernels do not take, with the kernels that join split tiles.
 #include "um_paged.cuh"
 
 namespace um {
@@ -103,7 +103,7 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) plan_kernel(Pl
     __syncthreads();
     if (blockIdx.x == 0 && tid == 0) {
         a.q_start[a.n_seqs] = (int32_t)min(total, (int64_t)INT32_MAX);
-        *a.free_left = free - (int)taken;
+        if (a.free_left) *a.free_left = free - (int)taken;
         *a.balance = (int32_t)max((int64_t)INT32_MIN, (int64_t)free - (int64_t)asked);
     }
 
@@ -348,108 +348,201 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
 // Block (c, y) joins rows of the tile that begins in share c and ends in a
 // later one: weights 2^(m_i - max m) over the shares' partials, added in a
 // fixed order, so the result does not depend on which share finished first.
-// A long axis with few rows leaves many partials of few rows (one request of
-// 131072 keys: 76 of 4): there the 8 warps of a block share one row's
-// partials (WPR = 8); chunks leave two or three of up to 256 rows: a warp a
-// row (WPR = 1).  One warp a row at 76 partials took 82 us, eight take 6.
-template <typename T, int DP, int WPR>
-__global__ void __launch_bounds__(256) combine_kernel(AttnArgs a, int ctas) {
-    constexpr int kRowsOfBlock = 8 / WPR, kC = DP / 32;
-    extern __shared__ float weight[];        // [kRowsOfBlock][ctas]
-    __shared__ float2 total[kRowsOfBlock];   // maximum, sum
-    __shared__ float part[WPR == 1 ? 1 : WPR][WPR == 1 ? 1 : DP];
-    __shared__ int last;
-    pdl_wait();
-    const int c = blockIdx.x, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    int slot = -1;
-    int4 d = make_int4(0, 0, 0, 0);
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const int4 e = a.part_desc[2 * c + s];
-        if (e.x == kPartFirst) {
-            slot = s;
-            d = e;
-        }
+// The work is a chain of dependent loads (records, statistics, outputs), so
+// each step is one round of loads for the whole block.  A long axis with few
+// rows leaves many partials of few rows (one request of 131072 keys: 76 of
+// 4): a block a row, its 8 warps over the partials.  Chunks leave two or
+// three partials of up to 256 rows: a block 32 rows, a warp four of them.
+struct Span {
+    int slot, n;                // place of the first partial, shares of the tile
+    int tok0, n_rows, h;
+};
+
+// The tile that begins in share c, the same for the whole block; false
+// without one.  kind[i]: what share c + i holds of it (n values, shared).
+__device__ __forceinline__ bool find_span(const AttnArgs &a, int c, int ctas, int *kind,
+                                          int *last, Span *s) {
+    int4 d = a.part_desc[2 * c];
+    s->slot = 0;
+    if (threadIdx.x == 0) *last = ctas - 1;
+    for (int i = c + 1 + (int)threadIdx.x; i < ctas; i += blockDim.x)
+        kind[i - c] = a.part_desc[2 * i].x;
+    if (d.x != kPartFirst) {
+        d = a.part_desc[2 * c + 1];
+        s->slot = 1;
     }
-    const int row0 = blockIdx.y * kRowsOfBlock;
-    if (slot < 0 || row0 >= d.z * a.group) return;   // the same in the whole block
-    if (threadIdx.x == 0) last = ctas - 1;
+    if (d.x != kPartFirst) return false;
+    s->tok0 = d.y;
+    s->n_rows = d.z * a.group;
+    s->h = d.w;
     __syncthreads();
-    for (int i = c + 1 + (int)threadIdx.x; i < ctas; i += 256)
-        if (a.part_desc[2 * i].x == kPartLast) {
-            atomicMin(&last, i);
+    for (int i = 1 + (int)threadIdx.x; i < ctas - c; i += blockDim.x)
+        if (kind[i] == kPartLast) {
+            atomicMin(last, c + i);
             break;
         }
+    if (threadIdx.x == 0) kind[0] = kPartFirst;
     __syncthreads();
-    const int n = last - c + 1;              // shares of this tile
-    const int local = w / WPR, row = row0 + local;
-    const bool live = row < d.z * a.group;
-    auto record = [&](int i) {               // the i-th share's row
-        return ((int64_t)2 * (c + i) + (i ? 0 : slot)) * a.rows + row;
-    };
-    if (w % WPR == 0 && live) {              // a warp: the row's maximum, weights and sum
+    s->n = *last - c + 1;
+    return true;
+}
+__device__ __forceinline__ int64_t record_of(const AttnArgs &a, const Span &s, int c, int i,
+                                             int row) {
+    return ((int64_t)2 * (c + i) + (i ? 0 : s.slot)) * a.rows + row;
+}
+__device__ __forceinline__ int64_t head_of(const AttnArgs &a, const Span &s, int row) {
+    return (int64_t)(s.tok0 + row / a.group) * a.q_heads + s.h * a.group + row % a.group;
+}
+__device__ __forceinline__ float lse_of(float m, float sum) {   // m in log2 units
+    return sum == 0.f ? -INFINITY : (m + log2f(sum)) / kLog2e;
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(256) join_row_kernel(AttnArgs a, int ctas) {
+    constexpr int kC = DP / 32;
+    extern __shared__ int shared[];
+    int *kind = shared;
+    float *weight = reinterpret_cast<float *>(shared + ctas);
+    __shared__ int last;
+    __shared__ float warp_max[8], warp_sum[8], part[8][DP];
+    pdl_wait();
+    const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    Span s;
+    if (!find_span(a, c, ctas, kind, &last, &s)) return;
+    for (int row = blockIdx.y; row < s.n_rows; row += gridDim.y) {
         float m = -INFINITY;
-        for (int i = lane; i < n; i += 32)
-            if (i == 0 || a.part_desc[2 * (c + i)].x >= kPartMiddle)
-                m = fmaxf(m, a.part_ml[record(i)].x);
+        float2 ml[2];                        // up to 512 shares
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = tid + 256 * k;
+            ml[k] = make_float2(-INFINITY, 0.f);
+            if (i < s.n && kind[i] != kPartNone) ml[k] = a.part_ml[record_of(a, s, c, i, row)];
+            m = fmaxf(m, ml[k].x);
+        }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (lane == 0) warp_max[w] = m;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m = fmaxf(m, warp_max[k]);
         const float base = m == -INFINITY ? 0.f : m;
         float sum = 0.f;
-        for (int i = lane; i < n; i += 32) {
-            float f = 0.f;                   // a share without a block of this tile
-            if (i == 0 || a.part_desc[2 * (c + i)].x >= kPartMiddle) {
-                const float2 ml = a.part_ml[record(i)];
-                f = exp2f(ml.x - base);
-                sum = fmaf(f, ml.y, sum);
-            }
-            weight[local * ctas + i] = f;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = tid + 256 * k;
+            const float f = exp2f(ml[k].x - base);
+            if (i < s.n) weight[i] = f;      // 0 for a share without a block of this tile
+            sum = fmaf(f, ml[k].y, sum);
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) total[local] = make_float2(m, sum);
-    }
-    __syncthreads();
-    float acc[kC];
+        if (lane == 0) warp_sum[w] = sum;
+        __syncthreads();
+        float acc[kC];
 #pragma unroll
-    for (int k = 0; k < kC; ++k) acc[k] = 0.f;
-    if (live) {
-#pragma unroll 4
-        for (int i = w % WPR; i < n; i += WPR) {
-            const float f = weight[local * ctas + i];
-            if (f == 0.f) continue;          // also what an absent partial holds
-            const float *o = a.part_o + record(i) * DP + lane;
+        for (int k = 0; k < kC; ++k) acc[k] = 0.f;
+#pragma unroll 8
+        for (int i = w; i < s.n; i += 8) {
+            const float f = weight[i];
+            if (f == 0.f) continue;          // an absent partial holds anything
+            const float *o = a.part_o + record_of(a, s, c, i, row) * DP + lane;
 #pragma unroll
             for (int k = 0; k < kC; ++k) acc[k] = fmaf(f, o[32 * k], acc[k]);
         }
-    }
-    if constexpr (WPR > 1) {
 #pragma unroll
         for (int k = 0; k < kC; ++k) part[w][lane + 32 * k] = acc[k];
         __syncthreads();
-        if (w != 0) return;
+        sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < kC; ++k)
-            for (int i = 1; i < WPR; ++i) acc[k] += part[i][lane + 32 * k];
+        for (int k = 0; k < 8; ++k) sum += warp_sum[k];
+        const int64_t head = head_of(a, s, row);
+        if (tid < a.D) {
+            float x = 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x += part[k][tid];
+            static_cast<T *>(a.out)[head * a.D + tid] = from_f<T>(sum == 0.f ? 0.f : x / sum);
+        }
+        if (a.lse && tid == 0) a.lse[head] = lse_of(m, sum);
+        __syncthreads();                     // the next row reuses the shared arrays
     }
-    if (!live) return;
-    const float2 ml = total[local];
-    const int64_t head = (int64_t)(d.y + row / a.group) * a.q_heads + d.w * a.group + row % a.group;
-    T *o = static_cast<T *>(a.out) + head * a.D;
-    const float r = 1.f / ml.y;
+}
+
+constexpr int kJoinRows = 32;
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(256) join_rows_kernel(AttnArgs a, int ctas) {
+    constexpr int kC = DP / 32;
+    extern __shared__ int shared[];
+    int *kind = shared;
+    float *weight = reinterpret_cast<float *>(shared + ctas);   // [n][kJoinRows]
+    __shared__ int last;
+    __shared__ float scale[kJoinRows];       // 1 / sum, 0 for a row without keys
+    pdl_wait();
+    const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    Span s;
+    if (!find_span(a, c, ctas, kind, &last, &s)) return;
+    for (int row0 = blockIdx.y * kJoinRows; row0 < s.n_rows; row0 += gridDim.y * kJoinRows) {
+        if (tid < kJoinRows && row0 + tid < s.n_rows) {
+            float m = -INFINITY, sum = 0.f;
+            for (int i = 0; i < s.n; ++i)
+                if (kind[i] != kPartNone)
+                    m = fmaxf(m, a.part_ml[record_of(a, s, c, i, row0 + tid)].x);
+            const float base = m == -INFINITY ? 0.f : m;
+            for (int i = 0; i < s.n; ++i) {
+                float f = 0.f;               // a share without a block of this tile
+                if (kind[i] != kPartNone) {
+                    const float2 ml = a.part_ml[record_of(a, s, c, i, row0 + tid)];
+                    f = exp2f(ml.x - base);
+                    sum = fmaf(f, ml.y, sum);
+                }
+                weight[i * kJoinRows + tid] = f;
+            }
+            scale[tid] = sum == 0.f ? 0.f : 1.f / sum;
+            if (a.lse) a.lse[head_of(a, s, row0 + tid)] = lse_of(m, sum);
+        }
+        __syncthreads();
+        float acc[kJoinRows / 8][kC];
 #pragma unroll
-    for (int k = 0; k < kC; ++k)
-        if (lane + 32 * k < a.D) o[lane + 32 * k] = from_f<T>(ml.y == 0.f ? 0.f : acc[k] * r);
-    if (a.lse && lane == 0) a.lse[head] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) / kLog2e;
+        for (int r = 0; r < kJoinRows / 8; ++r)
+#pragma unroll
+            for (int k = 0; k < kC; ++k) acc[r][k] = 0.f;
+        for (int i = 0; i < s.n; ++i) {
+            if (kind[i] == kPartNone) continue;
+#pragma unroll
+            for (int r = 0; r < kJoinRows / 8; ++r) {
+                const int row = w + 8 * r;
+                if (row0 + row >= s.n_rows) continue;
+                const float f = weight[i * kJoinRows + row];
+                const float *o = a.part_o + record_of(a, s, c, i, row0 + row) * DP + lane;
+#pragma unroll
+                for (int k = 0; k < kC; ++k)
+                    acc[r][k] = f == 0.f ? acc[r][k] : fmaf(f, o[32 * k], acc[r][k]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kJoinRows / 8; ++r) {
+            const int row = w + 8 * r;
+            if (row0 + row >= s.n_rows) continue;
+            T *o = static_cast<T *>(a.out) + head_of(a, s, row0 + row) * a.D;
+#pragma unroll
+            for (int k = 0; k < kC; ++k)
+                if (lane + 32 * k < a.D) o[lane + 32 * k] = from_f<T>(acc[r][k] * scale[row]);
+        }
+        __syncthreads();                     // the next rows reuse the shared arrays
+    }
 }
 
 template <typename T, int DP>
 cudaError_t combine_dim(const AttnArgs &a, int ctas, bool pdl, cudaStream_t st) {
-    if (a.rows <= 16)
-        return launch_kernel(pdl, combine_kernel<T, DP, 8>, dim3(ctas, a.rows), 256,
-                             sizeof(float) * ctas, st, a, ctas);
-    return launch_kernel(pdl, combine_kernel<T, DP, 1>, dim3(ctas, (a.rows + 7) / 8), 256,
-                         sizeof(float) * 8 * ctas, st, a, ctas);
+    // blocks for the rows that the caller's bound announces; a block goes on
+    // to further rows where there are more
+    const int rows = a.rows < a.rows_hint ? a.rows : a.rows_hint;
+    if (rows <= 64)
+        return launch_kernel(pdl, join_row_kernel<T, DP>, dim3(ctas, rows), 256,
+                             (size_t)8 * ctas, st, a, ctas);
+    return launch_kernel(pdl, join_rows_kernel<T, DP>,
+                         dim3(ctas, (rows + kJoinRows - 1) / kJoinRows), 256,
+                         (size_t)4 * (1 + kJoinRows) * ctas, st, a, ctas);
 }
 
 template <typename T> cudaError_t combine(const AttnArgs &a, int ctas, int dp, bool pdl,
@@ -610,7 +703,7 @@ extern "C" ultramem_status ultramem_paged_plan(const int32_t *ctx_lens, const in
                                                int32_t *slots, int32_t *free_left,
                                                int32_t *balance, void *stream) {
     if (n_seqs < 0 || n_tokens < 0 || table_width < 0 || !page_size_ok(page_size) || !free_count ||
-        !q_start || !free_left || !balance || free_left == free_count || balance == free_count ||
+        !q_start || !balance || free_left == free_count || balance == free_count ||
         balance == free_left)
         return ULTRAMEM_EINVAL;
     if (n_seqs > 0 && (!ctx_lens || !new_lens || !kv_lens || kv_lens == ctx_lens ||
@@ -740,6 +833,7 @@ extern "C" ultramem_status ultramem_paged_attention(
     a.rows = l.rows;
     a.tq = l.tq;
     a.extra = l.extra;
+    a.rows_hint = (int)((int64_t)max_new * group < l.rows ? (int64_t)max_new * group : l.rows);
     a.scale = scale;
     a.scale_log2 = scale * kLog2e;
     cudaStream_t st = (cudaStream_t)stream;

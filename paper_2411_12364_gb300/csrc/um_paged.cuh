@@ -13,7 +13,7 @@
 // boundary inside a tile is moved to the next block of KB keys.  A tile that
 // lies in one share is written straight to the output; one that crosses
 // shares leaves a partial (maximum, sum, unnormalised output) per share,
-// which combine_kernel joins in share order.
+// which the join kernels add in share order.
 #pragma once
 
 #include "um_internal.cuh"
@@ -38,6 +38,7 @@ struct AttnArgs {
     int n_seqs, n_tokens, q_heads, kv_heads, group, D;
     int page_shift, table_width, n_pages;
     int rows;                   // rows of a tile, padded (the partials' stride)
+    int rows_hint;              // rows that tiles are expected to have
     int tq;                     // tokens of a tile
     int extra;                  // a tile's fixed cost, in keys
     float scale, scale_log2;    // the scores' factor, and times log2(e)

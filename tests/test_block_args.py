@@ -37,7 +37,7 @@ def test_plan_arguments():
     good = [FAKE, 2 * FAKE, 2, 16, 3 * FAKE, 4, 4 * FAKE, 5 * FAKE, 8, 6 * FAKE, 7 * FAKE,
             8 * FAKE, 9 * FAKE, 10 * FAKE, None]
     for at, bad in ((0, None), (1, None), (2, -1), (3, 0), (3, 17), (4, None), (5, -1), (6, None),
-                    (7, None), (8, -1), (9, None), (10, None), (10, FAKE), (11, None), (12, None),
+                    (7, None), (8, -1), (9, None), (10, None), (10, FAKE), (11, None),
                     (12, 5 * FAKE), (13, None), (13, 5 * FAKE), (13, 9 * FAKE)):
         args = list(good)
         args[at] = bad
