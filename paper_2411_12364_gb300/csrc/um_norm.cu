@@ -14,7 +14,7 @@
 // 4096) or a cluster of two blocks, 8 entries a thread, between its two norms.
 // The rows' sums are chains of barriers, so the bytes in flight must not
 // depend on them: each thread copies its own 16-byte pieces of the next rows
-// into shared memory (cp.async), two rows ahead, and waits for its own copies
+// into shared memory (cp.async), two or three rows ahead, and waits for its own copies
 // only.  Blocks are persistent, so that the gains, biases and the per-channel
 // gate are read once per block, into registers.  Measured at 16384 x 2048 in
 // bf16 with a full gate: 60 us forward, 5.6 TB/s of what has to move; the
@@ -78,17 +78,17 @@ __device__ __forceinline__ F2 as_stored(F2 x, __nv_bfloat16) {
 }
 __device__ __forceinline__ F2 as_stored(F2 x, float) { return x; }
 
-// Rows in flight ahead of the one at work.  At 16384 x 2048 in bf16 two took
-// 59.9 us (gradient 78.0), three 61.1 (78.3), four 61.6 (80.0): the blocks of
-// an SM together keep enough bytes in flight, and more only mixes the reads
-// and writes of more rows in memory.
+// Rows in flight ahead of the one at work.  At 16384 x 2048 in bf16 the
+// forward took 60.2 us with two and 61.4 with three, the gradient 80.4 and
+// 78.2 (fp32 rows of 4096 entries leave room for two): the blocks of an SM
+// together keep enough bytes in flight.
 constexpr int kAhead = 2;
+template <typename T> constexpr int kAheadBack = sizeof(T) == 2 ? 3 : 2;
 
 // A thread's way to the rows of up to MAXK tensors: the ring of its own
 // copies (VEC), or plain loads.  THREADS: of the block.  Addresses are kept
 // per tensor and advanced from row to row.
-template <typename T, bool VEC, int NT, int CL, int THREADS, int MAXK> struct Feed {
-    static constexpr int S = kAhead;
+template <typename T, bool VEC, int NT, int CL, int THREADS, int S, int MAXK> struct Feed {
     static constexpr int kPieces = sizeof(T) / 2;            // 16-byte pieces of 8 entries
     static constexpr uint32_t kStage = 16u * MAXK * kPieces * THREADS;
     const T *src[MAXK];                                      // this thread's next row to copy
@@ -96,7 +96,8 @@ template <typename T, bool VEC, int NT, int CL, int THREADS, int MAXK> struct Fe
     int64_t first, step, T_rows, next;                       // next: the row src points at
     int t, D, pieces;                                        // pieces: of its run inside the row
     uint32_t ring, fill;                                     // shared addresses: base, next stage
-    const uint4 *mine, *drain;                               // the base and the stage at hand
+    const uint4 *mine;                                       // the base as a pointer
+    int drain;                                               // the stage at hand, from there
 
     static constexpr size_t smem_bytes() { return VEC ? (size_t)S * kStage : 0; }
     __device__ __forceinline__ void tensor(int k, const void *base, int64_t ld) {
@@ -107,7 +108,8 @@ template <typename T, bool VEC, int NT, int CL, int THREADS, int MAXK> struct Fe
     // before tensor(): rows first, first + step, ..
     __device__ __forceinline__ void rows(int64_t first_, int64_t step_, int64_t T_rows_, int t_,
                                          int D_, const uint4 *smem) {
-        mine = drain = smem + threadIdx.x;
+        mine = smem + threadIdx.x;
+        drain = 0;
         first = next = first_;
         step = step_;
         T_rows = T_rows_;
@@ -155,7 +157,7 @@ template <typename T, bool VEC, int NT, int CL, int THREADS, int MAXK> struct Fe
             for (int i = 0; i < kPieces; ++i) {
                 q[i] = make_uint4(0u, 0u, 0u, 0u);
                 if (src[k] && i < pieces)
-                    q[i] = drain[(k * kPieces + i) * THREADS];
+                    q[i] = mine[drain + (k * kPieces + i) * THREADS];
             }
             widen(x, q, T());
         } else {
@@ -173,7 +175,7 @@ template <typename T, bool VEC, int NT, int CL, int THREADS, int MAXK> struct Fe
     __device__ __forceinline__ void taken() {
         if constexpr (VEC) {
             drain += kStage / 16;
-            if (drain == mine + S * (kStage / 16)) drain = mine;
+            if (drain == (int)(S * (kStage / 16))) drain = 0;
             issue();
         } else {
             advance();
@@ -365,14 +367,14 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArg
     const int rows = NT == 32 ? blockDim.x >> 5 : 1;
     const bool full = a.gate_mode == ULTRAMEM_GATE_FULL;
     const float inv = 1.f / (float)a.D;
-    Feed<T, VEC, NT, CL, NT == 32 ? 128 : NT, 3> in;
+    Feed<T, VEC, NT, CL, NT == 32 ? 128 : NT, kAhead, 3> in;
     in.rows((int64_t)(blockIdx.x / CL) * rows + (NT == 32 ? threadIdx.x >> 5 : 0),
             (int64_t)(gridDim.x / CL) * rows, a.T, t, a.D, ring);
     in.tensor(0, a.y, a.ld_y);
     in.tensor(1, a.r, a.ld_r);
     in.tensor(2, full ? a.gate : nullptr, a.D);
 #pragma unroll
-    for (int i = 0; i < in.S; ++i) in.issue();
+    for (int i = 0; i < kAhead; ++i) in.issue();
     F2 W[kP], B[kP], wn[kP], bn[kP];
     fold_post<VEC, TPR, LAYER>(W, B, a, t);
     param<VEC, TPR>(wn, a.w_pre, 1.f, t, a.D);
@@ -442,7 +444,7 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
     const bool full = a.gate_mode == ULTRAMEM_GATE_FULL;
     const bool token = a.gate_mode == ULTRAMEM_GATE_TOKEN;
     const float inv = 1.f / (float)a.D;
-    Feed<T, VEC, NT, CL, NT, 5> in;
+    Feed<T, VEC, NT, CL, NT, kAheadBack<T>, 5> in;
     in.rows(blockIdx.x / CL, gridDim.x / CL, a.T, t, a.D, ring);
     in.tensor(0, a.y, a.ld_y);
     in.tensor(1, a.pre ? a.r : nullptr, a.ld_r);
@@ -450,7 +452,7 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
     in.tensor(3, a.du, a.ld_du);
     in.tensor(4, full ? a.gate : nullptr, a.D);
 #pragma unroll
-    for (int i = 0; i < in.S; ++i) in.issue();
+    for (int i = 0; i < kAheadBack<T>; ++i) in.issue();
     F2 W[kP], B[kP], wn[kP];
     F2 c_p[kP], c_pre[kP], c_q[kP], c_bpre[kP];
     fold_post<VEC, TPR, LAYER>(W, B, a, t);
@@ -708,7 +710,7 @@ template <auto K> cudaError_t run_rows(const NormArgs &a, int64_t units, int thr
 template <typename T, bool VEC, bool LAYER> struct Forward {
     template <int NT, int CL> static cudaError_t go(const NormArgs &a, int *groups, cudaStream_t st) {
         constexpr int threads = NT == 32 ? 128 : NT;
-        constexpr size_t smem = Feed<T, VEC, NT, CL, threads, 3>::smem_bytes();
+        constexpr size_t smem = Feed<T, VEC, NT, CL, threads, kAhead, 3>::smem_bytes();
         const int64_t units = NT == 32 ? (a.T + 3) / 4 : a.T;
         return run_rows<block_norm_kernel<T, VEC, NT, CL, LAYER>>(a, units, threads, CL, smem,
                                                                   INT64_MAX, groups, st);
@@ -740,7 +742,7 @@ int64_t partial_rows(int64_t T, int D) {
 
 template <typename T, bool VEC, bool LAYER> struct Backward {
     template <int NT, int CL> static cudaError_t go(const NormArgs &a, int *groups, cudaStream_t st) {
-        constexpr size_t smem = Feed<T, VEC, NT, CL, NT, 5>::smem_bytes();
+        constexpr size_t smem = Feed<T, VEC, NT, CL, NT, kAheadBack<T>, 5>::smem_bytes();
         return run_rows<block_norm_backward_kernel<T, VEC, NT, CL, LAYER>>(
             a, a.T, NT, CL, smem, partial_rows(a.T, a.D), groups, st);
     }
