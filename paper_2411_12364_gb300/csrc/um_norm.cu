@@ -42,14 +42,20 @@ struct NormArgs {
 };
 
 // ---- a row in registers ------------------------------------------------
-// Thread t of the NT CL threads of a row holds 8 entries as 4 pairs.  With
-// 16-byte aligned rows (VEC) these are one run, entries 8 t.., one or two
-// 16-byte accesses; otherwise single entries t + NT CL e, so that a warp's
-// accesses are still consecutive.
+// Thread t of the NT CL threads of a row holds 8 entries as 4 pairs.  Rows on
+// 16-byte boundaries (kRun): one run, entries 8 t.., in one or two 16-byte
+// accesses.  Rows on 4-byte boundaries (kWord: any fp32 row, bf16 rows of even
+// width): 4-byte words t + NT CL i, so that a warp's accesses are still
+// consecutive.  Other bf16 rows (kHalf; every second row of an odd width
+// starts inside a word): the same pairs of entries, from the one or two words
+// that hold them.
+enum { kRun = 16, kWord = 4, kHalf = 2 };
 constexpr int kP = 4;
 
-template <bool VEC, int TPR> __device__ __forceinline__ int col_of(int t, int e) {
-    return VEC ? 8 * t + e : t + TPR * e;
+template <typename T, int MODE, int TPR> __device__ __forceinline__ int col_of(int t, int e) {
+    if constexpr (MODE == kRun) return 8 * t + e;
+    if constexpr (sizeof(T) == 2) return 2 * (t + TPR * (e >> 1)) + (e & 1);
+    return t + TPR * e;
 }
 
 __device__ __forceinline__ void widen(F2 (&x)[kP], const uint4 *q, __nv_bfloat16) {
@@ -80,137 +86,205 @@ __device__ __forceinline__ F2 as_stored(F2 x, float) { return x; }
 
 // Rows in flight ahead of the one at work.  At 16384 x 2048 in bf16 the
 // forward took 60.2 us with two and 61.4 with three, the gradient 80.4 and
-// 78.2 (fp32 rows of 4096 entries leave room for two): the blocks of an SM
-// together keep enough bytes in flight.
+// 78.2 (fp32 and odd rows of 4096 entries leave room for two): the blocks of
+// an SM together keep enough bytes in flight.
 constexpr int kAhead = 2;
-template <typename T> constexpr int kAheadBack = sizeof(T) == 2 ? 3 : 2;
+template <typename T, int MODE>
+constexpr int kAheadBack = sizeof(T) == 2 && MODE != kHalf ? 3 : 2;
 
-// A thread's way to the rows of up to MAXK tensors: the ring of its own
-// copies (VEC), or plain loads.  THREADS: of the block.  Addresses are kept
-// per tensor and advanced from row to row.
-template <typename T, bool VEC, int NT, int CL, int THREADS, int S, int MAXK> struct Feed {
-    static constexpr int kPieces = sizeof(T) / 2;            // 16-byte pieces of 8 entries
-    static constexpr uint32_t kStage = 16u * MAXK * kPieces * THREADS;
+// A thread's way to the rows of up to MAXK tensors: a ring of its own copies
+// in shared memory.  THREADS: of the block.  Addresses are kept per tensor and
+// advanced from row to row.
+template <typename T, int MODE, int NT, int CL, int THREADS, int S, int MAXK> struct Feed {
+    static constexpr int kTpr = NT * CL;
+    static constexpr int kBytes = MODE == kRun ? 16 : 4;                     // of a copy
+    // copies of 8 entries (kHalf: two words a pair)
+    static constexpr int kCopies = MODE == kHalf ? 8 : 8 * (int)sizeof(T) / kBytes;
+    static constexpr int kPer = kBytes / (int)sizeof(T);                     // entries of a copy
+    static constexpr int kApart = MODE == kRun ? kPer : kPer * kTpr;         // entries between copies
+    static constexpr uint32_t kStage = (uint32_t)MAXK * kCopies * kBytes * THREADS;
     const T *src[MAXK];                                      // this thread's next row to copy
     int64_t hop[MAXK];                                       // entries from one of its rows to the next
     int64_t first, step, T_rows, next;                       // next: the row src points at
-    int t, D, pieces;                                        // pieces: of its run inside the row
+    int t, D, copies;                                        // copies: that lie inside the row
     uint32_t ring, fill;                                     // shared addresses: base, next stage
-    const uint4 *mine;                                       // the base as a pointer
+    const char *mine;                                        // the base as a pointer
     int drain;                                               // the stage at hand, from there
+    uint32_t inside, flips;                                  // kHalf: bit k, the row at hand starts
+                                                             // inside a word, and its rows alternate
 
-    static constexpr size_t smem_bytes() { return VEC ? (size_t)S * kStage : 0; }
+    static constexpr size_t smem_bytes() { return (size_t)S * kStage; }
+    __device__ __forceinline__ int start() const {           // of this thread's entries
+        return MODE == kRun ? 8 * t : MODE == kWord ? kPer * t : 0;
+    }
     __device__ __forceinline__ void tensor(int k, const void *base, int64_t ld) {
-        src[k] = base ? static_cast<const T *>(base) + first * ld + (VEC ? (pieces ? 8 * t : 0) : 0)
-                      : nullptr;
+        src[k] = base ? static_cast<const T *>(base) + first * ld + (copies ? start() : 0) : nullptr;
         hop[k] = step * ld;
+        if constexpr (MODE == kHalf) {
+            inside |= (uint32_t)(((uintptr_t)src[k] >> 1) & 1) << k;
+            flips |= (uint32_t)(hop[k] & 1) << k;
+        }
     }
     // before tensor(): rows first, first + step, ..
     __device__ __forceinline__ void rows(int64_t first_, int64_t step_, int64_t T_rows_, int t_,
-                                         int D_, const uint4 *smem) {
-        mine = smem + threadIdx.x;
-        drain = 0;
+                                         int D_, void *smem) {
         first = next = first_;
         step = step_;
         T_rows = T_rows_;
         t = t_;
         D = D_;
-        // fp32 rows of 4 mod 8 entries end inside a run
-        pieces = VEC ? max(0, min(kPieces, (D - 8 * t) / (int)(16 / sizeof(T)))) : 0;
-        ring = fill = (uint32_t)__cvta_generic_to_shared(smem) + 16u * threadIdx.x;
+        copies = 0;
+        inside = flips = 0;
+        if constexpr (MODE != kHalf)
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) copies += start() + i * kApart < D ? 1 : 0;
+        mine = static_cast<char *>(smem) + kBytes * threadIdx.x;
+        drain = 0;
+        ring = fill = (uint32_t)__cvta_generic_to_shared(mine);
     }
     // starts the copies of this thread's next row
     __device__ __forceinline__ void issue() {
-        if constexpr (VEC) {
-            if (next < T_rows && pieces) {
+        if (next < T_rows) {
 #pragma unroll
-                for (int k = 0; k < MAXK; ++k)
-                    if (src[k])
+            for (int k = 0; k < MAXK; ++k) {
+                if (!src[k]) continue;
+                const uint32_t dst = fill + k * kCopies * THREADS * kBytes;
+                if constexpr (MODE == kHalf) {
+                    copy_pairs(dst, src[k]);
+                } else {
 #pragma unroll
-                        for (int i = 0; i < kPieces; ++i)
-                            if (kPieces == 1 || i < pieces)
-                                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(
-                                                 fill + 16u * (k * kPieces + i) * THREADS),
-                                             "l"(src[k] + 16 / sizeof(T) * i)
-                                             : "memory");
+                    for (int i = 0; i < kCopies; ++i)
+                        if (i < copies) copy(dst + i * THREADS * kBytes, src[k] + i * kApart);
+                }
+                src[k] += hop[k];
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            advance();
-            next += step;
-            fill += kStage;
-            if (fill == ring + S * kStage) fill = ring;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        next += step;
+        fill += kStage;
+        if (fill == ring + S * kStage) fill = ring;
+    }
+    __device__ __forceinline__ static void copy(uint32_t dst, const void *from) {
+        if constexpr (kBytes == 16)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(from)
+                         : "memory");
+        else
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(from)
+                         : "memory");
+    }
+    // The words of pair t + kTpr i.  A row that starts inside a word shares its
+    // first word with what precedes it, and the last word may reach past the
+    // row's end: neither outer half is read unless it is the row's own or
+    // (before a later row's start) the previous row's.
+    __device__ __forceinline__ void copy_pairs(uint32_t dst, const T *row) const {
+        const bool in = ((uintptr_t)row >> 1) & 1;
+        const char *word = reinterpret_cast<const char *>((uintptr_t)row & ~(uintptr_t)3);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int q = t + kTpr * i;
+            if (2 * q >= D) break;
+            const uint32_t lo = dst + 2 * i * THREADS * 4, hi = lo + THREADS * 4;
+            if (in && q == 0) {              // the entry alone, in the word's upper half
+                const uint32_t x = (uint32_t)*reinterpret_cast<const uint16_t *>(row) << 16;
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(lo), "r"(x) : "memory");
+            } else if (!in && 2 * q + 1 >= D) {   // the entry alone, in the lower half
+                const uint32_t x = *reinterpret_cast<const uint16_t *>(row + 2 * q);
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(lo), "r"(x) : "memory");
+            } else {
+                copy(lo, word + 4 * (int64_t)q);
+            }
+            if (in && 2 * q + 1 < D) {
+                if (2 * q + 2 >= D) {        // the pair's second entry ends the row
+                    const uint32_t x = *reinterpret_cast<const uint16_t *>(row + 2 * q + 1);
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(hi), "r"(x) : "memory");
+                } else {
+                    copy(hi, word + 4 * (int64_t)q + 4);
+                }
+            }
         }
     }
-    __device__ __forceinline__ void advance() {
-#pragma unroll
-        for (int k = 0; k < MAXK; ++k)
-            if (src[k]) src[k] += hop[k];
-    }
     __device__ __forceinline__ void wait() {
-        if constexpr (VEC) asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
     }
     // the row's entries of tensor k (zeros past D and without a tensor)
     __device__ __forceinline__ void take(F2 (&x)[kP], int k) {
-        if constexpr (VEC) {
-            uint4 q[kPieces];
+        const char *from = mine + drain + k * kCopies * THREADS * kBytes;
+        if constexpr (MODE == kRun) {
+            uint4 q[kCopies];
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
+            for (int i = 0; i < kCopies; ++i) {
                 q[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (src[k] && i < pieces)
-                    q[i] = mine[drain + (k * kPieces + i) * THREADS];
+                if (src[k] && i < copies)
+                    q[i] = *reinterpret_cast<const uint4 *>(from + i * THREADS * kBytes);
             }
             widen(x, q, T());
         } else {
-            float v[2 * kP];
+            uint32_t q[kCopies];
 #pragma unroll
-            for (int e = 0; e < 2 * kP; ++e) {
-                const int c = t + NT * CL * e;
-                v[e] = src[k] && c < D ? to_f(src[k][c]) : 0.f;
+            for (int i = 0; i < kCopies; ++i) {
+                // kHalf: words 2 i and 2 i + 1 of pair i, the second for entries of
+                // a row that starts inside a word
+                const bool have = MODE == kHalf
+                    ? 2 * (t + kTpr * (i >> 1)) + (i & 1) < D && (!(i & 1) || (inside >> k & 1))
+                    : i < copies;
+                q[i] = 0u;
+                if (src[k] && have)
+                    q[i] = *reinterpret_cast<const uint32_t *>(from + i * THREADS * kBytes);
             }
 #pragma unroll
-            for (int e = 0; e < kP; ++e) x[e] = f2(v[2 * e], v[2 * e + 1]);
+            for (int e = 0; e < kP; ++e) {
+                if constexpr (sizeof(T) == 4) {
+                    x[e] = f2(__uint_as_float(q[2 * e]), __uint_as_float(q[2 * e + 1]));
+                } else {
+                    uint32_t v = q[MODE == kHalf ? 2 * e : e];
+                    if (MODE == kHalf && (inside >> k & 1)) v = __funnelshift_r(v, q[2 * e + 1], 16);
+                    x[e] = f2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+                }
+            }
         }
     }
     // the row is taken: its place gets a further row
     __device__ __forceinline__ void taken() {
-        if constexpr (VEC) {
-            drain += kStage / 16;
-            if (drain == (int)(S * (kStage / 16))) drain = 0;
-            issue();
-        } else {
-            advance();
-        }
+        drain += kStage;
+        if (drain == (int)(S * kStage)) drain = 0;
+        if constexpr (MODE == kHalf) inside ^= flips;
+        issue();
     }
     // a contiguous output's row, dst its start
     __device__ __forceinline__ void put(T *dst, const F2 (&x)[kP]) const {
-        if constexpr (VEC && sizeof(T) == 2) {
-            if (pieces)
+        if constexpr (MODE == kRun && sizeof(T) == 2) {
+            if (copies)
                 *reinterpret_cast<uint4 *>(dst + 8 * t) =
                     make_uint4(pack(x[0]), pack(x[1]), pack(x[2]), pack(x[3]));
-        } else if constexpr (VEC) {
+        } else if constexpr (MODE == kRun) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                if (i < pieces) {
+                if (i < copies) {
                     const float2 lo = split(x[2 * i]), hi = split(x[2 * i + 1]);
                     *reinterpret_cast<float4 *>(dst + 8 * t + 4 * i) =
                         make_float4(lo.x, lo.y, hi.x, hi.y);
                 }
+        } else if constexpr (MODE == kWord && sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < kP; ++i)
+                if (i < copies)
+                    *reinterpret_cast<uint32_t *>(dst + 2 * (t + kTpr * i)) = pack(x[i]);
         } else {
 #pragma unroll
             for (int e = 0; e < kP; ++e) {
                 const float2 v = split(x[e]);
-                const int c = t + NT * CL * 2 * e;
-                if (c < D) dst[c] = from_f<T>(v.x);
-                if (c + NT * CL < D) dst[c + NT * CL] = from_f<T>(v.y);
+                const int c0 = col_of<T, MODE, kTpr>(t, 2 * e), c1 = col_of<T, MODE, kTpr>(t, 2 * e + 1);
+                if (c0 < D) dst[c0] = from_f<T>(v.x);
+                if (c1 < D) dst[c1] = from_f<T>(v.y);
             }
         }
     }
 };
 
 // a parameter vector, or `fill` everywhere without one; zeros past D
-template <bool VEC, int TPR>
+template <typename T, int MODE, int TPR>
 __device__ __forceinline__ void param(F2 (&x)[kP], const float *p, float fill, int t, int D) {
-    if constexpr (VEC) {
+    if constexpr (MODE == kRun) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -224,7 +298,7 @@ __device__ __forceinline__ void param(F2 (&x)[kP], const float *p, float fill, i
         float v[2 * kP];
 #pragma unroll
         for (int e = 0; e < 2 * kP; ++e) {
-            const int c = t + TPR * e;
+            const int c = col_of<T, MODE, TPR>(t, e);
             v[e] = c < D ? (p ? p[c] : fill) : 0.f;
         }
 #pragma unroll
@@ -233,13 +307,14 @@ __device__ __forceinline__ void param(F2 (&x)[kP], const float *p, float fill, i
 }
 
 // clears the entries past D
-template <bool VEC, int TPR> __device__ __forceinline__ void clip(F2 (&x)[kP], int t, int D) {
-    if (col_of<VEC, TPR>(t, 7) < D) return;   // the thread's last entry is its largest column
+template <typename T, int MODE, int TPR>
+__device__ __forceinline__ void clip(F2 (&x)[kP], int t, int D) {
+    if (col_of<T, MODE, TPR>(t, 7) < D) return;   // the thread's last entry is its largest column
 #pragma unroll
     for (int e = 0; e < kP; ++e) {
         const float2 v = split(x[e]);
-        x[e] = f2(col_of<VEC, TPR>(t, 2 * e) < D ? v.x : 0.f,
-                  col_of<VEC, TPR>(t, 2 * e + 1) < D ? v.y : 0.f);
+        x[e] = f2(col_of<T, MODE, TPR>(t, 2 * e) < D ? v.x : 0.f,
+                  col_of<T, MODE, TPR>(t, 2 * e + 1) < D ? v.y : 0.f);
     }
 }
 
@@ -314,7 +389,7 @@ template <int NT, int CL> struct RowSum {
 
 // x <- the normalised row (entries past D stay 0); the mean (layer) is
 // subtracted before the squares are summed, so nothing cancels
-template <bool VEC, int NT, int CL, bool LAYER, typename Sum>
+template <typename T, int MODE, int NT, int CL, bool LAYER, typename Sum>
 __device__ __forceinline__ void normalise(F2 (&x)[kP], int D, float inv, float eps, int t,
                                           Sum &sum) {
     float s[1];
@@ -324,7 +399,7 @@ __device__ __forceinline__ void normalise(F2 (&x)[kP], int D, float inv, float e
         const F2 mean = f2(-s[0] * inv);
 #pragma unroll
         for (int e = 0; e < kP; ++e) x[e] = x[e] + mean;
-        clip<VEC, NT * CL>(x, t, D);
+        clip<T, MODE, NT * CL>(x, t, D);
     }
     F2 q = x[0] * x[0];
 #pragma unroll
@@ -339,13 +414,13 @@ __device__ __forceinline__ void normalise(F2 (&x)[kP], int D, float inv, float e
 // What the first norm's gain and bias, the per-channel gate and the output's
 // scale make of a normalised row, as one factor and one offset a channel:
 // out_scale gate (.) (w x + b) = W x + B.  (x itself without the first norm.)
-template <bool VEC, int TPR, bool LAYER>
+template <typename T, int MODE, int TPR, bool LAYER>
 __device__ __forceinline__ void fold_post(F2 (&W)[kP], F2 (&B)[kP], const NormArgs &a, int t) {
     F2 g[kP];
     const bool channel = a.gate_mode == ULTRAMEM_GATE_CHANNEL;
-    param<VEC, TPR>(g, channel ? static_cast<const float *>(a.gate) : nullptr, 1.f, t, a.D);
-    param<VEC, TPR>(W, a.post ? a.w_post : nullptr, 1.f, t, a.D);
-    if constexpr (LAYER) param<VEC, TPR>(B, a.post ? a.b_post : nullptr, 0.f, t, a.D);
+    param<T, MODE, TPR>(g, channel ? static_cast<const float *>(a.gate) : nullptr, 1.f, t, a.D);
+    param<T, MODE, TPR>(W, a.post ? a.w_post : nullptr, 1.f, t, a.D);
+    if constexpr (LAYER) param<T, MODE, TPR>(B, a.post ? a.b_post : nullptr, 0.f, t, a.D);
     const F2 s = f2(a.out_scale);
 #pragma unroll
     for (int e = 0; e < kP; ++e) {
@@ -356,7 +431,7 @@ __device__ __forceinline__ void fold_post(F2 (&W)[kP], F2 (&B)[kP], const NormAr
 }
 
 // A row per NT CL threads, grid-stride; rows of one warp go four to a block.
-template <typename T, bool VEC, int NT, int CL, bool LAYER>
+template <typename T, int MODE, int NT, int CL, bool LAYER>
 __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArgs a) {
     constexpr int TPR = NT * CL;
     extern __shared__ uint4 ring[];
@@ -367,7 +442,7 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArg
     const int rows = NT == 32 ? blockDim.x >> 5 : 1;
     const bool full = a.gate_mode == ULTRAMEM_GATE_FULL;
     const float inv = 1.f / (float)a.D;
-    Feed<T, VEC, NT, CL, NT == 32 ? 128 : NT, kAhead, 3> in;
+    Feed<T, MODE, NT, CL, NT == 32 ? 128 : NT, kAhead, 3> in;
     in.rows((int64_t)(blockIdx.x / CL) * rows + (NT == 32 ? threadIdx.x >> 5 : 0),
             (int64_t)(gridDim.x / CL) * rows, a.T, t, a.D, ring);
     in.tensor(0, a.y, a.ld_y);
@@ -376,9 +451,9 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArg
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) in.issue();
     F2 W[kP], B[kP], wn[kP], bn[kP];
-    fold_post<VEC, TPR, LAYER>(W, B, a, t);
-    param<VEC, TPR>(wn, a.w_pre, 1.f, t, a.D);
-    if constexpr (LAYER) param<VEC, TPR>(bn, a.b_pre, 0.f, t, a.D);
+    fold_post<T, MODE, TPR, LAYER>(W, B, a, t);
+    param<T, MODE, TPR>(wn, a.w_pre, 1.f, t, a.D);
+    if constexpr (LAYER) param<T, MODE, TPR>(bn, a.b_pre, 0.f, t, a.D);
     const F2 res = f2(a.res_scale);
     T *u_row = static_cast<T *>(a.u) + in.first * a.D, *n_row = nullptr;
     if (a.pre) n_row = static_cast<T *>(a.n) + in.first * a.D;
@@ -390,7 +465,7 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArg
         in.take(u, 1);
         if (full) in.take(g, 2);
         in.taken();
-        if (a.post) normalise<VEC, NT, CL, LAYER>(z, a.D, inv, a.eps, t, sum);
+        if (a.post) normalise<T, MODE, NT, CL, LAYER>(z, a.D, inv, a.eps, t, sum);
 #pragma unroll
         for (int e = 0; e < kP; ++e) z[e] = LAYER ? fma2(z[e], W[e], B[e]) : z[e] * W[e];
         if (full) {
@@ -409,7 +484,7 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArg
             // gradient taken from the stored stream is that of this function.
 #pragma unroll
             for (int e = 0; e < kP; ++e) u[e] = as_stored(u[e], T());
-            normalise<VEC, NT, CL, LAYER>(u, a.D, inv, a.eps, t, sum);
+            normalise<T, MODE, NT, CL, LAYER>(u, a.D, inv, a.eps, t, sum);
 #pragma unroll
             for (int e = 0; e < kP; ++e) u[e] = LAYER ? fma2(u[e], wn[e], bn[e]) : u[e] * wn[e];
             in.put(n_row, u);
@@ -433,7 +508,7 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArg
 // the schedule).
 enum { kColP, kColPre, kColQ, kColBPre };   // order of the partial rows (the last two: layer)
 
-template <typename T, bool VEC, int NT, int CL, bool LAYER>
+template <typename T, int MODE, int NT, int CL, bool LAYER>
 __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
     block_norm_backward_kernel(NormArgs a) {
     constexpr int TPR = NT * CL;
@@ -444,7 +519,7 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
     const bool full = a.gate_mode == ULTRAMEM_GATE_FULL;
     const bool token = a.gate_mode == ULTRAMEM_GATE_TOKEN;
     const float inv = 1.f / (float)a.D;
-    Feed<T, VEC, NT, CL, NT, kAheadBack<T>, 5> in;
+    Feed<T, MODE, NT, CL, NT, kAheadBack<T, MODE>, 5> in;
     in.rows(blockIdx.x / CL, gridDim.x / CL, a.T, t, a.D, ring);
     in.tensor(0, a.y, a.ld_y);
     in.tensor(1, a.pre ? a.r : nullptr, a.ld_r);
@@ -452,11 +527,11 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
     in.tensor(3, a.du, a.ld_du);
     in.tensor(4, full ? a.gate : nullptr, a.D);
 #pragma unroll
-    for (int i = 0; i < kAheadBack<T>; ++i) in.issue();
+    for (int i = 0; i < kAheadBack<T, MODE>; ++i) in.issue();
     F2 W[kP], B[kP], wn[kP];
     F2 c_p[kP], c_pre[kP], c_q[kP], c_bpre[kP];
-    fold_post<VEC, TPR, LAYER>(W, B, a, t);
-    param<VEC, TPR>(wn, a.w_pre, 1.f, t, a.D);
+    fold_post<T, MODE, TPR, LAYER>(W, B, a, t);
+    param<T, MODE, TPR>(wn, a.w_pre, 1.f, t, a.D);
 #pragma unroll
     for (int e = 0; e < kP; ++e) c_p[e] = c_pre[e] = c_q[e] = c_bpre[e] = f2(0.f);
     const F2 res = f2(a.res_scale);
@@ -497,8 +572,8 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
                 y[e] = y[e] + my;
                 u[e] = u[e] + mu;
             }
-            clip<VEC, TPR>(y, t, a.D);
-            clip<VEC, TPR>(u, t, a.D);
+            clip<T, MODE, TPR>(y, t, a.D);
+            clip<T, MODE, TPR>(u, t, a.D);
         }
         {
             F2 q0 = y[0] * y[0], q1 = u[0] * u[0], q2 = wd[0] * u[0];
@@ -528,7 +603,7 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
             y[e] = y[e] * ry2;                 // from here the normalised row
             u[e] = res * gu[e];
         }
-        if constexpr (LAYER) clip<VEC, TPR>(gu, t, a.D);
+        if constexpr (LAYER) clip<T, MODE, TPR>(gu, t, a.D);
         if (dr_row) {
             in.put(dr_row, u);
             dr_row += hop;
@@ -585,7 +660,7 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
     float *part = a.part + (int64_t)(blockIdx.x / CL) * (LAYER ? 4 : 2) * a.D;
     auto leave = [&](int k, const F2 (&c)[kP]) {
         float *dst = part + (int64_t)k * a.D;
-        if constexpr (VEC) {
+        if constexpr (MODE == kRun) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (8 * t + 4 * i < a.D) {
@@ -597,9 +672,9 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
 #pragma unroll
             for (int e = 0; e < kP; ++e) {
                 const float2 v = split(c[e]);
-                const int at = t + TPR * 2 * e;
-                if (at < a.D) dst[at] = v.x;
-                if (at + TPR < a.D) dst[at + TPR] = v.y;
+                const int x = col_of<T, MODE, TPR>(t, 2 * e), y = col_of<T, MODE, TPR>(t, 2 * e + 1);
+                if (x < a.D) dst[x] = v.x;
+                if (y < a.D) dst[y] = v.y;
             }
         }
     };
@@ -707,12 +782,12 @@ template <auto K> cudaError_t run_rows(const NormArgs &a, int64_t units, int thr
     return cudaLaunchKernelEx(&cfg, K, a);
 }
 
-template <typename T, bool VEC, bool LAYER> struct Forward {
+template <typename T, int MODE, bool LAYER> struct Forward {
     template <int NT, int CL> static cudaError_t go(const NormArgs &a, int *groups, cudaStream_t st) {
         constexpr int threads = NT == 32 ? 128 : NT;
-        constexpr size_t smem = Feed<T, VEC, NT, CL, threads, kAhead, 3>::smem_bytes();
+        constexpr size_t smem = Feed<T, MODE, NT, CL, threads, kAhead, 3>::smem_bytes();
         const int64_t units = NT == 32 ? (a.T + 3) / 4 : a.T;
-        return run_rows<block_norm_kernel<T, VEC, NT, CL, LAYER>>(a, units, threads, CL, smem,
+        return run_rows<block_norm_kernel<T, MODE, NT, CL, LAYER>>(a, units, threads, CL, smem,
                                                                   INT64_MAX, groups, st);
     }
     static cudaError_t launch(const NormArgs &a, int *groups, cudaStream_t st) {
@@ -740,10 +815,10 @@ int64_t partial_rows(int64_t T, int D) {
     return n < most ? n : most;
 }
 
-template <typename T, bool VEC, bool LAYER> struct Backward {
+template <typename T, int MODE, bool LAYER> struct Backward {
     template <int NT, int CL> static cudaError_t go(const NormArgs &a, int *groups, cudaStream_t st) {
-        constexpr size_t smem = Feed<T, VEC, NT, CL, NT, kAheadBack<T>, 5>::smem_bytes();
-        return run_rows<block_norm_backward_kernel<T, VEC, NT, CL, LAYER>>(
+        constexpr size_t smem = Feed<T, MODE, NT, CL, NT, kAheadBack<T, MODE>, 5>::smem_bytes();
+        return run_rows<block_norm_backward_kernel<T, MODE, NT, CL, LAYER>>(
             a, a.T, NT, CL, smem, partial_rows(a.T, a.D), groups, st);
     }
     static cudaError_t launch(const NormArgs &a, int *groups, cudaStream_t st) {
@@ -759,21 +834,24 @@ template <typename T, bool VEC, bool LAYER> struct Backward {
 };
 
 // groups: the blocks (or clusters) launched
-template <template <typename, bool, bool> class Op>
-cudaError_t dispatch(const NormArgs &a, int dtype, bool layer, bool vec, int *groups,
+template <template <typename, int, bool> class Op>
+cudaError_t dispatch(const NormArgs &a, int dtype, bool layer, int mode, int *groups,
                      cudaStream_t st) {
-    if (dtype == ULTRAMEM_BF16) {
-        if (vec)
-            return layer ? Op<__nv_bfloat16, true, true>::launch(a, groups, st)
-                         : Op<__nv_bfloat16, true, false>::launch(a, groups, st);
-        return layer ? Op<__nv_bfloat16, false, true>::launch(a, groups, st)
-                     : Op<__nv_bfloat16, false, false>::launch(a, groups, st);
-    }
-    if (vec)
-        return layer ? Op<float, true, true>::launch(a, groups, st)
-                     : Op<float, true, false>::launch(a, groups, st);
-    return layer ? Op<float, false, true>::launch(a, groups, st)
-                 : Op<float, false, false>::launch(a, groups, st);
+    using B = __nv_bfloat16;
+    if (dtype == ULTRAMEM_BF16 && mode == kRun)
+        return layer ? Op<B, kRun, true>::launch(a, groups, st)
+                     : Op<B, kRun, false>::launch(a, groups, st);
+    if (dtype == ULTRAMEM_BF16 && mode == kWord)
+        return layer ? Op<B, kWord, true>::launch(a, groups, st)
+                     : Op<B, kWord, false>::launch(a, groups, st);
+    if (dtype == ULTRAMEM_BF16)
+        return layer ? Op<B, kHalf, true>::launch(a, groups, st)
+                     : Op<B, kHalf, false>::launch(a, groups, st);
+    if (mode == kRun)
+        return layer ? Op<float, kRun, true>::launch(a, groups, st)
+                     : Op<float, kRun, false>::launch(a, groups, st);
+    return layer ? Op<float, kWord, true>::launch(a, groups, st)
+                 : Op<float, kWord, false>::launch(a, groups, st);
 }
 
 bool valid(const ultramem_block_norm_args *p) {
@@ -813,16 +891,17 @@ NormArgs args_of(const ultramem_block_norm_args *p) {
     return a;
 }
 
-// rows of whole 16-byte words that start on 16-byte boundaries
-bool rows_aligned(int dtype, int D, std::initializer_list<const void *> ptrs,
-                  std::initializer_list<int64_t> lds) {
-    const int per = dtype == ULTRAMEM_BF16 ? 8 : 4;
-    if (D % per) return false;
-    for (const void *p : ptrs)
-        if (!aligned16(p)) return false;
-    for (int64_t ld : lds)
-        if (ld % per) return false;
-    return true;
+// The widest access that all rows allow: `rows` and `lds` are the row tensors
+// and their row distances, `vectors` fp32 vectors that kRun reads by 16 bytes.
+int mode_of(int dtype, int D, std::initializer_list<const void *> rows,
+            std::initializer_list<int64_t> lds, std::initializer_list<const void *> vectors) {
+    const int es = dtype == ULTRAMEM_BF16 ? 2 : 4;
+    uintptr_t low = (uintptr_t)D * es;
+    for (const void *p : rows) low |= (uintptr_t)p;
+    for (int64_t ld : lds) low |= (uintptr_t)(ld * es);
+    uintptr_t wide = low;
+    for (const void *p : vectors) wide |= (uintptr_t)p;
+    return wide % 16 == 0 ? kRun : low % 4 == 0 ? kWord : kHalf;
 }
 
 }  // namespace
@@ -839,14 +918,14 @@ extern "C" ultramem_status ultramem_block_norm(const ultramem_block_norm_args *p
     a.r = r;
     a.u = u;
     a.n = n;
-    const void *channel_or_full = p->gate_mode == ULTRAMEM_GATE_TOKEN ? nullptr : p->gate;
-    const bool vec = um::rows_aligned(p->dtype, p->dim, {p->y, r, u, n, p->w_post, p->b_post, p->w_pre, p->b_pre,
-                                       channel_or_full},
-                                      {p->ld_y, p->ld_r});
+    const void *full = p->gate_mode == ULTRAMEM_GATE_FULL ? p->gate : nullptr;
+    const void *channel = p->gate_mode == ULTRAMEM_GATE_CHANNEL ? p->gate : nullptr;
+    const int mode = um::mode_of(p->dtype, p->dim, {p->y, r, u, n, full}, {p->ld_y, p->ld_r},
+                                 {p->w_post, p->b_post, p->w_pre, p->b_pre, channel});
     cudaGetLastError();
     int groups = 0;
     return um::status_from_cuda(um::dispatch<um::Forward>(
-        a, p->dtype, p->kind == ULTRAMEM_NORM_LAYER, vec, &groups, (cudaStream_t)stream));
+        a, p->dtype, p->kind == ULTRAMEM_NORM_LAYER, mode, &groups, (cudaStream_t)stream));
 }
 
 extern "C" int64_t ultramem_block_norm_backward_workspace(int64_t n_tokens, int32_t dim) {
@@ -896,14 +975,15 @@ extern "C" ultramem_status ultramem_block_norm_backward(
     a.dgate_rows = channel_gate ? nullptr : dgate;
     a.part = static_cast<float *>(workspace);
     const bool full = p->gate_mode == ULTRAMEM_GATE_FULL;
-    const bool vec = um::rows_aligned(
+    const void *channel = p->gate_mode == ULTRAMEM_GATE_CHANNEL ? p->gate : nullptr;
+    const int mode = um::mode_of(
         p->dtype, D,
-        {p->y, p->pre ? u : nullptr, du, dn, dy, dr, p->w_post, p->b_post, p->w_pre, p->b_pre,
-         p->gate_mode == ULTRAMEM_GATE_TOKEN ? nullptr : p->gate, full ? dgate : nullptr},
-        {p->ld_y, p->pre ? p->ld_r : 0, du ? ld_du : 0, dn ? ld_dn : 0});
+        {p->y, p->pre ? u : nullptr, du, dn, dy, dr, full ? p->gate : nullptr, full ? dgate : nullptr},
+        {p->ld_y, p->pre ? p->ld_r : 0, du ? ld_du : 0, dn ? ld_dn : 0},
+        {p->w_post, p->b_post, p->w_pre, p->b_pre, channel});
     const bool layer = p->kind == ULTRAMEM_NORM_LAYER;
     int groups = 0;
-    cudaError_t e = um::dispatch<um::Backward>(a, p->dtype, layer, vec, &groups, st);
+    cudaError_t e = um::dispatch<um::Backward>(a, p->dtype, layer, mode, &groups, st);
     if (e != cudaSuccess) return um::status_from_cuda(e);
     bool any = false;
     for (float *o : sums) any = any || o;

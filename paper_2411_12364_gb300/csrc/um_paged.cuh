@@ -10,7 +10,9 @@
 // order (request, head, tile), form one axis.  CTA c of C takes the
 // c-th of C equal shares of that axis, so the CTAs finish together whatever
 // the requests' lengths are, without any table made on the host.  A share
-// boundary inside a tile is moved to the next block of KB keys.  A tile that
+// boundary inside a tile is moved to the next block of KB keys, and a tile of
+// at most twice its fixed cost in keys is not split (its halves would cost
+// more than they save) but goes with the share it starts in.  A tile that
 // lies in one share is written straight to the output; one that crosses
 // shares leaves a partial (maximum, sum, unnormalised output) per share,
 // which the join kernels add in share order.
@@ -179,7 +181,15 @@ struct Walk {
                 }
             }
             const int keys = q.keys(c.t, a.tq);
-            const int64_t len = (int64_t)keys + a.extra, take = min(c.left, len - c.off);
+            const bool whole = keys <= 2 * a.extra;
+            const int64_t len = (int64_t)keys + a.extra;
+            if (whole && c.off > 0) {        // begun and finished by an earlier share
+                c.left -= len - c.off;
+                c.off = 0;
+                ++c.t;
+                continue;
+            }
+            const int64_t take = whole ? len : min(c.left, len - c.off);
             tok0 = q.tok0 + c.t * a.tq;
             n_tok = min(a.tq, q.n - c.t * a.tq);
             h = c.h;

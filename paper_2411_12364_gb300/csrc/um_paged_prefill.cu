@@ -150,7 +150,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     using C = Cfg<DP>;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t kv_full[C::kStages], kv_empty[C::kStages], kv_raw[C::kStages];
-    __shared__ uint64_t q_full, q_empty, s_full[2], p_most[2], p_full[2], o_full[2], turn[2], drained[2];
+    __shared__ uint64_t q_full, q_empty, s_full[2], p_most[2], p_full[2], o_full[2], turn[2];
+    __shared__ uint64_t drained[2];
     __shared__ int64_t scratch[kThreads / 32 + 1];
     __shared__ Cursor cur;
     __shared__ uint32_t tmem_base;
@@ -254,7 +255,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                             uint32_t x[16];
                             tc::tmem_ld16(to + 16 * c, o);
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(o[k] * f);
+                            for (int k = 0; k < 16; ++k) {
+                                asm volatile("" : "+f"(o[k]));   // after the load's wait
+                                x[k] = __float_as_uint(o[k] * f);
+                            }
                             tmem_st16(to + 16 * c, x);
                         }
                     }
