@@ -101,7 +101,6 @@ template <typename T, int MODE, int NT, int CL, int THREADS, int S, int MAXK> st
     // copies of 8 entries (kHalf: two words a pair)
     static constexpr int kCopies = MODE == kHalf ? 8 : 8 * (int)sizeof(T) / kBytes;
     static constexpr int kPer = kBytes / (int)sizeof(T);                     // entries of a copy
-    static constexpr int kApart = MODE == kRun ? kPer : kPer * kTpr;         // entries between copies
     static constexpr uint32_t kStage = (uint32_t)MAXK * kCopies * kBytes * THREADS;
     const T *src[MAXK];                                      // this thread's next row to copy
     int64_t hop[MAXK];                                       // entries from one of its rows to the next
@@ -114,6 +113,8 @@ template <typename T, int MODE, int NT, int CL, int THREADS, int S, int MAXK> st
                                                              // inside a word, and its rows alternate
 
     static constexpr size_t smem_bytes() { return (size_t)S * kStage; }
+    // entries between a thread's copies
+    __device__ static constexpr int apart() { return MODE == kRun ? kPer : kPer * kTpr; }
     __device__ __forceinline__ int start() const {           // of this thread's entries
         return MODE == kRun ? 8 * t : MODE == kWord ? kPer * t : 0;
     }
@@ -137,7 +138,7 @@ template <typename T, int MODE, int NT, int CL, int THREADS, int S, int MAXK> st
         inside = flips = 0;
         if constexpr (MODE != kHalf)
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i) copies += start() + i * kApart < D ? 1 : 0;
+            for (int i = 0; i < kCopies; ++i) copies += start() + i * apart() < D ? 1 : 0;
         mine = static_cast<char *>(smem) + kBytes * threadIdx.x;
         drain = 0;
         ring = fill = (uint32_t)__cvta_generic_to_shared(mine);
@@ -154,7 +155,7 @@ template <typename T, int MODE, int NT, int CL, int THREADS, int S, int MAXK> st
                 } else {
 #pragma unroll
                     for (int i = 0; i < kCopies; ++i)
-                        if (i < copies) copy(dst + i * THREADS * kBytes, src[k] + i * kApart);
+                        if (i < copies) copy(dst + i * THREADS * kBytes, src[k] + i * apart());
                 }
                 src[k] += hop[k];
             }

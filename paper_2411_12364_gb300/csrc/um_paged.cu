@@ -174,95 +174,158 @@ __global__ void __launch_bounds__(256) append_kernel(const W *k, const W *v, int
 }
 
 // ---- attention, CUDA cores --------------------------------------------------
-// fp32 storage, and bf16 heads wider than the tensor-core kernels take.  A
-// block holds a tile of ROWS rows and walks its keys in blocks of kKeys: the
-// scores of the block by dot products from shared memory, the running maximum
-// and sum of each row, the values added into registers.  Bound by the fp32
-// pipes (and at few rows by shared-memory reads); sums are fp32 throughout.
-constexpr int kKeys = 32;
+// fp32 storage, and bf16 heads that the tensor-core kernels do not take.  A
+// block holds a tile of ROWS rows and walks its keys in blocks of kKeys, which
+// cp.async brings in as stored, one block ahead: the scores by dot products
+// from shared memory, the running maximum and sum of each row, the values
+// added into registers.  Sums are fp32 throughout.
+//
+// What bounds it: reads of shared memory and the fp32 pipes.  Many rows (64)
+// share every read among 8 rows of a warp; a thread accumulates 4 rows x 4 ND
+// columns.  Few rows (8, 16: single tokens) leave nothing to share, so there
+// the threads of one column group split the keys between them, each with all
+// rows, and add up at the tile's end.
 constexpr int kThreads = 256;
 
-template <int ROWS> __host__ __device__ constexpr size_t rows_smem(int dp) {
-    // q [ROWS][dp + 4], k [kKeys][dp + 4], v [kKeys][dp], p [ROWS][kKeys + 1]
-    return sizeof(float) * ((size_t)(ROWS + kKeys) * (dp + 4) + (size_t)kKeys * dp +
-                            (size_t)ROWS * (kKeys + 1));
+template <typename T, int ROWS, int ND> struct RowsCfg {
+    static constexpr int DP = 64 * ND;
+    static constexpr int kKeys = ND <= 2 ? 64 : 32;
+    static constexpr bool kFew = ROWS <= 16;
+    static constexpr int kPitch = DP * (int)sizeof(T) + 16;      // of a key, bytes
+    static constexpr int kLdQ = DP + 4, kLdP = ROWS + 4;         // floats
+    static_assert(kKeys * DP * (int)sizeof(T) / 16 % kThreads == 0, "whole rounds of copies");
+    static constexpr int kQuads = 16 * ND;                       // groups of 4 columns
+    static constexpr int kGroups = kFew ? kThreads / kQuads : 1; // that split the keys
+    static constexpr size_t kStage = (size_t)2 * kKeys * kPitch; // K and V of a block
+    static constexpr size_t kJoin = kFew ? (size_t)kGroups * ROWS * DP * 4 : 0;
+    static constexpr size_t kRing = 2 * kStage > kJoin ? 2 * kStage : kJoin;
+    static constexpr size_t kSmem =
+        sizeof(float) * ((size_t)ROWS * kLdQ + (size_t)kKeys * kLdP) + kRing;
+    static constexpr int kPerSm = kSmem <= 115000 ? 2 : 1;
+};
+
+__device__ __forceinline__ float4 load4(const float *p) {
+    return *reinterpret_cast<const float4 *>(p);
+}
+__device__ __forceinline__ float4 load4(const __nv_bfloat16 *p) {
+    const uint2 q = *reinterpret_cast<const uint2 *>(p);
+    return make_float4(__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xffff0000u),
+                       __uint_as_float(q.y << 16), __uint_as_float(q.y & 0xffff0000u));
 }
 
-template <typename T, int ROWS, int ND>   // head dims padded to 64 ND
+template <typename T, int ROWS, int ND>
 __global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
-    constexpr int DP = 64 * ND, LD = DP + 4;
-    constexpr int RPT = ROWS / 16;            // rows a thread accumulates
-    constexpr int TPR = kThreads / ROWS;      // threads of a row's softmax
-    constexpr int KPT = kKeys / TPR;          // keys each of them holds
-    extern __shared__ float smem[];
-    float *qs = smem, *ks = qs + ROWS * LD, *vs = ks + kKeys * LD, *ps = vs + kKeys * DP;
+    using C = RowsCfg<T, ROWS, ND>;
+    constexpr int DP = C::DP, kKeys = C::kKeys;
+    constexpr int TPR = kThreads / ROWS;         // threads of a row's softmax
+    constexpr int KPT = kKeys / TPR;             // keys each of them holds
+    constexpr int RPT = C::kFew ? ROWS : 4;      // rows a thread accumulates
+    constexpr int NQ = C::kFew ? 1 : ND;         // groups of 4 columns of each
+    extern __shared__ __align__(16) float smem[];
+    float *qs = smem, *ps = qs + ROWS * C::kLdQ;              // p [key][row]
+    char *ring = reinterpret_cast<char *>(ps + kKeys * C::kLdP);
     __shared__ float alpha[ROWS], denom[ROWS], top[ROWS];
     __shared__ int64_t scratch[kThreads / 32 + 1];
     __shared__ Cursor cur;
-    __shared__ int pages[kKeys];
     const int tid = threadIdx.x, page_mask = (1 << a.page_shift) - 1;
-    place_share<kThreads>(a, blockIdx.x, gridDim.x, kKeys, 4 * kKeys, scratch, &cur);
+    place_share<kThreads>(a, blockIdx.x, gridDim.x, kKeys, kKeys, scratch, &cur);
+    pdl_trigger();
     int4 *desc = a.part_desc + 2 * blockIdx.x;
     if (tid == 0) desc[0] = desc[1] = make_int4(kPartNone, 0, 0, 0);
     Walk wk;
     wk.begin(a, cur);
-    const int rg = tid >> 4, cg = tid & 15;   // this thread's rows rg RPT.., columns 4 cg + 64 i
     const int srow = tid / TPR, spos = tid % TPR;
+    const int quad = C::kFew ? tid % C::kQuads : tid & 15;
+    const int group = C::kFew ? tid / C::kQuads : 0;          // of the keys
+    const int row0 = C::kFew ? 0 : (tid >> 4) * 4;
+
+    // starts the copies of block j into a stage: 16-byte pieces, zeros for keys
+    // without a page and columns past the width.  All of a thread's table reads
+    // come first, so that they wait for memory once.
+    auto fetch = [&](int j, int stage) {
+        constexpr int kPieces = DP * (int)sizeof(T) / 16, kEach = 16 / (int)sizeof(T);
+        constexpr int kTimes = kKeys * kPieces / kThreads;
+        const uint32_t dst0 = (uint32_t)__cvta_generic_to_shared(ring + stage * C::kStage);
+        int page[kTimes];
+#pragma unroll
+        for (int n = 0; n < kTimes; ++n) {
+            const int i = tid + n * kThreads, key = i / kPieces, c = (i % kPieces) * kEach;
+            page[n] = c < a.D ? page_of(a, wk.c.r, j * kKeys + key, wk.kv) : -1;
+        }
+#pragma unroll
+        for (int n = 0; n < kTimes; ++n) {
+            const int i = tid + n * kThreads, key = i / kPieces, c = (i % kPieces) * kEach;
+            const int64_t row = ((((int64_t)page[n] * a.kv_heads + wk.h) << a.page_shift) +
+                                 ((j * kKeys + key) & page_mask)) * a.D + c;
+            const int64_t from = page[n] < 0 ? 0 : row;
+            const uint32_t dst = dst0 + key * C::kPitch + c * (int)sizeof(T);
+            const int bytes = page[n] < 0 ? 0 : 16;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst),
+                         "l"(static_cast<const T *>(a.k) + from), "r"(bytes) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                             dst + kKeys * C::kPitch),
+                         "l"(static_cast<const T *>(a.v) + from), "r"(bytes) : "memory");
+        }
+    };
+    auto key_at = [&](int stage, int which, int key) {        // which 0: K, 1: V
+        return reinterpret_cast<const T *>(ring + stage * C::kStage +
+                                           (which * kKeys + key) * C::kPitch);
+    };
+
     while (wk.next(a, kKeys)) {
         const int n_rows = wk.n_tok * a.group;
-        __syncthreads();
-        for (int i = tid; i < ROWS * DP; i += kThreads) {
-            const int row = i / DP, c = i - row * DP;
-            float x = 0.f;
-            if (row < n_rows && c < a.D)
-                x = to_f(static_cast<const T *>(
-                    a.q)[(wk.tok0 + row / a.group) * a.q_stride +
-                         (int64_t)(wk.h * a.group + row % a.group) * a.D + c]);
-            qs[row * LD + c] = x;
+        __syncthreads();                         // the tile before is done with shared memory
+        fetch(wk.j0, 0);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        // queries: a warp a row, the lanes over its columns
+#pragma unroll 4
+        for (int row = tid >> 5; row < ROWS; row += kThreads / 32) {
+            const int tok = row / a.group;
+            const T *q = static_cast<const T *>(a.q) + (wk.tok0 + tok) * a.q_stride +
+                         (int64_t)(wk.h * a.group + row - tok * a.group) * a.D;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i) {
+                const int c = (tid & 31) + 32 * i;
+                qs[row * C::kLdQ + c] = row < n_rows && c < a.D ? to_f(q[c]) : 0.f;
+            }
         }
-        float acc[RPT][4 * ND];
+        float acc[RPT][4 * NQ];
 #pragma unroll
         for (int i = 0; i < RPT; ++i)
 #pragma unroll
-            for (int c = 0; c < 4 * ND; ++c) acc[i][c] = 0.f;
+            for (int c = 0; c < 4 * NQ; ++c) acc[i][c] = 0.f;
         // each thread of a row keeps the row's maximum; the sum is its share
         float m = -INFINITY, l = 0.f;
         const int limit = min(wk.kv, wk.pos0 + srow / a.group + 1);   // keys this row sees
-        for (int j = wk.j0; j < wk.j1; ++j) {
-            const int key0 = j * kKeys;
+        int stage = 0;
+        for (int j = wk.j0; j < wk.j1; ++j, stage ^= 1) {
+            if (j + 1 < wk.j1) fetch(j + 1, stage ^ 1);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncthreads();
-            if (tid < kKeys) pages[tid] = page_of(a, wk.c.r, key0 + tid, wk.kv);
-            __syncthreads();
-            for (int i = tid; i < kKeys * DP; i += kThreads) {
-                const int key = i / DP, c = i - key * DP;
-                float x = 0.f, y = 0.f;
-                if (pages[key] >= 0 && c < a.D) {
-                    const int64_t at = ((((int64_t)pages[key] * a.kv_heads + wk.h)
-                                         << a.page_shift) + ((key0 + key) & page_mask)) * a.D + c;
-                    x = to_f(static_cast<const T *>(a.k)[at]);
-                    y = to_f(static_cast<const T *>(a.v)[at]);
-                }
-                ks[key * LD + c] = x;
-                vs[key * DP + c] = y;
+            // of 64 rows a warp has 8 in both products: one without any goes on
+            if (!C::kFew && 8 * (tid >> 5) >= n_rows) {
+                __syncthreads();
+                __syncthreads();
+                continue;
             }
-            __syncthreads();
             // scores: this thread's row, keys spos + TPR i
             float s[KPT];
 #pragma unroll
             for (int i = 0; i < KPT; ++i) s[i] = 0.f;
+#pragma unroll 4
             for (int c = 0; c < DP; c += 4) {
-                const float4 x = *reinterpret_cast<const float4 *>(qs + srow * LD + c);
+                const float4 x = load4(qs + srow * C::kLdQ + c);
 #pragma unroll
                 for (int i = 0; i < KPT; ++i) {
-                    const float4 y =
-                        *reinterpret_cast<const float4 *>(ks + (spos + TPR * i) * LD + c);
+                    const float4 y = load4(key_at(stage, 0, spos + TPR * i) + c);
                     s[i] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[i]))));
                 }
             }
             float mx = m;
 #pragma unroll
             for (int i = 0; i < KPT; ++i) {
-                s[i] = key0 + spos + TPR * i < limit ? s[i] * a.scale_log2 : -INFINITY;
+                s[i] = j * kKeys + spos + TPR * i < limit ? s[i] * a.scale_log2 : -INFINITY;
                 mx = fmaxf(mx, s[i]);
             }
 #pragma unroll
@@ -276,70 +339,103 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
             for (int i = 0; i < KPT; ++i) {
                 const float p = exp2f(s[i] - base);
                 l += p;
-                ps[srow * (kKeys + 1) + spos + TPR * i] = p;
+                ps[(spos + TPR * i) * C::kLdP + srow] = p;
             }
             if (spos == 0) alpha[srow] = f;
             __syncthreads();
+            if (!C::kFew || group < C::kGroups) {
 #pragma unroll
-            for (int i = 0; i < RPT; ++i) {
-                const float g = alpha[rg * RPT + i];
+                for (int i = 0; i < RPT; ++i) {
+                    const float g = alpha[row0 + i];
 #pragma unroll
-                for (int c = 0; c < 4 * ND; ++c) acc[i][c] *= g;
-            }
-            for (int key = 0; key < kKeys; ++key) {
-                float p[RPT];
+                    for (int c = 0; c < 4 * NQ; ++c) acc[i][c] *= g;
+                }
+#pragma unroll 2
+                for (int key = group; key < kKeys; key += C::kGroups) {
+                    float p[RPT];
 #pragma unroll
-                for (int i = 0; i < RPT; ++i) p[i] = ps[(rg * RPT + i) * (kKeys + 1) + key];
+                    for (int i = 0; i < RPT; i += 4) {
+                        const float4 x = load4(ps + key * C::kLdP + row0 + i);
+                        p[i] = x.x;
+                        p[i + 1] = x.y;
+                        p[i + 2] = x.z;
+                        p[i + 3] = x.w;
+                    }
 #pragma unroll
-                for (int d = 0; d < ND; ++d) {
-                    const float4 y =
-                        *reinterpret_cast<const float4 *>(vs + key * DP + 64 * d + 4 * cg);
+                    for (int d = 0; d < NQ; ++d) {
+                        const float4 y = load4(key_at(stage, 1, key) + 4 * quad + 64 * d);
 #pragma unroll
-                    for (int i = 0; i < RPT; ++i) {
-                        acc[i][4 * d] = fmaf(p[i], y.x, acc[i][4 * d]);
-                        acc[i][4 * d + 1] = fmaf(p[i], y.y, acc[i][4 * d + 1]);
-                        acc[i][4 * d + 2] = fmaf(p[i], y.z, acc[i][4 * d + 2]);
-                        acc[i][4 * d + 3] = fmaf(p[i], y.w, acc[i][4 * d + 3]);
+                        for (int i = 0; i < RPT; ++i) {
+                            acc[i][4 * d] = fmaf(p[i], y.x, acc[i][4 * d]);
+                            acc[i][4 * d + 1] = fmaf(p[i], y.y, acc[i][4 * d + 1]);
+                            acc[i][4 * d + 2] = fmaf(p[i], y.z, acc[i][4 * d + 2]);
+                            acc[i][4 * d + 3] = fmaf(p[i], y.w, acc[i][4 * d + 3]);
+                        }
                     }
                 }
             }
+            __syncthreads();                     // the stage is free for the block after next
         }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
         for (int o = TPR / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-        __syncthreads();
         if (spos == 0) {
             denom[srow] = l;
             top[srow] = m;
         }
+        if constexpr (C::kFew) {                 // the groups' sums, through the ring
+            float *join = reinterpret_cast<float *>(ring);
+            if (group < C::kGroups)
+#pragma unroll
+                for (int i = 0; i < RPT; ++i)
+                    *reinterpret_cast<float4 *>(join + (group * ROWS + i) * DP + 4 * quad) =
+                        make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+        }
         __syncthreads();
-        const int64_t rec = (int64_t)blockIdx.x * 2 + wk.slot;
         if (wk.part != kPartNone && tid == 0)
             desc[wk.slot] = make_int4(wk.part, wk.tok0, wk.n_tok, wk.h);
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-            const int row = rg * RPT + i;
-            if (row >= n_rows) continue;
+        auto write = [&](int row, int col, float4 x) {
             if (wk.part != kPartNone) {
-                float *o = a.part_o + (rec * a.rows + row) * DP + 4 * cg;
-#pragma unroll
-                for (int d = 0; d < ND; ++d)
-                    *reinterpret_cast<float4 *>(o + 64 * d) = make_float4(
-                        acc[i][4 * d], acc[i][4 * d + 1], acc[i][4 * d + 2], acc[i][4 * d + 3]);
-                if (cg == 0) a.part_ml[rec * a.rows + row] = make_float2(top[row], denom[row]);
-                continue;
+                const int64_t rec = ((int64_t)blockIdx.x * 2 + wk.slot) * a.rows + row;
+                *reinterpret_cast<float4 *>(a.part_o + rec * DP + col) = x;
+                if (col == 0) a.part_ml[rec] = make_float2(top[row], denom[row]);
+                return;
             }
             const int64_t head = (int64_t)(wk.tok0 + row / a.group) * a.q_heads +
                                  wk.h * a.group + row % a.group;
-            const float r = denom[row] > 0.f ? 1.f / denom[row] : denom[row];
-            T *o = static_cast<T *>(a.out) + head * a.D;
-#pragma unroll
-            for (int c = 0; c < 4 * ND; ++c) {
-                const int col = 64 * (c >> 2) + 4 * cg + (c & 3);
-                if (col < a.D) o[col] = from_f<T>(denom[row] == 0.f ? 0.f : acc[i][c] * r);
+            const bool none = denom[row] == 0.f;
+            const float r = none ? 0.f : 1.f / denom[row];
+            T *o = static_cast<T *>(a.out) + head * a.D + col;
+            if (col < a.D) {                     // widths are multiples of 8
+                o[0] = from_f<T>(none ? 0.f : x.x * r);
+                o[1] = from_f<T>(none ? 0.f : x.y * r);
+                o[2] = from_f<T>(none ? 0.f : x.z * r);
+                o[3] = from_f<T>(none ? 0.f : x.w * r);
             }
-            if (a.lse && cg == 0)
-                a.lse[head] = denom[row] == 0.f ? -INFINITY
-                                                : (top[row] + log2f(denom[row])) / kLog2e;
+            if (a.lse && col == 0)
+                a.lse[head] = none ? -INFINITY : (top[row] + log2f(denom[row])) / kLog2e;
+        };
+        if constexpr (C::kFew) {
+            const float *join = reinterpret_cast<const float *>(ring);
+            for (int i = tid; i < n_rows * C::kQuads; i += kThreads) {
+                const int row = i / C::kQuads, col = 4 * (i - row * C::kQuads);
+                float4 x = load4(join + row * DP + col);
+#pragma unroll
+                for (int g = 1; g < C::kGroups; ++g) {
+                    const float4 y = load4(join + (g * ROWS + row) * DP + col);
+                    x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+                }
+                write(row, col, x);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < RPT; ++i)
+#pragma unroll
+                for (int d = 0; d < NQ; ++d)
+                    if (row0 + i < n_rows)
+                        write(row0 + i, 4 * quad + 64 * d,
+                              make_float4(acc[i][4 * d], acc[i][4 * d + 1], acc[i][4 * d + 2],
+                                          acc[i][4 * d + 3]));
         }
     }
 }
@@ -557,7 +653,7 @@ template <typename T> cudaError_t combine(const AttnArgs &a, int ctas, int dp, b
 
 template <typename T, int ROWS, int ND> cudaError_t rows_go(const AttnArgs &a, int ctas,
                                                             cudaStream_t st) {
-    constexpr size_t smem = rows_smem<ROWS>(64 * ND);
+    constexpr size_t smem = RowsCfg<T, ROWS, ND>::kSmem;
     static const cudaError_t set = cudaFuncSetAttribute(
         rows_kernel<T, ROWS, ND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (set != cudaSuccess) return set;
@@ -565,14 +661,37 @@ template <typename T, int ROWS, int ND> cudaError_t rows_go(const AttnArgs &a, i
     return cudaGetLastError();
 }
 
-template <typename T, int ROWS> cudaError_t rows_dim(const AttnArgs &a, int ctas,
-                                                     cudaStream_t st) {
-    switch ((a.D + 63) / 64) {
-    case 1: return rows_go<T, ROWS, 1>(a, ctas, st);
-    case 2: return rows_go<T, ROWS, 2>(a, ctas, st);
-    case 3: return rows_go<T, ROWS, 3>(a, ctas, st);
-    default: return rows_go<T, ROWS, 4>(a, ctas, st);
-    }
+// Calls f with the kernel's types for a storage type, tile height and width.
+struct RowsPlan {
+    int per_sm, keys;
+};
+template <typename F> auto rows_variant(int32_t dtype, int rows, int dim, F &&f) {
+    auto width = [&](auto t, auto r) {
+        using T = decltype(t);
+        constexpr int R = decltype(r)::value;
+        switch ((dim + 63) / 64) {
+        case 1: return f(RowsCfg<T, R, 1>(), t, r, std::integral_constant<int, 1>());
+        case 2: return f(RowsCfg<T, R, 2>(), t, r, std::integral_constant<int, 2>());
+        case 3: return f(RowsCfg<T, R, 3>(), t, r, std::integral_constant<int, 3>());
+        default: return f(RowsCfg<T, R, 4>(), t, r, std::integral_constant<int, 4>());
+        }
+    };
+    auto height = [&](auto t) {
+        if (rows <= 8) return width(t, std::integral_constant<int, 8>());
+        if (rows <= 16) return width(t, std::integral_constant<int, 16>());
+        return width(t, std::integral_constant<int, 64>());
+    };
+    return dtype == ULTRAMEM_BF16 ? height(__nv_bfloat16()) : height(float());
+}
+RowsPlan rows_plan(int32_t dtype, int rows, int dim) {
+    return rows_variant(dtype, rows, dim, [](auto cfg, auto, auto, auto) {
+        return RowsPlan{decltype(cfg)::kPerSm, decltype(cfg)::kKeys};
+    });
+}
+cudaError_t launch_rows(const AttnArgs &a, int32_t dtype, int ctas, cudaStream_t st) {
+    return rows_variant(dtype, a.rows, a.D, [&](auto, auto t, auto r, auto nd) {
+        return rows_go<decltype(t), decltype(r)::value, decltype(nd)::value>(a, ctas, st);
+    });
 }
 
 // ---- the call's plan --------------------------------------------------------
@@ -581,13 +700,13 @@ template <typename T, int ROWS> cudaError_t rows_dim(const AttnArgs &a, int ctas
 // 128 wide; a call of at most 16 rows a request and key/value head reads each
 // key for those rows alone and goes to the decode kernel (M = 16), any other
 // to the 2 x 128-row kernel.  Everything else runs on the CUDA cores.
-enum Path { kRows16, kRows64, kDecode, kPrefill };
+enum Path { kRows, kDecode, kPrefill };
 
 Path path_of(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim, int32_t max_new,
              bool tensor) {
     const bool few = (int64_t)max_new * (q_heads / kv_heads) <= 16;
     if (dtype == ULTRAMEM_BF16 && dim <= 128 && tensor) return few ? kDecode : kPrefill;
-    return few ? kRows16 : kRows64;
+    return kRows;
 }
 
 struct Layout {
@@ -595,19 +714,29 @@ struct Layout {
     int64_t o, ml, desc, total;     // byte offsets in the workspace
 };
 
-Layout layout_of(Path path, int32_t group, int32_t dim) {
+Layout layout_of(Path path, int32_t dtype, int32_t group, int32_t dim, int32_t max_new) {
     Layout l = {};
+    const int sms = device_sm_count();
     l.dp = (dim + 63) / 64 * 64;
-    l.ctas = path == kPrefill ? device_sm_count() : 2 * device_sm_count();
     if (path == kPrefill) {
+        l.ctas = sms;
         l.tq = 2 * (128 / group);
         l.rows = l.tq * group;
+        // what reading the queries and writing the output of a tile measured,
+        // in the time of so many keys
+        l.extra = l.dp == 128 ? 384 : 256;
+    } else if (path == kDecode) {
+        l.ctas = 2 * sms;
+        l.rows = 16;
+        l.extra = 64;
     } else {
-        l.rows = path == kRows64 ? 64 : 16;
-        l.tq = l.rows / group;
+        const int64_t rows = (int64_t)max_new * group;
+        l.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 64;
+        const RowsPlan p = rows_plan(dtype, l.rows, dim);
+        l.ctas = p.per_sm * sms;
+        l.extra = p.keys;
     }
-    // one block of the kernel's keys: what a tile costs besides its keys
-    l.extra = path == kPrefill ? (l.dp == 128 ? 384 : 256) : path == kDecode ? 64 : 32;
+    if (path != kPrefill) l.tq = l.rows / group;
     l.o = 0;
     l.ml = l.o + (int64_t)l.ctas * 2 * l.rows * l.dp * 4;
     l.desc = (l.ml + (int64_t)l.ctas * 2 * l.rows * 8 + 15) & ~15ll;
@@ -776,7 +905,7 @@ extern "C" int64_t ultramem_paged_attention_workspace(int32_t dtype, int32_t q_h
     int64_t most = 0;
     for (const bool tensor : {false, true}) {
         const Path p = path_of(dtype, q_heads, kv_heads, head_dim, max_new, tensor);
-        const int64_t n = layout_of(p, q_heads / kv_heads, head_dim).total;
+        const int64_t n = layout_of(p, dtype, q_heads / kv_heads, head_dim, max_new).total;
         most = n > most ? n : most;
     }
     return most;
@@ -806,7 +935,7 @@ extern "C" ultramem_status ultramem_paged_attention(
     const int align = few ? 4 : 16;
     const bool tensor = ((uintptr_t)q | (uintptr_t)out) % align == 0 && q_stride * es % align == 0;
     const Path path = path_of(c->dtype, q_heads, c->kv_heads, c->head_dim, max_new, tensor);
-    const Layout l = layout_of(path, group, c->head_dim);
+    const Layout l = layout_of(path, c->dtype, group, c->head_dim, max_new);
     AttnArgs a = {};
     a.q = q;
     a.k = c->k;
@@ -839,7 +968,6 @@ extern "C" ultramem_status ultramem_paged_attention(
     cudaStream_t st = (cudaStream_t)stream;
     cudaGetLastError();
     cudaError_t e = cudaSuccess;
-    const bool bf = c->dtype == ULTRAMEM_BF16;
     if (path == kDecode || path == kPrefill) {
         if (!(a.err = error_word())) return ULTRAMEM_ECUDA;
         CUtensorMap mq, mk, mv;
@@ -857,10 +985,8 @@ extern "C" ultramem_status ultramem_paged_attention(
                 return ULTRAMEM_ECUDA;
             e = launch_prefill(a, mq, mk, mv, l.ctas, st);
         }
-    } else if (path == kRows16) {
-        e = bf ? rows_dim<__nv_bfloat16, 16>(a, l.ctas, st) : rows_dim<float, 16>(a, l.ctas, st);
     } else {
-        e = bf ? rows_dim<__nv_bfloat16, 64>(a, l.ctas, st) : rows_dim<float, 64>(a, l.ctas, st);
+        e = launch_rows(a, c->dtype, l.ctas, st);
     }
     if (e == cudaSuccess) e = launch_combine(a, l.ctas, l.dp, c->dtype, true, st);
     return um::status_from_cuda(e);
