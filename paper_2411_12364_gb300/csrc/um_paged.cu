@@ -963,13 +963,12 @@ extern "C" ultramem_status ultramem_paged_attention(
     a.tq = l.tq;
     a.extra = l.extra;
     a.rows_hint = (int)((int64_t)max_new * group < l.rows ? (int64_t)max_new * group : l.rows);
-    a.scale = scale;
     a.scale_log2 = scale * kLog2e;
     cudaStream_t st = (cudaStream_t)stream;
     cudaGetLastError();
     cudaError_t e = cudaSuccess;
     if (path == kDecode || path == kPrefill) {
-        if (!(a.err = error_word())) return ULTRAMEM_ECUDA;
+        if (!(a.err = error_word())) return ULTRAMEM_ENODEV;
         CUtensorMap mq, mk, mv;
         const uint64_t D = c->head_dim, P = c->page_size;
         const uint64_t outer = (uint64_t)c->n_pages * c->kv_heads;
@@ -977,12 +976,12 @@ extern "C" ultramem_status ultramem_paged_attention(
                                              : prefill_box_rows(c->page_size);
         if (!encode(&mk, c->k, D, P, outer, D, P * D, box, 1) ||
             !encode(&mv, c->v, D, P, outer, D, P * D, box, 1))
-            return ULTRAMEM_ECUDA;
+            return um::status_from_cuda(cudaErrorInvalidValue);
         if (path == kDecode) {
             e = launch_decode(a, mk, mv, l.ctas, st);
         } else {
             if (!encode(&mq, q, D, q_heads, n_tokens, D, q_stride, group, l.tq / 2))
-                return ULTRAMEM_ECUDA;
+                return um::status_from_cuda(cudaErrorInvalidValue);
             e = launch_prefill(a, mq, mk, mv, l.ctas, st);
         }
     } else {

@@ -36,14 +36,13 @@ struct AttnArgs {
     int4 *part_desc;            // [C][2] (kind, first token, tokens, head)
     int *err;
     int64_t q_stride;           // elements between tokens of q
-    int64_t n_slots;            // pages * page size
     int n_seqs, n_tokens, q_heads, kv_heads, group, D;
     int page_shift, table_width, n_pages;
     int rows;                   // rows of a tile, padded (the partials' stride)
     int rows_hint;              // rows that tiles are expected to have
     int tq;                     // tokens of a tile
     int extra;                  // a tile's fixed cost, in keys
-    float scale, scale_log2;    // the scores' factor, and times log2(e)
+    float scale_log2;           // the scores' factor times log2(e)
 };
 
 enum { kPartNone = 0, kPartFirst = 1, kPartMiddle = 2, kPartLast = 3 };

@@ -2,6 +2,7 @@
 requests, the append against indexing, and the attention against a 64-bit
 softmax over the gathered pages, at the lengths, head groups, widths, page
 sizes and strides where the kernels change path."""
+import ctypes
 import math
 
 import numpy as np
@@ -424,3 +425,60 @@ def test_refusals_of_the_python_calls(gpu_lib):
         paged_plan(kv, kv, c.table, _i32([1]), _i32([1, 2]), 16, 1)
     with pytest.raises(binding.UltraMemError):
         paged_plan(kv, _i32([1]), c.table, _i32([1]), _i32([1]), 24, 1)
+
+
+def test_offsets_past_32_bits(gpu_lib):
+    """Pages whose entries lie past 2^31 elements into the cache, for each
+    kernel that reads or writes it."""
+    hk, page, dim = 8, 256, 64
+    n_pages = (1 << 31) // (hk * page * dim) + 40
+    for dtype, n in ((BF16, 1), (BF16, 50), (F32, 1), (F32, 30)):
+        kc = torch.empty(n_pages, hk, page, dim, dtype=dtype, device="cuda")
+        vc = torch.empty_like(kc)
+        used = [n_pages - 1, 3, n_pages - 20]
+        for p in used:
+            kc[p] = float("nan")
+            vc[p] = float("nan")
+        kv = 600
+        gen = torch.Generator(device="cuda").manual_seed(12)
+        k, v = (torch.randn(kv, hk, dim, generator=gen, device="cuda").to(dtype) for _ in range(2))
+        table = _i32([used])
+        pos = torch.arange(kv, device="cuda")
+        slots = (table[0, pos // page] * page + pos % page).to(torch.int32)
+        paged_append(kc, vc, k, v, slots)
+        q = torch.randn(n, 2 * hk, dim, generator=gen, device="cuda").to(dtype)
+        out = paged_attention(q, kc, vc, table, _i32([0, n]), _i32([kv]), n).double()
+        kk, vv = (x.double().repeat_interleave(2, 1) for x in (k, v))
+        s = torch.einsum("nhd,khd->hnk", q.double(), kk) / math.sqrt(dim)
+        s = s.masked_fill(pos[None, :] > kv - n + torch.arange(n, device="cuda")[:, None], -math.inf)
+        p = torch.softmax(s, -1)
+        want = torch.einsum("hnk,khd->nhd", p, vv)
+        a = torch.einsum("hnk,khd->nhd", p, vv.abs())
+        low = 2 * EPS16 if dtype == BF16 else 0.0
+        assert ((out - want).abs() <= (low + 1e-4) * a).all()
+        del kc, vc
+
+
+def test_workspace_is_not_read_before_it_is_written(gpu_lib):
+    """Any contents of the workspace give the same result."""
+    lib = binding.load()
+    for dtype, reqs in ((BF16, [(3000, 1), (70, 1)]), (BF16, [(3000, 90), (70, 5)]),
+                        (F32, [(3000, 1)]), (F32, [(900, 70)])):
+        c = Case(reqs, 8, 2, 128, 16, dtype, seed=13)
+        want, want_lse = c.run()
+        cache = binding.KVCache(c.k.data_ptr(), c.v.data_ptr(), *c.k.shape,
+                                binding.BF16 if dtype == BF16 else binding.F32)
+        need = lib.ultramem_paged_attention_workspace(cache.dtype, 8, 2, 128, c.max_new)
+        start, kv = _i32(c.start), _i32([k for k, _ in reqs])
+        for fill in (0, 255, 1):
+            ws = torch.full((need,), fill, dtype=torch.uint8, device="cuda")
+            out, lse = torch.empty_like(want), torch.empty_like(want_lse)
+            q = c.q
+            st = lib.ultramem_paged_attention(
+                ctypes.byref(cache), q.data_ptr(), q.stride(0), 8, start.data_ptr(), kv.data_ptr(),
+                c.table.data_ptr(), c.table.shape[1], len(reqs), c.start[-1], c.max_new,
+                1 / math.sqrt(128), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), need,
+                torch.cuda.current_stream().cuda_stream)
+            assert st == binding.OK
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    assert lib.ultramem_paged_check(None) == binding.OK
