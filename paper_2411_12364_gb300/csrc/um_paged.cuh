@@ -47,6 +47,9 @@ struct AttnArgs {
 
 enum { kPartNone = 0, kPartFirst = 1, kPartMiddle = 2, kPartLast = 3 };
 
+// The most keys of a tile that is not split.
+__host__ __device__ inline int whole_keys(const AttnArgs &a) { return 2 * a.extra; }
+
 // One request's part of the axis.
 struct Request {
     int tok0, n, kv;            // first token in the batch, new tokens, keys
@@ -180,7 +183,7 @@ struct Walk {
                 }
             }
             const int keys = q.keys(c.t, a.tq);
-            const bool whole = keys <= 2 * a.extra;
+            const bool whole = keys <= whole_keys(a);
             const int64_t len = (int64_t)keys + a.extra;
             if (whole && c.off > 0) {        // begun and finished by an earlier share
                 c.left -= len - c.off;

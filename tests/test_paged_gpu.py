@@ -482,3 +482,14 @@ def test_workspace_is_not_read_before_it_is_written(gpu_lib):
             assert st == binding.OK
             assert torch.equal(out, want) and torch.equal(lse, want_lse)
     assert lib.ultramem_paged_check(None) == binding.OK
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kv", [60, 64, 120, 128, 130, 250, 510, 760, 768, 770, 800])
+def test_tables_around_the_length_that_is_never_split(dtype, kv, gpu_lib):
+    """Row capacities on both sides of the lengths whose tiles stay whole."""
+    for n in (1, min(kv, 40)):
+        c = Case([(kv, n), (17, n if n <= 17 else 17)], 8, 1, 64, 16, dtype, seed=14)
+        c.check(*c.run())
+        c = Case([(kv, n)], 4, 1, 128, 32, dtype, seed=15)
+        c.check(*c.run())
