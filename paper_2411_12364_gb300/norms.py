@@ -9,6 +9,7 @@ As in binding.py, these functions marshal arguments only.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 
 import torch
 
@@ -69,7 +70,13 @@ def _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale
         None if w_pre is None else _vector("w_pre", w_pre, D),
         None if b_pre is None else _vector("b_pre", b_pre, D), ld_y, 0, T, D, code, kind_code,
         1 if post else 0, 1 if pre else 0, mode, res_scale, out_scale, eps)
-    return a, y, mode
+    return a, y
+
+
+@functools.lru_cache(maxsize=256)
+def _workspace(T, D):
+    """Bytes of the backward's workspace, a function of the sizes alone."""
+    return int(_b.load().ultramem_block_norm_backward_workspace(T, D))
 
 
 def _given(name, t, y):
@@ -85,8 +92,7 @@ def block_norm(y, residual, w_post=None, b_post=None, gate=None, w_pre=None, b_p
     (n is None without ``pre``).  gate: fp32 [D], or [T, 1] or [T, D] in y's
     type.  ``u`` and ``n`` may be given; u may be the residual itself and n
     may be y, updated in place."""
-    a, y, _ = _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale, post,
-                    pre)
+    a, y = _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale, post, pre)
     shape, dtype = y.shape, y.dtype
     residual, a.ld_r = _rows("residual", residual, shape, dtype)
     u = torch.empty(shape, dtype=dtype, device=y.device) if u is None else _given("u", u, y)
@@ -109,8 +115,7 @@ def block_norm_backward(y, u, du, dn=None, w_post=None, b_post=None, gate=None, 
     du of u (may be None) and dn of n (with ``pre``): a dict of dy, dr,
     dw_post, db_post, dw_pre, db_pre, dgate (None where the forward has no such
     input; gains and biases are fp32, and absent gains get no gradient)."""
-    a, y, mode = _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale,
-                       post, pre)
+    a, y = _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale, post, pre)
     shape, dtype, device = y.shape, y.dtype, y.device
     T, D = shape
     u, a.ld_r = _rows("u", u, shape, dtype)
@@ -125,38 +130,29 @@ def block_norm_backward(y, u, du, dn=None, w_post=None, b_post=None, gate=None, 
     lib = _b._lib or _b.load()
     dy = torch.empty(shape, dtype=dtype, device=device)
     dr = torch.empty(shape, dtype=dtype, device=device)
-    # the gradients of the fp32 vectors, and the workspace: one allocation each
-    names = []
-    if post:
-        if w_post is not None:
-            names.append("dw_post")
-        if b_post is not None:
-            names.append("db_post")
-    if pre:
-        if w_pre is not None:
-            names.append("dw_pre")
-        if b_pre is not None:
-            names.append("db_pre")
-    if mode == GATE_CHANNEL:
-        names.append("dgate")
-    got = {"dy": dy, "dr": dr, "dw_post": None, "db_post": None, "dw_pre": None, "db_pre": None,
-           "dgate": None}
-    ptr = {}
-    if names:
-        vectors = torch.empty((len(names), D), dtype=torch.float32, device=device)
-        base = vectors.data_ptr()
-        for i, (name, v) in enumerate(zip(names, vectors.unbind(0))):
-            got[name] = v
-            ptr[name] = base + 4 * D * i
-    if mode > GATE_CHANNEL:
-        got["dgate"] = torch.empty_like(gate)
-        ptr["dgate"] = got["dgate"].data_ptr()
-    nbytes = lib.ultramem_block_norm_backward_workspace(T, D)
+    dw_post = db_post = dw_pre = db_pre = dgate = None
+    p_wpost = p_bpost = p_wpre = p_bpre = p_gate = None
+    if post and w_post is not None:
+        dw_post = torch.empty(D, dtype=torch.float32, device=device)
+        p_wpost = dw_post.data_ptr()
+    if post and b_post is not None:
+        db_post = torch.empty(D, dtype=torch.float32, device=device)
+        p_bpost = db_post.data_ptr()
+    if pre and w_pre is not None:
+        dw_pre = torch.empty(D, dtype=torch.float32, device=device)
+        p_wpre = dw_pre.data_ptr()
+    if pre and b_pre is not None:
+        db_pre = torch.empty(D, dtype=torch.float32, device=device)
+        p_bpre = db_pre.data_ptr()
+    if gate is not None:
+        dgate = torch.empty_like(gate)
+        p_gate = dgate.data_ptr()
+    nbytes = _workspace(T, D)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     status = lib.ultramem_block_norm_backward(
         C.byref(a), u.data_ptr(), du_ptr, ld_du, dn_ptr, ld_dn, dy.data_ptr(), dr.data_ptr(),
-        ptr.get("dgate"), ptr.get("dw_post"), ptr.get("db_post"), ptr.get("dw_pre"),
-        ptr.get("db_pre"), ws.data_ptr(), nbytes, _b._stream())
+        p_gate, p_wpost, p_bpost, p_wpre, p_bpre, ws.data_ptr(), nbytes, _b._stream())
     if status:
         raise _b.UltraMemError(status, "ultramem_block_norm_backward")
-    return got
+    return {"dy": dy, "dr": dr, "dw_post": dw_post, "db_post": db_post, "dw_pre": dw_pre,
+            "db_pre": db_pre, "dgate": dgate}

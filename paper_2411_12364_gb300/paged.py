@@ -17,6 +17,7 @@ fallback, and an argument that the library cannot take raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 
 import torch
@@ -84,21 +85,20 @@ def paged_plan(ctx_lens, new_lens, block_table, free_pages, free_count, page_siz
         free_ptr = _int32("free_left", free_left)
         if free_left.numel() != 1:
             raise ValueError("free_left must have one element")
-    # one allocation for the outputs, one after the other
-    sizes = (R + 1, R, n_tokens, 1)
-    buf = torch.empty(2 * R + 2 + n_tokens, dtype=torch.int32, device=ctx_lens.device)
-    base = buf.data_ptr()
-    lens = base + 4 * (R + 1)
-    slots = lens + 4 * R
+    device = ctx_lens.device
+    q_start = torch.empty(R + 1, dtype=torch.int32, device=device)
+    kv_lens = torch.empty(R, dtype=torch.int32, device=device)
+    slots = torch.empty(n_tokens, dtype=torch.int32, device=device)
+    balance = torch.empty(1, dtype=torch.int32, device=device)
     lib = _b._lib or _b.load()
     status = lib.ultramem_paged_plan(
         _int32("ctx_lens", ctx_lens), _int32("new_lens", new_lens), R, page_size,
         _int32("block_table", block_table), table_shape[1], _int32("free_pages", free_pages),
-        _int32("free_count", free_count), n_tokens, base, lens, slots, free_ptr,
-        slots + 4 * n_tokens, _b._stream())
+        _int32("free_count", free_count), n_tokens, q_start.data_ptr(), kv_lens.data_ptr(),
+        slots.data_ptr(), free_ptr, balance.data_ptr(), _b._stream())
     if status:
         raise _b.UltraMemError(status, "ultramem_paged_plan")
-    return buf.split_with_sizes(sizes)
+    return q_start, kv_lens, slots, balance
 
 
 def paged_append(k_cache, v_cache, k, v, slots):
@@ -116,6 +116,13 @@ def paged_append(k_cache, v_cache, k, v, slots):
                                        _int32("slots", slots), T, _b._stream())
     if status:
         raise _b.UltraMemError(status, "ultramem_paged_append")
+
+
+@functools.lru_cache(maxsize=256)
+def _workspace(dtype, q_heads, kv_heads, head_dim, max_new):
+    """Bytes of the attention's workspace, a function of the sizes alone."""
+    return int(_b.load().ultramem_paged_attention_workspace(dtype, q_heads, kv_heads, head_dim,
+                                                            max_new))
 
 
 def paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new: int, scale=None,
@@ -142,7 +149,7 @@ def paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new:
         raise ValueError("out must be a contiguous CUDA tensor of q's shape and type")
     lse = torch.empty((T, H), dtype=torch.float32, device=device) if with_lse else None
     lib = _b._lib or _b.load()
-    nbytes = lib.ultramem_paged_attention_workspace(c.dtype, H, heads, dim, max_new)
+    nbytes = _workspace(c.dtype, H, heads, dim, max_new)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     status = lib.ultramem_paged_attention(
         C.byref(c), q.data_ptr(), qs, H, _int32("q_start", q_start), _int32("kv_lens", kv_lens),
