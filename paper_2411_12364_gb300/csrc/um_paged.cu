@@ -3,6 +3,7 @@
 // the attention kernel of the storages and head widths that the tensor-core
 // kernels do not take, with the kernels that join split tiles.
 #include "um_paged.cuh"
+#include "um_pair.cuh"
 
 namespace um {
 namespace paged {
@@ -183,13 +184,14 @@ __global__ void __launch_bounds__(256) append_kernel(const W *k, const W *v, int
 // from shared memory, the running maximum and sum of each row, the values
 // added into registers.  Sums are fp32 throughout.
 //
-// What bounds it: reads of shared memory and the fp32 pipes.  Many rows (64)
-// share every read among 8 rows of a warp; a thread accumulates 4 rows x 4 ND
-// columns.  Few rows (8, 16: single tokens) leave nothing to share, so there
-// the threads of one column group split the keys between them, each with all
-// rows, and add up at the tile's end.  Measured in fp32: 6 single tokens over
-// up to 31 k keys (16 / 8 heads x 128) 296 us, 2.9 TB/s; 2 chunks of up to 49
-// tokens over 2 k keys (10 / 2 heads x 128) 48 us.
+// What bounds it: reads of shared memory and the fp32 pipes, on which the
+// products run as packed pairs.  Many rows (64) share every read among 8 rows
+// of a warp; a thread accumulates 4 rows x 4 ND columns.  Few rows (8, 16:
+// single tokens) leave nothing to share, so there the threads of one column
+// group split the keys between them, each with 8 rows, and add up at the
+// tile's end.  Measured in fp32: 6 single tokens over
+// up to 31 k keys (16 / 8 heads x 128) 304 us, 2.9 TB/s; 2 chunks of up to 49
+// tokens over 2 k keys (10 / 2 heads x 128) 45 us.
 constexpr int kThreads = 256;
 
 template <typename T, int ROWS, int ND> struct RowsCfg {
@@ -200,7 +202,9 @@ template <typename T, int ROWS, int ND> struct RowsCfg {
     static constexpr int kLdQ = DP + 4, kLdP = ROWS + 4;         // floats
     static_assert(kKeys * DP * (int)sizeof(T) / 16 % kThreads == 0, "whole rounds of copies");
     static constexpr int kQuads = 16 * ND;                       // groups of 4 columns
-    static constexpr int kGroups = kFew ? kThreads / kQuads : 1; // that split the keys
+    static constexpr int kRowGroups = kFew ? ROWS / 8 : 16;      // of 8 or 4 rows
+    static constexpr int kGroups =                               // that split the keys
+        kFew ? kThreads / (kQuads * kRowGroups) : 1;
     static constexpr size_t kStage = (size_t)2 * kKeys * kPitch; // K and V of a block
     static constexpr size_t kJoin = kFew ? (size_t)kGroups * ROWS * DP * 4 : 0;
     static constexpr size_t kRing = 2 * kStage > kJoin ? 2 * kStage : kJoin;
@@ -219,12 +223,12 @@ __device__ __forceinline__ float4 load4(const __nv_bfloat16 *p) {
 }
 
 template <typename T, int ROWS, int ND>
-__global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, RowsCfg<T, ROWS, ND>::kPerSm) rows_kernel(AttnArgs a) {
     using C = RowsCfg<T, ROWS, ND>;
     constexpr int DP = C::DP, kKeys = C::kKeys;
     constexpr int TPR = kThreads / ROWS;         // threads of a row's softmax
     constexpr int KPT = kKeys / TPR;             // keys each of them holds
-    constexpr int RPT = C::kFew ? ROWS : 4;      // rows a thread accumulates
+    constexpr int RPT = C::kFew ? 8 : 4;         // rows a thread accumulates
     constexpr int NQ = C::kFew ? 1 : ND;         // groups of 4 columns of each
     extern __shared__ __align__(16) float smem[];
     float *qs = smem, *ps = qs + ROWS * C::kLdQ;              // p [key][row]
@@ -241,8 +245,8 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
     wk.begin(a, cur);
     const int srow = tid / TPR, spos = tid % TPR;
     const int quad = C::kFew ? tid % C::kQuads : tid & 15;
-    const int group = C::kFew ? tid / C::kQuads : 0;          // of the keys
-    const int row0 = C::kFew ? 0 : (tid >> 4) * 4;
+    const int group = C::kFew ? tid / (C::kQuads * C::kRowGroups) : 0;   // of the keys
+    const int row0 = C::kFew ? tid / C::kQuads % C::kRowGroups * 8 : (tid >> 4) * 4;
 
     // starts the copies of block j into a stage: 16-byte pieces, zeros for keys
     // without a page and columns past the width.  All of a thread's table reads
@@ -294,11 +298,11 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
                 qs[row * C::kLdQ + c] = row < n_rows && c < a.D ? to_f(q[c]) : 0.f;
             }
         }
-        float acc[RPT][4 * NQ];
+        F2 acc[RPT][2 * NQ];
 #pragma unroll
         for (int i = 0; i < RPT; ++i)
 #pragma unroll
-            for (int c = 0; c < 4 * NQ; ++c) acc[i][c] = 0.f;
+            for (int c = 0; c < 2 * NQ; ++c) acc[i][c] = f2(0.f);
         // each thread of a row keeps the row's maximum; the sum is its share
         float m = -INFINITY, l = 0.f;
         const int limit = min(wk.kv, wk.pos0 + srow / a.group + 1);   // keys this row sees
@@ -315,68 +319,82 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
                 continue;
             }
             // scores: this thread's row, keys spos + TPR i
-            float s[KPT];
+            F2 dot[KPT];
 #pragma unroll
-            for (int i = 0; i < KPT; ++i) s[i] = 0.f;
+            for (int i = 0; i < KPT; ++i) dot[i] = f2(0.f);
 #pragma unroll 4
             for (int c = 0; c < DP; c += 4) {
                 const float4 x = load4(qs + srow * C::kLdQ + c);
+                const F2 x0 = f2(x.x, x.y), x1 = f2(x.z, x.w);
 #pragma unroll
                 for (int i = 0; i < KPT; ++i) {
                     const float4 y = load4(key_at(stage, 0, spos + TPR * i) + c);
-                    s[i] = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s[i]))));
+                    dot[i] = fma2(x0, f2(y.x, y.y), dot[i]);
+                    dot[i] = fma2(x1, f2(y.z, y.w), dot[i]);
                 }
             }
+            float s[KPT];
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) s[i] = both(dot[i]);
             float mx = m;
 #pragma unroll
             for (int i = 0; i < KPT; ++i) {
-                s[i] = j * kKeys + spos + TPR * i < limit ? s[i] * a.scale_log2 : -INFINITY;
+                s[i] = j * kKeys + spos + TPR * i < limit ? s[i] : -INFINITY;
                 mx = fmaxf(mx, s[i]);
             }
 #pragma unroll
             for (int o = TPR / 2; o > 0; o >>= 1)
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            const float base = mx == -INFINITY ? 0.f : mx;   // a row without keys so far
-            const float f = exp2f(m - base);
+            // exponents as one product and difference: what rounds is the
+            // difference, not the score; a row without keys so far refers to 0
+            const float base = mx == -INFINITY ? 0.f : -mx * a.scale_log2;
+            const float f = exp2f(fmaf(m, a.scale_log2, base));
             m = mx;
-            l *= f;
+            float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < KPT; ++i) {
-                const float p = exp2f(s[i] - base);
-                l += p;
+                const float p = exp2f(fmaf(s[i], a.scale_log2, base));
+                sum += p;
                 ps[(spos + TPR * i) * C::kLdP + srow] = p;
             }
+            l = fmaf(l, f, sum);
             if (spos == 0) alpha[srow] = f;
             __syncthreads();
             if (!C::kFew || group < C::kGroups) {
+                // a block's sum is taken by itself and then added, so that a long
+                // axis is a sum of short ones
+                F2 blk[RPT][2 * NQ];
 #pragma unroll
-                for (int i = 0; i < RPT; ++i) {
-                    const float g = alpha[row0 + i];
+                for (int i = 0; i < RPT; ++i)
 #pragma unroll
-                    for (int c = 0; c < 4 * NQ; ++c) acc[i][c] *= g;
-                }
+                    for (int c = 0; c < 2 * NQ; ++c) blk[i][c] = f2(0.f);
 #pragma unroll 2
                 for (int key = group; key < kKeys; key += C::kGroups) {
-                    float p[RPT];
+                    F2 p[RPT];
 #pragma unroll
                     for (int i = 0; i < RPT; i += 4) {
                         const float4 x = load4(ps + key * C::kLdP + row0 + i);
-                        p[i] = x.x;
-                        p[i + 1] = x.y;
-                        p[i + 2] = x.z;
-                        p[i + 3] = x.w;
+                        p[i] = f2(x.x);
+                        p[i + 1] = f2(x.y);
+                        p[i + 2] = f2(x.z);
+                        p[i + 3] = f2(x.w);
                     }
 #pragma unroll
                     for (int d = 0; d < NQ; ++d) {
                         const float4 y = load4(key_at(stage, 1, key) + 4 * quad + 64 * d);
+                        const F2 y0 = f2(y.x, y.y), y1 = f2(y.z, y.w);
 #pragma unroll
                         for (int i = 0; i < RPT; ++i) {
-                            acc[i][4 * d] = fmaf(p[i], y.x, acc[i][4 * d]);
-                            acc[i][4 * d + 1] = fmaf(p[i], y.y, acc[i][4 * d + 1]);
-                            acc[i][4 * d + 2] = fmaf(p[i], y.z, acc[i][4 * d + 2]);
-                            acc[i][4 * d + 3] = fmaf(p[i], y.w, acc[i][4 * d + 3]);
+                            blk[i][2 * d] = fma2(p[i], y0, blk[i][2 * d]);
+                            blk[i][2 * d + 1] = fma2(p[i], y1, blk[i][2 * d + 1]);
                         }
                     }
+                }
+#pragma unroll
+                for (int i = 0; i < RPT; ++i) {
+                    const F2 g = f2(alpha[row0 + i]);
+#pragma unroll
+                    for (int c = 0; c < 2 * NQ; ++c) acc[i][c] = fma2(acc[i][c], g, blk[i][c]);
                 }
             }
             __syncthreads();                     // the stage is free for the block after next
@@ -386,15 +404,17 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
         for (int o = TPR / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
         if (spos == 0) {
             denom[srow] = l;
-            top[srow] = m;
+            top[srow] = m * a.scale_log2;        // in log2 units, -inf without keys
         }
         if constexpr (C::kFew) {                 // the groups' sums, through the ring
             float *join = reinterpret_cast<float *>(ring);
             if (group < C::kGroups)
 #pragma unroll
-                for (int i = 0; i < RPT; ++i)
-                    *reinterpret_cast<float4 *>(join + (group * ROWS + i) * DP + 4 * quad) =
-                        make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+                for (int i = 0; i < RPT; ++i) {
+                    const float2 lo = split(acc[i][0]), hi = split(acc[i][1]);
+                    *reinterpret_cast<float4 *>(join + (group * ROWS + row0 + i) * DP + 4 * quad) =
+                        make_float4(lo.x, lo.y, hi.x, hi.y);
+                }
         }
         __syncthreads();
         if (wk.part != kPartNone && tid == 0)
@@ -437,10 +457,10 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(AttnArgs a) {
             for (int i = 0; i < RPT; ++i)
 #pragma unroll
                 for (int d = 0; d < NQ; ++d)
-                    if (row0 + i < n_rows)
-                        write(row0 + i, 4 * quad + 64 * d,
-                              make_float4(acc[i][4 * d], acc[i][4 * d + 1], acc[i][4 * d + 2],
-                                          acc[i][4 * d + 3]));
+                    if (row0 + i < n_rows) {
+                        const float2 lo = split(acc[i][2 * d]), hi = split(acc[i][2 * d + 1]);
+                        write(row0 + i, 4 * quad + 64 * d, make_float4(lo.x, lo.y, hi.x, hi.y));
+                    }
         }
     }
 }
