@@ -43,14 +43,21 @@ constexpr int kThreads = 384;
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 88;
 static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * 168, "register split");
 constexpr uint32_t kHalfBytes = 128 * 128;     // 128 rows x 64 columns of bf16
-constexpr int kMost = 96;                      // keys whose weights are handed over first
 constexpr float kRaise = 8.f;                  // log2 units
 
 template <int DP> struct Cfg {
     static constexpr int kHalves = DP / 64;                   // 64-column halves of a row
     static constexpr uint32_t kTile = kHalfBytes * kHalves;   // 128 rows
-    static constexpr int kStages = DP == 128 ? 5 : 10;
-    static constexpr size_t kSmem = (size_t)kTile * (2 + kStages) + 1024;
+    // Width 64: a stage holds a block's K and V together, which saves the
+    // issuing warps a wait and a commit a block, and the weights are handed
+    // over in one go.  Width 128 has room for five halves of such stages and
+    // takes K and V one by one, and the weights in two parts.
+    static constexpr bool kPaired = DP == 64;
+    static constexpr int kParts = kPaired ? 2 : 1;            // tiles of a stage
+    static constexpr int kStages = 5;
+    static constexpr uint32_t kStage = kTile * kParts;
+    static constexpr int kMost = kPaired ? kKeys : 96;        // keys handed over first
+    static constexpr size_t kSmem = (size_t)kTile * 2 + (size_t)kStage * kStages + 1024;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -286,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         p[k] = *reinterpret_cast<const uint32_t *>(&b);
                     }
                     tmem_st16(ts + 16 * c, p);
-                    if (c == kMost / 32 - 1) {   // the product over these keys may start
+                    if (!C::kPaired && c == C::kMost / 32 - 1) {   // their product may start
                         tmem_st_wait();
                         tc::tc_fence_before();
                         tc::mbar_arrive(&p_most[i]);
@@ -383,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool leader = elect_one();
         const uint64_t q_desc = tc::desc_k_sw128(tc::smem_u32(qs + i * C::kTile));
         const uint64_t k_desc = tc::desc_k_sw128(tc::smem_u32(ring));
-        const uint64_t v_desc = desc_mn_sw128(tc::smem_u32(ring));
+        const uint64_t v_desc = desc_mn_sw128(tc::smem_u32(ring + (C::kPaired ? C::kTile : 0)));
         const uint32_t t_s = uniform(tmem) + 128 * i, t_o = uniform(tmem) + 256 + DP * i;
         int stage = 0;
         uint32_t phase = 0, tiles = 0, p_phase = 0, turns = 0;
@@ -397,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (leader) tc::mma_commit(bar);
         };
         auto scores = [&](int st) {
-            const uint64_t kd = k_desc + (uint32_t)st * (C::kTile >> 4);
+            const uint64_t kd = k_desc + (uint32_t)st * (C::kStage >> 4);
             if (leader) {
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k) {
@@ -408,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         };
         auto output = [&](int st, int k0, int k1, bool add) {   // keys 16 k0 .. 16 k1
-            const uint64_t vd = v_desc + (uint32_t)st * (C::kTile >> 4);
+            const uint64_t vd = v_desc + (uint32_t)st * (C::kStage >> 4);
             if (leader) {
 #pragma unroll
                 for (int k = k0; k < k1; ++k)
@@ -425,37 +432,42 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!(ok = warp_wait(&kv_full[stage], phase))) break;
             tc::tc_fence_after();
             if (j0 < e) scores(stage);
-            commit(&kv_empty[stage]);
+            if constexpr (!C::kPaired) {
+                commit(&kv_empty[stage]);
+                advance();
+            }
             if (j0 + 1 == end) commit(&q_empty);
-            advance();
             for (int j = j0; j < end; ++j) {
-                const int sv = stage;
-                if (!(ok = warp_wait(&kv_full[stage], phase))) break;
+                const int sv = stage;            // V of this block, then K of the next
+                if (!C::kPaired && !(ok = warp_wait(&kv_full[stage], phase))) break;
                 advance();
                 const bool more = j + 1 < end;
                 const int sk = stage;
                 if (more && !(ok = warp_wait(&kv_full[stage], phase))) break;
-                if (j < e && !(ok = warp_wait(&p_most[i], p_phase))) break;
+                if (!C::kPaired && j < e && !(ok = warp_wait(&p_most[i], p_phase))) break;
                 // half 0 goes first: it waits for half 1's turn before, half 1
                 // for half 0's at this block
                 if (!(ok = warp_wait(&turn[i ^ 1], (turns & 1) ^ (i == 0)))) break;
                 ++turns;
                 if (j < e) {
                     tc::tc_fence_after();
-                    output(sv, 0, kMost / 16, j > j0);
+                    if constexpr (!C::kPaired) output(sv, 0, C::kMost / 16, j > j0);
                     if (!(ok = warp_wait(&p_full[i], p_phase))) break;
                     p_phase ^= 1;
                     tc::tc_fence_after();
-                    output(sv, kMost / 16, kKeys / 16, true);
+                    if constexpr (C::kPaired)
+                        output(sv, 0, kKeys / 16, j > j0);
+                    else
+                        output(sv, C::kMost / 16, kKeys / 16, true);
                     if (j + 1 == e) commit(&o_full[i]);
                 }
                 if (j + 1 < e) scores(sk);
                 if (leader) tc::mbar_arrive(&turn[i]);
                 commit(&kv_empty[sv]);
                 if (more) {
-                    commit(&kv_empty[sk]);
+                    if (!C::kPaired) commit(&kv_empty[sk]);
                     if (j + 2 == end) commit(&q_empty);
-                    advance();
+                    if (!C::kPaired) advance();
                 }
             }
         }
@@ -500,29 +512,36 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int z = page < 0 ? a.n_pages * a.kv_heads : page * a.kv_heads + wk.h;
                 page = lane < pages ? page_of(a, wk.c.r, key + kKeys, wk.kv) : -1;
 #pragma unroll
-                for (int which = 0; which < 2; ++which) {   // K, then V
-                    if (!(ok = warp_wait(&kv_empty[stage], phase ^ 1))) break;
-                    uint64_t *bar = which && j == tail ? &kv_raw[stage] : &kv_full[stage];
-                    if (leader) tc::mbar_arrive_expect_tx(bar, C::kTile);
+                for (int part = 0; part < 2; ++part) {   // K, then V
+                    if (part == 0 || !C::kPaired) {
+                        if (!(ok = warp_wait(&kv_empty[stage], phase ^ 1))) break;
+                    }
+                    uint64_t *bar = (part || C::kPaired) && j == tail ? &kv_raw[stage]
+                                                                      : &kv_full[stage];
+                    if (leader && (part == 0 || !C::kPaired))
+                        tc::mbar_arrive_expect_tx(bar, C::kStage);
                     // the pages one by one with uniform coordinates: a copy a
                     // lane took longer to issue than a block of 16-token pages
                     // takes to compute
+                    uint8_t *at = ring + (size_t)stage * C::kStage +
+                                  (C::kPaired ? part * C::kTile : 0);
 #pragma unroll 8
                     for (int p = 0; p < pages; ++p) {
                         const int zp = (int)__shfl_sync(0xffffffffu, z, p);
                         const int rp = (j * kKeys + p * box_rows) & page_mask;
                         if (leader) {
-                            uint8_t *dst = ring + (size_t)stage * C::kTile + p * box_rows * 128;
 #pragma unroll
                             for (int x = 0; x < C::kHalves; ++x)
-                                tc::tma_load_3d(dst + x * kHalfBytes, which ? &map_v : &map_k, bar,
-                                                64 * x, rp, zp);
+                                tc::tma_load_3d(at + p * box_rows * 128 + x * kHalfBytes,
+                                                part ? &map_v : &map_k, bar, 64 * x, rp, zp);
                         }
                     }
-                    ++issued;
-                    if (++stage == C::kStages) {
-                        stage = 0;
-                        phase ^= 1;
+                    if (part == 1 || !C::kPaired) {
+                        ++issued;
+                        if (++stage == C::kStages) {
+                            stage = 0;
+                            phase ^= 1;
+                        }
                     }
                 }
             }
@@ -547,14 +566,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             const Halves hv(wk, tq_half);
             if (!hv.live(wk)) continue;
             const int tail = hv.tail(wk, page_mask);
-            const int n = 2 * (hv.end - wk.j0);              // stages this tile takes
+            const int each = C::kPaired ? 1 : 2;             // stages of a block
+            const int n = each * (hv.end - wk.j0);           // and of this tile
             if (tail >= 0) {
-                const int st = (stage + 2 * (tail - wk.j0) + 1) % C::kStages;
+                const int st = (stage + each * (tail - wk.j0) + each - 1) % C::kStages;
                 if (!(ok = warp_wait(&kv_raw[st], (raw_phase >> st) & 1))) break;
                 raw_phase ^= 1u << st;
                 const int from = wk.kv - tail * kKeys;
                 const int to = min(kKeys, (from | page_mask) + 1);
-                uint8_t *v = ring + (size_t)st * C::kTile;
+                uint8_t *v = ring + (size_t)st * C::kStage + (C::kPaired ? C::kTile : 0);
                 for (int x = 0; x < C::kHalves; ++x)
                     for (int k = from * 8 + lane; k < to * 8; k += 32)
                         *reinterpret_cast<uint4 *>(v + x * kHalfBytes + k * 16) =
