@@ -49,14 +49,13 @@ template <int DP> struct Cfg {
     static constexpr int kHalves = DP / 64;                   // 64-column halves of a row
     static constexpr uint32_t kTile = kHalfBytes * kHalves;   // 128 rows
     // Width 64: a stage holds a block's K and V together, which saves the
-    // issuing warps a wait and a commit a block, and the weights are handed
-    // over in one go.  Width 128 has room for five halves of such stages and
-    // takes K and V one by one, and the weights in two parts.
+    // issuing warps a wait and a commit a block (295 -> 273 us for the ragged
+    // chunks below).  Width 128 has room for two such stages and a half, so it
+    // takes K and V one by one (two whole stages: 305 instead of 223 us).
     static constexpr bool kPaired = DP == 64;
     static constexpr int kParts = kPaired ? 2 : 1;            // tiles of a stage
     static constexpr int kStages = 5;
     static constexpr uint32_t kStage = kTile * kParts;
-    static constexpr int kMost = kPaired ? kKeys : 96;        // keys handed over first
     static constexpr size_t kSmem = (size_t)kTile * 2 + (size_t)kStage * kStages + 1024;
 };
 
@@ -162,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     using C = Cfg<DP>;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t kv_full[C::kStages], kv_empty[C::kStages], kv_raw[C::kStages];
-    __shared__ uint64_t q_full, q_empty, s_full[2], p_most[2], p_full[2], o_full[2], turn[2];
+    __shared__ uint64_t q_full, q_empty, s_full[2], p_full[2], o_full[2], turn[2];
     __shared__ uint64_t drained[2];
     __shared__ int64_t scratch[kThreads / 32 + 1];
     __shared__ Cursor cur;
@@ -180,7 +179,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::mbar_init(&q_empty, 2);
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&s_full[i], 1);
-            tc::mbar_init(&p_most[i], kHalfRows);
             tc::mbar_init(&p_full[i], kHalfRows);
             tc::mbar_init(&o_full[i], 1);
             tc::mbar_init(&turn[i], 1);
@@ -293,11 +291,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                         p[k] = *reinterpret_cast<const uint32_t *>(&b);
                     }
                     tmem_st16(ts + 16 * c, p);
-                    if (!C::kPaired && c == C::kMost / 32 - 1) {   // their product may start
-                        tmem_st_wait();
-                        tc::tc_fence_before();
-                        tc::mbar_arrive(&p_most[i]);
-                    }
                 }
                 l += both(sum[0] + sum[1]);
                 tmem_st_wait();
@@ -414,11 +407,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc::mma_commit(&s_full[i]);
             }
         };
-        auto output = [&](int st, int k0, int k1, bool add) {   // keys 16 k0 .. 16 k1
+        auto output = [&](int st, bool add) {
             const uint64_t vd = v_desc + (uint32_t)st * (C::kStage >> 4);
             if (leader) {
 #pragma unroll
-                for (int k = k0; k < k1; ++k)
+                for (int k = 0; k < kKeys / 16; ++k)
                     mma_bf16_ts(t_o, t_s + 8 * k, vd + k * (16 * 128 >> 4), idesc_o, add || k > 0);
             }
         };
@@ -444,21 +437,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool more = j + 1 < end;
                 const int sk = stage;
                 if (more && !(ok = warp_wait(&kv_full[stage], phase))) break;
-                if (!C::kPaired && j < e && !(ok = warp_wait(&p_most[i], p_phase))) break;
                 // half 0 goes first: it waits for half 1's turn before, half 1
                 // for half 0's at this block
                 if (!(ok = warp_wait(&turn[i ^ 1], (turns & 1) ^ (i == 0)))) break;
                 ++turns;
                 if (j < e) {
-                    tc::tc_fence_after();
-                    if constexpr (!C::kPaired) output(sv, 0, C::kMost / 16, j > j0);
                     if (!(ok = warp_wait(&p_full[i], p_phase))) break;
                     p_phase ^= 1;
                     tc::tc_fence_after();
-                    if constexpr (C::kPaired)
-                        output(sv, 0, kKeys / 16, j > j0);
-                    else
-                        output(sv, C::kMost / 16, kKeys / 16, true);
+                    output(sv, j > j0);
                     if (j + 1 == e) commit(&o_full[i]);
                 }
                 if (j + 1 < e) scores(sk);
