@@ -20,14 +20,15 @@
 // the same value, so the quotient is the same, and the pass over O in TMEM
 // that a raise costs is rare.
 //
-// Measured: 4 prompts of 4096 tokens (16 / 4 heads x 128) 202 us without the
-// join of split tiles, 1360 TFLOP/s of what the causal rows need, the tensor
-// pipe 61 % active; 8 ragged chunks over up to 31 k keys at width 64 287 us,
-// 905 TFLOP/s.
+// Measured: 4 prompts of 4096 tokens (16 / 4 heads x 128) 197 us without the
+// join of split tiles, 1396 TFLOP/s of what the causal rows need, the tensor
+// pipe 64 % active; 8 ragged chunks over up to 31 k keys at width 64 264 us,
+// 985 TFLOP/s.
 //
 // Warps: 0-3 and 4-7 the halves' softmax and output, 8 and 11 the halves'
-// products (one thread each), 9 the copies (TMA: K and V blocks, a box per page, in a ring; Q
-// per tile), 10 clears what a last page holds past the request's length.
+// products (one elected thread each), 9 the copies (TMA: K and V blocks, a box
+// per page, in a ring; Q per tile), 10 clears what a last page holds past the
+// request's length.
 #include "um_paged.cuh"
 #include "um_pair.cuh"
 #include "um_tc.cuh"
