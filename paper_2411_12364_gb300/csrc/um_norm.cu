@@ -905,6 +905,19 @@ int mode_of(int dtype, int D, std::initializer_list<const void *> rows,
     return wide % 16 == 0 ? kRun : low % 4 == 0 ? kWord : kHalf;
 }
 
+// Whether all pointers lie on boundaries of `size` bytes.
+bool on_boundary(int size, std::initializer_list<const void *> pointers) {
+    uintptr_t low = 0;
+    for (const void *p : pointers) low |= (uintptr_t)p;
+    return low % size == 0;
+}
+// The same of a call's parameters and its gate (and the gate's gradient).
+bool params_on_boundary(const ultramem_block_norm_args *p, const void *dgate) {
+    const bool channel = p->gate_mode == ULTRAMEM_GATE_CHANNEL;
+    return on_boundary(4, {p->w_post, p->b_post, p->w_pre, p->b_pre}) &&
+           on_boundary(channel || p->dtype == ULTRAMEM_F32 ? 4 : 2, {p->gate, dgate});
+}
+
 }  // namespace
 }  // namespace um
 
@@ -914,6 +927,9 @@ extern "C" ultramem_status ultramem_block_norm(const ultramem_block_norm_args *p
     if (p->n_tokens == 0) return ULTRAMEM_OK;
     if (!p->y || !r || !u || (p->pre != 0) != (n != nullptr) || p->ld_y < p->dim ||
         p->ld_r < p->dim)
+        return ULTRAMEM_EINVAL;
+    const int es = p->dtype == ULTRAMEM_BF16 ? 2 : 4;
+    if (!um::on_boundary(es, {p->y, r, u, n}) || !um::params_on_boundary(p, nullptr))
         return ULTRAMEM_EINVAL;
     um::NormArgs a = um::args_of(p);
     a.r = r;
@@ -964,6 +980,11 @@ extern "C" ultramem_status ultramem_block_norm_backward(
     if (!p->y || p->ld_y < D || (p->pre && (!u || !dn || p->ld_r < D || ld_dn < D)) ||
         (du && ld_du < D) || (!du && !dn) || !workspace || !um::aligned16(workspace) ||
         workspace_bytes < ultramem_block_norm_backward_workspace(p->n_tokens, D))
+        return ULTRAMEM_EINVAL;
+    const int es = p->dtype == ULTRAMEM_BF16 ? 2 : 4;
+    if (!um::on_boundary(es, {p->y, p->pre ? u : nullptr, du, dn, dy, dr}) ||
+        !um::on_boundary(4, {dw_post, db_post, dw_pre, db_pre}) ||
+        !um::params_on_boundary(p, dgate))
         return ULTRAMEM_EINVAL;
     um::NormArgs a = um::args_of(p);
     a.r = u;
