@@ -365,8 +365,9 @@ typedef struct ultramem_kv_cache {
  * ctx_lens[r] cached tokens and brings new_lens[r] (negative counts as 0).
  *   block_table [n_seqs][table_width]: row r's first ceil(ctx/page_size)
  *           entries are read, the entries of new pages are written;
- *   free_pages, free_count [1]: the free list; new pages are taken from its
- *           end, request by request (page k of the call's new ones is
+ *   free_pages [n_free], free_count [1]: the free list and its length (a
+ *           larger one counts as n_free); new pages are taken from its end,
+ *           request by request (page k of the call's new ones is
  *           free_pages[free_count - 1 - k]);
  *   q_start [n_seqs + 1]: first token of each request in the packed batch
  *           (exclusive sum of new_lens);
@@ -387,9 +388,9 @@ typedef struct ultramem_kv_cache {
 ultramem_status ultramem_paged_plan(const int32_t *ctx_lens, const int32_t *new_lens,
                                     int32_t n_seqs, int32_t page_size, int32_t *block_table,
                                     int32_t table_width, const int32_t *free_pages,
-                                    const int32_t *free_count, int32_t n_tokens, int32_t *q_start,
-                                    int32_t *kv_lens, int32_t *slots, int32_t *free_left,
-                                    int32_t *balance, void *stream);
+                                    const int32_t *free_count, int32_t n_free, int32_t n_tokens,
+                                    int32_t *q_start, int32_t *kv_lens, int32_t *slots,
+                                    int32_t *free_left, int32_t *balance, void *stream);
 
 /* The new tokens' keys and values k, v [n_tokens][kv_heads][head_dim] (rows of
  * tokens k_stride and v_stride elements apart) into their slots.  Slots
@@ -415,7 +416,8 @@ ultramem_status ultramem_paged_append(const ultramem_kv_cache *cache, const void
  * accumulate in fp32; with bf16 storage the weights enter the second product
  * as bf16.
  * max_new: an upper bound of n_r known on the host; it chooses the kernel and
- * the workspace (a larger n_r is still computed right).  Rows of out that
+ * the workspace (a larger n_r is still computed right, but 0 says that no
+ * request has rows, and nothing is launched).  Rows of out that
  * belong to no request are not written.  workspace: 16-byte aligned, at least
  * ultramem_paged_attention_workspace bytes, not shared by calls that overlap.
  * ULTRAMEM_EINVAL for invalid sizes, types or null pointers and a scale that
@@ -481,7 +483,8 @@ ultramem_status ultramem_block_norm(const ultramem_block_norm_args *args, const 
  *           dtype [n_tokens][dim] for a full one;
  *   dw_post, db_post, dw_pre, db_pre  fp32 [dim] (written, not accumulated).
  * The sums over tokens are added in a fixed order.  workspace: 16-byte
- * aligned, at least ultramem_block_norm_backward_workspace bytes. */
+ * aligned, at least ultramem_block_norm_backward_workspace bytes.  Both calls
+ * want each pointer on its entries' boundary (ULTRAMEM_EINVAL otherwise). */
 ultramem_status ultramem_block_norm_backward(const ultramem_block_norm_args *args, const void *u,
                                              const void *du, int64_t ld_du, const void *dn,
                                              int64_t ld_dn, void *dy, void *dr, void *dgate,

@@ -144,7 +144,8 @@ def load(path: str | None = None) -> C.CDLL:
         lib.ultramem_shard_pool.argtypes = [P, P, P, I32, P, P, P, P]
         lib.ultramem_shard_pool.restype = I32
         F = C.c_float
-        lib.ultramem_paged_plan.argtypes = [P, P, I32, I32, P, I32, P, P, I32, P, P, P, P, P, P]
+        lib.ultramem_paged_plan.argtypes = [P, P, I32, I32, P, I32, P, P, I32, I32, P, P, P, P, P,
+                                            P]
         lib.ultramem_paged_plan.restype = I32
         lib.ultramem_paged_append.argtypes = [P, P, I64, P, I64, P, I32, P]
         lib.ultramem_paged_append.restype = I32

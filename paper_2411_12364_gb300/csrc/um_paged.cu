@@ -22,7 +22,7 @@ namespace {
 struct PlanArgs {
     const int32_t *ctx, *fresh, *free_pages, *free_count;
     int32_t *table, *q_start, *kv_lens, *slots, *free_left, *balance;
-    int n_seqs, n_tokens, page_shift, table_width;
+    int n_seqs, n_tokens, page_shift, table_width, n_free;
 };
 
 struct PlanRequest {
@@ -51,7 +51,7 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) plan_kernel(Pl
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const int per = (a.n_seqs + THREADS - 1) / THREADS;
     const int r0 = min(a.n_seqs, tid * per), r1 = min(a.n_seqs, r0 + per);
-    const int free = max(0, *a.free_count);
+    const int free = max(0, min(*a.free_count, a.n_free));
     PlanRequest q;
     int64_t need = 0, tok = 0;
     for (int r = r0; r < r1; ++r) {
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<T, ROWS, ND>::kPerSm) rows_k
 #pragma unroll
             for (int c = 0; c < 2 * NQ; ++c) acc[i][c] = f2(0.f);
         // each thread of a row keeps the row's maximum; the sum is its share
-        float m = -INFINITY, l = 0.f;
+        float m = -INFINITY, l = 0.f, base = 0.f;
         const int limit = min(wk.kv, wk.pos0 + srow / a.group + 1);   // keys this row sees
         int stage = 0;
         for (int j = wk.j0; j < wk.j1; ++j, stage ^= 1) {
@@ -347,8 +347,9 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<T, ROWS, ND>::kPerSm) rows_k
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
             // exponents as one product and difference: what rounds is the
             // difference, not the score; a row without keys so far refers to 0
-            const float base = mx == -INFINITY ? 0.f : -mx * a.scale_log2;
-            const float f = exp2f(fmaf(m, a.scale_log2, base));
+            const float before = base;
+            base = mx == -INFINITY ? 0.f : -mx * a.scale_log2;
+            const float f = m == -INFINITY ? 0.f : exp2f(base - before);
             m = mx;
             float sum = 0.f;
 #pragma unroll
@@ -466,16 +467,21 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<T, ROWS, ND>::kPerSm) rows_k
 }
 
 // ---- join of split tiles ----------------------------------------------------
-// Block (c, y) joins rows of the tile that begins in share c and ends in a
-// later one: weights 2^(m_i - max m) over the shares' partials, added in a
+// Weights 2^(m_i - max m) over the shares' partials of a tile, added in a
 // fixed order, so the result does not depend on which share finished first.
 // The work is a chain of dependent loads (records, statistics, outputs), so
-// each step is one round of loads for the whole block.  A long axis with few
-// rows leaves many partials of few rows (one request of 131072 keys: 76 of
-// 4): a block a row, its 8 warps over the partials.  Chunks leave two or
-// three partials of up to 256 rows: a block 32 rows, a warp four of them.
-// (76 partials a row by one warp took 82 us, by a block 10, most of it the
-// first touch of memory.)
+// each step is one round of loads.
+//
+// Up to 16 rows a tile (single tokens: one request of 131072 keys leaves 76
+// partials of 4 rows): block (c, y) takes row y of the tile that begins in
+// share c, its 8 warps split the partials (10 us; by one warp 82).  Taller
+// tiles: every block lists the split tiles and takes its part of all (tile,
+// rows) units, a warp one row or four.  One row where tiles are few and
+// their partials many, so that a row's loads over the partials fill the
+// flight (29 and 64 tokens over 48 k and 65 k keys: 33 and 54 us with the
+// attention, four rows 77 and 76); four rows where most tiles have two or
+// three partials (4 prompts of 4096: 208 us, one row 215; 8 ragged chunks 273
+// and 281).
 struct Span {
     int slot, n;                // place of the first partial, shares of the tile
     int tok0, n_rows, h;
@@ -590,91 +596,167 @@ __global__ void __launch_bounds__(256) join_row_kernel(AttnArgs a, int ctas) {
     }
 }
 
-constexpr int kJoinRows = 32;
+// A place of join_rows_kernel's list of split tiles.
+struct Split {
+    int4 desc;                  // of the tile's first partial
+    int first, slot, last;      // its share and place, the tile's last share
+    int pad;
+};
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(256) join_rows_kernel(AttnArgs a, int ctas) {
-    constexpr int kC = DP / 32;
-    extern __shared__ int shared[];
-    int *kind = shared;
-    float *weight = reinterpret_cast<float *>(shared + ctas);   // [n][kJoinRows]
-    __shared__ int last;
-    __shared__ float scale[kJoinRows];       // 1 / sum, 0 for a row without keys
+// RW: rows a warp takes at a time.
+template <typename T, int DP, int RW>
+__global__ void __launch_bounds__(256, DP > 128 ? 2 : 3)
+    join_rows_kernel(AttnArgs a, int ctas, int groups) {
+    constexpr int V = DP % 128 == 0 ? 4 : 2, kN = DP / (32 * V);   // a lane's columns: kN runs of V
+    constexpr int kRows = 8 * RW, kSub = 32 / RW;
+    using W = std::conditional_t<V == 4, float4, float2>;
+    extern __shared__ __align__(16) char joined[];
+    Split *split = reinterpret_cast<Split *>(joined);
+    int *kind = reinterpret_cast<int *>(split + ctas);
+    __shared__ int2 count[8];
     pdl_wait();
-    const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-    Span s;
-    if (!find_span(a, c, ctas, kind, &last, &s)) return;
-    for (int row0 = blockIdx.y * kJoinRows; row0 < s.n_rows; row0 += gridDim.y * kJoinRows) {
-        if (tid < kJoinRows && row0 + tid < s.n_rows) {
-            float m = -INFINITY, sum = 0.f;
-            for (int i = 0; i < s.n; ++i)
-                if (kind[i] != kPartNone)
-                    m = fmaxf(m, a.part_ml[record_of(a, s, c, i, row0 + tid)].x);
-            const float base = m == -INFINITY ? 0.f : m;
-            for (int i = 0; i < s.n; ++i) {
-                float f = 0.f;               // a share without a block of this tile
-                if (kind[i] != kPartNone) {
-                    const float2 ml = a.part_ml[record_of(a, s, c, i, row0 + tid)];
-                    f = exp2f(ml.x - base);
-                    sum = fmaf(f, ml.y, sum);
-                }
-                weight[i * kJoinRows + tid] = f;
-            }
-            scale[tid] = sum == 0.f ? 0.f : 1.f / sum;
-            if (a.lse) a.lse[head_of(a, s, row0 + tid)] = lse_of(m, sum);
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    // the split tiles in order: tiles follow one another on the axis, so the
+    // k-th first partial and the k-th last one are of the same tile
+    int n_first = 0, n_last = 0;
+    for (int c0 = 0; c0 < ctas; c0 += 256) {
+        const int c = c0 + tid;
+        int4 d0 = make_int4(kPartNone, 0, 0, 0), d1 = d0;
+        if (c < ctas) {
+            d0 = a.part_desc[2 * c];
+            d1 = a.part_desc[2 * c + 1];
+            kind[c] = d0.x;
         }
+        const bool is_first = d0.x == kPartFirst || d1.x == kPartFirst, is_last = d0.x == kPartLast;
+        const unsigned f = __ballot_sync(0xffffffffu, is_first);
+        const unsigned l = __ballot_sync(0xffffffffu, is_last);
+        if (lane == 0) count[w] = make_int2(__popc(f), __popc(l));
         __syncthreads();
-        float acc[kJoinRows / 8][kC];
+        const unsigned below = (1u << lane) - 1;
+        int kf = n_first + __popc(f & below), kl = n_last + __popc(l & below);
+        for (int i = 0; i < 8; ++i) {
+            const int2 x = count[i];
+            if (i < w) {
+                kf += x.x;
+                kl += x.y;
+            }
+            n_first += x.x;
+            n_last += x.y;
+        }
+        if (is_first) {
+            const int slot = d0.x == kPartFirst ? 0 : 1;
+            split[kf].desc = slot ? d1 : d0;
+            split[kf].first = c;
+            split[kf].slot = slot;
+        }
+        if (is_last) split[kl].last = c;
+        __syncthreads();
+    }
+    for (int unit = blockIdx.x; unit < n_first * groups; unit += gridDim.x) {
+        const Split &p = split[unit / groups];
+        const int c = p.first, n_rows = p.desc.z * a.group;
+        const int n = (unit / groups < n_last ? p.last : ctas - 1) - c + 1;
+        const Span s = {p.slot, n, p.desc.y, n_rows, p.desc.w};
+        for (int row0 = unit % groups * kRows + w * RW; row0 < n_rows; row0 += groups * kRows) {
+            // lane (sub, r): partials sub, sub + kSub .. of row row0 + r
+            const int mine = row0 + lane % RW, sub = lane / RW;
+            auto stat = [&](int i) {
+                float2 ml = make_float2(-INFINITY, 0.f);   // without a block of this tile
+                if (i < n && mine < n_rows && (i == 0 || kind[c + i] != kPartNone))
+                    ml = a.part_ml[record_of(a, s, c, i, mine)];
+                return ml;
+            };
+            const float2 head = stat(sub);
+            float m = head.x, sum = 0.f;
+            for (int i = sub + kSub; i < n; i += kSub) m = fmaxf(m, stat(i).x);
 #pragma unroll
-        for (int r = 0; r < kJoinRows / 8; ++r)
+            for (int o = 16; o >= RW; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            const float base = m == -INFINITY ? 0.f : m;
+            float acc[RW][kN][V];
 #pragma unroll
-            for (int k = 0; k < kC; ++k) acc[r][k] = 0.f;
-        for (int i = 0; i < s.n; ++i) {
-            if (kind[i] == kPartNone) continue;
+            for (int r = 0; r < RW; ++r)
 #pragma unroll
-            for (int r = 0; r < kJoinRows / 8; ++r) {
-                const int row = w + 8 * r;
-                if (row0 + row >= s.n_rows) continue;
-                const float f = weight[i * kJoinRows + row];
-                const float *o = a.part_o + record_of(a, s, c, i, row0 + row) * DP + lane;
+                for (int k = 0; k < kN; ++k)
 #pragma unroll
-                for (int k = 0; k < kC; ++k)
-                    acc[r][k] = f == 0.f ? acc[r][k] : fmaf(f, o[32 * k], acc[r][k]);
+                    for (int e = 0; e < V; ++e) acc[r][k][e] = 0.f;
+            for (int i0 = 0; i0 < n; i0 += kSub) {
+                const float2 ml = i0 ? stat(i0 + sub) : head;
+                const float weight = exp2f(ml.x - base);
+                sum = fmaf(weight, ml.y, sum);
+                const int left = min(kSub, n - i0);
+#pragma unroll(8 / RW)
+                for (int i = 0; i < left; ++i)
+#pragma unroll
+                    for (int r = 0; r < RW; ++r) {
+                        const float f = __shfl_sync(0xffffffffu, weight, i * RW + r);
+                        if (row0 + r >= n_rows) continue;
+                        const int64_t rec = record_of(a, s, c, i0 + i, row0 + r);
+                        const W *o = reinterpret_cast<const W *>(a.part_o + rec * DP) + lane;
+#pragma unroll
+                        for (int k = 0; k < kN; ++k) {
+                            const W x = o[32 * k];
+                            const float *v = reinterpret_cast<const float *>(&x);
+#pragma unroll
+                            for (int e = 0; e < V; ++e) {   // an absent partial holds anything
+                                const float y = fmaf(f, v[e], acc[r][k][e]);
+                                acc[r][k][e] = f == 0.f ? acc[r][k][e] : y;
+                            }
+                        }
+                    }
+            }
+#pragma unroll
+            for (int o = 16; o >= RW; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (a.lse && sub == 0 && mine < n_rows) a.lse[head_of(a, s, mine)] = lse_of(m, sum);
+            const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+            for (int r = 0; r < RW; ++r) {
+                const float x = __shfl_sync(0xffffffffu, inverse, r);
+                if (row0 + r >= n_rows) continue;
+                T *o = static_cast<T *>(a.out) + head_of(a, s, row0 + r) * a.D;
+#pragma unroll
+                for (int k = 0; k < kN; ++k)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const int col = 32 * V * k + V * lane + e;
+                        if (col < a.D) o[col] = from_f<T>(acc[r][k][e] * x);
+                    }
             }
         }
-#pragma unroll
-        for (int r = 0; r < kJoinRows / 8; ++r) {
-            const int row = w + 8 * r;
-            if (row0 + row >= s.n_rows) continue;
-            T *o = static_cast<T *>(a.out) + head_of(a, s, row0 + row) * a.D;
-#pragma unroll
-            for (int k = 0; k < kC; ++k)
-                if (lane + 32 * k < a.D) o[lane + 32 * k] = from_f<T>(acc[r][k] * scale[row]);
-        }
-        __syncthreads();                     // the next rows reuse the shared arrays
     }
 }
 
+template <typename T, int DP, int RW>
+cudaError_t join_rows(const AttnArgs &a, int ctas, int rows, bool pdl, cudaStream_t st) {
+    const int groups = (rows + 8 * RW - 1) / (8 * RW);
+    const int most = device_sm_count() * (RW == 1 ? 8 : 4), units = ctas * groups;
+    return launch_kernel(pdl, join_rows_kernel<T, DP, RW>, dim3(units < most ? units : most), 256,
+                         (size_t)ctas * (sizeof(Split) + 4), st, a, ctas, groups);
+}
+
+// max_new and the batch bound the number of tiles: a few tiles on all CTAs
+// leave many partials each.
 template <typename T, int DP>
-cudaError_t combine_dim(const AttnArgs &a, int ctas, bool pdl, cudaStream_t st) {
+cudaError_t combine_dim(const AttnArgs &a, int ctas, int max_new, bool pdl, cudaStream_t st) {
     // blocks for the rows that the caller's bound announces; a block goes on
     // to further rows where there are more
     const int rows = a.rows < a.rows_hint ? a.rows : a.rows_hint;
-    if (rows <= 64)
-        return launch_kernel(pdl, join_row_kernel<T, DP>, dim3(ctas, rows), 256,
-                             (size_t)8 * ctas, st, a, ctas);
-    return launch_kernel(pdl, join_rows_kernel<T, DP>,
-                         dim3(ctas, (rows + kJoinRows - 1) / kJoinRows), 256,
-                         (size_t)4 * (1 + kJoinRows) * ctas, st, a, ctas);
+    if (rows <= 16)
+        return launch_kernel(pdl, join_row_kernel<T, DP>, dim3(ctas, rows), 256, (size_t)8 * ctas,
+                             st, a, ctas);
+    const int64_t of_max = (int64_t)a.n_seqs * ((max_new + (int64_t)a.tq - 1) / a.tq);
+    const int64_t of_all = (int64_t)a.n_seqs + a.n_tokens / a.tq;
+    const int64_t tiles = (of_max < of_all ? of_max : of_all) * a.kv_heads;
+    return 2 * tiles <= ctas ? join_rows<T, DP, 1>(a, ctas, rows, pdl, st)
+                             : join_rows<T, DP, 4>(a, ctas, rows, pdl, st);
 }
 
-template <typename T> cudaError_t combine(const AttnArgs &a, int ctas, int dp, bool pdl,
-                                          cudaStream_t st) {
+template <typename T> cudaError_t combine(const AttnArgs &a, int ctas, int dp, int max_new,
+                                          bool pdl, cudaStream_t st) {
     switch (dp) {
-    case 64: return combine_dim<T, 64>(a, ctas, pdl, st);
-    case 128: return combine_dim<T, 128>(a, ctas, pdl, st);
-    case 192: return combine_dim<T, 192>(a, ctas, pdl, st);
-    default: return combine_dim<T, 256>(a, ctas, pdl, st);
+    case 64: return combine_dim<T, 64>(a, ctas, max_new, pdl, st);
+    case 128: return combine_dim<T, 128>(a, ctas, max_new, pdl, st);
+    case 192: return combine_dim<T, 192>(a, ctas, max_new, pdl, st);
+    default: return combine_dim<T, 256>(a, ctas, max_new, pdl, st);
     }
 }
 
@@ -764,8 +846,8 @@ Layout layout_of(Path path, int32_t dtype, int32_t group, int32_t dim, int32_t m
         l.extra = p.keys;
     }
     if (path != kPrefill) l.tq = l.rows / group;
-    // join_row_kernel's threads hold two shares each
-    if (l.ctas > 512) l.ctas = 512;
+    // what the join kernels hold: two shares a thread, 100 bytes a share
+    if (l.ctas > 480) l.ctas = 480;
     l.o = 0;
     l.ml = l.o + (int64_t)l.ctas * 2 * l.rows * l.dp * 4;
     l.desc = (l.ml + (int64_t)l.ctas * 2 * l.rows * 8 + 15) & ~15ll;
@@ -841,10 +923,10 @@ bool heads_ok(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim, int
 
 }  // namespace
 
-cudaError_t launch_combine(const AttnArgs &a, int ctas, int dp, int dtype, bool pdl,
+cudaError_t launch_combine(const AttnArgs &a, int ctas, int dp, int dtype, int max_new, bool pdl,
                            cudaStream_t st) {
-    return dtype == ULTRAMEM_BF16 ? combine<__nv_bfloat16>(a, ctas, dp, pdl, st)
-                                  : combine<float>(a, ctas, dp, pdl, st);
+    return dtype == ULTRAMEM_BF16 ? combine<__nv_bfloat16>(a, ctas, dp, max_new, pdl, st)
+                                  : combine<float>(a, ctas, dp, max_new, pdl, st);
 }
 
 }  // namespace paged
@@ -856,21 +938,22 @@ extern "C" ultramem_status ultramem_paged_plan(const int32_t *ctx_lens, const in
                                                int32_t n_seqs, int32_t page_size,
                                                int32_t *block_table, int32_t table_width,
                                                const int32_t *free_pages,
-                                               const int32_t *free_count, int32_t n_tokens,
-                                               int32_t *q_start, int32_t *kv_lens,
-                                               int32_t *slots, int32_t *free_left,
-                                               int32_t *balance, void *stream) {
-    if (n_seqs < 0 || n_tokens < 0 || table_width < 0 || !page_size_ok(page_size) || !free_count ||
-        !q_start || !balance || free_left == free_count || balance == free_count ||
-        balance == free_left)
+                                               const int32_t *free_count, int32_t n_free,
+                                               int32_t n_tokens, int32_t *q_start,
+                                               int32_t *kv_lens, int32_t *slots,
+                                               int32_t *free_left, int32_t *balance,
+                                               void *stream) {
+    if (n_seqs < 0 || n_tokens < 0 || table_width < 0 || n_free < 0 ||
+        !page_size_ok(page_size) || !free_count || !q_start || !balance ||
+        free_left == free_count || balance == free_count || balance == free_left)
         return ULTRAMEM_EINVAL;
     if (n_seqs > 0 && (!ctx_lens || !new_lens || !kv_lens || kv_lens == ctx_lens ||
                        kv_lens == new_lens || (table_width > 0 && !block_table)))
         return ULTRAMEM_EINVAL;
-    if (n_tokens > 0 && (!slots || !free_pages)) return ULTRAMEM_EINVAL;
+    if ((n_tokens > 0 && !slots) || (n_free > 0 && !free_pages)) return ULTRAMEM_EINVAL;
     PlanArgs a = {ctx_lens, new_lens,  free_pages, free_count, block_table,
                   q_start,  kv_lens,   slots,      free_left,  balance,
-                  n_seqs,   n_tokens,  shift_of(page_size),    table_width};
+                  n_seqs,   n_tokens,  shift_of(page_size),    table_width, n_free};
     cudaStream_t st = (cudaStream_t)stream;
     cudaGetLastError();
     // more than 256 requests: wider blocks, so that no thread walks many
@@ -1019,7 +1102,8 @@ extern "C" ultramem_status ultramem_paged_attention(
     // tables that hold no more keys than a tile keeps whole leave nothing to
     // join (a launch less: 3 us of a call of 10 to 20)
     const int64_t held = (int64_t)table_width << a.page_shift;
-    if (e == cudaSuccess && held > whole_keys(a)) e = launch_combine(a, l.ctas, l.dp, c->dtype, true, st);
+    if (e == cudaSuccess && held > whole_keys(a))
+        e = launch_combine(a, l.ctas, l.dp, c->dtype, max_new, true, st);
     return um::status_from_cuda(e);
 }
 

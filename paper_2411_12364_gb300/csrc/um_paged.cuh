@@ -236,7 +236,7 @@ cudaError_t launch_decode(const AttnArgs &a, const CUtensorMap &k, const CUtenso
                           cudaStream_t st);
 cudaError_t launch_prefill(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &k,
                            const CUtensorMap &v, int ctas, cudaStream_t st);
-cudaError_t launch_combine(const AttnArgs &a, int ctas, int dp, int dtype, bool pdl,
+cudaError_t launch_combine(const AttnArgs &a, int ctas, int dp, int dtype, int max_new, bool pdl,
                            cudaStream_t st);
 
 }  // namespace paged

@@ -94,8 +94,8 @@ def paged_plan(ctx_lens, new_lens, block_table, free_pages, free_count, page_siz
     status = lib.ultramem_paged_plan(
         _int32("ctx_lens", ctx_lens), _int32("new_lens", new_lens), R, page_size,
         _int32("block_table", block_table), table_shape[1], _int32("free_pages", free_pages),
-        _int32("free_count", free_count), n_tokens, q_start.data_ptr(), kv_lens.data_ptr(),
-        slots.data_ptr(), free_ptr, balance.data_ptr(), _b._stream())
+        _int32("free_count", free_count), free_pages.numel(), n_tokens, q_start.data_ptr(),
+        kv_lens.data_ptr(), slots.data_ptr(), free_ptr, balance.data_ptr(), _b._stream())
     if status:
         raise _b.UltraMemError(status, "ultramem_paged_plan")
     return q_start, kv_lens, slots, balance
@@ -131,7 +131,8 @@ def paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new:
     q_start [R+1]) over the pages of block_table [R, width]: out like q, and
     the rows' log-sum-exp [tokens, q_heads] fp32 when ``with_lse``.  max_new:
     the most new tokens a request has (a host number); scale: default
-    1 / sqrt(head_dim)."""
+    1 / sqrt(head_dim).  Rows that belong to no request (past q_start[R]) are
+    not written."""
     c, shape, dtype = _cache(k_cache, v_cache)
     heads, dim = shape[1], shape[3]
     q, qs = _rows("q", q, 0, dim, dtype)

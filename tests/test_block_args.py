@@ -34,11 +34,11 @@ def test_invalid_caches_are_refused(bad):
 
 def test_plan_arguments():
     lib = binding.load()
-    good = [FAKE, 2 * FAKE, 2, 16, 3 * FAKE, 4, 4 * FAKE, 5 * FAKE, 8, 6 * FAKE, 7 * FAKE,
+    good = [FAKE, 2 * FAKE, 2, 16, 3 * FAKE, 4, 4 * FAKE, 5 * FAKE, 7, 8, 6 * FAKE, 7 * FAKE,
             8 * FAKE, 9 * FAKE, 10 * FAKE, None]
     for at, bad in ((0, None), (1, None), (2, -1), (3, 0), (3, 17), (4, None), (5, -1), (6, None),
-                    (7, None), (8, -1), (9, None), (10, None), (10, FAKE), (11, None),
-                    (12, 5 * FAKE), (13, None), (13, 5 * FAKE), (13, 9 * FAKE)):
+                    (7, None), (8, -1), (9, -1), (10, None), (11, None), (11, FAKE), (12, None),
+                    (13, 5 * FAKE), (14, None), (14, 5 * FAKE), (14, 9 * FAKE)):
         args = list(good)
         args[at] = bad
         assert lib.ultramem_paged_plan(*args) == binding.EINVAL, (at, bad)
@@ -137,3 +137,36 @@ def test_norm_backward_pointers():
     args = list(good)
     args[0] = C.byref(off)
     assert lib.ultramem_block_norm_backward(*args) == binding.EINVAL
+
+
+@pytest.mark.parametrize("dtype,es", [(binding.BF16, 2), (binding.F32, 4)])
+def test_norm_pointers_inside_an_entry(dtype, es):
+    lib = binding.load()
+    need = lib.ultramem_block_norm_backward_workspace(4, 64)
+    a = _norm_args(dtype=dtype)
+    for at in (1, 2, 3):
+        args = [C.byref(a), FAKE, FAKE, FAKE, None]
+        args[at] = FAKE + es // 2
+        assert lib.ultramem_block_norm(*args) == binding.EINVAL, at
+    good = [C.byref(a), FAKE, FAKE, 64, FAKE, 64, FAKE, FAKE, None, FAKE, None, FAKE, None, FAKE,
+            need, None]
+    for at in (1, 2, 4, 6, 7):
+        args = list(good)
+        args[at] = FAKE + es // 2
+        assert lib.ultramem_block_norm_backward(*args) == binding.EINVAL, at
+    for at in (9, 11):       # fp32 whatever the rows are
+        args = list(good)
+        args[at] = FAKE + 2
+        assert lib.ultramem_block_norm_backward(*args) == binding.EINVAL, at
+    for name in ("y", "w_post", "w_pre"):
+        off = _norm_args(dtype=dtype, **{name: FAKE + (es // 2 if name == "y" else 2)})
+        assert lib.ultramem_block_norm(C.byref(off), FAKE, FAKE, FAKE, None) == binding.EINVAL
+        args = [C.byref(off)] + good[1:]
+        assert lib.ultramem_block_norm_backward(*args) == binding.EINVAL, name
+    for mode, shift in ((1, 2), (2, es // 2), (3, es // 2)):
+        off = _norm_args(dtype=dtype, gate_mode=mode, gate=FAKE + shift)
+        assert lib.ultramem_block_norm(C.byref(off), FAKE, FAKE, FAKE, None) == binding.EINVAL
+        off = _norm_args(dtype=dtype, gate_mode=mode, gate=FAKE)
+        args = [C.byref(off)] + good[1:]
+        args[8] = FAKE + shift
+        assert lib.ultramem_block_norm_backward(*args) == binding.EINVAL, mode

@@ -93,6 +93,18 @@ def test_plan_refuses_what_does_not_fit(gpu_lib):
     _check_plan([3, 0, 9], [10, 10, 2], 4, 16, 9, 9, n_tokens=40)
 
 
+def test_plan_counts_no_more_pages_than_the_list_has(gpu_lib):
+    args = (_i32([0, 0]), _i32([40, 40]))
+    pages = _i32([7, 8, 9, 4])
+    out = []
+    for free in (4, 5, 1 << 30):
+        table, left = torch.full((2, 4), -1, dtype=torch.int32, device="cuda"), _i32([0])
+        q_start, kv, slots, balance = paged_plan(*args, table, pages, _i32([free]), 16, 80, left)
+        out.append([x.tolist() for x in (table, left, q_start, kv, slots, balance)])
+    assert out[0][0] == [[4, 9, 8, -1], [-1] * 4] and out[0][1] == [1] and out[0][3] == [40, 0]
+    assert out[1] == out[0] and out[2] == out[0]
+
+
 def test_plan_of_idle_negative_and_long_requests(gpu_lib):
     _check_plan([0, 5, 0], [0, 0, 0], 3, 16, 2, 2, n_tokens=0)
     _check_plan([-3, 7, 4], [5, -2, 1], 3, 16, 4, 4)
@@ -272,6 +284,20 @@ def test_long_axis_is_split_and_joined(dtype, kv, n, page, gpu_lib):
     c.check(out, lse)
     again = c.run()                       # the join's order is fixed
     assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.parametrize("dtype,dim", [(BF16, 64), (BF16, 128), (BF16, 192), (F32, 128), (F32, 256)])
+@pytest.mark.parametrize("reqs", [[(20011, 29)], [(15000, 150), (40, 3)],
+                                  [(3000 + 77 * i, 20 + 9 * i) for i in range(12)]],
+                         ids=["one", "two", "several"])
+def test_tall_tiles_in_many_or_few_shares(dtype, dim, reqs, gpu_lib):
+    """17 and more rows a tile: many partials each, and few."""
+    c = Case(reqs, 10, 2, dim, 32, dtype, seed=14, peak=2.0)
+    out, lse = c.run()
+    c.check(out, lse)
+    again = c.run()                       # the join's order is fixed
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    c.check(*c.run(max_new=2))            # less than there is
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
