@@ -189,14 +189,17 @@ __global__ void __launch_bounds__(256) append_kernel(const W *k, const W *v, int
 // of a warp; a thread accumulates 4 rows x 4 ND columns.  Few rows (8, 16:
 // single tokens) leave nothing to share, so there the threads of one column
 // group split the keys between them, each with 8 rows, and add up at the
-// tile's end.  Measured in fp32: 6 single tokens over
-// up to 31 k keys (16 / 8 heads x 128) 304 us, 2.9 TB/s; 2 chunks of up to 49
-// tokens over 2 k keys (10 / 2 heads x 128) 45 us.
+// tile's end, and warps whose rows are not there take no scores (each reads
+// all keys: 295 -> 238 us for the first case below).  Blocks of 64 keys are for
+// up to 256 bytes a key, 32 keep two CTAs an SM beyond (238 -> 183 us).
+// Measured in fp32: 6 single tokens over up to 31 k keys (16 / 8 heads x 128)
+// 183 us, 4.5 TB/s; 8 chunks of up to 45 tokens over up to 24 k keys (8 / 2
+// heads x 128) 418 us.
 constexpr int kThreads = 256;
 
 template <typename T, int ROWS, int ND> struct RowsCfg {
     static constexpr int DP = 64 * ND;
-    static constexpr int kKeys = ND <= 2 ? 64 : 32;
+    static constexpr int kKeys = ND * (int)sizeof(T) <= 4 ? 64 : 32;   // of a block
     static constexpr bool kFew = ROWS <= 16;
     static constexpr int kPitch = DP * (int)sizeof(T) + 16;      // of a key, bytes
     static constexpr int kLdQ = DP + 4, kLdP = ROWS + 4;         // floats
@@ -312,54 +315,58 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<T, ROWS, ND>::kPerSm) rows_k
             asm volatile("cp.async.commit_group;" ::: "memory");
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncthreads();
-            // of 64 rows a warp has 8 in both products: one without any goes on
-            if (!C::kFew && 8 * (tid >> 5) >= n_rows) {
+            // a warp has ROWS / 8 rows' scores: one without any rows goes on to
+            // the values (of 64 rows it has the same rows there, and none)
+            const bool live = ROWS / 8 * (tid >> 5) < n_rows;
+            if (!C::kFew && !live) {
                 __syncthreads();
                 __syncthreads();
                 continue;
             }
-            // scores: this thread's row, keys spos + TPR i
-            F2 dot[KPT];
+            if (live) {
+                // scores: this thread's row, keys spos + TPR i
+                F2 dot[KPT];
 #pragma unroll
-            for (int i = 0; i < KPT; ++i) dot[i] = f2(0.f);
+                for (int i = 0; i < KPT; ++i) dot[i] = f2(0.f);
 #pragma unroll 4
-            for (int c = 0; c < DP; c += 4) {
-                const float4 x = load4(qs + srow * C::kLdQ + c);
-                const F2 x0 = f2(x.x, x.y), x1 = f2(x.z, x.w);
+                for (int c = 0; c < DP; c += 4) {
+                    const float4 x = load4(qs + srow * C::kLdQ + c);
+                    const F2 x0 = f2(x.x, x.y), x1 = f2(x.z, x.w);
+#pragma unroll
+                    for (int i = 0; i < KPT; ++i) {
+                        const float4 y = load4(key_at(stage, 0, spos + TPR * i) + c);
+                        dot[i] = fma2(x0, f2(y.x, y.y), dot[i]);
+                        dot[i] = fma2(x1, f2(y.z, y.w), dot[i]);
+                    }
+                }
+                float s[KPT];
+#pragma unroll
+                for (int i = 0; i < KPT; ++i) s[i] = both(dot[i]);
+                float mx = m;
 #pragma unroll
                 for (int i = 0; i < KPT; ++i) {
-                    const float4 y = load4(key_at(stage, 0, spos + TPR * i) + c);
-                    dot[i] = fma2(x0, f2(y.x, y.y), dot[i]);
-                    dot[i] = fma2(x1, f2(y.z, y.w), dot[i]);
+                    s[i] = j * kKeys + spos + TPR * i < limit ? s[i] : -INFINITY;
+                    mx = fmaxf(mx, s[i]);
                 }
+#pragma unroll
+                for (int o = TPR / 2; o > 0; o >>= 1)
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                // exponents as one product and difference: what rounds is the
+                // difference, not the score; a row without keys so far refers to 0
+                const float before = base;
+                base = mx == -INFINITY ? 0.f : -mx * a.scale_log2;
+                const float f = m == -INFINITY ? 0.f : exp2f(base - before);
+                m = mx;
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < KPT; ++i) {
+                    const float p = exp2f(fmaf(s[i], a.scale_log2, base));
+                    sum += p;
+                    ps[(spos + TPR * i) * C::kLdP + srow] = p;
+                }
+                l = fmaf(l, f, sum);
+                if (spos == 0) alpha[srow] = f;
             }
-            float s[KPT];
-#pragma unroll
-            for (int i = 0; i < KPT; ++i) s[i] = both(dot[i]);
-            float mx = m;
-#pragma unroll
-            for (int i = 0; i < KPT; ++i) {
-                s[i] = j * kKeys + spos + TPR * i < limit ? s[i] : -INFINITY;
-                mx = fmaxf(mx, s[i]);
-            }
-#pragma unroll
-            for (int o = TPR / 2; o > 0; o >>= 1)
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            // exponents as one product and difference: what rounds is the
-            // difference, not the score; a row without keys so far refers to 0
-            const float before = base;
-            base = mx == -INFINITY ? 0.f : -mx * a.scale_log2;
-            const float f = m == -INFINITY ? 0.f : exp2f(base - before);
-            m = mx;
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < KPT; ++i) {
-                const float p = exp2f(fmaf(s[i], a.scale_log2, base));
-                sum += p;
-                ps[(spos + TPR * i) * C::kLdP + srow] = p;
-            }
-            l = fmaf(l, f, sum);
-            if (spos == 0) alpha[srow] = f;
             __syncthreads();
             if (!C::kFew || group < C::kGroups) {
                 // a block's sum is taken by itself and then added, so that a long
