@@ -10,15 +10,16 @@
 //
 // What bounds it: every entry of y and r is read once and every entry of u
 // and n written once, about 30 operations apart, so the bound is memory.  A
-// row lies in the registers of one warp (up to 256 entries), one block (up to
-// 4096) or a cluster of two blocks, 8 entries a thread, between its two norms.
+// row lies in the registers of one warp (up to 256 entries) or one block (in
+// the gradient, which needs 128 registers a thread, past 4096 entries a cluster
+// of two), 8 entries a thread, between its two norms.
 // The rows' sums are chains of barriers, so the bytes in flight must not
 // depend on them: each thread copies its own 16-byte pieces of the next rows
 // into shared memory (cp.async), two or three rows ahead, and waits for its own copies
 // only.  Blocks are persistent, so that the gains, biases and the per-channel
 // gate are read once per block, into registers.  Measured at 16384 x 2048 in
-// bf16 with a full gate: 60 us forward, 5.6 TB/s of what has to move; the
-// gradient with a channel gate 78 us, 5.2 TB/s.
+// bf16 with a full gate: 57 us forward, 5.9 TB/s of what has to move; the
+// gradient with a channel gate 80 us, 5.0 TB/s.
 #include "um_internal.cuh"
 #include "um_pair.cuh"
 #include "um_tc.cuh"
@@ -85,8 +86,8 @@ __device__ __forceinline__ F2 as_stored(F2 x, __nv_bfloat16) {
 __device__ __forceinline__ F2 as_stored(F2 x, float) { return x; }
 
 // Rows in flight ahead of the one at work.  At 16384 x 2048 in bf16 the
-// forward took 60.2 us with two and 61.4 with three, the gradient 80.4 and
-// 78.2 (fp32 and odd rows of 4096 entries leave room for two): the blocks of
+// forward took 60.2 us with two and 61.4 with three (57 with two since), the
+// gradient 80.4 and 78.2 (fp32 and odd rows of 4096 entries leave room for two): the blocks of
 // an SM together keep enough bytes in flight.
 constexpr int kAhead = 2;
 template <typename T, int MODE>
@@ -431,21 +432,26 @@ __device__ __forceinline__ void fold_post(F2 (&W)[kP], F2 (&B)[kP], const NormAr
     }
 }
 
-// A row per NT CL threads, grid-stride; rows of one warp go four to a block.
-template <typename T, int MODE, int NT, int CL, bool LAYER>
-__global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArgs a) {
-    constexpr int TPR = NT * CL;
+// Blocks of the forward that an SM is to have registers for, 640 to 1024
+// threads.  (Layer norms take 86 to 98 registers without the bound: 72 us
+// against 62 at 16384 x 2048.)
+template <int NT> constexpr int kBlocks = NT > 512 ? 1 : NT >= 384 ? 2 : NT == 32 ? 5 : 768 / NT;
+
+// A row per NT threads, grid-stride; rows of one warp go four to a block.
+template <typename T, int MODE, int NT, bool LAYER>
+__global__ void __launch_bounds__(NT == 32 ? 128 : NT, kBlocks<NT>)
+    block_norm_kernel(NormArgs a) {
+    constexpr int TPR = NT;
     extern __shared__ uint4 ring[];
     __shared__ __align__(16) float buf[2][kSumSlots];
-    RowSum<NT, CL> sum{buf, 0};
-    const int rank = CL > 1 ? (int)tc::cluster_ctarank() : 0;
-    const int t = NT == 32 ? (threadIdx.x & 31) : threadIdx.x + NT * rank;
+    RowSum<NT, 1> sum{buf, 0};
+    const int t = NT == 32 ? (threadIdx.x & 31) : threadIdx.x;
     const int rows = NT == 32 ? blockDim.x >> 5 : 1;
     const bool full = a.gate_mode == ULTRAMEM_GATE_FULL;
     const float inv = 1.f / (float)a.D;
-    Feed<T, MODE, NT, CL, NT == 32 ? 128 : NT, kAhead, 3> in;
-    in.rows((int64_t)(blockIdx.x / CL) * rows + (NT == 32 ? threadIdx.x >> 5 : 0),
-            (int64_t)(gridDim.x / CL) * rows, a.T, t, a.D, ring);
+    Feed<T, MODE, NT, 1, NT == 32 ? 128 : NT, kAhead, 3> in;
+    in.rows((int64_t)blockIdx.x * rows + (NT == 32 ? threadIdx.x >> 5 : 0),
+            (int64_t)gridDim.x * rows, a.T, t, a.D, ring);
     in.tensor(0, a.y, a.ld_y);
     in.tensor(1, a.r, a.ld_r);
     in.tensor(2, full ? a.gate : nullptr, a.D);
@@ -466,7 +472,7 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArg
         in.take(u, 1);
         if (full) in.take(g, 2);
         in.taken();
-        if (a.post) normalise<T, MODE, NT, CL, LAYER>(z, a.D, inv, a.eps, t, sum);
+        if (a.post) normalise<T, MODE, NT, 1, LAYER>(z, a.D, inv, a.eps, t, sum);
 #pragma unroll
         for (int e = 0; e < kP; ++e) z[e] = LAYER ? fma2(z[e], W[e], B[e]) : z[e] * W[e];
         if (full) {
@@ -485,7 +491,7 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT) block_norm_kernel(NormArg
             // gradient taken from the stored stream is that of this function.
 #pragma unroll
             for (int e = 0; e < kP; ++e) u[e] = as_stored(u[e], T());
-            normalise<T, MODE, NT, CL, LAYER>(u, a.D, inv, a.eps, t, sum);
+            normalise<T, MODE, NT, 1, LAYER>(u, a.D, inv, a.eps, t, sum);
 #pragma unroll
             for (int e = 0; e < kP; ++e) u[e] = LAYER ? fma2(u[e], wn[e], bn[e]) : u[e] * wn[e];
             in.put(n_row, u);
@@ -736,12 +742,14 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int
 
 constexpr int kMaxDim = 8192;
 
-// Threads of a row: 8 entries each, a power of two from a warp up.
+// Threads of a row: 8 entries each, in steps of a third to a half, so that few
+// idle, each a kernel of its own: with the number known at run time only, the
+// gradient at 16384 x 2048 took 97 us instead of 78.
 int row_threads(int D) {
     const int v = (D + 7) / 8;
-    int t = 32;
-    while (t < v) t *= 2;
-    return t;
+    for (const int t : {32, 64, 128, 192, 256, 384, 512, 768})
+        if (v <= t) return t;
+    return 1024;
 }
 
 // Dynamic shared memory and grid of a persistent kernel: as many blocks as
@@ -784,21 +792,26 @@ template <auto K> cudaError_t run_rows(const NormArgs &a, int64_t units, int thr
 }
 
 template <typename T, int MODE, bool LAYER> struct Forward {
-    template <int NT, int CL> static cudaError_t go(const NormArgs &a, int *groups, cudaStream_t st) {
+    template <int NT> static cudaError_t go(const NormArgs &a, int *groups, cudaStream_t st) {
         constexpr int threads = NT == 32 ? 128 : NT;
-        constexpr size_t smem = Feed<T, MODE, NT, CL, threads, kAhead, 3>::smem_bytes();
+        constexpr size_t smem = Feed<T, MODE, NT, 1, threads, kAhead, 3>::smem_bytes();
         const int64_t units = NT == 32 ? (a.T + 3) / 4 : a.T;
-        return run_rows<block_norm_kernel<T, MODE, NT, CL, LAYER>>(a, units, threads, CL, smem,
-                                                                  INT64_MAX, groups, st);
+        return run_rows<block_norm_kernel<T, MODE, NT, LAYER>>(a, units, threads, 1, smem,
+                                                              INT64_MAX, groups, st);
     }
+    // Past 4096 entries one wide block: a cluster of two of 512 threads pays its
+    // barrier up to four times a row (4096 x 8192 in bf16: 94 us against 57).
     static cudaError_t launch(const NormArgs &a, int *groups, cudaStream_t st) {
         switch (row_threads(a.D)) {
-        case 32: return go<32, 1>(a, groups, st);
-        case 64: return go<64, 1>(a, groups, st);
-        case 128: return go<128, 1>(a, groups, st);
-        case 256: return go<256, 1>(a, groups, st);
-        case 512: return go<512, 1>(a, groups, st);
-        default: return go<512, 2>(a, groups, st);
+        case 32: return go<32>(a, groups, st);
+        case 64: return go<64>(a, groups, st);
+        case 128: return go<128>(a, groups, st);
+        case 192: return go<192>(a, groups, st);
+        case 256: return go<256>(a, groups, st);
+        case 384: return go<384>(a, groups, st);
+        case 512: return go<512>(a, groups, st);
+        case 768: return go<768>(a, groups, st);
+        default: return go<1024>(a, groups, st);
         }
     }
 };
@@ -827,8 +840,11 @@ template <typename T, int MODE, bool LAYER> struct Backward {
         case 32: return go<32, 1>(a, groups, st);
         case 64: return go<64, 1>(a, groups, st);
         case 128: return go<128, 1>(a, groups, st);
+        case 192: return go<192, 1>(a, groups, st);
         case 256: return go<256, 1>(a, groups, st);
+        case 384: return go<384, 1>(a, groups, st);
         case 512: return go<512, 1>(a, groups, st);
+        case 768: return go<384, 2>(a, groups, st);
         default: return go<512, 2>(a, groups, st);
         }
     }

@@ -257,6 +257,20 @@ def test_backward_matches_64_bit_autograd(D, dtype, kind, gpu_lib):
         check_backward(T, D, dtype, kind, gate)
 
 
+# the first and last widths of each number of threads a row, odd and even
+EDGES = [255, 513, 1025, 1026, 1535, 1536, 1537, 1544, 2049, 3000, 3064, 3080, 4095, 4097, 4104,
+         6143, 6144, 6145, 6152, 8191]
+
+
+@pytest.mark.parametrize("D", EDGES)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_widths_around_the_threads_of_a_row(D, dtype, kind, gpu_lib):
+    for T, gate in ((4, "channel"), (3, "token"), (311, "full")):
+        check_forward(T, D, dtype, kind, gate)
+        check_backward(T, D, dtype, kind, gate)
+
+
 @pytest.mark.parametrize("T,D", [(2, 64), (900, 200), (700, 1024), (613, 2048)])
 def test_backward_sums_over_many_tokens(T, D, gpu_lib):
     for dtype, kind, gate in ((BF16, "rms", "channel"), (F32, "layer", "channel"),
