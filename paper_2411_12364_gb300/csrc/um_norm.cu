@@ -521,6 +521,9 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
     constexpr int TPR = NT * CL;
     extern __shared__ uint4 ring[];
     __shared__ __align__(16) float buf[2][kSumSlots];
+    // the peer's shared memory may be written only once the peer runs: arrive
+    // here and wait below, behind the first copies and the parameters' loads
+    if constexpr (CL > 1) tc::cluster_arrive_relaxed();
     RowSum<NT, CL> sum{buf, 0};
     const int t = threadIdx.x + (CL > 1 ? NT * (int)tc::cluster_ctarank() : 0);
     const bool full = a.gate_mode == ULTRAMEM_GATE_FULL;
@@ -542,6 +545,7 @@ __global__ void __launch_bounds__(NT, NT < 512 ? 512 / NT : 1)
 #pragma unroll
     for (int e = 0; e < kP; ++e) c_p[e] = c_pre[e] = c_q[e] = c_bpre[e] = f2(0.f);
     const F2 res = f2(a.res_scale);
+    if constexpr (CL > 1) tc::cluster_wait();   // before the first sum stores into the peer
 
     auto row_of = [&](void *base) { return static_cast<T *>(base) + in.first * a.D; };
     T *dr_row = a.dr ? row_of(a.dr) : nullptr, *dy_row = a.dy ? row_of(a.dy) : nullptr;
