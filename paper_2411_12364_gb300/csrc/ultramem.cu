@@ -9,6 +9,7 @@
 #include <atomic>
 #include <new>
 
+#include "um_device.cuh"
 #include "um_internal.cuh"
 
 using um::Dims;
@@ -1235,17 +1236,14 @@ cudaError_t launch_copy16(const void *src, void *dst, size_t bytes, cudaStream_t
 ultramem_status status_from_cuda(cudaError_t e) { return from_cuda(e); }
 
 int device_sm_count() {
-    static int n = 0;
-    if (!n) {
-        int dev = 0, v = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess ||
-            cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v < 1) {
-            cudaGetLastError();
-            v = 1;
-        }
-        n = v;
-    }
-    return n;
+    static PerDevice<int> sms;
+    int n = 0;
+    const cudaError_t e = sms.get(&n, [](int dev, int *v) {
+        return cudaDeviceGetAttribute(v, cudaDevAttrMultiProcessorCount, dev);
+    });
+    if (e == cudaSuccess && n > 0) return n;
+    cudaGetLastError();
+    return 1;
 }
 
 // The seeded shuffle's multiplier and offset, for entry points defined in

@@ -253,7 +253,7 @@ constexpr size_t kSmemPerSM = 233472;     // 228 KB per SM
 constexpr size_t kSmemPerCta = 232448;    // 227 KB at most per CTA
 constexpr size_t kSmemReserved = 1024;    // the driver's reservation per CTA
 
-int device_sm_count();
+int device_sm_count();   // of the current device
 
 // The status of a CUDA call for entry points defined outside ultramem.cu (the
 // error's text is kept for ultramem_last_error).

@@ -20,6 +20,7 @@
 // gate are read once per block, into registers.  Measured at 16384 x 2048 in
 // bf16 with a full gate: 57 us forward, 5.9 TB/s of what has to move; the
 // gradient with a channel gate 80 us, 5.0 TB/s.
+#include "um_device.cuh"
 #include "um_internal.cuh"
 #include "um_pair.cuh"
 #include "um_tc.cuh"
@@ -757,25 +758,23 @@ int row_threads(int D) {
 }
 
 // Dynamic shared memory and grid of a persistent kernel: as many blocks as
-// the SMs hold, asked of the driver once per kernel.
-template <auto K> int resident_blocks(int threads, size_t smem) {
-    static const int n = [&] {
-        int b = 0;
-        if (cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
-                cudaSuccess ||
-            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&b, K, threads, smem) != cudaSuccess) {
-            cudaGetLastError();
-            return 0;
-        }
-        return b;
-    }();
-    return n;
+// the SMs hold, asked of the driver once per kernel and device.
+template <auto K> cudaError_t resident_blocks(int threads, size_t smem, int *n) {
+    static PerDevice<int> blocks;
+    return blocks.get(n, [&](int, int *b) {
+        cudaError_t e =
+            cudaFuncSetAttribute(K, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e == cudaSuccess)
+            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(b, K, threads, smem);
+        return e == cudaSuccess && *b < 1 ? cudaErrorInvalidConfiguration : e;
+    });
 }
 
 template <auto K> cudaError_t run_rows(const NormArgs &a, int64_t units, int threads, int cl,
                                        size_t smem, int64_t most, int *groups, cudaStream_t st) {
-    const int fit = resident_blocks<K>(threads, smem);
-    if (fit < 1) return cudaErrorInvalidConfiguration;
+    int fit = 0;
+    const cudaError_t e = resident_blocks<K>(threads, smem, &fit);
+    if (e != cudaSuccess) return e;
     int64_t grid = (int64_t)device_sm_count() * fit / cl;   // clusters (or blocks)
     grid = grid < most ? grid : most;
     grid = grid < units ? grid : units;

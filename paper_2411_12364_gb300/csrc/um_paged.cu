@@ -2,6 +2,7 @@
 // (paged_plan), the new keys and values into their pages (paged_append), and
 // the attention kernel of the storages and head widths that the tensor-core
 // kernels do not take, with the kernels that join split tiles.
+#include "um_device.cuh"
 #include "um_paged.cuh"
 #include "um_pair.cuh"
 
@@ -770,9 +771,8 @@ template <typename T> cudaError_t combine(const AttnArgs &a, int ctas, int dp, i
 template <typename T, int ROWS, int ND> cudaError_t rows_go(const AttnArgs &a, int ctas,
                                                             cudaStream_t st) {
     constexpr size_t smem = RowsCfg<T, ROWS, ND>::kSmem;
-    static const cudaError_t set = cudaFuncSetAttribute(
-        rows_kernel<T, ROWS, ND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (set != cudaSuccess) return set;
+    const cudaError_t e = allow_dynamic_smem<rows_kernel<T, ROWS, ND>>(smem);
+    if (e != cudaSuccess) return e;
     rows_kernel<T, ROWS, ND><<<ctas, kThreads, smem, st>>>(a);
     return cudaGetLastError();
 }
@@ -870,18 +870,20 @@ bool encode(CUtensorMap *map, const void *base, uint64_t inner, uint64_t mid, ui
                             const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                             const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static const Fn fn = [] {
+    static std::atomic<Fn> known{nullptr};   // the driver's, the same for every device
+    Fn fn = known.load();
+    if (!fn) {
         cudaDriverEntryPointQueryResult q;
         void *f = nullptr;
         if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000,
                                              cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess) {
+            q != cudaDriverEntryPointSuccess || !f) {
             cudaGetLastError();
-            f = nullptr;
+            return false;
         }
-        return reinterpret_cast<Fn>(f);
-    }();
-    if (!fn) return false;
+        fn = reinterpret_cast<Fn>(f);
+        known.store(fn);
+    }
     const cuuint64_t dims[3] = {inner, mid, outer};
     const cuuint64_t strides[2] = {mid_stride * 2, outer_stride * 2};
     const cuuint32_t box[3] = {64, box_mid, box_outer}, step[3] = {1, 1, 1};
@@ -892,16 +894,21 @@ bool encode(CUtensorMap *map, const void *base, uint64_t inner, uint64_t mid, ui
 }
 
 // Set by a kernel whose bounded wait gave up; read and cleared by
-// ultramem_paged_check.
+// ultramem_paged_check.  Each device has its own.
 __device__ int g_error;
 
 int *error_word() {
-    static int *const p = [] {
+    static PerDevice<int *> word;
+    int *p = nullptr;
+    const cudaError_t e = word.get(&p, [](int, int **at) {
         void *a = nullptr;
-        if (cudaGetSymbolAddress(&a, g_error) != cudaSuccess) cudaGetLastError();
-        return static_cast<int *>(a);
-    }();
-    return p;
+        const cudaError_t found = cudaGetSymbolAddress(&a, g_error);
+        *at = static_cast<int *>(a);
+        return found;
+    });
+    if (e == cudaSuccess) return p;
+    cudaGetLastError();
+    return nullptr;
 }
 
 int shift_of(int32_t page_size) {

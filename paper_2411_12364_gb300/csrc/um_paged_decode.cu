@@ -16,6 +16,7 @@
 // Measured: 64 requests of up to 8192 keys (16 / 4 heads x 128, pages of 16)
 // 84 us without the join of split tiles, 6.3 TB/s; one request of 131072 keys
 // 46 us, 5.8 TB/s.
+#include "um_device.cuh"
 #include "um_paged.cuh"
 #include "um_tc.cuh"
 
@@ -381,9 +382,8 @@ __global__ void __launch_bounds__(kThreads, 2)
 
 template <int DP> cudaError_t go(const AttnArgs &a, const CUtensorMap &k, const CUtensorMap &v,
                                  int box_rows, int ctas, cudaStream_t st) {
-    static const cudaError_t set = cudaFuncSetAttribute(
-        decode_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<DP>::kSmem);
-    if (set != cudaSuccess) return set;
+    const cudaError_t e = allow_dynamic_smem<decode_kernel<DP>>(Cfg<DP>::kSmem);
+    if (e != cudaSuccess) return e;
     decode_kernel<DP><<<ctas, kThreads, Cfg<DP>::kSmem, st>>>(k, v, a, box_rows);
     return cudaGetLastError();
 }

@@ -29,6 +29,7 @@
 // products (one elected thread each), 9 the copies (TMA: K and V blocks, a box
 // per page, in a ring; Q per tile), 10 clears what a last page holds past the
 // request's length.
+#include "um_device.cuh"
 #include "um_paged.cuh"
 #include "um_pair.cuh"
 #include "um_tc.cuh"
@@ -583,9 +584,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 template <int DP>
 cudaError_t go(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v,
                int ctas, cudaStream_t st) {
-    static const cudaError_t set = cudaFuncSetAttribute(
-        prefill_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<DP>::kSmem);
-    if (set != cudaSuccess) return set;
+    const cudaError_t e = allow_dynamic_smem<prefill_kernel<DP>>(Cfg<DP>::kSmem);
+    if (e != cudaSuccess) return e;
     prefill_kernel<DP><<<ctas, kThreads, Cfg<DP>::kSmem, st>>>(
         q, k, v, a, prefill_box_rows(1 << a.page_shift));
     return cudaGetLastError();
