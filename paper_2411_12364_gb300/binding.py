@@ -215,10 +215,20 @@ def key_ln(keys: torch.Tensor, g: torch.Tensor, b: torch.Tensor | None = None,
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream():
+def _stream(device=None):
     if _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(torch.cuda.current_device() if device is None else device)
     return torch.cuda.current_stream().cuda_stream
+
+
+def _on_device(name: str, t: torch.Tensor) -> int:
+    """The current device's index, whose stream a call launches on; raises
+    unless ``t`` lies there."""
+    if t.is_cuda:
+        device = torch.cuda.current_device()
+        if t.get_device() == device:
+            return device
+    raise ValueError(f"{name} must be a CUDA tensor on the current device")
 
 
 _CFG_KEYS = ("d_in", "d_k", "heads", "rank", "n", "expand_e", "d_v", "d_out", "topk",

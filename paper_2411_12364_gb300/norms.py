@@ -4,7 +4,8 @@ ultramem_block_norm):
 
     z = N_post(y),  u = res_scale r + out_scale gate (.) z,  n = N_pre(u)
 
-As in binding.py, these functions marshal arguments only.
+As in binding.py, these functions marshal arguments only.  They launch on the
+current stream of the current device, where every tensor has to lie.
 """
 from __future__ import annotations
 
@@ -20,11 +21,11 @@ _KINDS = {"rms": 0, "layer": 1}
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = 0, 1, 2, 3
 
 
-def _rows(name, t, shape, dtype):
-    """A [T, D] CUDA tensor; its rows may be strided apart.  Returns it and
-    the distance of its rows."""
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor of y's shape {tuple(shape)} and type")
+def _rows(name, t, shape, dtype, dev):
+    """A [T, D] tensor; its rows may be strided apart.  Returns it and the
+    distance of its rows."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must be a tensor of y's shape {tuple(shape)}, type and device")
     s0, s1 = t.stride()
     d = shape[1]
     if s1 == 1 and s0 >= d:
@@ -34,9 +35,10 @@ def _rows(name, t, shape, dtype):
     return t.contiguous(), d
 
 
-def _vector(name, t, d):
-    if t.dtype != torch.float32 or t.numel() != d or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous fp32 CUDA tensor of {d} entries")
+def _vector(name, t, d, dev):
+    if t.dtype != torch.float32 or t.numel() != d or t.get_device() != dev or \
+            not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous fp32 tensor of {d} entries on y's device")
     return t.data_ptr()
 
 
@@ -47,12 +49,13 @@ def _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale
         raise ValueError("y must be a CUDA tensor [tokens, dim], fp32 or bf16")
     if kind_code is None:
         raise ValueError(f"kind must be one of {tuple(_KINDS)}")
-    y, ld_y = _rows("y", y, shape, dtype)
+    dev = _b._on_device("y", y)
+    y, ld_y = _rows("y", y, shape, dtype, dev)
     T, D = shape
     mode, gate_ptr = GATE_NONE, None
     if gate is not None:
-        if not gate.is_cuda or not gate.is_contiguous():
-            raise ValueError("gate must be a contiguous CUDA tensor")
+        if gate.get_device() != dev or not gate.is_contiguous():
+            raise ValueError("gate must be a contiguous tensor on y's device")
         gate_shape = gate.shape
         if gate_shape == (D,) and gate.dtype == torch.float32:
             mode = GATE_CHANNEL
@@ -65,23 +68,25 @@ def _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale
                              "type")
         gate_ptr = gate.data_ptr()
     a = _b.BlockNormArgs(
-        y.data_ptr(), gate_ptr, None if w_post is None else _vector("w_post", w_post, D),
-        None if b_post is None else _vector("b_post", b_post, D),
-        None if w_pre is None else _vector("w_pre", w_pre, D),
-        None if b_pre is None else _vector("b_pre", b_pre, D), ld_y, 0, T, D, code, kind_code,
+        y.data_ptr(), gate_ptr, None if w_post is None else _vector("w_post", w_post, D, dev),
+        None if b_post is None else _vector("b_post", b_post, D, dev),
+        None if w_pre is None else _vector("w_pre", w_pre, D, dev),
+        None if b_pre is None else _vector("b_pre", b_pre, D, dev), ld_y, 0, T, D, code, kind_code,
         1 if post else 0, 1 if pre else 0, mode, res_scale, out_scale, eps)
-    return a, y
+    return a, y, dev
 
 
 @functools.lru_cache(maxsize=256)
-def _workspace(T, D):
-    """Bytes of the backward's workspace, a function of the sizes alone."""
+def _workspace(dev, T, D):
+    """Bytes of the backward's workspace, a function of the sizes and the
+    (current) device alone."""
     return int(_b.load().ultramem_block_norm_backward_workspace(T, D))
 
 
-def _given(name, t, y):
-    if t.shape != y.shape or t.dtype != y.dtype or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{name} must be contiguous, of y's shape and type")
+def _given(name, t, y, dev):
+    if t.shape != y.shape or t.dtype != y.dtype or not t.is_contiguous() or \
+            t.get_device() != dev:
+        raise ValueError(f"{name} must be contiguous, of y's shape, type and device")
     return t
 
 
@@ -92,17 +97,20 @@ def block_norm(y, residual, w_post=None, b_post=None, gate=None, w_pre=None, b_p
     (n is None without ``pre``).  gate: fp32 [D], or [T, 1] or [T, D] in y's
     type.  ``u`` and ``n`` may be given; u may be the residual itself and n
     may be y, updated in place."""
-    a, y = _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale, post, pre)
+    a, y, dev = _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale, post,
+                      pre)
     shape, dtype = y.shape, y.dtype
-    residual, a.ld_r = _rows("residual", residual, shape, dtype)
-    u = torch.empty(shape, dtype=dtype, device=y.device) if u is None else _given("u", u, y)
+    residual, a.ld_r = _rows("residual", residual, shape, dtype, dev)
+    u = torch.empty(shape, dtype=dtype, device=y.device) if u is None else _given("u", u, y, dev)
     if not pre:
         n = None
+    elif n is None:
+        n = torch.empty(shape, dtype=dtype, device=y.device)
     else:
-        n = torch.empty(shape, dtype=dtype, device=y.device) if n is None else _given("n", n, y)
+        n = _given("n", n, y, dev)
     lib = _b._lib or _b.load()
     status = lib.ultramem_block_norm(C.byref(a), residual.data_ptr(), u.data_ptr(),
-                                     None if n is None else n.data_ptr(), _b._stream())
+                                     None if n is None else n.data_ptr(), _b._stream(dev))
     if status:
         raise _b.UltraMemError(status, "ultramem_block_norm")
     return u, n
@@ -115,17 +123,18 @@ def block_norm_backward(y, u, du, dn=None, w_post=None, b_post=None, gate=None, 
     du of u (may be None) and dn of n (with ``pre``): a dict of dy, dr,
     dw_post, db_post, dw_pre, db_pre, dgate (None where the forward has no such
     input; gains and biases are fp32, and absent gains get no gradient)."""
-    a, y = _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale, post, pre)
+    a, y, dev = _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale, post,
+                      pre)
     shape, dtype, device = y.shape, y.dtype, y.device
     T, D = shape
-    u, a.ld_r = _rows("u", u, shape, dtype)
+    u, a.ld_r = _rows("u", u, shape, dtype, dev)
     du_ptr = dn_ptr = None
     ld_du = ld_dn = 0
     if du is not None:
-        du, ld_du = _rows("du", du, shape, dtype)
+        du, ld_du = _rows("du", du, shape, dtype, dev)
         du_ptr = du.data_ptr()
     if dn is not None:
-        dn, ld_dn = _rows("dn", dn, shape, dtype)
+        dn, ld_dn = _rows("dn", dn, shape, dtype, dev)
         dn_ptr = dn.data_ptr()
     lib = _b._lib or _b.load()
     dy = torch.empty(shape, dtype=dtype, device=device)
@@ -147,11 +156,11 @@ def block_norm_backward(y, u, du, dn=None, w_post=None, b_post=None, gate=None, 
     if gate is not None:
         dgate = torch.empty_like(gate)
         p_gate = dgate.data_ptr()
-    nbytes = _workspace(T, D)
+    nbytes = _workspace(dev, T, D)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     status = lib.ultramem_block_norm_backward(
         C.byref(a), u.data_ptr(), du_ptr, ld_du, dn_ptr, ld_dn, dy.data_ptr(), dr.data_ptr(),
-        p_gate, p_wpost, p_bpost, p_wpre, p_bpre, ws.data_ptr(), nbytes, _b._stream())
+        p_gate, p_wpost, p_bpost, p_wpre, p_bpre, ws.data_ptr(), nbytes, _b._stream(dev))
     if status:
         raise _b.UltraMemError(status, "ultramem_block_norm_backward")
     return {"dy": dy, "dr": dr, "dw_post": dw_post, "db_post": db_post, "dw_pre": dw_pre,

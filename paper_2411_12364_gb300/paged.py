@@ -12,7 +12,8 @@ list are int32 device tensors; no call waits for the GPU.  One step:
     out = paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new)
 
 As in binding.py, these functions marshal arguments only; there is no
-fallback, and an argument that the library cannot take raises.
+fallback, and an argument that the library cannot take raises.  They launch on
+the current stream of the current device, where every tensor has to lie.
 """
 from __future__ import annotations
 
@@ -27,9 +28,9 @@ from . import binding as _b
 _DTYPES = {torch.float32: _b.F32, torch.bfloat16: _b.BF16}
 
 
-def _int32(name, t):
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor")
+def _int32(name, t, dev):
+    if t.dtype != torch.int32 or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor on the current device")
     return t.data_ptr()
 
 
@@ -39,21 +40,22 @@ def _cache(k_cache, v_cache):
         raise ValueError("k_cache and v_cache must be [n_pages, kv_heads, page_size, head_dim] "
                          "of one type")
     code = _DTYPES.get(dtype)
-    if code is None or not (k_cache.is_cuda and v_cache.is_cuda):
-        raise ValueError("the cache must be fp32 or bf16 CUDA tensors")
+    dev = _b._on_device("k_cache", k_cache)
+    if code is None or v_cache.get_device() != dev:
+        raise ValueError("the cache must be fp32 or bf16 CUDA tensors on the current device")
     if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
         raise ValueError("the cache must be contiguous")
-    return _b.KVCache(k_cache.data_ptr(), v_cache.data_ptr(), *shape, code), shape, dtype
+    return _b.KVCache(k_cache.data_ptr(), v_cache.data_ptr(), *shape, code), shape, dtype, dev
 
 
-def _rows(name, t, heads, dim, dtype):
+def _rows(name, t, heads, dim, dtype, dev):
     """A [tokens, heads, dim] tensor whose tokens may be strided apart, and
     their distance."""
     shape = t.shape
     if len(shape) != 3 or shape[2] != dim or (heads and shape[1] != heads) or \
-            t.dtype != dtype or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor [tokens, {heads or 'heads'}, {dim}] "
-                         f"of the cache's type")
+            t.dtype != dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must be a tensor [tokens, {heads or 'heads'}, {dim}] of the "
+                         f"cache's type and device")
     s0, s1, s2 = t.stride()
     row = shape[1] * dim
     if s2 == 1 and s1 == dim and s0 >= row:
@@ -80,9 +82,10 @@ def paged_plan(ctx_lens, new_lens, block_table, free_pages, free_count, page_siz
                          "free_count one element")
     if n_tokens < 0:
         raise ValueError("n_tokens must not be negative")
+    dev = _b._on_device("ctx_lens", ctx_lens)
     free_ptr = None
     if free_left is not None:
-        free_ptr = _int32("free_left", free_left)
+        free_ptr = _int32("free_left", free_left, dev)
         if free_left.numel() != 1:
             raise ValueError("free_left must have one element")
     device = ctx_lens.device
@@ -92,10 +95,11 @@ def paged_plan(ctx_lens, new_lens, block_table, free_pages, free_count, page_siz
     balance = torch.empty(1, dtype=torch.int32, device=device)
     lib = _b._lib or _b.load()
     status = lib.ultramem_paged_plan(
-        _int32("ctx_lens", ctx_lens), _int32("new_lens", new_lens), R, page_size,
-        _int32("block_table", block_table), table_shape[1], _int32("free_pages", free_pages),
-        _int32("free_count", free_count), free_pages.numel(), n_tokens, q_start.data_ptr(),
-        kv_lens.data_ptr(), slots.data_ptr(), free_ptr, balance.data_ptr(), _b._stream())
+        _int32("ctx_lens", ctx_lens, dev), _int32("new_lens", new_lens, dev), R, page_size,
+        _int32("block_table", block_table, dev), table_shape[1],
+        _int32("free_pages", free_pages, dev), _int32("free_count", free_count, dev),
+        free_pages.numel(), n_tokens, q_start.data_ptr(),
+        kv_lens.data_ptr(), slots.data_ptr(), free_ptr, balance.data_ptr(), _b._stream(dev))
     if status:
         raise _b.UltraMemError(status, "ultramem_paged_plan")
     return q_start, kv_lens, slots, balance
@@ -104,23 +108,24 @@ def paged_plan(ctx_lens, new_lens, block_table, free_pages, free_count, page_siz
 def paged_append(k_cache, v_cache, k, v, slots):
     """Writes k, v [tokens, kv_heads, head_dim] (tokens may be strided, as
     slices of one projection's output) into their slots [tokens]."""
-    c, shape, dtype = _cache(k_cache, v_cache)
+    c, shape, dtype, dev = _cache(k_cache, v_cache)
     heads, dim = shape[1], shape[3]
-    k, ks = _rows("k", k, heads, dim, dtype)
-    v, vs = _rows("v", v, heads, dim, dtype)
+    k, ks = _rows("k", k, heads, dim, dtype, dev)
+    v, vs = _rows("v", v, heads, dim, dtype, dev)
     T = k.shape[0]
     if v.shape[0] != T or slots.numel() != T:
         raise ValueError("k, v and slots must have a row for each token")
     lib = _b._lib or _b.load()
     status = lib.ultramem_paged_append(C.byref(c), k.data_ptr(), ks, v.data_ptr(), vs,
-                                       _int32("slots", slots), T, _b._stream())
+                                       _int32("slots", slots, dev), T, _b._stream(dev))
     if status:
         raise _b.UltraMemError(status, "ultramem_paged_append")
 
 
 @functools.lru_cache(maxsize=256)
-def _workspace(dtype, q_heads, kv_heads, head_dim, max_new):
-    """Bytes of the attention's workspace, a function of the sizes alone."""
+def _workspace(dev, dtype, q_heads, kv_heads, head_dim, max_new):
+    """Bytes of the attention's workspace, a function of the sizes and the
+    (current) device alone."""
     return int(_b.load().ultramem_paged_attention_workspace(dtype, q_heads, kv_heads, head_dim,
                                                             max_new))
 
@@ -133,9 +138,9 @@ def paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new:
     the most new tokens a request has (a host number); scale: default
     1 / sqrt(head_dim).  Rows that belong to no request (past q_start[R]) are
     not written."""
-    c, shape, dtype = _cache(k_cache, v_cache)
+    c, shape, dtype, dev = _cache(k_cache, v_cache)
     heads, dim = shape[1], shape[3]
-    q, qs = _rows("q", q, 0, dim, dtype)
+    q, qs = _rows("q", q, 0, dim, dtype, dev)
     q_shape, device = q.shape, q.device
     T, H, _ = q_shape
     R = kv_lens.numel()
@@ -146,17 +151,18 @@ def paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new:
     if out is None:
         out = torch.empty(q_shape, dtype=dtype, device=device)
     elif out.shape != q_shape or out.dtype != dtype or not out.is_contiguous() or \
-            not out.is_cuda:
-        raise ValueError("out must be a contiguous CUDA tensor of q's shape and type")
+            out.get_device() != dev:
+        raise ValueError("out must be a contiguous tensor of q's shape, type and device")
     lse = torch.empty((T, H), dtype=torch.float32, device=device) if with_lse else None
     lib = _b._lib or _b.load()
-    nbytes = _workspace(c.dtype, H, heads, dim, max_new)
+    nbytes = _workspace(dev, c.dtype, H, heads, dim, max_new)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     status = lib.ultramem_paged_attention(
-        C.byref(c), q.data_ptr(), qs, H, _int32("q_start", q_start), _int32("kv_lens", kv_lens),
-        _int32("block_table", block_table), table_shape[1], R, T, max_new,
+        C.byref(c), q.data_ptr(), qs, H, _int32("q_start", q_start, dev),
+        _int32("kv_lens", kv_lens, dev), _int32("block_table", block_table, dev), table_shape[1], R,
+        T, max_new,
         1.0 / math.sqrt(dim) if scale is None else scale, out.data_ptr(),
-        None if lse is None else lse.data_ptr(), ws.data_ptr(), nbytes, _b._stream())
+        None if lse is None else lse.data_ptr(), ws.data_ptr(), nbytes, _b._stream(dev))
     if status:
         raise _b.UltraMemError(status, "ultramem_paged_attention")
     return (out, lse) if with_lse else out
