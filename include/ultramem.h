@@ -470,18 +470,23 @@ typedef struct ultramem_block_norm_args {
 } ultramem_block_norm_args;
 
 /* u [n_tokens][dim] and, with pre, n [n_tokens][dim] (else NULL), contiguous.
- * u may be r itself (contiguous), and n may be y. */
+ * Each may be y, r or a full gate itself, where that is contiguous (u = r and
+ * n = y update in place).  They must not overlap each other, nor an input in
+ * any other way (ULTRAMEM_EINVAL). */
 ultramem_status ultramem_block_norm(const ultramem_block_norm_args *args, const void *r, void *u,
                                     void *n, void *stream);
 
 /* The gradient at the y and u of a forward (u as it was stored; args->ld_r is
  * its row distance).  du, dn: gradients of u (NULL: zero; rows ld_du apart)
  * and n (with pre; rows ld_dn apart).  Outputs, each NULL to skip:
- *   dy, dr [n_tokens][dim] dtype, contiguous; dy may be du or dn, and dr may
- *           be the other, when those are contiguous;
+ *   dy, dr [n_tokens][dim] dtype, contiguous;
  *   dgate   fp32 [dim] for a channel gate, dtype [n_tokens] for a token gate,
  *           dtype [n_tokens][dim] for a full one;
  *   dw_post, db_post, dw_pre, db_pre  fp32 [dim] (written, not accumulated).
+ * dy, dr and a full dgate may be y, u, du, dn or a full gate itself, where that
+ * is contiguous; dgate and the sums may be the gate and the vectors that they
+ * are the gradients of.  Outputs must not overlap one another, nor an input in
+ * any other way, and the workspace nothing (ULTRAMEM_EINVAL).
  * The sums over tokens are added in a fixed order.  workspace: 16-byte
  * aligned, at least ultramem_block_norm_backward_workspace bytes.  Both calls
  * want each pointer on its entries' boundary (ULTRAMEM_EINVAL otherwise). */

@@ -22,6 +22,7 @@
 // gradient with a channel gate 80 us, 5.0 TB/s.
 #include "um_device.cuh"
 #include "um_internal.cuh"
+#include "um_overlap.cuh"
 #include "um_pair.cuh"
 #include "um_tc.cuh"
 
@@ -735,12 +736,12 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int
         if (o.db_pre) o.db_pre[c] = q;
         return;
     }
+    // all read before the first write: a gradient may take its vector's place
     const float g = o.out_scale * (o.gate ? o.gate[c] : 1.f);
+    const float wp = o.w_post ? o.w_post[c] : 1.f, bp = o.b_post ? o.b_post[c] : 0.f;
     if (o.dw_post) o.dw_post[c] = g * v;
     if (o.db_post) o.db_post[c] = g * q;
-    if (o.dgate)
-        o.dgate[c] = o.out_scale *
-                     fmaf(o.w_post ? o.w_post[c] : 1.f, v, (o.b_post ? o.b_post[c] : 0.f) * q);
+    if (o.dgate) o.dgate[c] = o.out_scale * fmaf(wp, v, bp * q);
 }
 
 // ---- launches ----------------------------------------------------------
@@ -937,6 +938,79 @@ bool params_on_boundary(const ultramem_block_norm_args *p, const void *dgate) {
            on_boundary(channel || p->dtype == ULTRAMEM_F32 ? 4 : 2, {p->gate, dgate});
 }
 
+// A row tensor, and the call's vectors and gate.
+Memory rows_of(const ultramem_block_norm_args *p, const void *at, int64_t ld) {
+    const int64_t es = p->dtype == ULTRAMEM_BF16 ? 2 : 4;
+    return {at, p->dim * es, p->n_tokens, ld * es};
+}
+Memory vector_of(const ultramem_block_norm_args *p, const void *at) {
+    return {at, p->dim * (int64_t)sizeof(float)};
+}
+// the gate, or its gradient
+Memory gate_of(const ultramem_block_norm_args *p, const void *at) {
+    if (p->gate_mode == ULTRAMEM_GATE_FULL) return rows_of(p, at, p->dim);
+    if (p->gate_mode == ULTRAMEM_GATE_CHANNEL) return vector_of(p, at);
+    return {at, (int64_t)p->n_tokens * (p->dtype == ULTRAMEM_BF16 ? 2 : 4)};
+}
+
+// A row of an output is written after that row of every input was read and
+// while other rows are not: an output may be a row tensor itself.  Anything
+// else that outputs share, with one another or with an input, goes wrong.
+bool forward_apart(const ultramem_block_norm_args *p, const void *r, const void *u,
+                   const void *n) {
+    const Memory out[2] = {rows_of(p, u, p->dim), rows_of(p, n, p->dim)};
+    if (overlap(out[0], out[1])) return false;
+    for (const Memory &o : out) {
+        if (!same_or_apart(o, rows_of(p, p->y, p->ld_y)) ||
+            !same_or_apart(o, rows_of(p, r, p->ld_r)))
+            return false;
+        const Memory gate = gate_of(p, p->gate);
+        if (p->gate_mode == ULTRAMEM_GATE_FULL ? !same_or_apart(o, gate) : overlap(o, gate))
+            return false;
+        for (const void *v : {p->w_post, p->b_post, p->w_pre, p->b_pre})
+            if (overlap(o, vector_of(p, v))) return false;
+    }
+    return true;
+}
+
+// The same of the gradient.  A sum over the tokens and a gate's gradient may
+// also take the place of the vector or gate that it is the gradient of; the
+// partial sums' workspace shares nothing.
+bool backward_apart(const ultramem_block_norm_args *p, const void *u, const void *du,
+                    int64_t ld_du, const void *dn, int64_t ld_dn, const void *dy, const void *dr,
+                    const void *dgate, const float *dw_post, const float *db_post,
+                    const float *dw_pre, const float *db_pre, const void *workspace,
+                    int64_t workspace_bytes) {
+    enum { kDy, kDr, kDgate, kDwPost, kDbPost, kDwPre, kDbPre, kWorkspace, kOut };
+    const Memory out[kOut] = {rows_of(p, dy, p->dim), rows_of(p, dr, p->dim), gate_of(p, dgate),
+                              vector_of(p, dw_post),  vector_of(p, db_post),
+                              vector_of(p, dw_pre),   vector_of(p, db_pre),
+                              {workspace, workspace_bytes}};
+    for (int i = 0; i < kOut; ++i)
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i], out[j])) return false;
+    const bool full = p->gate_mode == ULTRAMEM_GATE_FULL;
+    const Memory rows[4] = {rows_of(p, p->y, p->ld_y), rows_of(p, p->pre ? u : nullptr, p->ld_r),
+                            rows_of(p, du, ld_du), rows_of(p, dn, ld_dn)};
+    // what an output may be itself: -1 the row tensors, else the one of that gradient
+    const struct {
+        Memory in;
+        int own;
+    } others[5] = {{gate_of(p, p->gate), full ? -1 : kDgate},  {vector_of(p, p->w_post), kDwPost},
+                   {vector_of(p, p->b_post), kDbPost},         {vector_of(p, p->w_pre), kDwPre},
+                   {vector_of(p, p->b_pre), kDbPre}};
+    for (int i = 0; i < kOut; ++i) {
+        const bool is_rows = i == kDy || i == kDr || (full && i == kDgate);
+        for (const Memory &in : rows)
+            if (is_rows ? !same_or_apart(out[i], in) : overlap(out[i], in)) return false;
+        for (const auto &o : others) {
+            const bool itself = o.own == i || (o.own == -1 && is_rows);
+            if (itself ? !same_or_apart(out[i], o.in) : overlap(out[i], o.in)) return false;
+        }
+    }
+    return true;
+}
+
 }  // namespace
 }  // namespace um
 
@@ -948,7 +1022,8 @@ extern "C" ultramem_status ultramem_block_norm(const ultramem_block_norm_args *p
         p->ld_r < p->dim)
         return ULTRAMEM_EINVAL;
     const int es = p->dtype == ULTRAMEM_BF16 ? 2 : 4;
-    if (!um::on_boundary(es, {p->y, r, u, n}) || !um::params_on_boundary(p, nullptr))
+    if (!um::on_boundary(es, {p->y, r, u, n}) || !um::params_on_boundary(p, nullptr) ||
+        !um::forward_apart(p, r, u, n))
         return ULTRAMEM_EINVAL;
     um::NormArgs a = um::args_of(p);
     a.r = r;
@@ -1003,7 +1078,10 @@ extern "C" ultramem_status ultramem_block_norm_backward(
     const int es = p->dtype == ULTRAMEM_BF16 ? 2 : 4;
     if (!um::on_boundary(es, {p->y, p->pre ? u : nullptr, du, dn, dy, dr}) ||
         !um::on_boundary(4, {dw_post, db_post, dw_pre, db_pre}) ||
-        !um::params_on_boundary(p, dgate))
+        !um::params_on_boundary(p, dgate) ||
+        !um::backward_apart(p, u, du, ld_du, dn, ld_dn, dy, dr, dgate, dw_post, db_post, dw_pre,
+                            db_pre, workspace,
+                            ultramem_block_norm_backward_workspace(p->n_tokens, D)))
         return ULTRAMEM_EINVAL;
     um::NormArgs a = um::args_of(p);
     a.r = u;

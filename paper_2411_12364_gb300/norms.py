@@ -96,7 +96,8 @@ def block_norm(y, residual, w_post=None, b_post=None, gate=None, w_pre=None, b_p
     """(u, n) for a block's output y [T, D] and the residual stream before it
     (n is None without ``pre``).  gate: fp32 [D], or [T, 1] or [T, D] in y's
     type.  ``u`` and ``n`` may be given; u may be the residual itself and n
-    may be y, updated in place."""
+    may be y, updated in place (or the other way round), but they must not
+    overlap each other."""
     a, y, dev = _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale, post,
                       pre)
     shape, dtype = y.shape, y.dtype
