@@ -381,10 +381,10 @@ typedef struct ultramem_kv_cache {
  *           below zero the number of pages that the step was short of.
  * A request is refused, and its table row left alone, when its pages and
  * those that it and earlier requests need exceed the free list, its row is
- * too narrow, or its tokens reach past n_tokens.  Outputs must not overlap
- * inputs (except the table, updated in place).  Repeating the call with the
- * same inputs gives the same result.  ULTRAMEM_EINVAL for a page size that a
- * cache cannot have, negative sizes or null pointers. */
+ * too narrow, or its tokens reach past n_tokens.  Outputs and the table must
+ * not overlap one another or an input.  Repeating the call with the same
+ * inputs gives the same result.  ULTRAMEM_EINVAL for a page size that a cache
+ * cannot have, negative sizes, null pointers or an overlap. */
 ultramem_status ultramem_paged_plan(const int32_t *ctx_lens, const int32_t *new_lens,
                                     int32_t n_seqs, int32_t page_size, int32_t *block_table,
                                     int32_t table_width, const int32_t *free_pages,
@@ -394,7 +394,8 @@ ultramem_status ultramem_paged_plan(const int32_t *ctx_lens, const int32_t *new_
 
 /* The new tokens' keys and values k, v [n_tokens][kv_heads][head_dim] (rows of
  * tokens k_stride and v_stride elements apart) into their slots.  Slots
- * outside the cache (-1) are skipped; two tokens must not share a slot. */
+ * outside the cache (-1) are skipped; two tokens must not share a slot, and k
+ * and v must not lie in slots that the call writes. */
 ultramem_status ultramem_paged_append(const ultramem_kv_cache *cache, const void *k,
                                       int64_t k_stride, const void *v, int64_t v_stride,
                                       const int32_t *slots, int32_t n_tokens, void *stream);
@@ -420,6 +421,9 @@ ultramem_status ultramem_paged_append(const ultramem_kv_cache *cache, const void
  * request has rows, and nothing is launched).  Rows of out that
  * belong to no request are not written.  workspace: 16-byte aligned, at least
  * ultramem_paged_attention_workspace bytes, not shared by calls that overlap.
+ * out may be q itself where q is contiguous; otherwise out, lse and workspace
+ * must not overlap one another, q, the lengths or the table (ULTRAMEM_EINVAL),
+ * nor the pages that the call reads.
  * ULTRAMEM_EINVAL for invalid sizes, types or null pointers and a scale that
  * is not positive and finite. */
 ultramem_status ultramem_paged_attention(const ultramem_kv_cache *cache, const void *q,

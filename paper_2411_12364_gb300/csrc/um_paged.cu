@@ -2,7 +2,10 @@
 // (paged_plan), the new keys and values into their pages (paged_append), and
 // the attention kernel of the storages and head widths that the tensor-core
 // kernels do not take, with the kernels that join split tiles.
+#include <initializer_list>
+
 #include "um_device.cuh"
+#include "um_overlap.cuh"
 #include "um_paged.cuh"
 #include "um_pair.cuh"
 
@@ -935,6 +938,19 @@ bool heads_ok(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim, int
            dim <= kMaxHeadDim && dim % 8 == 0 && max_new >= 0;
 }
 
+// Whether a call's outputs (contiguous) share no memory with one another or
+// with its inputs.
+bool apart(std::initializer_list<Memory> outputs, std::initializer_list<Memory> inputs) {
+    for (const Memory *o = outputs.begin(); o != outputs.end(); ++o) {
+        for (const Memory *p = outputs.begin(); p != o; ++p)
+            if (overlap(*o, *p)) return false;
+        for (const Memory &in : inputs)
+            if (overlap(*o, in)) return false;
+    }
+    return true;
+}
+Memory ints(const int32_t *p, int64_t n) { return {p, n * (int64_t)sizeof(int32_t)}; }
+
 }  // namespace
 
 cudaError_t launch_combine(const AttnArgs &a, int ctas, int dp, int dtype, int max_new, bool pdl,
@@ -958,13 +974,17 @@ extern "C" ultramem_status ultramem_paged_plan(const int32_t *ctx_lens, const in
                                                int32_t *free_left, int32_t *balance,
                                                void *stream) {
     if (n_seqs < 0 || n_tokens < 0 || table_width < 0 || n_free < 0 ||
-        !page_size_ok(page_size) || !free_count || !q_start || !balance ||
-        free_left == free_count || balance == free_count || balance == free_left)
+        !page_size_ok(page_size) || !free_count || !q_start || !balance)
         return ULTRAMEM_EINVAL;
-    if (n_seqs > 0 && (!ctx_lens || !new_lens || !kv_lens || kv_lens == ctx_lens ||
-                       kv_lens == new_lens || (table_width > 0 && !block_table)))
+    if (n_seqs > 0 && (!ctx_lens || !new_lens || !kv_lens || (table_width > 0 && !block_table)))
         return ULTRAMEM_EINVAL;
     if ((n_tokens > 0 && !slots) || (n_free > 0 && !free_pages)) return ULTRAMEM_EINVAL;
+    if (!apart({ints(q_start, (int64_t)n_seqs + 1), ints(kv_lens, n_seqs), ints(slots, n_tokens),
+                ints(free_left, 1), ints(balance, 1),
+                ints(block_table, (int64_t)n_seqs * table_width)},
+               {ints(ctx_lens, n_seqs), ints(new_lens, n_seqs), ints(free_pages, n_free),
+                ints(free_count, 1)}))
+        return ULTRAMEM_EINVAL;
     PlanArgs a = {ctx_lens, new_lens,  free_pages, free_count, block_table,
                   q_start,  kv_lens,   slots,      free_left,  balance,
                   n_seqs,   n_tokens,  shift_of(page_size),    table_width, n_free};
@@ -1051,8 +1071,19 @@ extern "C" ultramem_status ultramem_paged_attention(
         (uintptr_t)q % es || (uintptr_t)out % es || (table_width > 0 && !block_table) ||
         !workspace || ((uintptr_t)workspace & 15))
         return ULTRAMEM_EINVAL;
-    if (workspace_bytes < ultramem_paged_attention_workspace(c->dtype, q_heads, c->kv_heads,
-                                                             c->head_dim, max_new))
+    const int64_t need = ultramem_paged_attention_workspace(c->dtype, q_heads, c->kv_heads,
+                                                            c->head_dim, max_new);
+    if (workspace_bytes < need) return ULTRAMEM_EINVAL;
+    // a token's head is written after its query was read: out may be q itself
+    const int64_t row = (int64_t)q_heads * c->head_dim * es;
+    const um::Memory mem_q = {q, row, n_tokens, q_stride * es}, mem_out = {out, row * n_tokens},
+                     mem_lse = ints(reinterpret_cast<int32_t *>(lse), (int64_t)n_tokens * q_heads),
+                     mem_ws = {workspace, need};
+    if (!um::same_or_apart(mem_out, mem_q) || um::overlap(mem_lse, mem_q) ||
+        um::overlap(mem_ws, mem_q) ||
+        !apart({mem_out, mem_lse, mem_ws},
+               {ints(q_start, (int64_t)n_seqs + 1), ints(kv_lens, n_seqs),
+                ints(block_table, (int64_t)n_seqs * table_width)}))
         return ULTRAMEM_EINVAL;
     const int group = q_heads / c->kv_heads;
     // 4-byte fragments of q and out suffice for the decode kernel; TMA wants

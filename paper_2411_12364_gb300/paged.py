@@ -137,7 +137,7 @@ def paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new:
     the rows' log-sum-exp [tokens, q_heads] fp32 when ``with_lse``.  max_new:
     the most new tokens a request has (a host number); scale: default
     1 / sqrt(head_dim).  Rows that belong to no request (past q_start[R]) are
-    not written."""
+    not written.  ``out`` may be a contiguous q itself."""
     c, shape, dtype, dev = _cache(k_cache, v_cache)
     heads, dim = shape[1], shape[3]
     q, qs = _rows("q", q, 0, dim, dtype, dev)
