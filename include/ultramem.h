@@ -409,8 +409,8 @@ ultramem_status ultramem_paged_append(const ultramem_kv_cache *cache, const void
  * reads key/value head h / (q_heads / kv_heads) (q_heads a multiple of
  * kv_heads, at most 64 to one); out [n_tokens][q_heads][head_dim] contiguous;
  * lse fp32 [n_tokens][q_heads] or NULL.  A row that sees no key gets out = 0
- * and lse = -inf.  kv_lens is capped at what the table's row can hold; a table
- * entry outside the cache reads as zeros.  Cache entries past a request's
+ * and lse = -inf.  kv_lens is capped at what the table's row can hold and at
+ * 2^31 - 1024; a table entry outside the cache reads as zeros.  Cache entries past a request's
  * length are never used, whatever they hold.  Keys and values that only
  * later rows of the same request see may meet a row with weight 0: a
  * non-finite value there may make the row NaN.  Scores, sums and outputs

@@ -221,6 +221,12 @@ def _stream(device=None):
     return torch.cuda.current_stream().cuda_stream
 
 
+def _fits_int32(*sizes: int):
+    """Raises for a size that the library's 32-bit arguments cannot hold."""
+    if max(sizes) > 0x7fffffff:
+        raise ValueError("sizes must be below 2^31")
+
+
 def _on_device(name: str, t: torch.Tensor) -> int:
     """The current device's index, whose stream a call launches on; raises
     unless ``t`` lies there."""

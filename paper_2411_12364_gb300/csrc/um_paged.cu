@@ -53,8 +53,9 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) plan_kernel(Pl
     __shared__ int64_t need_at[THREADS], tok_at[THREADS + 1];   // before thread i's run
     __shared__ unsigned long long taken, asked;
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-    const int per = (a.n_seqs + THREADS - 1) / THREADS;
-    const int r0 = min(a.n_seqs, tid * per), r1 = min(a.n_seqs, r0 + per);
+    const int64_t per = ((int64_t)a.n_seqs + THREADS - 1) / THREADS;
+    const int r0 = (int)min((int64_t)a.n_seqs, tid * per);
+    const int r1 = (int)min((int64_t)a.n_seqs, r0 + per);
     const int free = max(0, min(*a.free_count, a.n_free));
     PlanRequest q;
     int64_t need = 0, tok = 0;
@@ -115,7 +116,8 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) plan_kernel(Pl
     }
 
     const int tokens = (int)min(total, (int64_t)a.n_tokens);
-    for (int i = blockIdx.x * THREADS + tid; i < a.n_tokens; i += gridDim.x * THREADS) {
+    for (int64_t i = (int64_t)blockIdx.x * THREADS + tid; i < a.n_tokens;
+         i += (int64_t)gridDim.x * THREADS) {
         if (i >= tokens) {   // past the batch's tokens
             a.slots[i] = -1;
             continue;
@@ -129,7 +131,7 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) plan_kernel(Pl
                 hi = m - 1;
         }
         int64_t upto = need_at[lo], at = tok_at[lo];
-        int r = lo * per;
+        int r = (int)(lo * per);
         for (;; ++r) {
             q.read(a, r);
             upto += q.need;

@@ -25,6 +25,9 @@ namespace paged {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxHeadDim = 256;
+// The most keys of a request: whole blocks, and the block after the last one
+// has numbers below 2^31 too (the table is read a block ahead).
+constexpr int kMaxKeys = INT32_MAX - 1023;
 
 struct AttnArgs {
     const void *q, *k, *v;
@@ -60,7 +63,8 @@ struct Request {
         if (end > a.n_tokens) end = a.n_tokens;
         n = end > tok0 ? end - tok0 : 0;
         kv = a.kv_lens[r];
-        const int64_t held = (int64_t)a.table_width << a.page_shift;
+        int64_t held = (int64_t)a.table_width << a.page_shift;
+        if (held > kMaxKeys) held = kMaxKeys;
         if (kv > held) kv = (int)held;
         if (kv < 0) kv = 0;
     }
@@ -98,8 +102,9 @@ template <int THREADS>
 __device__ __forceinline__ void place_share(const AttnArgs &a, int c, int ctas, int kb,
                                             int64_t min_share, int64_t *scratch, Cursor *cur) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-    const int per = (a.n_seqs + THREADS - 1) / THREADS;
-    const int r0 = min(a.n_seqs, tid * per), r1 = min(a.n_seqs, r0 + per);
+    const int64_t per = ((int64_t)a.n_seqs + THREADS - 1) / THREADS;
+    const int r0 = (int)min((int64_t)a.n_seqs, tid * per);
+    const int r1 = (int)min((int64_t)a.n_seqs, r0 + per);
     int64_t mine = 0;
     Request q;
     for (int r = r0; r < r1; ++r) {

@@ -50,6 +50,7 @@ def _args(y, gate, w_post, b_post, w_pre, b_pre, kind, eps, res_scale, out_scale
     if kind_code is None:
         raise ValueError(f"kind must be one of {tuple(_KINDS)}")
     dev = _b._on_device("y", y)
+    _b._fits_int32(*shape)
     y, ld_y = _rows("y", y, shape, dtype, dev)
     T, D = shape
     mode, gate_ptr = GATE_NONE, None

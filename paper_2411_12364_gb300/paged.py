@@ -82,6 +82,7 @@ def paged_plan(ctx_lens, new_lens, block_table, free_pages, free_count, page_siz
                          "free_count one element")
     if n_tokens < 0:
         raise ValueError("n_tokens must not be negative")
+    _b._fits_int32(n_tokens, R, table_shape[1], free_pages.numel(), page_size)
     dev = _b._on_device("ctx_lens", ctx_lens)
     free_ptr = None
     if free_left is not None:
@@ -115,6 +116,7 @@ def paged_append(k_cache, v_cache, k, v, slots):
     T = k.shape[0]
     if v.shape[0] != T or slots.numel() != T:
         raise ValueError("k, v and slots must have a row for each token")
+    _b._fits_int32(T)
     lib = _b._lib or _b.load()
     status = lib.ultramem_paged_append(C.byref(c), k.data_ptr(), ks, v.data_ptr(), vs,
                                        _int32("slots", slots, dev), T, _b._stream(dev))
@@ -148,6 +150,7 @@ def paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new:
     if q_start.numel() != R + 1 or len(table_shape) != 2 or table_shape[0] != R:
         raise ValueError("block_table and kv_lens must have a row for each request, q_start one "
                          "more")
+    _b._fits_int32(T, R, table_shape[1], max_new)
     if out is None:
         out = torch.empty(q_shape, dtype=dtype, device=device)
     elif out.shape != q_shape or out.dtype != dtype or not out.is_contiguous() or \
