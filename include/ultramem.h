@@ -344,10 +344,11 @@ ultramem_status ultramem_shard_pool(ultramem_layer *layer, const int64_t *idx, c
  * A decoder block puts the layer next to attention and norms.  The calls below
  * serve that: a paged cache of keys and values with the attention that reads
  * it, and the norms before and after a block fused with its gate and residual
- * scale, with their gradient.  They take no layer handle and keep nothing
- * between calls; scratch is a workspace that the caller passes.  All pointers
- * are DEVICE; every call is asynchronous on `stream`, never waits for the
- * GPU, and may be captured in a CUDA graph.
+ * scale, with their gradient.  They take no layer handle; scratch is a
+ * workspace that the caller passes, and nothing is kept between calls but one
+ * error word a device (ultramem_paged_check).  All pointers are DEVICE, of the
+ * current device; every call but the check is asynchronous on `stream`, never
+ * waits for the GPU, and may be captured in a CUDA graph.
  *
  * The cache holds pages of page_size tokens for all key/value heads.  A slot
  * is page * page_size + the token's place in the page; a request's block table
@@ -436,9 +437,12 @@ ultramem_status ultramem_paged_attention(const ultramem_kv_cache *cache, const v
 /* Bytes of workspace for such calls (0 for arguments that the call refuses). */
 int64_t ultramem_paged_attention_workspace(int32_t dtype, int32_t q_heads, int32_t kv_heads,
                                            int32_t head_dim, int32_t max_new);
-/* Synchronises `stream`, then reads and clears the attention kernels' error
- * word: ULTRAMEM_ETIMEOUT if a bounded wait gave up in a call since the last
- * check (its output is then meaningless; never expected). */
+/* Reads and clears the attention kernels' error word behind the work on
+ * `stream`, and waits for that: ULTRAMEM_ETIMEOUT if a bounded wait gave up
+ * since the last check (the output of that call is then meaningless; never
+ * expected).  The word is the current device's, whatever stream the call was
+ * on: of several threads that check, one gets the answer.  Reading and
+ * clearing is one step, so a timeout of another stream is not lost between. */
 ultramem_status ultramem_paged_check(void *stream);
 
 enum { ULTRAMEM_NORM_RMS = 0, ULTRAMEM_NORM_LAYER = 1 };
@@ -515,6 +519,10 @@ int64_t ultramem_block_norm_backward_workspace(int64_t n_tokens, int32_t dim);
  * is meaningless.  ultramem_check then returns ULTRAMEM_ETIMEOUT once; the
  * hook disarms itself after one forward.
  *
+ * ultramem_debug_paged_probe: a kernel on `stream` whose wait gives up in the
+ * same way and is recorded in the current device's word of
+ * ultramem_paged_check, which then returns ULTRAMEM_ETIMEOUT once.
+ *
  * ultramem_debug_fail_alloc: the nth device allocation (0-based, counted
  * from this call, over all layers of the process) that the library makes
  * fails as if the device were out of memory, without calling the allocator;
@@ -522,6 +530,7 @@ int64_t ultramem_block_norm_backward_workspace(int64_t n_tokens, int32_t dim);
  * device allocations the library holds (every live layer's workspace), so a
  * test can check that a failed create releases everything it took. */
 ultramem_status ultramem_debug_wait_probe(ultramem_layer *layer);
+ultramem_status ultramem_debug_paged_probe(void *stream);
 void ultramem_debug_fail_alloc(int32_t nth);
 int32_t ultramem_debug_live_allocations(void);
 

@@ -33,7 +33,8 @@ EXPORTS = ("ultramem_create", "ultramem_destroy", "ultramem_forward",
            "ultramem_shard_route", "ultramem_shard_lookup", "ultramem_shard_pool",
            "ultramem_paged_plan", "ultramem_paged_append", "ultramem_paged_attention",
            "ultramem_paged_attention_workspace", "ultramem_paged_check", "ultramem_block_norm",
-           "ultramem_block_norm_backward", "ultramem_block_norm_backward_workspace")
+           "ultramem_block_norm_backward", "ultramem_block_norm_backward_workspace",
+           "ultramem_debug_paged_probe")
 
 
 class Config(C.Structure):
@@ -156,6 +157,8 @@ def load(path: str | None = None) -> C.CDLL:
         lib.ultramem_paged_attention_workspace.restype = I64
         lib.ultramem_paged_check.argtypes = [P]
         lib.ultramem_paged_check.restype = I32
+        lib.ultramem_debug_paged_probe.argtypes = [P]
+        lib.ultramem_debug_paged_probe.restype = I32
         lib.ultramem_block_norm.argtypes = [P, P, P, P, P]
         lib.ultramem_block_norm.restype = I32
         lib.ultramem_block_norm_backward.argtypes = [P, P, P, I64, P, I64, P, P, P, P, P, P, P, P,

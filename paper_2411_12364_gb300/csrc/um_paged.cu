@@ -3,11 +3,13 @@
 // the attention kernel of the storages and head widths that the tensor-core
 // kernels do not take, with the kernels that join split tiles.
 #include <initializer_list>
+#include <mutex>
 
 #include "um_device.cuh"
 #include "um_overlap.cuh"
 #include "um_paged.cuh"
 #include "um_pair.cuh"
+#include "um_tc.cuh"
 
 namespace um {
 namespace paged {
@@ -901,19 +903,31 @@ bool encode(CUtensorMap *map, const void *base, uint64_t inner, uint64_t mid, ui
 // Set by a kernel whose bounded wait gave up; read and cleared by
 // ultramem_paged_check.  Each device has its own.
 __device__ int g_error;
+__device__ int g_taken;         // what the check at hand read; checks take turns
+std::mutex g_check;
 
-int *error_word() {
+template <int &SYMBOL> int *word_of() {
     static PerDevice<int *> word;
     int *p = nullptr;
     const cudaError_t e = word.get(&p, [](int, int **at) {
         void *a = nullptr;
-        const cudaError_t found = cudaGetSymbolAddress(&a, g_error);
+        const cudaError_t found = cudaGetSymbolAddress(&a, SYMBOL);
         *at = static_cast<int *>(a);
         return found;
     });
     if (e == cudaSuccess) return p;
     cudaGetLastError();
     return nullptr;
+}
+int *error_word() { return word_of<g_error>(); }
+
+// Reads and clears the word in one step: a timeout that a kernel of another
+// stream records meanwhile is in this answer or in the next one.
+__global__ void take_error_kernel(int *word, int *taken) { *taken = atomicExch(word, 0); }
+
+__global__ void probe_kernel(int *err) {
+    __shared__ uint64_t never;
+    tc::probe_timeout(&never, err, kErrTimeout);
 }
 
 int shift_of(int32_t page_size) {
@@ -1155,13 +1169,24 @@ extern "C" ultramem_status ultramem_paged_attention(
 }
 
 extern "C" ultramem_status ultramem_paged_check(void *stream) {
-    int *word = error_word();
-    if (!word) return ULTRAMEM_ENODEV;
+    int *word = error_word(), *taken = word_of<g_taken>();
+    if (!word || !taken) return ULTRAMEM_ENODEV;
     int err = 0;
     cudaStream_t st = (cudaStream_t)stream;
-    cudaError_t e = cudaMemcpyAsync(&err, word, sizeof err, cudaMemcpyDeviceToHost, st);
-    if (e == cudaSuccess) e = cudaMemsetAsync(word, 0, sizeof err, st);
+    cudaGetLastError();
+    const std::lock_guard<std::mutex> turn(g_check);
+    take_error_kernel<<<1, 1, 0, st>>>(word, taken);
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess) e = cudaMemcpyAsync(&err, taken, sizeof err, cudaMemcpyDeviceToHost, st);
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
     if (e != cudaSuccess) return um::status_from_cuda(e);
     return err & um::kErrTimeout ? ULTRAMEM_ETIMEOUT : ULTRAMEM_OK;
+}
+
+extern "C" ultramem_status ultramem_debug_paged_probe(void *stream) {
+    int *word = error_word();
+    if (!word) return ULTRAMEM_ENODEV;
+    cudaGetLastError();
+    probe_kernel<<<1, 32, 0, (cudaStream_t)stream>>>(word);
+    return um::status_from_cuda(cudaGetLastError());
 }

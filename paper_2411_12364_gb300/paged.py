@@ -172,5 +172,6 @@ def paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new:
 
 
 def paged_check() -> int:
-    """Syncs the current stream and returns the attention kernels' status."""
+    """Syncs the current stream and returns the attention kernels' status on
+    the current device since the last check, whatever stream they ran on."""
     return int(_b.load().ultramem_paged_check(_b._stream()))
