@@ -426,7 +426,7 @@ ultramem_status ultramem_paged_append(const ultramem_kv_cache *cache, const void
  * must not overlap one another, q, the lengths or the table (ULTRAMEM_EINVAL),
  * nor the pages that the call reads.
  * ULTRAMEM_EINVAL for invalid sizes, types or null pointers and a scale that
- * is not positive and finite. */
+ * is not positive or, times log2(e), not finite in fp32. */
 ultramem_status ultramem_paged_attention(const ultramem_kv_cache *cache, const void *q,
                                          int64_t q_stride, int32_t q_heads,
                                          const int32_t *q_start, const int32_t *kv_lens,

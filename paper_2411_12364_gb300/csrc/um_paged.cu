@@ -1079,7 +1079,7 @@ extern "C" ultramem_status ultramem_paged_attention(
     int32_t table_width, int32_t n_seqs, int32_t n_tokens, int32_t max_new, float scale, void *out,
     float *lse, void *workspace, int64_t workspace_bytes, void *stream) {
     if (!cache_ok(c) || !heads_ok(c->dtype, q_heads, c->kv_heads, c->head_dim, max_new) ||
-        n_seqs < 0 || n_tokens < 0 || table_width < 0 || !(scale > 0.f) || !(scale < INFINITY))
+        n_seqs < 0 || n_tokens < 0 || table_width < 0 || !(scale > 0.f) || !(scale * kLog2e < INFINITY))
         return ULTRAMEM_EINVAL;
     if (n_tokens == 0 || n_seqs == 0 || max_new == 0) return ULTRAMEM_OK;
     const int es = c->dtype == ULTRAMEM_BF16 ? 2 : 4;
