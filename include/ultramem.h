@@ -377,9 +377,12 @@ typedef struct ultramem_kv_cache {
  *   kv_lens [n_seqs]: ctx + new; 0 for a refused request, whose rows then
  *           attend to nothing;
  *   free_left [1]: the free list's length after the call (NULL to skip);
- *   balance [1]: free_count less the pages asked for up to the last request
- *           that was served: free_left when none was refused before it, and
- *           below zero the number of pages that the step was short of.
+ *   balance [1]: free_count less the pages that the requests up to the last
+ *           served one asked for, refused ones among them (one that needs no
+ *           page is served too).  It equals free_left when all of those were
+ *           granted their pages.  It does not tell whether requests were
+ *           refused (kv_lens and slots do), counts none after the last served
+ *           one, and is not the next call's free_count (free_left is).
  * A request is refused, and its table row left alone, when its pages and
  * those that it and earlier requests need exceed the free list, its row is
  * too narrow, or its tokens reach past n_tokens.  Outputs and the table must

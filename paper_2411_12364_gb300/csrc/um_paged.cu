@@ -860,7 +860,8 @@ Layout layout_of(Path path, int32_t dtype, int32_t group, int32_t dim, int32_t m
         l.extra = p.keys;
     }
     if (path != kPrefill) l.tq = l.rows / group;
-    // what the join kernels hold: two shares a thread, 100 bytes a share
+    // what the join kernels hold: join_row_kernel two shares a thread (512),
+    // join_rows_kernel 36 bytes of shared memory a share (17 KB)
     if (l.ctas > 480) l.ctas = 480;
     l.o = 0;
     l.ml = l.o + (int64_t)l.ctas * 2 * l.rows * l.dp * 4;

@@ -72,8 +72,9 @@ def paged_plan(ctx_lens, new_lens, block_table, free_pages, free_count, page_siz
     New pages come from the end of free_pages[:free_count], whose length
     after the call goes to free_left [1] (the next call's free_count, another
     tensor than this call's).  A request that does not fit is refused (slots
-    -1, kv_len 0); balance is free_count less the pages asked for up to the
-    last request served, so below zero what the step was short of."""
+    -1, kv_len 0).  balance is free_count less the pages that requests up to
+    the last served one asked for, refused ones among them: it is neither the
+    next free_count nor a count of what refused requests lack."""
     R = ctx_lens.numel()
     table_shape = block_table.shape
     if new_lens.numel() != R or len(table_shape) != 2 or table_shape[0] != R or \
