@@ -412,16 +412,16 @@ ultramem_status ultramem_paged_append(const ultramem_kv_cache *cache, const void
  * q [n_tokens][q_heads][head_dim] with tokens q_stride elements apart; head h
  * reads key/value head h / (q_heads / kv_heads) (q_heads a multiple of
  * kv_heads, at most 64 to one); out [n_tokens][q_heads][head_dim] contiguous;
- * lse fp32 [n_tokens][q_heads] or NULL.  A row that sees no key gets out = 0
- * and lse = -inf.  kv_lens is capped at what the table's row can hold and at
+ * lse fp32 [n_tokens][q_heads] or NULL.  A row that sees no key, or only keys
+ * whose scores are -inf, gets out = 0 and lse = -inf.  kv_lens is capped at what the table's row can hold and at
  * 2^31 - 1024; a table entry outside the cache reads as zeros.  Cache entries past a request's
  * length are never used, whatever they hold.  Keys and values that only
  * later rows of the same request see may meet a row with weight 0: a
  * non-finite value there may make the row NaN.  Scores, sums and outputs
  * accumulate in fp32; with bf16 storage the weights enter the second product
  * as bf16.
- * max_new: an upper bound of n_r known on the host; it chooses the kernel and
- * the workspace (a larger n_r is still computed right, but 0 says that no
+ * max_new: an upper bound of n_r known on the host; it chooses one kernel for
+ * all of the call's requests, and the workspace (a larger n_r is still computed right, but 0 says that no
  * request has rows, and nothing is launched).  Rows of out that
  * belong to no request are not written.  workspace: 16-byte aligned, at least
  * ultramem_paged_attention_workspace bytes, not shared by calls that overlap.

@@ -162,8 +162,11 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) plan_kernel(Pl
 // ---- append --------------------------------------------------------------
 // A scatter of whole rows: each thread moves one piece (16 bytes where the
 // rows are aligned to that, else one element) of a token's keys and the same
-// piece of its values.  Bound by memory: each byte is read and written once
-// (16384 tokens of 4 heads x 128 in bf16: 11 us, 6 TB/s; 64 tokens: a launch).
+// piece of its values.  Each byte is read and written once, 9.9 us of memory
+// traffic for 16384 tokens of 4 heads x 128 in bf16; calls in a row take 14.4
+// us, 4.7 TB/s.  What it waits for is latency: each thread has a 64-bit
+// division, then the slot's load, then one piece in flight (issue 60 % active,
+// the largest stall a load's).  64 tokens: a launch.
 template <typename W>
 __global__ void __launch_bounds__(256) append_kernel(const W *k, const W *v, int64_t k_stride,
                                                      int64_t v_stride, const int32_t *slots,
@@ -495,8 +498,8 @@ __global__ void __launch_bounds__(kThreads, RowsCfg<T, ROWS, ND>::kPerSm) rows_k
 // their partials many, so that a row's loads over the partials fill the
 // flight (29 and 64 tokens over 48 k and 65 k keys: 33 and 54 us with the
 // attention, four rows 77 and 76); four rows where most tiles have two or
-// three partials (4 prompts of 4096: 208 us, one row 215; 8 ragged chunks 273
-// and 281).
+// three partials (4 prompts of 4096, 213 us with the attention, and 8 ragged
+// chunks, 280: 7 and 8 us less than with one row).
 struct Span {
     int slot, n;                // place of the first partial, shares of the tile
     int tok0, n_rows, h;

@@ -23,7 +23,9 @@
 // Measured: 4 prompts of 4096 tokens (16 / 4 heads x 128) 197 us without the
 // join of split tiles, 1396 TFLOP/s of what the causal rows need, the tensor
 // pipe 64 % active; 8 ragged chunks over up to 31 k keys at width 64 264 us,
-// 985 TFLOP/s.
+// 985 TFLOP/s.  The softmax threads spill 22 of their registers (88 bytes a
+// thread; the compiler holds the kernel to the 168 of the launch, of which a
+// row's scores take 128); the other roles spill none.
 //
 // Warps: 0-3 and 4-7 the halves' softmax and output, 8 and 11 the halves'
 // products (one elected thread each), 9 the copies (TMA: K and V blocks, a box

@@ -5,7 +5,9 @@ ultramem_block_norm):
     z = N_post(y),  u = res_scale r + out_scale gate (.) z,  n = N_pre(u)
 
 As in binding.py, these functions marshal arguments only.  They launch on the
-current stream of the current device, where every tensor has to lie.
+current stream of the current device, where every tensor has to lie.  Autograd
+does not see them: their outputs require no gradient, whatever the inputs do;
+a training step calls block_norm_backward.
 """
 from __future__ import annotations
 

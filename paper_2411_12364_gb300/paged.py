@@ -13,7 +13,8 @@ list are int32 device tensors; no call waits for the GPU.  One step:
 
 As in binding.py, these functions marshal arguments only; there is no
 fallback, and an argument that the library cannot take raises.  They launch on
-the current stream of the current device, where every tensor has to lie.
+the current stream of the current device, where every tensor has to lie, and
+autograd does not see them.
 """
 from __future__ import annotations
 
@@ -138,7 +139,8 @@ def paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new:
     """Causal attention of q [tokens, q_heads, head_dim] (requests packed by
     q_start [R+1]) over the pages of block_table [R, width]: out like q, and
     the rows' log-sum-exp [tokens, q_heads] fp32 when ``with_lse``.  max_new:
-    the most new tokens a request has (a host number); scale: default
+    the most new tokens a request has (a host number, which chooses one kernel
+    for the whole call); scale: default
     1 / sqrt(head_dim).  Rows that belong to no request (past q_start[R]) are
     not written.  ``out`` may be a contiguous q itself."""
     c, shape, dtype, dev = _cache(k_cache, v_cache)
