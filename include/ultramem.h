@@ -509,6 +509,115 @@ ultramem_status ultramem_block_norm_backward(const ultramem_block_norm_args *arg
                                              int64_t workspace_bytes, void *stream);
 int64_t ultramem_block_norm_backward_workspace(int64_t n_tokens, int32_t dim);
 
+/* The gradient of the attention of whole sequences: requests whose rows are all
+ * new (nothing cached before them), as a training step has them.  At the q and
+ * out of such a ultramem_paged_attention call, its lse and the k, v that were
+ * appended, for the gradient dout of out:
+ *   P_ij = e^(scale q_i . k_j - lse_i) (j <= i),  d_i = dout_i . out_i
+ *   dS_ij = scale P_ij (dout_i . v_j - d_i)
+ *   dq_i = sum_j dS_ij k_j,  dk_j = sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i
+ * with the sums of dk and dv over all query heads of a key/value head.  A row
+ * whose lse is -inf takes no part: its dq is 0.  Sequence r holds the tokens
+ * q_start[r] .. q_start[r + 1] - 1 (q_start [n_seqs + 1] does not decrease; a
+ * sequence of no tokens is fine).  Rows that belong to no sequence are not
+ * written.  The probabilities are computed again, none are stored; sums are
+ * fp32 in a fixed order.  With bf16 storage P and dS enter the products as
+ * bf16.  All tensors are rows of tokens, `*_stride` elements apart, of
+ * heads x head_dim contiguous entries; lse fp32 [n_tokens][q_heads].
+ * Outputs must not overlap one another, nor an input, and the workspace
+ * (16-byte aligned, at least ..._workspace bytes) nothing (ULTRAMEM_EINVAL). */
+typedef struct ultramem_attention_grad {
+    const void *q, *out, *dout;   /* [n_tokens][q_heads][head_dim]                            */
+    const void *k, *v;            /* [n_tokens][kv_heads][head_dim]                           */
+    void *dq, *dk, *dv;           /* like q, k and v                                          */
+    const float *lse;             /* [n_tokens][q_heads]                                      */
+    const int32_t *q_start;       /* [n_seqs + 1]                                             */
+    int64_t q_stride, out_stride, dout_stride, k_stride, v_stride;
+    int64_t dq_stride, dk_stride, dv_stride;
+    int32_t n_tokens, n_seqs;
+    int32_t q_heads, kv_heads;    /* as in the attention: at most 64 to one                   */
+    int32_t head_dim;             /* a multiple of 8, up to 256                               */
+    int32_t dtype;                /* ULTRAMEM_F32 or ULTRAMEM_BF16                            */
+    float scale;                  /* positive and, times log2(e), finite in fp32              */
+} ultramem_attention_grad;
+ultramem_status ultramem_paged_attention_backward(const ultramem_attention_grad *args,
+                                                  void *workspace, int64_t workspace_bytes,
+                                                  void *stream);
+/* Bytes of workspace for such calls (0 for sizes that the call refuses). */
+int64_t ultramem_paged_attention_backward_workspace(int32_t dtype, int32_t n_tokens,
+                                                    int32_t n_seqs, int32_t q_heads,
+                                                    int32_t kv_heads, int32_t head_dim);
+
+/* ---- the two ends of a decoder on its vocabulary ----------------------------
+ * The embedding of token ids and the loss over the vocabulary, each with its
+ * gradient.  As above: no handle, scratch in a workspace that the caller
+ * passes, asynchronous on `stream`, capturable in a CUDA graph; the error word
+ * is the one of ultramem_paged_check.  Ids and labels are int32
+ * (ids_bytes 4) or int64 (ids_bytes 8); vocab is 1..2^30, dim 1..65536, and
+ * rows are `ld_*` elements apart. */
+
+/* out[t] = scale table[ids[t]], rounded once; a zero row for an id outside
+ * [0, vocab).  table [vocab][dim], out [n_tokens][dim] contiguous, which must
+ * not overlap the table or the ids (ULTRAMEM_EINVAL). */
+ultramem_status ultramem_embedding(const void *table, int64_t ld_table, int32_t dtype,
+                                   int32_t vocab, int32_t dim, const void *ids, int32_t ids_bytes,
+                                   int32_t n_tokens, float scale, void *out, void *stream);
+
+/* The gradient of the table: dtable[v] = scale sum of dout[t] over the tokens
+ * with ids[t] = v (0 without one; ids outside [0, vocab) count nowhere), or
+ * with `accumulate` that sum added to what dtable holds (rows without a token
+ * are left alone).  The sums are fp32, each in a fixed order, and rounded
+ * once.  dout [n_tokens][dim] of `dtype`; dtable [vocab][dim] contiguous, of
+ * `table_dtype`.  dtable and the workspace (16-byte aligned) overlap nothing
+ * (ULTRAMEM_EINVAL). */
+ultramem_status ultramem_embedding_backward(const void *ids, int32_t ids_bytes, int32_t n_tokens,
+                                            const void *dout, int64_t ld_dout, int32_t dtype,
+                                            int32_t vocab, int32_t dim, float scale, void *dtable,
+                                            int32_t table_dtype, int32_t accumulate,
+                                            void *workspace, int64_t workspace_bytes,
+                                            void *stream);
+int64_t ultramem_embedding_backward_workspace(int32_t n_tokens, int32_t dim);
+
+/* The softmax cross entropy of hidden states x [n_tokens][dim] against the
+ * output weights w [vocab][dim] (both `dtype`):
+ *   z_tv = logit_scale x_t . w_v,  lse_t = log sum_v e^(z_tv),
+ *   loss_t = lse_t - z_{t, label_t}
+ * A label outside [0, vocab) marks a token that does not count: its loss is 0
+ * and it takes no part in the gradient, whatever its x holds (its lse is
+ * computed all the same).  The logits are made tile by tile and not kept.
+ * Products of bf16 storage are exact and add in fp32; fp32 storage enters them
+ * as three bf16 terms a value (24 bits).  logit_scale is finite.  loss and lse
+ * fp32 [n_tokens]; they and the workspace (16-byte aligned) overlap nothing. */
+typedef struct ultramem_cross_entropy_args {
+    const void *x, *w;
+    const void *labels;           /* [n_tokens], int32 or int64                               */
+    int64_t ld_x, ld_w;
+    int32_t n_tokens, vocab, dim;
+    int32_t dtype;                /* ULTRAMEM_F32 or ULTRAMEM_BF16                            */
+    int32_t labels_bytes;         /* 4 or 8                                                   */
+    float logit_scale;
+} ultramem_cross_entropy_args;
+ultramem_status ultramem_cross_entropy(const ultramem_cross_entropy_args *args, float *loss,
+                                       float *lse, void *workspace, int64_t workspace_bytes,
+                                       void *stream);
+int64_t ultramem_cross_entropy_workspace(int32_t dtype, int32_t n_tokens, int32_t vocab,
+                                         int32_t dim);
+
+/* The gradient at the lse of that call, for the gradients dloss [n_tokens]
+ * (fp32) of the losses:
+ *   G_tv = logit_scale dloss_t (e^(z_tv - lse_t) - [v = label_t]),
+ *   dx = G w,  dw = G^T x
+ * The logits are computed again in pieces of the vocabulary; G enters the
+ * products in `dtype` (bf16 storage: rounded to bf16).  dx [n_tokens][dim] and
+ * dw [vocab][dim], contiguous, of `dtype`; each NULL to skip.  They and the
+ * workspace overlap nothing. */
+ultramem_status ultramem_cross_entropy_backward(const ultramem_cross_entropy_args *args,
+                                                const float *lse, const float *dloss, void *dx,
+                                                void *dw, void *workspace, int64_t workspace_bytes,
+                                                void *stream);
+int64_t ultramem_cross_entropy_backward_workspace(int32_t dtype, int32_t n_tokens, int32_t vocab,
+                                                  int32_t dim);
+
 /* Failure-path hooks for tests; they inject failures on the host or behind
  * a bounded wait, never a device fault.
  *

@@ -34,7 +34,11 @@ EXPORTS = ("ultramem_create", "ultramem_destroy", "ultramem_forward",
            "ultramem_paged_plan", "ultramem_paged_append", "ultramem_paged_attention",
            "ultramem_paged_attention_workspace", "ultramem_paged_check", "ultramem_block_norm",
            "ultramem_block_norm_backward", "ultramem_block_norm_backward_workspace",
-           "ultramem_debug_paged_probe")
+           "ultramem_debug_paged_probe", "ultramem_paged_attention_backward",
+           "ultramem_paged_attention_backward_workspace", "ultramem_embedding",
+           "ultramem_embedding_backward", "ultramem_embedding_backward_workspace",
+           "ultramem_cross_entropy", "ultramem_cross_entropy_workspace",
+           "ultramem_cross_entropy_backward", "ultramem_cross_entropy_backward_workspace")
 
 
 class Config(C.Structure):
@@ -64,6 +68,22 @@ class BlockNormArgs(C.Structure):
         [("ld_y", C.c_int64), ("ld_r", C.c_int64)] + [(name, C.c_int32) for name in (
             "n_tokens", "dim", "dtype", "kind", "post", "pre", "gate_mode")] + \
         [(name, C.c_float) for name in ("res_scale", "out_scale", "eps")]
+
+
+class AttentionGrad(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in (
+        "q", "out", "dout", "k", "v", "dq", "dk", "dv", "lse", "q_start")] + \
+        [(name, C.c_int64) for name in (
+            "q_stride", "out_stride", "dout_stride", "k_stride", "v_stride", "dq_stride",
+            "dk_stride", "dv_stride")] + [(name, C.c_int32) for name in (
+                "n_tokens", "n_seqs", "q_heads", "kv_heads", "head_dim", "dtype")] + \
+        [("scale", C.c_float)]
+
+
+class CrossEntropyArgs(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("x", "w", "labels")] + \
+        [("ld_x", C.c_int64), ("ld_w", C.c_int64)] + [(name, C.c_int32) for name in (
+            "n_tokens", "vocab", "dim", "dtype", "labels_bytes")] + [("logit_scale", C.c_float)]
 
 
 class UltraMemError(RuntimeError):
@@ -166,6 +186,25 @@ def load(path: str | None = None) -> C.CDLL:
         lib.ultramem_block_norm_backward.restype = I32
         lib.ultramem_block_norm_backward_workspace.argtypes = [I64, I32]
         lib.ultramem_block_norm_backward_workspace.restype = I64
+        lib.ultramem_paged_attention_backward.argtypes = [P, P, I64, P]
+        lib.ultramem_paged_attention_backward.restype = I32
+        lib.ultramem_paged_attention_backward_workspace.argtypes = [I32] * 6
+        lib.ultramem_paged_attention_backward_workspace.restype = I64
+        lib.ultramem_embedding.argtypes = [P, I64, I32, I32, I32, P, I32, I32, F, P, P]
+        lib.ultramem_embedding.restype = I32
+        lib.ultramem_embedding_backward.argtypes = [P, I32, I32, P, I64, I32, I32, I32, F, P, I32,
+                                                    I32, P, I64, P]
+        lib.ultramem_embedding_backward.restype = I32
+        lib.ultramem_embedding_backward_workspace.argtypes = [I32, I32]
+        lib.ultramem_embedding_backward_workspace.restype = I64
+        lib.ultramem_cross_entropy.argtypes = [P, P, P, P, I64, P]
+        lib.ultramem_cross_entropy.restype = I32
+        lib.ultramem_cross_entropy_workspace.argtypes = [I32] * 4
+        lib.ultramem_cross_entropy_workspace.restype = I64
+        lib.ultramem_cross_entropy_backward.argtypes = [P, P, P, P, P, P, I64, P]
+        lib.ultramem_cross_entropy_backward.restype = I32
+        lib.ultramem_cross_entropy_backward_workspace.argtypes = [I32] * 4
+        lib.ultramem_cross_entropy_backward_workspace.restype = I64
         _lib = lib
         return lib
 

@@ -1,0 +1,36 @@
+// um_attn_grad.cuh -- the gradient of the attention of whole sequences: the
+// call's arguments and the list of tiles, shared by its kernels.
+#pragma once
+
+#include "um_internal.cuh"
+
+namespace um {
+namespace attn_grad {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kMaxHeadDim = 256;
+
+// One block of a sequence's rows (keys or queries).
+struct Block {
+    int tok0, n;              // the sequence's first token and its tokens
+    int b;                    // the block's number in the sequence
+};
+
+struct Args {
+    const void *q, *k, *v, *out, *dout;
+    void *dq, *dk, *dv;
+    const float *lse;
+    const int32_t *q_start;
+    int64_t q_stride, k_stride, v_stride, out_stride, dout_stride, dq_stride, dk_stride, dv_stride;
+    float2 *rows;             // [T][q_heads]: (lse in log2 units, +inf where it is -inf; d_i)
+    int4 *blocks;             // [most]: tok0, n, b of each block of `block` rows
+    int *count;               // of them
+    int *err;
+    int n_seqs, T, q_heads, kv_heads, group, D;
+    int block;                // rows of a block
+    int most;                 // blocks that the list holds
+    float scale, scale_log2;
+};
+
+}  // namespace attn_grad
+}  // namespace um

@@ -1,0 +1,578 @@
+// um_embed.cu -- the embedding of token ids and its gradient.
+//
+// Forward: out[t] = scale table[id_t], one read and one write of a row a
+// token.
+//
+// Gradient: dtable[v] = scale sum_{t: id_t = v} dout[t].  The tokens are sorted
+// by id (stable, so a row's tokens stay in their order), the sorted list is
+// cut into chunks of equal length, and a block sums the runs of equal ids in
+// its chunk in fp32.  A run inside one chunk is written at once; one that
+// crosses chunks leaves a partial sum a chunk, which a last kernel adds in
+// chunk order.  No sum depends on the order in which blocks run, and a
+// frequent id costs no more than rare ones.
+#include "um_device.cuh"
+#include "um_internal.cuh"
+#include "um_overlap.cuh"
+
+namespace um {
+namespace embed {
+namespace {
+
+constexpr int kMaxVocab = 1 << 30;
+constexpr int kMaxDim = 65536;
+
+// ---- values, 8 at a time where rows allow 16-byte accesses -------------------
+
+__device__ __forceinline__ void load8(const float *p, float (&v)[8]) {
+    const float4 a = __ldg(reinterpret_cast<const float4 *>(p));
+    const float4 b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+    v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&v)[8]) {
+    const uint4 a = __ldg(reinterpret_cast<const uint4 *>(p));
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8]) {
+    reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&v)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+// N values (8, or 1 where rows are not aligned)
+template <typename T, int N> __device__ __forceinline__ void load(const T *p, float (&v)[N]) {
+    if constexpr (N == 8) {
+        load8(p, v);
+    } else {
+        v[0] = to_f(p[0]);
+    }
+}
+template <typename T, int N> __device__ __forceinline__ void store(T *p, const float (&v)[N]) {
+    if constexpr (N == 8) {
+        store8(p, v);
+    } else {
+        p[0] = from_f<T>(v[0]);
+    }
+}
+
+// the id of token t, or -1 outside [0, vocab)
+__device__ __forceinline__ int id_of(const void *ids, int wide, int64_t t, int vocab) {
+    const int64_t id = wide ? static_cast<const int64_t *>(ids)[t]
+                            : (int64_t) static_cast<const int32_t *>(ids)[t];
+    return id >= 0 && id < vocab ? (int)id : -1;
+}
+
+// ---- forward -------------------------------------------------------------
+
+// A thread an N-wide piece of a row.
+template <typename T, int N>
+__global__ void __launch_bounds__(256)
+    embed_kernel(const T *table, int64_t ld, int vocab, int D, const void *ids, int wide,
+                 int64_t n_tokens, float scale, T *out) {
+    const int pieces = D / N;
+    const int64_t total = n_tokens * pieces, step = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += step) {
+        const int64_t t = i / pieces;
+        const int c = (int)(i - t * pieces) * N;
+        const int id = id_of(ids, wide, t, vocab);
+        float v[N];
+        if (id >= 0) {
+            load<T, N>(table + (int64_t)id * ld + c, v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] *= scale;
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = 0.f;
+        }
+        store<T, N>(out + t * D + c, v);
+    }
+}
+
+// ---- the tokens sorted by id -------------------------------------------------
+// A radix sort from the lowest digit, 8 bits or less at a time.  A block takes
+// kTile keys in order, a warp 32 x kRounds of them: a key's place among the
+// keys of its digit is the number of equal digits before it in its warp (by
+// matching the lanes of a round, and a counter a warp and digit from round to
+// round), in the warps before, and in the blocks before.
+
+constexpr int kSortThreads = 1024;
+constexpr int kRounds = 16;
+constexpr int kTile = kSortThreads * kRounds;
+constexpr int kDigits = 256;
+constexpr int kWarps = kSortThreads / 32;
+
+struct SortArgs {
+    const void *ids;
+    int *key[2], *tok[2];     // [T], in turns
+    int *hist;                // [tiles][kDigits] of a pass
+    int T, vocab, wide, bits, passes, tiles;
+};
+
+__host__ __device__ __forceinline__ int pass_bits(int bits, int passes) {
+    return (bits + passes - 1) / passes;
+}
+
+// key `i` before pass `p`; an id outside the table sorts behind all others
+__device__ __forceinline__ int key_at(const SortArgs &a, int p, int i) {
+    if (p > 0) return (p & 1 ? a.key[0] : a.key[1])[i];
+    const int id = id_of(a.ids, a.wide, i, a.vocab);
+    return id < 0 ? a.vocab : id;
+}
+
+struct SortShared {
+    int count[kWarps][kDigits];
+    int base[kDigits];
+    int scan[kDigits / 32];
+};
+
+// Pass p of tile `tile`; with `hist` its digits' counts of all tiles are known.
+__device__ void sort_pass(const SortArgs &a, int p, int tile, bool hist, SortShared &s) {
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    const int db = pass_bits(a.bits, a.passes), shift = p * db;
+    const uint32_t mask = (1u << db) - 1u;
+    for (int i = tid; i < kWarps * kDigits; i += kSortThreads) (&s.count[0][0])[i] = 0;
+    __syncthreads();
+    int *key_to = p & 1 ? a.key[1] : a.key[0], *tok_to = p & 1 ? a.tok[1] : a.tok[0];
+    const int *tok_from = p & 1 ? a.tok[0] : a.tok[1];
+    int key[kRounds], rank[kRounds];
+    const int64_t first = (int64_t)tile * kTile + w * 32 * kRounds + lane;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int64_t i = first + r * 32;
+        key[r] = i < a.T ? key_at(a, p, (int)i) : -1;
+    }
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const bool live = first + r * 32 < a.T;
+        const uint32_t d = live ? ((uint32_t)key[r] >> shift) & mask : kDigits;
+        const uint32_t same = __match_any_sync(0xffffffffu, d);
+        const int before = live ? s.count[w][d] : 0;
+        __syncwarp();
+        if (live && lane == __ffs(same) - 1) s.count[w][d] = before + __popc(same);
+        __syncwarp();
+        rank[r] = before + __popc(same & ((1u << lane) - 1u));
+    }
+    __syncthreads();
+    int total = 0, at = 0;
+    if (tid < kDigits) {
+        for (int i = 0; i < kWarps; ++i) {
+            const int c = s.count[i][tid];
+            s.count[i][tid] = total;
+            total += c;
+        }
+        if (hist) {
+            total = 0;
+            for (int i = 0; i < a.tiles; ++i) {
+                const int c = a.hist[(int64_t)i * kDigits + tid];
+                if (i < tile) at += c;
+                total += c;
+            }
+        }
+        int upto = total;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        if (lane == 31) s.scan[w] = upto;
+        at += upto - total;
+    }
+    __syncthreads();
+    if (tid < kDigits) {
+        for (int i = 0; i < w; ++i) at += s.scan[i];
+        s.base[tid] = at;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int64_t i = first + r * 32;
+        if (i >= a.T) continue;
+        const uint32_t d = ((uint32_t)key[r] >> shift) & mask;
+        const int to = s.base[d] + s.count[w][d] + rank[r];
+        key_to[to] = key[r];
+        tok_to[to] = p > 0 ? tok_from[i] : (int)i;
+    }
+}
+
+// zeros over dtable, the blocks `block` of `blocks` sharing it
+__device__ __forceinline__ void fill_zeros(uint4 *at, int64_t n16, void *rest, int rest_bytes,
+                                           int block, int blocks) {
+    const int64_t step = (int64_t)blocks * blockDim.x;
+    for (int64_t i = (int64_t)block * blockDim.x + threadIdx.x; i < n16; i += step)
+        at[i] = make_uint4(0, 0, 0, 0);
+    if (block == 0 && threadIdx.x < rest_bytes) static_cast<uint8_t *>(rest)[threadIdx.x] = 0;
+}
+
+struct FillArgs {
+    uint8_t *at;              // null: nothing to fill
+    int64_t bytes;
+};
+
+// The part `part` of `parts` of the fill.
+__device__ __forceinline__ void fill(const FillArgs &f, int part, int parts, int block,
+                                     int blocks) {
+    if (!f.at) return;
+    // whole 16-byte pieces from the first boundary on; the ends byte by byte
+    const int64_t head = min(f.bytes, (int64_t)(-(uintptr_t)f.at & 15));
+    const int64_t n16 = (f.bytes - head) / 16;
+    const int64_t lo = n16 * part / parts, hi = n16 * (part + 1) / parts;
+    uint4 *body = reinterpret_cast<uint4 *>(f.at + head);
+    if (part == 0 && block == 0 && threadIdx.x < head) f.at[threadIdx.x] = 0;
+    const int tail = part == parts - 1 ? (int)(f.bytes - head - n16 * 16) : 0;
+    fill_zeros(body + lo, hi - lo, f.at + f.bytes - tail, tail, block, blocks);
+}
+
+// The whole sort of at most kTile tokens by block 0; the others zero dtable.
+__global__ void __launch_bounds__(kSortThreads) sort_small_kernel(SortArgs a, FillArgs f) {
+    __shared__ SortShared s;
+    pdl_wait();
+    pdl_trigger();
+    if (blockIdx.x == 0) {
+        for (int p = 0; p < a.passes; ++p) {
+            sort_pass(a, p, 0, false, s);
+            __syncthreads();
+        }
+    } else {
+        fill(f, 0, 1, blockIdx.x - 1, gridDim.x - 1);
+    }
+}
+
+// Digit counts of pass p, a block a tile; blocks past them zero a part of dtable.
+__global__ void __launch_bounds__(kSortThreads)
+    sort_count_kernel(SortArgs a, int p, FillArgs f, int part, int parts) {
+    __shared__ int count[kDigits];
+    pdl_wait();
+    pdl_trigger();
+    const int tile = blockIdx.x;
+    if (tile >= a.tiles) {
+        fill(f, part, parts, tile - a.tiles, gridDim.x - a.tiles);
+        return;
+    }
+    const int db = pass_bits(a.bits, a.passes);
+    if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int r = 0; r < kRounds; ++r) {
+        const int64_t i = (int64_t)tile * kTile + r * kSortThreads + threadIdx.x;
+        if (i < a.T)
+            atomicAdd(&count[((uint32_t)key_at(a, p, (int)i) >> (p * db)) & ((1u << db) - 1u)], 1);
+    }
+    __syncthreads();
+    if (threadIdx.x < kDigits) a.hist[(int64_t)tile * kDigits + threadIdx.x] = count[threadIdx.x];
+}
+
+__global__ void __launch_bounds__(kSortThreads)
+    sort_place_kernel(SortArgs a, int p, FillArgs f, int part, int parts) {
+    __shared__ SortShared s;
+    pdl_wait();
+    pdl_trigger();
+    if ((int)blockIdx.x < a.tiles)
+        sort_pass(a, p, blockIdx.x, true, s);
+    else
+        fill(f, part, parts, blockIdx.x - a.tiles, gridDim.x - a.tiles);
+}
+
+// ---- the sums ----------------------------------------------------------------
+
+struct SumArgs {
+    const int *key, *tok;     // sorted
+    const void *dout;
+    int64_t ld;
+    void *dtable;
+    float *part;              // [chunks][2][D]: a chunk's first and last run, where they cross
+    int T, D, vocab, chunk, chunks, accumulate;
+    float scale;
+};
+
+template <typename O, int N>
+__device__ __forceinline__ void write_row(const SumArgs &a, int id, int c, const float (&s)[N]) {
+    O *to = static_cast<O *>(a.dtable) + (int64_t)id * a.D + c;
+    float v[N];
+    if (a.accumulate) {
+        load<O, N>(to, v);
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = fmaf(a.scale, s[k], v[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = a.scale * s[k];
+    }
+    store<O, N>(to, v);
+}
+
+// A block a chunk of the sorted tokens and blockDim x N columns.
+template <typename T, typename O, int N>
+__global__ void __launch_bounds__(256) sum_kernel(SumArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const int c = (blockIdx.y * blockDim.x + threadIdx.x) * N;
+    const int lo = blockIdx.x * a.chunk;
+    const int hi = (int)min((int64_t)a.T, (int64_t)lo + a.chunk);
+    if (c >= a.D) return;
+    const T *dout = static_cast<const T *>(a.dout) + c;
+    const bool joined = lo > 0 && a.key[lo - 1] == a.key[lo];
+    float *part = a.part + (int64_t)blockIdx.x * 2 * a.D + c;
+    int start = lo;           // of the run at hand
+    float sum[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) sum[k] = 0.f;
+    constexpr int kAhead = 4;
+    for (int64_t i0 = lo; i0 < hi; i0 += kAhead) {
+        float v[kAhead][N];
+        int id[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int i = (int)min(i0 + j, (int64_t)hi - 1);
+            id[j] = a.key[i];
+            load<T, N>(dout + (int64_t)a.tok[i] * a.ld, v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (i0 + j >= hi) break;
+            const int i = (int)i0 + j;
+#pragma unroll
+            for (int k = 0; k < N; ++k) sum[k] += v[j][k];
+            const int next = i + 1 < a.T ? a.key[i + 1] : -1;
+            if (next == id[j] && i + 1 < hi) continue;
+            if (id[j] < a.vocab) {
+                if (start == lo && joined)
+                    store<float, N>(part, sum);             // goes on from the chunk before
+                else if (next == id[j])
+                    store<float, N>(part + a.D, sum);       // goes on in the next chunk
+                else
+                    write_row<O, N>(a, id[j], c, sum);
+            }
+            start = i + 1;
+#pragma unroll
+            for (int k = 0; k < N; ++k) sum[k] = 0.f;
+        }
+    }
+}
+
+// Runs that start in chunk blockIdx.x and cross its end: their partial sums.
+template <typename O, int N> __global__ void __launch_bounds__(64) join_kernel(SumArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const int end = (blockIdx.x + 1) * a.chunk;   // < T: the last chunk has none
+    const int id = a.key[end - 1];
+    if (id >= a.vocab || a.key[end] != id) return;
+    const int lo = end - a.chunk;
+    // all of this chunk, and what goes on from the chunk before: not its start
+    if (a.key[lo] == id && lo > 0 && a.key[lo - 1] == id) return;
+    const int c = (blockIdx.y * blockDim.x + threadIdx.x) * N;
+    if (c >= a.D) return;
+    // chunks whose first key is still `id`: they are sorted, so a search finds the last
+    int first = blockIdx.x + 1, last = a.chunks - 1;
+    while (first < last) {
+        const int m = (first + last + 1) >> 1;
+        if (a.key[(int64_t)m * a.chunk] == id)
+            first = m;
+        else
+            last = m - 1;
+    }
+    float sum[N], v[N];
+    load<float, N>(a.part + ((int64_t)blockIdx.x * 2 + 1) * a.D + c, sum);
+#pragma unroll 8
+    for (int i = blockIdx.x + 1; i <= last; ++i) {
+        load<float, N>(a.part + (int64_t)i * 2 * a.D + c, v);
+#pragma unroll
+        for (int k = 0; k < N; ++k) sum[k] += v[k];
+    }
+    write_row<O, N>(a, id, c, sum);
+}
+
+// ---- launches ------------------------------------------------------------------
+
+// Tokens of a chunk: at least 32, and at most 4096 chunks, so that the partial
+// sums of an id that fills the batch are joined in as many steps.
+int chunk_of(int T) {
+    const int c = (int)(((int64_t)T + 4095) / 4096);
+    return c < 32 ? 32 : c;
+}
+
+struct Layout {
+    int chunk, chunks, tiles;
+    int64_t key[2], tok[2], hist, part, total;
+};
+Layout layout_of(int T, int D) {
+    Layout l = {};
+    l.chunk = chunk_of(T);
+    l.chunks = (T + l.chunk - 1) / l.chunk;
+    l.tiles = (int)(((int64_t)T + kTile - 1) / kTile);
+    const int64_t keys = ((int64_t)T * 4 + 15) & ~15ll;
+    int64_t at = 0;
+    for (int i = 0; i < 2; ++i) {
+        l.key[i] = at;
+        l.tok[i] = at + keys;
+        at += 2 * keys;
+    }
+    l.hist = at;
+    at += (int64_t)l.tiles * kDigits * 4;
+    l.part = at;
+    l.total = at + (int64_t)l.chunks * 2 * D * 4;
+    return l;
+}
+
+template <typename T, typename O, int N>
+cudaError_t sums(const SumArgs &a, cudaStream_t st) {
+    const int pieces = a.D / N;
+    const int threads = pieces >= 256 ? 256 : (pieces + 31) / 32 * 32;
+    cudaError_t e = launch_kernel(true, sum_kernel<T, O, N>,
+                                  dim3(a.chunks, (pieces + threads - 1) / threads), threads, 0, st,
+                                  a);
+    if (e == cudaSuccess && a.chunks > 1)
+        e = launch_kernel(true, join_kernel<O, N>, dim3(a.chunks - 1, (pieces + 63) / 64), 64, 0,
+                          st, a);
+    return e;
+}
+template <typename T, typename O> cudaError_t sums_n(const SumArgs &a, bool wide, cudaStream_t st) {
+    return wide ? sums<T, O, 8>(a, st) : sums<T, O, 1>(a, st);
+}
+
+bool dtype_ok(int32_t t) { return t == ULTRAMEM_F32 || t == ULTRAMEM_BF16; }
+int size_of(int32_t t) { return t == ULTRAMEM_BF16 ? 2 : 4; }
+bool sizes_ok(int32_t vocab, int32_t dim, int32_t ids_bytes, int32_t n_tokens, float scale) {
+    return vocab >= 1 && vocab <= kMaxVocab && dim >= 1 && dim <= kMaxDim &&
+           (ids_bytes == 4 || ids_bytes == 8) && n_tokens >= 0 && isfinite(scale);
+}
+
+}  // namespace
+}  // namespace embed
+}  // namespace um
+
+using namespace um::embed;
+
+extern "C" ultramem_status ultramem_embedding(const void *table, int64_t ld_table, int32_t dtype,
+                                              int32_t vocab, int32_t dim, const void *ids,
+                                              int32_t ids_bytes, int32_t n_tokens, float scale,
+                                              void *out, void *stream) {
+    if (!dtype_ok(dtype) || !sizes_ok(vocab, dim, ids_bytes, n_tokens, scale))
+        return ULTRAMEM_EINVAL;
+    if (n_tokens == 0) return ULTRAMEM_OK;
+    const int es = size_of(dtype);
+    if (!table || !ids || !out || ld_table < dim || ((uintptr_t)table | (uintptr_t)out) % es ||
+        (uintptr_t)ids % ids_bytes)
+        return ULTRAMEM_EINVAL;
+    const int64_t row = (int64_t)dim * es;
+    if (!um::apart({{out, row * n_tokens}}, {{table, row, vocab, ld_table * es},
+                                             {ids, (int64_t)n_tokens * ids_bytes}}))
+        return ULTRAMEM_EINVAL;
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaGetLastError();
+    const bool wide = dim % 8 == 0 && ((uintptr_t)table | (uintptr_t)out) % 16 == 0 &&
+                      ld_table * es % 16 == 0;
+    const int64_t pieces = (int64_t)n_tokens * (wide ? dim / 8 : dim);
+    const int64_t most = (int64_t)um::device_sm_count() * 64, blocks = (pieces + 255) / 256;
+    const unsigned grid = (unsigned)(blocks < most ? blocks : most);
+    auto go = [&](auto t, auto n) {
+        using T = decltype(t);
+        embed_kernel<T, decltype(n)::value><<<grid, 256, 0, st>>>(
+            static_cast<const T *>(table), ld_table, vocab, dim, ids, ids_bytes == 8, n_tokens,
+            scale, static_cast<T *>(out));
+    };
+    using One = std::integral_constant<int, 1>;
+    using Eight = std::integral_constant<int, 8>;
+    if (dtype == ULTRAMEM_BF16)
+        wide ? go(__nv_bfloat16(), Eight()) : go(__nv_bfloat16(), One());
+    else
+        wide ? go(float(), Eight()) : go(float(), One());
+    return um::status_from_cuda(cudaGetLastError());
+}
+
+extern "C" int64_t ultramem_embedding_backward_workspace(int32_t n_tokens, int32_t dim) {
+    if (n_tokens < 0 || dim < 1 || dim > kMaxDim) return 0;
+    return layout_of(n_tokens, dim).total;
+}
+
+extern "C" ultramem_status ultramem_embedding_backward(
+    const void *ids, int32_t ids_bytes, int32_t n_tokens, const void *dout, int64_t ld_dout,
+    int32_t dtype, int32_t vocab, int32_t dim, float scale, void *dtable, int32_t table_dtype,
+    int32_t accumulate, void *workspace, int64_t workspace_bytes, void *stream) {
+    if (!dtype_ok(dtype) || !dtype_ok(table_dtype) || (accumulate != 0 && accumulate != 1) ||
+        !sizes_ok(vocab, dim, ids_bytes, n_tokens, scale) || !dtable ||
+        (uintptr_t)dtable % size_of(table_dtype))
+        return ULTRAMEM_EINVAL;
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaGetLastError();
+    const int64_t out_bytes = (int64_t)vocab * dim * size_of(table_dtype);
+    if (n_tokens == 0) {
+        if (accumulate) return ULTRAMEM_OK;
+        return um::status_from_cuda(cudaMemsetAsync(dtable, 0, out_bytes, st));
+    }
+    const int es = size_of(dtype);
+    const Layout l = layout_of(n_tokens, dim);
+    if (!ids || !dout || ld_dout < dim || (uintptr_t)ids % ids_bytes || (uintptr_t)dout % es ||
+        !workspace || ((uintptr_t)workspace & 15) || workspace_bytes < l.total)
+        return ULTRAMEM_EINVAL;
+    if (!um::apart({{dtable, out_bytes}, {workspace, l.total}},
+                   {{ids, (int64_t)n_tokens * ids_bytes},
+                    {dout, (int64_t)dim * es, n_tokens, ld_dout * es}}))
+        return ULTRAMEM_EINVAL;
+    char *ws = static_cast<char *>(workspace);
+    SortArgs s = {};
+    s.ids = ids;
+    for (int i = 0; i < 2; ++i) {
+        s.key[i] = reinterpret_cast<int *>(ws + l.key[i]);
+        s.tok[i] = reinterpret_cast<int *>(ws + l.tok[i]);
+    }
+    s.hist = reinterpret_cast<int *>(ws + l.hist);
+    s.T = n_tokens;
+    s.vocab = vocab;
+    s.wide = ids_bytes == 8;
+    s.tiles = l.tiles;
+    while ((vocab >> s.bits) != 0) ++s.bits;   // keys 0..vocab
+    s.passes = (s.bits + 7) / 8;
+    const FillArgs f = {accumulate ? nullptr : static_cast<uint8_t *>(dtable), out_bytes};
+    // blocks that zero dtable beside the sorting ones
+    const int64_t want = (out_bytes + 65535) / 65536;
+    const int spare = accumulate ? 0 : (int)(want < um::device_sm_count() ? want
+                                                                          : um::device_sm_count());
+    cudaError_t e = cudaSuccess;
+    if (l.tiles == 1) {
+        e = um::launch_kernel(false, sort_small_kernel, dim3(1 + spare), kSortThreads, 0, st, s, f);
+    } else {
+        const int parts = 2 * s.passes;
+        for (int p = 0; p < s.passes && e == cudaSuccess; ++p) {
+            e = um::launch_kernel(p > 0, sort_count_kernel, dim3(l.tiles + spare), kSortThreads, 0,
+                                  st, s, p, f, 2 * p, parts);
+            if (e == cudaSuccess)
+                e = um::launch_kernel(true, sort_place_kernel, dim3(l.tiles + spare), kSortThreads,
+                                      0, st, s, p, f, 2 * p + 1, parts);
+        }
+    }
+    if (e != cudaSuccess) return um::status_from_cuda(e);
+    SumArgs a = {};
+    a.key = s.key[(s.passes - 1) & 1];
+    a.tok = s.tok[(s.passes - 1) & 1];
+    a.dout = dout;
+    a.ld = ld_dout;
+    a.dtable = dtable;
+    a.part = reinterpret_cast<float *>(ws + l.part);
+    a.T = n_tokens;
+    a.D = dim;
+    a.vocab = vocab;
+    a.chunk = l.chunk;
+    a.chunks = l.chunks;
+    a.accumulate = accumulate;
+    a.scale = scale;
+    const bool wide = dim % 8 == 0 && ((uintptr_t)dout | (uintptr_t)dtable) % 16 == 0 &&
+                      ld_dout * es % 16 == 0;
+    using B = __nv_bfloat16;
+    if (dtype == ULTRAMEM_BF16)
+        e = table_dtype == ULTRAMEM_BF16 ? sums_n<B, B>(a, wide, st) : sums_n<B, float>(a, wide, st);
+    else
+        e = table_dtype == ULTRAMEM_BF16 ? sums_n<float, B>(a, wide, st)
+                                         : sums_n<float, float>(a, wide, st);
+    return um::status_from_cuda(e);
+}

@@ -873,37 +873,6 @@ Layout layout_of(Path path, int32_t dtype, int32_t group, int32_t dim, int32_t m
     return l;
 }
 
-// A map of 64-column boxes over a bf16 tensor [outer][mid][inner] with the
-// given strides in elements; zeros outside.
-bool encode(CUtensorMap *map, const void *base, uint64_t inner, uint64_t mid, uint64_t outer,
-            uint64_t mid_stride, uint64_t outer_stride, uint32_t box_mid, uint32_t box_outer) {
-    using Fn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
-                            const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                            const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static std::atomic<Fn> known{nullptr};   // the driver's, the same for every device
-    Fn fn = known.load();
-    if (!fn) {
-        cudaDriverEntryPointQueryResult q;
-        void *f = nullptr;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000,
-                                             cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess || !f) {
-            cudaGetLastError();
-            return false;
-        }
-        fn = reinterpret_cast<Fn>(f);
-        known.store(fn);
-    }
-    const cuuint64_t dims[3] = {inner, mid, outer};
-    const cuuint64_t strides[2] = {mid_stride * 2, outer_stride * 2};
-    const cuuint32_t box[3] = {64, box_mid, box_outer}, step[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides,
-              box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
-           CUDA_SUCCESS;
-}
-
 // Set by a kernel whose bounded wait gave up; read and cleared by
 // ultramem_paged_check.  Each device has its own.
 __device__ int g_error;
@@ -923,8 +892,6 @@ template <int &SYMBOL> int *word_of() {
     cudaGetLastError();
     return nullptr;
 }
-int *error_word() { return word_of<g_error>(); }
-
 // Reads and clears the word in one step: a timeout that a kernel of another
 // stream records meanwhile is in this answer or in the next one.
 __global__ void take_error_kernel(int *word, int *taken) { *taken = atomicExch(word, 0); }
@@ -958,20 +925,42 @@ bool heads_ok(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim, int
            dim <= kMaxHeadDim && dim % 8 == 0 && max_new >= 0;
 }
 
-// Whether a call's outputs (contiguous) share no memory with one another or
-// with its inputs.
-bool apart(std::initializer_list<Memory> outputs, std::initializer_list<Memory> inputs) {
-    for (const Memory *o = outputs.begin(); o != outputs.end(); ++o) {
-        for (const Memory *p = outputs.begin(); p != o; ++p)
-            if (overlap(*o, *p)) return false;
-        for (const Memory &in : inputs)
-            if (overlap(*o, in)) return false;
-    }
-    return true;
-}
 Memory ints(const int32_t *p, int64_t n) { return {p, n * (int64_t)sizeof(int32_t)}; }
 
 }  // namespace
+
+int *error_word() { return word_of<g_error>(); }
+
+// A map of 64-column boxes over a bf16 tensor [outer][mid][inner] with the
+// given strides in elements; zeros outside.
+bool encode(CUtensorMap *map, const void *base, uint64_t inner, uint64_t mid, uint64_t outer,
+            uint64_t mid_stride, uint64_t outer_stride, uint32_t box_mid, uint32_t box_outer) {
+    using Fn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
+                            const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                            const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static std::atomic<Fn> known{nullptr};   // the driver's, the same for every device
+    Fn fn = known.load();
+    if (!fn) {
+        cudaDriverEntryPointQueryResult q;
+        void *f = nullptr;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000,
+                                             cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess || !f) {
+            cudaGetLastError();
+            return false;
+        }
+        fn = reinterpret_cast<Fn>(f);
+        known.store(fn);
+    }
+    const cuuint64_t dims[3] = {inner, mid, outer};
+    const cuuint64_t strides[2] = {mid_stride * 2, outer_stride * 2};
+    const cuuint32_t box[3] = {64, box_mid, box_outer}, step[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides,
+              box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+           CUDA_SUCCESS;
+}
 
 cudaError_t launch_combine(const AttnArgs &a, int ctas, int dp, int dtype, int max_new, bool pdl,
                            cudaStream_t st) {
@@ -999,7 +988,7 @@ extern "C" ultramem_status ultramem_paged_plan(const int32_t *ctx_lens, const in
     if (n_seqs > 0 && (!ctx_lens || !new_lens || !kv_lens || (table_width > 0 && !block_table)))
         return ULTRAMEM_EINVAL;
     if ((n_tokens > 0 && !slots) || (n_free > 0 && !free_pages)) return ULTRAMEM_EINVAL;
-    if (!apart({ints(q_start, (int64_t)n_seqs + 1), ints(kv_lens, n_seqs), ints(slots, n_tokens),
+    if (!um::apart({ints(q_start, (int64_t)n_seqs + 1), ints(kv_lens, n_seqs), ints(slots, n_tokens),
                 ints(free_left, 1), ints(balance, 1),
                 ints(block_table, (int64_t)n_seqs * table_width)},
                {ints(ctx_lens, n_seqs), ints(new_lens, n_seqs), ints(free_pages, n_free),
@@ -1101,7 +1090,7 @@ extern "C" ultramem_status ultramem_paged_attention(
                      mem_ws = {workspace, need};
     if (!um::same_or_apart(mem_out, mem_q) || um::overlap(mem_lse, mem_q) ||
         um::overlap(mem_ws, mem_q) ||
-        !apart({mem_out, mem_lse, mem_ws},
+        !um::apart({mem_out, mem_lse, mem_ws},
                {ints(q_start, (int64_t)n_seqs + 1), ints(kv_lens, n_seqs),
                 ints(block_table, (int64_t)n_seqs * table_width)}))
         return ULTRAMEM_EINVAL;

@@ -231,6 +231,14 @@ __device__ __forceinline__ int page_of(const AttnArgs &a, int r, int key, int kv
     return p < 0 || p >= a.n_pages ? -1 : p;
 }
 
+// The current device's error word of the calls without a handle (null when it
+// cannot be found): kernels whose bounded wait gave up set kErrTimeout.
+int *error_word();
+// A map of 64-column boxes over a bf16 tensor [outer][mid][inner] with the
+// given strides in elements; zeros outside.  False when it cannot be made.
+bool encode(CUtensorMap *map, const void *base, uint64_t inner, uint64_t mid, uint64_t outer,
+            uint64_t mid_stride, uint64_t outer_stride, uint32_t box_mid, uint32_t box_outer);
+
 // bf16, heads up to 128 wide: at most 16 rows a tile (um_paged_decode.cu), or
 // two halves of 128 rows (um_paged_prefill.cu).  The maps are over the cache
 // as [pages x heads][page size][head width] with boxes of 64 columns x

@@ -11,6 +11,9 @@ list are int32 device tensors; no call waits for the GPU.  One step:
     paged_append(k_cache, v_cache, k, v, slots)            # in every block
     out = paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new)
 
+A training step, whose requests are whole sequences, takes its gradient with
+paged_attention_backward.
+
 As in binding.py, these functions marshal arguments only; there is no
 fallback, and an argument that the library cannot take raises.  They launch on
 the current stream of the current device, where every tensor has to lie, and
@@ -172,6 +175,76 @@ def paged_attention(q, k_cache, v_cache, block_table, q_start, kv_lens, max_new:
     if status:
         raise _b.UltraMemError(status, "ultramem_paged_attention")
     return (out, lse) if with_lse else out
+
+
+@functools.lru_cache(maxsize=256)
+def _grad_workspace(dev, dtype, T, R, q_heads, kv_heads, head_dim):
+    """Bytes of the gradient's workspace, by the sizes and the (current)
+    device alone."""
+    return int(_b.load().ultramem_paged_attention_backward_workspace(dtype, T, R, q_heads,
+                                                                     kv_heads, head_dim))
+
+
+def _grad_rows(name, t, shape, dtype, dev):
+    """A given output [tokens, heads, dim], whose tokens may be strided apart."""
+    s0, s1, s2 = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or s2 != 1 or \
+            s1 != shape[2] or (s0 < shape[1] * shape[2] and shape[0] > 1):
+        raise ValueError(f"{name} must be a tensor {tuple(shape)} of q's type and device, a token's "
+                         "heads contiguous")
+    return t, max(s0, shape[1] * shape[2])
+
+
+def paged_attention_backward(q, k, v, out, lse, dout, q_start, scale=None, dq=None, dk=None,
+                             dv=None):
+    """(dq, dk, dv) of the attention of whole sequences: requests without cached
+    tokens, packed by q_start [R+1], at q [tokens, q_heads, head_dim], the k
+    and v [tokens, kv_heads, head_dim] that were appended, and the out and lse
+    that ``paged_attention`` gave for them, for the gradient dout of out.
+    scale as there.  Tokens of all but lse may be strided apart, as slices of
+    one projection's output; dq, dk and dv may be given, slices of one
+    gradient among them.  Rows that belong to no sequence are not written."""
+    dev = _b._on_device("q", q)
+    if q.dim() != 3 or k.dim() != 3 or q.dtype not in _DTYPES:
+        raise ValueError("q, k and v must be [tokens, heads, head_dim], fp32 or bf16")
+    T, H, D = q.shape
+    heads, dtype = k.shape[1], q.dtype
+    q, qs = _rows("q", q, H, D, dtype, dev)
+    out, os = _rows("out", out, H, D, dtype, dev)
+    dout, ds = _rows("dout", dout, H, D, dtype, dev)
+    k, ks = _rows("k", k, heads, D, dtype, dev)
+    v, vs = _rows("v", v, heads, D, dtype, dev)
+    if any(t.shape[0] != T for t in (out, dout, k, v)):
+        raise ValueError("q, k, v, out and dout must have a row for each token")
+    if lse.shape != (T, H) or lse.dtype != torch.float32 or lse.get_device() != dev or \
+            not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous fp32 tensor [tokens, q_heads] on q's device")
+    R = q_start.numel() - 1
+    if R < 0:
+        raise ValueError("q_start must have an entry more than there are sequences")
+    _b._fits_int32(T, R)
+    starts = _int32("q_start", q_start, dev)
+    grads, strides = [], []
+    for name, t, shape in (("dq", dq, (T, H, D)), ("dk", dk, (T, heads, D)),
+                           ("dv", dv, (T, heads, D))):
+        if t is None:
+            t = torch.empty(shape, dtype=dtype, device=q.device)
+        t, stride = _grad_rows(name, t, shape, dtype, dev)
+        grads.append(t)
+        strides.append(stride)
+    code = _DTYPES[dtype]
+    a = _b.AttentionGrad(
+        q.data_ptr(), out.data_ptr(), dout.data_ptr(), k.data_ptr(), v.data_ptr(),
+        *(t.data_ptr() for t in grads), lse.data_ptr(), starts, qs, os, ds, ks, vs, *strides, T, R,
+        H, heads, D, code, 1.0 / math.sqrt(D) if scale is None else scale)
+    lib = _b._lib or _b.load()
+    nbytes = _grad_workspace(dev, code, T, R, H, heads, D)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    status = lib.ultramem_paged_attention_backward(C.byref(a), ws.data_ptr(), nbytes,
+                                                   _b._stream(dev))
+    if status:
+        raise _b.UltraMemError(status, "ultramem_paged_attention_backward")
+    return tuple(grads)
 
 
 def paged_check() -> int:
