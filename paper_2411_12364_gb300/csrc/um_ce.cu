@@ -1,15 +1,24 @@
 // um_ce.cu -- the softmax cross entropy of hidden states against a vocabulary's
 // output weights, without the logits in memory, and its gradient.
 //
-// Forward: a block makes a 64 x 64 tile of logits and leaves, for each of its
-// tokens, the maximum and the sum of e^(z - maximum) over the tile's columns
-// (and the label's logit, in the tile that has it); a second kernel joins the
-// tiles' pairs.  Gradient: the logits again, in pieces of the vocabulary; a
-// piece's G = scale dloss (e^(z - lse) - onehot) goes to the workspace, and
-// two products read it: dx += G W, dw = G^T x.
+// Forward: z = x W^T in 256 x n tiles on pairs of SMs (um_pair_gemm.cuh); the
+// epilogue leaves, for each token, the maximum and the sum of e^(z - maximum)
+// over the tile's columns (and the label's logit, in the tile that has it),
+// and a second kernel joins the tiles' pairs: T V / n values instead of T V.
+//
+// Gradient: the logits again, in pieces of the vocabulary; a piece's
+// G = scale dloss (e^(z - lse) - onehot) goes to the workspace in the storage
+// type, and two products read it: dx = G W (summed over the pieces) and
+// dw = G^T x (a piece's rows).  Bound by the tensor cores: 2 T V D operations
+// a product.
+//
+// Storage in fp32 enters the products as three bf16 terms a value, v = a + b + c
+// with residues of 2^-9, 2^-17 and 2^-25 of |v|; the six products of terms that
+// reach 2^-24 of the result are added, the smallest first.
 #include "um_device.cuh"
-#include "um_internal.cuh"
 #include "um_overlap.cuh"
+#include "um_paged.cuh"
+#include "um_pair_gemm.cuh"
 
 namespace um {
 namespace ce {
@@ -17,197 +26,451 @@ namespace {
 
 constexpr int kMaxVocab = 1 << 30;
 constexpr int kMaxDim = 65536;
-constexpr int kTile = 64, kStep = 16;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+// bytes of a piece's G, and of its weights where they are rearranged: large
+// enough that a piece's products fill the GPU many times over, and a
+// small part of its memory
 constexpr int64_t kPieceBytes = 512ll << 20;
 
-struct Args {
-    const void *x, *w, *labels;
-    int64_t ld_x, ld_w;
-    int T, V, D, wide;
-    float scale;
-    const float *lse_in, *dloss;
-    float *loss, *lse, *target;
-    float2 *part;             // [tiles][T]
-    float *g;                 // [T][piece]
-    float *dx_sum;            // [T][D]
-    void *dx, *dw;
-    int v0, vn, piece;        // the piece at hand
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+struct Labels {
+    const void *at;
+    int wide, V;
+    // the label of token t, or -1 for one that does not count
+    __device__ __forceinline__ int operator()(int64_t t) const {
+        const int64_t l = wide ? static_cast<const int64_t *>(at)[t]
+                               : (int64_t) static_cast<const int32_t *>(at)[t];
+        return l >= 0 && l < V ? (int)l : -1;
+    }
 };
 
-__device__ __forceinline__ int label_of(const Args &a, int64_t t) {
-    const int64_t l = a.wide ? static_cast<const int64_t *>(a.labels)[t]
-                             : (int64_t) static_cast<const int32_t *>(a.labels)[t];
-    return l >= 0 && l < a.V ? (int)l : -1;
+// ---- operands as planes --------------------------------------------------------
+// src [R][D] (rows ld apart) -> dst [planes][R][Dp], Dp = D rounded up to 8:
+// fp32 values as three bf16 terms, bf16 ones as they are, for operands that
+// TMA cannot read where they lie.  With `labels`, rows of tokens that do not
+// count become zeros, so that weight 0 never meets what they hold.
+template <typename T, bool ALIGNED>
+__global__ void __launch_bounds__(256)
+    planes_kernel(const T *src, int64_t ld, int64_t R, int D, int Dp, __nv_bfloat16 *dst,
+                  Labels labels) {
+    constexpr int P = sizeof(T) == 4 ? 3 : 1;
+    pdl_wait();
+    pdl_trigger();
+    const int pieces = Dp / 8;
+    const int64_t total = R * pieces, step = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += step) {
+        const int64_t r = i / pieces;
+        const int c = (int)(i - r * pieces) * 8;
+        const bool counts = !labels.at || labels(r) >= 0;
+        float v[8];
+        if (ALIGNED && counts) {
+            if constexpr (P == 1) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(src + r * ld + c);
+                *reinterpret_cast<uint4 *>(dst + r * Dp + c) = x;
+                continue;
+            } else {
+                const float4 x = reinterpret_cast<const float4 *>(src + r * ld + c)[0];
+                const float4 y = reinterpret_cast<const float4 *>(src + r * ld + c)[1];
+                v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+                v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                v[k] = counts && c + k < D ? to_f(src[r * ld + c + k]) : 0.f;
+        }
+#pragma unroll
+        for (int q = 0; q < P; ++q) {
+            uint32_t o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+                o[k] = *reinterpret_cast<const uint32_t *>(&b);
+                v[2 * k] -= __low2float(b);
+                v[2 * k + 1] -= __high2float(b);
+            }
+            *reinterpret_cast<uint4 *>(dst + ((int64_t)q * R + r) * Dp + c) =
+                make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    }
 }
 
-// C[i][j] = sum_k A(i, k) B(j, k) of a 64 x 64 tile, 4 x 4 a thread: row
-// ty * 4 + r, column tx * 4 + c.
-template <typename FA, typename FB>
-__device__ __forceinline__ void tile_product(int m, int n, int k, FA a, FB b, float (&c)[4][4]) {
-    __shared__ float sa[kStep][kTile + 4], sb[kStep][kTile + 4];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+// ---- forward -------------------------------------------------------------------
+
+struct LseEpi {
+    Labels labels;
+    float2 *part;             // [tiles][T]: maximum (log2 units) and sum
+    float *target;            // [T]: the label's logit
+    int T, vn, v0, tile0;     // columns of the piece, its first one, its first tile
+    float scale, scale_log2;
+
+    __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
+                                               const pair::Plan &p) const {
+        const int64_t tok = t.m0 + row;
+        const int label = tok < T ? labels(tok) - (v0 + t.n0) : -1;   // the tile's column
+        const int cols = min(p.n_tile, vn - t.n0);
+        float m = -INFINITY, l = 0.f;
+        for (int c = 0; c < cols; c += 32) {
+            float z[32];
+            pair::load32(tmem + c, z);
+            if (label >= c && label < c + 32) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+                for (int k = 0; k < 32; ++k)
+                    if (label == c + k) target[tok] = z[k] * scale;
+            }
+            float top = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c[i][j] = 0.f;
-    for (int k0 = 0; k0 < k; k0 += kStep) {
-        for (int i = threadIdx.x; i < kTile * kStep; i += 256) {
-            const int r = i / kStep, kk = i % kStep;
-            sa[kk][r] = r < m && k0 + kk < k ? a(r, k0 + kk) : 0.f;
-            sb[kk][r] = r < n && k0 + kk < k ? b(r, k0 + kk) : 0.f;
+            for (int k = 0; k < 32; ++k) z[k] *= scale_log2;
+            if (c + 32 > cols) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (c + k >= cols) z[k] = -INFINITY;
+            }
+#pragma unroll
+            for (int k = 0; k < 32; ++k) top = fmaxf(top, z[k]);
+            top = fmaxf(m, top);
+            const float shift = top == -INFINITY ? 0.f : top;
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < 32; ++k) s[k & 3] += ex2(z[k] - shift);
+            l = fmaf(l, ex2(m - shift), (s[0] + s[1]) + (s[2] + s[3]));
+            m = top;
         }
+        if (tok < T) part[(int64_t)(tile0 + t.n0 / p.n_tile) * T + tok] = make_float2(m, l);
+    }
+};
+
+// A block joins the tiles' pairs of 32 tokens, a warp every 32nd tile.
+__global__ void __launch_bounds__(1024)
+    join_kernel(const float2 *part, const float *target, Labels labels, int T, int tiles,
+                float *loss, float *lse) {
+    __shared__ float2 got[32][33];
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    auto add = [](float2 &a, float2 b) {
+        const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.f : top;
+        a.y = a.y * ex2(a.x - shift) + b.y * ex2(b.x - shift);
+        a.x = top;
+    };
+    for (int64_t t0 = (int64_t)blockIdx.x * 32; t0 < T; t0 += (int64_t)gridDim.x * 32) {
+        float2 a = make_float2(-INFINITY, 0.f);
+        if (t0 + lane < T)
+            for (int i = w; i < tiles; i += 32) add(a, part[(int64_t)i * T + t0 + lane]);
+        got[w][lane] = a;
         __syncthreads();
+        const int64_t t = t0 + w;       // now a warp a token
+        a = got[lane][w];
 #pragma unroll
-        for (int kk = 0; kk < kStep; ++kk)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    c[i][j] = fmaf(sa[kk][ty * 4 + i], sb[kk][tx * 4 + j], c[i][j]);
+        for (int o = 16; o; o >>= 1)
+            add(a, make_float2(__shfl_xor_sync(0xffffffffu, a.x, o),
+                               __shfl_xor_sync(0xffffffffu, a.y, o)));
+        if (lane == 0 && t < T) {
+            const float v = kLn2 * (a.x + log2f(a.y));
+            lse[t] = v;
+            loss[t] = labels(t) >= 0 ? v - target[t] : 0.f;
+        }
         __syncthreads();
     }
 }
 
-template <typename T> __device__ __forceinline__ void logits(const Args &a, int t0, int v0, int vn,
-                                                             float (&z)[4][4]) {
-    const T *x = static_cast<const T *>(a.x) + (int64_t)t0 * a.ld_x;
-    const T *w = static_cast<const T *>(a.w) + (int64_t)v0 * a.ld_w;
-    tile_product(min(kTile, a.T - t0), vn, a.D, [&](int i, int k) { return to_f(x[i * a.ld_x + k]); },
-                 [&](int j, int k) { return to_f(w[j * a.ld_w + k]); }, z);
-}
+// ---- gradient ------------------------------------------------------------------
 
-template <typename T> __global__ void __launch_bounds__(256) lse_kernel(Args a) {
-    const int t0 = blockIdx.y * kTile, v0 = blockIdx.x * kTile, vn = min(kTile, a.V - v0);
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float z[4][4];
-    logits<T>(a, t0, v0, vn, z);
+// 32 values to a row of T, from column c on; `wide`: the row allows 16 bytes
+template <typename T>
+__device__ __forceinline__ void store32(T *to, const float (&v)[32], int left, bool wide) {
+    if (wide && left >= 32) {
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t t = t0 + ty * 4 + i;
-        const int label = t < a.T ? label_of(a, t) : -1;
-        float m = -INFINITY, l = 0.f;
+            for (int k = 0; k < 8; ++k)
+                reinterpret_cast<float4 *>(to)[k] =
+                    make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            z[i][j] *= a.scale;
-            if (tx * 4 + j < vn) {
-                m = fmaxf(m, z[i][j]);
-                if (label == v0 + tx * 4 + j) a.target[t] = z[i][j];
+            for (int k = 0; k < 4; ++k) {
+                uint32_t o[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const __nv_bfloat162 b =
+                        __floats2bfloat162_rn(v[8 * k + 2 * j], v[8 * k + 2 * j + 1]);
+                    o[j] = *reinterpret_cast<const uint32_t *>(&b);
+                }
+                reinterpret_cast<uint4 *>(to)[k] = make_uint4(o[0], o[1], o[2], o[3]);
             }
         }
+        return;
+    }
 #pragma unroll
-        for (int o = 8; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        if (m > -INFINITY)
+    for (int k = 0; k < 32; ++k)
+        if (k < left) to[k] = from_f<T>(v[k]);
+}
+
+// P planes of G [P][T][ld]; ld is a multiple of 32, and columns up to the next
+// multiple of 32 past vn are written (as zeros).
+template <int P> struct GradEpi {
+    Labels labels;
+    const float *lse, *dloss;
+    __nv_bfloat16 *g;
+    int64_t ld;
+    int T, vn, v0;
+    float scale, scale_log2;
+
+    __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
+                                               const pair::Plan &p) const {
+        const int64_t tok = t.m0 + row;
+        const bool live = tok < T;
+        const int label = live ? labels(tok) : -1;
+        const int at = label - (v0 + t.n0);
+        const float d = label >= 0 ? dloss[tok] * scale : 0.f;
+        const float shift = label >= 0 ? -lse[tok] * kLog2e : 0.f;
+        const int cols = min(p.n_tile, vn - t.n0);
+        for (int c = 0; c < cols; c += 32) {
+            float z[32];
+            pair::load32(tmem + c, z);
+            if (!live) continue;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (tx * 4 + j < vn) l += expf(z[i][j] - m);
+            for (int k = 0; k < 32; ++k) {
+                float e = ex2(fmaf(z[k], scale_log2, shift));
+                if (at == c + k) e -= 1.f;
+                z[k] = label >= 0 && c + k < cols ? e * d : 0.f;
+            }
+            __nv_bfloat16 *to = g + tok * ld + t.n0 + c;
 #pragma unroll
-        for (int o = 8; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-        if (tx == 0 && t < a.T) a.part[(int64_t)blockIdx.x * a.T + t] = make_float2(m, l);
+            for (int q = 0; q < P; ++q) {
+                store32(to + (int64_t)q * T * ld, z, 32, true);
+                if (q + 1 < P)
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) z[k] -= __bfloat162float(__float2bfloat16_rn(z[k]));
+            }
+        }
+    }
+};
+
+// A product's rows [M][N]: to `out` in T, or, with `part`, in fp32 to
+// part [splits][M][N], added to what it holds when `add`.
+template <typename T> struct StoreEpi {
+    T *out;
+    float *part;
+    int64_t M, N;
+    int add, wide;
+
+    __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
+                                               const pair::Plan &p) const {
+        const int64_t r = t.m0 + row;
+        const int cols = (int)min((int64_t)p.n_tile, N - t.n0);
+        for (int c = 0; c < cols; c += 32) {
+            float v[32];
+            pair::load32(tmem + c, v);
+            if (r >= M) continue;
+            const int left = cols - c;
+            if (!part) {
+                store32(out + r * N + t.n0 + c, v, left, wide);
+                continue;
+            }
+            float *to = part + ((int64_t)t.split * M + r) * N + t.n0 + c;
+            if (add) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (k < left) v[k] += to[k];
+            }
+            store32(to, v, left, N % 4 == 0);
+        }
+    }
+};
+
+// out = sum of part [splits][n] over the splits, in order
+template <typename T>
+__global__ void __launch_bounds__(256)
+    sum_splits_kernel(const float *part, int splits, int64_t n, T *out) {
+    pdl_wait();
+    pdl_trigger();
+    const int64_t step = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += step) {
+        float s = part[i];
+        for (int k = 1; k < splits; ++k) s += part[k * n + i];
+        out[i] = from_f<T>(s);
     }
 }
 
-__global__ void __launch_bounds__(256) join_kernel(Args a, int tiles) {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (t >= a.T) return;
-    float m = -INFINITY, l = 0.f;
-    for (int i = 0; i < tiles; ++i) {
-        const float2 p = a.part[(int64_t)i * a.T + t];
-        const float top = fmaxf(m, p.x);
-        if (top == -INFINITY) continue;
-        l = l * expf(m - top) + p.y * expf(p.x - top);
-        m = top;
-    }
-    const float lse = m + logf(l);
-    a.lse[t] = lse;
-    a.loss[t] = label_of(a, t) >= 0 ? lse - a.target[t] : 0.f;
-}
+// ---- the calls' plans ------------------------------------------------------------
 
-template <typename T> __global__ void __launch_bounds__(256) g_kernel(Args a) {
-    const int t0 = blockIdx.y * kTile, c0 = blockIdx.x * kTile, vn = min(kTile, a.vn - c0);
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float z[4][4];
-    logits<T>(a, t0, a.v0 + c0, vn, z);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t t = t0 + ty * 4 + i;
-        if (t >= a.T) continue;
-        const int label = label_of(a, t);
-        const float d = label >= 0 ? a.dloss[t] * a.scale : 0.f, lse = a.lse_in[t];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = c0 + tx * 4 + j;
-            if (c >= a.vn) continue;
-            const float p = expf(z[i][j] * a.scale - lse) - (label == a.v0 + c ? 1.f : 0.f);
-            const float g = label >= 0 ? to_f(from_f<T>(p * d)) : 0.f;
-            a.g[t * a.piece + c] = g;
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t pad256(int64_t n) { return (n + 255) & ~255ll; }
+int pairs_of_sms() {
+    const int n = device_sm_count() / 2;
+    return n < 1 ? 1 : n;
+}
+int planes_of(int32_t dtype) { return dtype == ULTRAMEM_F32 ? 3 : 1; }
+
+// The product of [M][K] and [N][K]: tiles, and splits of K where there are
+// fewer tiles than pairs of SMs.
+// n_tile: the widest tile, unless narrower ones share out among the pairs more
+// evenly; `step` 32, or 128 where the columns are MN-major (boxes of 64 columns a CTA).
+// splits (at most `most`, 64 or fewer): a tile's time is its k blocks (512 cycles each) and
+// about 3000 cycles; a split costs a pass over the output in fp32.
+pair::Plan plan_of(int64_t M, int64_t N, int64_t K, int planes, int step, int most) {
+    pair::Plan p = {};
+    const int64_t pairs = pairs_of_sms();
+    p.m_tiles = (int)ceil_div(M, pair::kTileM);
+    p.k_blocks = (int)ceil_div(K, 64);
+    p.pairs = planes == 3 ? pair::kSplitPairs : 1;
+    double best = 0;
+    for (int n = pair::kMaxN; n >= 128; n -= step) {
+        const int64_t nt = ceil_div(N, n);
+        // a second share of a pair's time is the last that a split can save
+        for (int s = 1; s <= most && s <= p.k_blocks; ++s) {
+            if (s > 1 && p.m_tiles * nt * (s - 1) >= 2 * pairs) break;
+            const int64_t waves = ceil_div(p.m_tiles * nt * s, pairs);
+            const double tile = (double)ceil_div(p.k_blocks, s) * p.pairs * 2.0 * n + 3000.0;
+            // 2000 cycles and s writes and reads of the output at 3 KB a cycle
+            const double join = s > 1 ? 2000.0 + (double)M * N * 8.0 * s / 3000.0 : 0.0;
+            const double cost = waves * tile + join;
+            if (best == 0 || cost < 0.97 * best) {
+                best = cost;
+                p.n_tile = n;
+                p.n_tiles = (int)nt;
+                p.splits = s;
+            }
         }
     }
+    p.group_m = 8;
+    return p;
 }
 
-template <typename T> __global__ void __launch_bounds__(256) dx_kernel(Args a) {
-    const int t0 = blockIdx.y * kTile, c0 = blockIdx.x * kTile;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const T *w = static_cast<const T *>(a.w) + (int64_t)a.v0 * a.ld_w + c0;
-    const float *g = a.g + (int64_t)t0 * a.piece;
-    float c[4][4];
-    tile_product(min(kTile, a.T - t0), min(kTile, a.D - c0), a.vn,
-                 [&](int i, int k) { return g[(int64_t)i * a.piece + k]; },
-                 [&](int j, int k) { return to_f(w[k * a.ld_w + j]); }, c);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t t = t0 + ty * 4 + i;
-            const int col = c0 + tx * 4 + j;
-            if (t >= a.T || col >= a.D) continue;
-            const float v = c[i][j] + (a.v0 ? a.dx_sum[t * a.D + col] : 0.f);
-            if (a.v0 + a.vn == a.V)
-                static_cast<T *>(a.dx)[t * a.D + col] = from_f<T>(v);
-            else
-                a.dx_sum[t * a.D + col] = v;
-        }
+// rows x [K or columns]: K-major boxes of `rows` rows, or MN-major ones of 64 k
+bool operand(CUtensorMap *map, const void *at, int64_t inner, int64_t rows, int64_t ld, int planes,
+             int64_t plane, uint32_t box) {
+    return paged::encode(map, at, inner, rows, planes, ld, plane, box, 1);
 }
 
-template <typename T> __global__ void __launch_bounds__(256) dw_kernel(Args a) {
-    const int r0 = blockIdx.y * kTile, c0 = blockIdx.x * kTile;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const T *x = static_cast<const T *>(a.x) + c0;
-    const float *g = a.g + r0;
-    float c[4][4];
-    tile_product(min(kTile, a.vn - r0), min(kTile, a.D - c0), a.T,
-                 [&](int i, int k) { return g[(int64_t)k * a.piece + i]; },
-                 [&](int j, int k) {   // a token that does not count: whatever x holds
-                     return label_of(a, k) >= 0 ? to_f(x[k * a.ld_x + j]) : 0.f;
-                 }, c);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t v = (int64_t)a.v0 + r0 + ty * 4 + i;
-            const int col = c0 + tx * 4 + j;
-            if (r0 + ty * 4 + i < a.vn && col < a.D)
-                static_cast<T *>(a.dw)[v * a.D + col] = from_f<T>(c[i][j]);
-        }
+template <class Epi, bool A_MN, bool B_MN>
+cudaError_t multiply(const CUtensorMap &a, const CUtensorMap &b, const pair::Plan &p, const Epi &epi,
+                     cudaStream_t st) {
+    cudaError_t e = allow_dynamic_smem<pair::gemm_kernel<Epi, A_MN, B_MN>>(pair::kSmem);
+    if (e != cudaSuccess) return e;
+    const int64_t items = (int64_t)p.m_tiles * p.n_tiles * p.splits, pairs = pairs_of_sms();
+    return launch_kernel(true, pair::gemm_kernel<Epi, A_MN, B_MN>,
+                         dim3((unsigned)(2 * (items < pairs ? items : pairs))), pair::kThreads,
+                         pair::kSmem, st, a, b, p, epi);
 }
 
-// ---- the calls' plans --------------------------------------------------------
+// Whether TMA reads a matrix where it lies.
+bool as_it_lies(int32_t dtype, const void *at, int64_t ld) {
+    return dtype == ULTRAMEM_BF16 && (uintptr_t)at % 16 == 0 && ld * 2 % 16 == 0;
+}
+int64_t padded(int64_t D) { return (D + 7) & ~7ll; }
 
-int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+template <typename T>
+cudaError_t planes_t(const void *src, int64_t ld, int64_t R, int D, void *dst, Labels labels,
+                     bool pdl, cudaStream_t st) {
+    const int Dp = (int)padded(D);
+    const int64_t blocks = ceil_div(R * (Dp / 8), 256), most = (int64_t)device_sm_count() * 16;
+    const unsigned grid = (unsigned)(blocks < most ? blocks : most);
+    const bool aligned = D % 8 == 0 && (uintptr_t)src % 16 == 0 && ld * sizeof(T) % 16 == 0;
+    const T *s = static_cast<const T *>(src);
+    __nv_bfloat16 *d = static_cast<__nv_bfloat16 *>(dst);
+    return aligned ? launch_kernel(pdl, planes_kernel<T, true>, grid, 256, 0, st, s, ld, R, D, Dp, d,
+                                   labels)
+                   : launch_kernel(pdl, planes_kernel<T, false>, grid, 256, 0, st, s, ld, R, D, Dp,
+                                   d, labels);
+}
+cudaError_t to_planes(int32_t dtype, const void *src, int64_t ld, int64_t R, int D, void *dst,
+                      Labels labels, bool pdl, cudaStream_t st) {
+    return dtype == ULTRAMEM_BF16
+               ? planes_t<__nv_bfloat16>(src, ld, R, D, dst, labels, pdl, st)
+               : planes_t<float>(src, ld, R, D, dst, labels, pdl, st);
+}
+
+// A matrix as the products read it: where it lies, or its planes.
+struct Matrix {
+    const void *at;
+    int64_t ld, plane;
+    int planes;
+};
 
 bool sizes_ok(int32_t dtype, int32_t T, int32_t V, int32_t D) {
     return (dtype == ULTRAMEM_F32 || dtype == ULTRAMEM_BF16) && T >= 0 && V >= 1 &&
-           V <= kMaxVocab && D >= 1 && D <= kMaxDim;
+           V <= kMaxVocab && D >= 1 && D <= kMaxDim &&
+           ceil_div(T, pair::kTileM) * ceil_div(V, 128) <= INT32_MAX &&     // tiles
+           ceil_div(T, pair::kTileM) * ceil_div(D, 128) * 64 <= INT32_MAX;
 }
 
-int piece_of(int32_t T, int32_t V) {
-    int64_t n = kPieceBytes / 4 / (T > 0 ? T : 1) / kTile * kTile;
-    if (n < kTile) n = kTile;
-    return (int)(n < V ? n : V);
+// Rows of the vocabulary whose planes fit a piece's bytes.
+int64_t rows_in_planes(int32_t dtype, int32_t D) {
+    const int64_t n = kPieceBytes / (planes_of(dtype) * padded(D) * 2) / 256 * 256;
+    return n < 256 ? 256 : n;
+}
+// `limit` rows or fewer a piece, in equal pieces of whole tiles
+int64_t piece_of(int64_t V, int64_t limit) {
+    if (V <= limit) return V;
+    const int64_t n = ceil_div(V, limit);
+    return ceil_div(ceil_div(V, n), 256) * 256;
+}
+
+struct ForwardLayout {
+    int64_t piece;            // of the vocabulary, when the weights are rearranged
+    int64_t tiles;            // of all pieces, at most
+    int64_t part, target, x, w, total;
+};
+ForwardLayout forward_layout(int32_t dtype, int64_t T, int64_t V, int32_t D) {
+    ForwardLayout l = {};
+    l.piece = piece_of(V, rows_in_planes(dtype, D));
+    // a tile is at least 128 columns wide, and pieces are whole tiles but for the last of each
+    l.tiles = ceil_div(V, 128) + ceil_div(V, l.piece);
+    const int64_t es = planes_of(dtype) * padded(D) * 2;
+    l.part = 0;
+    l.target = pad256(l.tiles * T * 8);
+    l.x = l.target + pad256(T * 4);
+    l.w = l.x + pad256(T * es);
+    l.total = l.w + pad256(l.piece * es) + 256;
+    return l;
+}
+
+struct BackwardLayout {
+    int64_t piece, ld;        // ld: of G
+    int64_t x, w, g, dx, dw, total;
+    int dx_splits, dw_splits; // at most
+    pair::Plan logits, x_plan, w_plan;       // of a whole piece
+};
+BackwardLayout backward_layout(int32_t dtype, int64_t T, int64_t V, int32_t D) {
+    BackwardLayout l = {};
+    const int P = planes_of(dtype);
+    int64_t limit = kPieceBytes / (2 * P * (T > 0 ? T : 1)) / 256 * 256;
+    if (limit < 256) limit = 256;
+    const int64_t rows = rows_in_planes(dtype, D);
+    l.piece = piece_of(V, limit < rows ? limit : rows);
+    l.ld = (l.piece + 31) & ~31ll;
+    // partial sums stay below a piece's bytes
+    auto most = [](int64_t m, int64_t n) {
+        const int64_t s = kPieceBytes / (m * n * 4);
+        return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+    };
+    const int64_t t = T > 0 ? T : 1;
+    l.logits = plan_of(t, l.piece, D, P, 32, 1);
+    l.x_plan = plan_of(t, D, l.piece, P, 128, most(t, D));
+    l.w_plan = plan_of(l.piece, D, t, P, 128, most(l.piece, D));
+    l.dx_splits = l.x_plan.splits;
+    l.dw_splits = l.w_plan.splits;
+    const int64_t es = P * padded(D) * 2;
+    l.x = 0;
+    l.w = pad256(T * es);
+    l.g = l.w + pad256(l.piece * es);
+    l.dx = l.g + pad256(P * T * l.ld * 2);
+    l.dw = l.dx + (l.dx_splits > 1 || l.piece < V ? pad256(4 * l.dx_splits * T * D) : 0);
+    l.total = l.dw + (l.dw_splits > 1 ? pad256(4 * l.dw_splits * l.piece * D) : 0) + 256;
+    return l;
 }
 
 bool args_ok(const ultramem_cross_entropy_args *p) {
     return p && sizes_ok(p->dtype, p->n_tokens, p->vocab, p->dim) &&
-           (p->labels_bytes == 4 || p->labels_bytes == 8) && isfinite(p->logit_scale);
+           (p->labels_bytes == 4 || p->labels_bytes == 8) && isfinite(p->logit_scale) &&
+           isfinite(p->logit_scale * kLog2e);
 }
 bool inputs_ok(const ultramem_cross_entropy_args *p) {
     const int es = p->dtype == ULTRAMEM_BF16 ? 2 : 4;
@@ -219,19 +482,146 @@ Memory rows_of(const ultramem_cross_entropy_args *p, const void *at, int64_t n, 
     const int64_t es = p->dtype == ULTRAMEM_BF16 ? 2 : 4;
     return {at, p->dim * es, n, ld * es};
 }
-Args args_of(const ultramem_cross_entropy_args *p) {
-    Args a = {};
-    a.x = p->x;
-    a.w = p->w;
-    a.labels = p->labels;
-    a.ld_x = p->ld_x;
-    a.ld_w = p->ld_w;
-    a.T = p->n_tokens;
-    a.V = p->vocab;
-    a.D = p->dim;
-    a.wide = p->labels_bytes == 8;
-    a.scale = p->logit_scale;
-    return a;
+Labels labels_of(const ultramem_cross_entropy_args *p) {
+    return {p->labels, p->labels_bytes == 8, p->vocab};
+}
+char *aligned256(void *p) {
+    return reinterpret_cast<char *>(((uintptr_t)p + 255) & ~(uintptr_t)255);
+}
+const char *row_at(const ultramem_cross_entropy_args *p, int64_t v) {
+    return static_cast<const char *>(p->w) + v * p->ld_w * (p->dtype == ULTRAMEM_BF16 ? 2 : 4);
+}
+
+cudaError_t forward(const ultramem_cross_entropy_args *p, const ForwardLayout &l, float *loss,
+                    float *lse, char *ws, int *err, cudaStream_t st) {
+    const int P = planes_of(p->dtype), D = p->dim;
+    const int64_t T = p->n_tokens, Dp = padded(D);
+    cudaError_t e = cudaSuccess;
+    bool pdl = false;
+    Matrix x = {p->x, p->ld_x, T * p->ld_x, 1};
+    if (!as_it_lies(p->dtype, p->x, p->ld_x)) {
+        x = {ws + l.x, Dp, T * Dp, P};
+        e = to_planes(p->dtype, p->x, p->ld_x, T, D, ws + l.x, {}, false, st);
+        pdl = true;
+    }
+    const bool direct = as_it_lies(p->dtype, p->w, p->ld_w);
+    const int64_t piece = direct ? p->vocab : l.piece;
+    LseEpi epi = {};
+    epi.labels = labels_of(p);
+    epi.part = reinterpret_cast<float2 *>(ws + l.part);
+    epi.target = reinterpret_cast<float *>(ws + l.target);
+    epi.T = p->n_tokens;
+    epi.scale = p->logit_scale;
+    epi.scale_log2 = p->logit_scale * kLog2e;
+    for (int64_t v0 = 0; v0 < p->vocab && e == cudaSuccess; v0 += piece) {
+        const int64_t vn = p->vocab - v0 < piece ? p->vocab - v0 : piece;
+        Matrix w = {row_at(p, v0), p->ld_w, vn * p->ld_w, 1};
+        if (!direct) {
+            w = {ws + l.w, Dp, vn * Dp, P};
+            e = to_planes(p->dtype, row_at(p, v0), p->ld_w, vn, D, ws + l.w, {}, pdl, st);
+            if (e != cudaSuccess) break;
+        }
+        pair::Plan plan = plan_of(T, vn, D, P, 32, 1);
+        plan.err = err;
+        CUtensorMap ma, mb;
+        if (!operand(&ma, x.at, D, T, x.ld, x.planes, x.plane, 128) ||
+            !operand(&mb, w.at, D, vn, w.ld, w.planes, w.plane, plan.n_tile / 2))
+            return cudaErrorInvalidValue;
+        epi.vn = (int)vn;
+        epi.v0 = (int)v0;
+        e = multiply<LseEpi, false, false>(ma, mb, plan, epi, st);
+        epi.tile0 += plan.n_tiles;
+        pdl = true;
+    }
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = ceil_div(T, 32);
+    return launch_kernel(true, join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), 1024, 0,
+                         st, (const float2 *)epi.part, (const float *)epi.target, epi.labels,
+                         p->n_tokens, epi.tile0, loss, lse);
+}
+
+template <typename T, int P>
+cudaError_t backward(const ultramem_cross_entropy_args *p, const BackwardLayout &l,
+                     const float *lse, const float *dloss, void *dx, void *dw, char *ws, int *err,
+                     cudaStream_t st) {
+    const int D = p->dim;
+    const int64_t N = p->n_tokens, Dp = padded(D);
+    cudaError_t e = cudaSuccess;
+    // dw reads x with weights that are 0 for tokens that do not count
+    bool pdl = false;
+    Matrix x = {p->x, p->ld_x, N * p->ld_x, 1};
+    if (dw || !as_it_lies(p->dtype, p->x, p->ld_x)) {
+        x = {ws + l.x, Dp, N * Dp, P};
+        e = to_planes(p->dtype, p->x, p->ld_x, N, D, ws + l.x, labels_of(p), false, st);
+        pdl = true;
+    }
+    const bool direct = as_it_lies(p->dtype, p->w, p->ld_w);
+    GradEpi<P> ge = {};
+    ge.labels = labels_of(p);
+    ge.lse = lse;
+    ge.dloss = dloss;
+    ge.g = reinterpret_cast<__nv_bfloat16 *>(ws + l.g);
+    ge.ld = l.ld;
+    ge.T = p->n_tokens;
+    ge.scale = p->logit_scale;
+    ge.scale_log2 = p->logit_scale * kLog2e;
+    const bool dx_parts = l.dx_splits > 1 || l.piece < p->vocab;
+    float *dx_sum = dx_parts ? reinterpret_cast<float *>(ws + l.dx) : nullptr;
+    float *dw_sum = l.dw_splits > 1 ? reinterpret_cast<float *>(ws + l.dw) : nullptr;
+    auto wide = [&](const void *at) { return (uintptr_t)at % 16 == 0 && D * sizeof(T) % 16 == 0; };
+    auto sum_splits = [&](const float *part, int splits, int64_t n, T *out) {
+        const int64_t blocks = ceil_div(n, 1024), most = (int64_t)device_sm_count() * 16;
+        return launch_kernel(true, sum_splits_kernel<T>,
+                             dim3((unsigned)(blocks < most ? blocks : most)), 256, 0, st, part,
+                             splits, n, out);
+    };
+    for (int64_t v0 = 0; v0 < p->vocab && e == cudaSuccess; v0 += l.piece) {
+        const int64_t vn = p->vocab - v0 < l.piece ? p->vocab - v0 : l.piece;
+        Matrix w = {row_at(p, v0), p->ld_w, vn * p->ld_w, 1};
+        if (!direct) {
+            w = {ws + l.w, Dp, vn * Dp, P};
+            e = to_planes(p->dtype, row_at(p, v0), p->ld_w, vn, D, ws + l.w, {}, pdl, st);
+            if (e != cudaSuccess) break;
+        }
+        CUtensorMap ma, mb;
+        pair::Plan plan = l.logits;
+        plan.n_tiles = (int)ceil_div(vn, plan.n_tile);
+        plan.err = err;
+        if (!operand(&ma, x.at, D, N, x.ld, x.planes, x.plane, 128) ||
+            !operand(&mb, w.at, D, vn, w.ld, w.planes, w.plane, plan.n_tile / 2))
+            return cudaErrorInvalidValue;
+        ge.vn = (int)vn;
+        ge.v0 = (int)v0;
+        e = multiply<GradEpi<P>, false, false>(ma, mb, plan, ge, st);
+        pdl = true;
+        if (dx && e == cudaSuccess) {            // [N][D] = G [N][vn] W [vn][D]
+            plan = l.x_plan;
+            plan.k_blocks = (int)ceil_div(vn, 64);
+            // a short last piece: fewer splits, the other sums stay as they are
+            if (plan.splits > plan.k_blocks) plan.splits = plan.k_blocks;
+            plan.err = err;
+            if (!operand(&ma, ge.g, vn, N, l.ld, P, N * l.ld, 128) ||
+                !operand(&mb, w.at, D, vn, w.ld, w.planes, w.plane, 64))
+                return cudaErrorInvalidValue;
+            const StoreEpi<T> se = {static_cast<T *>(dx), dx_sum, N, D, v0 > 0, wide(dx)};
+            e = multiply<StoreEpi<T>, false, true>(ma, mb, plan, se, st);
+        }
+        if (dw && e == cudaSuccess) {            // [vn][D] = G^T [vn][N] x [N][D]
+            plan = l.w_plan;
+            plan.m_tiles = (int)ceil_div(vn, pair::kTileM);
+            plan.err = err;
+            if (!operand(&ma, ge.g, vn, N, l.ld, P, N * l.ld, 64) ||
+                !operand(&mb, x.at, D, N, x.ld, x.planes, x.plane, 64))
+                return cudaErrorInvalidValue;
+            T *out = static_cast<T *>(dw) + v0 * D;
+            const StoreEpi<T> se = {out, dw_sum, vn, D, 0, wide(out)};
+            e = multiply<StoreEpi<T>, true, true>(ma, mb, plan, se, st);
+            if (dw_sum && e == cudaSuccess) e = sum_splits(dw_sum, l.dw_splits, vn * D, out);
+        }
+    }
+    if (dx && dx_sum && e == cudaSuccess)
+        e = sum_splits(dx_sum, l.dx_splits, N * D, static_cast<T *>(dx));
+    return e;
 }
 
 }  // namespace
@@ -243,7 +633,7 @@ using namespace um::ce;
 extern "C" int64_t ultramem_cross_entropy_workspace(int32_t dtype, int32_t n_tokens,
                                                     int32_t vocab, int32_t dim) {
     if (!sizes_ok(dtype, n_tokens, vocab, dim)) return 0;
-    return (int64_t)n_tokens * (8ll * ceil_div(vocab, kTile) + 4);
+    return forward_layout(dtype, n_tokens, vocab, dim).total;
 }
 
 extern "C" ultramem_status ultramem_cross_entropy(const ultramem_cross_entropy_args *p,
@@ -251,7 +641,8 @@ extern "C" ultramem_status ultramem_cross_entropy(const ultramem_cross_entropy_a
                                                   int64_t workspace_bytes, void *stream) {
     if (!args_ok(p)) return ULTRAMEM_EINVAL;
     if (p->n_tokens == 0) return ULTRAMEM_OK;
-    const int64_t need = ultramem_cross_entropy_workspace(p->dtype, p->n_tokens, p->vocab, p->dim);
+    const ForwardLayout l = forward_layout(p->dtype, p->n_tokens, p->vocab, p->dim);
+    const int64_t need = l.total;
     if (!inputs_ok(p) || !loss || !lse || ((uintptr_t)loss | (uintptr_t)lse) % 4 || !workspace ||
         ((uintptr_t)workspace & 15) || workspace_bytes < need)
         return ULTRAMEM_EINVAL;
@@ -260,27 +651,17 @@ extern "C" ultramem_status ultramem_cross_entropy(const ultramem_cross_entropy_a
                    {rows_of(p, p->x, T, p->ld_x), rows_of(p, p->w, p->vocab, p->ld_w),
                     {p->labels, T * p->labels_bytes}}))
         return ULTRAMEM_EINVAL;
-    Args a = args_of(p);
-    a.loss = loss;
-    a.lse = lse;
-    const int tiles = ceil_div(a.V, kTile);
-    a.part = static_cast<float2 *>(workspace);
-    a.target = reinterpret_cast<float *>(a.part + T * tiles);
-    cudaStream_t st = (cudaStream_t)stream;
     cudaGetLastError();
-    const dim3 grid(tiles, ceil_div(T, kTile));
-    if (p->dtype == ULTRAMEM_BF16)
-        lse_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(a);
-    else
-        lse_kernel<float><<<grid, 256, 0, st>>>(a);
-    join_kernel<<<ceil_div(T, 256), 256, 0, st>>>(a, tiles);
-    return um::status_from_cuda(cudaGetLastError());
+    int *err = um::paged::error_word();
+    if (!err) return ULTRAMEM_ENODEV;
+    return um::status_from_cuda(
+        forward(p, l, loss, lse, aligned256(workspace), err, (cudaStream_t)stream));
 }
 
 extern "C" int64_t ultramem_cross_entropy_backward_workspace(int32_t dtype, int32_t n_tokens,
                                                              int32_t vocab, int32_t dim) {
     if (!sizes_ok(dtype, n_tokens, vocab, dim)) return 0;
-    return 4ll * n_tokens * ((int64_t)piece_of(n_tokens, vocab) + dim);
+    return backward_layout(dtype, n_tokens, vocab, dim).total;
 }
 
 extern "C" ultramem_status ultramem_cross_entropy_backward(const ultramem_cross_entropy_args *p,
@@ -296,8 +677,8 @@ extern "C" ultramem_status ultramem_cross_entropy_backward(const ultramem_cross_
     if (p->n_tokens == 0)
         return dw ? um::status_from_cuda(cudaMemsetAsync(dw, 0, dw_bytes, st)) : ULTRAMEM_OK;
     if (!dx && !dw) return ULTRAMEM_OK;
-    const int64_t need =
-        ultramem_cross_entropy_backward_workspace(p->dtype, p->n_tokens, p->vocab, p->dim);
+    const BackwardLayout l = backward_layout(p->dtype, p->n_tokens, p->vocab, p->dim);
+    const int64_t need = l.total;
     if (!inputs_ok(p) || !lse || !dloss || ((uintptr_t)lse | (uintptr_t)dloss) % 4 || !workspace ||
         ((uintptr_t)workspace & 15) || workspace_bytes < need)
         return ULTRAMEM_EINVAL;
@@ -306,26 +687,11 @@ extern "C" ultramem_status ultramem_cross_entropy_backward(const ultramem_cross_
                    {rows_of(p, p->x, T, p->ld_x), rows_of(p, p->w, p->vocab, p->ld_w),
                     {p->labels, T * p->labels_bytes}, {lse, T * 4}, {dloss, T * 4}}))
         return ULTRAMEM_EINVAL;
-    Args a = args_of(p);
-    a.lse_in = lse;
-    a.dloss = dloss;
-    a.dx = dx;
-    a.dw = dw;
-    a.piece = piece_of(a.T, a.V);
-    a.g = static_cast<float *>(workspace);
-    a.dx_sum = a.g + T * a.piece;
-    for (a.v0 = 0; a.v0 < a.V; a.v0 += a.piece) {
-        a.vn = a.V - a.v0 < a.piece ? a.V - a.v0 : a.piece;
-        const dim3 g_grid(ceil_div(a.vn, kTile), ceil_div(T, kTile));
-        const dim3 dx_grid(ceil_div(a.D, kTile), ceil_div(T, kTile));
-        const dim3 dw_grid(ceil_div(a.D, kTile), ceil_div(a.vn, kTile));
-        auto go = [&](auto t) {
-            using E = decltype(t);
-            g_kernel<E><<<g_grid, 256, 0, st>>>(a);
-            if (dx) dx_kernel<E><<<dx_grid, 256, 0, st>>>(a);
-            if (dw) dw_kernel<E><<<dw_grid, 256, 0, st>>>(a);
-        };
-        p->dtype == ULTRAMEM_BF16 ? go(__nv_bfloat16()) : go(float());
-    }
-    return um::status_from_cuda(cudaGetLastError());
+    int *err = um::paged::error_word();
+    if (!err) return ULTRAMEM_ENODEV;
+    char *ws = aligned256(workspace);
+    return um::status_from_cuda(
+        p->dtype == ULTRAMEM_BF16
+            ? backward<__nv_bfloat16, 1>(p, l, lse, dloss, dx, dw, ws, err, st)
+            : backward<float, 3>(p, l, lse, dloss, dx, dw, ws, err, st));
 }

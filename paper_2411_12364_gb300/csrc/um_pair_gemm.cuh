@@ -1,0 +1,317 @@
+// um_pair_gemm.cuh -- D = A B^T on pairs of SMs (tcgen05.mma.cta_group::2), bf16
+// operands, fp32 accumulators: a persistent kernel with 256 x n_tile output
+// tiles and an epilogue of the caller's.
+//
+// A cluster of two CTAs makes a tile: each holds 128 rows of A and half of the
+// tile's columns of B in shared memory, and the accumulators of its 128 rows
+// in its own TMEM.  One k block of 64 is 16 KiB of A and up to 16 KiB of B a
+// CTA, half of B's bytes of a one-CTA tile of the same shape; that is what
+// the pair is for, because a 128 x 256 tile on one SM would read 96 bytes a
+// cycle from shared memory and take as many by copies.  Two accumulators of
+// up to 256 columns fill TMEM, so that the epilogue of a tile runs under the
+// products of the next one.
+//
+// Each operand is K-major (rows of A or B, k contiguous) or MN-major (rows of
+// k, the row index of A or B contiguous), so that a matrix and its transpose
+// are read from the same memory.  An operand may be given as up to three
+// planes that add up to it (fp32 values as three bf16 terms): the k loop then
+// runs over pairs of planes, smallest products first.
+//
+// Warps of a CTA: 0 copies (TMA, one elected thread), 1 products (one thread
+// of the pair's first CTA), 2-5 epilogue.  Waits are bounded; one that gives
+// up sets the error word, and the others run into their own limits.
+#pragma once
+
+#include "um_internal.cuh"
+#include "um_tc.cuh"
+
+namespace um {
+namespace pair {
+
+constexpr int kThreads = 192;
+constexpr int kTileM = 256, kMaxN = 256;
+constexpr int kStages = 6;
+constexpr uint32_t kOperand = 128 * 128;                  // 128 rows (or columns) x 64 k
+constexpr uint32_t kStage = 2 * kOperand;
+constexpr size_t kSmem = (size_t)kStages * kStage + 1024;
+constexpr uint32_t kGroupBytes = 64 * 128;                // MN-major: 64 columns x 64 k
+
+// Pairs of planes in the order that they are added: the smallest first.
+constexpr int kSplitPairs = 6;
+__device__ __forceinline__ int a_plane(int pairs, int i) {
+    return pairs == 1 ? 0 : (0x001012 >> (4 * (5 - i))) & 15;
+}
+__device__ __forceinline__ int b_plane(int pairs, int i) {
+    return pairs == 1 ? 0 : (0x010210 >> (4 * (5 - i))) & 15;
+}
+
+struct Plan {
+    int m_tiles, n_tiles, n_tile, splits;    // splits: of the k blocks, a tile each
+    int k_blocks, pairs;                     // k blocks of a plane, pairs of planes
+    int group_m;                             // row tiles that run side by side
+    int *err;
+};
+
+struct Tile {
+    int m0, n0, split, kb0, kb1;             // first row and column, k blocks [kb0, kb1)
+    __device__ __forceinline__ Tile(const Plan &p, int item) {
+        const int tiles = p.m_tiles * p.n_tiles;
+        split = item / tiles;
+        int i = item - split * tiles;
+        const int band = p.group_m * p.n_tiles, g = i / band;
+        i -= g * band;
+        const int height = min(p.group_m, p.m_tiles - g * p.group_m);
+        n0 = i / height * p.n_tile;
+        m0 = (g * p.group_m + i % height) * kTileM;
+        kb0 = (int)((int64_t)p.k_blocks * split / p.splits);
+        kb1 = (int)((int64_t)p.k_blocks * (split + 1) / p.splits);
+    }
+};
+
+// ---- what differs from one CTA's instructions ---------------------------------
+
+// a copy whose bytes are counted by a barrier of either CTA of the pair
+__device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, uint32_t bar, int x,
+                                         int y, int z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(tc::smem_u32(dst)),
+        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+__device__ __forceinline__ void remote_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ bool wait_cluster(uint64_t *bar, uint32_t parity) {
+    const long long start = clock64();
+    for (;;) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(tc::smem_u32(bar)), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if (clock64() - start > tc::kWaitLimitCycles) return false;
+    }
+}
+__device__ __forceinline__ void mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
+                                    uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// arrives on `bar` of both CTAs once this thread's products so far are done
+__device__ __forceinline__ void commit_both(uint64_t *bar) {
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
+        " [%0], %1;" ::"r"(tc::smem_u32(bar)),
+        "h"((uint16_t)3)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_alloc(uint32_t *dst, uint32_t ncols) {   // whole warp
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     tc::smem_u32(dst)),
+                 "r"(ncols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {   // whole warp
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols)
+                 : "memory");
+}
+
+// An MN-major operand: 64 columns of 64 k in 128-byte rows, swizzled; 8 k are
+// 1024 bytes apart (stride offset), the next 64 columns 8 KiB (leading offset).
+__device__ __forceinline__ uint64_t desc_mn(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(kGroupBytes >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+constexpr uint32_t kAColumns = 1u << 15, kBColumns = 1u << 16;   // idesc: MN-major
+
+// 32 columns of this thread's accumulator row
+__device__ __forceinline__ void load32(uint32_t taddr, float (&v)[32]) {
+    uint32_t r[32];
+    tc::tmem_ld32_nowait(taddr, r);
+    tc::tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        asm volatile("" : "+r"(r[i]));     // after the wait
+        v[i] = __uint_as_float(r[i]);
+    }
+}
+
+// Epi: epi(tile, row, tmem, plan) by the 128 threads of the epilogue, row =
+// the tile's row (0..255) of this thread, tmem = its accumulators' address.
+template <class Epi, bool A_MN, bool B_MN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    gemm_kernel(const __grid_constant__ CUtensorMap map_a,
+                const __grid_constant__ CUtensorMap map_b, Plan p, Epi epi) {
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drained;
+    __shared__ uint32_t tmem_base;
+    uint8_t *ring = raw + ((1024 - (tc::smem_u32(raw) & 1023)) & 1023);
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = tc::cluster_ctarank();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            tc::mbar_init(&full[s], 1);      // the first CTA's counts both CTAs' copies
+            tc::mbar_init(&empty[s], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            tc::mbar_init(&acc_full[i], 1);
+            tc::mbar_init(&acc_empty[i], 8);     // the epilogue warps of both CTAs
+        }
+        tc::mbar_init(&drained, 1);
+        tc::fence_mbar_init();
+        tc::prefetch_tensormap(&map_a);
+        tc::prefetch_tensormap(&map_b);
+    }
+    __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+    if (w == 1) tmem_alloc(&tmem_base, 512);
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::cluster_sync();                      // the peer's barriers and TMEM are there
+    tc::tc_fence_after();
+    const uint32_t tmem = tmem_base;
+    const int items = p.m_tiles * p.n_tiles * p.splits;
+    const int first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    bool ok = true;
+
+    if (w == 0) {
+        if (lane == 0) {
+            const uint32_t half = (uint32_t)p.n_tile / 2;
+            const uint32_t bytes = 2 * (kOperand + half * 128);
+            int s = 0, issued = 0;
+            uint32_t phase = 0;
+            for (int item = first; ok && item < items; item += step) {
+                const Tile t(p, item);
+                const int m0 = t.m0 + 128 * (int)rank, n0 = t.n0 + (int)(half * rank);
+                for (int q = 0; ok && q < p.pairs; ++q) {
+                    const int za = a_plane(p.pairs, q), zb = b_plane(p.pairs, q);
+                    for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                        if (!(ok = wait_cluster(&empty[s], phase ^ 1))) break;
+                        if (rank == 0) tc::mbar_arrive_expect_tx(&full[s], bytes);
+                        const uint32_t bar = tc::mapa_shared(tc::smem_u32(&full[s]), 0);
+                        uint8_t *a = ring + (size_t)s * kStage, *b = a + kOperand;
+                        if (A_MN) {
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+                                tma_load(a + j * kGroupBytes, &map_a, bar, m0 + 64 * j, kb * 64, za);
+                        } else {
+                            tma_load(a, &map_a, bar, kb * 64, m0, za);
+                        }
+                        if (B_MN) {
+                            for (uint32_t j = 0; j < half / 64; ++j)
+                                tma_load(b + j * kGroupBytes, &map_b, bar, n0 + 64 * (int)j,
+                                         kb * 64, zb);
+                        } else {
+                            tma_load(b, &map_b, bar, kb * 64, n0, zb);
+                        }
+                        ++issued;
+                        if (++s == kStages) {
+                            s = 0;
+                            phase ^= 1;
+                        }
+                    }
+                }
+            }
+            // the last products' arrivals at this CTA's barriers, before it may leave
+            for (int i = 0; ok && i < kStages && i < issued; ++i) {
+                if (--s < 0) {
+                    s = kStages - 1;
+                    phase ^= 1;
+                }
+                ok = wait_cluster(&empty[s], phase);
+            }
+            if (!ok) {
+                atomicOr(p.err, kErrTimeout);
+                // copies in flight end by themselves: give them far longer than they take
+                const long long start = clock64();
+                while (clock64() - start < 4000000ll) __nanosleep(1000);
+            }
+        }
+    } else if (w == 1) {
+        if (rank == 0 && lane == 0) {
+            const uint32_t idesc = tc::idesc_bf16_f32(kTileM, 0) | ((uint32_t)(p.n_tile >> 3) << 17) |
+                                   (A_MN ? kAColumns : 0u) | (B_MN ? kBColumns : 0u);
+            const uint32_t base = tc::smem_u32(ring);
+            const uint64_t a_desc = A_MN ? desc_mn(base) : tc::desc_k_sw128(base);
+            const uint64_t b_desc = B_MN ? desc_mn(base + kOperand) : tc::desc_k_sw128(base + kOperand);
+            // 16 k further: 16 rows of 128 bytes (MN-major), or 32 bytes along the rows
+            constexpr uint32_t a_step = (A_MN ? 16 * 128 : 32) >> 4;
+            constexpr uint32_t b_step = (B_MN ? 16 * 128 : 32) >> 4;
+            int s = 0;
+            uint32_t phase = 0, n = 0;
+            for (int item = first; ok && item < items; item += step, ++n) {
+                const Tile t(p, item);
+                const int buf = n & 1;
+                if (!(ok = wait_cluster(&acc_empty[buf], ((n >> 1) & 1) ^ 1))) break;
+                tc::tc_fence_after();
+                const uint32_t d = tmem + buf * 256;
+                const int blocks = (t.kb1 - t.kb0) * p.pairs;
+                for (int kb = 0; kb < blocks; ++kb) {
+                    if (!(ok = wait_cluster(&full[s], phase))) break;
+                    tc::tc_fence_after();
+                    const uint32_t at = (uint32_t)s * (kStage >> 4);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        mma(d, a_desc + at + k * a_step, b_desc + at + k * b_step, idesc,
+                            kb > 0 || k > 0);
+                    commit_both(&empty[s]);
+                    if (++s == kStages) {
+                        s = 0;
+                        phase ^= 1;
+                    }
+                }
+                if (ok) commit_both(&acc_full[buf]);
+            }
+            if (!ok) {       // products in flight end before anything is freed
+                atomicOr(p.err, kErrTimeout);
+                asm volatile(
+                    "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+                        tc::smem_u32(&drained))
+                    : "memory");
+                tc::mbar_wait(&drained, 0);
+            }
+        }
+    } else {
+        const int quarter = w & 3;
+        const int row = 128 * (int)rank + quarter * 32 + lane;
+        uint32_t n = 0;
+        for (int item = first; ok && item < items; item += step, ++n) {
+            const Tile t(p, item);
+            const int buf = n & 1;
+            ok = __all_sync(0xffffffffu, wait_cluster(&acc_full[buf], (n >> 1) & 1));
+            if (!ok) break;
+            tc::tc_fence_after();
+            epi(t, row, tmem + buf * 256 + ((uint32_t)(quarter * 32) << 16), p);
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) remote_arrive(tc::mapa_shared(tc::smem_u32(&acc_empty[buf]), 0));
+        }
+        if (!ok && lane == 0) atomicOr(p.err, kErrTimeout);
+    }
+    __syncwarp();
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::cluster_sync();                      // nothing of the peer's is in use any more
+    tc::tc_fence_after();
+    if (w == 1) tmem_dealloc(tmem, 512);
+}
+
+}  // namespace pair
+}  // namespace um
