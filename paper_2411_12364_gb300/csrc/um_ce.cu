@@ -321,7 +321,7 @@ pair::Plan plan_of(int64_t M, int64_t N, int64_t K, int planes, int step, int mo
     p.k_blocks = (int)ceil_div(K, 64);
     p.pairs = planes == 3 ? pair::kSplitPairs : 1;
     double best = 0;
-    for (int n = pair::kMaxN; n >= 128; n -= step) {
+    for (int n = planes == 3 ? pair::kExactN : pair::kMaxN; n >= 128; n -= step) {
         const int64_t nt = ceil_div(N, n);
         // a second share of a pair's time is the last that a split can save
         for (int s = 1; s <= most && s <= p.k_blocks; ++s) {
@@ -349,13 +349,13 @@ bool operand(CUtensorMap *map, const void *at, int64_t inner, int64_t rows, int6
     return paged::encode(map, at, inner, rows, planes, ld, plane, box, 1);
 }
 
-template <class Epi, bool A_MN, bool B_MN>
+template <class Epi, bool A_MN, bool B_MN, bool EXACT>
 cudaError_t multiply(const CUtensorMap &a, const CUtensorMap &b, const pair::Plan &p, const Epi &epi,
                      cudaStream_t st) {
-    cudaError_t e = allow_dynamic_smem<pair::gemm_kernel<Epi, A_MN, B_MN>>(pair::kSmem);
+    cudaError_t e = allow_dynamic_smem<pair::gemm_kernel<Epi, A_MN, B_MN, EXACT>>(pair::kSmem);
     if (e != cudaSuccess) return e;
     const int64_t items = (int64_t)p.m_tiles * p.n_tiles * p.splits, pairs = pairs_of_sms();
-    return launch_kernel(true, pair::gemm_kernel<Epi, A_MN, B_MN>,
+    return launch_kernel(true, pair::gemm_kernel<Epi, A_MN, B_MN, EXACT>,
                          dim3((unsigned)(2 * (items < pairs ? items : pairs))), pair::kThreads,
                          pair::kSmem, st, a, b, p, epi);
 }
@@ -529,7 +529,8 @@ cudaError_t forward(const ultramem_cross_entropy_args *p, const ForwardLayout &l
             return cudaErrorInvalidValue;
         epi.vn = (int)vn;
         epi.v0 = (int)v0;
-        e = multiply<LseEpi, false, false>(ma, mb, plan, epi, st);
+        e = P == 3 ? multiply<LseEpi, false, false, true>(ma, mb, plan, epi, st)
+                   : multiply<LseEpi, false, false, false>(ma, mb, plan, epi, st);
         epi.tile0 += plan.n_tiles;
         pdl = true;
     }
@@ -592,7 +593,7 @@ cudaError_t backward(const ultramem_cross_entropy_args *p, const BackwardLayout 
             return cudaErrorInvalidValue;
         ge.vn = (int)vn;
         ge.v0 = (int)v0;
-        e = multiply<GradEpi<P>, false, false>(ma, mb, plan, ge, st);
+        e = multiply<GradEpi<P>, false, false, P == 3>(ma, mb, plan, ge, st);
         pdl = true;
         if (dx && e == cudaSuccess) {            // [N][D] = G [N][vn] W [vn][D]
             plan = l.x_plan;
@@ -604,7 +605,7 @@ cudaError_t backward(const ultramem_cross_entropy_args *p, const BackwardLayout 
                 !operand(&mb, w.at, D, vn, w.ld, w.planes, w.plane, 64))
                 return cudaErrorInvalidValue;
             const StoreEpi<T> se = {static_cast<T *>(dx), dx_sum, N, D, v0 > 0, wide(dx)};
-            e = multiply<StoreEpi<T>, false, true>(ma, mb, plan, se, st);
+            e = multiply<StoreEpi<T>, false, true, P == 3>(ma, mb, plan, se, st);
         }
         if (dw && e == cudaSuccess) {            // [vn][D] = G^T [vn][N] x [N][D]
             plan = l.w_plan;
@@ -615,7 +616,7 @@ cudaError_t backward(const ultramem_cross_entropy_args *p, const BackwardLayout 
                 return cudaErrorInvalidValue;
             T *out = static_cast<T *>(dw) + v0 * D;
             const StoreEpi<T> se = {out, dw_sum, vn, D, 0, wide(out)};
-            e = multiply<StoreEpi<T>, true, true>(ma, mb, plan, se, st);
+            e = multiply<StoreEpi<T>, true, true, P == 3>(ma, mb, plan, se, st);
             if (dw_sum && e == cudaSuccess) e = sum_splits(dw_sum, l.dw_splits, vn * D, out);
         }
     }
