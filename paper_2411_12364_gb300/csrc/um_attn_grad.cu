@@ -82,7 +82,7 @@ template <typename T> __global__ void __launch_bounds__(256) prepare_kernel(Args
         if (lane == 0) {
             const float lse = a.lse[i];
             // weights e^(score - inf) = 0 for a row that saw nothing
-            a.rows[i] = make_float2(lse == -INFINITY ? INFINITY : lse, s);
+            a.rows[(int64_t)h * a.T + t] = make_float2(lse == -INFINITY ? INFINITY : lse, s);
         }
     }
 }
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Args a) {
         load_rows<T, DP>(h0, a.q, a.q_stride, (int64_t)head * a.D, first, kHeld, end, a.D);
         load_rows<T, DP>(h1, a.dout, a.dout_stride, (int64_t)head * a.D, first, kHeld, end, a.D);
         if (threadIdx.x < kHeld && first + threadIdx.x < end) {
-            const float2 r = a.rows[(first + threadIdx.x) * a.q_heads + head];
+            const float2 r = a.rows[(int64_t)head * a.T + first + threadIdx.x];
             lse[threadIdx.x] = r.x;
             di[threadIdx.x] = r.y;
         }
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Args a) {
                 load_rows<T, DP>(s1, a.dout, a.dout_stride, (int64_t)h * a.D, r0, kStream, end,
                                  a.D);
                 if (threadIdx.x < kStream && r0 + threadIdx.x < end) {
-                    const float2 r = a.rows[(r0 + threadIdx.x) * a.q_heads + h];
+                    const float2 r = a.rows[(int64_t)h * a.T + r0 + threadIdx.x];
                     lse[threadIdx.x] = r.x;
                     di[threadIdx.x] = r.y;
                 }
@@ -289,16 +289,20 @@ template <typename T> cudaError_t launch_prepare(const Args &a, cudaStream_t st)
 
 int block_of(int32_t dim) { return dim > 128 ? 32 : 64; }
 
+// Blocks of the sequences, at most: whole ones, and a short one for each that
+// has tokens.
+int64_t most_blocks(int32_t T, int32_t n_seqs, int block) {
+    return T / block + (n_seqs < T ? n_seqs : T);
+}
+
 struct Layout {
     int block, most;
     int64_t rows, blocks, count, total;
 };
-Layout layout_of(int32_t dtype, int32_t T, int32_t n_seqs, int32_t q_heads, int32_t dim) {
+Layout layout_of(int32_t T, int32_t n_seqs, int32_t q_heads, int32_t dim) {
     Layout l = {};
-    (void)dtype;
     l.block = block_of(dim);
-    // a sequence's last block may be short: no more of them than sequences or tokens
-    const int64_t most = T / l.block + (int64_t)(n_seqs < T ? n_seqs : T);
+    const int64_t most = most_blocks(T, n_seqs, l.block);
     l.most = (int)most;
     l.rows = 0;
     l.blocks = ((int64_t)T * q_heads * 8 + 15) & ~15ll;
@@ -314,8 +318,7 @@ bool heads_ok(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim) {
 }
 // what grids and offsets hold
 bool sizes_ok(int32_t T, int32_t n_seqs, int32_t q_heads, int32_t dim) {
-    return T >= 0 && n_seqs >= 0 &&
-           ((int64_t)T / block_of(dim) + (n_seqs < T ? n_seqs : T)) * q_heads <= INT32_MAX;
+    return T >= 0 && n_seqs >= 0 && most_blocks(T, n_seqs, block_of(dim)) * q_heads <= INT32_MAX;
 }
 
 }  // namespace
@@ -331,7 +334,7 @@ extern "C" int64_t ultramem_paged_attention_backward_workspace(int32_t dtype, in
     if (!heads_ok(dtype, q_heads, kv_heads, head_dim) ||
         !sizes_ok(n_tokens, n_seqs, q_heads, head_dim))
         return 0;
-    return layout_of(dtype, n_tokens, n_seqs, q_heads, head_dim).total;
+    return layout_of(n_tokens, n_seqs, q_heads, head_dim).total;
 }
 
 extern "C" ultramem_status ultramem_paged_attention_backward(const ultramem_attention_grad *p,
@@ -355,7 +358,7 @@ extern "C" ultramem_status ultramem_paged_attention_backward(const ultramem_atte
     if (p->q_stride < qr || p->out_stride < qr || p->dout_stride < qr || p->dq_stride < qr ||
         p->k_stride < kr || p->v_stride < kr || p->dk_stride < kr || p->dv_stride < kr)
         return ULTRAMEM_EINVAL;
-    const Layout l = layout_of(p->dtype, p->n_tokens, p->n_seqs, p->q_heads, p->head_dim);
+    const Layout l = layout_of(p->n_tokens, p->n_seqs, p->q_heads, p->head_dim);
     if (workspace_bytes < l.total) return ULTRAMEM_EINVAL;
     const int64_t T = p->n_tokens;
     auto rows_of = [&](const void *at, int64_t row, int64_t stride) {
@@ -416,7 +419,25 @@ extern "C" ultramem_status ultramem_paged_attention_backward(const ultramem_atte
     cudaStream_t st = (cudaStream_t)stream;
     cudaGetLastError();
     cudaError_t e;
-    if (p->dtype == ULTRAMEM_BF16) {
+    // TMA reads the inputs, and the outputs leave, in 16-byte pieces
+    const uintptr_t low = (uintptr_t)p->q | (uintptr_t)p->k | (uintptr_t)p->v | (uintptr_t)p->dout |
+                          (uintptr_t)p->dq | (uintptr_t)p->dk | (uintptr_t)p->dv |
+                          (uintptr_t)((p->q_stride | p->k_stride | p->v_stride | p->dout_stride |
+                                       p->dq_stride | p->dk_stride | p->dv_stride) * es);
+    if (p->dtype == ULTRAMEM_BF16 && p->head_dim <= 128 && low % 16 == 0) {
+        if (!(a.err = um::paged::error_word())) return ULTRAMEM_ENODEV;
+        a.block = kTensorBlock;
+        a.most = (int)most_blocks(p->n_tokens, p->n_seqs, kTensorBlock);
+        CUtensorMap q, k, v, dout;
+        auto map = [&](CUtensorMap *m, const void *x, int heads, int64_t stride) {
+            return um::paged::encode(m, x, a.D, heads, T, a.D, stride, 1, kTensorBlock);
+        };
+        if (!map(&q, a.q, a.q_heads, a.q_stride) || !map(&k, a.k, a.kv_heads, a.k_stride) ||
+            !map(&v, a.v, a.kv_heads, a.v_stride) || !map(&dout, a.dout, a.q_heads, a.dout_stride))
+            return um::status_from_cuda(cudaErrorInvalidValue);
+        e = launch_prepare<__nv_bfloat16>(a, st);
+        if (e == cudaSuccess) e = launch_tensor(a, q, k, v, dout, st);
+    } else if (p->dtype == ULTRAMEM_BF16) {
         e = launch_prepare<__nv_bfloat16>(a, st);
         if (e == cudaSuccess) e = rows_dim<__nv_bfloat16>(a, st);
     } else {

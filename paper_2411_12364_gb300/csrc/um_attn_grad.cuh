@@ -2,6 +2,8 @@
 // call's arguments and the list of tiles, shared by its kernels.
 #pragma once
 
+#include <cuda.h>
+
 #include "um_internal.cuh"
 
 namespace um {
@@ -10,19 +12,13 @@ namespace attn_grad {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxHeadDim = 256;
 
-// One block of a sequence's rows (keys or queries).
-struct Block {
-    int tok0, n;              // the sequence's first token and its tokens
-    int b;                    // the block's number in the sequence
-};
-
 struct Args {
     const void *q, *k, *v, *out, *dout;
     void *dq, *dk, *dv;
     const float *lse;
     const int32_t *q_start;
     int64_t q_stride, k_stride, v_stride, out_stride, dout_stride, dq_stride, dk_stride, dv_stride;
-    float2 *rows;             // [T][q_heads]: (lse in log2 units, +inf where it is -inf; d_i)
+    float2 *rows;             // [q_heads][T]: (lse, +inf where it is -inf; d_i)
     int4 *blocks;             // [most]: tok0, n, b of each block of `block` rows
     int *count;               // of them
     int *err;
@@ -31,6 +27,12 @@ struct Args {
     int most;                 // blocks that the list holds
     float scale, scale_log2;
 };
+
+// bf16, heads up to 128 wide (um_attn_grad_tc.cu): maps of boxes of 64 columns x
+// a head x 128 tokens over the inputs as [tokens][heads][width].
+constexpr int kTensorBlock = 128;
+cudaError_t launch_tensor(const Args &a, const CUtensorMap &q, const CUtensorMap &k,
+                          const CUtensorMap &v, const CUtensorMap &dout, cudaStream_t st);
 
 }  // namespace attn_grad
 }  // namespace um

@@ -33,12 +33,6 @@ constexpr float kLn2 = 0.6931471805599453f;
 // small part of its memory
 constexpr int64_t kPieceBytes = 512ll << 20;
 
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 struct Labels {
     const void *at;
     int wide, V;
@@ -138,8 +132,8 @@ struct LseEpi {
             const float shift = top == -INFINITY ? 0.f : top;
             float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < 32; ++k) s[k & 3] += ex2(z[k] - shift);
-            l = fmaf(l, ex2(m - shift), (s[0] + s[1]) + (s[2] + s[3]));
+            for (int k = 0; k < 32; ++k) s[k & 3] += tc::ex2(z[k] - shift);
+            l = fmaf(l, tc::ex2(m - shift), (s[0] + s[1]) + (s[2] + s[3]));
             m = top;
         }
         if (tok < T) part[(int64_t)(tile0 + t.n0 / p.n_tile) * T + tok] = make_float2(m, l);
@@ -156,7 +150,7 @@ __global__ void __launch_bounds__(1024)
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     auto add = [](float2 &a, float2 b) {
         const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.f : top;
-        a.y = a.y * ex2(a.x - shift) + b.y * ex2(b.x - shift);
+        a.y = a.y * tc::ex2(a.x - shift) + b.y * tc::ex2(b.x - shift);
         a.x = top;
     };
     for (int64_t t0 = (int64_t)blockIdx.x * 32; t0 < T; t0 += (int64_t)gridDim.x * 32) {
@@ -236,7 +230,7 @@ template <int P> struct GradEpi {
             if (!live) continue;
 #pragma unroll
             for (int k = 0; k < 32; ++k) {
-                float e = ex2(fmaf(z[k], scale_log2, shift));
+                float e = tc::ex2(fmaf(z[k], scale_log2, shift));
                 if (at == c + k) e -= 1.f;
                 z[k] = label >= 0 && c + k < cols ? e * d : 0.f;
             }

@@ -63,78 +63,12 @@ template <int DP> struct Cfg {
     static constexpr size_t kSmem = (size_t)kTile * 2 + (size_t)kStage * kStages + 1024;
 };
 
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0],"
-        " {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
-        "r"(r[15])
-        : "memory");
-}
 // 32 bytes, a whole sector, by one thread (dst 32-byte aligned)
 __device__ __forceinline__ void store32(void *dst, const uint32_t *r) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(r[0]),
                  "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
-// ties the values of a TMEM load to this point, after its wait
-__device__ __forceinline__ void arrived(uint32_t (&r)[32]) {
-#pragma unroll
-    for (int k = 0; k < 32; ++k) asm volatile("" : "+r"(r[k]));
-}
-__device__ __forceinline__ void tmem_st_wait() {
-    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-}
-
-// D += A B with A (the weights, 16-bit pairs along a row) in TMEM
-__device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc,
-                                            uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-
-// The values as the B operand: [key][64 columns] rows of 128 bytes, swizzled,
-// columns (N) contiguous: 8 keys are 1024 bytes apart (stride offset), the
-// next 64 columns a half (leading offset).
-__device__ __forceinline__ uint64_t desc_mn_sw128(uint32_t saddr) {
-    uint64_t d = 0;
-    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(kHalfBytes >> 4) << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
-constexpr uint32_t kBColumnsContiguous = 1u << 16;   // instruction descriptor: B is N-major
-
-__device__ __forceinline__ bool elect_one() {
-    uint32_t r;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "elect.sync _|p, 0xffffffff;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(r));
-    return r != 0;
-}
-// the same value in every lane, and known to be
-__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
-
-// a wait of a whole warp, with one answer for all lanes
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) {
-    return __all_sync(0xffffffffu, tc::mbar_wait(bar, parity));
-}
-
 // What each role needs of the tile at hand: blocks [j0, e[i]) of half i.
 struct Halves {
     int n_tok[2], e[2], end;
@@ -227,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int all_see = wk.pos0 + i * tq_half + 1;
             float m = -INFINITY, l = 0.f;
             for (int j = wk.j0; j < hv.e[i]; ++j) {
-                if (!warp_wait(&s_full[i], blocks & 1)) {
+                if (!tc::warp_wait(&s_full[i], blocks & 1)) {
                     ok = false;
                     break;
                 }
@@ -238,7 +172,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int c = 0; c < 4; ++c) tc::tmem_ld32_nowait(ts + 32 * c, s[c]);
                 tc::tmem_ld_wait();
 #pragma unroll
-                for (int c = 0; c < 4; ++c) arrived(s[c]);
+                for (int c = 0; c < 4; ++c) tc::arrived(s[c]);
                 if ((j + 1) * kKeys > all_see) {
                     const int left = limit - j * kKeys;
 #pragma unroll
@@ -259,7 +193,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool raise = (top - m) * a.scale_log2 > kRaise ||
                                    (m == -INFINITY && top > -INFINITY);
                 if (__any_sync(0xffffffffu, raise)) {
-                    const float f = raise ? ex2((m - top) * a.scale_log2) : 1.f;
+                    const float f = raise ? tc::ex2((m - top) * a.scale_log2) : 1.f;
                     if (raise) m = top;
                     l *= f;
                     if (j > wk.j0) {   // S_i is there, so all earlier products are done
@@ -273,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                                 asm volatile("" : "+f"(o[k]));   // after the load's wait
                                 x[k] = __float_as_uint(o[k] * f);
                             }
-                            tmem_st16(to + 16 * c, x);
+                            tc::tmem_st16(to + 16 * c, x);
                         }
                     }
                 }
@@ -287,24 +221,24 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const float2 y = split(fma2(f2(__uint_as_float(s[c][2 * k]),
                                                        __uint_as_float(s[c][2 * k + 1])),
                                                     scale, shift));
-                        const float e0 = ex2(y.x), e1 = ex2(y.y);
+                        const float e0 = tc::ex2(y.x), e1 = tc::ex2(y.y);
                         sum[k & 1] = sum[k & 1] + f2(e0, e1);
                         // weights as the A operand: one rounding to bf16, as
                         // large as that of the values; the sum keeps fp32
                         const __nv_bfloat162 b = __floats2bfloat162_rn(e0, e1);
                         p[k] = *reinterpret_cast<const uint32_t *>(&b);
                     }
-                    tmem_st16(ts + 16 * c, p);
+                    tc::tmem_st16(ts + 16 * c, p);
                 }
                 l += both(sum[0] + sum[1]);
-                tmem_st_wait();
+                tc::tmem_st_wait();
                 tc::tc_fence_before();
                 tc::mbar_arrive(&p_full[i]);
             }
             if (!ok) break;
             const bool any = hv.e[i] > wk.j0;
             if (any) {
-                if (!warp_wait(&o_full[i], tiles & 1)) {
+                if (!tc::warp_wait(&o_full[i], tiles & 1)) {
                     ok = false;
                     break;
                 }
@@ -332,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (any) {
                     tc::tmem_ld32_nowait(to + 32 * c, o);
                     tc::tmem_ld_wait();
-                    arrived(o);
+                    tc::arrived(o);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 32; ++k) o[k] = 0u;
@@ -382,13 +316,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         // left to themselves they may fall into step, and then their softmax
         // and their products collide (3090 instead of 2410 cycles a block) ----
         constexpr uint32_t idesc_s = tc::idesc_bf16_f32(128, kKeys);
-        constexpr uint32_t idesc_o = tc::idesc_bf16_f32(128, DP) | kBColumnsContiguous;
+        constexpr uint32_t idesc_o = tc::idesc_bf16_f32(128, DP) | tc::kBColumns;
         const int i = w == 8 ? 0 : 1;
-        const bool leader = elect_one();
+        const bool leader = tc::elect_one();
         const uint64_t q_desc = tc::desc_k_sw128(tc::smem_u32(qs + i * C::kTile));
         const uint64_t k_desc = tc::desc_k_sw128(tc::smem_u32(ring));
-        const uint64_t v_desc = desc_mn_sw128(tc::smem_u32(ring + (C::kPaired ? C::kTile : 0)));
-        const uint32_t t_s = uniform(tmem) + 128 * i, t_o = uniform(tmem) + 256 + DP * i;
+        const uint64_t v_desc = tc::desc_mn_sw128(tc::smem_u32(ring + (C::kPaired ? C::kTile : 0)), kHalfBytes);
+        const uint32_t t_s = tc::uniform(tmem) + 128 * i, t_o = tc::uniform(tmem) + 256 + DP * i;
         int stage = 0;
         uint32_t phase = 0, tiles = 0, p_phase = 0, turns = 0;
         auto advance = [&] {
@@ -416,17 +350,17 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (leader) {
 #pragma unroll
                 for (int k = 0; k < kKeys / 16; ++k)
-                    mma_bf16_ts(t_o, t_s + 8 * k, vd + k * (16 * 128 >> 4), idesc_o, add || k > 0);
+                    tc::mma_bf16_ts(t_o, t_s + 8 * k, vd + k * (16 * 128 >> 4), idesc_o, add || k > 0);
             }
         };
         while (ok && wk.next(a, kKeys)) {
             const Halves hv(wk, tq_half);
             if (!hv.live(wk)) continue;
-            const int j0 = uniform(wk.j0), end = uniform(hv.end);
-            const int e = uniform(i == 0 ? hv.e[0] : hv.e[1]);   // blocks past e: no products
-            if (!(ok = warp_wait(&q_full, tiles & 1))) break;
+            const int j0 = tc::uniform(wk.j0), end = tc::uniform(hv.end);
+            const int e = tc::uniform(i == 0 ? hv.e[0] : hv.e[1]);   // blocks past e: no products
+            if (!(ok = tc::warp_wait(&q_full, tiles & 1))) break;
             ++tiles;
-            if (!(ok = warp_wait(&kv_full[stage], phase))) break;
+            if (!(ok = tc::warp_wait(&kv_full[stage], phase))) break;
             tc::tc_fence_after();
             if (j0 < e) scores(stage);
             if constexpr (!C::kPaired) {
@@ -436,17 +370,17 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (j0 + 1 == end) commit(&q_empty);
             for (int j = j0; j < end; ++j) {
                 const int sv = stage;            // V of this block, then K of the next
-                if (!C::kPaired && !(ok = warp_wait(&kv_full[stage], phase))) break;
+                if (!C::kPaired && !(ok = tc::warp_wait(&kv_full[stage], phase))) break;
                 advance();
                 const bool more = j + 1 < end;
                 const int sk = stage;
-                if (more && !(ok = warp_wait(&kv_full[stage], phase))) break;
+                if (more && !(ok = tc::warp_wait(&kv_full[stage], phase))) break;
                 // half 0 goes first: it waits for half 1's turn before, half 1
                 // for half 0's at this block
-                if (!(ok = warp_wait(&turn[i ^ 1], (turns & 1) ^ (i == 0)))) break;
+                if (!(ok = tc::warp_wait(&turn[i ^ 1], (turns & 1) ^ (i == 0)))) break;
                 ++turns;
                 if (j < e) {
-                    if (!(ok = warp_wait(&p_full[i], p_phase))) break;
+                    if (!(ok = tc::warp_wait(&p_full[i], p_phase))) break;
                     p_phase ^= 1;
                     tc::tc_fence_after();
                     output(sv, j > j0);
@@ -465,7 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) {
             if (leader) atomicOr(a.err, kErrTimeout);
             commit(&drained[i]);               // products in flight end before TMEM is freed
-            warp_wait(&drained[i], 0);
+            tc::warp_wait(&drained[i], 0);
         }
     } else if (w == 9) {
         // ---- copies: the lanes read the table, one elected thread issues ----
@@ -474,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::prefetch_tensormap(&map_k);
             tc::prefetch_tensormap(&map_v);
         }
-        const bool leader = elect_one();
+        const bool leader = tc::elect_one();
         const int pages = kKeys / box_rows;
         const uint32_t q_bytes = (uint32_t)(tq_half * a.group) * 128 * C::kHalves;
         int stage = 0, issued = 0;
@@ -483,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const Halves hv(wk, tq_half);
             if (!hv.live(wk)) continue;
             const int tail = hv.tail(wk, page_mask);
-            if (!(ok = warp_wait(&q_empty, (tiles & 1) ^ 1))) break;
+            if (!(ok = tc::warp_wait(&q_empty, (tiles & 1) ^ 1))) break;
             ++tiles;
             if (lane == 0) {
                 const int n = hv.n_tok[1] ? 2 : 1;
@@ -505,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {   // K, then V
                     if (part == 0 || !C::kPaired) {
-                        if (!(ok = warp_wait(&kv_empty[stage], phase ^ 1))) break;
+                        if (!(ok = tc::warp_wait(&kv_empty[stage], phase ^ 1))) break;
                     }
                     uint64_t *bar = (part || C::kPaired) && j == tail ? &kv_raw[stage]
                                                                       : &kv_full[stage];
@@ -561,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int n = each * (hv.end - wk.j0);           // and of this tile
             if (tail >= 0) {
                 const int st = (stage + each * (tail - wk.j0) + each - 1) % C::kStages;
-                if (!(ok = warp_wait(&kv_raw[st], (raw_phase >> st) & 1))) break;
+                if (!(ok = tc::warp_wait(&kv_raw[st], (raw_phase >> st) & 1))) break;
                 raw_phase ^= 1u << st;
                 const int from = wk.kv - tail * kKeys;
                 const int to = min(kKeys, (from | page_mask) + 1);

@@ -137,29 +137,14 @@ __device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {  
                  : "memory");
 }
 
-// An MN-major operand: 64 columns of 64 k in 128-byte rows, swizzled; 8 k are
-// 1024 bytes apart (stride offset), the next 64 columns 8 KiB (leading offset).
-__device__ __forceinline__ uint64_t desc_mn(uint32_t saddr) {
-    uint64_t d = 0;
-    d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(kGroupBytes >> 4) << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
-constexpr uint32_t kAColumns = 1u << 15, kBColumns = 1u << 16;   // idesc: MN-major
-
 // 32 columns of this thread's accumulator row
 __device__ __forceinline__ void load32(uint32_t taddr, float (&v)[32]) {
     uint32_t r[32];
     tc::tmem_ld32_nowait(taddr, r);
     tc::tmem_ld_wait();
+    tc::arrived(r);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        asm volatile("" : "+r"(r[i]));     // after the wait
-        v[i] = __uint_as_float(r[i]);
-    }
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
 __device__ __forceinline__ void tmem_store32(uint32_t taddr, const float (&v)[32]) {
@@ -168,17 +153,8 @@ __device__ __forceinline__ void tmem_store32(uint32_t taddr, const float (&v)[32
         uint32_t r[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[16 * h + i]);
-        asm volatile(
-            "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0],"
-            " {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr + 16 * h),
-            "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-            "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
-            "r"(r[15])
-            : "memory");
+        tc::tmem_st16(taddr + 16 * h, r);
     }
-}
-__device__ __forceinline__ void tmem_store_wait() {
-    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
 // Epi: epi(tile, row, tmem, plan) by the 128 threads of the epilogue, row =
@@ -276,10 +252,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     } else if (w == 1) {
         if (rank == 0 && lane == 0) {
             const uint32_t idesc = tc::idesc_bf16_f32(kTileM, 0) | ((uint32_t)(p.n_tile >> 3) << 17) |
-                                   (A_MN ? kAColumns : 0u) | (B_MN ? kBColumns : 0u);
+                                   (A_MN ? tc::kAColumns : 0u) |
+                                   (B_MN ? tc::kBColumns : 0u);
             const uint32_t base = tc::smem_u32(ring);
-            const uint64_t a_desc = A_MN ? desc_mn(base) : tc::desc_k_sw128(base);
-            const uint64_t b_desc = B_MN ? desc_mn(base + kOperand) : tc::desc_k_sw128(base + kOperand);
+            const uint64_t a_desc = A_MN ? tc::desc_mn_sw128(base, kGroupBytes) : tc::desc_k_sw128(base);
+            const uint64_t b_desc = B_MN ? tc::desc_mn_sw128(base + kOperand, kGroupBytes)
+                                         : tc::desc_k_sw128(base + kOperand);
             // 16 k further: 16 rows of 128 bytes (MN-major), or 32 bytes along the rows
             constexpr uint32_t a_step = (A_MN ? 16 * 128 : 32) >> 4;
             constexpr uint32_t b_step = (B_MN ? 16 * 128 : 32) >> 4;
@@ -348,7 +326,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         }
                         tmem_store32(sum + c, v);
                     }
-                    tmem_store_wait();
+                    tc::tmem_st_wait();
                 } else {
                     epi(t, row, lanes + buf * kMaxN, p);
                 }
