@@ -24,9 +24,33 @@ namespace {
 
 // ---- preparation -------------------------------------------------------------
 
-// Block 0 lists the sequences' blocks; the others compute d_i, a warp a row
-// and head.
-template <typename T> __global__ void __launch_bounds__(256) prepare_kernel(Args a) {
+// 8 entries of a row from 16-byte (32-byte) pieces, or one by one
+template <typename T, bool WIDE> __device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
+    if constexpr (!WIDE) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = to_f(p[k]);
+    } else if constexpr (sizeof(T) == 4) {
+        const float4 x = reinterpret_cast<const float4 *>(p)[0];
+        const float4 y = reinterpret_cast<const float4 *>(p)[1];
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+        v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+    } else {
+        const uint4 x = *reinterpret_cast<const uint4 *>(p);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[2 * k] = __uint_as_float(w[k] << 16);
+            v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+        }
+    }
+}
+
+// Block 0 lists the sequences' blocks; the others compute d_i: 2^LANES lanes a
+// row and head, 8 entries each (a warp takes as many rows as fit, four times
+// over, so that enough loads are in flight; 4 x 4096 tokens x 16 heads x 128:
+// LATER us, bound by reading dout and out).
+template <typename T, bool WIDE> __global__ void __launch_bounds__(256)
+    prepare_kernel(Args a, int lanes_log2) {
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
@@ -69,20 +93,39 @@ template <typename T> __global__ void __launch_bounds__(256) prepare_kernel(Args
         if (threadIdx.x == 0) *a.count = min(total, a.most);
         return;
     }
-    const int64_t rows = (int64_t)a.T * a.q_heads, step = (int64_t)(gridDim.x - 1) * 8;
-    for (int64_t i = (int64_t)(blockIdx.x - 1) * 8 + w; i < rows; i += step) {
-        const int64_t t = i / a.q_heads;
-        const int h = (int)(i - t * a.q_heads);
-        const T *x = static_cast<const T *>(a.dout) + t * a.dout_stride + (int64_t)h * a.D;
-        const T *y = static_cast<const T *>(a.out) + t * a.out_stride + (int64_t)h * a.D;
-        float s = 0.f;
-        for (int c = lane; c < a.D; c += 32) s = fmaf(to_f(x[c]), to_f(y[c]), s);
+    constexpr int kAhead = 4;
+    const int per_row = 1 << lanes_log2, part = lane & (per_row - 1);
+    const int64_t rows = (int64_t)a.T * a.q_heads;
+    const int64_t per_warp = 32 >> lanes_log2, step = (int64_t)(gridDim.x - 1) * 8 * per_warp * kAhead;
+    const int64_t first = ((int64_t)(blockIdx.x - 1) * 8 + w) * per_warp * kAhead + (lane >> lanes_log2);
+    for (int64_t i0 = first; i0 - (lane >> lanes_log2) < rows; i0 += step) {
+        float x[kAhead][8], y[kAhead][8];
+        int64_t t[kAhead];
+        int h[kAhead];
 #pragma unroll
-        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane == 0) {
-            const float lse = a.lse[i];
-            // weights e^(score - inf) = 0 for a row that saw nothing
-            a.rows[(int64_t)h * a.T + t] = make_float2(lse == -INFINITY ? INFINITY : lse, s);
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t i = i0 + k * per_warp;
+            t[k] = i / a.q_heads;
+            h[k] = (int)(i - t[k] * a.q_heads);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) x[k][c] = y[k][c] = 0.f;
+            if (i < rows && part * 8 < a.D) {
+                const int64_t at = (int64_t)h[k] * a.D + part * 8;
+                load8<T, WIDE>(static_cast<const T *>(a.dout) + t[k] * a.dout_stride + at, x[k]);
+                load8<T, WIDE>(static_cast<const T *>(a.out) + t[k] * a.out_stride + at, y[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            float s = 0.f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) s = fmaf(x[k][c], y[k][c], s);
+            for (int o = per_row / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (part == 0 && i0 + k * per_warp < rows) {
+                const float lse = a.lse[i0 + k * per_warp];
+                // weights e^(score - inf) = 0 for a row that saw nothing
+                a.rows[(int64_t)h[k] * a.T + t[k]] = make_float2(lse == -INFINITY ? INFINITY : lse, s);
+            }
         }
     }
 }
@@ -281,9 +324,19 @@ template <typename T> cudaError_t rows_dim(const Args &a, cudaStream_t st) {
 }
 
 template <typename T> cudaError_t launch_prepare(const Args &a, cudaStream_t st) {
-    const int64_t rows = (int64_t)a.T * a.q_heads, want = (rows + 7) / 8;
+    int lanes = 0;                         // log2 of the lanes of a row: 8 entries each
+    while ((8 << lanes) < a.D) ++lanes;
+    const int64_t rows = (int64_t)a.T * a.q_heads, per_block = (8 * 4 * 32) >> lanes;
+    const int64_t want = (rows + per_block - 1) / per_block;
     const int64_t most = (int64_t)device_sm_count() * 8;
-    prepare_kernel<T><<<(unsigned)(1 + (want < most ? want : most)), 256, 0, st>>>(a);
+    const unsigned grid = (unsigned)(1 + (want < most ? want : most));
+    const bool wide =
+        ((uintptr_t)a.dout | (uintptr_t)a.out | (uintptr_t)((a.dout_stride | a.out_stride) * sizeof(T))) %
+            16 == 0;
+    if (wide)
+        prepare_kernel<T, true><<<grid, 256, 0, st>>>(a, lanes);
+    else
+        prepare_kernel<T, false><<<grid, 256, 0, st>>>(a, lanes);
     return cudaGetLastError();
 }
 

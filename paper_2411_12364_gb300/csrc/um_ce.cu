@@ -4,7 +4,7 @@
 // Forward: z = x W^T in 256 x n tiles on pairs of SMs (um_pair_gemm.cuh); the
 // epilogue leaves, for each token, the maximum and the sum of e^(z - maximum)
 // over the tile's columns (and the label's logit, in the tile that has it),
-// and a second kernel joins the tiles' pairs: T V / n values instead of T V.
+// and a second kernel joins the tiles' pairs.
 //
 // Gradient: the logits again, in pieces of the vocabulary; a piece's
 // G = scale dloss (e^(z - lse) - onehot) goes to the workspace in the storage
@@ -176,27 +176,30 @@ __global__ void __launch_bounds__(1024)
 
 // ---- gradient ------------------------------------------------------------------
 
-// 32 values to a row of T, from column c on; `wide`: the row allows 16 bytes
+// a whole sector by one thread (dst 32-byte aligned)
+__device__ __forceinline__ void store_sector(void *dst, const uint32_t (&r)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(r[0]),
+                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+// 32 values to a row of T, `left` of them there; `wide`: on 32-byte boundaries
 template <typename T>
 __device__ __forceinline__ void store32(T *to, const float (&v)[32], int left, bool wide) {
     if (wide && left >= 32) {
-        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                reinterpret_cast<float4 *>(to)[k] =
-                    make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
-        } else {
+        for (int k = 0; k < (int)sizeof(T); ++k) {
+            uint32_t o[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint32_t o[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (sizeof(T) == 4) {
+                    o[j] = __float_as_uint(v[8 * k + j]);
+                } else {
                     const __nv_bfloat162 b =
-                        __floats2bfloat162_rn(v[8 * k + 2 * j], v[8 * k + 2 * j + 1]);
+                        __floats2bfloat162_rn(v[16 * k + 2 * j], v[16 * k + 2 * j + 1]);
                     o[j] = *reinterpret_cast<const uint32_t *>(&b);
                 }
-                reinterpret_cast<uint4 *>(to)[k] = make_uint4(o[0], o[1], o[2], o[3]);
             }
+            store_sector(to + 32 / sizeof(T) * k, o);
         }
         return;
     }
@@ -229,11 +232,18 @@ template <int P> struct GradEpi {
             pair::load32(tmem + c, z);
             if (!live) continue;
 #pragma unroll
-            for (int k = 0; k < 32; ++k) {
-                float e = tc::ex2(fmaf(z[k], scale_log2, shift));
-                if (at == c + k) e -= 1.f;
-                z[k] = label >= 0 && c + k < cols ? e * d : 0.f;
+            for (int k = 0; k < 32; ++k) z[k] = tc::ex2(fmaf(z[k], scale_log2, shift));
+            if (at >= c && at < c + 32) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (at == c + k) z[k] -= 1.f;
             }
+            if (label < 0 || c + 32 > cols) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) z[k] = label >= 0 && c + k < cols ? z[k] : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 32; ++k) z[k] *= d;
             __nv_bfloat16 *to = g + tok * ld + t.n0 + c;
 #pragma unroll
             for (int q = 0; q < P; ++q) {
@@ -246,8 +256,8 @@ template <int P> struct GradEpi {
     }
 };
 
-// A product's rows [M][N]: to `out` in T, or, with `part`, in fp32 to
-// part [splits][M][N], added to what it holds when `add`.
+// A product's rows [M][N], with `add` on top of what part [splits][M][N] (fp32)
+// holds: to `out` in T, or without it back to part.
 template <typename T> struct StoreEpi {
     T *out;
     float *part;
@@ -263,32 +273,55 @@ template <typename T> struct StoreEpi {
             pair::load32(tmem + c, v);
             if (r >= M) continue;
             const int left = cols - c;
-            if (!part) {
-                store32(out + r * N + t.n0 + c, v, left, wide);
-                continue;
-            }
-            float *to = part + ((int64_t)t.split * M + r) * N + t.n0 + c;
-            if (add) {
+            float *sum = part + ((int64_t)t.split * M + r) * N + t.n0 + c;
+            if (add && left >= 32 && N % 4 == 0) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float4 x = reinterpret_cast<const float4 *>(sum)[k];
+                    v[4 * k] += x.x, v[4 * k + 1] += x.y, v[4 * k + 2] += x.z, v[4 * k + 3] += x.w;
+                }
+            } else if (add) {
 #pragma unroll
                 for (int k = 0; k < 32; ++k)
-                    if (k < left) v[k] += to[k];
+                    if (k < left) v[k] += sum[k];
             }
-            store32(to, v, left, N % 4 == 0);
+            if (out)
+                store32(out + r * N + t.n0 + c, v, left, wide);
+            else
+                store32(sum, v, left, N % 8 == 0);
         }
     }
 };
 
-// out = sum of part [splits][n] over the splits, in order
-template <typename T>
+// out = sum of part [splits][n] over the splits, in order; four values a thread
+// where n allows
+template <typename T, int N>
 __global__ void __launch_bounds__(256)
     sum_splits_kernel(const float *part, int splits, int64_t n, T *out) {
     pdl_wait();
     pdl_trigger();
-    const int64_t step = (int64_t)gridDim.x * blockDim.x;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += step) {
-        float s = part[i];
-        for (int k = 1; k < splits; ++k) s += part[k * n + i];
-        out[i] = from_f<T>(s);
+    const int64_t step = (int64_t)gridDim.x * blockDim.x * N;
+    for (int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * N; i < n; i += step) {
+        float s[N];
+#pragma unroll 4
+        for (int k = 0; k < splits; ++k) {
+            if constexpr (N == 4) {
+                const float4 x = *reinterpret_cast<const float4 *>(part + k * n + i);
+                const float v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[j] = k ? s[j] + v[j] : v[j];
+            } else {
+                s[0] = k ? s[0] + part[k * n + i] : part[k * n + i];
+            }
+        }
+        if constexpr (N == 4 && sizeof(T) == 4) {
+            *reinterpret_cast<float4 *>(out + i) = make_float4(s[0], s[1], s[2], s[3]);
+        } else if constexpr (N == 4) {
+            __nv_bfloat162 b[2] = {__floats2bfloat162_rn(s[0], s[1]), __floats2bfloat162_rn(s[2], s[3])};
+            *reinterpret_cast<uint2 *>(out + i) = *reinterpret_cast<const uint2 *>(b);
+        } else {
+            out[i] = from_f<T>(s[0]);
+        }
     }
 }
 
@@ -313,15 +346,15 @@ pair::Plan plan_of(int64_t M, int64_t N, int64_t K, int planes, int step, int mo
     const int64_t pairs = pairs_of_sms();
     p.m_tiles = (int)ceil_div(M, pair::kTileM);
     p.k_blocks = (int)ceil_div(K, 64);
-    p.pairs = planes == 3 ? pair::kSplitPairs : 1;
+    const int pairs_of_planes = planes == 3 ? 6 : 1;
     double best = 0;
-    for (int n = planes == 3 ? pair::kExactN : pair::kMaxN; n >= 128; n -= step) {
+    for (int n = planes == 3 ? pair::Shape<true>::kMaxN : pair::Shape<false>::kMaxN; n >= 128; n -= step) {
         const int64_t nt = ceil_div(N, n);
         // a second share of a pair's time is the last that a split can save
         for (int s = 1; s <= most && s <= p.k_blocks; ++s) {
             if (s > 1 && p.m_tiles * nt * (s - 1) >= 2 * pairs) break;
             const int64_t waves = ceil_div(p.m_tiles * nt * s, pairs);
-            const double tile = (double)ceil_div(p.k_blocks, s) * p.pairs * 2.0 * n + 3000.0;
+            const double tile = (double)ceil_div(p.k_blocks, s) * pairs_of_planes * 2.0 * n + 3000.0;
             // 2000 cycles and s writes and reads of the output at 3 KB a cycle
             const double join = s > 1 ? 2000.0 + (double)M * N * 8.0 * s / 3000.0 : 0.0;
             const double cost = waves * tile + join;
@@ -346,12 +379,12 @@ bool operand(CUtensorMap *map, const void *at, int64_t inner, int64_t rows, int6
 template <class Epi, bool A_MN, bool B_MN, bool EXACT>
 cudaError_t multiply(const CUtensorMap &a, const CUtensorMap &b, const pair::Plan &p, const Epi &epi,
                      cudaStream_t st) {
-    cudaError_t e = allow_dynamic_smem<pair::gemm_kernel<Epi, A_MN, B_MN, EXACT>>(pair::kSmem);
+    cudaError_t e = allow_dynamic_smem<pair::gemm_kernel<Epi, A_MN, B_MN, EXACT>>(pair::Shape<EXACT>::kSmem);
     if (e != cudaSuccess) return e;
     const int64_t items = (int64_t)p.m_tiles * p.n_tiles * p.splits, pairs = pairs_of_sms();
     return launch_kernel(true, pair::gemm_kernel<Epi, A_MN, B_MN, EXACT>,
                          dim3((unsigned)(2 * (items < pairs ? items : pairs))), pair::kThreads,
-                         pair::kSmem, st, a, b, p, epi);
+                         pair::Shape<EXACT>::kSmem, st, a, b, p, epi);
 }
 
 // Whether TMA reads a matrix where it lies.
@@ -563,12 +596,15 @@ cudaError_t backward(const ultramem_cross_entropy_args *p, const BackwardLayout 
     const bool dx_parts = l.dx_splits > 1 || l.piece < p->vocab;
     float *dx_sum = dx_parts ? reinterpret_cast<float *>(ws + l.dx) : nullptr;
     float *dw_sum = l.dw_splits > 1 ? reinterpret_cast<float *>(ws + l.dw) : nullptr;
-    auto wide = [&](const void *at) { return (uintptr_t)at % 16 == 0 && D * sizeof(T) % 16 == 0; };
+    auto wide = [&](const void *at) { return (uintptr_t)at % 32 == 0 && D * sizeof(T) % 32 == 0; };
     auto sum_splits = [&](const float *part, int splits, int64_t n, T *out) {
         const int64_t blocks = ceil_div(n, 1024), most = (int64_t)device_sm_count() * 16;
-        return launch_kernel(true, sum_splits_kernel<T>,
-                             dim3((unsigned)(blocks < most ? blocks : most)), 256, 0, st, part,
-                             splits, n, out);
+        const dim3 grid((unsigned)(blocks < most ? blocks : most));
+        return n % 4 == 0 && (uintptr_t)out % 16 == 0
+                   ? launch_kernel(true, sum_splits_kernel<T, 4>, grid, 256, 0, st, part,
+                                          splits, n, out)
+                          : launch_kernel(true, sum_splits_kernel<T, 1>, grid, 256, 0, st, part,
+                                          splits, n, out);
     };
     for (int64_t v0 = 0; v0 < p->vocab && e == cudaSuccess; v0 += l.piece) {
         const int64_t vn = p->vocab - v0 < l.piece ? p->vocab - v0 : l.piece;
@@ -598,7 +634,10 @@ cudaError_t backward(const ultramem_cross_entropy_args *p, const BackwardLayout 
             if (!operand(&ma, ge.g, vn, N, l.ld, P, N * l.ld, 128) ||
                 !operand(&mb, w.at, D, vn, w.ld, w.planes, w.plane, 64))
                 return cudaErrorInvalidValue;
-            const StoreEpi<T> se = {static_cast<T *>(dx), dx_sum, N, D, v0 > 0, wide(dx)};
+            // one split: the last piece adds the others' sums and writes dx itself
+            const bool here = l.dx_splits == 1 && v0 + vn == p->vocab;
+            const StoreEpi<T> se = {here ? static_cast<T *>(dx) : nullptr, dx_sum, N, D, v0 > 0,
+                                    wide(dx)};
             e = multiply<StoreEpi<T>, false, true, P == 3>(ma, mb, plan, se, st);
         }
         if (dw && e == cudaSuccess) {            // [vn][D] = G^T [vn][N] x [N][D]
@@ -609,12 +648,12 @@ cudaError_t backward(const ultramem_cross_entropy_args *p, const BackwardLayout 
                 !operand(&mb, x.at, D, N, x.ld, x.planes, x.plane, 64))
                 return cudaErrorInvalidValue;
             T *out = static_cast<T *>(dw) + v0 * D;
-            const StoreEpi<T> se = {out, dw_sum, vn, D, 0, wide(out)};
+            const StoreEpi<T> se = {dw_sum ? nullptr : out, dw_sum, vn, D, 0, wide(out)};
             e = multiply<StoreEpi<T>, true, true, P == 3>(ma, mb, plan, se, st);
             if (dw_sum && e == cudaSuccess) e = sum_splits(dw_sum, l.dw_splits, vn * D, out);
         }
     }
-    if (dx && dx_sum && e == cudaSuccess)
+    if (dx && l.dx_splits > 1 && e == cudaSuccess)
         e = sum_splits(dx_sum, l.dx_splits, N * D, static_cast<T *>(dx));
     return e;
 }

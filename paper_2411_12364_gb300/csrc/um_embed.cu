@@ -104,8 +104,7 @@ __global__ void __launch_bounds__(256)
 // A radix sort from the lowest digit, 8 bits or less at a time.  A block takes
 // kTile keys in order, a warp 32 x kRounds of them: a key's place among the
 // keys of its digit is the number of equal digits before it in its warp (by
-// matching the lanes of a round, and a counter a warp and digit from round to
-// round), in the warps before, and in the blocks before.
+// ballots in a round, and a counter a warp and digit from round to round), in the warps before, and in the blocks before.
 
 constexpr int kSortThreads = 1024;
 constexpr int kRounds = 16;
@@ -156,8 +155,14 @@ __device__ void sort_pass(const SortArgs &a, int p, int tile, bool hist, SortSha
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
         const bool live = first + r * 32 < a.T;
-        const uint32_t d = live ? ((uint32_t)key[r] >> shift) & mask : kDigits;
-        const uint32_t same = __match_any_sync(0xffffffffu, d);
+        const uint32_t d = ((uint32_t)key[r] >> shift) & mask;
+        // the lanes with this digit, a ballot a bit (a matching instruction took
+        // the single block 25 us a pass instead of LATER)
+        uint32_t same = __ballot_sync(0xffffffffu, live);
+        for (int b = 0; b < db; ++b) {
+            const uint32_t set = __ballot_sync(0xffffffffu, (d >> b) & 1u);
+            same &= (d >> b) & 1u ? set : ~set;
+        }
         const int before = live ? s.count[w][d] : 0;
         __syncwarp();
         if (live && lane == __ffs(same) - 1) s.count[w][d] = before + __popc(same);
@@ -311,57 +316,102 @@ __device__ __forceinline__ void write_row(const SumArgs &a, int id, int c, const
     store<O, N>(to, v);
 }
 
-// A block a chunk of the sorted tokens and blockDim x N columns.
+// values as they are loaded: 8 (16 or 32 bytes), or one
+template <typename T, int N> struct Raw {
+    uint4 x[N == 8 ? sizeof(T) / 2 : 1];
+    __device__ __forceinline__ void get(const T *p) {
+        if constexpr (N == 8) {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) x[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+        } else {
+            x[0].x = __float_as_uint(to_f(p[0]));
+        }
+    }
+    __device__ __forceinline__ void add_to(float (&s)[N]) const {
+        if constexpr (N == 1) {
+            s[0] += __uint_as_float(x[0].x);
+        } else {
+#pragma unroll
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+                const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if constexpr (sizeof(T) == 4) {
+                        s[4 * i + k] += __uint_as_float(w[k]);
+                    } else {
+                        s[2 * k] += __uint_as_float(w[k] << 16);
+                        s[2 * k + 1] += __uint_as_float(w[k] & 0xffff0000u);
+                    }
+                }
+            }
+        }
+    }
+};
+
+// A block a chunk of the sorted tokens and blockDim x N columns; the list in
+// steps of 32 tokens by way of shared memory, the rows 8 ahead, because
+// the time is that of the loads' latency (LATER).
 template <typename T, typename O, int N>
 __global__ void __launch_bounds__(256) sum_kernel(SumArgs a) {
+    constexpr int kList = 32, kAhead = 8;
+    __shared__ int key[kList + 1], tok[kList];
     pdl_wait();
     pdl_trigger();
     const int c = (blockIdx.y * blockDim.x + threadIdx.x) * N;
     const int lo = blockIdx.x * a.chunk;
     const int hi = (int)min((int64_t)a.T, (int64_t)lo + a.chunk);
-    if (c >= a.D) return;
+    const bool live = c < a.D;
     const T *dout = static_cast<const T *>(a.dout) + c;
     const bool joined = lo > 0 && a.key[lo - 1] == a.key[lo];
     float *part = a.part + (int64_t)blockIdx.x * 2 * a.D + c;
-    int start = lo;           // of the run at hand
+    bool head = true;         // the run at hand starts the chunk
     float sum[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) sum[k] = 0.f;
-    constexpr int kAhead = 4;
-    for (int64_t i0 = lo; i0 < hi; i0 += kAhead) {
-        float v[kAhead][N];
-        int id[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int i = (int)min(i0 + j, (int64_t)hi - 1);
-            id[j] = a.key[i];
-            load<T, N>(dout + (int64_t)a.tok[i] * a.ld, v[j]);
+    for (int64_t i0 = lo; i0 < hi; i0 += kList) {
+        const int n = (int)min((int64_t)kList, hi - i0);
+        __syncthreads();
+        if (threadIdx.x < kList) {
+            const int64_t i = i0 + threadIdx.x;
+            key[threadIdx.x] = i < a.T ? a.key[i] : -1;
+            tok[threadIdx.x] = a.tok[min(i, (int64_t)hi - 1)];
+            if (threadIdx.x == 0) key[kList] = i + kList < a.T ? a.key[i + kList] : -1;
         }
+        __syncthreads();
+        if (!live) continue;
+#pragma unroll 1
+        for (int j0 = 0; j0 < n; j0 += kAhead) {
+            Raw<T, N> v[kAhead];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (i0 + j >= hi) break;
-            const int i = (int)i0 + j;
+            for (int j = 0; j < kAhead; ++j) v[j].get(dout + (int64_t)tok[j0 + j] * a.ld);
 #pragma unroll
-            for (int k = 0; k < N; ++k) sum[k] += v[j][k];
-            const int next = i + 1 < a.T ? a.key[i + 1] : -1;
-            if (next == id[j] && i + 1 < hi) continue;
-            if (id[j] < a.vocab) {
-                if (start == lo && joined)
-                    store<float, N>(part, sum);             // goes on from the chunk before
-                else if (next == id[j])
-                    store<float, N>(part + a.D, sum);       // goes on in the next chunk
-                else
-                    write_row<O, N>(a, id[j], c, sum);
+            for (int j = 0; j < kAhead; ++j) {
+                if (j0 + j >= n) break;
+                v[j].add_to(sum);
+                const int id = key[j0 + j], next = key[j0 + j + 1];
+                const bool last = i0 + j0 + j + 1 == hi;
+                if (next == id && !last) continue;
+                if (id < a.vocab) {
+                    if (head && joined)
+                        store<float, N>(part, sum);             // goes on from the chunk before
+                    else if (next == id)
+                        store<float, N>(part + a.D, sum);       // goes on in the next chunk
+                    else
+                        write_row<O, N>(a, id, c, sum);
+                }
+                head = false;
+#pragma unroll
+                for (int k = 0; k < N; ++k) sum[k] = 0.f;
             }
-            start = i + 1;
-#pragma unroll
-            for (int k = 0; k < N; ++k) sum[k] = 0.f;
         }
     }
 }
 
-// Runs that start in chunk blockIdx.x and cross its end: their partial sums.
-template <typename O, int N> __global__ void __launch_bounds__(64) join_kernel(SumArgs a) {
+// Runs that start in chunk blockIdx.x and cross its end: their partial sums, in
+// the order of the chunks.  Four groups of 64 threads take a quarter of them
+// each, so that a frequent id takes a quarter of the steps.
+template <typename O, int N> __global__ void __launch_bounds__(256) join_kernel(SumArgs a) {
+    __shared__ float quarter[3][64][N];
     pdl_wait();
     pdl_trigger();
     const int end = (blockIdx.x + 1) * a.chunk;   // < T: the last chunk has none
@@ -370,8 +420,8 @@ template <typename O, int N> __global__ void __launch_bounds__(64) join_kernel(S
     const int lo = end - a.chunk;
     // all of this chunk, and what goes on from the chunk before: not its start
     if (a.key[lo] == id && lo > 0 && a.key[lo - 1] == id) return;
-    const int c = (blockIdx.y * blockDim.x + threadIdx.x) * N;
-    if (c >= a.D) return;
+    const int g = threadIdx.x >> 6, tid = threadIdx.x & 63;
+    const int c = (blockIdx.y * 64 + tid) * N;
     // chunks whose first key is still `id`: they are sorted, so a search finds the last
     int first = blockIdx.x + 1, last = a.chunks - 1;
     while (first < last) {
@@ -381,14 +431,29 @@ template <typename O, int N> __global__ void __launch_bounds__(64) join_kernel(S
         else
             last = m - 1;
     }
-    float sum[N], v[N];
-    load<float, N>(a.part + ((int64_t)blockIdx.x * 2 + 1) * a.D + c, sum);
-#pragma unroll 8
-    for (int i = blockIdx.x + 1; i <= last; ++i) {
-        load<float, N>(a.part + (int64_t)i * 2 * a.D + c, v);
+    // this chunk's part is its last run's (index 1), those of the others their first's
+    const int n = last - (int)blockIdx.x + 1, from = n * g / 4, to = n * (g + 1) / 4;
+    float sum[N];
 #pragma unroll
-        for (int k = 0; k < N; ++k) sum[k] += v[k];
+    for (int k = 0; k < N; ++k) sum[k] = 0.f;
+    if (c < a.D) {
+#pragma unroll 8
+        for (int i = from; i < to; ++i) {
+            float v[N];
+            load<float, N>(a.part + ((int64_t)(blockIdx.x + i) * 2 + (i == 0)) * a.D + c, v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) sum[k] += v[k];
+        }
+        if (g > 0)
+#pragma unroll
+            for (int k = 0; k < N; ++k) quarter[g - 1][tid][k] = sum[k];
     }
+    __syncthreads();
+    if (g > 0 || c >= a.D) return;
+#pragma unroll
+    for (int q = 0; q < 3; ++q)
+#pragma unroll
+        for (int k = 0; k < N; ++k) sum[k] += quarter[q][tid][k];
     write_row<O, N>(a, id, c, sum);
 }
 
@@ -432,7 +497,7 @@ cudaError_t sums(const SumArgs &a, cudaStream_t st) {
                                   dim3(a.chunks, (pieces + threads - 1) / threads), threads, 0, st,
                                   a);
     if (e == cudaSuccess && a.chunks > 1)
-        e = launch_kernel(true, join_kernel<O, N>, dim3(a.chunks - 1, (pieces + 63) / 64), 64, 0,
+        e = launch_kernel(true, join_kernel<O, N>, dim3(a.chunks - 1, (pieces + 63) / 64), 256, 0,
                           st, a);
     return e;
 }

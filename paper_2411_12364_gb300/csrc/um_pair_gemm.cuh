@@ -13,17 +13,18 @@
 //
 // Each operand is K-major (rows of A or B, k contiguous) or MN-major (rows of
 // k, the row index of A or B contiguous), so that a matrix and its transpose
-// are read from the same memory.  An operand may be given as up to three
-// planes that add up to it (fp32 values as three bf16 terms): the k loop then
-// runs over pairs of planes, smallest products first.
+// are read from the same memory.
 //
-// The tensor cores cut off what a sum loses in its last place, so a sum of n
-// steps of 16 k may be n units of 2^-24 short.  That is far below a
-// rounding to bf16 but not below fp32: with EXACT a sum in the tensor cores ends
-// after 4 k blocks (16 steps), and the epilogue adds it to the tile's sum
-// (rounded to nearest), which it keeps in TMEM beside the two accumulators; tiles
-// are then 128 columns wide.  (Gradient of 333 tokens against 5003 x 509 in
-// fp32: relative error 3e-6 without, 4e-7 with it, 107 and 146 us.)
+// EXACT: operands of fp32 values, each three bf16 planes that add up to it.  A
+// k block's three planes of A and of B are copied once and multiplied in
+// the six pairs that reach 2^-24 of the product, the smallest first.  The
+// tensor cores cut off what a sum loses in its last place, so a sum of n
+// steps of 16 k may be n units of 2^-24 short.  That is far below a rounding to
+// bf16 but not below fp32: the sum in the tensor cores ends after a k block
+// (24 steps), and the epilogue adds it to the tile's sum (rounded to
+// nearest), which it keeps in TMEM beside the two accumulators.  (Gradient of
+// 333 tokens against 5003 x 509: relative error 3e-6 with one sum a tile, 4e-7
+// so; LATER us.)
 //
 // Warps of a CTA: 0 copies (TMA, one elected thread), 1 products (one thread
 // of the pair's first CTA), 2-5 epilogue.  Waits are bounded; one that gives
@@ -37,27 +38,22 @@ namespace um {
 namespace pair {
 
 constexpr int kThreads = 192;
-constexpr int kTileM = 256, kMaxN = 256;
-constexpr int kStages = 6;
+constexpr int kTileM = 256;
 constexpr uint32_t kOperand = 128 * 128;                  // 128 rows (or columns) x 64 k
-constexpr uint32_t kStage = 2 * kOperand;
-constexpr size_t kSmem = (size_t)kStages * kStage + 1024;
 constexpr uint32_t kGroupBytes = 64 * 128;                // MN-major: 64 columns x 64 k
 
-// Pairs of planes in the order that they are added: the smallest first.
-constexpr int kSplitPairs = 6;
-__device__ __forceinline__ int a_plane(int pairs, int i) {
-    return pairs == 1 ? 0 : (0x001012 >> (4 * (5 - i))) & 15;
-}
-__device__ __forceinline__ int b_plane(int pairs, int i) {
-    return pairs == 1 ? 0 : (0x010210 >> (4 * (5 - i))) & 15;
-}
-
-constexpr int kExactN = 128, kExactBlocks = 4;
+template <bool EXACT> struct Shape {
+    static constexpr int kMaxN = EXACT ? 128 : 256;
+    static constexpr int kPlanes = EXACT ? 3 : 1;
+    static constexpr int kStages = EXACT ? 3 : 6;
+    static constexpr uint32_t kB = kOperand * kMaxN / 256;        // a CTA's half of the columns
+    static constexpr uint32_t kStage = kPlanes * (kOperand + kB);
+    static constexpr size_t kSmem = (size_t)kStages * kStage + 1024;
+};
 
 struct Plan {
     int m_tiles, n_tiles, n_tile, splits;    // splits: of the k blocks, a tile each
-    int k_blocks, pairs;                     // k blocks of a plane, pairs of planes
+    int k_blocks;
     int group_m;                             // row tiles that run side by side
     int *err;
 };
@@ -163,6 +159,8 @@ template <class Epi, bool A_MN, bool B_MN, bool EXACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap map_a,
                 const __grid_constant__ CUtensorMap map_b, Plan p, Epi epi) {
+    using S = Shape<EXACT>;
+    constexpr int kStages = S::kStages;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drained;
     __shared__ uint32_t tmem_base;
@@ -199,38 +197,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     if (w == 0) {
         if (lane == 0) {
             const uint32_t half = (uint32_t)p.n_tile / 2;
-            const uint32_t bytes = 2 * (kOperand + half * 128);
+            const uint32_t bytes = 2 * S::kPlanes * (kOperand + half * 128);
             int s = 0, issued = 0;
             uint32_t phase = 0;
             for (int item = first; ok && item < items; item += step) {
                 const Tile t(p, item);
                 const int m0 = t.m0 + 128 * (int)rank, n0 = t.n0 + (int)(half * rank);
-                for (int q = 0; ok && q < p.pairs; ++q) {
-                    const int za = a_plane(p.pairs, q), zb = b_plane(p.pairs, q);
-                    for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                        if (!(ok = wait_cluster(&empty[s], phase ^ 1))) break;
-                        if (rank == 0) tc::mbar_arrive_expect_tx(&full[s], bytes);
-                        const uint32_t bar = tc::mapa_shared(tc::smem_u32(&full[s]), 0);
-                        uint8_t *a = ring + (size_t)s * kStage, *b = a + kOperand;
+                for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                    if (!(ok = wait_cluster(&empty[s], phase ^ 1))) break;
+                    if (rank == 0) tc::mbar_arrive_expect_tx(&full[s], bytes);
+                    const uint32_t bar = tc::mapa_shared(tc::smem_u32(&full[s]), 0);
+                    uint8_t *at = ring + (size_t)s * S::kStage;
+#pragma unroll
+                    for (int z = 0; z < S::kPlanes; ++z) {
+                        uint8_t *a = at + z * kOperand;
+                        uint8_t *b = at + S::kPlanes * kOperand + z * S::kB;
                         if (A_MN) {
 #pragma unroll
                             for (int j = 0; j < 2; ++j)
-                                tma_load(a + j * kGroupBytes, &map_a, bar, m0 + 64 * j, kb * 64, za);
+                                tma_load(a + j * kGroupBytes, &map_a, bar, m0 + 64 * j, kb * 64, z);
                         } else {
-                            tma_load(a, &map_a, bar, kb * 64, m0, za);
+                            tma_load(a, &map_a, bar, kb * 64, m0, z);
                         }
                         if (B_MN) {
                             for (uint32_t j = 0; j < half / 64; ++j)
                                 tma_load(b + j * kGroupBytes, &map_b, bar, n0 + 64 * (int)j,
-                                         kb * 64, zb);
+                                         kb * 64, z);
                         } else {
-                            tma_load(b, &map_b, bar, kb * 64, n0, zb);
+                            tma_load(b, &map_b, bar, kb * 64, n0, z);
                         }
-                        ++issued;
-                        if (++s == kStages) {
-                            s = 0;
-                            phase ^= 1;
-                        }
+                    }
+                    ++issued;
+                    if (++s == kStages) {
+                        s = 0;
+                        phase ^= 1;
                     }
                 }
             }
@@ -256,8 +256,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                                    (B_MN ? tc::kBColumns : 0u);
             const uint32_t base = tc::smem_u32(ring);
             const uint64_t a_desc = A_MN ? tc::desc_mn_sw128(base, kGroupBytes) : tc::desc_k_sw128(base);
-            const uint64_t b_desc = B_MN ? tc::desc_mn_sw128(base + kOperand, kGroupBytes)
-                                         : tc::desc_k_sw128(base + kOperand);
+            constexpr uint32_t b_at = S::kPlanes * kOperand;
+            const uint64_t b_desc = B_MN ? tc::desc_mn_sw128(base + b_at, kGroupBytes)
+                                         : tc::desc_k_sw128(base + b_at);
             // 16 k further: 16 rows of 128 bytes (MN-major), or 32 bytes along the rows
             constexpr uint32_t a_step = (A_MN ? 16 * 128 : 32) >> 4;
             constexpr uint32_t b_step = (B_MN ? 16 * 128 : 32) >> 4;
@@ -265,22 +266,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             uint32_t phase = 0, n = 0;
             for (int item = first; ok && item < items; item += step) {
                 const Tile t(p, item);
-                const int blocks = (t.kb1 - t.kb0) * p.pairs;
-                const int most = EXACT ? kExactBlocks : blocks;      // of a sum
+                const int blocks = t.kb1 - t.kb0, most = EXACT ? 1 : blocks;   // of a sum
                 for (int b0 = 0; ok && b0 < blocks; b0 += most, ++n) {
                     const int buf = n & 1;
                     if (!(ok = wait_cluster(&acc_empty[buf], ((n >> 1) & 1) ^ 1))) break;
                     tc::tc_fence_after();
-                    const uint32_t d = tmem + buf * (EXACT ? kExactN : kMaxN);
-                    const int b1 = min(blocks, b0 + most);
-                    for (int kb = b0; kb < b1; ++kb) {
+                    const uint32_t d = tmem + buf * S::kMaxN;
+                    for (int kb = b0; kb < b0 + most; ++kb) {
                         if (!(ok = wait_cluster(&full[s], phase))) break;
                         tc::tc_fence_after();
-                        const uint32_t at = (uint32_t)s * (kStage >> 4);
+                        const uint32_t at = (uint32_t)s * (S::kStage >> 4);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            mma(d, a_desc + at + k * a_step, b_desc + at + k * b_step, idesc,
-                                kb > b0 || k > 0);
+                        for (int i = 0; i < (EXACT ? 6 : 1); ++i) {
+                            // pairs of planes: the smallest products first
+                            constexpr int plane_a[6] = {2, 1, 0, 1, 0, 0};
+                            constexpr int plane_b[6] = {0, 1, 2, 0, 1, 0};
+                            const uint32_t pa = EXACT ? plane_a[i] * (kOperand >> 4) : 0;
+                            const uint32_t pb = EXACT ? plane_b[i] * (S::kB >> 4) : 0;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                mma(d, a_desc + at + pa + k * a_step, b_desc + at + pb + k * b_step,
+                                    idesc, kb > b0 || i > 0 || k > 0);
+                        }
                         commit_both(&empty[s]);
                         if (++s == kStages) {
                             s = 0;
@@ -306,15 +313,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         uint32_t n = 0;
         for (int item = first; ok && item < items; item += step) {
             const Tile t(p, item);
-            const int blocks = (t.kb1 - t.kb0) * p.pairs;
-            const int sums = EXACT ? (blocks + kExactBlocks - 1) / kExactBlocks : 1;
+            const int sums = EXACT ? t.kb1 - t.kb0 : 1;
             for (int i = 0; i < sums; ++i, ++n) {
                 const int buf = n & 1;
                 ok = __all_sync(0xffffffffu, wait_cluster(&acc_full[buf], (n >> 1) & 1));
                 if (!ok) break;
                 tc::tc_fence_after();
                 if constexpr (EXACT) {
-                    const uint32_t from = lanes + buf * kExactN, sum = lanes + 2 * kExactN;
+                    const uint32_t from = lanes + buf * S::kMaxN, sum = lanes + 2 * S::kMaxN;
                     for (int c = 0; c < p.n_tile; c += 32) {
                         float v[32];
                         load32(from + c, v);
@@ -328,13 +334,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     }
                     tc::tmem_st_wait();
                 } else {
-                    epi(t, row, lanes + buf * kMaxN, p);
+                    epi(t, row, lanes + buf * S::kMaxN, p);
                 }
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) remote_arrive(tc::mapa_shared(tc::smem_u32(&acc_empty[buf]), 0));
             }
-            if (EXACT && ok) epi(t, row, lanes + 2 * kExactN, p);
+            if (EXACT && ok) epi(t, row, lanes + 2 * S::kMaxN, p);
         }
         if (!ok && lane == 0) atomicOr(p.err, kErrTimeout);
     }
