@@ -102,11 +102,19 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256)
         float x[kAhead][8], y[kAhead][8];
         int64_t t[kAhead];
         int h[kAhead];
+        t[0] = i0 / a.q_heads;
+        h[0] = (int)(i0 - t[0] * a.q_heads);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const int64_t i = i0 + k * per_warp;
-            t[k] = i / a.q_heads;
-            h[k] = (int)(i - t[k] * a.q_heads);
+            if (k > 0) {
+                t[k] = t[k - 1];
+                h[k] = h[k - 1] + (int)per_warp;
+                while (h[k] >= a.q_heads) {
+                    h[k] -= a.q_heads;
+                    ++t[k];
+                }
+            }
 #pragma unroll
             for (int c = 0; c < 8; ++c) x[k][c] = y[k][c] = 0.f;
             if (i < rows && part * 8 < a.D) {

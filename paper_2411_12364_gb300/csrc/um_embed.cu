@@ -13,6 +13,7 @@
 #include "um_device.cuh"
 #include "um_internal.cuh"
 #include "um_overlap.cuh"
+#include "um_tc.cuh"
 
 namespace um {
 namespace embed {
@@ -102,14 +103,15 @@ __global__ void __launch_bounds__(256)
 
 // ---- the tokens sorted by id -------------------------------------------------
 // A radix sort from the lowest digit, 8 bits or less at a time.  A block takes
-// kTile keys in order, a warp 32 x kRounds of them: a key's place among the
+// kTile keys in order, a warp 32 x kRounds of them at most: a key's place among the
 // keys of its digit is the number of equal digits before it in its warp (by
 // ballots in a round, and a counter a warp and digit from round to round), in the warps before, and in the blocks before.
 
 constexpr int kSortThreads = 1024;
-constexpr int kRounds = 16;
+constexpr int kRounds = 4;
 constexpr int kTile = kSortThreads * kRounds;
 constexpr int kDigits = 256;
+constexpr int kCluster = 8;               // blocks that sort together
 constexpr int kWarps = kSortThreads / 32;
 
 struct SortArgs {
@@ -117,6 +119,7 @@ struct SortArgs {
     int *key[2], *tok[2];     // [T], in turns
     int *hist;                // [tiles][kDigits] of a pass
     int T, vocab, wide, bits, passes, tiles;
+    int tile;                 // keys of a tile, at most kTile
 };
 
 __host__ __device__ __forceinline__ int pass_bits(int bits, int passes) {
@@ -132,82 +135,135 @@ __device__ __forceinline__ int key_at(const SortArgs &a, int p, int i) {
 
 struct SortShared {
     int count[kWarps][kDigits];
-    int base[kDigits];
-    int scan[kDigits / 32];
+    int first[kDigits];       // of a digit's keys in the tile's order
+    int move[kDigits];        // from there to their place among all tiles' keys
+    int scan[2][kDigits / 32];
+    int part[2][kSortThreads / kDigits][kDigits];
+    int key[kTile], tok[kTile];          // the tile in order
 };
 
-// Pass p of tile `tile`; with `hist` its digits' counts of all tiles are known.
-__device__ void sort_pass(const SortArgs &a, int p, int tile, bool hist, SortShared &s) {
+// The exclusive sum of `v` over threads 0..kDigits - 1, two block barriers.
+__device__ __forceinline__ int digits_before(int v, int *scan) {
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    int upto = v;
+    if (threadIdx.x < kDigits) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        if (lane == 31) scan[w] = upto;
+    }
+    __syncthreads();
+    int at = upto - v;
+    if (threadIdx.x < kDigits)
+        for (int i = 0; i < w; ++i) at += scan[i];
+    return at;
+}
+
+// Ranks of the keys among the equal digits before them in their warp, whose
+// counts are left in count[warp]; a warp holds 32 x rounds keys in order.
+__device__ __forceinline__ void rank_keys(const int (&key)[kRounds], int (&rank)[kRounds], int rounds,
+                                          int mine, int n, int shift, int db,
+                                          int (&count)[kDigits]) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t mask = (1u << db) - 1u;
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        if (r >= rounds) break;
+        const bool live = mine + r * 32 < n;
+        const uint32_t d = ((uint32_t)key[r] >> shift) & mask;
+        // the lanes with this digit, a ballot a bit
+        uint32_t same = __ballot_sync(0xffffffffu, live);
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {
+            if (b >= db) break;
+            const bool set = d & (1u << b);
+            const uint32_t lanes = __ballot_sync(0xffffffffu, set);
+            same &= set ? lanes : ~lanes;
+        }
+        const int before = live ? count[d] : 0;
+        __syncwarp();
+        if (live && lane == __ffs(same) - 1) count[d] = before + __popc(same);
+        __syncwarp();
+        rank[r] = before + __popc(same & ((1u << lane) - 1u));
+    }
+}
+// Thread d < kDigits: the warps' counts of digit d become their sums before a
+// warp; returns the block's count.
+__device__ __forceinline__ int sum_warps(int (&count)[kWarps][kDigits]) {
+    int here = 0;
+    for (int i = 0; i < kWarps; ++i) {
+        const int c = count[i][threadIdx.x];
+        count[i][threadIdx.x] = here;
+        here += c;
+    }
+    return here;
+}
+
+// Pass p of tile `tile`, whose digits' counts are in hist with those of the
+// others.  The keys go to their places by way of shared memory, because a
+// warp's 32 keys scatter over as many sectors.
+__device__ __forceinline__ void sort_pass(const SortArgs &a, int p, int tile, SortShared &s) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const int db = pass_bits(a.bits, a.passes), shift = p * db;
     const uint32_t mask = (1u << db) - 1u;
     for (int i = tid; i < kWarps * kDigits; i += kSortThreads) (&s.count[0][0])[i] = 0;
-    __syncthreads();
     int *key_to = p & 1 ? a.key[1] : a.key[0], *tok_to = p & 1 ? a.tok[1] : a.tok[0];
     const int *tok_from = p & 1 ? a.tok[0] : a.tok[1];
+    const int64_t start = (int64_t)tile * a.tile;
+    const int n = (int)min((int64_t)a.tile, a.T - start);
+    const int rounds = a.tile / kSortThreads;
     int key[kRounds], rank[kRounds];
-    const int64_t first = (int64_t)tile * kTile + w * 32 * kRounds + lane;
+    const int mine = w * 32 * rounds + lane;
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
-        const int64_t i = first + r * 32;
-        key[r] = i < a.T ? key_at(a, p, (int)i) : -1;
-    }
-#pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-        const bool live = first + r * 32 < a.T;
-        const uint32_t d = ((uint32_t)key[r] >> shift) & mask;
-        // the lanes with this digit, a ballot a bit (a matching instruction took
-        // the single block 25 us a pass instead of LATER)
-        uint32_t same = __ballot_sync(0xffffffffu, live);
-        for (int b = 0; b < db; ++b) {
-            const uint32_t set = __ballot_sync(0xffffffffu, (d >> b) & 1u);
-            same &= (d >> b) & 1u ? set : ~set;
-        }
-        const int before = live ? s.count[w][d] : 0;
-        __syncwarp();
-        if (live && lane == __ffs(same) - 1) s.count[w][d] = before + __popc(same);
-        __syncwarp();
-        rank[r] = before + __popc(same & ((1u << lane) - 1u));
+        const int i = mine + r * 32;
+        key[r] = r < rounds && i < n ? key_at(a, p, (int)(start + i)) : -1;
     }
     __syncthreads();
-    int total = 0, at = 0;
-    if (tid < kDigits) {
-        for (int i = 0; i < kWarps; ++i) {
-            const int c = s.count[i][tid];
-            s.count[i][tid] = total;
-            total += c;
+    rank_keys(key, rank, rounds, mine, n, shift, db, s.count[w]);
+    __syncthreads();
+    int here = 0, all = 0, tiles_before = 0;
+    if (tid < kDigits) here = sum_warps(s.count);
+    {   // four threads a digit share the tiles
+        int c_all = 0, c_before = 0;
+        const int d = tid & (kDigits - 1);
+#pragma unroll 8
+        for (int i = tid / kDigits; i < a.tiles; i += 4) {
+            const int c = a.hist[(int64_t)i * kDigits + d];
+            if (i < tile) c_before += c;
+            c_all += c;
         }
-        if (hist) {
-            total = 0;
-            for (int i = 0; i < a.tiles; ++i) {
-                const int c = a.hist[(int64_t)i * kDigits + tid];
-                if (i < tile) at += c;
-                total += c;
+        s.part[0][tid / kDigits][d] = c_all;
+        s.part[1][tid / kDigits][d] = c_before;
+        __syncthreads();
+        if (tid < kDigits)
+            for (int i = 0; i < 4; ++i) {
+                all += s.part[0][i][tid];
+                tiles_before += s.part[1][i][tid];
             }
-        }
-        int upto = total;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += v;
-        }
-        if (lane == 31) s.scan[w] = upto;
-        at += upto - total;
     }
-    __syncthreads();
+    const int first = digits_before(here, s.scan[0]), global = digits_before(all, s.scan[1]);
     if (tid < kDigits) {
-        for (int i = 0; i < w; ++i) at += s.scan[i];
-        s.base[tid] = at;
+        s.first[tid] = first;
+        s.move[tid] = global + tiles_before - first;
     }
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
-        const int64_t i = first + r * 32;
-        if (i >= a.T) continue;
+        const int i = mine + r * 32;
+        if (r >= rounds || i >= n) continue;
         const uint32_t d = ((uint32_t)key[r] >> shift) & mask;
-        const int to = s.base[d] + s.count[w][d] + rank[r];
-        key_to[to] = key[r];
-        tok_to[to] = p > 0 ? tok_from[i] : (int)i;
+        const int to = s.first[d] + s.count[w][d] + rank[r];
+        s.key[to] = key[r];
+        s.tok[to] = p > 0 ? tok_from[start + i] : (int)(start + i);
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += kSortThreads) {
+        const int k = s.key[i], to = i + s.move[((uint32_t)k >> shift) & mask];
+        key_to[to] = k;
+        tok_to[to] = s.tok[i];
     }
 }
 
@@ -239,19 +295,90 @@ __device__ __forceinline__ void fill(const FillArgs &f, int part, int parts, int
     fill_zeros(body + lo, hi - lo, f.at + f.bytes - tail, tail, block, blocks);
 }
 
-// The whole sort of at most kTile tokens by block 0; the others zero dtable.
-__global__ void __launch_bounds__(kSortThreads) sort_small_kernel(SortArgs a, FillArgs f) {
-    __shared__ SortShared s;
-    pdl_wait();
+// Zeros over dtable by one block an SM, all resident at once, so that the sort
+// starts beside it (inside the sort's launch, whose blocks hold 80 KB of shared
+// memory, 200 MB took 43 us instead of 34).
+__global__ void __launch_bounds__(1024) fill_kernel(FillArgs f) {
     pdl_trigger();
-    if (blockIdx.x == 0) {
-        for (int p = 0; p < a.passes; ++p) {
-            sort_pass(a, p, 0, false, s);
-            __syncthreads();
+    fill(f, 0, 1, blockIdx.x, gridDim.x);
+}
+
+// The whole sort of at most kCluster tiles by a cluster: block b holds places
+// b * tile .. of the list in its shared memory, and the blocks send their
+// digits' counts and their keys to one another's, so that the sort does not
+// wait for a memory that the fill keeps busy.  (By a single block the sort of
+// 16384 tokens took 18 us a pass, bound by issuing its 80000 instructions; by
+// a cluster by way of global memory 7 us alone and 15 beside the fill; LATER so.)
+// It reads and writes nothing of the fill's and runs beside it; it ends after
+// it, and so what follows finds both done.
+struct ClusterShared {
+    int count[kWarps][kDigits];
+    int counts[kCluster][kDigits];       // of the blocks
+    int base[kDigits];                   // of a digit's keys of this block in the list
+    int scan[kDigits / 32];
+    int key[2][kTile], tok[2][kTile];    // this block's places, before and after a pass
+};
+__device__ __forceinline__ void store_peer(int *at, int rank, int v) {
+    const uint32_t to = tc::mapa_shared(tc::smem_u32(at), (uint32_t)rank);
+    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(to), "r"(v) : "memory");
+}
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kSortThreads)
+    sort_small_kernel(SortArgs a) {
+    extern __shared__ __align__(16) uint8_t raw[];
+    ClusterShared &s = *reinterpret_cast<ClusterShared *>(raw);
+    pdl_trigger();
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5, block = blockIdx.x;
+    const int db = pass_bits(a.bits, a.passes);
+    const uint32_t mask = (1u << db) - 1u;
+    const int start = block * a.tile, n = max(0, min(a.tile, a.T - start));
+    const int rounds = a.tile / kSortThreads, mine = w * 32 * rounds + lane;
+    tc::cluster_sync();                  // the peers have started
+    for (int p = 0; p < a.passes; ++p) {
+        const int shift = p * db;
+        for (int i = tid; i < kWarps * kDigits; i += kSortThreads) (&s.count[0][0])[i] = 0;
+        int key[kRounds], tok[kRounds], rank[kRounds];
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int i = mine + r * 32;
+            const bool live = r < rounds && i < n;
+            key[r] = !live ? -1 : p ? s.key[p & 1][i] : key_at(a, 0, start + i);
+            tok[r] = !live ? 0 : p ? s.tok[p & 1][i] : start + i;
         }
-    } else {
-        fill(f, 0, 1, blockIdx.x - 1, gridDim.x - 1);
+        __syncthreads();
+        rank_keys(key, rank, rounds, mine, n, shift, db, s.count[w]);
+        __syncthreads();
+        if (tid < kDigits) {
+            const int here = sum_warps(s.count);
+            for (int i = 0; i < kCluster; ++i) store_peer(&s.counts[block][tid], i, here);
+        }
+        tc::cluster_sync();
+        int all = 0, before = 0;
+        if (tid < kDigits)
+            for (int i = 0; i < kCluster; ++i) {
+                const int c = s.counts[i][tid];
+                if (i < block) before += c;
+                all += c;
+            }
+        const int first = digits_before(all, s.scan);
+        if (tid < kDigits) s.base[tid] = first + before;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            if (r >= rounds || mine + r * 32 >= n) continue;
+            const uint32_t d = ((uint32_t)key[r] >> shift) & mask;
+            const int to = s.base[d] + s.count[w][d] + rank[r];
+            const int peer = to / a.tile, at = to - peer * a.tile;
+            store_peer(&s.key[(p + 1) & 1][at], peer, key[r]);
+            store_peer(&s.tok[(p + 1) & 1][at], peer, tok[r]);
+        }
+        tc::cluster_sync();
     }
+    const int last = a.passes & 1;
+    for (int i = tid; i < n; i += kSortThreads) {
+        a.key[0][start + i] = s.key[last][i];
+        a.tok[0][start + i] = s.tok[last][i];
+    }
+    pdl_wait();
 }
 
 // Digit counts of pass p, a block a tile; blocks past them zero a part of dtable.
@@ -270,7 +397,7 @@ __global__ void __launch_bounds__(kSortThreads)
     __syncthreads();
 #pragma unroll 4
     for (int r = 0; r < kRounds; ++r) {
-        const int64_t i = (int64_t)tile * kTile + r * kSortThreads + threadIdx.x;
+        const int64_t i = (int64_t)tile * a.tile + r * kSortThreads + threadIdx.x;
         if (i < a.T)
             atomicAdd(&count[((uint32_t)key_at(a, p, (int)i) >> (p * db)) & ((1u << db) - 1u)], 1);
     }
@@ -280,11 +407,12 @@ __global__ void __launch_bounds__(kSortThreads)
 
 __global__ void __launch_bounds__(kSortThreads)
     sort_place_kernel(SortArgs a, int p, FillArgs f, int part, int parts) {
-    __shared__ SortShared s;
+    extern __shared__ __align__(16) uint8_t raw[];
+    SortShared &s = *reinterpret_cast<SortShared *>(raw);
     pdl_wait();
     pdl_trigger();
     if ((int)blockIdx.x < a.tiles)
-        sort_pass(a, p, blockIdx.x, true, s);
+        sort_pass(a, p, blockIdx.x, s);
     else
         fill(f, part, parts, blockIdx.x - a.tiles, gridDim.x - a.tiles);
 }
@@ -348,46 +476,48 @@ template <typename T, int N> struct Raw {
     }
 };
 
-// A block a chunk of the sorted tokens and blockDim x N columns; the list in
-// steps of 32 tokens by way of shared memory, the rows 8 ahead, because
-// the time is that of the loads' latency (LATER).
+// blockDim.x x N columns of blockDim.y chunks of the sorted tokens; the list in
+// steps of 32 tokens by way of shared memory, the rows two sets ahead,
+// because the time is that of the loads' latency.
 template <typename T, typename O, int N>
-__global__ void __launch_bounds__(256) sum_kernel(SumArgs a) {
-    constexpr int kList = 32, kAhead = 8;
-    __shared__ int key[kList + 1], tok[kList];
+__global__ void __launch_bounds__(256, sizeof(T) == 4 ? 2 : 4) sum_kernel(SumArgs a) {
+    constexpr int kList = 32, kAhead = 4;
+    __shared__ int keys[32][kList + 1], toks[32][kList];
     pdl_wait();
     pdl_trigger();
+    int *key = keys[threadIdx.y], *tok = toks[threadIdx.y];
     const int c = (blockIdx.y * blockDim.x + threadIdx.x) * N;
-    const int lo = blockIdx.x * a.chunk;
+    const int64_t chunk = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const int lo = (int)min((int64_t)a.T, chunk * a.chunk);
     const int hi = (int)min((int64_t)a.T, (int64_t)lo + a.chunk);
     const bool live = c < a.D;
     const T *dout = static_cast<const T *>(a.dout) + c;
-    const bool joined = lo > 0 && a.key[lo - 1] == a.key[lo];
-    float *part = a.part + (int64_t)blockIdx.x * 2 * a.D + c;
+    const bool joined = lo > 0 && lo < hi && a.key[lo - 1] == a.key[lo];
+    float *part = a.part + chunk * 2 * a.D + c;
     bool head = true;         // the run at hand starts the chunk
     float sum[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) sum[k] = 0.f;
-    for (int64_t i0 = lo; i0 < hi; i0 += kList) {
-        const int n = (int)min((int64_t)kList, hi - i0);
+    for (int64_t i0 = lo; i0 < (int64_t)lo + a.chunk; i0 += kList) {    // as often in all rows
+        const int n = (int)max((int64_t)0, min((int64_t)kList, hi - i0));
         __syncthreads();
-        if (threadIdx.x < kList) {
-            const int64_t i = i0 + threadIdx.x;
-            key[threadIdx.x] = i < a.T ? a.key[i] : -1;
-            tok[threadIdx.x] = a.tok[min(i, (int64_t)hi - 1)];
-            if (threadIdx.x == 0) key[kList] = i + kList < a.T ? a.key[i + kList] : -1;
+        for (int k = threadIdx.x; k <= kList; k += blockDim.x) {
+            const int64_t i = i0 + k;
+            key[k] = i < a.T ? a.key[i] : -1;
+            if (k < kList) tok[k] = hi > lo ? a.tok[min(i, (int64_t)hi - 1)] : 0;
         }
         __syncthreads();
-        if (!live) continue;
-#pragma unroll 1
-        for (int j0 = 0; j0 < n; j0 += kAhead) {
-            Raw<T, N> v[kAhead];
+        if (!live || n == 0) continue;
+        Raw<T, N> v[2][kAhead];
+        auto fetch = [&](Raw<T, N> (&to)[kAhead], int j0) {
 #pragma unroll
-            for (int j = 0; j < kAhead; ++j) v[j].get(dout + (int64_t)tok[j0 + j] * a.ld);
+            for (int j = 0; j < kAhead; ++j) to[j].get(dout + (int64_t)tok[j0 + j] * a.ld);
+        };
+        auto add = [&](const Raw<T, N> (&from)[kAhead], int j0) {
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 if (j0 + j >= n) break;
-                v[j].add_to(sum);
+                from[j].add_to(sum);
                 const int id = key[j0 + j], next = key[j0 + j + 1];
                 const bool last = i0 + j0 + j + 1 == hi;
                 if (next == id && !last) continue;
@@ -403,6 +533,14 @@ __global__ void __launch_bounds__(256) sum_kernel(SumArgs a) {
 #pragma unroll
                 for (int k = 0; k < N; ++k) sum[k] = 0.f;
             }
+        };
+        fetch(v[0], 0);
+#pragma unroll 1
+        for (int j0 = 0; j0 < n; j0 += 2 * kAhead) {
+            if (j0 + kAhead < n) fetch(v[1], j0 + kAhead);
+            add(v[0], j0);
+            if (j0 + 2 * kAhead < n) fetch(v[0], j0 + 2 * kAhead);
+            add(v[1], j0 + kAhead);
         }
     }
 }
@@ -422,14 +560,13 @@ template <typename O, int N> __global__ void __launch_bounds__(256) join_kernel(
     if (a.key[lo] == id && lo > 0 && a.key[lo - 1] == id) return;
     const int g = threadIdx.x >> 6, tid = threadIdx.x & 63;
     const int c = (blockIdx.y * 64 + tid) * N;
-    // chunks whose first key is still `id`: they are sorted, so a search finds the last
-    int first = blockIdx.x + 1, last = a.chunks - 1;
-    while (first < last) {
-        const int m = (first + last + 1) >> 1;
-        if (a.key[(int64_t)m * a.chunk] == id)
-            first = m;
-        else
-            last = m - 1;
+    // the last chunk whose first key is still `id`, 256 chunks at a look
+    int last = blockIdx.x;
+    for (;;) {
+        const int64_t m = (int64_t)last + 1 + threadIdx.x;
+        const int more = __syncthreads_count(m < a.chunks && a.key[m * a.chunk] == id);
+        last += more;
+        if (more < 256) break;
     }
     // this chunk's part is its last run's (index 1), those of the others their first's
     const int n = last - (int)blockIdx.x + 1, from = n * g / 4, to = n * (g + 1) / 4;
@@ -459,22 +596,28 @@ template <typename O, int N> __global__ void __launch_bounds__(256) join_kernel(
 
 // ---- launches ------------------------------------------------------------------
 
-// Tokens of a chunk: at least 32, and at most 4096 chunks, so that the partial
-// sums of an id that fills the batch are joined in as many steps.
+// Tokens of a chunk: 32, fewer in a short batch (512 chunks and more occupy the
+// GPU), and at most 8192 chunks, so that the partial sums of an id that fills the
+// batch are joined in a quarter as many steps.
 int chunk_of(int T) {
-    const int c = (int)(((int64_t)T + 4095) / 4096);
-    return c < 32 ? 32 : c;
+    const int most = (int)(((int64_t)T + 8191) / 8192), few = T / 512;
+    const int c = few < 8 ? 8 : few < 32 ? few : 32;
+    return c < most ? most : c;
 }
 
 struct Layout {
-    int chunk, chunks, tiles;
+    int chunk, chunks, tile, tiles;
     int64_t key[2], tok[2], hist, part, total;
 };
 Layout layout_of(int T, int D) {
     Layout l = {};
     l.chunk = chunk_of(T);
     l.chunks = (T + l.chunk - 1) / l.chunk;
-    l.tiles = (int)(((int64_t)T + kTile - 1) / kTile);
+    // up to a cluster's tiles: as many as it has blocks, of whole rounds
+    const int64_t least = ((int64_t)T + kCluster - 1) / kCluster;
+    const int64_t rounds = (least + kSortThreads - 1) / kSortThreads;
+    l.tile = kSortThreads * (int)(rounds < 1 ? 1 : rounds < kRounds ? rounds : kRounds);
+    l.tiles = (int)(((int64_t)T + l.tile - 1) / l.tile);
     const int64_t keys = ((int64_t)T * 4 + 15) & ~15ll;
     int64_t at = 0;
     for (int i = 0; i < 2; ++i) {
@@ -492,10 +635,11 @@ Layout layout_of(int T, int D) {
 template <typename T, typename O, int N>
 cudaError_t sums(const SumArgs &a, cudaStream_t st) {
     const int pieces = a.D / N;
-    const int threads = pieces >= 256 ? 256 : (pieces + 31) / 32 * 32;
+    // 256 threads a block: columns, and as many chunks as fit beside them (32 at most)
+    const int x = pieces >= 256 ? 256 : (pieces + 7) / 8 * 8, y = 256 / x;
     cudaError_t e = launch_kernel(true, sum_kernel<T, O, N>,
-                                  dim3(a.chunks, (pieces + threads - 1) / threads), threads, 0, st,
-                                  a);
+                                  dim3((a.chunks + y - 1) / y, (pieces + x - 1) / x), dim3(x, y), 0,
+                                  st, a);
     if (e == cudaSuccess && a.chunks > 1)
         e = launch_kernel(true, join_kernel<O, N>, dim3(a.chunks - 1, (pieces + 63) / 64), 256, 0,
                           st, a);
@@ -596,30 +740,38 @@ extern "C" ultramem_status ultramem_embedding_backward(
     s.vocab = vocab;
     s.wide = ids_bytes == 8;
     s.tiles = l.tiles;
+    s.tile = l.tile;
     while ((vocab >> s.bits) != 0) ++s.bits;   // keys 0..vocab
     s.passes = (s.bits + 7) / 8;
     const FillArgs f = {accumulate ? nullptr : static_cast<uint8_t *>(dtable), out_bytes};
     // blocks that zero dtable beside the sorting ones
     const int64_t want = (out_bytes + 65535) / 65536;
-    const int spare = accumulate ? 0 : (int)(want < um::device_sm_count() ? want
-                                                                          : um::device_sm_count());
+    const int spare =
+        accumulate ? 0 : (int)(want < um::device_sm_count() ? want : um::device_sm_count());
     cudaError_t e = cudaSuccess;
-    if (l.tiles == 1) {
-        e = um::launch_kernel(false, sort_small_kernel, dim3(1 + spare), kSortThreads, 0, st, s, f);
+    if (l.tiles <= kCluster) {
+        e = um::allow_dynamic_smem<sort_small_kernel>(sizeof(ClusterShared));
+        if (e == cudaSuccess && !accumulate)
+            e = um::launch_kernel(false, fill_kernel, dim3(spare), 1024, 0, st, f);
+        if (e == cudaSuccess)
+            e = um::launch_kernel(!accumulate, sort_small_kernel, dim3(kCluster), kSortThreads,
+                                  sizeof(ClusterShared), st, s);
     } else {
         const int parts = 2 * s.passes;
+        e = um::allow_dynamic_smem<sort_place_kernel>(sizeof(SortShared));
         for (int p = 0; p < s.passes && e == cudaSuccess; ++p) {
             e = um::launch_kernel(p > 0, sort_count_kernel, dim3(l.tiles + spare), kSortThreads, 0,
                                   st, s, p, f, 2 * p, parts);
             if (e == cudaSuccess)
                 e = um::launch_kernel(true, sort_place_kernel, dim3(l.tiles + spare), kSortThreads,
-                                      0, st, s, p, f, 2 * p + 1, parts);
+                                      sizeof(SortShared), st, s, p, f, 2 * p + 1, parts);
         }
     }
     if (e != cudaSuccess) return um::status_from_cuda(e);
     SumArgs a = {};
-    a.key = s.key[(s.passes - 1) & 1];
-    a.tok = s.tok[(s.passes - 1) & 1];
+    const int at = l.tiles <= kCluster ? 0 : (s.passes - 1) & 1;
+    a.key = s.key[at];
+    a.tok = s.tok[at];
     a.dout = dout;
     a.ld = ld_dout;
     a.dtable = dtable;
