@@ -20,11 +20,15 @@
 // under dV_j and S_{j+1}.  Narrow heads and held rows leave room in TMEM for a
 // second block of scores, issued one block ahead.
 //
-// Warps: 0-7 P and dS (a thread a held row, four warps for each half of the
-// streamed columns) and the output, 8 products, 9 copies (TMA), 10 the streamed rows'
-// lse and d, and zeros over what a last block holds past the sequence (weight
-// 0 times anything there must stay 0).
+// Warps: 0-15 P and dS (a thread a held row, four warps for each quarter of the
+// streamed columns) and the output, 16 products, 17 copies (TMA), 18 the streamed
+// rows' lse and d, and zeros over what a last block holds past the sequence
+// (weight 0 times anything there must stay 0).  P and dS are a chain of loads
+// from TMEM, exponentials, stores and barriers; eight warps for them took
+// 2500 cycles a block, waiting for one another's latencies.
 #include "um_attn_grad.cuh"
+
+#include <type_traits>
 
 #include "um_device.cuh"
 #include "um_pair.cuh"
@@ -34,7 +38,8 @@ namespace um {
 namespace attn_grad {
 namespace {
 
-constexpr int kThreads = 384;
+constexpr int kSoftmax = 16;                     // warps that make P and dS
+constexpr int kThreads = (kSoftmax + 4) * 32;
 constexpr int kRows = 128;                       // held, and streamed at a time
 constexpr uint32_t kHalfBytes = 128 * 128;       // 128 rows x 64 columns of bf16
 
@@ -129,16 +134,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&bar.s_full[i], 1);
             tc::mbar_init(&bar.row_full[i], 32);
-            tc::mbar_init(&bar.row_empty[i], 8);
+            tc::mbar_init(&bar.row_empty[i], kSoftmax);
         }
         tc::mbar_init(&bar.dp_full, 1);
-        tc::mbar_init(&bar.p_full, 8);
-        tc::mbar_init(&bar.ds_full, 8);
+        tc::mbar_init(&bar.p_full, kSoftmax);
+        tc::mbar_init(&bar.ds_full, kSoftmax);
         tc::mbar_init(&bar.out_full, 1);
         tc::mbar_init(&bar.drained, 1);
         tc::fence_mbar_init();
     }
-    if (w == 8) tc::tmem_alloc(&bar.tmem, 512);
+    if (w == kSoftmax) tc::tmem_alloc(&bar.tmem, 512);
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
@@ -147,8 +152,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t t_dp = 128 * C::kScores, t_o0 = t_dp + 128, t_o1 = t_o0 + (KEYS ? DP : 0);
     bool ok = true;
 
-    if (w < 8) {
-        const int part = w >> 2, row = (w & 3) * 32 + lane;    // half of the columns, held row
+    if (w < kSoftmax) {
+        const int part = w >> 2, row = (w & 3) * 32 + lane;    // quarter of the columns, held row
         const uint32_t lanes = tmem + ((uint32_t)((w & 3) * 32) << 16);
         const int held = wk.b * kRows + row;                   // in the sequence
         const F2 scale = f2(a.scale_log2);
@@ -160,99 +165,84 @@ __global__ void __launch_bounds__(kThreads, 1)
             own_d = f2(-r.y);
         }
         uint32_t s_phase = 0;                                  // a bit a block of scores
-        for (int j = 0; j < steps; ++j) {
+        // A block's P and dS; MASKED: the diagonal block, whose rows see the keys
+        // up to their own, and a short last one.
+        auto block = [&](auto masked, int j) {
+            constexpr bool MASKED = decltype(masked)::value;
             const int sb = j % C::kScores, st = j & 1;
-            const int str0 = wk.block<KEYS>(j) * kRows + 64 * part;   // the first streamed column
-            // rows see the keys up to their own; the last block may be short
-            const bool masked = wk.block<KEYS>(j) == wk.b || wk.tail(wk.block<KEYS>(j));
-            const float *lse = row_lse + st * kRows + 64 * part, *d = row_d + st * kRows + 64 * part;
-            if (KEYS && !(ok = tc::warp_wait(&bar.row_full[st], (j >> 1) & 1))) break;
-            if (!(ok = tc::warp_wait(&bar.s_full[sb], (s_phase >> sb) & 1))) break;
+            const int str0 = wk.block<KEYS>(j) * kRows + 32 * part;   // the first streamed column
+            const float *lse = row_lse + st * kRows + 32 * part, *d = row_d + st * kRows + 32 * part;
+            auto sees = [&](int k) {
+                const int at = str0 + k;
+                return KEYS ? held <= at && at < wk.n : at <= held;
+            };
+            if (KEYS && !tc::warp_wait(&bar.row_full[st], (j >> 1) & 1)) return false;
+            if (!tc::warp_wait(&bar.s_full[sb], (s_phase >> sb) & 1)) return false;
             s_phase ^= 1u << sb;
             tc::tc_fence_after();
-            const uint32_t ts = lanes + 128 * sb + 64 * part, tdp = lanes + t_dp + 64 * part;
-            uint32_t s[2][32];
-            tc::tmem_ld32_nowait(ts, s[0]);
-            tc::tmem_ld32_nowait(ts + 32, s[1]);
+            const uint32_t ts = lanes + 128 * sb + 32 * part, tdp = lanes + t_dp + 32 * part;
+            uint32_t s[32], p[16];
+            tc::tmem_ld32_nowait(ts, s);
             tc::tmem_ld_wait();
-            tc::arrived(s[0]);
-            tc::arrived(s[1]);
+            tc::arrived(s);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t p[16];
-#pragma unroll
-                for (int k = 0; k < 32; k += 4) {
-                    F2 l0 = own_lse, l1 = own_lse;
-                    if (KEYS) {
-                        const float4 v = *reinterpret_cast<const float4 *>(lse + 32 * c + k);
-                        l0 = f2(v.x, v.y);
-                        l1 = f2(v.z, v.w);
-                    }
-                    const float2 y0 = split(fma2(
-                        f2(__uint_as_float(s[c][k]), __uint_as_float(s[c][k + 1])), scale, l0));
-                    const float2 y1 = split(fma2(
-                        f2(__uint_as_float(s[c][k + 2]), __uint_as_float(s[c][k + 3])), scale, l1));
-                    float e[4] = {tc::ex2(y0.x), tc::ex2(y0.y), tc::ex2(y1.x), tc::ex2(y1.y)};
-                    if (masked) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int at = str0 + 32 * c + k + i;
-                            const bool sees = KEYS ? held <= at && at < wk.n : at <= held;
-                            e[i] = sees ? e[i] : 0.f;
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[c][k + i] = __float_as_uint(e[i]);
-                    // weights as an operand: one rounding to bf16, as large as
-                    // that of the values they multiply
-                    p[k / 2] = pack(e[0], e[1]);
-                    p[k / 2 + 1] = pack(e[2], e[3]);
+            for (int k = 0; k < 32; k += 4) {
+                F2 l0 = own_lse, l1 = own_lse;
+                if (KEYS) {
+                    const float4 v = *reinterpret_cast<const float4 *>(lse + k);
+                    l0 = f2(v.x, v.y);
+                    l1 = f2(v.z, v.w);
                 }
-                if (KEYS) tc::tmem_st16(ts + 16 * c, p);
+                const float2 y0 =
+                    split(fma2(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), scale, l0));
+                const float2 y1 =
+                    split(fma2(f2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), scale, l1));
+                float e[4] = {tc::ex2(y0.x), tc::ex2(y0.y), tc::ex2(y1.x), tc::ex2(y1.y)};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (MASKED) e[i] = sees(k + i) ? e[i] : 0.f;
+                    s[k + i] = __float_as_uint(e[i]);
+                }
+                // weights as an operand: one rounding to bf16, as large as that
+                // of the values they multiply
+                p[k / 2] = pack(e[0], e[1]);
+                p[k / 2 + 1] = pack(e[2], e[3]);
             }
             if (KEYS) {
+                tc::tmem_st16(ts, p);
                 tc::tmem_st_wait();
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) tc::mbar_arrive(&bar.p_full);
             }
-            if (!(ok = tc::warp_wait(&bar.dp_full, j & 1))) break;
+            if (!tc::warp_wait(&bar.dp_full, j & 1)) return false;
             tc::tc_fence_after();
-            uint32_t g[2][32];
-            tc::tmem_ld32_nowait(tdp, g[0]);
-            tc::tmem_ld32_nowait(tdp + 32, g[1]);
+            uint32_t g[32];
+            tc::tmem_ld32_nowait(tdp, g);
             tc::tmem_ld_wait();
-            tc::arrived(g[0]);
-            tc::arrived(g[1]);
+            tc::arrived(g);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t p[16];
-#pragma unroll
-                for (int k = 0; k < 32; k += 4) {
-                    F2 d0 = own_d, d1 = own_d;
-                    if (KEYS) {
-                        const float4 v = *reinterpret_cast<const float4 *>(d + 32 * c + k);
-                        d0 = f2(v.x, v.y);
-                        d1 = f2(v.z, v.w);
-                    }
-                    const F2 x0 = f2(__uint_as_float(g[c][k]), __uint_as_float(g[c][k + 1])) + d0;
-                    const F2 x1 = f2(__uint_as_float(g[c][k + 2]), __uint_as_float(g[c][k + 3])) + d1;
-                    float2 y0 =
-                        split(f2(__uint_as_float(s[c][k]), __uint_as_float(s[c][k + 1])) * x0);
-                    float2 y1 =
-                        split(f2(__uint_as_float(s[c][k + 2]), __uint_as_float(s[c][k + 3])) * x1);
-                    if (!KEYS && masked) {     // V past the sequence may be anything
-                        const int at = str0 + 32 * c + k;
-                        y0.x = at <= held ? y0.x : 0.f;
-                        y0.y = at + 1 <= held ? y0.y : 0.f;
-                        y1.x = at + 2 <= held ? y1.x : 0.f;
-                        y1.y = at + 3 <= held ? y1.y : 0.f;
-                    }
-                    p[k / 2] = pack(y0.x, y0.y);
-                    p[k / 2 + 1] = pack(y1.x, y1.y);
+            for (int k = 0; k < 32; k += 4) {
+                F2 d0 = own_d, d1 = own_d;
+                if (KEYS) {
+                    const float4 v = *reinterpret_cast<const float4 *>(d + k);
+                    d0 = f2(v.x, v.y);
+                    d1 = f2(v.z, v.w);
                 }
-                tc::tmem_st16((KEYS ? tdp : ts) + 16 * c, p);
+                const F2 x0 = f2(__uint_as_float(g[k]), __uint_as_float(g[k + 1])) + d0;
+                const F2 x1 = f2(__uint_as_float(g[k + 2]), __uint_as_float(g[k + 3])) + d1;
+                float2 y0 = split(f2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])) * x0);
+                float2 y1 = split(f2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])) * x1);
+                if (MASKED && !KEYS) {     // V past the sequence may be anything
+                    y0.x = sees(k) ? y0.x : 0.f;
+                    y0.y = sees(k + 1) ? y0.y : 0.f;
+                    y1.x = sees(k + 2) ? y1.x : 0.f;
+                    y1.y = sees(k + 3) ? y1.y : 0.f;
+                }
+                p[k / 2] = pack(y0.x, y0.y);
+                p[k / 2 + 1] = pack(y1.x, y1.y);
             }
+            tc::tmem_st16(KEYS ? tdp : ts, p);
             tc::tmem_st_wait();
             tc::tc_fence_before();
             __syncwarp();
@@ -260,6 +250,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc::mbar_arrive(&bar.ds_full);
                 if (KEYS) tc::mbar_arrive(&bar.row_empty[st]);
             }
+            return true;
+        };
+        for (int j = 0; ok && j < steps; ++j) {
+            const int b = wk.block<KEYS>(j);
+            ok = b == wk.b || wk.tail(b) ? block(std::true_type(), j) : block(std::false_type(), j);
         }
         if (ok) ok = tc::warp_wait(&bar.out_full, 0);
         if (ok) {
@@ -277,20 +272,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float f = scaled ? a.scale : 1.f;
 #pragma unroll
                 for (int c = 0; c < DP / 64; ++c) {
-                    const int col = part * (DP / 2) + 32 * c;
-                    uint32_t v[32];
-                    tc::tmem_ld32_nowait(lanes + (o == 0 ? t_o0 : t_o1) + col, v);
-                    tc::tmem_ld_wait();
-                    tc::arrived(v);
+                    const int col = part * (DP / 4) + 16 * c;
+                    float v[16];
+                    tc::tmem_ld16(lanes + (o == 0 ? t_o0 : t_o1) + col, v);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) asm volatile("" : "+f"(v[k]));   // after the wait
                     if (held >= wk.n) continue;
 #pragma unroll
-                    for (int k = 0; k < 32; k += 8) {
+                    for (int k = 0; k < 16; k += 8) {
                         if (col + k >= a.D) break;
                         uint32_t x[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            x[i] = pack(__uint_as_float(v[k + 2 * i]) * f,
-                                        __uint_as_float(v[k + 2 * i + 1]) * f);
+                            x[i] = pack(v[k + 2 * i] * f, v[k + 2 * i + 1] * f);
                         *reinterpret_cast<uint4 *>(to + col + k) =
                             make_uint4(x[0], x[1], x[2], x[3]);
                     }
@@ -299,7 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::tc_fence_before();
         }
         if (!ok && lane == 0) atomicOr(a.err, kErrTimeout);
-    } else if (w == 8) {
+    } else if (w == kSoftmax) {
         // ---- products: the whole warp waits, one elected thread issues ----
         constexpr uint32_t idesc_s = tc::idesc_bf16_f32(128, 128);
         constexpr uint32_t idesc_o = tc::idesc_bf16_f32(128, DP) | tc::kBColumns;
@@ -328,8 +322,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (leader) {
 #pragma unroll
                 for (int k = 0; k < kRows / 16; ++k)
-                    // each half of the columns was written where its scores were
-                    tc::mma_bf16_ts(base + to, base + x + (k >> 2) * 64 + (k & 3) * 8,
+                    // each quarter of the columns was written where its scores were
+                    tc::mma_bf16_ts(base + to, base + x + (k >> 1) * 32 + (k & 1) * 8,
                                     y + k * (16 * 128 >> 4), idesc_o, add || k > 0);
             }
         };
@@ -385,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             commit(&bar.drained);              // products in flight end before TMEM is freed
             tc::warp_wait(&bar.drained, 0);
         }
-    } else if (w == 9) {
+    } else if (w == kSoftmax + 1) {
         // ---- copies, in the order in which the products read them ----
         if (lane == 0) {
             tc::prefetch_tensormap(&map_h0);
@@ -435,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         }
         __syncwarp();
-    } else if (w == 10) {
+    } else if (w == kSoftmax + 2) {
         uint32_t l_raw = 0, s_raw = 0;         // phases, a bit a stage
         const int from = wk.n & (kRows - 1);
         for (int j = 0; ok && j < steps; ++j) {
@@ -471,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
     __syncthreads();
-    if (w == 8) tc::tmem_dealloc(tmem, 512);
+    if (w == kSoftmax) tc::tmem_dealloc(tmem, 512);
 }
 
 template <int DP, bool KEYS>
