@@ -24,82 +24,136 @@ namespace {
 
 // ---- preparation -------------------------------------------------------------
 
-// 8 entries of a row from 16-byte (32-byte) pieces, or one by one
-template <typename T, bool WIDE> __device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
-    if constexpr (!WIDE) {
+// 8 entries of a row as they are loaded, in 16-byte pieces or one by one
+template <typename T, bool WIDE> struct Eight {
+    uint4 x[sizeof(T) / 2];
+    __device__ __forceinline__ void get(const T *p) {
+        if constexpr (WIDE) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = to_f(p[k]);
-    } else if constexpr (sizeof(T) == 4) {
-        const float4 x = reinterpret_cast<const float4 *>(p)[0];
-        const float4 y = reinterpret_cast<const float4 *>(p)[1];
-        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-        v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
-    } else {
-        const uint4 x = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i) x[i] = reinterpret_cast<const uint4 *>(p)[i];
+        } else {
+            T v[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[2 * k] = __uint_as_float(w[k] << 16);
-            v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+            for (int k = 0; k < 8; ++k) v[k] = p[k];
+            memcpy(x, v, sizeof v);
+        }
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) x[i] = make_uint4(0, 0, 0, 0);
+    }
+};
+__device__ __forceinline__ float dot4(uint4 a, uint4 b, float s, const float *) {
+    s = fmaf(__uint_as_float(a.x), __uint_as_float(b.x), s);
+    s = fmaf(__uint_as_float(a.y), __uint_as_float(b.y), s);
+    s = fmaf(__uint_as_float(a.z), __uint_as_float(b.z), s);
+    return fmaf(__uint_as_float(a.w), __uint_as_float(b.w), s);
+}
+__device__ __forceinline__ float dot4(uint4 a, uint4 b, float s, const __nv_bfloat16 *) {
+    const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        s = fmaf(__uint_as_float(x[i] << 16), __uint_as_float(y[i] << 16), s);
+        s = fmaf(__uint_as_float(x[i] & 0xffff0000u), __uint_as_float(y[i] & 0xffff0000u), s);
+    }
+    return s;
+}
+
+// The lists of blocks, by one thread block.  A sequence of n blocks has one of
+// each length 1..n, in rows that see a key block and in keys that a row
+// block sees, so that one count by length places both lists, the longest first
+// (lengths past kLengths count as that).
+constexpr int kLengths = 1024;
+__device__ void list_blocks(const Args &a) {
+    __shared__ int count[kLengths + 1], at[2][kLengths + 1], scan[8];
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    auto sequence = [&](int64_t r, int &tok0, int &n) {
+        tok0 = max(0, a.q_start[r]);
+        n = max(0, min(a.T, a.q_start[r + 1]) - tok0);
+        return (int)(((int64_t)n + a.block - 1) / a.block);
+    };
+    for (int i = tid; i <= kLengths; i += 256) count[i] = 0;
+    __syncthreads();
+    // by a sequence's own number of blocks, and what lies past the last length
+    for (int64_t r = tid; r < a.n_seqs; r += 256) {
+        int tok0, n;
+        const int blocks = sequence(r, tok0, n);
+        if (blocks) atomicAdd(&count[min(blocks, kLengths)], 1);
+        if (blocks > kLengths) atomicAdd(&count[0], blocks - kLengths);
+    }
+    __syncthreads();
+    // blocks of length l: sequences of at least l blocks; four lengths a thread,
+    // from the longest, sums over threads by a scan
+    const int top = kLengths - 4 * tid;
+    int own[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += own[i] = count[top - i];
+    auto before = [&](int v) {
+        int upto = v;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        __syncthreads();
+        if (lane == 31) scan[w] = upto;
+        __syncthreads();
+        int base = upto - v;
+        for (int i = 0; i < w; ++i) base += scan[i];
+        return base;
+    };
+    int longer = before(sum), of[4], total = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) total += of[i] = longer += own[i];
+    if (tid == 0) {
+        total += count[0];                  // the blocks past the last length, counted as that
+        of[0] += count[0];
+    }
+    int start = before(total);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        at[0][top - i] = at[1][top - i] = start;
+        start += of[i];
+    }
+    if (tid == 255) *a.count = min(start, a.most);
+    __syncthreads();
+    // a warp a sequence, so that a long one is listed in few steps
+    for (int64_t r0 = 0; r0 < a.n_seqs; r0 += 256) {
+        int tok0 = 0, n = 0, blocks = 0;
+        if (r0 + tid < a.n_seqs) blocks = sequence(r0 + tid, tok0, n);
+        for (int i = 0; i < 32; ++i) {
+            const int t0 = __shfl_sync(0xffffffffu, tok0, i);
+            const int tn = __shfl_sync(0xffffffffu, n, i);
+            const int nb = __shfl_sync(0xffffffffu, blocks, i);
+            for (int b = lane; b < nb; b += 32) {
+                const int k = atomicAdd(&at[0][min(nb - b, kLengths)], 1);
+                if (k < a.most) a.blocks[k] = make_int4(t0, tn, b, 0);
+                const int q = atomicAdd(&at[1][min(b + 1, kLengths)], 1);
+                if (q < a.most) a.blocks[a.most + q] = make_int4(t0, tn, b, 0);
+            }
         }
     }
 }
 
-// Block 0 lists the sequences' blocks; the others compute d_i: 2^LANES lanes a
-// row and head, 8 entries each (a warp takes as many rows as fit, four times
-// over, so that enough loads are in flight; 4 x 4096 tokens x 16 heads x 128:
-// LATER us, bound by reading dout and out).
+// Block 0 lists the sequences' blocks; the others compute d_i: 2^lanes_log2 lanes
+// a row and head, 8 entries each (a warp takes as many rows as fit, four times
+// over, so that enough loads are in flight).  Bound by reading dout and out.
 template <typename T, bool WIDE> __global__ void __launch_bounds__(256)
     prepare_kernel(Args a, int lanes_log2) {
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     if (blockIdx.x == 0) {
-        __shared__ int scan[8], first[256], total;
-        if (threadIdx.x == 0) total = 0;
-        __syncthreads();
-        for (int64_t r0 = 0; r0 < a.n_seqs; r0 += 256) {
-            const int64_t r = r0 + threadIdx.x;
-            int tok0 = 0, n = 0;
-            if (r < a.n_seqs) {
-                tok0 = max(0, a.q_start[r]);
-                n = max(0, min(a.T, a.q_start[r + 1]) - tok0);
-            }
-            const int blocks = (int)(((int64_t)n + a.block - 1) / a.block);
-            int upto = blocks;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += v;
-            }
-            if (lane == 31) scan[w] = upto;
-            __syncthreads();
-            int base = total;
-            for (int i = 0; i < w; ++i) base += scan[i];
-            first[threadIdx.x] = base + upto - blocks;
-            __syncthreads();
-            if (threadIdx.x == 255) total = base + upto;
-            // a warp a sequence, so that a long one is listed in few steps
-            for (int i = 0; i < 32; ++i) {
-                const int t0 = __shfl_sync(0xffffffffu, tok0, i);
-                const int tn = __shfl_sync(0xffffffffu, n, i);
-                const int nb = __shfl_sync(0xffffffffu, blocks, i);
-                const int at = first[w * 32 + i];
-                for (int b = lane; b < nb; b += 32)
-                    if (at + b < a.most) a.blocks[at + b] = make_int4(t0, tn, b, 0);
-            }
-            __syncthreads();
-        }
-        if (threadIdx.x == 0) *a.count = min(total, a.most);
+        list_blocks(a);
         return;
     }
     constexpr int kAhead = 4;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int per_row = 1 << lanes_log2, part = lane & (per_row - 1);
     const int64_t rows = (int64_t)a.T * a.q_heads;
     const int64_t per_warp = 32 >> lanes_log2, step = (int64_t)(gridDim.x - 1) * 8 * per_warp * kAhead;
     const int64_t first = ((int64_t)(blockIdx.x - 1) * 8 + w) * per_warp * kAhead + (lane >> lanes_log2);
     for (int64_t i0 = first; i0 - (lane >> lanes_log2) < rows; i0 += step) {
-        float x[kAhead][8], y[kAhead][8];
+        Eight<T, WIDE> x[kAhead], y[kAhead];
         int64_t t[kAhead];
         int h[kAhead];
         t[0] = i0 / a.q_heads;
@@ -115,19 +169,21 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256)
                     ++t[k];
                 }
             }
-#pragma unroll
-            for (int c = 0; c < 8; ++c) x[k][c] = y[k][c] = 0.f;
             if (i < rows && part * 8 < a.D) {
                 const int64_t at = (int64_t)h[k] * a.D + part * 8;
-                load8<T, WIDE>(static_cast<const T *>(a.dout) + t[k] * a.dout_stride + at, x[k]);
-                load8<T, WIDE>(static_cast<const T *>(a.out) + t[k] * a.out_stride + at, y[k]);
+                x[k].get(static_cast<const T *>(a.dout) + t[k] * a.dout_stride + at);
+                y[k].get(static_cast<const T *>(a.out) + t[k] * a.out_stride + at);
+            } else {
+                x[k].zero();
+                y[k].zero();
             }
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             float s = 0.f;
 #pragma unroll
-            for (int c = 0; c < 8; ++c) s = fmaf(x[k][c], y[k][c], s);
+            for (int c = 0; c < (int)sizeof(T) / 2; ++c)
+                s = dot4(x[k].x[c], y[k].x[c], s, static_cast<const T *>(nullptr));
             for (int o = per_row / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
             if (part == 0 && i0 + k * per_warp < rows) {
                 const float lse = a.lse[i0 + k * per_warp];
@@ -170,24 +226,19 @@ __device__ __forceinline__ void load_rows(float *dst, const void *src, int64_t s
 // KEYS: holds keys and values, streams queries and output gradients, writes dk
 // and dv; else the other way round, and dq.
 template <typename T, int DP, bool KEYS>
-__global__ void __launch_bounds__(kThreads) rows_kernel(Args a) {
+__device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta) {
     using S = Shape<DP>;
     constexpr int kHeld = S::kHeld, kPad = S::kPad, kWPad = S::kWPad;
     constexpr int kH = kHeld / 16;                       // held rows of a thread's scores
     constexpr int kC = DP / 16;                          // columns of a thread's sums
-    extern __shared__ float sm[];
     float *h0 = sm, *h1 = h0 + kHeld * kPad;             // K and V, or Q and dout
     float *s0 = h1 + kHeld * kPad, *s1 = s0 + kStream * kPad;
     float *wp = s1 + kStream * kPad, *wd = wp + kStream * kWPad;   // P and dS, [streamed][held]
     float *lse = wd + kStream * kWPad, *di = lse + 64;
-    pdl_wait();
-    pdl_trigger();
     const int heads = KEYS ? a.kv_heads : a.q_heads;
-    const int index = blockIdx.x / heads, head = blockIdx.x % heads;
-    const int count = *a.count;
-    if (index >= count) return;
-    // the longest first: early keys are seen by most rows, late rows see most keys
-    const int4 blk = a.blocks[KEYS ? index : count - 1 - index];
+    const int index = (int)(cta / heads), head = (int)(cta % heads);
+    if (index >= *a.count) return;
+    const int4 blk = a.blocks[KEYS ? index : a.most + index];   // the longest first
     const int64_t tok0 = blk.x, end = tok0 + blk.y;
     const int64_t first = tok0 + (int64_t)blk.z * kHeld;
     const int kv = KEYS ? head : head / a.group;
@@ -315,16 +366,25 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Args a) {
     }
 }
 
+// Both roles in one launch, held keys first.
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads) rows_kernel(Args a) {
+    extern __shared__ float sm[];
+    pdl_wait();
+    pdl_trigger();
+    const unsigned keys = (unsigned)a.most * a.kv_heads;
+    if (blockIdx.x < keys)
+        rows_run<T, DP, true>(sm, a, blockIdx.x);
+    else
+        rows_run<T, DP, false>(sm, a, blockIdx.x - keys);
+}
+
 template <typename T, int DP> cudaError_t rows_go(const Args &a, cudaStream_t st) {
-    cudaError_t e = allow_dynamic_smem<rows_kernel<T, DP, true>>(Shape<DP>::kSmem);
-    if (e == cudaSuccess) e = allow_dynamic_smem<rows_kernel<T, DP, false>>(Shape<DP>::kSmem);
-    if (e == cudaSuccess)
-        e = launch_kernel(true, rows_kernel<T, DP, true>, dim3((unsigned)a.most * a.kv_heads),
-                          kThreads, Shape<DP>::kSmem, st, a);
-    if (e == cudaSuccess)
-        e = launch_kernel(true, rows_kernel<T, DP, false>, dim3((unsigned)a.most * a.q_heads),
-                          kThreads, Shape<DP>::kSmem, st, a);
-    return e;
+    const cudaError_t e = allow_dynamic_smem<rows_kernel<T, DP>>(Shape<DP>::kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(true, rows_kernel<T, DP>,
+                         dim3((unsigned)a.most * (a.kv_heads + a.q_heads)), kThreads,
+                         Shape<DP>::kSmem, st, a);
 }
 template <typename T> cudaError_t rows_dim(const Args &a, cudaStream_t st) {
     return a.D <= 64 ? rows_go<T, 64>(a, st)
@@ -367,7 +427,7 @@ Layout layout_of(int32_t T, int32_t n_seqs, int32_t q_heads, int32_t dim) {
     l.most = (int)most;
     l.rows = 0;
     l.blocks = ((int64_t)T * q_heads * 8 + 15) & ~15ll;
-    l.count = l.blocks + most * 16;
+    l.count = l.blocks + 2 * most * 16;
     l.total = l.count + 16;
     return l;
 }
@@ -379,7 +439,7 @@ bool heads_ok(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim) {
 }
 // what grids and offsets hold
 bool sizes_ok(int32_t T, int32_t n_seqs, int32_t q_heads, int32_t dim) {
-    return T >= 0 && n_seqs >= 0 && most_blocks(T, n_seqs, block_of(dim)) * q_heads <= INT32_MAX;
+    return T >= 0 && n_seqs >= 0 && most_blocks(T, n_seqs, block_of(dim)) * 2 * q_heads <= INT32_MAX;
 }
 
 }  // namespace

@@ -19,7 +19,8 @@ struct Args {
     const int32_t *q_start;
     int64_t q_stride, k_stride, v_stride, out_stride, dout_stride, dq_stride, dk_stride, dv_stride;
     float2 *rows;             // [q_heads][T]: (lse, +inf where it is -inf; d_i)
-    int4 *blocks;             // [most]: tok0, n, b of each block of `block` rows
+    int4 *blocks;             // [2][most]: tok0, n, b of each block of `block` rows, by the
+                              // rows behind it, and by the keys before it, longest first
     int *count;               // of them
     int *err;
     int n_seqs, T, q_heads, kv_heads, group, D;

@@ -51,17 +51,32 @@ template <int DP, bool KEYS> struct Cfg {
     // streamed tiles that the sums read last (Q or K), and the others (dO or V)
     static constexpr int kLong = DP == 128 ? 3 : 4;
     static constexpr int kShort = DP == 128 ? 2 : 3;
+    // a second warp for the sums, where a commit may stand between them and
+    // the scores that take their operands' place
+    static constexpr bool kTwo = !KEYS;
     static constexpr int kTiles = 2 + kLong + kShort;
     static constexpr size_t kSmem = (size_t)kTile * kTiles + 2 * 2 * kRows * 4 + 512;
 };
 
 struct Bars {
     uint64_t held, long_full[4], long_raw[4], long_empty[4], short_full[4], short_raw[4],
-        short_empty[4], s_full[2], dp_full, p_full, ds_full, row_full[2], row_empty[2], out_full,
-        drained;
+        short_empty[4], s_full[2], dp_full, p_full[2], ds_full[2], row_full[2], row_empty[2], out_full,
+        drained[2];
     uint32_t tmem;
 };
 static_assert(sizeof(Bars) <= 512, "barriers");
+
+// A place in a ring of N stages and the phase of its barriers.
+template <int N> struct Stage {
+    int at = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++at == N) {
+            at = 0;
+            phase ^= 1;
+        }
+    }
+};
 
 // What a CTA works on: `steps` streamed blocks.
 struct Work {
@@ -92,13 +107,10 @@ __device__ __forceinline__ uint32_t pack(float x, float y) {
 }
 
 template <int DP, bool KEYS>
-__global__ void __launch_bounds__(kThreads, 1)
-    grad_kernel(const __grid_constant__ CUtensorMap map_h0,
-                const __grid_constant__ CUtensorMap map_h1,
-                const __grid_constant__ CUtensorMap map_l,
-                const __grid_constant__ CUtensorMap map_s, Args a) {
+__device__ __forceinline__ void run(uint8_t *sm, const CUtensorMap &map_h0,
+                                    const CUtensorMap &map_h1, const CUtensorMap &map_l,
+                                    const CUtensorMap &map_s, const Args &a, unsigned cta) {
     using C = Cfg<DP, KEYS>;
-    extern __shared__ __align__(1024) uint8_t sm[];
     uint8_t *held0 = sm, *held1 = sm + C::kTile, *ring_l = sm + 2 * C::kTile,
             *ring_s = ring_l + C::kLong * C::kTile;
     float *row_lse = reinterpret_cast<float *>(ring_s + C::kShort * C::kTile);   // [2][kRows]
@@ -106,17 +118,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     Bars &bar = *reinterpret_cast<Bars *>(row_d + 2 * kRows);
     const int tid = threadIdx.x, w = tid >> 5, lane = tid & 31;
 
-    pdl_wait();
     const int heads = KEYS ? a.kv_heads : a.q_heads;
-    const int count = *a.count, index = blockIdx.x / heads;
-    if (index >= count) return;
-    const int4 blk = a.blocks[KEYS ? index : count - 1 - index];   // the longest first
+    const int index = (int)(cta / heads);
+    if (index >= *a.count) return;
+    const int4 blk = a.blocks[KEYS ? index : a.most + index];   // the longest first
     Work wk;
     wk.tok0 = blk.x;
     wk.n = blk.y;
     wk.b = blk.z;
     wk.blocks = (blk.y + kRows - 1) / kRows;
-    wk.head = blockIdx.x % heads;
+    wk.head = (int)(cta % heads);
     wk.kv = KEYS ? wk.head : wk.head / a.group;
     wk.steps = KEYS ? a.group * (wk.blocks - wk.b) : wk.b + 1;
     const int steps = wk.steps;
@@ -133,14 +144,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&bar.s_full[i], 1);
+            // two of each, in turns: the warp that waits for one may be a step late
+            tc::mbar_init(&bar.p_full[i], kSoftmax);
+            tc::mbar_init(&bar.ds_full[i], kSoftmax);
             tc::mbar_init(&bar.row_full[i], 32);
             tc::mbar_init(&bar.row_empty[i], kSoftmax);
         }
         tc::mbar_init(&bar.dp_full, 1);
-        tc::mbar_init(&bar.p_full, kSoftmax);
-        tc::mbar_init(&bar.ds_full, kSoftmax);
         tc::mbar_init(&bar.out_full, 1);
-        tc::mbar_init(&bar.drained, 1);
+        tc::mbar_init(&bar.drained[0], 1);
+        tc::mbar_init(&bar.drained[1], 1);
         tc::fence_mbar_init();
     }
     if (w == kSoftmax) tc::tmem_alloc(&bar.tmem, 512);
@@ -179,6 +192,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (KEYS && !tc::warp_wait(&bar.row_full[st], (j >> 1) & 1)) return false;
             if (!tc::warp_wait(&bar.s_full[sb], (s_phase >> sb) & 1)) return false;
             s_phase ^= 1u << sb;
+            // these scores were issued behind dV of kScores steps before, and dP
+            // behind dK of the step before: their stages are free
+            if (!C::kTwo && j >= C::kScores && w == 0 && lane == 0)
+                tc::mbar_arrive(&bar.short_empty[(j - C::kScores) % C::kShort]);
             tc::tc_fence_after();
             const uint32_t ts = lanes + 128 * sb + 32 * part, tdp = lanes + t_dp + 32 * part;
             uint32_t s[32], p[16];
@@ -213,9 +230,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc::tmem_st_wait();
                 tc::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) tc::mbar_arrive(&bar.p_full);
+                if (lane == 0) tc::mbar_arrive(&bar.p_full[st]);
             }
             if (!tc::warp_wait(&bar.dp_full, j & 1)) return false;
+            if (!C::kTwo && j > 0 && w == 0 && lane == 0)
+                tc::mbar_arrive(&bar.long_empty[(j - 1) % C::kLong]);
             tc::tc_fence_after();
             uint32_t g[32];
             tc::tmem_ld32_nowait(tdp, g);
@@ -247,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) {
-                tc::mbar_arrive(&bar.ds_full);
+                tc::mbar_arrive(&bar.ds_full[st]);
                 if (KEYS) tc::mbar_arrive(&bar.row_empty[st]);
             }
             return true;
@@ -293,8 +312,13 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc::tc_fence_before();
         }
         if (!ok && lane == 0) atomicOr(a.err, kErrTimeout);
-    } else if (w == kSoftmax) {
-        // ---- products: the whole warp waits, one elected thread issues ----
+    } else if (w == kSoftmax || (C::kTwo && w == kSoftmax + 3)) {
+        // ---- products: the whole warp waits, one elected thread issues.  A
+        // wait costs the issuing warp about 100 cycles, a commit as much and a
+        // product 24.  With keys held one warp issues everything, in the order
+        // that the buffers allow without a wait for a product's end; with rows held
+        // it would be busy for longer than the products run (2600 cycles a
+        // block at width 128), and a second one issues the sums ----
         constexpr uint32_t idesc_s = tc::idesc_bf16_f32(128, 128);
         constexpr uint32_t idesc_o = tc::idesc_bf16_f32(128, DP) | tc::kBColumns;
         const bool leader = tc::elect_one();
@@ -305,7 +329,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint64_t s_k = tc::desc_k_sw128(tc::smem_u32(ring_s));
         const uint64_t l_mn = tc::desc_mn_sw128(tc::smem_u32(ring_l), kHalfBytes);
         const uint64_t s_mn = tc::desc_mn_sw128(tc::smem_u32(ring_s), kHalfBytes);
-        uint32_t l_phase = 0, s_phase = 0;     // a bit a stage
         auto commit = [&](uint64_t *b) {
             if (leader) tc::mma_commit(b);
         };
@@ -327,57 +350,70 @@ __global__ void __launch_bounds__(kThreads, 1)
                                     y + k * (16 * 128 >> 4), idesc_o, add || k > 0);
             }
         };
-        auto scores = [&](int j) {
-            const int st = j % C::kLong;
-            if (!tc::warp_wait(&bar.long_full[st], (l_phase >> st) & 1)) return false;
-            l_phase ^= 1u << st;
+        Stage<C::kLong> l;
+        Stage<C::kShort> h;
+        auto scores = [&](int j) {               // S of step j, the l-th stage
+            if (!tc::warp_wait(&bar.long_full[l.at], l.phase)) return false;
             tc::tc_fence_after();
-            product(128 * (j % C::kScores), h0, l_k + (uint32_t)st * (C::kTile >> 4));
+            product(128 * (j % C::kScores), h0, l_k + (uint32_t)l.at * (C::kTile >> 4));
             commit(&bar.s_full[j % C::kScores]);
+            l.next();
             return true;
         };
-        auto other = [&](int j) {               // dP of step j
-            const int st = j % C::kShort;
-            if (!tc::warp_wait(&bar.short_full[st], (s_phase >> st) & 1)) return false;
-            s_phase ^= 1u << st;
+        auto other = [&] {                       // dP of the next step
+            if (!tc::warp_wait(&bar.short_full[h.at], h.phase)) return false;
             tc::tc_fence_after();
-            product(t_dp, h1, s_k + (uint32_t)st * (C::kTile >> 4));
+            product(t_dp, h1, s_k + (uint32_t)h.at * (C::kTile >> 4));
             commit(&bar.dp_full);
-            if (!KEYS) commit(&bar.short_empty[st]);
+            if (!KEYS) commit(&bar.short_empty[h.at]);
+            h.next();
             return true;
         };
-        ok = tc::warp_wait(&bar.held, 0);
-        for (int j = 0; ok && j < C::kScores && j < steps; ++j) ok = scores(j);
-        if (!KEYS && ok) ok = other(0);
-        for (int j = 0; ok && j < steps; ++j) {
-            const uint32_t sl = (uint32_t)(j % C::kLong) * (C::kTile >> 4);
-            const uint32_t ss = (uint32_t)(j % C::kShort) * (C::kTile >> 4);
-            if (KEYS) {
-                if (!(ok = other(j))) break;
-                if (!(ok = tc::warp_wait(&bar.p_full, j & 1))) break;
-                tc::tc_fence_after();
-                sum(t_o0, 128 * (j % C::kScores), s_mn + ss, j > 0);
-                commit(&bar.short_empty[j % C::kShort]);
-                if (j + C::kScores < steps && !(ok = scores(j + C::kScores))) break;
-                if (!(ok = tc::warp_wait(&bar.ds_full, j & 1))) break;
-                tc::tc_fence_after();
-                sum(t_o1, t_dp, l_mn + sl, j > 0);
-                commit(&bar.long_empty[j % C::kLong]);
-            } else {
-                if (!(ok = tc::warp_wait(&bar.ds_full, j & 1))) break;
-                tc::tc_fence_after();
-                if (j + 1 < steps && !(ok = other(j + 1))) break;
-                sum(t_o0, 128 * (j % C::kScores), l_mn + sl, j > 0);
-                commit(&bar.long_empty[j % C::kLong]);
-                if (j + C::kScores < steps && !(ok = scores(j + C::kScores))) break;
-            }
-        }
-        if (ok) {
-            commit(&bar.out_full);
+        auto sum_short = [&](int j, const Stage<C::kShort> &st) {   // dV
+            if (!tc::warp_wait(&bar.p_full[j & 1], (j >> 1) & 1)) return false;
+            tc::tc_fence_after();
+            sum(t_o0, 128 * (j % C::kScores), s_mn + (uint32_t)st.at * (C::kTile >> 4), j > 0);
+            return true;
+        };
+        auto sum_long = [&](int j, const Stage<C::kLong> &st) {     // dK or dQ
+            if (!tc::warp_wait(&bar.ds_full[j & 1], (j >> 1) & 1)) return false;
+            tc::tc_fence_after();
+            sum(KEYS ? t_o1 : t_o0, KEYS ? t_dp : 128 * (j % C::kScores),
+                l_mn + (uint32_t)st.at * (C::kTile >> 4), j > 0);
+            if (C::kTwo) commit(&bar.long_empty[st.at]);
+            return true;
+        };
+        if (!C::kTwo) {
+            // what a step's stages are free of is told to the copies by the warps
+            // that wait for the commits behind it
+            Stage<C::kLong> ls;
+            Stage<C::kShort> hs;
+            ok = tc::warp_wait(&bar.held, 0);
+            for (int j = 0; ok && j < C::kScores && j < steps; ++j) ok = scores(j);
+            for (int j = 0; ok && j < steps; ++j, ls.next(), hs.next())
+                ok = other() && sum_short(j, hs) &&
+                     (j + C::kScores >= steps || scores(j + C::kScores)) && sum_long(j, ls);
+            if (ok) commit(&bar.out_full);
+        } else if (w == kSoftmax) {
+            Stage<C::kLong> ls;
+            ok = tc::warp_wait(&bar.held, 0);
+            for (int j = 0; ok && j < C::kScores && j < steps; ++j) ok = scores(j);
+            if (ok) ok = other();
+            for (int j = 0; ok && j + 1 < steps; ++j, ls.next())
+                // dP was read, and dS by the sum, whose place S of step j + 2 takes
+                ok = tc::warp_wait(&bar.ds_full[j & 1], (j >> 1) & 1) && other() &&
+                     (j + C::kScores >= steps ||
+                      (tc::warp_wait(&bar.long_empty[ls.at], ls.phase) && scores(j + C::kScores)));
         } else {
+            Stage<C::kLong> ls;
+            for (int j = 0; ok && j < steps; ++j, ls.next()) ok = sum_long(j, ls);
+            if (ok) commit(&bar.out_full);
+        }
+        if (!ok) {
             if (leader) atomicOr(a.err, kErrTimeout);
-            commit(&bar.drained);              // products in flight end before TMEM is freed
-            tc::warp_wait(&bar.drained, 0);
+            uint64_t *drained = &bar.drained[w == kSoftmax ? 0 : 1];
+            commit(drained);                   // products in flight end before TMEM is freed
+            tc::warp_wait(drained, 0);
         }
     } else if (w == kSoftmax + 1) {
         // ---- copies, in the order in which the products read them ----
@@ -468,25 +504,37 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (w == kSoftmax) tc::tmem_dealloc(tmem, 512);
 }
 
-template <int DP, bool KEYS>
-cudaError_t go(const Args &a, const CUtensorMap &h0, const CUtensorMap &h1, const CUtensorMap &l,
-               const CUtensorMap &s, cudaStream_t st) {
-    using C = Cfg<DP, KEYS>;
-    const cudaError_t e = allow_dynamic_smem<grad_kernel<DP, KEYS>>(C::kSmem);
+// Both roles in one launch: the long tiles of held keys first, and the many
+// short ones of held rows fill the SMs that those leave.
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+    grad_kernel(const __grid_constant__ CUtensorMap q, const __grid_constant__ CUtensorMap k,
+                const __grid_constant__ CUtensorMap v, const __grid_constant__ CUtensorMap dout,
+                Args a) {
+    extern __shared__ __align__(1024) uint8_t sm[];
+    pdl_wait();
+    const unsigned keys = (unsigned)a.most * a.kv_heads;
+    if (blockIdx.x < keys)
+        run<DP, true>(sm, k, v, q, dout, a, blockIdx.x);
+    else
+        run<DP, false>(sm, q, dout, k, v, a, blockIdx.x - keys);
+}
+
+template <int DP>
+cudaError_t go(const Args &a, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v,
+               const CUtensorMap &dout, cudaStream_t st) {
+    static_assert(Cfg<DP, true>::kSmem == Cfg<DP, false>::kSmem, "one launch");
+    const cudaError_t e = allow_dynamic_smem<grad_kernel<DP>>(Cfg<DP, true>::kSmem);
     if (e != cudaSuccess) return e;
-    const int heads = KEYS ? a.kv_heads : a.q_heads;
-    return launch_kernel(true, grad_kernel<DP, KEYS>, dim3((unsigned)a.most * heads), kThreads,
-                         C::kSmem, st, h0, h1, l, s, a);
+    return launch_kernel(true, grad_kernel<DP>, dim3((unsigned)a.most * (a.kv_heads + a.q_heads)),
+                         kThreads, Cfg<DP, true>::kSmem, st, q, k, v, dout, a);
 }
 
 }  // namespace
 
 cudaError_t launch_tensor(const Args &a, const CUtensorMap &q, const CUtensorMap &k,
                           const CUtensorMap &v, const CUtensorMap &dout, cudaStream_t st) {
-    const cudaError_t e = a.D <= 64 ? go<64, true>(a, k, v, q, dout, st)
-                                    : go<128, true>(a, k, v, q, dout, st);
-    if (e != cudaSuccess) return e;
-    return a.D <= 64 ? go<64, false>(a, q, dout, k, v, st) : go<128, false>(a, q, dout, k, v, st);
+    return a.D <= 64 ? go<64>(a, q, k, v, dout, st) : go<128>(a, q, k, v, dout, st);
 }
 
 }  // namespace attn_grad
