@@ -105,7 +105,7 @@ struct LseEpi {
     float scale, scale_log2;
 
     __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
-                                               const pair::Plan &p) const {
+                                               const pair::Plan &p, pair::Scratch &scratch) const {
         const int64_t tok = t.m0 + row;
         const int label = tok < T ? labels(tok) - (v0 + t.n0) : -1;   // the tile's column
         const int cols = min(p.n_tile, vn - t.n0);
@@ -182,30 +182,22 @@ __device__ __forceinline__ void store_sector(void *dst, const uint32_t (&r)[8]) 
                  "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                  : "memory");
 }
-// 32 values to a row of T, `left` of them there; `wide`: on 32-byte boundaries
-template <typename T>
-__device__ __forceinline__ void store32(T *to, const float (&v)[32], int left, bool wide) {
-    if (wide && left >= 32) {
+// 32 values to a row of T, on a 32-byte boundary
+template <typename T> __device__ __forceinline__ void store32(T *to, const float (&v)[32]) {
 #pragma unroll
-        for (int k = 0; k < (int)sizeof(T); ++k) {
-            uint32_t o[8];
+    for (int k = 0; k < (int)sizeof(T); ++k) {
+        uint32_t o[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if constexpr (sizeof(T) == 4) {
-                    o[j] = __float_as_uint(v[8 * k + j]);
-                } else {
-                    const __nv_bfloat162 b =
-                        __floats2bfloat162_rn(v[16 * k + 2 * j], v[16 * k + 2 * j + 1]);
-                    o[j] = *reinterpret_cast<const uint32_t *>(&b);
-                }
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (sizeof(T) == 4) {
+                o[j] = __float_as_uint(v[8 * k + j]);
+            } else {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[16 * k + 2 * j], v[16 * k + 2 * j + 1]);
+                o[j] = *reinterpret_cast<const uint32_t *>(&b);
             }
-            store_sector(to + 32 / sizeof(T) * k, o);
         }
-        return;
+        store_sector(to + 32 / sizeof(T) * k, o);
     }
-#pragma unroll
-    for (int k = 0; k < 32; ++k)
-        if (k < left) to[k] = from_f<T>(v[k]);
 }
 
 // P planes of G [P][T][ld]; ld is a multiple of 32, and columns up to the next
@@ -219,7 +211,7 @@ template <int P> struct GradEpi {
     float scale, scale_log2;
 
     __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
-                                               const pair::Plan &p) const {
+                                               const pair::Plan &p, pair::Scratch &scratch) const {
         const int64_t tok = t.m0 + row;
         const bool live = tok < T;
         const int label = live ? labels(tok) : -1;
@@ -247,7 +239,7 @@ template <int P> struct GradEpi {
             __nv_bfloat16 *to = g + tok * ld + t.n0 + c;
 #pragma unroll
             for (int q = 0; q < P; ++q) {
-                store32(to + (int64_t)q * T * ld, z, 32, true);
+                store32(to + (int64_t)q * T * ld, z);
                 if (q + 1 < P)
 #pragma unroll
                     for (int k = 0; k < 32; ++k) z[k] -= __bfloat162float(__float2bfloat16_rn(z[k]));
@@ -256,71 +248,100 @@ template <int P> struct GradEpi {
     }
 };
 
-// A product's rows [M][N], with `add` on top of what part [splits][M][N] (fp32)
-// holds: to `out` in T, or without it back to part.
+// A product's rows [M][N], with `add` on top of what part [splits][M][ld] (fp32,
+// ld a multiple of 8) holds: to `out` in T, or without it back to part.  Where
+// out's rows allow 32-byte stores (`wide`), each thread stores its row; else a
+// warp turns 16 columns of its 32 rows at a time, so that lanes store
+// neighbours (one by one, a column of 32 rows at a time, an odd width made the
+// gradient of 333 tokens against 5003 x 509 LATER instead of LATER us).
 template <typename T> struct StoreEpi {
     T *out;
     float *part;
-    int64_t M, N;
+    int64_t M, N, ld;
     int add, wide;
 
     __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
-                                               const pair::Plan &p) const {
+                                               const pair::Plan &p, pair::Scratch &scratch) const {
         const int64_t r = t.m0 + row;
-        const int cols = (int)min((int64_t)p.n_tile, N - t.n0);
+        const int cols = (int)min((int64_t)p.n_tile, N - t.n0), lane = threadIdx.x & 31;
         for (int c = 0; c < cols; c += 32) {
             float v[32];
             pair::load32(tmem + c, v);
-            if (r >= M) continue;
             const int left = cols - c;
-            float *sum = part + ((int64_t)t.split * M + r) * N + t.n0 + c;
-            if (add && left >= 32 && N % 4 == 0) {
+            if (r < M) {
+                float *sum = part + ((int64_t)t.split * M + r) * ld + t.n0 + c;
+                if (add) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float4 x = reinterpret_cast<const float4 *>(sum)[k];
-                    v[4 * k] += x.x, v[4 * k + 1] += x.y, v[4 * k + 2] += x.z, v[4 * k + 3] += x.w;
+                    for (int k = 0; k < 32; k += 4) {
+                        if (k >= left) break;            // rows are padded to 8
+                        const float4 x = *reinterpret_cast<const float4 *>(sum + k);
+                        v[k] += x.x, v[k + 1] += x.y, v[k + 2] += x.z, v[k + 3] += x.w;
+                    }
                 }
-            } else if (add) {
+                if (!out) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k)
-                    if (k < left) v[k] += sum[k];
+                    for (int k = 0; k < 32; k += 8) {
+                        if (k >= left) break;
+                        const uint32_t o[8] = {__float_as_uint(v[k]),     __float_as_uint(v[k + 1]),
+                                               __float_as_uint(v[k + 2]), __float_as_uint(v[k + 3]),
+                                               __float_as_uint(v[k + 4]), __float_as_uint(v[k + 5]),
+                                               __float_as_uint(v[k + 6]), __float_as_uint(v[k + 7])};
+                        store_sector(sum + k, o);
+                    }
+                } else if (wide && left >= 32) {
+                    store32(out + r * N + t.n0 + c, v);
+                }
             }
-            if (out)
-                store32(out + r * N + t.n0 + c, v, left, wide);
-            else
-                store32(sum, v, left, N % 8 == 0);
+            if (!out || (wide && left >= 32)) continue;
+            const int64_t row0 = r - lane;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (16 * h >= left) break;
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 16; ++k) scratch.v[lane][k] = v[16 * h + k];
+                __syncwarp();
+                const int k = lane & 15;
+#pragma unroll 8
+                for (int i = lane >> 4; i < 32; i += 2)
+                    if (row0 + i < M && 16 * h + k < left)
+                        out[(row0 + i) * N + t.n0 + c + 16 * h + k] = from_f<T>(scratch.v[i][k]);
+            }
         }
     }
 };
 
-// out = sum of part [splits][n] over the splits, in order; four values a thread
-// where n allows
-template <typename T, int N>
+// out [M][N] = sum of part [splits][M][ld] over the splits, in order; four
+// columns a thread
+template <typename T>
 __global__ void __launch_bounds__(256)
-    sum_splits_kernel(const float *part, int splits, int64_t n, T *out) {
+    sum_splits_kernel(const float *part, int splits, int64_t M, int N, int ld, T *out, int wide) {
     pdl_wait();
     pdl_trigger();
-    const int64_t step = (int64_t)gridDim.x * blockDim.x * N;
-    for (int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * N; i < n; i += step) {
-        float s[N];
+    const int pieces = ld / 4;
+    const int64_t n = M * pieces, step = (int64_t)gridDim.x * blockDim.x;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += step) {
+        const int64_t r = i / pieces;
+        const int c = (int)(i - r * pieces) * 4;
+        const float *from = part + r * ld + c;
+        float4 s = *reinterpret_cast<const float4 *>(from);
 #pragma unroll 4
-        for (int k = 0; k < splits; ++k) {
-            if constexpr (N == 4) {
-                const float4 x = *reinterpret_cast<const float4 *>(part + k * n + i);
-                const float v[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[j] = k ? s[j] + v[j] : v[j];
-            } else {
-                s[0] = k ? s[0] + part[k * n + i] : part[k * n + i];
-            }
+        for (int k = 1; k < splits; ++k) {
+            const float4 x = *reinterpret_cast<const float4 *>(from + k * M * ld);
+            s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
         }
-        if constexpr (N == 4 && sizeof(T) == 4) {
-            *reinterpret_cast<float4 *>(out + i) = make_float4(s[0], s[1], s[2], s[3]);
-        } else if constexpr (N == 4) {
-            __nv_bfloat162 b[2] = {__floats2bfloat162_rn(s[0], s[1]), __floats2bfloat162_rn(s[2], s[3])};
-            *reinterpret_cast<uint2 *>(out + i) = *reinterpret_cast<const uint2 *>(b);
-        } else {
-            out[i] = from_f<T>(s[0]);
+        T *to = out + r * N + c;
+        if (!wide) {
+            const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (c + k < N) to[k] = from_f<T>(v[k]);
+        } else if constexpr (sizeof(T) == 4) {
+            if (c < N) *reinterpret_cast<float4 *>(to) = s;
+        } else if (c < N) {
+            const __nv_bfloat162 b[2] = {__floats2bfloat162_rn(s.x, s.y),
+                                         __floats2bfloat162_rn(s.z, s.w)};
+            *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(b);
         }
     }
 }
@@ -489,8 +510,8 @@ BackwardLayout backward_layout(int32_t dtype, int64_t T, int64_t V, int32_t D) {
     l.w = pad256(T * es);
     l.g = l.w + pad256(l.piece * es);
     l.dx = l.g + pad256(P * T * l.ld * 2);
-    l.dw = l.dx + (l.dx_splits > 1 || l.piece < V ? pad256(4 * l.dx_splits * T * D) : 0);
-    l.total = l.dw + (l.dw_splits > 1 ? pad256(4 * l.dw_splits * l.piece * D) : 0) + 256;
+    l.dw = l.dx + (l.dx_splits > 1 || l.piece < V ? pad256(4 * l.dx_splits * T * padded(D)) : 0);
+    l.total = l.dw + (l.dw_splits > 1 ? pad256(4 * l.dw_splits * l.piece * padded(D)) : 0) + 256;
     return l;
 }
 
@@ -597,14 +618,12 @@ cudaError_t backward(const ultramem_cross_entropy_args *p, const BackwardLayout 
     float *dx_sum = dx_parts ? reinterpret_cast<float *>(ws + l.dx) : nullptr;
     float *dw_sum = l.dw_splits > 1 ? reinterpret_cast<float *>(ws + l.dw) : nullptr;
     auto wide = [&](const void *at) { return (uintptr_t)at % 32 == 0 && D * sizeof(T) % 32 == 0; };
-    auto sum_splits = [&](const float *part, int splits, int64_t n, T *out) {
-        const int64_t blocks = ceil_div(n, 1024), most = (int64_t)device_sm_count() * 16;
-        const dim3 grid((unsigned)(blocks < most ? blocks : most));
-        return n % 4 == 0 && (uintptr_t)out % 16 == 0
-                   ? launch_kernel(true, sum_splits_kernel<T, 4>, grid, 256, 0, st, part,
-                                          splits, n, out)
-                          : launch_kernel(true, sum_splits_kernel<T, 1>, grid, 256, 0, st, part,
-                                          splits, n, out);
+    auto sum_splits = [&](const float *part, int splits, int64_t m, T *out) {
+        const int64_t blocks = ceil_div(m * (Dp / 4), 256), most = (int64_t)device_sm_count() * 32;
+        return launch_kernel(true, sum_splits_kernel<T>,
+                             dim3((unsigned)(blocks < most ? blocks : most)), 256, 0, st, part,
+                             splits, m, D, (int)Dp, out,
+                             (int)((uintptr_t)out % 16 == 0 && D % 4 == 0));
     };
     for (int64_t v0 = 0; v0 < p->vocab && e == cudaSuccess; v0 += l.piece) {
         const int64_t vn = p->vocab - v0 < l.piece ? p->vocab - v0 : l.piece;
@@ -636,7 +655,7 @@ cudaError_t backward(const ultramem_cross_entropy_args *p, const BackwardLayout 
                 return cudaErrorInvalidValue;
             // one split: the last piece adds the others' sums and writes dx itself
             const bool here = l.dx_splits == 1 && v0 + vn == p->vocab;
-            const StoreEpi<T> se = {here ? static_cast<T *>(dx) : nullptr, dx_sum, N, D, v0 > 0,
+            const StoreEpi<T> se = {here ? static_cast<T *>(dx) : nullptr, dx_sum, N, D, Dp, v0 > 0,
                                     wide(dx)};
             e = multiply<StoreEpi<T>, false, true, P == 3>(ma, mb, plan, se, st);
         }
@@ -648,13 +667,13 @@ cudaError_t backward(const ultramem_cross_entropy_args *p, const BackwardLayout 
                 !operand(&mb, x.at, D, N, x.ld, x.planes, x.plane, 64))
                 return cudaErrorInvalidValue;
             T *out = static_cast<T *>(dw) + v0 * D;
-            const StoreEpi<T> se = {dw_sum ? nullptr : out, dw_sum, vn, D, 0, wide(out)};
+            const StoreEpi<T> se = {dw_sum ? nullptr : out, dw_sum, vn, D, Dp, 0, wide(out)};
             e = multiply<StoreEpi<T>, true, true, P == 3>(ma, mb, plan, se, st);
-            if (dw_sum && e == cudaSuccess) e = sum_splits(dw_sum, l.dw_splits, vn * D, out);
+            if (dw_sum && e == cudaSuccess) e = sum_splits(dw_sum, l.dw_splits, vn, out);
         }
     }
     if (dx && l.dx_splits > 1 && e == cudaSuccess)
-        e = sum_splits(dx_sum, l.dx_splits, N * D, static_cast<T *>(dx));
+        e = sum_splits(dx_sum, l.dx_splits, N, static_cast<T *>(dx));
     return e;
 }
 

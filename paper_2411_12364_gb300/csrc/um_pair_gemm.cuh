@@ -42,13 +42,19 @@ constexpr int kTileM = 256;
 constexpr uint32_t kOperand = 128 * 128;                  // 128 rows (or columns) x 64 k
 constexpr uint32_t kGroupBytes = 64 * 128;                // MN-major: 64 columns x 64 k
 
+// Shared memory of an epilogue warp, to turn rows by threads into rows by
+// lanes (17 floats a row: no bank conflicts either way).
+struct Scratch {
+    float v[32][17];
+};
+
 template <bool EXACT> struct Shape {
     static constexpr int kMaxN = EXACT ? 128 : 256;
     static constexpr int kPlanes = EXACT ? 3 : 1;
     static constexpr int kStages = EXACT ? 3 : 6;
     static constexpr uint32_t kB = kOperand * kMaxN / 256;        // a CTA's half of the columns
     static constexpr uint32_t kStage = kPlanes * (kOperand + kB);
-    static constexpr size_t kSmem = (size_t)kStages * kStage + 1024;
+    static constexpr size_t kSmem = (size_t)kStages * kStage + 1024 + 4 * sizeof(Scratch);
 };
 
 struct Plan {
@@ -153,8 +159,9 @@ __device__ __forceinline__ void tmem_store32(uint32_t taddr, const float (&v)[32
     }
 }
 
-// Epi: epi(tile, row, tmem, plan) by the 128 threads of the epilogue, row =
-// the tile's row (0..255) of this thread, tmem = its accumulators' address.
+// Epi: epi(tile, row, tmem, plan, scratch) by the 128 threads of the epilogue,
+// row = the tile's row (0..255) of this thread, tmem = its accumulators' address,
+// scratch the warp's.
 template <class Epi, bool A_MN, bool B_MN, bool EXACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap map_a,
@@ -310,6 +317,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int quarter = w & 3;
         const int row = 128 * (int)rank + quarter * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+        Scratch &scratch = reinterpret_cast<Scratch *>(ring + (size_t)kStages * S::kStage)[quarter];
         uint32_t n = 0;
         for (int item = first; ok && item < items; item += step) {
             const Tile t(p, item);
@@ -334,13 +342,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     }
                     tc::tmem_st_wait();
                 } else {
-                    epi(t, row, lanes + buf * S::kMaxN, p);
+                    epi(t, row, lanes + buf * S::kMaxN, p, scratch);
                 }
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) remote_arrive(tc::mapa_shared(tc::smem_u32(&acc_empty[buf]), 0));
             }
-            if (EXACT && ok) epi(t, row, lanes + 2 * S::kMaxN, p);
+            if (EXACT && ok) epi(t, row, lanes + 2 * S::kMaxN, p, scratch);
         }
         if (!ok && lane == 0) atomicOr(p.err, kErrTimeout);
     }
