@@ -99,18 +99,20 @@ __global__ void __launch_bounds__(256)
 
 struct LseEpi {
     Labels labels;
-    float2 *part;             // [tiles][T]: maximum (log2 units) and sum
+    float2 *part;             // [half tiles][T]: maximum (log2 units) and sum
     float *target;            // [T]: the label's logit
-    int T, vn, v0, tile0;     // columns of the piece, its first one, its first tile
+    int T, vn, v0, tile0;     // columns of the piece, its first one, its first half tile
+    int n_tile;
     float scale, scale_log2;
 
+    template <class Turn>
     __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
-                                               const pair::Plan &p, pair::Scratch &scratch) const {
+                                               int half, int c0, int c1, Turn &scratch) const {
         const int64_t tok = t.m0 + row;
         const int label = tok < T ? labels(tok) - (v0 + t.n0) : -1;   // the tile's column
-        const int cols = min(p.n_tile, vn - t.n0);
+        const int cols = min(c1, vn - t.n0);
         float m = -INFINITY, l = 0.f;
-        for (int c = 0; c < cols; c += 32) {
+        for (int c = c0; c < cols; c += 32) {
             float z[32];
             pair::load32(tmem + c, z);
             if (label >= c && label < c + 32) {
@@ -136,7 +138,7 @@ struct LseEpi {
             l = fmaf(l, tc::ex2(m - shift), (s[0] + s[1]) + (s[2] + s[3]));
             m = top;
         }
-        if (tok < T) part[(int64_t)(tile0 + t.n0 / p.n_tile) * T + tok] = make_float2(m, l);
+        if (tok < T) part[(int64_t)(tile0 + 2 * (t.n0 / n_tile) + half) * T + tok] = make_float2(m, l);
     }
 };
 
@@ -210,16 +212,17 @@ template <int P> struct GradEpi {
     int T, vn, v0;
     float scale, scale_log2;
 
+    template <class Turn>
     __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
-                                               const pair::Plan &p, pair::Scratch &scratch) const {
+                                               int half, int c0, int c1, Turn &scratch) const {
         const int64_t tok = t.m0 + row;
         const bool live = tok < T;
         const int label = live ? labels(tok) : -1;
         const int at = label - (v0 + t.n0);
         const float d = label >= 0 ? dloss[tok] * scale : 0.f;
         const float shift = label >= 0 ? -lse[tok] * kLog2e : 0.f;
-        const int cols = min(p.n_tile, vn - t.n0);
-        for (int c = 0; c < cols; c += 32) {
+        const int cols = min(c1, vn - t.n0);
+        for (int c = c0; c < cols; c += 32) {
             float z[32];
             pair::load32(tmem + c, z);
             if (!live) continue;
@@ -251,7 +254,7 @@ template <int P> struct GradEpi {
 // A product's rows [M][N], with `add` on top of what part [splits][M][ld] (fp32,
 // ld a multiple of 8) holds: to `out` in T, or without it back to part.  Where
 // out's rows allow 32-byte stores (`wide`), each thread stores its row; else a
-// warp turns 16 columns of its 32 rows at a time, so that lanes store
+// warp turns 8 or 16 columns of its 32 rows at a time, so that lanes store
 // neighbours (one by one, a column of 32 rows at a time, an odd width made the
 // gradient of 333 tokens against 5003 x 509 LATER instead of LATER us).
 template <typename T> struct StoreEpi {
@@ -260,11 +263,12 @@ template <typename T> struct StoreEpi {
     int64_t M, N, ld;
     int add, wide;
 
+    template <class Turn>
     __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
-                                               const pair::Plan &p, pair::Scratch &scratch) const {
+                                               int half, int c0, int c1, Turn &scratch) const {
         const int64_t r = t.m0 + row;
-        const int cols = (int)min((int64_t)p.n_tile, N - t.n0), lane = threadIdx.x & 31;
-        for (int c = 0; c < cols; c += 32) {
+        const int cols = (int)min((int64_t)c1, N - t.n0), lane = threadIdx.x & 31;
+        for (int c = c0; c < cols; c += 32) {
             float v[32];
             pair::load32(tmem + c, v);
             const int left = cols - c;
@@ -294,18 +298,19 @@ template <typename T> struct StoreEpi {
             }
             if (!out || (wide && left >= 32)) continue;
             const int64_t row0 = r - lane;
+            constexpr int W = Turn::kCols, kRows = 32 / W;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (16 * h >= left) break;
+            for (int h = 0; h < 32; h += W) {
+                if (h >= left) break;
                 __syncwarp();
 #pragma unroll
-                for (int k = 0; k < 16; ++k) scratch.v[lane][k] = v[16 * h + k];
+                for (int k = 0; k < W; ++k) scratch.v[lane][k] = v[h + k];
                 __syncwarp();
-                const int k = lane & 15;
+                const int k = lane % W;
 #pragma unroll 8
-                for (int i = lane >> 4; i < 32; i += 2)
-                    if (row0 + i < M && 16 * h + k < left)
-                        out[(row0 + i) * N + t.n0 + c + 16 * h + k] = from_f<T>(scratch.v[i][k]);
+                for (int i = lane / W; i < 32; i += kRows)
+                    if (row0 + i < M && h + k < left)
+                        out[(row0 + i) * N + t.n0 + c + h + k] = from_f<T>(scratch.v[i][k]);
             }
         }
     }
@@ -360,8 +365,9 @@ int planes_of(int32_t dtype) { return dtype == ULTRAMEM_F32 ? 3 : 1; }
 // fewer tiles than pairs of SMs.
 // n_tile: the widest tile, unless narrower ones share out among the pairs more
 // evenly; `step` 32, or 128 where the columns are MN-major (boxes of 64 columns a CTA).
-// splits (at most `most`, 64 or fewer): a tile's time is its k blocks (512 cycles each) and
-// about 3000 cycles; a split costs a pass over the output in fp32.
+// splits (at most `most`, 64 or fewer): a tile's time is its k blocks (2 cycles a
+// column, and no less than 480 for the copies: 128 columns took 615) and about 3000
+// cycles; a split costs a pass over the output in fp32.
 pair::Plan plan_of(int64_t M, int64_t N, int64_t K, int planes, int step, int most) {
     pair::Plan p = {};
     const int64_t pairs = pairs_of_sms();
@@ -375,7 +381,8 @@ pair::Plan plan_of(int64_t M, int64_t N, int64_t K, int planes, int step, int mo
         for (int s = 1; s <= most && s <= p.k_blocks; ++s) {
             if (s > 1 && p.m_tiles * nt * (s - 1) >= 2 * pairs) break;
             const int64_t waves = ceil_div(p.m_tiles * nt * s, pairs);
-            const double tile = (double)ceil_div(p.k_blocks, s) * pairs_of_planes * 2.0 * n + 3000.0;
+            const double block = pairs_of_planes * 2.0 * n;
+            const double tile = (double)ceil_div(p.k_blocks, s) * (block > 480. ? block : 480.) + 3000.0;
             // 2000 cycles and s writes and reads of the output at 3 KB a cycle
             const double join = s > 1 ? 2000.0 + (double)M * N * 8.0 * s / 3000.0 : 0.0;
             const double cost = waves * tile + join;
@@ -463,14 +470,14 @@ int64_t piece_of(int64_t V, int64_t limit) {
 
 struct ForwardLayout {
     int64_t piece;            // of the vocabulary, when the weights are rearranged
-    int64_t tiles;            // of all pieces, at most
+    int64_t tiles;            // half tiles of all pieces, at most
     int64_t part, target, x, w, total;
 };
 ForwardLayout forward_layout(int32_t dtype, int64_t T, int64_t V, int32_t D) {
     ForwardLayout l = {};
     l.piece = piece_of(V, rows_in_planes(dtype, D));
     // a tile is at least 128 columns wide, and pieces are whole tiles but for the last of each
-    l.tiles = ceil_div(V, 128) + ceil_div(V, l.piece);
+    l.tiles = 2 * (ceil_div(V, 128) + ceil_div(V, l.piece));
     const int64_t es = planes_of(dtype) * padded(D) * 2;
     l.part = 0;
     l.target = pad256(l.tiles * T * 8);
@@ -577,9 +584,10 @@ cudaError_t forward(const ultramem_cross_entropy_args *p, const ForwardLayout &l
             return cudaErrorInvalidValue;
         epi.vn = (int)vn;
         epi.v0 = (int)v0;
+        epi.n_tile = plan.n_tile;
         e = P == 3 ? multiply<LseEpi, false, false, true>(ma, mb, plan, epi, st)
                    : multiply<LseEpi, false, false, false>(ma, mb, plan, epi, st);
-        epi.tile0 += plan.n_tiles;
+        epi.tile0 += 2 * plan.n_tiles;
         pdl = true;
     }
     if (e != cudaSuccess) return e;

@@ -27,7 +27,8 @@
 // so; LATER us.)
 //
 // Warps of a CTA: 0 copies (TMA, one elected thread), 1 products (one thread
-// of the pair's first CTA), 2-5 epilogue.  Waits are bounded; one that gives
+// of the pair's first CTA), 2-9 epilogue (four for each half of the columns: with
+// four in all, tiles of up to 16 k blocks took as long as their epilogue).  Waits are bounded; one that gives
 // up sets the error word, and the others run into their own limits.
 #pragma once
 
@@ -37,15 +38,17 @@
 namespace um {
 namespace pair {
 
-constexpr int kThreads = 192;
+constexpr int kEpilogue = 8;                             // warps
+constexpr int kThreads = (2 + kEpilogue) * 32;
 constexpr int kTileM = 256;
 constexpr uint32_t kOperand = 128 * 128;                  // 128 rows (or columns) x 64 k
 constexpr uint32_t kGroupBytes = 64 * 128;                // MN-major: 64 columns x 64 k
 
 // Shared memory of an epilogue warp, to turn rows by threads into rows by
-// lanes (17 floats a row: no bank conflicts either way).
-struct Scratch {
-    float v[32][17];
+// lanes (an odd row: no bank conflicts either way).
+template <int COLS> struct Scratch {
+    static constexpr int kCols = COLS;
+    float v[32][COLS + 1];
 };
 
 template <bool EXACT> struct Shape {
@@ -54,7 +57,8 @@ template <bool EXACT> struct Shape {
     static constexpr int kStages = EXACT ? 3 : 6;
     static constexpr uint32_t kB = kOperand * kMaxN / 256;        // a CTA's half of the columns
     static constexpr uint32_t kStage = kPlanes * (kOperand + kB);
-    static constexpr size_t kSmem = (size_t)kStages * kStage + 1024 + 4 * sizeof(Scratch);
+    using Turn = Scratch<EXACT ? 8 : 16>;                         // what fits
+    static constexpr size_t kSmem = (size_t)kStages * kStage + 1024 + kEpilogue * sizeof(Turn);
 };
 
 struct Plan {
@@ -159,9 +163,10 @@ __device__ __forceinline__ void tmem_store32(uint32_t taddr, const float (&v)[32
     }
 }
 
-// Epi: epi(tile, row, tmem, plan, scratch) by the 128 threads of the epilogue,
-// row = the tile's row (0..255) of this thread, tmem = its accumulators' address,
-// scratch the warp's.
+// Epi: epi(tile, row, tmem, half, c0, c1, scratch) by the threads of the epilogue:
+// the tile's row (0..255) of this thread, its accumulators' address, which half of
+// the columns is its and that half's columns [c0, c1) (c0 a multiple of 32), the
+// warp's scratch.
 template <class Epi, bool A_MN, bool B_MN, bool EXACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap map_a,
@@ -181,7 +186,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
         for (int i = 0; i < 2; ++i) {
             tc::mbar_init(&acc_full[i], 1);
-            tc::mbar_init(&acc_empty[i], 8);     // the epilogue warps of both CTAs
+            tc::mbar_init(&acc_empty[i], 2 * kEpilogue);   // the warps of both CTAs
         }
         tc::mbar_init(&drained, 1);
         tc::fence_mbar_init();
@@ -317,7 +322,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int quarter = w & 3;
         const int row = 128 * (int)rank + quarter * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-        Scratch &scratch = reinterpret_cast<Scratch *>(ring + (size_t)kStages * S::kStage)[quarter];
+        typename S::Turn &scratch =
+            reinterpret_cast<typename S::Turn *>(ring + (size_t)kStages * S::kStage)[w - 2];
+        const int half = (w - 2) >> 2, middle = (p.n_tile / 2 + 31) & ~31;
+        const int c0 = half ? middle : 0, c1 = half ? p.n_tile : middle;
         uint32_t n = 0;
         for (int item = first; ok && item < items; item += step) {
             const Tile t(p, item);
@@ -329,7 +337,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 tc::tc_fence_after();
                 if constexpr (EXACT) {
                     const uint32_t from = lanes + buf * S::kMaxN, sum = lanes + 2 * S::kMaxN;
-                    for (int c = 0; c < p.n_tile; c += 32) {
+                    for (int c = c0; c < c1; c += 32) {
                         float v[32];
                         load32(from + c, v);
                         if (i > 0) {
@@ -342,13 +350,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     }
                     tc::tmem_st_wait();
                 } else {
-                    epi(t, row, lanes + buf * S::kMaxN, p, scratch);
+                    epi(t, row, lanes + buf * S::kMaxN, half, c0, c1, scratch);
                 }
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) remote_arrive(tc::mapa_shared(tc::smem_u32(&acc_empty[buf]), 0));
             }
-            if (EXACT && ok) epi(t, row, lanes + 2 * S::kMaxN, p, scratch);
+            if (EXACT && ok) epi(t, row, lanes + 2 * S::kMaxN, half, c0, c1, scratch);
         }
         if (!ok && lane == 0) atomicOr(p.err, kErrTimeout);
     }
