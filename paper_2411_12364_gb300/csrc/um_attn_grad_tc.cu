@@ -468,6 +468,16 @@ __device__ __forceinline__ void run(uint8_t *sm, const CUtensorMap &map_h0,
     } else if (w == kSoftmax + 2) {
         uint32_t l_raw = 0, s_raw = 0;         // phases, a bit a stage
         const int from = wk.n & (kRows - 1);
+        float2 ahead[kRows / 32];              // of the next step: in flight while this one runs
+        auto rows_of = [&](int j) {
+            const float2 *rows = a.rows + (int64_t)(wk.kv * a.group + wk.group_of(j)) * a.T + wk.tok0;
+#pragma unroll
+            for (int i = 0; i < kRows / 32; ++i) {
+                const int r = wk.block<KEYS>(j) * kRows + 32 * i + lane;
+                ahead[i] = r < wk.n ? rows[r] : make_float2(INFINITY, 0.f);
+            }
+        };
+        if (KEYS) rows_of(0);
         for (int j = 0; ok && j < steps; ++j) {
             const int b = wk.block<KEYS>(j);
             if (wk.tail(b)) {
@@ -487,15 +497,13 @@ __device__ __forceinline__ void run(uint8_t *sm, const CUtensorMap &map_h0,
             if (!KEYS) continue;
             const int st = j & 1;
             if (!(ok = tc::warp_wait(&bar.row_empty[st], ((j >> 1) & 1) ^ 1))) break;
-            const float2 *rows = a.rows + (int64_t)(wk.kv * a.group + wk.group_of(j)) * a.T + wk.tok0;
 #pragma unroll
-            for (int i = 0; i < kRows; i += 32) {
-                const int r = b * kRows + i + lane;
-                const float2 v = r < wk.n ? rows[r] : make_float2(INFINITY, 0.f);
-                row_lse[st * kRows + i + lane] = -v.x * kLog2e;
-                row_d[st * kRows + i + lane] = -v.y;
+            for (int i = 0; i < kRows / 32; ++i) {
+                row_lse[st * kRows + 32 * i + lane] = -ahead[i].x * kLog2e;
+                row_d[st * kRows + 32 * i + lane] = -ahead[i].y;
             }
             tc::mbar_arrive(&bar.row_full[st]);
+            if (j + 1 < steps) rows_of(j + 1);
         }
         if (!ok && lane == 0) atomicOr(a.err, kErrTimeout);
     }
