@@ -10,7 +10,9 @@ closes that the same way:
 
 Training: the gradient of the second half (block_norm around the memory
 layer's lookup) down to the value table, the slot weights, the projectors, the
-gains and the gate.
+gains and the gate; and a whole step of the first half between its ends, from
+token ids to the loss and back: embedding, attention of packed sequences,
+cross entropy against the same table, and the gradients of all of them.
 
     python examples/decoder_block.py [--steps N]
 """
@@ -28,8 +30,10 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2411_12364_gb300 import workloads  # noqa: E402
 from paper_2411_12364_gb300.binding import UltraMemLayer  # noqa: E402
 from paper_2411_12364_gb300.norms import block_norm, block_norm_backward  # noqa: E402
-from paper_2411_12364_gb300.paged import (paged_append, paged_attention, paged_check,  # noqa: E402
-                                          paged_plan)
+from paper_2411_12364_gb300.paged import (paged_append, paged_attention,  # noqa: E402
+                                          paged_attention_backward, paged_check, paged_plan)
+from paper_2411_12364_gb300.vocab import (cross_entropy, cross_entropy_backward,  # noqa: E402
+                                          embedding, embedding_backward)
 
 BF16 = torch.bfloat16
 
@@ -37,11 +41,11 @@ BF16 = torch.bfloat16
 class Cache:
     """Pages of one block's keys and values, and the pages' bookkeeping."""
 
-    def __init__(self, n_pages, requests, width, kv_heads, head_dim, page_size=16):
+    def __init__(self, n_pages, requests, width, kv_heads, head_dim, page_size=16, dtype=BF16):
         self.page_size = page_size
         shape = (n_pages, kv_heads, page_size, head_dim)
-        self.k = torch.zeros(shape, dtype=BF16, device="cuda")
-        self.v = torch.zeros(shape, dtype=BF16, device="cuda")
+        self.k = torch.zeros(shape, dtype=dtype, device="cuda")
+        self.v = torch.zeros(shape, dtype=dtype, device="cuda")
         self.table = torch.full((requests, width), -1, dtype=torch.int32, device="cuda")
         self.free_pages = torch.arange(n_pages, dtype=torch.int32, device="cuda")
         # the free list's length before and after a step change places
@@ -103,6 +107,61 @@ class DecoderBlock:
         return dict(g, dvalues=dvalues, dw=dw, dw_proj=dw_proj)
 
 
+class AttentionStep:
+    """One attention block between the ends of a language model, whose table
+    embeds the ids and scores the vocabulary."""
+
+    def __init__(self, vocab, dim, q_heads, kv_heads, head_dim, dtype=BF16, seed=0):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+
+        def randn(*shape, std=1.0):
+            return torch.randn(*shape, generator=gen, device="cuda") * std
+
+        self.heads, self.kv_heads, self.head_dim = q_heads, kv_heads, head_dim
+        self.scale = dim ** 0.5
+        self.table = randn(vocab, dim, std=dim ** -0.5).to(dtype)
+        self.w_qkv = randn((q_heads + 2 * kv_heads) * head_dim, dim, std=dim ** -0.5).to(dtype)
+        self.w_o = randn(dim, q_heads * head_dim, std=(q_heads * head_dim) ** -0.5).to(dtype)
+        self.w_in = 1 + 0.1 * randn(dim)              # the gain before attention
+        self.norm = dict(w_post=1 + 0.1 * randn(dim), gate=0.5 + 0.1 * randn(dim),
+                         w_pre=1 + 0.1 * randn(dim))
+
+    def step(self, ids, labels, lens):
+        """The tokens' losses and the gradient of their mean over the labelled
+        ones, for sequences of lens tokens (host numbers) packed in ids."""
+        h, hk, hd = self.heads, self.kv_heads, self.head_dim
+        x = embedding(self.table, ids, scale=self.scale)
+        none = torch.zeros_like(x)                    # no block before the first norm
+        _, n = block_norm(none, x, w_pre=self.w_in, post=False)
+        qkv = (n @ self.w_qkv.T).view(-1, h + 2 * hk, hd)
+        q, k, v = qkv[:, :h], qkv[:, h:h + hk], qkv[:, h + hk:]
+        pages = [-(-length // 16) for length in lens]
+        cache = Cache(sum(pages), len(lens), max(pages), hk, hd, dtype=x.dtype)
+        q_start, kv_lens, slots, max_new = cache.plan(lens)
+        paged_append(cache.k, cache.v, k, v, slots)
+        a, lse_rows = paged_attention(q, cache.k, cache.v, cache.table, q_start, kv_lens, max_new,
+                                      with_lse=True)
+        y = a.view(-1, h * hd) @ self.w_o.T
+        u, out = block_norm(y, x, **self.norm)
+        loss, lse = cross_entropy(out, self.table, labels)
+
+        counts = (labels >= 0) & (labels < self.table.shape[0])
+        dloss = counts.float() / counts.sum().clamp(min=1)
+        dout, dtable = cross_entropy_backward(out, self.table, labels, lse, dloss)
+        g = block_norm_backward(y, u, None, dout, **self.norm)
+        da = (g["dy"] @ self.w_o).view(-1, h, hd)
+        dqkv = torch.empty_like(qkv)
+        paged_attention_backward(q, k, v, a, lse_rows, da, q_start, dq=dqkv[:, :h],
+                                 dk=dqkv[:, h:h + hk], dv=dqkv[:, h + hk:])
+        flat = dqkv.view(dqkv.shape[0], -1)
+        g_in = block_norm_backward(none, x, g["dr"], flat @ self.w_qkv, w_pre=self.w_in, post=False)
+        embedding_backward(ids, g_in["dr"], self.table.shape[0], scale=self.scale, dtable=dtable,
+                           accumulate=True)
+        return loss, dict(table=dtable, w_qkv=flat.T @ n, w_o=g["dy"].T @ a.view(-1, h * hd),
+                          w_in=g_in["dw_pre"], w_post=g["dw_post"], gate=g["dgate"],
+                          w_pre=g["dw_pre"])
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--steps", type=int, default=4, help="decode steps after the prompts")
@@ -127,6 +186,11 @@ def main():
     grads = block.memory_gradient(u, n, du, dn)
     print("gradients:", ", ".join(f"{k} {tuple(v.shape)}" for k, v in grads.items()
                                   if v is not None))
+    model = AttentionStep(vocab=5000, dim=512, q_heads=8, kv_heads=2, head_dim=64)
+    ids = torch.randint(0, 5000, (sum(prompts),), generator=gen, device="cuda")
+    loss, grads = model.step(ids, ids.roll(-1), prompts)
+    print(f"loss {loss.mean().item():.3f}, gradients:",
+          ", ".join(f"{k} {tuple(v.shape)}" for k, v in grads.items()))
     assert block.layer.check() == 0 and paged_check() == 0
     block.layer.close()
 

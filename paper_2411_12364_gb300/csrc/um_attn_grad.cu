@@ -413,7 +413,7 @@ int block_of(int32_t dim) { return dim > 128 ? 32 : 64; }
 // Blocks of the sequences, at most: whole ones, and a short one for each that
 // has tokens.
 int64_t most_blocks(int32_t T, int32_t n_seqs, int block) {
-    return T / block + (n_seqs < T ? n_seqs : T);
+    return (int64_t)T / block + (n_seqs < T ? n_seqs : T);
 }
 
 struct Layout {

@@ -24,7 +24,7 @@
 // (24 steps), and the epilogue adds it to the tile's sum (rounded to
 // nearest), which it keeps in TMEM beside the two accumulators.  (Gradient of
 // 333 tokens against 5003 x 509: relative error 3e-6 with one sum a tile, 4e-7
-// so; LATER us.)
+// so; 146 us with each pair of planes copied for itself, 111 so.)
 //
 // Warps of a CTA: 0 copies (TMA, one elected thread), 1 products (one thread
 // of the pair's first CTA), 2-9 epilogue (four for each half of the columns: with

@@ -209,6 +209,10 @@ def paged_attention_backward(q, k, v, out, lse, dout, q_start, scale=None, dq=No
         raise ValueError("q, k and v must be [tokens, heads, head_dim], fp32 or bf16")
     T, H, D = q.shape
     heads, dtype = k.shape[1], q.dtype
+    R = q_start.numel() - 1
+    if R < 0 or q_start.dim() != 1:
+        raise ValueError("q_start must have an entry more than there are sequences")
+    _b._fits_int32(T, R, k.shape[0])
     q, qs = _rows("q", q, H, D, dtype, dev)
     out, os = _rows("out", out, H, D, dtype, dev)
     dout, ds = _rows("dout", dout, H, D, dtype, dev)
@@ -219,10 +223,6 @@ def paged_attention_backward(q, k, v, out, lse, dout, q_start, scale=None, dq=No
     if lse.shape != (T, H) or lse.dtype != torch.float32 or lse.get_device() != dev or \
             not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 tensor [tokens, q_heads] on q's device")
-    R = q_start.numel() - 1
-    if R < 0:
-        raise ValueError("q_start must have an entry more than there are sequences")
-    _b._fits_int32(T, R)
     starts = _int32("q_start", q_start, dev)
     grads, strides = [], []
     for name, t, shape in (("dq", dq, (T, H, D)), ("dk", dk, (T, heads, D)),

@@ -37,6 +37,7 @@ def _matrix(name, t, dev):
                          "device")
     if shape[1] < 1:
         raise ValueError(f"{name} must have columns")
+    _b._fits_int32(*shape)
     s0, s1 = t.stride()
     if (s1 == 1 or shape[1] == 1) and (s0 >= shape[1] or shape[0] <= 1):
         return t, max(s0, shape[1])
@@ -74,7 +75,7 @@ def embedding(table, ids, scale: float = 1.0, out=None):
     table, ld = _matrix("table", table, dev)
     V, D = table.shape
     T = ids.numel()
-    _b._fits_int32(T, V, D)
+    _b._fits_int32(T)
     p_ids, ids_bytes = _ids("ids", ids, T, dev)
     if out is None:
         out = torch.empty((T, D), dtype=table.dtype, device=table.device)
@@ -104,7 +105,7 @@ def embedding_backward(ids, dout, vocab: int, scale: float = 1.0, dtable=None,
     dev = _b._on_device("dout", dout)
     dout, ld = _matrix("dout", dout, dev)
     T, D = dout.shape
-    _b._fits_int32(T, D, vocab)
+    _b._fits_int32(vocab)
     p_ids, ids_bytes = _ids("ids", ids, T, dev)
     if dtable is not None:
         if dtable.dtype not in _DTYPES:
@@ -136,7 +137,6 @@ def _ce_args(x, w, labels, logit_scale):
     V = w.shape[0]
     if w.shape[1] != D or w.dtype != x.dtype:
         raise ValueError("w must be [vocab, dim] of x's type")
-    _b._fits_int32(T, V, D)
     p_labels, labels_bytes = _ids("labels", labels, T, dev)
     a = _b.CrossEntropyArgs(x.data_ptr(), w.data_ptr(), p_labels, ld_x, ld_w, T, V, D,
                             _DTYPES[x.dtype], labels_bytes, logit_scale)
