@@ -18,6 +18,7 @@
 #include "um_device.cuh"
 #include "um_overlap.cuh"
 #include "um_paged.cuh"
+#include "um_pair.cuh"
 #include "um_pair_gemm.cuh"
 
 namespace um {
@@ -97,7 +98,12 @@ __global__ void __launch_bounds__(256)
 
 // ---- forward -------------------------------------------------------------------
 
-struct LseEpi {
+// Its results are fp32: past kLongSum entries a row the sums in the tensor cores
+// are cut (lse of 2048 entries off by 6e-7 of its size, growing with the
+// entries; in sums of 1024 by 4e-7, and 16384 x 32000 x 2048 in 1366 instead of 1314 us).
+constexpr int kLongSum = 2048;
+template <int SUM> struct LseEpi {
+    static constexpr int kSumBlocks = SUM;
     Labels labels;
     float2 *part;             // [half tiles][T]: maximum (log2 units) and sum
     float *target;            // [T]: the label's logit
@@ -105,37 +111,56 @@ struct LseEpi {
     int n_tile;
     float scale, scale_log2;
 
-    template <class Turn>
-    __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
-                                               int half, int c0, int c1, Turn &scratch) const {
+    template <int N> LseEpi<N> cut() const {
+        return {labels, part, target, T, vn, v0, tile0, n_tile, scale, scale_log2};
+    }
+    __device__ __forceinline__ int fetch(const pair::Tile &t, int row) const {
         const int64_t tok = t.m0 + row;
-        const int label = tok < T ? labels(tok) - (v0 + t.n0) : -1;   // the tile's column
+        return tok < T ? labels(tok) - (v0 + t.n0) : -1;     // the tile's column
+    }
+    template <class Sums, class Turn>
+    __device__ __forceinline__ void operator()(const pair::Tile &t, int row, Sums &sums,
+                                               int half, int c0, int c1, int label,
+                                               Turn &scratch) const {
+        const int64_t tok = t.m0 + row;
         const int cols = min(c1, vn - t.n0);
+        // to log2 units; where the scale is negative the sums change their sign first,
+        // and where it is 0 they become 0
+        const float by = scale_log2 == 0.f ? 1.f : fabsf(scale_log2);
         float m = -INFINITY, l = 0.f;
-        for (int c = c0; c < cols; c += 32) {
-            float z[32];
-            pair::load32(tmem + c, z);
+#pragma unroll
+        for (int i = 0; i < Sums::kChunks; ++i) {
+            const int c = c0 + 32 * i;
+            if (c >= cols) break;
+            float place[32];
+            float (&z)[32] = sums.get(i, place);
             if (label >= c && label < c + 32) {
 #pragma unroll
                 for (int k = 0; k < 32; ++k)
                     if (label == c + k) target[tok] = z[k] * scale;
             }
-            float top = -INFINITY;
+            if (scale_log2 <= 0.f) {
 #pragma unroll
-            for (int k = 0; k < 32; ++k) z[k] *= scale_log2;
+                for (int k = 0; k < 32; ++k) z[k] = scale_log2 < 0.f ? -z[k] : z[k] * 0.f;
+            }
             if (c + 32 > cols) {
 #pragma unroll
                 for (int k = 0; k < 32; ++k)
                     if (c + k >= cols) z[k] = -INFINITY;
             }
+            float top = fmaxf(z[0], z[1]);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) top = fmaxf(top, z[k]);
-            top = fmaxf(m, top);
+            for (int k = 2; k < 32; k += 2) top = max3(top, z[k], z[k + 1]);
+            top = fmaxf(m, top * by);
             const float shift = top == -INFINITY ? 0.f : top;
-            float s[4] = {0.f, 0.f, 0.f, 0.f};
+            const F2 f = f2(by), less = f2(-shift);
+            F2 s[2] = {f2(0.f), f2(0.f)};
 #pragma unroll
-            for (int k = 0; k < 32; ++k) s[k & 3] += tc::ex2(z[k] - shift);
-            l = fmaf(l, tc::ex2(m - shift), (s[0] + s[1]) + (s[2] + s[3]));
+            for (int k = 0; k < 32; k += 2) {
+                const float2 y = split(fma2(f2(z[k], z[k + 1]), f, less));
+                s[(k >> 1) & 1] = s[(k >> 1) & 1] + f2(tc::ex2(y.x), tc::ex2(y.y));
+            }
+            l = fmaf(l, tc::ex2(m - shift), both(s[0] + s[1]));
             m = top;
         }
         if (tok < T) part[(int64_t)(tile0 + 2 * (t.n0 / n_tile) + half) * T + tok] = make_float2(m, l);
@@ -205,6 +230,7 @@ template <typename T> __device__ __forceinline__ void store32(T *to, const float
 // P planes of G [P][T][ld]; ld is a multiple of 32, and columns up to the next
 // multiple of 32 past vn are written (as zeros).
 template <int P> struct GradEpi {
+    static constexpr int kSumBlocks = 0;
     Labels labels;
     const float *lse, *dloss;
     __nv_bfloat16 *g;
@@ -212,19 +238,31 @@ template <int P> struct GradEpi {
     int T, vn, v0;
     float scale, scale_log2;
 
-    template <class Turn>
-    __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
-                                               int half, int c0, int c1, Turn &scratch) const {
+    struct Row {
+        int label;
+        float d, shift;
+    };
+    __device__ __forceinline__ Row fetch(const pair::Tile &t, int row) const {
+        const int64_t tok = t.m0 + row;
+        const int label = tok < T ? labels(tok) : -1;
+        return {label, label >= 0 ? dloss[tok] * scale : 0.f,
+                label >= 0 ? -lse[tok] * kLog2e : 0.f};
+    }
+    template <class Sums, class Turn>
+    __device__ __forceinline__ void operator()(const pair::Tile &t, int row, Sums &sums,
+                                               int half, int c0, int c1, const Row &r,
+                                               Turn &scratch) const {
         const int64_t tok = t.m0 + row;
         const bool live = tok < T;
-        const int label = live ? labels(tok) : -1;
-        const int at = label - (v0 + t.n0);
-        const float d = label >= 0 ? dloss[tok] * scale : 0.f;
-        const float shift = label >= 0 ? -lse[tok] * kLog2e : 0.f;
+        const int label = r.label, at = label - (v0 + t.n0);
+        const float d = r.d, shift = r.shift;
         const int cols = min(c1, vn - t.n0);
-        for (int c = c0; c < cols; c += 32) {
-            float z[32];
-            pair::load32(tmem + c, z);
+#pragma unroll
+        for (int i = 0; i < Sums::kChunks; ++i) {
+            const int c = c0 + 32 * i;
+            if (c >= cols) break;
+            float place[32];
+            float (&z)[32] = sums.get(i, place);
             if (!live) continue;
 #pragma unroll
             for (int k = 0; k < 32; ++k) z[k] = tc::ex2(fmaf(z[k], scale_log2, shift));
@@ -258,19 +296,24 @@ template <int P> struct GradEpi {
 // neighbours (each thread along its row: gradient of 333 tokens against 5003 x
 // 509 111 us, so 96).
 template <typename T> struct StoreEpi {
+    static constexpr int kSumBlocks = 0;
     T *out;
     float *part;
     int64_t M, N, ld;
     int add, wide;
 
-    template <class Turn>
-    __device__ __forceinline__ void operator()(const pair::Tile &t, int row, uint32_t tmem,
-                                               int half, int c0, int c1, Turn &scratch) const {
+    __device__ __forceinline__ int fetch(const pair::Tile &, int) const { return 0; }
+    template <class Sums, class Turn>
+    __device__ __forceinline__ void operator()(const pair::Tile &t, int row, Sums &sums,
+                                               int half, int c0, int c1, int, Turn &scratch) const {
         const int64_t r = t.m0 + row;
         const int cols = (int)min((int64_t)c1, N - t.n0), lane = threadIdx.x & 31;
-        for (int c = c0; c < cols; c += 32) {
-            float v[32];
-            pair::load32(tmem + c, v);
+#pragma unroll
+        for (int j = 0; j < Sums::kChunks; ++j) {
+            const int c = c0 + 32 * j;
+            if (c >= cols) break;
+            float place[32];
+            float (&x)[32] = sums.get(j, place);
             const int left = cols - c;
             if (r < M) {
                 float *sum = part + ((int64_t)t.split * M + r) * ld + t.n0 + c;
@@ -278,22 +321,22 @@ template <typename T> struct StoreEpi {
 #pragma unroll
                     for (int k = 0; k < 32; k += 4) {
                         if (k >= left) break;            // rows are padded to 8
-                        const float4 x = *reinterpret_cast<const float4 *>(sum + k);
-                        v[k] += x.x, v[k + 1] += x.y, v[k + 2] += x.z, v[k + 3] += x.w;
+                        const float4 y = *reinterpret_cast<const float4 *>(sum + k);
+                        x[k] += y.x, x[k + 1] += y.y, x[k + 2] += y.z, x[k + 3] += y.w;
                     }
                 }
                 if (!out) {
 #pragma unroll
                     for (int k = 0; k < 32; k += 8) {
                         if (k >= left) break;
-                        const uint32_t o[8] = {__float_as_uint(v[k]),     __float_as_uint(v[k + 1]),
-                                               __float_as_uint(v[k + 2]), __float_as_uint(v[k + 3]),
-                                               __float_as_uint(v[k + 4]), __float_as_uint(v[k + 5]),
-                                               __float_as_uint(v[k + 6]), __float_as_uint(v[k + 7])};
+                        const uint32_t o[8] = {__float_as_uint(x[k]),     __float_as_uint(x[k + 1]),
+                                               __float_as_uint(x[k + 2]), __float_as_uint(x[k + 3]),
+                                               __float_as_uint(x[k + 4]), __float_as_uint(x[k + 5]),
+                                               __float_as_uint(x[k + 6]), __float_as_uint(x[k + 7])};
                         store_sector(sum + k, o);
                     }
                 } else if (wide && left >= 32) {
-                    store32(out + r * N + t.n0 + c, v);
+                    store32(out + r * N + t.n0 + c, x);
                 }
             }
             if (!out || (wide && left >= 32)) continue;
@@ -304,7 +347,7 @@ template <typename T> struct StoreEpi {
                 if (h >= left) break;
                 __syncwarp();
 #pragma unroll
-                for (int k = 0; k < W; ++k) scratch.v[lane][k] = v[h + k];
+                for (int k = 0; k < W; ++k) scratch.v[lane][k] = x[h + k];
                 __syncwarp();
                 const int k = lane % W;
 #pragma unroll 8
@@ -566,7 +609,7 @@ cudaError_t forward(const ultramem_cross_entropy_args *p, const ForwardLayout &l
     }
     const bool direct = as_it_lies(p->dtype, p->w, p->ld_w, T, kMostForward);
     const int64_t piece = direct ? p->vocab : l.piece;
-    LseEpi epi = {};
+    LseEpi<0> epi = {};
     epi.labels = labels_of(p);
     epi.part = reinterpret_cast<float2 *>(ws + l.part);
     epi.target = reinterpret_cast<float *>(ws + l.target);
@@ -590,8 +633,12 @@ cudaError_t forward(const ultramem_cross_entropy_args *p, const ForwardLayout &l
         epi.vn = (int)vn;
         epi.v0 = (int)v0;
         epi.n_tile = plan.n_tile;
-        e = P == 3 ? multiply<LseEpi, false, false, true>(ma, mb, plan, epi, st)
-                   : multiply<LseEpi, false, false, false>(ma, mb, plan, epi, st);
+        if (P == 3)
+            e = multiply<LseEpi<0>, false, false, true>(ma, mb, plan, epi, st);
+        else if (D <= kLongSum)
+            e = multiply<LseEpi<0>, false, false, false>(ma, mb, plan, epi, st);
+        else
+            e = multiply<LseEpi<16>, false, false, false>(ma, mb, plan, epi.cut<16>(), st);
         epi.tile0 += 2 * plan.n_tiles;
         pdl = true;
     }

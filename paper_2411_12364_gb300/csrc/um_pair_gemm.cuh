@@ -15,16 +15,20 @@
 // k, the row index of A or B contiguous), so that a matrix and its transpose
 // are read from the same memory.
 //
+// The tensor cores cut off what a sum loses in its last place, so a sum of many
+// steps of 16 k comes out short: logits of 2048 k by 1e-6 of their size.  That is
+// far below a rounding to bf16 but not below fp32.  An operation with kSumBlocks
+// ends the sum in the tensor cores after so many k blocks; the epilogue adds it
+// to the tile's (rounded to nearest), which it holds in registers, while the
+// products go on in the other accumulator.  (Held so for every operation, the
+// products were 2 to 4 % slower.)
+//
 // EXACT: operands of fp32 values, each three bf16 planes that add up to it.  A
 // k block's three planes of A and of B are copied once and multiplied in
-// the six pairs that reach 2^-24 of the product, the smallest first.  The
-// tensor cores cut off what a sum loses in its last place, so a sum of n
-// steps of 16 k may be n units of 2^-24 short.  That is far below a rounding to
-// bf16 but not below fp32: the sum in the tensor cores ends after a k block
-// (24 steps), and the epilogue adds it to the tile's sum (rounded to
-// nearest), which it keeps in TMEM beside the two accumulators.  (Gradient of
-// 333 tokens against 5003 x 509: relative error 3e-6 with one sum a tile, 4e-7
-// so; 146 us with each pair of planes copied for itself, 111 so.)
+// the six pairs that reach 2^-24 of the product, the smallest first, a sum a k
+// block (24 steps).  (Gradient of 333 tokens against 5003 x 509: relative error
+// 3e-6 with one sum a tile, 4e-7 so; 146 us with each pair of planes copied for
+// itself, 111 so.)
 //
 // Warps of a CTA: 0 copies (TMA, one elected thread), 1 products (one thread
 // of the pair's first CTA), 2-9 epilogue (four for each half of the columns: with
@@ -153,26 +157,36 @@ __device__ __forceinline__ void load32(uint32_t taddr, float (&v)[32]) {
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-__device__ __forceinline__ void tmem_store32(uint32_t taddr, const float (&v)[32]) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        uint32_t r[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[16 * h + i]);
-        tc::tmem_st16(taddr + 16 * h, r);
+// A thread's sums of its row, 32 columns at a time, to be used up: in registers, or
+// (C = 0) read from TMEM into the place given as they are asked for.
+template <int C> struct Sums {
+    static constexpr int kChunks = C;
+    float v[C][32];
+    using Chunk = float (&)[32];
+    __device__ __forceinline__ Chunk get(int i, float (&)[32]) { return v[i]; }
+};
+template <> struct Sums<0> {
+    static constexpr int kChunks = 4;
+    uint32_t tmem;
+    using Chunk = float (&)[32];
+    __device__ __forceinline__ Chunk get(int i, float (&z)[32]) {
+        load32(tmem + 32 * i, z);
+        return z;
     }
-}
+};
 
-// Epi: epi(tile, row, tmem, half, c0, c1, scratch) by the threads of the epilogue:
-// the tile's row (0..255) of this thread, its accumulators' address, which half of
-// the columns is its and that half's columns [c0, c1) (c0 a multiple of 32), the
-// warp's scratch.
+// Epi: epi(tile, row, sums, half, c0, c1, fetched, scratch) by the threads of the
+// epilogue: the tile's row (0..255) of this thread, its sums of columns [c0, c1)
+// (c0 a multiple of 32) in 32s, which half of the columns that is, what
+// fetch(tile, row) read before the products were waited for, and the warp's scratch.
+// Epi::kSumBlocks: k blocks of a sum in the tensor cores, 0 for all of a tile.
 template <class Epi, bool A_MN, bool B_MN, bool EXACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap map_a,
                 const __grid_constant__ CUtensorMap map_b, Plan p, Epi epi) {
     using S = Shape<EXACT>;
     constexpr int kStages = S::kStages;
+    constexpr int kSum = EXACT ? 1 : Epi::kSumBlocks;    // k blocks of a sum
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drained;
     __shared__ uint32_t tmem_base;
@@ -278,13 +292,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             uint32_t phase = 0, n = 0;
             for (int item = first; ok && item < items; item += step) {
                 const Tile t(p, item);
-                const int blocks = t.kb1 - t.kb0, most = EXACT ? 1 : blocks;   // of a sum
+                const int blocks = t.kb1 - t.kb0, most = kSum ? kSum : blocks;
                 for (int b0 = 0; ok && b0 < blocks; b0 += most, ++n) {
                     const int buf = n & 1;
                     if (!(ok = wait_cluster(&acc_empty[buf], ((n >> 1) & 1) ^ 1))) break;
                     tc::tc_fence_after();
                     const uint32_t d = tmem + buf * S::kMaxN;
-                    for (int kb = b0; kb < b0 + most; ++kb) {
+                    for (int kb = b0; kb < min(blocks, b0 + most); ++kb) {
                         if (!(ok = wait_cluster(&full[s], phase))) break;
                         tc::tc_fence_after();
                         const uint32_t at = (uint32_t)s * (S::kStage >> 4);
@@ -329,34 +343,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         uint32_t n = 0;
         for (int item = first; ok && item < items; item += step) {
             const Tile t(p, item);
-            const int sums = EXACT ? t.kb1 - t.kb0 : 1;
+            const int sums = kSum ? (t.kb1 - t.kb0 + kSum - 1) / kSum : 1;
+            Sums<kSum ? S::kMaxN / 64 : 0> all;
+            const auto fetched = epi.fetch(t, row);
             for (int i = 0; i < sums; ++i, ++n) {
                 const int buf = n & 1;
                 ok = __all_sync(0xffffffffu, wait_cluster(&acc_full[buf], (n >> 1) & 1));
                 if (!ok) break;
                 tc::tc_fence_after();
-                if constexpr (EXACT) {
-                    const uint32_t from = lanes + buf * S::kMaxN, sum = lanes + 2 * S::kMaxN;
-                    for (int c = c0; c < c1; c += 32) {
-                        float v[32];
-                        load32(from + c, v);
-                        if (i > 0) {
-                            float o[32];
-                            load32(sum + c, o);
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) v[k] += o[k];
-                        }
-                        tmem_store32(sum + c, v);
-                    }
-                    tc::tmem_st_wait();
+                const uint32_t at = lanes + buf * S::kMaxN + c0;
+                if constexpr (kSum == 0) {
+                    all.tmem = at;
+                    epi(t, row, all, half, c0, c1, fetched, scratch);
                 } else {
-                    epi(t, row, lanes + buf * S::kMaxN, half, c0, c1, scratch);
+#pragma unroll
+                    for (int c = 0; c < S::kMaxN / 64; ++c) {
+                        if (c0 + 32 * c >= c1) break;
+                        if (i == 0) {
+                            load32(at + 32 * c, all.v[c]);
+                        } else {
+                            float x[32];
+                            load32(at + 32 * c, x);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) all.v[c][k] += x[k];
+                        }
+                    }
                 }
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) remote_arrive(tc::mapa_shared(tc::smem_u32(&acc_empty[buf]), 0));
             }
-            if (EXACT && ok) epi(t, row, lanes + 2 * S::kMaxN, half, c0, c1, scratch);
+            if constexpr (kSum != 0)
+                if (ok) epi(t, row, all, half, c0, c1, fetched, scratch);
         }
         if (!ok && lane == 0) atomicOr(p.err, kErrTimeout);
     }
