@@ -197,42 +197,71 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256)
 // ---- the CUDA-core kernel ----------------------------------------------------
 // 256 threads hold a block of HELD rows and stream blocks of 32.  A thread
 // computes HELD / 16 x 2 scores and as many dout . v from shared memory, then,
-// with P and dS in shared memory, its part of the held rows' sums.  Bound by
-// the fp32 pipes and shared-memory reads.
+// with P and dS in shared memory, its part of the held rows' sums.  The next block
+// is on its way into registers meanwhile (heads up to 128 wide).  Bound by the fp32
+// pipes and shared-memory reads, and in a short batch by the steps of its
+// longest block: there blocks are half as high (5 sequences of up to 300 tokens,
+// 4 heads x 80: 62 us; 133 with blocks of 64, columns padded to 128 and no loads ahead).
 
 constexpr int kStream = 32;
 constexpr int kThreads = 256;
 
-template <int DP> struct Shape {
-    static constexpr int kHeld = DP == 256 ? 32 : 64;
+template <int DP, int HELD> struct Shape {
     static constexpr int kPad = DP + 4;                  // conflict-free rows
-    static constexpr int kWPad = kHeld + 4;
+    static constexpr int kWPad = HELD + 4;
+    static constexpr bool kPrefetch = DP <= 128;
     static constexpr size_t kSmem =
-        sizeof(float) * ((size_t)2 * (kHeld + kStream) * kPad + 2 * kStream * kWPad + 2 * 64);
+        sizeof(float) * ((size_t)2 * (HELD + kStream) * kPad + 2 * kStream * kWPad + 2 * 64);
 };
 
-// `rows` rows of a tensor from row `first` into dst, zeros past `end`.
-template <typename T, int DP>
-__device__ __forceinline__ void load_rows(float *dst, const void *src, int64_t stride, int64_t head,
-                                          int64_t first, int rows, int64_t end, int D) {
-    constexpr int kPad = Shape<DP>::kPad;
-    const T *p = static_cast<const T *>(src) + head;
-    for (int i = threadIdx.x; i < rows * DP; i += kThreads) {
-        const int r = i / DP, c = i % DP;
-        dst[r * kPad + c] = first + r < end && c < D ? to_f(p[(first + r) * stride + c]) : 0.f;
-    }
+__device__ __forceinline__ float4 load4(const float *p, bool wide) {
+    if (wide) return *reinterpret_cast<const float4 *>(p);
+    return make_float4(p[0], p[1], p[2], p[3]);
 }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16 *p, bool wide) {
+    if (wide) {
+        const uint2 x = *reinterpret_cast<const uint2 *>(p);
+        return make_float4(__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xffff0000u),
+                           __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xffff0000u));
+    }
+    return make_float4(to_f(p[0]), to_f(p[1]), to_f(p[2]), to_f(p[3]));
+}
+
+// ROWS rows of a tensor from row `first` on, zeros past `end`, in registers on
+// their way to shared memory.
+template <typename T, int DP, int ROWS> struct Block {
+    static constexpr int kN = ROWS * DP / 4 / kThreads;
+    static_assert(kN * kThreads * 4 == ROWS * DP, "whole pieces");
+    float4 v[kN];
+    __device__ __forceinline__ void get(const void *src, int64_t stride, int64_t head, int64_t first,
+                                        int64_t end, int D, bool wide) {
+        const T *p = static_cast<const T *>(src) + head;
+#pragma unroll
+        for (int k = 0; k < kN; ++k) {
+            const int i = k * kThreads + threadIdx.x, r = i / (DP / 4), c = i % (DP / 4) * 4;
+            v[k] = first + r < end && c < D ? load4(p + (first + r) * stride + c, wide)
+                                            : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    }
+    __device__ __forceinline__ void put(float *dst) const {
+#pragma unroll
+        for (int k = 0; k < kN; ++k) {
+            const int i = k * kThreads + threadIdx.x, r = i / (DP / 4), c = i % (DP / 4) * 4;
+            *reinterpret_cast<float4 *>(dst + r * (DP + 4) + c) = v[k];
+        }
+    }
+};
 
 // KEYS: holds keys and values, streams queries and output gradients, writes dk
 // and dv; else the other way round, and dq.
-template <typename T, int DP, bool KEYS>
+template <typename T, int DP, int HELD, bool KEYS>
 __device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta) {
-    using S = Shape<DP>;
-    constexpr int kHeld = S::kHeld, kPad = S::kPad, kWPad = S::kWPad;
-    constexpr int kH = kHeld / 16;                       // held rows of a thread's scores
-    constexpr int kC = DP / 16;                          // columns of a thread's sums
-    float *h0 = sm, *h1 = h0 + kHeld * kPad;             // K and V, or Q and dout
-    float *s0 = h1 + kHeld * kPad, *s1 = s0 + kStream * kPad;
+    using S = Shape<DP, HELD>;
+    constexpr int kPad = S::kPad, kWPad = S::kWPad;
+    constexpr int kH = HELD / 16;                        // held rows of a thread's scores
+    constexpr int kC = DP / 16, kV = kC % 4 ? 2 : 4;     // columns of a thread's sums, neighbours
+    float *h0 = sm, *h1 = h0 + HELD * kPad;              // K and V, or Q and dout
+    float *s0 = h1 + HELD * kPad, *s1 = s0 + kStream * kPad;
     float *wp = s1 + kStream * kPad, *wd = wp + kStream * kWPad;   // P and dS, [streamed][held]
     float *lse = wd + kStream * kWPad, *di = lse + 64;
     const int heads = KEYS ? a.kv_heads : a.q_heads;
@@ -240,155 +269,170 @@ __device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta)
     if (index >= *a.count) return;
     const int4 blk = a.blocks[KEYS ? index : a.most + index];   // the longest first
     const int64_t tok0 = blk.x, end = tok0 + blk.y;
-    const int64_t first = tok0 + (int64_t)blk.z * kHeld;
+    const int64_t first = tok0 + (int64_t)blk.z * HELD;
     const int kv = KEYS ? head : head / a.group;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const bool wide = a.wide;
     float acc0[kH][kC], acc1[kH][kC];                    // dv and dk, or (acc1) dq
 #pragma unroll
     for (int i = 0; i < kH; ++i)
 #pragma unroll
         for (int c = 0; c < kC; ++c) acc0[i][c] = acc1[i][c] = 0.f;
-    if (KEYS) {
-        load_rows<T, DP>(h0, a.k, a.k_stride, (int64_t)kv * a.D, first, kHeld, end, a.D);
-        load_rows<T, DP>(h1, a.v, a.v_stride, (int64_t)kv * a.D, first, kHeld, end, a.D);
-    } else {
-        load_rows<T, DP>(h0, a.q, a.q_stride, (int64_t)head * a.D, first, kHeld, end, a.D);
-        load_rows<T, DP>(h1, a.dout, a.dout_stride, (int64_t)head * a.D, first, kHeld, end, a.D);
-        if (threadIdx.x < kHeld && first + threadIdx.x < end) {
+    // what is streamed: Q and dout of the group's heads, or K and V
+    const void *src0 = KEYS ? a.q : a.k, *src1 = KEYS ? a.dout : a.v;
+    const int64_t st0 = KEYS ? a.q_stride : a.k_stride, st1 = KEYS ? a.dout_stride : a.v_stride;
+    const int64_t from = KEYS ? first : tok0, to = KEYS ? end : min(end, first + HELD);
+    const int per_head = (int)((to - from + kStream - 1) / kStream);
+    const int steps = (KEYS ? a.group : 1) * per_head;
+    Block<T, DP, kStream> n0, n1;
+    float2 row = make_float2(0.f, 0.f);
+    auto fetch = [&](int j) {
+        const int h = KEYS ? kv * a.group + j / per_head : kv;
+        const int64_t r0 = from + (int64_t)(j % per_head) * kStream;
+        n0.get(src0, st0, (int64_t)h * a.D, r0, end, a.D, wide);
+        n1.get(src1, st1, (int64_t)h * a.D, r0, end, a.D, wide);
+        if (KEYS && threadIdx.x < kStream && r0 + threadIdx.x < end)
+            row = a.rows[(int64_t)h * a.T + r0 + threadIdx.x];
+    };
+    {
+        Block<T, DP, HELD> b;
+        b.get(KEYS ? a.k : a.q, KEYS ? a.k_stride : a.q_stride, (int64_t)head * a.D, first, end, a.D,
+              wide);
+        b.put(h0);
+        b.get(KEYS ? a.v : a.dout, KEYS ? a.v_stride : a.dout_stride, (int64_t)head * a.D, first, end,
+              a.D, wide);
+        b.put(h1);
+        if (!KEYS && threadIdx.x < HELD && first + threadIdx.x < end) {
             const float2 r = a.rows[(int64_t)head * a.T + first + threadIdx.x];
             lse[threadIdx.x] = r.x;
             di[threadIdx.x] = r.y;
         }
     }
-    const int64_t from = KEYS ? first : tok0, to = KEYS ? end : min(end, first + kHeld);
-    for (int g = 0; g < (KEYS ? a.group : 1); ++g) {
-        const int h = KEYS ? kv * a.group + g : head;
-        for (int64_t r0 = from; r0 < to; r0 += kStream) {
-            __syncthreads();
-            if (KEYS) {
-                load_rows<T, DP>(s0, a.q, a.q_stride, (int64_t)h * a.D, r0, kStream, end, a.D);
-                load_rows<T, DP>(s1, a.dout, a.dout_stride, (int64_t)h * a.D, r0, kStream, end,
-                                 a.D);
-                if (threadIdx.x < kStream && r0 + threadIdx.x < end) {
-                    const float2 r = a.rows[(int64_t)h * a.T + r0 + threadIdx.x];
-                    lse[threadIdx.x] = r.x;
-                    di[threadIdx.x] = r.y;
-                }
-            } else {
-                load_rows<T, DP>(s0, a.k, a.k_stride, (int64_t)kv * a.D, r0, kStream, end, a.D);
-                load_rows<T, DP>(s1, a.v, a.v_stride, (int64_t)kv * a.D, r0, kStream, end, a.D);
-            }
-            __syncthreads();
-            float s[kH][2], dp[kH][2];
+    if (S::kPrefetch) fetch(0);
+    for (int j = 0; j < steps; ++j) {
+        const int64_t r0 = from + (int64_t)(j % per_head) * kStream;
+        if (!S::kPrefetch) fetch(j);
+        __syncthreads();
+        n0.put(s0);
+        n1.put(s1);
+        if (KEYS && threadIdx.x < kStream) {
+            lse[threadIdx.x] = row.x;
+            di[threadIdx.x] = row.y;
+        }
+        __syncthreads();
+        if (S::kPrefetch && j + 1 < steps) fetch(j + 1);
+        float s[kH][2], dp[kH][2];
 #pragma unroll
-            for (int i = 0; i < kH; ++i) s[i][0] = s[i][1] = dp[i][0] = dp[i][1] = 0.f;
+        for (int i = 0; i < kH; ++i) s[i][0] = s[i][1] = dp[i][0] = dp[i][1] = 0.f;
 #pragma unroll 4
-            for (int c = 0; c < DP; c += 4) {
-                float4 x0[2], x1[2];
+        for (int c = 0; c < DP; c += 4) {
+            float4 x0[2], x1[2];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    x0[j] = *reinterpret_cast<const float4 *>(s0 + (ty + 16 * j) * kPad + c);
-                    x1[j] = *reinterpret_cast<const float4 *>(s1 + (ty + 16 * j) * kPad + c);
+            for (int q = 0; q < 2; ++q) {
+                x0[q] = *reinterpret_cast<const float4 *>(s0 + (ty + 16 * q) * kPad + c);
+                x1[q] = *reinterpret_cast<const float4 *>(s1 + (ty + 16 * q) * kPad + c);
+            }
+#pragma unroll
+            for (int i = 0; i < kH; ++i) {
+                const float4 y0 = *reinterpret_cast<const float4 *>(h0 + (tx + 16 * i) * kPad + c);
+                const float4 y1 = *reinterpret_cast<const float4 *>(h1 + (tx + 16 * i) * kPad + c);
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    s[i][q] = fmaf(x0[q].x, y0.x, s[i][q]);
+                    s[i][q] = fmaf(x0[q].y, y0.y, s[i][q]);
+                    s[i][q] = fmaf(x0[q].z, y0.z, s[i][q]);
+                    s[i][q] = fmaf(x0[q].w, y0.w, s[i][q]);
+                    dp[i][q] = fmaf(x1[q].x, y1.x, dp[i][q]);
+                    dp[i][q] = fmaf(x1[q].y, y1.y, dp[i][q]);
+                    dp[i][q] = fmaf(x1[q].z, y1.z, dp[i][q]);
+                    dp[i][q] = fmaf(x1[q].w, y1.w, dp[i][q]);
                 }
+            }
+        }
 #pragma unroll
-                for (int i = 0; i < kH; ++i) {
-                    const float4 y0 =
-                        *reinterpret_cast<const float4 *>(h0 + (tx + 16 * i) * kPad + c);
-                    const float4 y1 =
-                        *reinterpret_cast<const float4 *>(h1 + (tx + 16 * i) * kPad + c);
+        for (int i = 0; i < kH; ++i)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        s[i][j] = fmaf(x0[j].x, y0.x, s[i][j]);
-                        s[i][j] = fmaf(x0[j].y, y0.y, s[i][j]);
-                        s[i][j] = fmaf(x0[j].z, y0.z, s[i][j]);
-                        s[i][j] = fmaf(x0[j].w, y0.w, s[i][j]);
-                        dp[i][j] = fmaf(x1[j].x, y1.x, dp[i][j]);
-                        dp[i][j] = fmaf(x1[j].y, y1.y, dp[i][j]);
-                        dp[i][j] = fmaf(x1[j].z, y1.z, dp[i][j]);
-                        dp[i][j] = fmaf(x1[j].w, y1.w, dp[i][j]);
-                    }
+            for (int q = 0; q < 2; ++q) {
+                const int held = tx + 16 * i, str = ty + 16 * q;
+                const int64_t at_row = KEYS ? r0 + str : first + held;
+                const int64_t key = KEYS ? first + held : r0 + str;
+                const int at = KEYS ? str : held;
+                float p = 0.f, d = 0.f;
+                if (key <= at_row && at_row < end) {
+                    p = expf(fmaf(s[i][q], a.scale, -lse[at]));
+                    d = a.scale * p * (dp[i][q] - di[at]);
                 }
+                wp[str * kWPad + held] = p;
+                wd[str * kWPad + held] = d;
+            }
+        __syncthreads();
+#pragma unroll 2
+        for (int r = 0; r < kStream; ++r) {
+            float p[kH], d[kH], x0[kC], x1[kC];
+#pragma unroll
+            for (int i = 0; i < kH; ++i) {
+                p[i] = wp[r * kWPad + ty * kH + i];
+                d[i] = wd[r * kWPad + ty * kH + i];
+            }
+#pragma unroll
+            for (int c = 0; c < kC; ++c) {
+                const int col = (c / kV * 16 + tx) * kV + c % kV;
+                x0[c] = s0[r * kPad + col];
+                if (KEYS) x1[c] = s1[r * kPad + col];
             }
 #pragma unroll
             for (int i = 0; i < kH; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int held = tx + 16 * i, str = ty + 16 * j;
-                    const int64_t row = KEYS ? r0 + str : first + held;
-                    const int64_t key = KEYS ? first + held : r0 + str;
-                    const int at = KEYS ? str : held;
-                    float p = 0.f, d = 0.f;
-                    if (key <= row && row < end) {
-                        p = expf(fmaf(s[i][j], a.scale, -lse[at]));
-                        d = a.scale * p * (dp[i][j] - di[at]);
-                    }
-                    wp[str * kWPad + held] = p;
-                    wd[str * kWPad + held] = d;
-                }
-            __syncthreads();
-#pragma unroll 2
-            for (int r = 0; r < kStream; ++r) {
-                float p[kH], d[kH], x0[kC], x1[kC];
-#pragma unroll
-                for (int i = 0; i < kH; ++i) {
-                    p[i] = wp[r * kWPad + ty * kH + i];
-                    d[i] = wd[r * kWPad + ty * kH + i];
-                }
-#pragma unroll
                 for (int c = 0; c < kC; ++c) {
-                    x0[c] = s0[r * kPad + (c / 4 * 16 + tx) * 4 + c % 4];
-                    x1[c] = s1[r * kPad + (c / 4 * 16 + tx) * 4 + c % 4];
+                    if (KEYS) acc0[i][c] = fmaf(p[i], x1[c], acc0[i][c]);
+                    acc1[i][c] = fmaf(d[i], x0[c], acc1[i][c]);
                 }
-#pragma unroll
-                for (int i = 0; i < kH; ++i)
-#pragma unroll
-                    for (int c = 0; c < kC; ++c) {
-                        if (KEYS) acc0[i][c] = fmaf(p[i], x1[c], acc0[i][c]);
-                        acc1[i][c] = fmaf(d[i], x0[c], acc1[i][c]);
-                    }
-            }
         }
     }
     T *o1 = static_cast<T *>(KEYS ? a.dk : a.dq), *o0 = static_cast<T *>(a.dv);
-    const int64_t st1 = KEYS ? a.dk_stride : a.dq_stride;
+    const int64_t out1 = KEYS ? a.dk_stride : a.dq_stride;
 #pragma unroll
     for (int i = 0; i < kH; ++i) {
-        const int64_t row = first + ty * kH + i;
-        if (row >= end) continue;
+        const int64_t at = first + ty * kH + i;
+        if (at >= end) continue;
 #pragma unroll
         for (int c = 0; c < kC; ++c) {
-            const int col = (c / 4 * 16 + tx) * 4 + c % 4;
+            const int col = (c / kV * 16 + tx) * kV + c % kV;
             if (col >= a.D) continue;
-            o1[row * st1 + (int64_t)head * a.D + col] = from_f<T>(acc1[i][c]);
-            if (KEYS)
-                o0[row * a.dv_stride + (int64_t)head * a.D + col] = from_f<T>(acc0[i][c]);
+            o1[at * out1 + (int64_t)head * a.D + col] = from_f<T>(acc1[i][c]);
+            if (KEYS) o0[at * a.dv_stride + (int64_t)head * a.D + col] = from_f<T>(acc0[i][c]);
         }
     }
 }
 
 // Both roles in one launch, held keys first.
-template <typename T, int DP>
+template <typename T, int DP, int HELD>
 __global__ void __launch_bounds__(kThreads) rows_kernel(Args a) {
     extern __shared__ float sm[];
     pdl_wait();
     pdl_trigger();
     const unsigned keys = (unsigned)a.most * a.kv_heads;
     if (blockIdx.x < keys)
-        rows_run<T, DP, true>(sm, a, blockIdx.x);
+        rows_run<T, DP, HELD, true>(sm, a, blockIdx.x);
     else
-        rows_run<T, DP, false>(sm, a, blockIdx.x - keys);
+        rows_run<T, DP, HELD, false>(sm, a, blockIdx.x - keys);
 }
 
-template <typename T, int DP> cudaError_t rows_go(const Args &a, cudaStream_t st) {
-    const cudaError_t e = allow_dynamic_smem<rows_kernel<T, DP>>(Shape<DP>::kSmem);
+template <typename T, int DP, int HELD> cudaError_t rows_go(const Args &a, cudaStream_t st) {
+    constexpr size_t smem = Shape<DP, HELD>::kSmem;
+    const cudaError_t e = allow_dynamic_smem<rows_kernel<T, DP, HELD>>(smem);
     if (e != cudaSuccess) return e;
-    return launch_kernel(true, rows_kernel<T, DP>,
-                         dim3((unsigned)a.most * (a.kv_heads + a.q_heads)), kThreads,
-                         Shape<DP>::kSmem, st, a);
+    return launch_kernel(true, rows_kernel<T, DP, HELD>,
+                         dim3((unsigned)a.most * (a.kv_heads + a.q_heads)), kThreads, smem, st, a);
+}
+template <typename T, int DP> cudaError_t rows_held(const Args &a, cudaStream_t st) {
+    return a.block == 32 ? rows_go<T, DP, 32>(a, st) : rows_go<T, DP, 64>(a, st);
 }
 template <typename T> cudaError_t rows_dim(const Args &a, cudaStream_t st) {
-    return a.D <= 64 ? rows_go<T, 64>(a, st)
-                     : a.D <= 128 ? rows_go<T, 128>(a, st) : rows_go<T, 256>(a, st);
+    if (a.D <= 64) return rows_held<T, 64>(a, st);
+    if (a.D <= 96) return rows_held<T, 96>(a, st);
+    if (a.D <= 128) return rows_held<T, 128>(a, st);
+    return rows_go<T, 256, 32>(a, st);
 }
 
 template <typename T> cudaError_t launch_prepare(const Args &a, cudaStream_t st) {
@@ -408,7 +452,11 @@ template <typename T> cudaError_t launch_prepare(const Args &a, cudaStream_t st)
     return cudaGetLastError();
 }
 
-int block_of(int32_t dim) { return dim > 128 ? 32 : 64; }
+// Rows of a block on the CUDA cores: 64, or 32 for wide heads and batches whose
+// higher blocks would leave SMs idle.
+int block_of(int32_t T, int32_t heads, int32_t dim) {
+    return dim > 128 || (int64_t)T / 64 * heads < 2 * device_sm_count() ? 32 : 64;
+}
 
 // Blocks of the sequences, at most: whole ones, and a short one for each that
 // has tokens.
@@ -417,14 +465,12 @@ int64_t most_blocks(int32_t T, int32_t n_seqs, int block) {
 }
 
 struct Layout {
-    int block, most;
     int64_t rows, blocks, count, total;
 };
-Layout layout_of(int32_t T, int32_t n_seqs, int32_t q_heads, int32_t dim) {
+Layout layout_of(int32_t T, int32_t n_seqs, int32_t q_heads) {
     Layout l = {};
-    l.block = block_of(dim);
-    const int64_t most = most_blocks(T, n_seqs, l.block);
-    l.most = (int)most;
+    // room for the lower blocks, whichever the call takes
+    const int64_t most = most_blocks(T, n_seqs, 32);
     l.rows = 0;
     l.blocks = ((int64_t)T * q_heads * 8 + 15) & ~15ll;
     l.count = l.blocks + 2 * most * 16;
@@ -438,8 +484,8 @@ bool heads_ok(int32_t dtype, int32_t q_heads, int32_t kv_heads, int32_t dim) {
            dim <= kMaxHeadDim && dim % 8 == 0;
 }
 // what grids and offsets hold
-bool sizes_ok(int32_t T, int32_t n_seqs, int32_t q_heads, int32_t dim) {
-    return T >= 0 && n_seqs >= 0 && most_blocks(T, n_seqs, block_of(dim)) * 2 * q_heads <= INT32_MAX;
+bool sizes_ok(int32_t T, int32_t n_seqs, int32_t q_heads) {
+    return T >= 0 && n_seqs >= 0 && most_blocks(T, n_seqs, 32) * 2 * q_heads <= INT32_MAX;
 }
 
 }  // namespace
@@ -453,9 +499,9 @@ extern "C" int64_t ultramem_paged_attention_backward_workspace(int32_t dtype, in
                                                                int32_t kv_heads,
                                                                int32_t head_dim) {
     if (!heads_ok(dtype, q_heads, kv_heads, head_dim) ||
-        !sizes_ok(n_tokens, n_seqs, q_heads, head_dim))
+        !sizes_ok(n_tokens, n_seqs, q_heads))
         return 0;
-    return layout_of(n_tokens, n_seqs, q_heads, head_dim).total;
+    return layout_of(n_tokens, n_seqs, q_heads).total;
 }
 
 extern "C" ultramem_status ultramem_paged_attention_backward(const ultramem_attention_grad *p,
@@ -463,7 +509,7 @@ extern "C" ultramem_status ultramem_paged_attention_backward(const ultramem_atte
                                                              int64_t workspace_bytes,
                                                              void *stream) {
     if (!p || !heads_ok(p->dtype, p->q_heads, p->kv_heads, p->head_dim) ||
-        !sizes_ok(p->n_tokens, p->n_seqs, p->q_heads, p->head_dim) || !(p->scale > 0.f) ||
+        !sizes_ok(p->n_tokens, p->n_seqs, p->q_heads) || !(p->scale > 0.f) ||
         !(p->scale * kLog2e < INFINITY))
         return ULTRAMEM_EINVAL;
     if (p->n_tokens == 0 || p->n_seqs == 0) return ULTRAMEM_OK;
@@ -479,7 +525,7 @@ extern "C" ultramem_status ultramem_paged_attention_backward(const ultramem_atte
     if (p->q_stride < qr || p->out_stride < qr || p->dout_stride < qr || p->dq_stride < qr ||
         p->k_stride < kr || p->v_stride < kr || p->dk_stride < kr || p->dv_stride < kr)
         return ULTRAMEM_EINVAL;
-    const Layout l = layout_of(p->n_tokens, p->n_seqs, p->q_heads, p->head_dim);
+    const Layout l = layout_of(p->n_tokens, p->n_seqs, p->q_heads);
     if (workspace_bytes < l.total) return ULTRAMEM_EINVAL;
     const int64_t T = p->n_tokens;
     auto rows_of = [&](const void *at, int64_t row, int64_t stride) {
@@ -533,18 +579,20 @@ extern "C" ultramem_status ultramem_paged_attention_backward(const ultramem_atte
     a.kv_heads = p->kv_heads;
     a.group = p->q_heads / p->kv_heads;
     a.D = p->head_dim;
-    a.block = l.block;
-    a.most = l.most;
+    a.block = block_of(p->n_tokens, p->q_heads + p->kv_heads, p->head_dim);
+    a.most = (int)most_blocks(p->n_tokens, p->n_seqs, a.block);
     a.scale = p->scale;
     a.scale_log2 = p->scale * kLog2e;
     cudaStream_t st = (cudaStream_t)stream;
     cudaGetLastError();
     cudaError_t e;
     // TMA reads the inputs, and the outputs leave, in 16-byte pieces
-    const uintptr_t low = (uintptr_t)p->q | (uintptr_t)p->k | (uintptr_t)p->v | (uintptr_t)p->dout |
-                          (uintptr_t)p->dq | (uintptr_t)p->dk | (uintptr_t)p->dv |
-                          (uintptr_t)((p->q_stride | p->k_stride | p->v_stride | p->dout_stride |
-                                       p->dq_stride | p->dk_stride | p->dv_stride) * es);
+    const uintptr_t in_low = (uintptr_t)p->q | (uintptr_t)p->k | (uintptr_t)p->v |
+                             (uintptr_t)p->dout |
+                             (uintptr_t)((p->q_stride | p->k_stride | p->v_stride | p->dout_stride) * es);
+    a.wide = in_low % (4 * es) == 0;
+    const uintptr_t low = in_low | (uintptr_t)p->dq | (uintptr_t)p->dk | (uintptr_t)p->dv |
+                          (uintptr_t)((p->dq_stride | p->dk_stride | p->dv_stride) * es);
     if (p->dtype == ULTRAMEM_BF16 && p->head_dim <= 128 && low % 16 == 0) {
         if (!(a.err = um::paged::error_word())) return ULTRAMEM_ENODEV;
         a.block = kTensorBlock;

@@ -25,7 +25,8 @@ struct Args {
     int *err;
     int n_seqs, T, q_heads, kv_heads, group, D;
     int block;                // rows of a block
-    int most;                 // blocks that the list holds
+    int most;                 // blocks that a list holds
+    int wide;                 // inputs whose rows allow loads of 4 entries
     float scale, scale_log2;
 };
 
