@@ -517,7 +517,9 @@ int64_t ultramem_block_norm_backward_workspace(int64_t n_tokens, int32_t dim);
  *   dS_ij = scale P_ij (dout_i . v_j - d_i)
  *   dq_i = sum_j dS_ij k_j,  dk_j = sum_i dS_ij q_i,  dv_j = sum_i P_ij dout_i
  * with the sums of dk and dv over all query heads of a key/value head.  A row
- * whose lse is -inf takes no part: its dq is 0.  Sequence r holds the tokens
+ * whose lse is -inf takes no part: its dq is 0.  Its dout, and q, k, v and dout
+ * of tokens of the same sequence that a row does not see, meet weight 0 and
+ * must be finite; what other sequences' rows hold is never used.  Sequence r holds the tokens
  * q_start[r] .. q_start[r + 1] - 1 (q_start [n_seqs + 1] does not decrease; a
  * sequence of no tokens is fine).  Rows that belong to no sequence are not
  * written.  The probabilities are computed again, none are stored; sums are

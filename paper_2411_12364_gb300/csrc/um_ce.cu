@@ -45,6 +45,20 @@ struct Labels {
     }
 };
 
+// The next of the bf16 terms that add up to v, and v less it.  A value that rounds
+// to infinity is cut instead, and an infinity or NaN is its own first term.
+__device__ __forceinline__ __nv_bfloat16 take_term(float &v) {
+    __nv_bfloat16 b = __float2bfloat16_rn(v);
+    if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) {
+        v = 0.f;
+        return b;
+    }
+    if (fabsf(__bfloat162float(b)) == INFINITY)
+        b = __ushort_as_bfloat16((unsigned short)(__float_as_uint(v) >> 16));
+    v -= __bfloat162float(b);
+    return b;
+}
+
 // ---- operands as planes --------------------------------------------------------
 // src [R][D] (rows ld apart) -> dst [planes][R][Dp], Dp = D rounded up to 64, so
 // that rows start on 128 bytes: fp32 values as three bf16 terms, bf16 ones as
@@ -85,10 +99,8 @@ __global__ void __launch_bounds__(256)
             uint32_t o[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+                const __nv_bfloat162 b = {take_term(v[2 * k]), take_term(v[2 * k + 1])};
                 o[k] = *reinterpret_cast<const uint32_t *>(&b);
-                v[2 * k] -= __low2float(b);
-                v[2 * k + 1] -= __high2float(b);
             }
             *reinterpret_cast<uint4 *>(dst + ((int64_t)q * R + r) * Dp + c) =
                 make_uint4(o[0], o[1], o[2], o[3]);
@@ -524,8 +536,13 @@ struct ForwardLayout {
 ForwardLayout forward_layout(int32_t dtype, int64_t T, int64_t V, int32_t D) {
     ForwardLayout l = {};
     l.piece = piece_of(V, rows_in_planes(dtype, D));
-    // a tile is at least 128 columns wide, and pieces are whole tiles but for the last of each
-    l.tiles = 2 * (ceil_div(V, 128) + ceil_div(V, l.piece));
+    // of the weights where they lie, or in pieces, the last of which may choose any width
+    const int P = planes_of(dtype);
+    const int64_t t = T > 0 ? T : 1, last = V % l.piece ? V % l.piece : l.piece;
+    const int64_t whole = ceil_div(V, plan_of(t, V, D, P, 32, 1).n_tile);
+    const int64_t pieces = (V - last) / l.piece * ceil_div(l.piece, plan_of(t, l.piece, D, P, 32, 1).n_tile) +
+                           ceil_div(last, 128);
+    l.tiles = 2 * (whole > pieces ? whole : pieces);
     const int64_t es = planes_of(dtype) * padded(D) * 2;
     l.part = 0;
     l.target = pad256(l.tiles * T * 8);
@@ -556,8 +573,8 @@ BackwardLayout backward_layout(int32_t dtype, int64_t T, int64_t V, int32_t D) {
     };
     const int64_t t = T > 0 ? T : 1;
     l.logits = plan_of(t, l.piece, D, P, 32, 1);
-    l.x_plan = plan_of(t, D, l.piece, P, 128, most(t, D));
-    l.w_plan = plan_of(l.piece, D, t, P, 128, most(l.piece, D));
+    l.x_plan = plan_of(t, D, l.piece, P, 128, most(t, padded(D)));
+    l.w_plan = plan_of(l.piece, D, t, P, 128, most(l.piece, padded(D)));
     l.dx_splits = l.x_plan.splits;
     l.dw_splits = l.w_plan.splits;
     const int64_t es = P * padded(D) * 2;

@@ -234,3 +234,62 @@ def test_captured_beside_an_eager_call(gpu_lib):
         torch.cuda.synchronize()
         check(got, q, k, v, out, lse, dout, lens, scale)
         assert all(torch.equal(a, b) for a, b in zip(got, eager))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_offsets_past_32_bits(gpu_lib, dtype):
+    """Tokens so far apart that the last ones' offsets pass 2^32 entries."""
+    lens, H, heads, D = [70, 60], 2, 1, 64
+    q, k, v, out, lse, dout, start, scale = inputs(lens, H, heads, D, dtype)
+    T, step = sum(lens), 2 ** 25 + 64        # 130 steps: 4.4e9 entries
+
+    def apart(x):
+        n = x.shape[1] * D
+        flat = torch.empty((T - 1) * step + n, dtype=dtype, device="cuda")
+        y = flat.as_strided((T, x.shape[1], D), (step, D, 1))
+        y.copy_(x)
+        return y
+
+    got = paged.paged_attention_backward(apart(q), k, apart(v), out, lse, apart(dout), start,
+                                         dq=apart(torch.zeros_like(q)))
+    check(got, q, k, v, out, lse, dout, lens, scale)
+
+
+def test_first_call_inside_a_capture(gpu_lib):
+    """In a process of its own, where nothing was looked up before."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    body = """
+import torch
+from paper_2411_12364_gb300 import binding, paged, vocab
+binding.load()
+bf = dict(dtype=torch.bfloat16, device="cuda")
+x, w = torch.randn(40, 64, **bf), torch.randn(300, 64, **bf)
+ids = torch.arange(40, device="cuda")
+q, k = torch.randn(40, 2, 64, **bf), torch.randn(40, 1, 64, **bf)
+lse = torch.full((40, 2), 5.0, device="cuda")
+start = torch.tensor([0, 40], dtype=torch.int32, device="cuda")
+stream = torch.cuda.Stream()
+stream.wait_stream(torch.cuda.current_stream())
+graph = torch.cuda.CUDAGraph()
+
+
+def run():
+    loss, row = vocab.cross_entropy(x, w, ids)
+    dx, dw = vocab.cross_entropy_backward(x, w, ids, row, torch.ones_like(row))
+    return (loss, dx, dw, vocab.embedding(w, ids), vocab.embedding_backward(ids, x, 300),
+            *paged.paged_attention_backward(q, k, k, q, lse, q, start))
+
+
+with torch.cuda.graph(graph, stream=stream):
+    held = run()
+graph.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(held, run()))
+print("done")
+"""
+    out = subprocess.run([sys.executable, "-c", body], cwd=root, capture_output=True, text=True,
+                         timeout=300)
+    assert out.returncode == 0 and out.stdout.strip() == "done", out.stdout + out.stderr

@@ -233,3 +233,53 @@ def test_captured_on_another_stream(gpu_lib):
         torch.cuda.synchronize()
         check_forward(x, w, labels, 1.0, (loss, lse))
         check_backward(x, w, labels, lse, dloss, 1.0, (dx, dw))
+
+
+def test_values_that_bf16_does_not_hold(gpu_lib):
+    """The largest fp32 values among the weights: their terms stay finite."""
+    x, w, labels, dloss = inputs(9, 40, 16, F32)
+    x[:, 3] = 0
+    x[0, 3] = 1e-30
+    w[7, 3], w[8, 3] = -torch.finfo(F32).max, torch.finfo(F32).max
+    labels[:] = torch.arange(9, device="cuda")
+    x[0] *= 1e-8                         # its logits stay in range
+    loss, lse = vocab.cross_entropy(x, w, labels)
+    z = x.double() @ w.double().T
+    keep = z.abs().amax(1) < 1e30
+    assert bool(keep[1:].all())
+    check_forward(x[1:], w, labels[1:], 1.0, (loss[1:], lse[1:]))
+
+
+def test_offsets_past_32_bits(gpu_lib):
+    """More than 2^32 entries in the weights and in their gradient."""
+    V, D = 2 ** 20 + 77, 4096
+    g = gen(11)
+    w = torch.zeros(V, D, dtype=BF16, device="cuda")
+    rows = torch.tensor([0, 5, V // 2, V - 1], device="cuda")
+    w[rows] = torch.randn(4, D, generator=g, device="cuda").to(BF16) * 0.03
+    x = torch.randn(3, D, generator=g, device="cuda").to(BF16)
+    labels = torch.tensor([V - 1, 5, V // 2], device="cuda")
+    loss, lse = vocab.cross_entropy(x, w, labels)
+    z = x.double() @ w[rows].double().T
+    want = torch.log((V - 4) + torch.exp(z).sum(1))
+    pick = z[torch.arange(3), torch.tensor([3, 1, 2])]
+    # all other logits are exactly 0; the rest as in check_forward
+    tol = z_error(x, w[rows], 1.0).amax(1) + 2.0 ** -20 + (256 + V / 64) * 2.0 ** -24
+    assert bool(((lse.double() - want).abs() <= tol).all())
+    assert bool(((loss.double() - (want - pick)).abs() <= 2 * tol).all())
+    dloss = torch.ones(3, device="cuda")
+    dx, dw = vocab.cross_entropy_backward(x, w, labels, lse, dloss)
+    # G and the results are rounded to bf16 (2^-8 each); the logits' errors, below
+    # 2^-10, scale p: together below 2^-6 of the sums of magnitudes
+    p = torch.exp(z - lse.double()[:, None])
+    p[torch.arange(3), torch.tensor([3, 1, 2])] -= 1
+    for i, r in enumerate(rows.tolist()):
+        want = p[:, i] @ x.double()
+        size = p[:, i].abs() @ x.double().abs()
+        assert bool(((dw[r].double() - want).abs() <= 2.0 ** -6 * size + 1e-30).all())
+    quiet = dw[1:5].double()             # rows of weight e^-lse alone
+    even = torch.exp(-lse.double()) @ x.double()
+    assert bool(((quiet - even).abs() <= 2.0 ** -6 * (torch.exp(-lse.double()) @ x.double().abs())).all())
+    want = p @ w[rows].double()
+    assert bool(((dx.double() - want).abs() <=
+                 2.0 ** -6 * (p.abs() @ w[rows].double().abs()) + 1e-30).all())

@@ -126,3 +126,42 @@ def test_captured_step(example, gpu_lib):
         eager = run()
         assert all(torch.equal(a, b) for a, b in zip(held, eager))
     assert paged_check() == 0
+
+
+def test_calls_at_once_on_two_streams(gpu_lib):
+    """Calls that overlap on the GPU, each with its own workspace, give what they
+    give one after another."""
+    from paper_2411_12364_gb300 import paged, vocab
+    gen = torch.Generator(device="cuda").manual_seed(9)
+
+    def randn(*shape, dtype=torch.bfloat16):
+        return torch.randn(*shape, generator=gen, device="cuda").to(dtype)
+
+    sets = []
+    for dtype, T, V, D in ((torch.bfloat16, 700, 3000, 256), (torch.float32, 200, 900, 100)):
+        x, w = randn(T, D, dtype=dtype), randn(V, D, dtype=dtype) * 0.1
+        ids = torch.randint(0, V, (T,), generator=gen, device="cuda")
+        q, k = randn(T, 4, 64, dtype=dtype), randn(T, 2, 64, dtype=dtype)
+        lse = torch.full((T, 4), 9.0, device="cuda")
+        start = torch.tensor([0, T // 3, T], dtype=torch.int32, device="cuda")
+        sets.append((x, w, ids, q, k, lse, start))
+
+    def run(x, w, ids, q, k, lse, start):
+        loss, row = vocab.cross_entropy(x, w, ids)
+        dx, dw = vocab.cross_entropy_backward(x, w, ids, row, torch.ones_like(row))
+        return (loss, dx, dw, vocab.embedding_backward(ids, x, w.shape[0]),
+                *paged.paged_attention_backward(q, k, k, q, lse, q, start))
+
+    alone = [run(*s) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[], []]
+    for _ in range(5):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(run(*sets[i]))
+    torch.cuda.synchronize()
+    for i, want in enumerate(alone):
+        for have in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(have, want))
+    assert paged_check() == 0
