@@ -185,14 +185,18 @@ def _grad_workspace(dev, dtype, T, R, q_heads, kv_heads, head_dim):
                                                                      kv_heads, head_dim))
 
 
-def _grad_rows(name, t, shape, dtype, dev):
-    """A given output [tokens, heads, dim], whose tokens may be strided apart."""
+def _grad_rows(name, t, n, heads, dim, dtype, dev, device):
+    """An output [tokens, heads, dim], new or given, whose tokens may be strided
+    apart, and their distance."""
+    shape, row = (n, heads, dim), heads * dim
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device), row
     s0, s1, s2 = t.stride() if t.dim() == 3 else (0, 0, 0)
     if t.shape != shape or t.dtype != dtype or t.get_device() != dev or s2 != 1 or \
-            s1 != shape[2] or (s0 < shape[1] * shape[2] and shape[0] > 1):
-        raise ValueError(f"{name} must be a tensor {tuple(shape)} of q's type and device, a token's "
+            s1 != dim or (s0 < row and n > 1):
+        raise ValueError(f"{name} must be a tensor {shape} of q's type and device, a token's "
                          "heads contiguous")
-    return t, max(s0, shape[1] * shape[2])
+    return t, max(s0, row)
 
 
 def paged_attention_backward(q, k, v, out, lse, dout, q_start, scale=None, dq=None, dk=None,
@@ -218,33 +222,29 @@ def paged_attention_backward(q, k, v, out, lse, dout, q_start, scale=None, dq=No
     dout, ds = _rows("dout", dout, H, D, dtype, dev)
     k, ks = _rows("k", k, heads, D, dtype, dev)
     v, vs = _rows("v", v, heads, D, dtype, dev)
-    if any(t.shape[0] != T for t in (out, dout, k, v)):
+    if not (out.shape[0] == dout.shape[0] == k.shape[0] == v.shape[0] == T):
         raise ValueError("q, k, v, out and dout must have a row for each token")
     if lse.shape != (T, H) or lse.dtype != torch.float32 or lse.get_device() != dev or \
             not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 tensor [tokens, q_heads] on q's device")
     starts = _int32("q_start", q_start, dev)
-    grads, strides = [], []
-    for name, t, shape in (("dq", dq, (T, H, D)), ("dk", dk, (T, heads, D)),
-                           ("dv", dv, (T, heads, D))):
-        if t is None:
-            t = torch.empty(shape, dtype=dtype, device=q.device)
-        t, stride = _grad_rows(name, t, shape, dtype, dev)
-        grads.append(t)
-        strides.append(stride)
+    device = q.device
+    dq, dqs = _grad_rows("dq", dq, T, H, D, dtype, dev, device)
+    dk, dks = _grad_rows("dk", dk, T, heads, D, dtype, dev, device)
+    dv, dvs = _grad_rows("dv", dv, T, heads, D, dtype, dev, device)
     code = _DTYPES[dtype]
     a = _b.AttentionGrad(
-        q.data_ptr(), out.data_ptr(), dout.data_ptr(), k.data_ptr(), v.data_ptr(),
-        *(t.data_ptr() for t in grads), lse.data_ptr(), starts, qs, os, ds, ks, vs, *strides, T, R,
-        H, heads, D, code, 1.0 / math.sqrt(D) if scale is None else scale)
+        q.data_ptr(), out.data_ptr(), dout.data_ptr(), k.data_ptr(), v.data_ptr(), dq.data_ptr(),
+        dk.data_ptr(), dv.data_ptr(), lse.data_ptr(), starts, qs, os, ds, ks, vs, dqs, dks, dvs, T,
+        R, H, heads, D, code, 1.0 / math.sqrt(D) if scale is None else scale)
     lib = _b._lib or _b.load()
     nbytes = _grad_workspace(dev, code, T, R, H, heads, D)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     status = lib.ultramem_paged_attention_backward(C.byref(a), ws.data_ptr(), nbytes,
                                                    _b._stream(dev))
     if status:
         raise _b.UltraMemError(status, "ultramem_paged_attention_backward")
-    return tuple(grads)
+    return dq, dk, dv
 
 
 def paged_check() -> int:

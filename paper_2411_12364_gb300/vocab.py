@@ -29,20 +29,22 @@ _INTS = {torch.int32: 4, torch.int64: 8}
 
 
 def _matrix(name, t, dev):
-    """A [rows, columns] tensor whose rows may be strided apart, and their
-    distance."""
+    """A [rows, columns] tensor whose rows may be strided apart, its sizes and
+    the rows' distance."""
     shape = t.shape
     if len(shape) != 2 or t.dtype not in _DTYPES or t.get_device() != dev:
         raise ValueError(f"{name} must be a tensor [rows, columns], fp32 or bf16, on the current "
                          "device")
-    if shape[1] < 1:
+    rows, columns = shape
+    if columns < 1:
         raise ValueError(f"{name} must have columns")
-    _b._fits_int32(*shape)
+    _b._fits_int32(rows, columns)
     s0, s1 = t.stride()
-    if (s1 == 1 or shape[1] == 1) and (s0 >= shape[1] or shape[0] <= 1):
-        return t, max(s0, shape[1])
-    t = t.contiguous()
-    return t, shape[1]
+    if s0 >= columns and (s1 == 1 or columns == 1):
+        return t, rows, columns, s0
+    if rows > 1 or (s1 != 1 and columns > 1):
+        t = t.contiguous()
+    return t, rows, columns, columns
 
 
 def _ids(name, t, n, dev):
@@ -68,21 +70,28 @@ def _output(name, t, shape, dtype, dev):
     return t
 
 
+def _gradient(name, t, shape, dtype, dev, device):
+    """An output asked for (True), given, or left out (None or False)."""
+    if t is True:
+        return torch.empty(shape, dtype=dtype, device=device)
+    return None if t is None or t is False else _output(name, t, shape, dtype, dev)
+
+
 def embedding(table, ids, scale: float = 1.0, out=None):
     """out [T, D] = scale * table[ids] for ids [T] (int32 or int64) into table
     [V, D]; a zero row for an id outside [0, V)."""
     dev = _b._on_device("table", table)
-    table, ld = _matrix("table", table, dev)
-    V, D = table.shape
+    table, V, D, ld = _matrix("table", table, dev)
     T = ids.numel()
     _b._fits_int32(T)
     p_ids, ids_bytes = _ids("ids", ids, T, dev)
+    dtype = table.dtype
     if out is None:
-        out = torch.empty((T, D), dtype=table.dtype, device=table.device)
+        out = torch.empty((T, D), dtype=dtype, device=table.device)
     else:
-        _output("out", out, (T, D), table.dtype, dev)
+        _output("out", out, (T, D), dtype, dev)
     lib = _b._lib or _b.load()
-    status = lib.ultramem_embedding(table.data_ptr(), ld, _DTYPES[table.dtype], V, D, p_ids,
+    status = lib.ultramem_embedding(table.data_ptr(), ld, _DTYPES[dtype], V, D, p_ids,
                                     ids_bytes, T, scale, out.data_ptr(), _b._stream(dev))
     if status:
         raise _b.UltraMemError(status, "ultramem_embedding")
@@ -103,8 +112,7 @@ def embedding_backward(ids, dout, vocab: int, scale: float = 1.0, dtable=None,
     ``dtable`` (fp32 or bf16) is given.  With ``accumulate`` the sums are added
     to what the given dtable holds.  The sums have a fixed order."""
     dev = _b._on_device("dout", dout)
-    dout, ld = _matrix("dout", dout, dev)
-    T, D = dout.shape
+    dout, T, D, ld = _matrix("dout", dout, dev)
     _b._fits_int32(vocab)
     p_ids, ids_bytes = _ids("ids", ids, T, dev)
     if dtable is not None:
@@ -131,16 +139,16 @@ def embedding_backward(ids, dout, vocab: int, scale: float = 1.0, dtable=None,
 
 def _ce_args(x, w, labels, logit_scale):
     dev = _b._on_device("x", x)
-    x, ld_x = _matrix("x", x, dev)
-    w, ld_w = _matrix("w", w, dev)
-    T, D = x.shape
-    V = w.shape[0]
-    if w.shape[1] != D or w.dtype != x.dtype:
+    x, T, D, ld_x = _matrix("x", x, dev)
+    w, V, w_dim, ld_w = _matrix("w", w, dev)
+    dtype = x.dtype
+    if w_dim != D or w.dtype != dtype:
         raise ValueError("w must be [vocab, dim] of x's type")
     p_labels, labels_bytes = _ids("labels", labels, T, dev)
-    a = _b.CrossEntropyArgs(x.data_ptr(), w.data_ptr(), p_labels, ld_x, ld_w, T, V, D,
-                            _DTYPES[x.dtype], labels_bytes, logit_scale)
-    return a, x, w, dev
+    code = _DTYPES[dtype]
+    a = _b.CrossEntropyArgs(x.data_ptr(), w.data_ptr(), p_labels, ld_x, ld_w, T, V, D, code,
+                            labels_bytes, logit_scale)
+    return a, x, w, dev, (code, T, V, D)
 
 
 def cross_entropy(x, w, labels, logit_scale: float = 1.0):
@@ -148,13 +156,13 @@ def cross_entropy(x, w, labels, logit_scale: float = 1.0):
     weights w [V, D]: z = logit_scale * x w^T, lse = log sum e^z, loss = lse -
     z[label].  A label outside [0, V) marks a token that does not count (loss
     0).  The logits are not kept."""
-    a, x, w, dev = _ce_args(x, w, labels, logit_scale)
-    T = a.n_tokens
-    loss = torch.empty(T, dtype=torch.float32, device=x.device)
-    lse = torch.empty(T, dtype=torch.float32, device=x.device)
+    a, x, w, dev, sizes = _ce_args(x, w, labels, logit_scale)
+    device = x.device
+    loss = torch.empty(sizes[1], dtype=torch.float32, device=device)
+    lse = torch.empty(sizes[1], dtype=torch.float32, device=device)
     lib = _b._lib or _b.load()
-    nbytes = _workspace(dev, "ultramem_cross_entropy_workspace", a.dtype, T, a.vocab, a.dim)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    nbytes = _workspace(dev, "ultramem_cross_entropy_workspace", *sizes)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     status = lib.ultramem_cross_entropy(C.byref(a), loss.data_ptr(), lse.data_ptr(),
                                         ws.data_ptr(), nbytes, _b._stream(dev))
     if status:
@@ -167,23 +175,18 @@ def cross_entropy_backward(x, w, labels, lse, dloss, logit_scale: float = 1.0, d
     and for the gradients dloss [T] (fp32) of its losses.  ``dx`` and ``dw``
     may be contiguous tensors to write, or False to leave that one out
     (None is returned for it)."""
-    a, x, w, dev = _ce_args(x, w, labels, logit_scale)
-    T, V, D = a.n_tokens, a.vocab, a.dim
+    a, x, w, dev, sizes = _ce_args(x, w, labels, logit_scale)
+    _, T, V, D = sizes
+    dtype, device = x.dtype, x.device
     p_lse, p_dloss = _floats("lse", lse, T, dev), _floats("dloss", dloss, T, dev)
-    got = []
-    for name, t, shape in (("dx", dx, (T, D)), ("dw", dw, (V, D))):
-        if t is None or t is False:
-            got.append(None)
-        elif t is True:
-            got.append(torch.empty(shape, dtype=x.dtype, device=x.device))
-        else:
-            got.append(_output(name, t, shape, x.dtype, dev))
+    dx = _gradient("dx", dx, (T, D), dtype, dev, device)
+    dw = _gradient("dw", dw, (V, D), dtype, dev, device)
     lib = _b._lib or _b.load()
-    nbytes = _workspace(dev, "ultramem_cross_entropy_backward_workspace", a.dtype, T, V, D)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    nbytes = _workspace(dev, "ultramem_cross_entropy_backward_workspace", *sizes)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     status = lib.ultramem_cross_entropy_backward(
-        C.byref(a), p_lse, p_dloss, *(None if t is None else t.data_ptr() for t in got),
-        ws.data_ptr(), nbytes, _b._stream(dev))
+        C.byref(a), p_lse, p_dloss, None if dx is None else dx.data_ptr(),
+        None if dw is None else dw.data_ptr(), ws.data_ptr(), nbytes, _b._stream(dev))
     if status:
         raise _b.UltraMemError(status, "ultramem_cross_entropy_backward")
-    return tuple(got)
+    return dx, dw
