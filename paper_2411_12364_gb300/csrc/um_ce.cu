@@ -38,11 +38,13 @@ struct Labels {
     const void *at;
     int wide, V;
     // the label of token t, or -1 for one that does not count
-    __device__ __forceinline__ int operator()(int64_t t) const {
-        const int64_t l = wide ? static_cast<const int64_t *>(at)[t]
-                               : (int64_t) static_cast<const int32_t *>(at)[t];
-        return l >= 0 && l < V ? (int)l : -1;
+    __device__ __forceinline__ int operator()(int64_t t) const { return of(load(t)); }
+    // the same in two steps: what a load gives, and what it says
+    __device__ __forceinline__ int64_t load(int64_t t) const {
+        return wide ? static_cast<const int64_t *>(at)[t]
+                    : (int64_t) static_cast<const int32_t *>(at)[t];
     }
+    __device__ __forceinline__ int of(int64_t l) const { return l >= 0 && l < V ? (int)l : -1; }
 };
 
 // The next of the bf16 terms that add up to v, and v less it.  A value that rounds
@@ -126,15 +128,16 @@ template <int SUM> struct LseEpi {
     template <int N> LseEpi<N> cut() const {
         return {labels, part, target, T, vn, v0, tile0, n_tile, scale, scale_log2};
     }
-    __device__ __forceinline__ int fetch(const pair::Tile &t, int row) const {
+    __device__ __forceinline__ int64_t fetch(const pair::Tile &t, int row) const {
         const int64_t tok = t.m0 + row;
-        return tok < T ? labels(tok) - (v0 + t.n0) : -1;     // the tile's column
+        return tok < T ? labels.load(tok) : -1;
     }
     template <class Sums, class Turn>
     __device__ __forceinline__ void operator()(const pair::Tile &t, int row, Sums &sums,
-                                               int half, int c0, int c1, int label,
+                                               int half, int c0, int c1, int64_t loaded,
                                                Turn &scratch) const {
         const int64_t tok = t.m0 + row;
+        const int label = labels.of(loaded) - (v0 + t.n0);       // the tile's column
         const int cols = min(c1, vn - t.n0);
         // to log2 units; where the scale is negative the sums change their sign first,
         // and where it is 0 they become 0
@@ -251,14 +254,13 @@ template <int P> struct GradEpi {
     float scale, scale_log2;
 
     struct Row {
-        int label;
-        float d, shift;
+        int64_t label;
+        float dloss, lse;
     };
     __device__ __forceinline__ Row fetch(const pair::Tile &t, int row) const {
         const int64_t tok = t.m0 + row;
-        const int label = tok < T ? labels(tok) : -1;
-        return {label, label >= 0 ? dloss[tok] * scale : 0.f,
-                label >= 0 ? -lse[tok] * kLog2e : 0.f};
+        if (tok >= T) return {-1, 0.f, 0.f};
+        return {labels.load(tok), dloss[tok], lse[tok]};
     }
     template <class Sums, class Turn>
     __device__ __forceinline__ void operator()(const pair::Tile &t, int row, Sums &sums,
@@ -266,8 +268,9 @@ template <int P> struct GradEpi {
                                                Turn &scratch) const {
         const int64_t tok = t.m0 + row;
         const bool live = tok < T;
-        const int label = r.label, at = label - (v0 + t.n0);
-        const float d = r.d, shift = r.shift;
+        const int label = labels.of(r.label), at = label - (v0 + t.n0);
+        const float d = label >= 0 ? r.dloss * scale : 0.f;
+        const float shift = label >= 0 ? -r.lse * kLog2e : 0.f;
         const int cols = min(c1, vn - t.n0);
 #pragma unroll
         for (int i = 0; i < Sums::kChunks; ++i) {

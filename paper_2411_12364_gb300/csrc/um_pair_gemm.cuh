@@ -83,8 +83,12 @@ struct Tile {
         const int height = min(p.group_m, p.m_tiles - g * p.group_m);
         n0 = i / height * p.n_tile;
         m0 = (g * p.group_m + i % height) * kTileM;
-        kb0 = (int)((int64_t)p.k_blocks * split / p.splits);
-        kb1 = (int)((int64_t)p.k_blocks * (split + 1) / p.splits);
+        kb0 = 0;
+        kb1 = p.k_blocks;
+        if (p.splits > 1) {                  // splits <= 64, k_blocks < 2^24
+            kb0 = (int)((uint32_t)p.k_blocks * (uint32_t)split / (uint32_t)p.splits);
+            kb1 = (int)((uint32_t)p.k_blocks * (uint32_t)(split + 1) / (uint32_t)p.splits);
+        }
     }
 };
 
@@ -99,8 +103,10 @@ __device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, uint
         "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
         : "memory");
 }
+// Relaxed: what it tells of are loads from TMEM, which tcgen05's fence orders; a
+// release for the cluster would also wait until the epilogue's stores are in L2.
 __device__ __forceinline__ void remote_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar)
                  : "memory");
 }
 __device__ __forceinline__ bool wait_cluster(uint64_t *bar, uint32_t parity) {
@@ -178,7 +184,7 @@ template <> struct Sums<0> {
 // Epi: epi(tile, row, sums, half, c0, c1, fetched, scratch) by the threads of the
 // epilogue: the tile's row (0..255) of this thread, its sums of columns [c0, c1)
 // (c0 a multiple of 32) in 32s, which half of the columns that is, what
-// fetch(tile, row) read before the products were waited for, and the warp's scratch.
+// fetch(tile, row) loaded while the tile before was worked on, and the warp's scratch.
 // Epi::kSumBlocks: k blocks of a sum in the tensor cores, 0 for all of a tile.
 template <class Epi, bool A_MN, bool B_MN, bool EXACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
@@ -341,11 +347,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         const int half = (w - 2) >> 2, middle = (p.n_tile / 2 + 31) & ~31;
         const int c0 = half ? middle : 0, c1 = half ? p.n_tile : middle;
         uint32_t n = 0;
+        Tile t(p, first);
+        auto fetched = epi.fetch(t, row);
         for (int item = first; ok && item < items; item += step) {
-            const Tile t(p, item);
             const int sums = kSum ? (t.kb1 - t.kb0 + kSum - 1) / kSum : 1;
             Sums<kSum ? S::kMaxN / 64 : 0> all;
-            const auto fetched = epi.fetch(t, row);
+            const Tile next(p, item + step < items ? item + step : item);
+            const auto ahead = epi.fetch(next, row);
             for (int i = 0; i < sums; ++i, ++n) {
                 const int buf = n & 1;
                 ok = __all_sync(0xffffffffu, wait_cluster(&acc_full[buf], (n >> 1) & 1));
@@ -375,6 +383,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             }
             if constexpr (kSum != 0)
                 if (ok) epi(t, row, all, half, c0, c1, fetched, scratch);
+            t = next;
+            fetched = ahead;
         }
         if (!ok && lane == 0) atomicOr(p.err, kErrTimeout);
     }
