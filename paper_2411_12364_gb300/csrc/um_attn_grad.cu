@@ -201,7 +201,8 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256)
 // is on its way into registers meanwhile (heads up to 128 wide).  Bound by the fp32
 // pipes and shared-memory reads, and in a short batch by the steps of its
 // longest block: there blocks are half as high (5 sequences of up to 300 tokens,
-// 4 heads x 80: 62 us; 133 with blocks of 64, columns padded to 128 and no loads ahead).
+// 4 heads x 80: 54 us; 133 with blocks of 64, columns padded to 128, no loads ahead
+// and a load for each of the sums' operands).
 
 constexpr int kStream = 32;
 constexpr int kThreads = 256;
@@ -225,6 +226,18 @@ __device__ __forceinline__ float4 load4(const __nv_bfloat16 *p, bool wide) {
                            __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xffff0000u));
     }
     return make_float4(to_f(p[0]), to_f(p[1]), to_f(p[2]), to_f(p[3]));
+}
+
+// 2 or 4 neighbours of shared memory, in one load
+template <int N> __device__ __forceinline__ void load_shared(const float *p, float *v) {
+    if constexpr (N == 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(p);
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+    } else {
+        static_assert(N == 2, "pairs");
+        const float2 x = *reinterpret_cast<const float2 *>(p);
+        v[0] = x.x, v[1] = x.y;
+    }
 }
 
 // ROWS rows of a tensor from row `first` on, zeros past `end`, in registers on
@@ -321,11 +334,12 @@ __device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta)
         }
         __syncthreads();
         if (S::kPrefetch && j + 1 < steps) fetch(j + 1);
+        const int live = (int)min((int64_t)kStream, to - r0);    // streamed rows
         float s[kH][2], dp[kH][2];
 #pragma unroll
         for (int i = 0; i < kH; ++i) s[i][0] = s[i][1] = dp[i][0] = dp[i][1] = 0.f;
 #pragma unroll 4
-        for (int c = 0; c < DP; c += 4) {
+        for (int c = 0; c < a.D; c += 4) {
             float4 x0[2], x1[2];
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
@@ -366,19 +380,16 @@ __device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta)
                 wd[str * kWPad + held] = d;
             }
         __syncthreads();
-#pragma unroll 2
-        for (int r = 0; r < kStream; ++r) {
+#pragma unroll 4
+        for (int r = 0; r < live; ++r) {
             float p[kH], d[kH], x0[kC], x1[kC];
+            if (KEYS) load_shared<kH>(wp + r * kWPad + ty * kH, p);
+            load_shared<kH>(wd + r * kWPad + ty * kH, d);
 #pragma unroll
-            for (int i = 0; i < kH; ++i) {
-                p[i] = wp[r * kWPad + ty * kH + i];
-                d[i] = wd[r * kWPad + ty * kH + i];
-            }
-#pragma unroll
-            for (int c = 0; c < kC; ++c) {
-                const int col = (c / kV * 16 + tx) * kV + c % kV;
-                x0[c] = s0[r * kPad + col];
-                if (KEYS) x1[c] = s1[r * kPad + col];
+            for (int c = 0; c < kC; c += kV) {
+                const int col = (c / kV * 16 + tx) * kV;
+                load_shared<kV>(s0 + r * kPad + col, x0 + c);
+                if (KEYS) load_shared<kV>(s1 + r * kPad + col, x1 + c);
             }
 #pragma unroll
             for (int i = 0; i < kH; ++i)
