@@ -17,6 +17,7 @@
 #include "um_device.cuh"
 #include "um_overlap.cuh"
 #include "um_paged.cuh"
+#include "um_tc.cuh"
 
 namespace um {
 namespace attn_grad {
@@ -265,10 +266,22 @@ template <typename T, int DP, int ROWS> struct Block {
     }
 };
 
+// 4 floats of shared memory at the same place of another CTA of the cluster
+__device__ __forceinline__ float4 load_peer(const float *p, uint32_t rank) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(tc::mapa_shared(tc::smem_u32(p), rank))
+                 : "memory");
+    return v;
+}
+
 // KEYS: holds keys and values, streams queries and output gradients, writes dk
-// and dv; else the other way round, and dq.
+// and dv; else the other way round, and dq.  `ranks` CTAs of a cluster may share
+// out the steps of a block of keys, and then its rows, of which each adds the sums
+// of all in their order.
 template <typename T, int DP, int HELD, bool KEYS>
-__device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta) {
+__device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta, int rank, int ranks) {
     using S = Shape<DP, HELD>;
     constexpr int kPad = S::kPad, kWPad = S::kWPad;
     constexpr int kH = HELD / 16;                        // held rows of a thread's scores
@@ -321,8 +334,8 @@ __device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta)
             di[threadIdx.x] = r.y;
         }
     }
-    if (S::kPrefetch) fetch(0);
-    for (int j = 0; j < steps; ++j) {
+    if (S::kPrefetch && rank < steps) fetch(rank);
+    for (int j = rank; j < steps; j += ranks) {
         const int64_t r0 = from + (int64_t)(j % per_head) * kStream;
         if (!S::kPrefetch) fetch(j);
         __syncthreads();
@@ -333,7 +346,7 @@ __device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta)
             di[threadIdx.x] = row.y;
         }
         __syncthreads();
-        if (S::kPrefetch && j + 1 < steps) fetch(j + 1);
+        if (S::kPrefetch && j + ranks < steps) fetch(j + ranks);
         const int live = (int)min((int64_t)kStream, to - r0);    // streamed rows
         float s[kH][2], dp[kH][2];
 #pragma unroll
@@ -402,6 +415,38 @@ __device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta)
     }
     T *o1 = static_cast<T *>(KEYS ? a.dk : a.dq), *o0 = static_cast<T *>(a.dv);
     const int64_t out1 = KEYS ? a.dk_stride : a.dq_stride;
+    if (KEYS && ranks > 1) {
+        __syncthreads();                                 // what the sums read is not needed any more
+#pragma unroll
+        for (int i = 0; i < kH; ++i)
+#pragma unroll
+            for (int c = 0; c < kC; ++c) {
+                const int at = (ty * kH + i) * kPad + (c / kV * 16 + tx) * kV + c % kV;
+                h0[at] = acc0[i][c];
+                h1[at] = acc1[i][c];
+            }
+        tc::cluster_sync();
+        const int pieces = a.D / 4;
+        for (int k = threadIdx.x; k < HELD / ranks * pieces; k += kThreads) {
+            const int r = rank + k / pieces * ranks, col = k % pieces * 4;
+            if (first + r >= end) continue;
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                const float *from = (o ? h1 : h0) + r * kPad + col;
+                float4 v = load_peer(from, 0);
+                for (int p = 1; p < ranks; ++p) {
+                    const float4 x = load_peer(from, p);
+                    v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
+                }
+                T *out = o ? o1 + (first + r) * out1 : o0 + (first + r) * a.dv_stride;
+                out += (int64_t)head * a.D + col;
+                out[0] = from_f<T>(v.x), out[1] = from_f<T>(v.y);
+                out[2] = from_f<T>(v.z), out[3] = from_f<T>(v.w);
+            }
+        }
+        tc::cluster_sync();                              // peers have read this CTA's sums
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < kH; ++i) {
         const int64_t at = first + ty * kH + i;
@@ -416,7 +461,8 @@ __device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta)
     }
 }
 
-// Both roles in one launch, held keys first.
+// Both roles in one launch, held keys first: a cluster a block of keys, or as many
+// blocks of rows as it has CTAs.
 template <typename T, int DP, int HELD>
 __global__ void __launch_bounds__(kThreads) rows_kernel(Args a) {
     extern __shared__ float sm[];
@@ -424,17 +470,19 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(Args a) {
     pdl_trigger();
     const unsigned keys = (unsigned)a.most * a.kv_heads;
     if (blockIdx.x < keys)
-        rows_run<T, DP, HELD, true>(sm, a, blockIdx.x);
+        rows_run<T, DP, HELD, true>(sm, a, blockIdx.x, blockIdx.z, gridDim.z);
     else
-        rows_run<T, DP, HELD, false>(sm, a, blockIdx.x - keys);
+        rows_run<T, DP, HELD, false>(sm, a, (blockIdx.x - keys) * gridDim.z + blockIdx.z, 0, 1);
 }
 
 template <typename T, int DP, int HELD> cudaError_t rows_go(const Args &a, cudaStream_t st) {
     constexpr size_t smem = Shape<DP, HELD>::kSmem;
     const cudaError_t e = allow_dynamic_smem<rows_kernel<T, DP, HELD>>(smem);
     if (e != cudaSuccess) return e;
-    return launch_kernel(true, rows_kernel<T, DP, HELD>,
-                         dim3((unsigned)a.most * (a.kv_heads + a.q_heads)), kThreads, smem, st, a);
+    const unsigned ranks = (unsigned)a.ranks, most = (unsigned)a.most;
+    const unsigned keys = most * a.kv_heads, rows = (most * a.q_heads + ranks - 1) / ranks;
+    return launch_kernel(true, ranks, rows_kernel<T, DP, HELD>, dim3(keys + rows, 1, ranks), kThreads,
+                         smem, st, a);
 }
 template <typename T, int DP> cudaError_t rows_held(const Args &a, cudaStream_t st) {
     return a.block == 32 ? rows_go<T, DP, 32>(a, st) : rows_go<T, DP, 64>(a, st);
@@ -467,6 +515,26 @@ template <typename T> cudaError_t launch_prepare(const Args &a, cudaStream_t st)
 // higher blocks would leave SMs idle.
 int block_of(int32_t T, int32_t heads, int32_t dim) {
     return dim > 128 || (int64_t)T / 64 * heads < 2 * device_sm_count() ? 32 : 64;
+}
+
+// CTAs that share out the steps of held keys on the CUDA cores.  A block of keys
+// has the query heads' steps one after another, `group` times those of a block of
+// rows: where that is far more than a slot's part of the whole batch, it
+// is divided until it is not (4 sequences of 512, 8 heads on 2 x 64: 358 us by
+// one CTA, 184 by 2, 179 by 4), and no more, because each holds and adds the block
+// again (16 sequences of 1000: 2353, 2394, 2564).  Less than rows' own steps helps
+// only while there are SMs to spare.  By the mean length: the host does not know the
+// others.
+int ranks_of(const Args &a) {
+    const int64_t mean = (a.T / a.n_seqs + kStream - 1) / kStream, steps = a.group * mean;
+    const int64_t all = (int64_t)a.most * a.q_heads * (mean + 1);    // of both roles
+    const int64_t slots = 2 * (int64_t)device_sm_count();
+    auto ctas = [&](int n) { return (int64_t)a.most * ((int64_t)n * a.kv_heads + a.q_heads); };
+    int n = 1;
+    while (n < 8 && 2 * n <= steps && 5 * steps * slots > 8 * n * all &&
+           (2 * n <= a.group || 2 * ctas(2 * n) <= slots))
+        n *= 2;
+    return n;
 }
 
 // Blocks of the sequences, at most: whole ones, and a short one for each that
@@ -594,6 +662,7 @@ extern "C" ultramem_status ultramem_paged_attention_backward(const ultramem_atte
     a.most = (int)most_blocks(p->n_tokens, p->n_seqs, a.block);
     a.scale = p->scale;
     a.scale_log2 = p->scale * kLog2e;
+    a.ranks = ranks_of(a);
     cudaStream_t st = (cudaStream_t)stream;
     cudaGetLastError();
     cudaError_t e;

@@ -26,6 +26,7 @@ struct Args {
     int n_seqs, T, q_heads, kv_heads, group, D;
     int block;                // rows of a block
     int most;                 // blocks that a list holds
+    int ranks;                // CTAs to a block (CUDA cores)
     int wide;                 // inputs whose rows allow loads of 4 entries
     float scale, scale_log2;
 };

@@ -123,6 +123,23 @@ def test_longer_sequences(gpu_lib, dtype, lens, H, heads, D):
     check(got, q, k, v, out, lse, dout, lens, scale)
 
 
+@pytest.mark.parametrize("dtype,lens,H,heads,D", [
+    (F32, [1] * 5, 8, 1, 64), (F32, [120], 4, 1, 80), (F32, [33], 1, 1, 64),
+    (F32, [512] * 4, 8, 2, 64), (F32, [1, 40, 7], 20, 4, 128), (F32, [100] * 16, 16, 2, 80),
+    (BF16, [250], 8, 1, 136), (BF16, [200, 3], 2, 1, 256), (F32, [0, 70, 0, 0], 64, 1, 8)])
+def test_blocks_shared_out(gpu_lib, dtype, lens, H, heads, D):
+    """Batches too short for one block of keys a thread block on the CUDA cores."""
+    q, k, v, out, lse, dout, start, scale = inputs(lens, H, heads, D, dtype)
+    T = q.shape[0]
+    given = [torch.full((T + 2, *x.shape[1:]), 9.0, dtype=dtype, device="cuda") for x in (q, k, v)]
+    dq, dk, dv = (x[1:T + 1] for x in given)
+    got = paged.paged_attention_backward(q, k, v, out, lse, dout, start, dq=dq, dk=dk, dv=dv)
+    check(got, q, k, v, out, lse, dout, lens, scale)
+    assert all(bool((x[0] == 9).all()) and bool((x[-1] == 9).all()) for x in given)
+    again = paged.paged_attention_backward(q, k, v, out, lse, dout, start)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("D", [64, 128])
 def test_rows_of_no_sequence(gpu_lib, dtype, D):
