@@ -266,16 +266,6 @@ template <typename T, int DP, int ROWS> struct Block {
     }
 };
 
-// 4 floats of shared memory at the same place of another CTA of the cluster
-__device__ __forceinline__ float4 load_peer(const float *p, uint32_t rank) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "r"(tc::mapa_shared(tc::smem_u32(p), rank))
-                 : "memory");
-    return v;
-}
-
 // KEYS: holds keys and values, streams queries and output gradients, writes dk
 // and dv; else the other way round, and dq.  `ranks` CTAs of a cluster may share
 // out the steps of a block of keys, and then its rows, of which each adds the sums
@@ -444,6 +434,7 @@ __device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta,
                 out[2] = from_f<T>(v.z), out[3] = from_f<T>(v.w);
             }
         }
+        __syncwarp();
         tc::cluster_sync();                              // peers have read this CTA's sums
         return;
     }
@@ -479,10 +470,8 @@ template <typename T, int DP, int HELD> cudaError_t rows_go(const Args &a, cudaS
     constexpr size_t smem = Shape<DP, HELD>::kSmem;
     const cudaError_t e = allow_dynamic_smem<rows_kernel<T, DP, HELD>>(smem);
     if (e != cudaSuccess) return e;
-    const unsigned ranks = (unsigned)a.ranks, most = (unsigned)a.most;
-    const unsigned keys = most * a.kv_heads, rows = (most * a.q_heads + ranks - 1) / ranks;
-    return launch_kernel(true, ranks, rows_kernel<T, DP, HELD>, dim3(keys + rows, 1, ranks), kThreads,
-                         smem, st, a);
+    return launch_kernel(true, (unsigned)a.ranks, rows_kernel<T, DP, HELD>, grid_of(a), kThreads, smem,
+                         st, a);
 }
 template <typename T, int DP> cudaError_t rows_held(const Args &a, cudaStream_t st) {
     return a.block == 32 ? rows_go<T, DP, 32>(a, st) : rows_go<T, DP, 64>(a, st);
@@ -517,22 +506,22 @@ int block_of(int32_t T, int32_t heads, int32_t dim) {
     return dim > 128 || (int64_t)T / 64 * heads < 2 * device_sm_count() ? 32 : 64;
 }
 
-// CTAs that share out the steps of held keys on the CUDA cores.  A block of keys
-// has the query heads' steps one after another, `group` times those of a block of
-// rows: where that is far more than a slot's part of the whole batch, it
-// is divided until it is not (4 sequences of 512, 8 heads on 2 x 64: 358 us by
-// one CTA, 184 by 2, 179 by 4), and no more, because each holds and adds the block
-// again (16 sequences of 1000: 2353, 2394, 2564).  Less than rows' own steps helps
-// only while there are SMs to spare.  By the mean length: the host does not know the
-// others.
-int ranks_of(const Args &a) {
-    const int64_t mean = (a.T / a.n_seqs + kStream - 1) / kStream, steps = a.group * mean;
+// CTAs that share out the steps of a block of held keys, with streamed blocks of
+// `stream` rows and room for `slots` CTAs.  A block of keys has the query heads'
+// steps one after another, `group` times those of a block of rows: where that is
+// far more than a slot's part of the whole batch, it is divided until it is not, and
+// no more, because each CTA holds and adds the block again.  (By 1, 2, 4 CTAs: bf16, one
+// sequence of 4096, 8 heads on 1 x 128, 323, 172, 99 us, 32 heads on 8, 320, 341, 424;
+// fp32, 4 sequences of 512, 8 heads on 2 x 64, 358, 184, 179, 16 of 1000, 2353, 2394,
+// 2564.)  More than `group` CTAs help only while `spare` SMs would be idle.  By the
+// mean length: the host does not know the others.
+int ranks_of(const Args &a, int stream, int64_t slots, int64_t spare) {
+    const int64_t mean = (a.T / a.n_seqs + stream - 1) / stream, steps = a.group * mean;
     const int64_t all = (int64_t)a.most * a.q_heads * (mean + 1);    // of both roles
-    const int64_t slots = 2 * (int64_t)device_sm_count();
     auto ctas = [&](int n) { return (int64_t)a.most * ((int64_t)n * a.kv_heads + a.q_heads); };
     int n = 1;
     while (n < 8 && 2 * n <= steps && 5 * steps * slots > 8 * n * all &&
-           (2 * n <= a.group || 2 * ctas(2 * n) <= slots))
+           (2 * n <= a.group || ctas(2 * n) <= spare))
         n *= 2;
     return n;
 }
@@ -662,7 +651,8 @@ extern "C" ultramem_status ultramem_paged_attention_backward(const ultramem_atte
     a.most = (int)most_blocks(p->n_tokens, p->n_seqs, a.block);
     a.scale = p->scale;
     a.scale_log2 = p->scale * kLog2e;
-    a.ranks = ranks_of(a);
+    const int64_t sms = um::device_sm_count();
+    a.ranks = ranks_of(a, kStream, 2 * sms, sms);
     cudaStream_t st = (cudaStream_t)stream;
     cudaGetLastError();
     cudaError_t e;
@@ -677,6 +667,7 @@ extern "C" ultramem_status ultramem_paged_attention_backward(const ultramem_atte
         if (!(a.err = um::paged::error_word())) return ULTRAMEM_ENODEV;
         a.block = kTensorBlock;
         a.most = (int)most_blocks(p->n_tokens, p->n_seqs, kTensorBlock);
+        a.ranks = ranks_of(a, kTensorBlock, sms, 0);       // <= group, as the kernel needs
         CUtensorMap q, k, v, dout;
         auto map = [&](CUtensorMap *m, const void *x, int heads, int64_t stride) {
             return um::paged::encode(m, x, a.D, heads, T, a.D, stride, 1, kTensorBlock);

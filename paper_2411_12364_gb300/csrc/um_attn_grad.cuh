@@ -5,6 +5,7 @@
 #include <cuda.h>
 
 #include "um_internal.cuh"
+#include "um_tc.cuh"
 
 namespace um {
 namespace attn_grad {
@@ -26,10 +27,27 @@ struct Args {
     int n_seqs, T, q_heads, kv_heads, group, D;
     int block;                // rows of a block
     int most;                 // blocks that a list holds
-    int ranks;                // CTAs to a block (CUDA cores)
+    int ranks;                // CTAs that share out a block of keys
     int wide;                 // inputs whose rows allow loads of 4 entries
     float scale, scale_log2;
 };
+
+// Clusters of `ranks` CTAs: one for each block of held keys, and one for as many
+// blocks of held rows as it has CTAs.
+inline dim3 grid_of(const Args &a) {
+    const unsigned ranks = (unsigned)a.ranks, most = (unsigned)a.most;
+    return dim3(most * a.kv_heads + (most * a.q_heads + ranks - 1) / ranks, 1, ranks);
+}
+
+// 4 floats of shared memory at the same place of another CTA of the cluster
+__device__ __forceinline__ float4 load_peer(const float *p, uint32_t rank) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(tc::mapa_shared(tc::smem_u32(p), rank))
+                 : "memory");
+    return v;
+}
 
 // bf16, heads up to 128 wide (um_attn_grad_tc.cu): maps of boxes of 64 columns x
 // a head x 128 tokens over the inputs as [tokens][heads][width].

@@ -126,9 +126,10 @@ def test_longer_sequences(gpu_lib, dtype, lens, H, heads, D):
 @pytest.mark.parametrize("dtype,lens,H,heads,D", [
     (F32, [1] * 5, 8, 1, 64), (F32, [120], 4, 1, 80), (F32, [33], 1, 1, 64),
     (F32, [512] * 4, 8, 2, 64), (F32, [1, 40, 7], 20, 4, 128), (F32, [100] * 16, 16, 2, 80),
-    (BF16, [250], 8, 1, 136), (BF16, [200, 3], 2, 1, 256), (F32, [0, 70, 0, 0], 64, 1, 8)])
+    (BF16, [250], 8, 1, 136), (BF16, [200, 3], 2, 1, 256), (F32, [0, 70, 0, 0], 64, 1, 8),
+    (BF16, [700], 8, 1, 128), (BF16, [129, 1, 1000], 16, 2, 64), (BF16, [5] * 3, 10, 2, 80)])
 def test_blocks_shared_out(gpu_lib, dtype, lens, H, heads, D):
-    """Batches too short for one block of keys a thread block on the CUDA cores."""
+    """Batches in which several thread blocks share out a block of keys."""
     q, k, v, out, lse, dout, start, scale = inputs(lens, H, heads, D, dtype)
     T = q.shape[0]
     given = [torch.full((T + 2, *x.shape[1:]), 9.0, dtype=dtype, device="cuda") for x in (q, k, v)]
