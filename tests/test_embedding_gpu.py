@@ -116,6 +116,40 @@ def test_gradient(gpu_lib, T, V, D, dtype, table_dtype):
         assert torch.equal(got, again)
 
 
+@pytest.mark.parametrize("T,V,D", [(512, 3, 1024), (512, 1, 8), (513, 40, 16), (512, 70001, 24),
+                                   (257, 609, 100), (60, 607, 8200), (500, 2, 1), (7, 1300, 2056)])
+@pytest.mark.parametrize("dtype,table_dtype", [(BF16, BF16), (F32, BF16), (BF16, F32)])
+def test_short_batches(gpu_lib, T, V, D, dtype, table_dtype):
+    """About the size up to which one launch does it all."""
+    g = gen(T + V + 7 * D)
+    ids = torch.randint(-1, V + 1, (T,), generator=g, device="cuda")
+    ids = torch.where(torch.rand(T, generator=g, device="cuda") < 0.3, V - 1, ids)
+    dout = randn(g, T, D, dtype=dtype)
+    want, size, count = reference(ids, dout, V, -1.5)
+    flat = torch.full((V + 2, D), 5.0, dtype=table_dtype, device="cuda")
+    got = vocab.embedding_backward(ids, dout, V, scale=-1.5, dtable=flat[1:V + 1])
+    assert bool(((got.double() - want).abs() <= bound(want, size, count, table_dtype)).all())
+    assert bool((flat[0] == 5).all()) and bool((flat[-1] == 5).all())
+    again = vocab.embedding_backward(ids.int(), dout, V, scale=-1.5,
+                                     dtable=torch.empty_like(got))
+    assert torch.equal(got, again)
+    old = randn(g, V, D, dtype=table_dtype)
+    got = vocab.embedding_backward(ids, dout, V, scale=-1.5, dtable=old.clone(), accumulate=True)
+    allowed = bound(want + old.double(), size + old.double().abs(), count + 1, table_dtype)
+    assert bool(((got.double() - want - old.double()).abs() <= allowed).all())
+    still = (count == 0).squeeze(1)
+    assert torch.equal(got[still], old[still])
+
+
+def test_sorted_gradient_offsets_past_32_bits(gpu_lib):
+    V, D, T = 2 ** 20 + 3, 4096, 600
+    dout = torch.ones(T, D, dtype=BF16, device="cuda")
+    ids = torch.full((T,), V - 1, device="cuda")
+    ids[::2] = V - 2
+    grad = vocab.embedding_backward(ids, dout, V)
+    assert bool((grad[-2:] == 300).all()) and int((grad != 0).sum()) == 2 * D
+
+
 def test_gradient_of_rows_apart_and_of_nothing(gpu_lib):
     g = gen(5)
     for start in (0, 3):
