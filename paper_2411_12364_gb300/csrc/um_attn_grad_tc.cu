@@ -29,8 +29,8 @@
 // a chain of loads from TMEM, exponentials, stores and barriers; eight warps for
 // them took 2500 cycles a block, waiting for one another's latencies.
 //
-// 4 sequences of 4096, 16 heads on 4 x 128: 609 us, 1.6 PFLOP/s of the seven
-// products, tensor pipe 71 % active; 24 of up to 2048, 16 heads on 2 x 64: 430 us,
+// 4 sequences of 4096, 16 heads on 4 x 128: 610 us, 1.6 PFLOP/s of the seven
+// products, tensor pipe 71 % active; 24 of up to 2048, 16 heads on 2 x 64: 438 us,
 // 38 % active, bound by that chain.
 #include "um_attn_grad.cuh"
 

@@ -10,7 +10,8 @@
 // G = scale dloss (e^(z - lse) - onehot) goes to the workspace in the storage
 // type, and two products read it: dx = G W (summed over the pieces) and
 // dw = G^T x (a piece's rows).  Bound by the tensor cores: 2 T V D operations
-// a product.
+// a product.  16384 tokens x 32000 x 2048 bf16: 1170 us (1.84 PFLOP/s) and, with the
+// gradient under the power cap, 4080 (1.58).
 //
 // Storage in fp32 enters the products as three bf16 terms a value, v = a + b + c
 // with residues of 2^-9, 2^-17 and 2^-25 of |v|; the six products of terms that
