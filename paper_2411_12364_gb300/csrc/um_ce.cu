@@ -21,6 +21,7 @@
 #include "um_paged.cuh"
 #include "um_pair.cuh"
 #include "um_pair_gemm.cuh"
+#include "um_planes.cuh"
 
 namespace um {
 namespace ce {
@@ -64,9 +65,10 @@ __device__ __forceinline__ __nv_bfloat16 take_term(float &v) {
 
 // ---- operands as planes --------------------------------------------------------
 // src [R][D] (rows ld apart) -> dst [planes][R][Dp], Dp = D rounded up to 64, so
-// that rows start on 128 bytes: fp32 values as three bf16 terms, bf16 ones as
-// they are, for operands that TMA cannot read well where they lie.  With `labels`, rows of tokens that do not
-// count become zeros, so that weight 0 never meets what they hold.
+// that rows start on 128 bytes, with zeros behind a row: fp32 values as three bf16
+// terms, bf16 ones as they are, for operands that TMA cannot read well where they
+// lie.  With `labels`, rows of tokens that do not count become zeros, so that
+// weight 0 never meets what they hold.
 template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(256)
     planes_kernel(const T *src, int64_t ld, int64_t R, int D, int Dp, __nv_bfloat16 *dst,
@@ -80,23 +82,13 @@ __global__ void __launch_bounds__(256)
         const int64_t r = i / pieces;
         const int c = (int)(i - r * pieces) * 8;
         const bool counts = !labels.at || labels(r) >= 0;
-        float v[8];
-        if (ALIGNED && counts) {
-            if constexpr (P == 1) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(src + r * ld + c);
-                *reinterpret_cast<uint4 *>(dst + r * Dp + c) = x;
-                continue;
-            } else {
-                const float4 x = reinterpret_cast<const float4 *>(src + r * ld + c)[0];
-                const float4 y = reinterpret_cast<const float4 *>(src + r * ld + c)[1];
-                v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-                v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                v[k] = counts && c + k < D ? to_f(src[r * ld + c + k]) : 0.f;
+        const Piece<T> from = counts ? read_piece(src + r * ld, c, D, ALIGNED) : Piece<T>{};
+        if constexpr (P == 1) {
+            *reinterpret_cast<uint4 *>(dst + r * Dp + c) = from.x[0];
+            continue;
         }
+        float v[8];
+        memcpy(v, &from, sizeof v);
 #pragma unroll
         for (int q = 0; q < P; ++q) {
             uint32_t o[4];
