@@ -583,7 +583,7 @@ int64_t ultramem_embedding_backward_workspace(int32_t n_tokens, int32_t dim);
 /* The softmax cross entropy of hidden states x [n_tokens][dim] against the
  * output weights w [vocab][dim] (both `dtype`):
  *   z_tv = logit_scale x_t . w_v,  lse_t = log sum_v e^(z_tv),
- *   loss_t = lse_t - z_{t, label_t}
+ *   loss_t = lse_t - z_{t, label_t}  (computed so that it is at least 0)
  * A label outside [0, vocab) marks a token that does not count: its loss is 0
  * and it takes no part in the gradient, whatever its x holds (its lse is
  * computed all the same).  The logits are made tile by tile and not kept.

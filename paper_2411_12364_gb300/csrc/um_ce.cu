@@ -109,17 +109,24 @@ __global__ void __launch_bounds__(256)
 // are cut (lse of 2048 entries off by 6e-7 of its size, growing with the
 // entries; in sums of 1024 by 4e-7, and 16384 x 32000 x 2048 in 1366 instead of 1314 us).
 constexpr int kLongSum = 2048;
+// what turns a difference of products (of the scale's sign) into one of exponents
+__device__ __forceinline__ float log2_units(float scale_log2) {
+    return scale_log2 == 0.f ? 1.f : fabsf(scale_log2);
+}
 template <int SUM> struct LseEpi {
     static constexpr int kSumBlocks = SUM;
     Labels labels;
-    float2 *part;             // [half tiles][T]: maximum (log2 units) and sum
-    float *target;            // [T]: the label's logit
+    // Maxima and the label's product are kept as the products come (their sign
+    // turned where the scale is negative, 0 where it is 0): differences of them
+    // are then 0 or of one sign without an error, and so is the loss made of them.
+    float2 *part;             // [half tiles][T]: maximum, sum of e^(|scale| (product - maximum))
+    float *target;            // [T]: the label's product
     int T, vn, v0, tile0;     // columns of the piece, its first one, its first half tile
     int n_tile;
-    float scale, scale_log2;
+    float scale_log2;
 
     template <int N> LseEpi<N> cut() const {
-        return {labels, part, target, T, vn, v0, tile0, n_tile, scale, scale_log2};
+        return {labels, part, target, T, vn, v0, tile0, n_tile, scale_log2};
     }
     __device__ __forceinline__ int64_t fetch(const pair::Tile &t, int row) const {
         const int64_t tok = t.m0 + row;
@@ -132,9 +139,7 @@ template <int SUM> struct LseEpi {
         const int64_t tok = t.m0 + row;
         const int label = labels.of(loaded) - (v0 + t.n0);       // the tile's column
         const int cols = min(c1, vn - t.n0);
-        // to log2 units; where the scale is negative the sums change their sign first,
-        // and where it is 0 they become 0
-        const float by = scale_log2 == 0.f ? 1.f : fabsf(scale_log2);
+        const float by = log2_units(scale_log2);
         float m = -INFINITY, l = 0.f;
 #pragma unroll
         for (int i = 0; i < Sums::kChunks; ++i) {
@@ -142,14 +147,14 @@ template <int SUM> struct LseEpi {
             if (c >= cols) break;
             float place[32];
             float (&z)[32] = sums.get(i, place);
-            if (label >= c && label < c + 32) {
-#pragma unroll
-                for (int k = 0; k < 32; ++k)
-                    if (label == c + k) target[tok] = z[k] * scale;
-            }
             if (scale_log2 <= 0.f) {
 #pragma unroll
                 for (int k = 0; k < 32; ++k) z[k] = scale_log2 < 0.f ? -z[k] : z[k] * 0.f;
+            }
+            if (label >= c && label < c + 32) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (label == c + k) target[tok] = z[k];
             }
             if (c + 32 > cols) {
 #pragma unroll
@@ -159,33 +164,39 @@ template <int SUM> struct LseEpi {
             float top = fmaxf(z[0], z[1]);
 #pragma unroll
             for (int k = 2; k < 32; k += 2) top = max3(top, z[k], z[k + 1]);
-            top = fmaxf(m, top * by);
+            top = fmaxf(m, top);
             const float shift = top == -INFINITY ? 0.f : top;
             const F2 f = f2(by), less = f2(-shift);
             F2 s[2] = {f2(0.f), f2(0.f)};
 #pragma unroll
             for (int k = 0; k < 32; k += 2) {
-                const float2 y = split(fma2(f2(z[k], z[k + 1]), f, less));
+                const float2 y = split((f2(z[k], z[k + 1]) + less) * f);
                 s[(k >> 1) & 1] = s[(k >> 1) & 1] + f2(tc::ex2(y.x), tc::ex2(y.y));
             }
-            l = fmaf(l, tc::ex2(m - shift), both(s[0] + s[1]));
+            l = fmaf(l, tc::ex2((m - shift) * by), both(s[0] + s[1]));
             m = top;
         }
         if (tok < T) part[(int64_t)(tile0 + 2 * (t.n0 / n_tile) + half) * T + tok] = make_float2(m, l);
     }
 };
 
-// A block joins the tiles' pairs of 32 tokens, a warp every 32nd tile.
+// A block joins the tiles' pairs of 32 tokens, a warp every 32nd tile.  The largest
+// product's term of the sum is exactly 1, so
+//   loss = |scale| (maximum - label's product) + ln(sum)
+// adds two values that are at least 0.  (As lse less the label's logit, each
+// rounded for itself, it came out as low as -4e-6 where a label of logit 60 held
+// nearly all the probability.)
 __global__ void __launch_bounds__(1024)
     join_kernel(const float2 *part, const float *target, Labels labels, int T, int tiles,
-                float *loss, float *lse) {
+                float scale, float scale_log2, float *loss, float *lse) {
     __shared__ float2 got[32][33];
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    auto add = [](float2 &a, float2 b) {
+    const float by = log2_units(scale_log2);
+    auto add = [by](float2 &a, float2 b) {
         const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.f : top;
-        a.y = a.y * tc::ex2(a.x - shift) + b.y * tc::ex2(b.x - shift);
+        a.y = a.y * tc::ex2((a.x - shift) * by) + b.y * tc::ex2((b.x - shift) * by);
         a.x = top;
     };
     for (int64_t t0 = (int64_t)blockIdx.x * 32; t0 < T; t0 += (int64_t)gridDim.x * 32) {
@@ -201,9 +212,9 @@ __global__ void __launch_bounds__(1024)
             add(a, make_float2(__shfl_xor_sync(0xffffffffu, a.x, o),
                                __shfl_xor_sync(0xffffffffu, a.y, o)));
         if (lane == 0 && t < T) {
-            const float v = kLn2 * (a.x + log2f(a.y));
-            lse[t] = v;
-            loss[t] = labels(t) >= 0 ? v - target[t] : 0.f;
+            const float size = fabsf(scale), rest = kLn2 * log2f(a.y);
+            lse[t] = fmaf(size, a.x, rest);
+            loss[t] = labels(t) >= 0 ? fmaf(size, a.x - target[t], rest) : 0.f;
         }
         __syncthreads();
     }
@@ -627,7 +638,6 @@ cudaError_t forward(const ultramem_cross_entropy_args *p, const ForwardLayout &l
     epi.part = reinterpret_cast<float2 *>(ws + l.part);
     epi.target = reinterpret_cast<float *>(ws + l.target);
     epi.T = p->n_tokens;
-    epi.scale = p->logit_scale;
     epi.scale_log2 = p->logit_scale * kLog2e;
     for (int64_t v0 = 0; v0 < p->vocab && e == cudaSuccess; v0 += piece) {
         const int64_t vn = p->vocab - v0 < piece ? p->vocab - v0 : piece;
@@ -659,7 +669,7 @@ cudaError_t forward(const ultramem_cross_entropy_args *p, const ForwardLayout &l
     const int64_t blocks = ceil_div(T, 32);
     return launch_kernel(true, join_kernel, dim3((unsigned)(blocks < 4096 ? blocks : 4096)), 1024, 0,
                          st, (const float2 *)epi.part, (const float *)epi.target, epi.labels,
-                         p->n_tokens, epi.tile0, loss, lse);
+                         p->n_tokens, epi.tile0, p->logit_scale, epi.scale_log2, loss, lse);
 }
 
 template <typename T, int P>
