@@ -109,6 +109,11 @@ __global__ void __launch_bounds__(256)
 // are cut (lse of 2048 entries off by 6e-7 of its size, growing with the
 // entries; in sums of 1024 by 4e-7, and 16384 x 32000 x 2048 in 1366 instead of 1314 us).
 constexpr int kLongSum = 2048;
+// what exponents are taken relative to: the maximum, or 0 beside an infinite one,
+// whose differences would be NaN
+__device__ __forceinline__ float shift_of(float top) {
+    return fabsf(top) == INFINITY ? 0.f : top;
+}
 // what turns a difference of products (of the scale's sign) into one of exponents
 __device__ __forceinline__ float log2_units(float scale_log2) {
     return scale_log2 == 0.f ? 1.f : fabsf(scale_log2);
@@ -165,7 +170,7 @@ template <int SUM> struct LseEpi {
 #pragma unroll
             for (int k = 2; k < 32; k += 2) top = max3(top, z[k], z[k + 1]);
             top = fmaxf(m, top);
-            const float shift = top == -INFINITY ? 0.f : top;
+            const float shift = shift_of(top);
             const F2 f = f2(by), less = f2(-shift);
             F2 s[2] = {f2(0.f), f2(0.f)};
 #pragma unroll
@@ -195,7 +200,7 @@ __global__ void __launch_bounds__(1024)
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const float by = log2_units(scale_log2);
     auto add = [by](float2 &a, float2 b) {
-        const float top = fmaxf(a.x, b.x), shift = top == -INFINITY ? 0.f : top;
+        const float top = fmaxf(a.x, b.x), shift = shift_of(top);
         a.y = a.y * tc::ex2((a.x - shift) * by) + b.y * tc::ex2((b.x - shift) * by);
         a.x = top;
     };
