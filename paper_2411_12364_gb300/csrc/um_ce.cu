@@ -190,7 +190,8 @@ template <int SUM> struct LseEpi {
 //   loss = |scale| (maximum - label's product) + ln(sum)
 // adds two values that are at least 0.  (As lse less the label's logit, each
 // rounded for itself, it came out as low as -4e-6 where a label of logit 60 held
-// nearly all the probability.)
+// nearly all the probability.  Exponents as differences times the scale instead of
+// one multiply-add: 5563 tokens x 107918 x 128 in 251 instead of 247.5 us.)
 __global__ void __launch_bounds__(1024)
     join_kernel(const float2 *part, const float *target, Labels labels, int T, int tiles,
                 float scale, float scale_log2, float *loss, float *lse) {
