@@ -209,8 +209,10 @@ __device__ __forceinline__ void run(uint8_t *sm, const CUtensorMap &map_h0,
             s_phase ^= 1u << sb;
             // these scores were issued behind dV of kScores steps before, and dP
             // behind dK of the step before: their stages are free
-            if (!C::kTwo && j >= C::kScores && w == 0 && lane == 0)
-                tc::mbar_arrive(&bar.short_empty[(j - C::kScores) % C::kShort]);
+            if (!C::kTwo && j >= C::kScores && w == 0) {
+                if (lane == 0) tc::mbar_arrive(&bar.short_empty[(j - C::kScores) % C::kShort]);
+                __syncwarp();
+            }
             tc::tc_fence_after();
             const uint32_t ts = lanes + 128 * sb + 32 * part, tdp = lanes + t_dp + 32 * part;
             uint32_t s[32], p[16];
@@ -248,8 +250,10 @@ __device__ __forceinline__ void run(uint8_t *sm, const CUtensorMap &map_h0,
                 if (lane == 0) tc::mbar_arrive(&bar.p_full[st]);
             }
             if (!tc::warp_wait(&bar.dp_full, j & 1)) return false;
-            if (!C::kTwo && j > 0 && w == 0 && lane == 0)
-                tc::mbar_arrive(&bar.long_empty[(j - 1) % C::kLong]);
+            if (!C::kTwo && j > 0 && w == 0) {
+                if (lane == 0) tc::mbar_arrive(&bar.long_empty[(j - 1) % C::kLong]);
+                __syncwarp();
+            }
             tc::tc_fence_after();
             uint32_t g[32];
             tc::tmem_ld32_nowait(tdp, g);
@@ -328,6 +332,7 @@ __device__ __forceinline__ void run(uint8_t *sm, const CUtensorMap &map_h0,
                 for (int c = 0; c < DP / 64; ++c) {
                     const int col = part * (DP / 4) + 16 * c;
                     float v[16];
+                    __syncwarp();                              // rows past the end go on below
                     tc::tmem_ld16(lanes + (o == 0 ? t_o0 : t_o1) + col, v);
 #pragma unroll
                     for (int k = 0; k < 16; ++k) asm volatile("" : "+f"(v[k]));   // after the wait

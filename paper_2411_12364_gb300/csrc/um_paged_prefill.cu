@@ -264,6 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int c = 0; c < DP / 32; ++c) {
                 uint32_t o[32];
                 if (any) {
+                    __syncwarp();                     // rows past the tile go on below
                     tc::tmem_ld32_nowait(to + 32 * c, o);
                     tc::tmem_ld_wait();
                     tc::arrived(o);

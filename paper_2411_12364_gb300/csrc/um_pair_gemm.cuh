@@ -156,6 +156,7 @@ __device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {  
 // 32 columns of this thread's accumulator row
 __device__ __forceinline__ void load32(uint32_t taddr, float (&v)[32]) {
     uint32_t r[32];
+    __syncwarp();                            // an operation may leave lanes early
     tc::tmem_ld32_nowait(taddr, r);
     tc::tmem_ld_wait();
     tc::arrived(r);

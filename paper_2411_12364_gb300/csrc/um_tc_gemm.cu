@@ -130,6 +130,7 @@ __device__ __forceinline__ void group_epilogue(const Op &op, const Tile &t, int 
 #pragma unroll
     for (int cc = 0; cc < NG / 2; ++cc) {
         uint32_t r[32];
+        __syncwarp();                                // waits and operations part lanes
         tmem_ld32_nowait(lane_base + (uint32_t)(cb + cc * 32), r);
         tmem_ld_wait();
 #pragma unroll
@@ -331,6 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const uint32_t cur = pre;
             if (c0 + 32 * kGroups < acc_n) pre = op.prefetch(t, row, c0 + 32 * kGroups);
             uint32_t r[kMaxAcc][32];
+            __syncwarp();
 #pragma unroll
             for (int a = 0; a < kMaxAcc; ++a)
                 if (a < op.n_acc) tmem_ld32_nowait(lane_base + (uint32_t)(a * acc_n + c0), r[a]);
@@ -363,6 +365,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float inv_per = 1.f / (float)per;
         for (int c0 = whalf * 32; c0 < n_tile; c0 += 32 * kGroups) {
             uint32_t r[32];
+            __syncwarp();
             tmem_ld32_nowait(lane_base + (uint32_t)c0, r);
             tmem_ld_wait();
 #pragma unroll
@@ -632,6 +635,7 @@ __global__ void __launch_bounds__(persistent_threads<Op>(), 1)
                     const uint32_t cur = pre;
                     if (c0 + 32 * kEG < acc_n) pre = op.prefetch(t, row, c0 + 32 * kEG);
                     uint32_t r[kMaxAcc][32];
+                    __syncwarp();
 #pragma unroll
                     for (int a = 0; a < kMaxAcc; ++a)
                         if (a < op.n_acc)
