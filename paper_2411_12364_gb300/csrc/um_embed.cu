@@ -26,14 +26,16 @@ constexpr int kMaxDim = 65536;
 
 // ---- values, 8 at a time where rows allow 16-byte accesses -------------------
 
+// Ordinary loads: the rows that sums are added to are written by the same kernel, and
+// partial sums by one that may still run when theirs starts.
 __device__ __forceinline__ void load8(const float *p, float (&v)[8]) {
-    const float4 a = __ldg(reinterpret_cast<const float4 *>(p));
-    const float4 b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+    const float4 a = reinterpret_cast<const float4 *>(p)[0];
+    const float4 b = reinterpret_cast<const float4 *>(p)[1];
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
     v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
 }
 __device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&v)[8]) {
-    const uint4 a = __ldg(reinterpret_cast<const uint4 *>(p));
+    const uint4 a = *reinterpret_cast<const uint4 *>(p);
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
