@@ -587,8 +587,12 @@ int64_t ultramem_embedding_backward_workspace(int32_t n_tokens, int32_t dim);
  * A label outside [0, vocab) marks a token that does not count: its loss is 0
  * and it takes no part in the gradient, whatever its x holds (its lse is
  * computed all the same).  The logits are made tile by tile and not kept.
- * Products of bf16 storage are exact and add in fp32; fp32 storage enters them
- * as three bf16 terms a value (24 bits).  logit_scale is finite.  loss and lse
+ * Products of bf16 storage are exact; their sums are fp32, truncated instead of
+ * rounded every 16 terms (less than 2^-23 of a sum each time; lse and loss of
+ * rows of more than 2048 entries: sums of 1024 at most, added up rounded).  fp32
+ * storage enters as three bf16 terms a value (24 bits), of which a sum of 64
+ * entries at most is truncated; an infinite entry, or a product past the range
+ * of fp32, makes the token's results NaN there.  logit_scale is finite.  loss and lse
  * fp32 [n_tokens]; they and the workspace (16-byte aligned) overlap nothing. */
 typedef struct ultramem_cross_entropy_args {
     const void *x, *w;
@@ -610,7 +614,9 @@ int64_t ultramem_cross_entropy_workspace(int32_t dtype, int32_t n_tokens, int32_
  *   G_tv = logit_scale dloss_t (e^(z_tv - lse_t) - [v = label_t]),
  *   dx = G w,  dw = G^T x
  * The logits are computed again in pieces of the vocabulary; G enters the
- * products in `dtype` (bf16 storage: rounded to bf16).  dx [n_tokens][dim] and
+ * products in `dtype` (bf16 storage: rounded to bf16).  Sums of bf16 storage
+ * are truncated as above, 65536 terms at most before they are added up in fp32
+ * (sums over more than 2^22 tokens: a 64th of them).  dx [n_tokens][dim] and
  * dw [vocab][dim], contiguous, of `dtype`; each NULL to skip.  They and the
  * workspace overlap nothing. */
 ultramem_status ultramem_cross_entropy_backward(const ultramem_cross_entropy_args *args,

@@ -433,21 +433,29 @@ int planes_of(int32_t dtype) { return dtype == ULTRAMEM_F32 ? 3 : 1; }
 // fewer tiles than pairs of SMs.
 // n_tile: the widest tile, unless narrower ones share out among the pairs more
 // evenly; `step` 32, or 128 where the columns are MN-major (boxes of 64 columns a CTA).
-// splits (at most `most`, 64 or fewer): a tile's time is its k blocks (2 cycles a
+// splits (at most `most`, 64 or fewer): as many as keep a sum below kMostSum terms in
+// the tensor cores, and more by time: a tile's time is its k blocks (2 cycles a
 // column, and no less than 480 for the copies: 128 columns took 615) and about 3000
 // cycles; a split costs a pass over the output in fp32.
+// kMostSum: the tensor cores cut off what a step of 16 terms loses in a sum's last
+// place, less than 2^-23 of it; 65536 terms of one sign lose less than 2^-11, an
+// eighth of half a step of bf16.  (fp32 storage adds its sums in fp32 after each k
+// block.)
+constexpr int64_t kMostSum = 65536;
 pair::Plan plan_of(int64_t M, int64_t N, int64_t K, int planes, int step, int most) {
     pair::Plan p = {};
     const int64_t pairs = pairs_of_sms();
     p.m_tiles = (int)ceil_div(M, pair::kTileM);
     p.k_blocks = (int)ceil_div(K, 64);
     const int pairs_of_planes = planes == 3 ? 6 : 1;
+    int least = planes == 3 ? 1 : (int)ceil_div(p.k_blocks, kMostSum / 64);
+    if (least > most) least = most;
     double best = 0;
     for (int n = planes == 3 ? pair::Shape<true>::kMaxN : pair::Shape<false>::kMaxN; n >= 128; n -= step) {
         const int64_t nt = ceil_div(N, n);
         // a second share of a pair's time is the last that a split can save
-        for (int s = 1; s <= most && s <= p.k_blocks; ++s) {
-            if (s > 1 && p.m_tiles * nt * (s - 1) >= 2 * pairs) break;
+        for (int s = least; s <= most && s <= p.k_blocks; ++s) {
+            if (s > least && p.m_tiles * nt * (s - 1) >= 2 * pairs) break;
             const int64_t waves = ceil_div(p.m_tiles * nt * s, pairs);
             const double block = pairs_of_planes * 2.0 * n;
             const double tile = (double)ceil_div(p.k_blocks, s) * (block > 480. ? block : 480.) + 3000.0;
