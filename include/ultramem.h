@@ -671,6 +671,13 @@ int32_t ultramem_debug_live_allocations(void);
  * ULTRAMEM_EINVAL for another mode. */
 ultramem_status ultramem_debug_candidates(ultramem_layer *layer, int32_t mode);
 
+/* Bytes of a piece of the vocabulary in the cross entropy and its gradient (G, or
+ * rearranged weights), for tests that want several pieces of a small one; 0: the
+ * default of 512 MB.  Holds for the workspace queries and calls of the process
+ * from then on: a call takes a workspace of the same setting.  ULTRAMEM_EINVAL
+ * for a negative number. */
+ultramem_status ultramem_debug_cross_entropy_piece(int64_t bytes);
+
 /* ABI version, currently 2. */
 int32_t ultramem_version(void);
 

@@ -38,7 +38,8 @@ EXPORTS = ("ultramem_create", "ultramem_destroy", "ultramem_forward",
            "ultramem_paged_attention_backward_workspace", "ultramem_embedding",
            "ultramem_embedding_backward", "ultramem_embedding_backward_workspace",
            "ultramem_cross_entropy", "ultramem_cross_entropy_workspace",
-           "ultramem_cross_entropy_backward", "ultramem_cross_entropy_backward_workspace")
+           "ultramem_cross_entropy_backward", "ultramem_cross_entropy_backward_workspace",
+           "ultramem_debug_cross_entropy_piece")
 
 
 class Config(C.Structure):
@@ -205,6 +206,8 @@ def load(path: str | None = None) -> C.CDLL:
         lib.ultramem_cross_entropy_backward.restype = I32
         lib.ultramem_cross_entropy_backward_workspace.argtypes = [I32] * 4
         lib.ultramem_cross_entropy_backward_workspace.restype = I64
+        lib.ultramem_debug_cross_entropy_piece.argtypes = [I64]
+        lib.ultramem_debug_cross_entropy_piece.restype = I32
         _lib = lib
         return lib
 

@@ -23,6 +23,8 @@
 #include "um_pair_gemm.cuh"
 #include "um_planes.cuh"
 
+#include <atomic>
+
 namespace um {
 namespace ce {
 namespace {
@@ -33,8 +35,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 // bytes of a piece's G, and of its weights where they are rearranged: large
 // enough that a piece's products fill the GPU many times over, and a
-// small part of its memory
+// small part of its memory.  Tests set fewer (ultramem_debug_cross_entropy_piece).
 constexpr int64_t kPieceBytes = 512ll << 20;
+std::atomic<int64_t> g_piece_bytes{kPieceBytes};
 
 struct Labels {
     const void *at;
@@ -539,7 +542,7 @@ bool sizes_ok(int32_t dtype, int32_t T, int32_t V, int32_t D) {
 
 // Rows of the vocabulary whose planes fit a piece's bytes.
 int64_t rows_in_planes(int32_t dtype, int32_t D) {
-    const int64_t n = kPieceBytes / (planes_of(dtype) * padded(D) * 2) / 256 * 256;
+    const int64_t n = g_piece_bytes.load() / (planes_of(dtype) * padded(D) * 2) / 256 * 256;
     return n < 256 ? 256 : n;
 }
 // `limit` rows or fewer a piece, in equal pieces of whole tiles
@@ -582,14 +585,15 @@ struct BackwardLayout {
 BackwardLayout backward_layout(int32_t dtype, int64_t T, int64_t V, int32_t D) {
     BackwardLayout l = {};
     const int P = planes_of(dtype);
-    int64_t limit = kPieceBytes / (2 * P * (T > 0 ? T : 1)) / 256 * 256;
+    const int64_t bytes = g_piece_bytes.load();
+    int64_t limit = bytes / (2 * P * (T > 0 ? T : 1)) / 256 * 256;
     if (limit < 256) limit = 256;
     const int64_t rows = rows_in_planes(dtype, D);
     l.piece = piece_of(V, limit < rows ? limit : rows);
     l.ld = (l.piece + 31) & ~31ll;
     // partial sums stay below a piece's bytes
-    auto most = [](int64_t m, int64_t n) {
-        const int64_t s = kPieceBytes / (m * n * 4);
+    auto most = [bytes](int64_t m, int64_t n) {
+        const int64_t s = bytes / (m * n * 4);
         return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
     };
     const int64_t t = T > 0 ? T : 1;
@@ -844,4 +848,10 @@ extern "C" ultramem_status ultramem_cross_entropy_backward(const ultramem_cross_
         p->dtype == ULTRAMEM_BF16
             ? backward<__nv_bfloat16, 1>(p, l, lse, dloss, dx, dw, ws, err, st)
             : backward<float, 3>(p, l, lse, dloss, dx, dw, ws, err, st));
+}
+
+extern "C" ultramem_status ultramem_debug_cross_entropy_piece(int64_t bytes) {
+    if (bytes < 0) return ULTRAMEM_EINVAL;
+    g_piece_bytes.store(bytes ? bytes : kPieceBytes);
+    return ULTRAMEM_OK;
 }
