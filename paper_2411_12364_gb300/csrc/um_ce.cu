@@ -495,14 +495,17 @@ cudaError_t multiply(const CUtensorMap &a, const CUtensorMap &b, const pair::Pla
 }
 
 // Whether a matrix is read where it lies: TMA wants rows on 16-byte boundaries.
-// Off 128 bytes it reads two lines for each row of a box, which costs a product
-// a third (logits of 9373 tokens x 14297 x 1400: 312 instead of 237 us); with
-// that many rows on the other side the copy pays.
-bool as_it_lies(int32_t dtype, const void *at, int64_t ld, int64_t others, int64_t most) {
-    const int align = others < most ? 16 : 128;
+// Off 128 bytes it reads two lines for each row of a box; a copy costs a launch and
+// a pass over the matrix, which pays from about 4096 tokens on and against as long a
+// vocabulary.  Read where they lie / copied, us, loss and gradient: 2048 tokens x
+// 14297 x 1400 57 / 68 and 196 / 205, x 32000 x 1000 94 / 111 and 285 / 298; 4096 x 60000
+// x 1000 355 / 337 and 1013 / 977; 8192 x 50000 x 328 228 / 242 and 900 / 844; 16384 x
+// 32000 x 1000 765 / 658 and 2215 / 2180.
+constexpr int64_t kShortSide = 4096;
+bool as_it_lies(int32_t dtype, const void *at, int64_t ld, int64_t T, int64_t V) {
+    const int align = T < kShortSide || V < kShortSide ? 16 : 128;
     return dtype == ULTRAMEM_BF16 && (uintptr_t)at % align == 0 && ld * 2 % align == 0;
 }
-constexpr int kMostForward = 2048, kMostBackward = 1024;
 int64_t padded(int64_t D) { return (D + 63) & ~63ll; }
 
 template <typename T>
@@ -644,12 +647,12 @@ cudaError_t forward(const ultramem_cross_entropy_args *p, const ForwardLayout &l
     cudaError_t e = cudaSuccess;
     bool pdl = false;
     Matrix x = {p->x, p->ld_x, T * p->ld_x, 1};
-    if (!as_it_lies(p->dtype, p->x, p->ld_x, p->vocab, kMostForward)) {
+    if (!as_it_lies(p->dtype, p->x, p->ld_x, T, p->vocab)) {
         x = {ws + l.x, Dp, T * Dp, P};
         e = to_planes(p->dtype, p->x, p->ld_x, T, D, ws + l.x, {}, false, st);
         pdl = true;
     }
-    const bool direct = as_it_lies(p->dtype, p->w, p->ld_w, T, kMostForward);
+    const bool direct = as_it_lies(p->dtype, p->w, p->ld_w, T, p->vocab);
     const int64_t piece = direct ? p->vocab : l.piece;
     LseEpi<0> epi = {};
     epi.labels = labels_of(p);
@@ -700,12 +703,12 @@ cudaError_t backward(const ultramem_cross_entropy_args *p, const BackwardLayout 
     // dw reads x with weights that are 0 for tokens that do not count
     bool pdl = false;
     Matrix x = {p->x, p->ld_x, N * p->ld_x, 1};
-    if (dw || !as_it_lies(p->dtype, p->x, p->ld_x, p->vocab, kMostBackward)) {
+    if (dw || !as_it_lies(p->dtype, p->x, p->ld_x, N, p->vocab)) {
         x = {ws + l.x, Dp, N * Dp, P};
         e = to_planes(p->dtype, p->x, p->ld_x, N, D, ws + l.x, labels_of(p), false, st);
         pdl = true;
     }
-    const bool direct = as_it_lies(p->dtype, p->w, p->ld_w, N, kMostBackward);
+    const bool direct = as_it_lies(p->dtype, p->w, p->ld_w, N, p->vocab);
     GradEpi<P> ge = {};
     ge.labels = labels_of(p);
     ge.lse = lse;

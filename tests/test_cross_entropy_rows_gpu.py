@@ -6,6 +6,8 @@ import pytest
 import torch
 
 from paper_2411_12364_gb300 import binding as b
+from paper_2411_12364_gb300 import vocab
+from tests.test_cross_entropy_gpu import check_backward, check_forward, inputs
 
 pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
@@ -39,3 +41,16 @@ def test_copies_end_with_their_rows(gpu_lib, dtype, D):
     assert torch.equal(copy.double().sum(0)[:, :D], x[:T, :D].double())
     assert not bool(copy[:, :, D:].any())
     assert bool(torch.isfinite(dx).all()) and bool(torch.isfinite(dw).all())
+
+
+@pytest.mark.parametrize("T,V", [(4095, 4200), (4100, 4200), (4200, 4095)])
+@pytest.mark.parametrize("D", [72, 128])
+def test_rows_where_they_lie_and_copied(gpu_lib, T, V, D):
+    """bf16 rows off 128 bytes: read where they lie, or copied where both sides are long."""
+    x, w, labels, dloss = inputs(T, V, D, BF16)
+    loss, lse = vocab.cross_entropy(x, w, labels)
+    check_forward(x, w, labels, 1.0, (loss, lse))
+    grads = vocab.cross_entropy_backward(x, w, labels, lse, dloss)
+    check_backward(x, w, labels, lse, dloss, 1.0, grads)
+    only = vocab.cross_entropy_backward(x, w, labels, lse, dloss, dw=False)
+    assert torch.equal(only[0], grads[0])
