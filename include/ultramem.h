@@ -525,7 +525,10 @@ int64_t ultramem_block_norm_backward_workspace(int64_t n_tokens, int32_t dim);
  * written.  The probabilities are computed again, none are stored; sums are
  * fp32 in a fixed order.  With bf16 storage P and dS enter the products as
  * bf16.  All tensors are rows of tokens, `*_stride` elements apart, of
- * heads x head_dim contiguous entries; lse fp32 [n_tokens][q_heads].
+ * heads x head_dim contiguous entries; lse fp32 [n_tokens][q_heads].  The
+ * tensor cores take bf16 storage of heads up to 128 wide whose tensors (lse
+ * aside) all start, and step from token to token, on 16 bytes; every other call
+ * runs on the CUDA cores, many times slower where sequences are long.
  * Outputs must not overlap one another, nor an input, and the workspace
  * (16-byte aligned, at least ..._workspace bytes) nothing (ULTRAMEM_EINVAL). */
 typedef struct ultramem_attention_grad {
@@ -593,7 +596,11 @@ int64_t ultramem_embedding_backward_workspace(int32_t n_tokens, int32_t dim);
  * storage enters as three bf16 terms a value (24 bits), of which a sum of 64
  * entries at most is truncated; an infinite entry, or a product past the range
  * of fp32, makes the token's results NaN there.  logit_scale is finite.  loss and lse
- * fp32 [n_tokens]; they and the workspace (16-byte aligned) overlap nothing. */
+ * fp32 [n_tokens]; they and the workspace (16-byte aligned) overlap nothing.
+ * The workspace has room for copies of x and of a piece of w (512 MB at most),
+ * which fp32 storage takes, and bf16 storage where rows are off 16 bytes, or off
+ * 128 with 4096 tokens and more against as long a vocabulary: the query does not
+ * know where they lie, so that other calls leave that room untouched. */
 typedef struct ultramem_cross_entropy_args {
     const void *x, *w;
     const void *labels;           /* [n_tokens], int32 or int64                               */
@@ -618,7 +625,9 @@ int64_t ultramem_cross_entropy_workspace(int32_t dtype, int32_t n_tokens, int32_
  * are truncated as above, 65536 terms at most before they are added up in fp32
  * (sums over more than 2^22 tokens: a 64th of them).  dx [n_tokens][dim] and
  * dw [vocab][dim], contiguous, of `dtype`; each NULL to skip.  They and the
- * workspace overlap nothing. */
+ * workspace overlap nothing.  The workspace is one for both, with the room for
+ * copies as above, for a piece of G (512 MB at most, or 256 rows of the vocabulary)
+ * and for partial sums (512 MB at most each for dx and dw, or one dx in fp32). */
 ultramem_status ultramem_cross_entropy_backward(const ultramem_cross_entropy_args *args,
                                                 const float *lse, const float *dloss, void *dx,
                                                 void *dw, void *workspace, int64_t workspace_bytes,

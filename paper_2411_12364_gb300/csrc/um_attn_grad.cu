@@ -31,7 +31,8 @@ template <typename T, bool WIDE> struct Eight {
     __device__ __forceinline__ void get(const T *p) {
         if constexpr (WIDE) {
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) x[i] = reinterpret_cast<const uint4 *>(p)[i];
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+                x[i] = reinterpret_cast<const uint4 *>(p)[i];
         } else {
             T v[8];
 #pragma unroll
@@ -151,8 +152,10 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256)
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const int per_row = 1 << lanes_log2, part = lane & (per_row - 1);
     const int64_t rows = (int64_t)a.T * a.q_heads;
-    const int64_t per_warp = 32 >> lanes_log2, step = (int64_t)(gridDim.x - 1) * 8 * per_warp * kAhead;
-    const int64_t first = ((int64_t)(blockIdx.x - 1) * 8 + w) * per_warp * kAhead + (lane >> lanes_log2);
+    const int64_t per_warp = 32 >> lanes_log2;
+    const int64_t step = (int64_t)(gridDim.x - 1) * 8 * per_warp * kAhead;
+    const int64_t first =
+        ((int64_t)(blockIdx.x - 1) * 8 + w) * per_warp * kAhead + (lane >> lanes_log2);
     for (int64_t i0 = first; i0 - (lane >> lanes_log2) < rows; i0 += step) {
         Eight<T, WIDE> x[kAhead], y[kAhead];
         int64_t t[kAhead];
@@ -189,7 +192,8 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(256)
             if (part == 0 && i0 + k * per_warp < rows) {
                 const float lse = a.lse[i0 + k * per_warp];
                 // weights e^(score - inf) = 0 for a row that saw nothing
-                a.rows[(int64_t)h[k] * a.T + t[k]] = make_float2(lse == -INFINITY ? INFINITY : lse, s);
+                a.rows[(int64_t)h[k] * a.T + t[k]] =
+                    make_float2(lse == -INFINITY ? INFINITY : lse, s);
             }
         }
     }
@@ -271,7 +275,8 @@ template <typename T, int DP, int ROWS> struct Block {
 // out the steps of a block of keys, and then its rows, of which each adds the sums
 // of all in their order.
 template <typename T, int DP, int HELD, bool KEYS>
-__device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta, int rank, int ranks) {
+__device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta, int rank,
+                                         int ranks) {
     using S = Shape<DP, HELD>;
     constexpr int kPad = S::kPad, kWPad = S::kWPad;
     constexpr int kH = HELD / 16;                        // held rows of a thread's scores
@@ -406,7 +411,7 @@ __device__ __forceinline__ void rows_run(float *sm, const Args &a, unsigned cta,
     T *o1 = static_cast<T *>(KEYS ? a.dk : a.dq), *o0 = static_cast<T *>(a.dv);
     const int64_t out1 = KEYS ? a.dk_stride : a.dq_stride;
     if (KEYS && ranks > 1) {
-        __syncthreads();                                 // what the sums read is not needed any more
+        __syncthreads();                                 // what the sums read may go
 #pragma unroll
         for (int i = 0; i < kH; ++i)
 #pragma unroll

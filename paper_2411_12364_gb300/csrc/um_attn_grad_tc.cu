@@ -69,8 +69,8 @@ template <int DP, bool KEYS> struct Cfg {
 
 struct Bars {
     uint64_t held, long_full[4], long_raw[4], long_empty[4], short_full[4], short_raw[4],
-        short_empty[4], s_full[2], dp_full, p_full[2], ds_full[2], row_full[2], row_empty[2], out_full,
-        drained[2];
+        short_empty[4], s_full[2], dp_full, p_full[2], ds_full[2], row_full[2], row_empty[2],
+        out_full, drained[2];
     uint32_t tmem;
 };
 static_assert(sizeof(Bars) <= 512, "barriers");

@@ -184,7 +184,8 @@ template <int SUM> struct LseEpi {
             l = fmaf(l, tc::ex2((m - shift) * by), both(s[0] + s[1]));
             m = top;
         }
-        if (tok < T) part[(int64_t)(tile0 + 2 * (t.n0 / n_tile) + half) * T + tok] = make_float2(m, l);
+        if (tok < T)
+            part[(int64_t)(tile0 + 2 * (t.n0 / n_tile) + half) * T + tok] = make_float2(m, l);
     }
 };
 
@@ -231,12 +232,6 @@ __global__ void __launch_bounds__(1024)
 
 // ---- gradient ------------------------------------------------------------------
 
-// a whole sector by one thread (dst 32-byte aligned)
-__device__ __forceinline__ void store_sector(void *dst, const uint32_t (&r)[8]) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(r[0]),
-                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-                 : "memory");
-}
 // 32 values to a row of T, on a 32-byte boundary
 template <typename T> __device__ __forceinline__ void store32(T *to, const float (&v)[32]) {
 #pragma unroll
@@ -247,11 +242,12 @@ template <typename T> __device__ __forceinline__ void store32(T *to, const float
             if constexpr (sizeof(T) == 4) {
                 o[j] = __float_as_uint(v[8 * k + j]);
             } else {
-                const __nv_bfloat162 b = __floats2bfloat162_rn(v[16 * k + 2 * j], v[16 * k + 2 * j + 1]);
+                const __nv_bfloat162 b =
+                    __floats2bfloat162_rn(v[16 * k + 2 * j], v[16 * k + 2 * j + 1]);
                 o[j] = *reinterpret_cast<const uint32_t *>(&b);
             }
         }
-        store_sector(to + 32 / sizeof(T) * k, o);
+        tc::store_sector(to + 32 / sizeof(T) * k, o);
     }
 }
 
@@ -361,7 +357,7 @@ template <typename T> struct StoreEpi {
                                                __float_as_uint(x[k + 2]), __float_as_uint(x[k + 3]),
                                                __float_as_uint(x[k + 4]), __float_as_uint(x[k + 5]),
                                                __float_as_uint(x[k + 6]), __float_as_uint(x[k + 7])};
-                        store_sector(sum + k, o);
+                        tc::store_sector(sum + k, o);
                     }
                 } else if (wide && left >= 32) {
                     store32(out + r * N + t.n0 + c, x);
@@ -454,14 +450,16 @@ pair::Plan plan_of(int64_t M, int64_t N, int64_t K, int planes, int step, int mo
     int least = planes == 3 ? 1 : (int)ceil_div(p.k_blocks, kMostSum / 64);
     if (least > most) least = most;
     double best = 0;
-    for (int n = planes == 3 ? pair::Shape<true>::kMaxN : pair::Shape<false>::kMaxN; n >= 128; n -= step) {
+    const int widest = planes == 3 ? pair::Shape<true>::kMaxN : pair::Shape<false>::kMaxN;
+    for (int n = widest; n >= 128; n -= step) {
         const int64_t nt = ceil_div(N, n);
         // a second share of a pair's time is the last that a split can save
         for (int s = least; s <= most && s <= p.k_blocks; ++s) {
             if (s > least && p.m_tiles * nt * (s - 1) >= 2 * pairs) break;
             const int64_t waves = ceil_div(p.m_tiles * nt * s, pairs);
             const double block = pairs_of_planes * 2.0 * n;
-            const double tile = (double)ceil_div(p.k_blocks, s) * (block > 480. ? block : 480.) + 3000.0;
+            const double tile =
+                (double)ceil_div(p.k_blocks, s) * (block > 480. ? block : 480.) + 3000.0;
             // 2000 cycles and s writes and reads of the output at 3 KB a cycle
             const double join = s > 1 ? 2000.0 + (double)M * N * 8.0 * s / 3000.0 : 0.0;
             const double cost = waves * tile + join;
@@ -484,14 +482,15 @@ bool operand(CUtensorMap *map, const void *at, int64_t inner, int64_t rows, int6
 }
 
 template <class Epi, bool A_MN, bool B_MN, bool EXACT>
-cudaError_t multiply(const CUtensorMap &a, const CUtensorMap &b, const pair::Plan &p, const Epi &epi,
-                     cudaStream_t st) {
-    cudaError_t e = allow_dynamic_smem<pair::gemm_kernel<Epi, A_MN, B_MN, EXACT>>(pair::Shape<EXACT>::kSmem);
+cudaError_t multiply(const CUtensorMap &a, const CUtensorMap &b, const pair::Plan &p,
+                     const Epi &epi, cudaStream_t st) {
+    constexpr size_t smem = pair::Shape<EXACT>::kSmem;
+    const cudaError_t e = allow_dynamic_smem<pair::gemm_kernel<Epi, A_MN, B_MN, EXACT>>(smem);
     if (e != cudaSuccess) return e;
     const int64_t items = (int64_t)p.m_tiles * p.n_tiles * p.splits, pairs = pairs_of_sms();
     return launch_kernel(true, pair::gemm_kernel<Epi, A_MN, B_MN, EXACT>,
                          dim3((unsigned)(2 * (items < pairs ? items : pairs))), pair::kThreads,
-                         pair::Shape<EXACT>::kSmem, st, a, b, p, epi);
+                         smem, st, a, b, p, epi);
 }
 
 // Whether a matrix is read where it lies: TMA wants rows on 16-byte boundaries.
@@ -567,8 +566,8 @@ ForwardLayout forward_layout(int32_t dtype, int64_t T, int64_t V, int32_t D) {
     const int P = planes_of(dtype);
     const int64_t t = T > 0 ? T : 1, last = V % l.piece ? V % l.piece : l.piece;
     const int64_t whole = ceil_div(V, plan_of(t, V, D, P, 32, 1).n_tile);
-    const int64_t pieces = (V - last) / l.piece * ceil_div(l.piece, plan_of(t, l.piece, D, P, 32, 1).n_tile) +
-                           ceil_div(last, 128);
+    const int64_t each = ceil_div(l.piece, plan_of(t, l.piece, D, P, 32, 1).n_tile);
+    const int64_t pieces = (V - last) / l.piece * each + ceil_div(last, 128);
     l.tiles = 2 * (whole > pieces ? whole : pieces);
     const int64_t es = planes_of(dtype) * padded(D) * 2;
     l.part = 0;

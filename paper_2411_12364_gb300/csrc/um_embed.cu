@@ -109,7 +109,8 @@ __global__ void __launch_bounds__(256)
 // A radix sort from the lowest digit, 8 bits or less at a time.  A block takes
 // kTile keys in order, a warp 32 x kRounds of them at most: a key's place among the
 // keys of its digit is the number of equal digits before it in its warp (by
-// ballots in a round, and a counter a warp and digit from round to round), in the warps before, and in the blocks before.
+// ballots in a round, and a counter a warp and digit from round to round), in the
+// warps before, and in the blocks before.
 
 constexpr int kSortThreads = 1024;
 constexpr int kRounds = 4;
@@ -167,8 +168,8 @@ __device__ __forceinline__ int digits_before(int v, int *scan) {
 
 // Ranks of the keys among the equal digits before them in their warp, whose
 // counts are left in count[warp]; a warp holds 32 x rounds keys in order.
-__device__ __forceinline__ void rank_keys(const int (&key)[kRounds], int (&rank)[kRounds], int rounds,
-                                          int mine, int n, int shift, int db,
+__device__ __forceinline__ void rank_keys(const int (&key)[kRounds], int (&rank)[kRounds],
+                                          int rounds, int mine, int n, int shift, int db,
                                           int (&count)[kDigits]) {
     const int lane = threadIdx.x & 31;
     const uint32_t mask = (1u << db) - 1u;
@@ -453,7 +454,8 @@ template <typename T, int N> struct Raw {
     __device__ __forceinline__ void get(const T *p) {
         if constexpr (N == 8) {
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T) / 2; ++i) x[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+            for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+                x[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
         } else {
             x[0].x = __float_as_uint(to_f(p[0]));
         }
@@ -754,8 +756,8 @@ template <typename T, typename O, int N>
 cudaError_t sums(const SumArgs &a, const void *ids, int wide, cudaStream_t st) {
     if (!a.key) {
         const int most = 4 * device_sm_count();
-        return launch_kernel(false, short_kernel<T, O, N>, dim3(a.vocab < most ? a.vocab : most), 256, 0,
-                             st, a, ids, wide);
+        return launch_kernel(false, short_kernel<T, O, N>, dim3(a.vocab < most ? a.vocab : most),
+                             256, 0, st, a, ids, wide);
     }
     const int pieces = a.D / N;
     // 256 threads a block: columns, and as many chunks as fit beside them (32 at most)
@@ -915,7 +917,8 @@ extern "C" ultramem_status ultramem_embedding_backward(
                       ld_dout * es % 16 == 0;
     using B = __nv_bfloat16;
     if (dtype == ULTRAMEM_BF16)
-        e = table_dtype == ULTRAMEM_BF16 ? sums_n<B, B>(a, ids, s.wide, wide, st) : sums_n<B, float>(a, ids, s.wide, wide, st);
+        e = table_dtype == ULTRAMEM_BF16 ? sums_n<B, B>(a, ids, s.wide, wide, st)
+                                         : sums_n<B, float>(a, ids, s.wide, wide, st);
     else
         e = table_dtype == ULTRAMEM_BF16 ? sums_n<float, B>(a, ids, s.wide, wide, st)
                                          : sums_n<float, float>(a, ids, s.wide, wide, st);

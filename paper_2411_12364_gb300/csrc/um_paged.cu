@@ -988,11 +988,11 @@ extern "C" ultramem_status ultramem_paged_plan(const int32_t *ctx_lens, const in
     if (n_seqs > 0 && (!ctx_lens || !new_lens || !kv_lens || (table_width > 0 && !block_table)))
         return ULTRAMEM_EINVAL;
     if ((n_tokens > 0 && !slots) || (n_free > 0 && !free_pages)) return ULTRAMEM_EINVAL;
-    if (!um::apart({ints(q_start, (int64_t)n_seqs + 1), ints(kv_lens, n_seqs), ints(slots, n_tokens),
-                ints(free_left, 1), ints(balance, 1),
-                ints(block_table, (int64_t)n_seqs * table_width)},
-               {ints(ctx_lens, n_seqs), ints(new_lens, n_seqs), ints(free_pages, n_free),
-                ints(free_count, 1)}))
+    if (!um::apart({ints(q_start, (int64_t)n_seqs + 1), ints(kv_lens, n_seqs),
+                    ints(slots, n_tokens), ints(free_left, 1), ints(balance, 1),
+                    ints(block_table, (int64_t)n_seqs * table_width)},
+                   {ints(ctx_lens, n_seqs), ints(new_lens, n_seqs), ints(free_pages, n_free),
+                    ints(free_count, 1)}))
         return ULTRAMEM_EINVAL;
     PlanArgs a = {ctx_lens, new_lens,  free_pages, free_count, block_table,
                   q_start,  kv_lens,   slots,      free_left,  balance,
@@ -1091,8 +1091,8 @@ extern "C" ultramem_status ultramem_paged_attention(
     if (!um::same_or_apart(mem_out, mem_q) || um::overlap(mem_lse, mem_q) ||
         um::overlap(mem_ws, mem_q) ||
         !um::apart({mem_out, mem_lse, mem_ws},
-               {ints(q_start, (int64_t)n_seqs + 1), ints(kv_lens, n_seqs),
-                ints(block_table, (int64_t)n_seqs * table_width)}))
+                   {ints(q_start, (int64_t)n_seqs + 1), ints(kv_lens, n_seqs),
+                    ints(block_table, (int64_t)n_seqs * table_width)}))
         return ULTRAMEM_EINVAL;
     const int group = q_heads / c->kv_heads;
     // 4-byte fragments of q and out suffice for the decode kernel; TMA wants

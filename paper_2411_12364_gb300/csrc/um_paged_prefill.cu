@@ -63,12 +63,6 @@ template <int DP> struct Cfg {
     static constexpr size_t kSmem = (size_t)kTile * 2 + (size_t)kStage * kStages + 1024;
 };
 
-// 32 bytes, a whole sector, by one thread (dst 32-byte aligned)
-__device__ __forceinline__ void store32(void *dst, const uint32_t *r) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(r[0]),
-                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-                 : "memory");
-}
 // What each role needs of the tile at hand: blocks [j0, e[i]) of half i.
 struct Halves {
     int n_tok[2], e[2], end;
@@ -276,7 +270,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (wk.part != kPartNone) {
                     float *dst = a.part_o + rec * DP + 32 * c;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) store32(dst + 8 * k, &o[8 * k]);
+                    for (int k = 0; k < 4; ++k) tc::store_sector(dst + 8 * k, &o[8 * k]);
                     continue;
                 }
                 __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + head * a.D + 32 * c;
@@ -291,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (wide) {
 #pragma unroll
                     for (int k = 0; k < 2; ++k)
-                        if (32 * c + 16 * k < a.D) store32(dst + 16 * k, &q[8 * k]);
+                        if (32 * c + 16 * k < a.D) tc::store_sector(dst + 16 * k, &q[8 * k]);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
@@ -322,7 +316,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool leader = tc::elect_one();
         const uint64_t q_desc = tc::desc_k_sw128(tc::smem_u32(qs + i * C::kTile));
         const uint64_t k_desc = tc::desc_k_sw128(tc::smem_u32(ring));
-        const uint64_t v_desc = tc::desc_mn_sw128(tc::smem_u32(ring + (C::kPaired ? C::kTile : 0)), kHalfBytes);
+        const uint64_t v_desc =
+            tc::desc_mn_sw128(tc::smem_u32(ring + (C::kPaired ? C::kTile : 0)), kHalfBytes);
         const uint32_t t_s = tc::uniform(tmem) + 128 * i, t_o = tc::uniform(tmem) + 256 + DP * i;
         int stage = 0;
         uint32_t phase = 0, tiles = 0, p_phase = 0, turns = 0;
@@ -351,7 +346,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (leader) {
 #pragma unroll
                 for (int k = 0; k < kKeys / 16; ++k)
-                    tc::mma_bf16_ts(t_o, t_s + 8 * k, vd + k * (16 * 128 >> 4), idesc_o, add || k > 0);
+                    tc::mma_bf16_ts(t_o, t_s + 8 * k, vd + k * (16 * 128 >> 4), idesc_o,
+                                    add || k > 0);
             }
         };
         while (ok && wk.next(a, kKeys)) {

@@ -32,8 +32,9 @@
 //
 // Warps of a CTA: 0 copies (TMA, one elected thread), 1 products (one thread
 // of the pair's first CTA), 2-9 epilogue (four for each half of the columns: with
-// four in all, tiles of up to 16 k blocks took as long as their epilogue).  Waits are bounded; one that gives
-// up sets the error word, and the others run into their own limits.
+// four in all, tiles of up to 16 k blocks took as long as their epilogue).  Waits are
+// bounded; one that gives up sets the error word, and the others run into their own
+// limits.
 #pragma once
 
 #include "um_internal.cuh"

@@ -222,7 +222,7 @@ __device__ __forceinline__ uint64_t desc_mn_sw128(uint32_t saddr, uint32_t group
     d |= (uint64_t)2 << 61;
     return d;
 }
-constexpr uint32_t kAColumns = 1u << 15, kBColumns = 1u << 16;   // instruction descriptor: such an A, B
+constexpr uint32_t kAColumns = 1u << 15, kBColumns = 1u << 16;   // instruction descriptor
 
 // Instruction descriptor of kind::f16 with bf16 A and B, fp32 D, both K-major.
 __host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N) {
@@ -260,6 +260,15 @@ __device__ __forceinline__ void mma_commit(uint64_t *bar) {
         "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
             smem_u32(bar))
         : "memory");
+}
+
+// ---- global memory ----
+
+// 32 bytes, a whole sector, by one thread (dst 32-byte aligned)
+__device__ __forceinline__ void store_sector(void *dst, const uint32_t *r) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "r"(r[0]),
+                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
 
 // ---- a warp that acts as one ----
