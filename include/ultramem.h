@@ -571,8 +571,8 @@ ultramem_status ultramem_embedding(const void *table, int64_t ld_table, int32_t 
 /* The gradient of the table: dtable[v] = scale sum of dout[t] over the tokens
  * with ids[t] = v (0 without one; ids outside [0, vocab) count nowhere), or
  * with `accumulate` that sum added to what dtable holds (rows without a token
- * are left alone).  The sums are fp32, each in a fixed order, and rounded
- * once.  dout [n_tokens][dim] of `dtype`; dtable [vocab][dim] contiguous, of
+ * are left alone).  The sums are fp32, each in an order that the sizes and the
+ * tensors' alignment fix, and rounded once.  dout [n_tokens][dim] of `dtype`; dtable [vocab][dim] contiguous, of
  * `table_dtype`.  dtable and the workspace (16-byte aligned) overlap nothing
  * (ULTRAMEM_EINVAL). */
 ultramem_status ultramem_embedding_backward(const void *ids, int32_t ids_bytes, int32_t n_tokens,

@@ -207,7 +207,9 @@ def paged_attention_backward(q, k, v, out, lse, dout, q_start, scale=None, dq=No
     that ``paged_attention`` gave for them, for the gradient dout of out.
     scale as there.  Tokens of all but lse may be strided apart, as slices of
     one projection's output; dq, dk and dv may be given, slices of one
-    gradient among them.  Rows that belong to no sequence are not written."""
+    gradient among them.  Rows that belong to no sequence are not written.
+    Tensors of bf16 that start or step off 16 bytes, and heads wider than 128,
+    take the CUDA cores, many times slower where sequences are long."""
     dev = _b._on_device("q", q)
     if q.dim() != 3 or k.dim() != 3 or q.dtype not in _DTYPES:
         raise ValueError("q, k and v must be [tokens, heads, head_dim], fp32 or bf16")

@@ -110,7 +110,8 @@ def embedding_backward(ids, dout, vocab: int, scale: float = 1.0, dtable=None,
     """The gradient of the table: dtable [vocab, D] with row v = scale times the
     sum of dout [T, D] over the tokens with ids[t] = v, in dout's type unless
     ``dtable`` (fp32 or bf16) is given.  With ``accumulate`` the sums are added
-    to what the given dtable holds.  The sums have a fixed order."""
+    to what the given dtable holds.  The sums have an order that the sizes and
+    the tensors' alignment fix."""
     dev = _b._on_device("dout", dout)
     dout, T, D, ld = _matrix("dout", dout, dev)
     _b._fits_int32(vocab)
@@ -154,8 +155,8 @@ def _ce_args(x, w, labels, logit_scale):
 def cross_entropy(x, w, labels, logit_scale: float = 1.0):
     """(loss, lse), fp32 [T], of hidden states x [T, D] against the output
     weights w [V, D]: z = logit_scale * x w^T, lse = log sum e^z, loss = lse -
-    z[label].  A label outside [0, V) marks a token that does not count (loss
-    0).  The logits are not kept."""
+    z[label], at least 0.  A label outside [0, V) marks a token that does not
+    count (loss 0).  The logits are not kept."""
     a, x, w, dev, sizes = _ce_args(x, w, labels, logit_scale)
     device = x.device
     loss = torch.empty(sizes[1], dtype=torch.float32, device=device)
