@@ -627,7 +627,8 @@ int64_t ultramem_cross_entropy_workspace(int32_t dtype, int32_t n_tokens, int32_
  * dw [vocab][dim], contiguous, of `dtype`; each NULL to skip.  They and the
  * workspace overlap nothing.  The workspace is one for both, with the room for
  * copies as above, for a piece of G (512 MB at most, or 256 rows of the vocabulary)
- * and for partial sums (512 MB at most each for dx and dw, or one dx in fp32). */
+ * and for partial sums (512 MB at most each for dx and dw, 2 GB for a dw of rows
+ * of more than 16384 entries, or one dx in fp32). */
 ultramem_status ultramem_cross_entropy_backward(const ultramem_cross_entropy_args *args,
                                                 const float *lse, const float *dloss, void *dx,
                                                 void *dw, void *workspace, int64_t workspace_bytes,

@@ -448,7 +448,8 @@ pair::Plan plan_of(int64_t M, int64_t N, int64_t K, int planes, int step, int mo
     p.k_blocks = (int)ceil_div(K, 64);
     const int pairs_of_planes = planes == 3 ? 6 : 1;
     int least = planes == 3 ? 1 : (int)ceil_div(p.k_blocks, kMostSum / 64);
-    if (least > most) least = most;
+    if (least > 64) least = 64;
+    if (most < least) most = least;
     double best = 0;
     const int widest = planes == 3 ? pair::Shape<true>::kMaxN : pair::Shape<false>::kMaxN;
     for (int n = widest; n >= 128; n -= step) {
@@ -593,7 +594,7 @@ BackwardLayout backward_layout(int32_t dtype, int64_t T, int64_t V, int32_t D) {
     const int64_t rows = rows_in_planes(dtype, D);
     l.piece = piece_of(V, limit < rows ? limit : rows);
     l.ld = (l.piece + 31) & ~31ll;
-    // partial sums stay below a piece's bytes
+    // partial sums stay below a piece's bytes, but for as many as long sums need
     auto most = [bytes](int64_t m, int64_t n) {
         const int64_t s = bytes / (m * n * 4);
         return (int)(s < 1 ? 1 : s > 64 ? 64 : s);

@@ -13,6 +13,7 @@ from tests.test_training_fake_cpu import CALLS
     (2560, 104000, 1280, 1),
     (140000, 1280, 2560, 1),      # sums over the tokens, 5 x 10 tiles of dw
     (60000, 1280, 2560, 0),
+    (100000, 1280, 65536, 1),     # a dw whose partial sums are larger than a piece
 ])
 def test_long_sums_are_split(fake_library, T, V, D, joins):
     run(fake_library, CALLS + f"""
