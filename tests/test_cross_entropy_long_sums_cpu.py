@@ -17,6 +17,7 @@ from tests.test_training_fake_cpu import CALLS
 ])
 def test_long_sums_are_split(fake_library, T, V, D, joins):
     run(fake_library, CALLS + f"""
+M = 1 << 40                       # further apart than the largest of the tensors
 assert ce_grad(T={T}, V={V}, D={D}) == b.OK
 assert sum("sum_splits_kernel" in line for line in log()) == {joins}, log()
 print("done")
