@@ -616,10 +616,12 @@ __global__ void __launch_bounds__(persistent_threads<Op>(), 1)
         const int quad = warp & 3, grp = (warp - 2) >> 2;
         const int row = quad * 32 + lane;
         int lt = 0;
-        for (int i = blockIdx.x; i < tiles && !abort_flag; i += gridDim.x, ++lt) {
+        for (int i = blockIdx.x; i < tiles; i += gridDim.x, ++lt) {
+            // a warp goes on or gives up as one: its lanes meet again below
+            if (__any_sync(0xffffffffu, abort_flag)) break;
             const Tile t = tile_of(i);
             const int buf = lt & 1;
-            if (!mbar_wait(&tfull[buf], (lt >> 1) & 1)) {
+            if (!warp_wait(&tfull[buf], (lt >> 1) & 1)) {
                 if (lane == 0) fail();
                 break;
             }
